@@ -248,7 +248,7 @@ def prepare(case, seed):
         st["layout"] = G.KVLayout(H, D, B, fmt, K_SCALE, V_SCALE) if case["packed"] else G.KVLayout(H, D, B, fmt)
         st["cache"] = G.PagedKV(1, nb, st["layout"].chunk_bytes, tensors=[st["data"]])
         st["max_new"] = max(new)
-        st["workspace"] = G.attend_workspace(st["layout"], case["heads"], sum(new), R, st["max_new"])
+        st["workspace"] = G.attend_workspace(st["layout"])
         st["out"] = torch.empty_like(st["q"])
     return st
 
