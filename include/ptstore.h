@@ -428,6 +428,114 @@ int ptstore_fetch_static(const void* hbm_pool, uint32_t hbm_blocks, uint32_t num
                          const ptstore_paged_cache_t* dst /*host struct*/, const int32_t* block_tables,
                          uint32_t* status_out, ptstore_stream_t stream);
 
+/* ---- operators around the paged cache ------------------------------------------------------------------------------
+ * What a model's step needs next to the store: the block tables and slots of its requests, its new K/V in the cache, and the attention
+ * of its new tokens over the cache (a fetched prefix and the new tokens alike).  They need no handle, allocate nothing, keep nothing
+ * between calls, only enqueue, and may be captured into a graph.  Each call works on ONE layer of the cache, on the current device.
+ * `status` is a device uint32 or NULL: PTSTORE_S_* bits are OR-ed into it (never cleared here).
+ */
+
+/* Formats of a cache chunk (the K or the V of one block in one layer).  Head sizes 64 and 128.
+ *   BF16, FP16: [block_tokens][num_kv_heads][head_dim], any block_tokens >= 1.
+ *   PACKED: 4 bits per element and an e4m3 scale per 16 elements of a token and head, [num_kv_heads][block_tokens / 16] tiles of
+ *     9 * head_dim bytes; block_tokens a multiple of 16.  value = (code - 8) * scale * tensor scale (k_scale, v_scale: powers of two in
+ *     2^-64 .. 2^64); every value is exact in bf16, and in fp16 within its range.  A tile: 16 rows of head_dim / 2 bytes of codes, element i in nibble i & 7 of
+ *     the row's 32-bit word i >> 3, 16-byte chunk c of row n at 16 * (n / rho * 8 + ((n % rho * head_dim / 32 + c) ^ 2 * (n / 4))),
+ *     rho = 256 / head_dim; then the scales, K [16 tokens][head_dim / 16], V [head_dim / 16][16 tokens].
+ * A chunk of any format is opaque bytes to the store: create it with num_kv_heads, head_dim and elem_bytes whose product with block_tokens
+ * is the chunk (PACKED: elem_bytes 1, head_dim * 9 / 16 bytes per token and head). */
+#define PTSTORE_KV_BF16    0u
+#define PTSTORE_KV_FP16    1u
+#define PTSTORE_KV_PACKED  2u
+
+typedef struct ptstore_kv_cache {
+  void*    base;                 /* K of cache block 0 in this layer (device, 16-byte aligned) */
+  uint64_t kv_stride_bytes;      /* K -> V, multiple of 16 */
+  uint64_t block_stride_bytes;   /* multiple of 16, >= the chunk */
+  uint32_t num_blocks, block_tokens, num_kv_heads, head_dim;
+  uint32_t format, reserved;
+  float    k_scale, v_scale;     /* PACKED only */
+} ptstore_kv_cache_t;
+
+/* Bytes of a chunk, 0 if the format does not support the sizes (host only). */
+uint64_t ptstore_kv_chunk_bytes(uint32_t format, uint32_t block_tokens, uint32_t num_kv_heads, uint32_t head_dim);
+
+/*
+ * Grows and shrinks block-table rows to ceil(lengths[r] / block_tokens) entries, from and to a stack of free blocks.
+ *   held          [R] entries that are set in row r, or NULL for none (a new batch)
+ *   free_ids      [free_capacity] the stack, free_count (device) entries of it in use, top = last
+ * First the surplus blocks of shrinking rows are pushed, in (request, block) order (their table entries stay as they are); then growing rows
+ * pop, in (request, block) order, each pop taking the top.  A row grows only if the growth of all requests up to and including it
+ * fits in the stack; otherwise it stays as it is (S_NOSPACE).  A length whose blocks exceed max_blocks leaves its row as it is (S_BOUNDS);
+ * a negative length counts as 0, and held and free_count are clamped to their ranges (S_BOUNDS).  Pushes beyond free_capacity are lost
+ * (S_BOUNDS).  held_out / free_count_out may be held / free_count themselves; no other arrays may overlap.
+ */
+int ptstore_assign_blocks(const int32_t* lengths, const int32_t* held, int32_t R, int32_t block_tokens, int32_t* block_tables /*[R][max_blocks]*/,
+                          int32_t max_blocks, int32_t* free_ids, int32_t free_capacity, const int32_t* free_count,
+                          int32_t* held_out /*[R]*/, int32_t* free_count_out /*[1]*/, uint32_t* status, ptstore_stream_t stream);
+
+/*
+ * Lists the new tokens of a batch: request r has lengths[r] tokens, of which min(done[r] * done_unit, lengths[r] - min_new) (at least 0)
+ * are in the cache already (done NULL: none; with done = the matched lengths of a lookup, done_unit = block_tokens and min_new = 1, a
+ * prompt that was found whole still computes its last token).
+ *   token_offsets [R + 1] exclusive prefix sums of the new tokens (at most 2^31 - 1)
+ *   slots         [max_tokens] token i of request r: block_tables[r][pos / block_tokens] * block_tokens + pos % block_tokens; -1 where the
+ *                 table entry is negative or pos is beyond the row (S_BOUNDS), and for entries behind the last token
+ *   positions     [max_tokens] or NULL: pos; -1 behind the last token
+ * New tokens beyond max_tokens are not listed (S_BOUNDS).  Outputs may not overlap inputs.
+ */
+int ptstore_map_slots(const int32_t* lengths, const int32_t* done, int32_t done_unit, int32_t min_new, int32_t R,
+                      const int32_t* block_tables, int32_t max_blocks, int32_t block_tokens, int64_t max_tokens,
+                      int32_t* token_offsets, int64_t* slots, int32_t* positions, uint32_t* status, ptstore_stream_t stream);
+
+/*
+ * Rows of K and V into the cache / out of it.  Row i of a head: head_dim contiguous 16-bit elements (dtype PTSTORE_KV_BF16 or _FP16) at
+ * i * token_stride + head * head_stride elements (multiples of 8; pointers 16-byte aligned); it belongs to cache slot slots[i] =
+ * block * block_tokens + token.  A slot of -1 is skipped (its row is neither written nor read); any other slot outside the cache too (S_BOUNDS).  Slots
+ * of a write other than -1 must be distinct.  A 16-bit cache takes rows of its own type only.
+ * PACKED, per 16 elements: scale = e4m3 nearest to max|x| / (7 t), at most 448 (t: the tensor scale); code = x / (scale t) to the nearest
+ * integer, ties to even, within -8 .. 7, plus 8.  All zero where the scale is zero.  Infinities saturate; a NaN makes its 16 elements NaN.
+ */
+int ptstore_kv_write(const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
+                     int64_t v_head_stride, int64_t tokens, uint32_t dtype, const int64_t* slots, const ptstore_kv_cache_t* cache /*host struct*/,
+                     uint32_t* status, ptstore_stream_t stream);
+int ptstore_kv_read(const ptstore_kv_cache_t* cache /*host struct*/, const int64_t* slots, int64_t tokens, uint32_t dtype, void* k,
+                    int64_t k_token_stride, int64_t k_head_stride, void* v, int64_t v_token_stride, int64_t v_head_stride,
+                    uint32_t* status, ptstore_stream_t stream);
+
+/*
+ * Causal attention of a batch's new tokens over the paged cache, which holds their own K/V too (ptstore_kv_write comes first):
+ *   out[i, hq] = sum_j softmax_j(scale * q[i, hq] . k[j, hq / group]) * v[j, hq / group],  group = num_heads / num_kv_heads,
+ * over the tokens j of the row's request with j <= pos, pos = lengths[r] - (rows of r) + (i - token_offsets[r]).
+ * A row that sees nothing (pos < 0, or no valid block) is zero; rows that belong to no request are left as they were.  Tokens whose table
+ * entry is outside the cache, or beyond the row of the table, are not seen (S_BOUNDS for the former).  What the cache holds
+ * behind a row's position has no influence, infinities and NaN included.
+ * Products take 16-bit operands (the cache's type; fp16 for PACKED) and add in 32 bits; maxima, sums and outputs up to the last rounding
+ * are 32 bits wide; probabilities are rounded to 16 bits before they meet V.
+ * The result of a call does not depend on timing: equal inputs give equal bits.
+ */
+typedef struct ptstore_attend {
+  uint32_t struct_size;          /* sizeof(ptstore_attend_t) */
+  uint32_t dtype;                /* of q and out: PTSTORE_KV_BF16 or PTSTORE_KV_FP16; a 16-bit cache has the same */
+  const void* q;                 /* [tokens][num_heads][head_dim], strides in elements (multiples of 8), 16-byte aligned */
+  int64_t  q_token_stride, q_head_stride;
+  void*    out;                  /* likewise; may be q itself */
+  int64_t  out_token_stride, out_head_stride;
+  const int32_t* token_offsets;  /* [requests + 1] rows of every request */
+  const int32_t* lengths;        /* [requests] tokens in the cache, the new ones among them */
+  const int32_t* block_tables;   /* [requests][max_blocks] */
+  int32_t  requests, max_blocks, num_heads;
+  int32_t  tokens;               /* rows of q and out */
+  int32_t  max_new;              /* at least the rows of any request: chooses the kernel (host) */
+  float    scale;                /* of the scores, usually 1 / sqrt(head_dim) */
+} ptstore_attend_t;
+
+/* Bytes of workspace (256-byte aligned device memory, ZERO before its first use).  A call leaves it ready for the next one, whatever that
+ * one's sizes; calls that share a workspace must not overlap. */
+uint64_t ptstore_attend_workspace_bytes(uint32_t head_dim);
+int ptstore_attend(const ptstore_attend_t* args /*host struct*/, const ptstore_kv_cache_t* cache /*host struct*/, void* workspace,
+                   uint64_t workspace_bytes, uint32_t* status, ptstore_stream_t stream);
+
 /* Static text for a PTSTORE_E_* code. */
 const char* ptstore_strerror(int code);
 

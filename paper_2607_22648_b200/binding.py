@@ -56,11 +56,28 @@ class Stats(C.Structure):
                 ("blocks_demoted", C.c_uint64), ("far_keys", C.c_uint64), ("blocks_promoted", C.c_uint64), ("gdsf_clock", C.c_uint64), ("blocks_fetched_distinct", C.c_uint64)]
 
 
+KV_BF16, KV_FP16, KV_PACKED = 0, 1, 2
+
+
+class KvCache(C.Structure):
+    _fields_ = [("base", C.c_void_p), ("kv_stride_bytes", C.c_uint64), ("block_stride_bytes", C.c_uint64),
+                ("num_blocks", C.c_uint32), ("block_tokens", C.c_uint32), ("num_kv_heads", C.c_uint32), ("head_dim", C.c_uint32),
+                ("format", C.c_uint32), ("reserved", C.c_uint32), ("k_scale", C.c_float), ("v_scale", C.c_float)]
+
+
+class Attend(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_uint32), ("q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("out", C.c_void_p), ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64), ("token_offsets", C.c_void_p),
+                ("lengths", C.c_void_p), ("block_tables", C.c_void_p), ("requests", C.c_int32), ("max_blocks", C.c_int32), ("num_heads", C.c_int32),
+                ("tokens", C.c_int32), ("max_new", C.c_int32), ("scale", C.c_float)]
+
+
 EXPORTS = ["ptstore_workspace_bytes", "ptstore_create", "ptstore_destroy", "ptstore_hash", "ptstore_lookup",
            "ptstore_fetch", "ptstore_insert", "ptstore_release", "ptstore_evict", "ptstore_status", "ptstore_stats",
            "ptstore_launch_count", "ptstore_last_cuda_error", "ptstore_strerror", "ptstore_fetch_static", "ptstore_promote", "ptstore_evict_async", "ptstore_join", "ptstore_stats_enqueue", "ptstore_lookup_fetch",
            "ptstore_reserve", "ptstore_set_wait_limit", "ptstore_time_next_copy", "ptstore_copy_probe",
-           "ptstore_insert_after_lookup", "ptstore_resumed_inserts"]
+           "ptstore_insert_after_lookup", "ptstore_resumed_inserts", "ptstore_kv_chunk_bytes", "ptstore_assign_blocks", "ptstore_map_slots",
+           "ptstore_kv_write", "ptstore_kv_read", "ptstore_attend_workspace_bytes", "ptstore_attend"]
 
 
 def _load():
@@ -97,6 +114,16 @@ def _load():
     lib.ptstore_launch_count.argtypes = [vp]
     lib.ptstore_last_cuda_error.argtypes = [vp]
     lib.ptstore_fetch_static.argtypes = [vp, u32, u32, u64, vp, vp, i32, i32, C.POINTER(PagedCache), vp, vp, vp]
+    i64 = C.c_int64
+    lib.ptstore_kv_chunk_bytes.restype = u64
+    lib.ptstore_kv_chunk_bytes.argtypes = [u32, u32, u32, u32]
+    lib.ptstore_assign_blocks.argtypes = [vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp]
+    lib.ptstore_map_slots.argtypes = [vp, vp, i32, i32, i32, vp, i32, i32, i64, vp, vp, vp, vp, vp]
+    lib.ptstore_kv_write.argtypes = [vp, i64, i64, vp, i64, i64, i64, u32, vp, C.POINTER(KvCache), vp, vp]
+    lib.ptstore_kv_read.argtypes = [C.POINTER(KvCache), vp, i64, u32, vp, i64, i64, vp, i64, i64, vp, vp]
+    lib.ptstore_attend_workspace_bytes.restype = u64
+    lib.ptstore_attend_workspace_bytes.argtypes = [u32]
+    lib.ptstore_attend.argtypes = [C.POINTER(Attend), C.POINTER(KvCache), vp, u64, vp, vp]
     lib.ptstore_strerror.restype = C.c_char_p
     lib.ptstore_strerror.argtypes = [C.c_int]
     return lib
@@ -160,6 +187,192 @@ def fetch_static(hbm_pool, hbm_blocks, layers, chunk_bytes, ids, matched, cache,
                                   C.byref(cache.desc), _ptr(block_tables), _ptr(status_out), _stream())
     if rc:
         raise PTStoreError(rc, "ptstore_fetch_static")
+
+
+# ---- operators around the paged cache: no store handle, work on the stream and device that are current -------------------------------
+_KV_DTYPES = {torch.bfloat16: KV_BF16, torch.float16: KV_FP16}
+
+
+def _check(rc, what):
+    if rc:
+        raise PTStoreError(rc, what)
+
+
+def _want(t, dtype, shape, what):
+    """An array argument of the operators: a contiguous tensor of this type on the current device (or pinned); shape None matches any size."""
+    ok = t is not None and t.dtype == dtype and t.dim() == len(shape) and all(n is None or n == m for n, m in zip(shape, t.shape))
+    if not ok or not t.is_contiguous():
+        raise ValueError("%s: needs a contiguous %s tensor of shape %s" % (what, dtype, [n if n is not None else "any" for n in shape]))
+    _here(t, what)
+
+
+def _here(t, what):
+    if t.is_cuda:
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError("%s: is on another device than the current one" % what)
+    elif not t.is_pinned():
+        raise ValueError("%s: needs device or pinned memory" % what)
+
+
+def _rows(t, layout, heads, what, tokens=None):
+    """[tokens][heads][dim] rows of 16-bit elements, any token and head strides."""
+    if t is None or t.dim() != 3 or t.dtype not in _KV_DTYPES or tuple(t.shape[1:]) != (heads, layout.dim) or t.stride(2) != 1:
+        raise ValueError("%s: needs a bfloat16 or float16 tensor [tokens, %d, %d], contiguous along the last axis" % (what, heads, layout.dim))
+    if tokens is not None and t.shape[0] != tokens:
+        raise ValueError("%s: needs %d rows" % (what, tokens))
+    _here(t, what)
+
+
+def _status_word(status):
+    if status is not None:
+        _want(status, torch.int32, [1], "status")
+
+
+class KVLayout:
+    """How a layer's K and V lie in the chunks of a PagedKV: kv heads, head size, tokens per block and format.  k_scale / v_scale are the
+    tensor scales of KV_PACKED (powers of two)."""
+
+    def __init__(self, heads, dim, block_tokens, format=KV_BF16, k_scale=1.0, v_scale=1.0):
+        self.heads, self.dim, self.block_tokens, self.format = heads, dim, block_tokens, format
+        self.k_scale, self.v_scale = k_scale, v_scale
+        self.chunk_bytes = int(lib.ptstore_kv_chunk_bytes(format, block_tokens, heads, dim))
+        if self.chunk_bytes == 0:
+            raise PTStoreError(E_INVAL, "ptstore_kv_chunk_bytes")
+
+    def store_args(self):
+        """dim and elem_bytes for a PTStore that holds chunks of this layout (the store moves opaque bytes)."""
+        return {"dim": self.dim * 9 // 16, "elem_bytes": 1} if self.format == KV_PACKED else {"dim": self.dim, "elem_bytes": 2}
+
+    def of(self, cache, layer):
+        """The C descriptor of one layer of a PagedKV."""
+        if not 0 <= layer < len(cache.tensors):
+            raise ValueError("layer %d of a cache of %d layers" % (layer, len(cache.tensors)))
+        t = cache.tensors[layer]
+        _here(t, "cache")
+        size = t.element_size()
+        if t.dim() < 2 or t.shape[0] != 2 or (t.numel() and t[0, 0].numel() * size != self.chunk_bytes) or not t[0, 0].is_contiguous():
+            raise ValueError("cache: needs [2, blocks, chunk] with contiguous chunks of %d bytes" % self.chunk_bytes)
+        return KvCache(t.data_ptr(), t.stride(0) * size, t.stride(1) * size, t.shape[1], self.block_tokens, self.heads, self.dim, self.format, 0,
+                       self.k_scale, self.v_scale)
+
+
+def assign_blocks(lengths, held, block_tables, free_ids, free_count, block_tokens, held_out=None, free_count_out=None, status=None):
+    """ptstore_assign_blocks: grows and shrinks block-table rows to the lengths, from and to the stack free_ids[:free_count].  held (None:
+    nothing held yet) and free_count are updated in place unless held_out / free_count_out are given.  Returns (held, free_count)."""
+    R = lengths.numel()
+    _want(lengths, torch.int32, [R], "lengths")
+    _want(block_tables, torch.int32, [R, None], "block_tables")
+    _want(free_ids, torch.int32, [None], "free_ids")
+    _want(free_count, torch.int32, [1], "free_count")
+    if held is not None:
+        _want(held, torch.int32, [R], "held")
+    if held_out is None:
+        held_out = held if held is not None else torch.empty_like(lengths)
+    if free_count_out is None:
+        free_count_out = free_count
+    _want(held_out, torch.int32, [R], "held_out")
+    _want(free_count_out, torch.int32, [1], "free_count_out")
+    _status_word(status)
+    _check(lib.ptstore_assign_blocks(_ptr(lengths), _ptr(held), R, block_tokens, _ptr(block_tables), block_tables.shape[1], _ptr(free_ids),
+                                     free_ids.numel(), _ptr(free_count), _ptr(held_out), _ptr(free_count_out), _ptr(status), _stream()),
+           "ptstore_assign_blocks")
+    return held_out, free_count_out
+
+
+def map_slots(lengths, done, block_tables, block_tokens, max_tokens, done_unit=1, min_new=0, token_offsets=None, slots=None, positions=None,
+              status=None):
+    """ptstore_map_slots: the new tokens of a batch.  done (tokens, times done_unit; None: none) are in the cache already; after a lookup
+    pass its matched lengths with done_unit=block_tokens, min_new=1.  Returns (token_offsets [R+1], slots int64 [max_tokens], positions)."""
+    R = lengths.numel()
+    _want(lengths, torch.int32, [R], "lengths")
+    if done is not None:
+        _want(done, torch.int32, [R], "done")
+    _want(block_tables, torch.int32, [R, None], "block_tables")
+    dev = lengths.device if lengths.is_cuda else torch.device("cuda", torch.cuda.current_device())
+    if token_offsets is None:
+        token_offsets = torch.empty(R + 1, dtype=torch.int32, device=dev)
+    if slots is None:
+        slots = torch.empty(max_tokens, dtype=torch.int64, device=dev)
+    if positions is None:
+        positions = torch.empty(max_tokens, dtype=torch.int32, device=dev)
+    _want(token_offsets, torch.int32, [R + 1], "token_offsets")
+    _want(slots, torch.int64, [max_tokens], "slots")
+    _want(positions, torch.int32, [max_tokens], "positions")
+    _status_word(status)
+    _check(lib.ptstore_map_slots(_ptr(lengths), _ptr(done), done_unit, min_new, R, _ptr(block_tables), block_tables.shape[1], block_tokens,
+                                 max_tokens, _ptr(token_offsets), _ptr(slots), _ptr(positions), _ptr(status), _stream()), "ptstore_map_slots")
+    return token_offsets, slots, positions
+
+
+def kv_write(layout, cache, layer, k, v, slots, status=None):
+    """ptstore_kv_write: rows k, v [tokens, heads, dim] into one layer of the paged cache at `slots` (int64; -1 skips a row)."""
+    desc = layout.of(cache, layer)
+    _want(slots, torch.int64, [None], "slots")
+    n = slots.numel()
+    _rows(k, layout, layout.heads, "k", n)
+    _rows(v, layout, layout.heads, "v", n)
+    if v.dtype != k.dtype:
+        raise ValueError("k and v: need one type")
+    _status_word(status)
+    _check(lib.ptstore_kv_write(_ptr(k), k.stride(0), k.stride(1), _ptr(v), v.stride(0), v.stride(1), n, _KV_DTYPES[k.dtype], _ptr(slots),
+                                C.byref(desc), _ptr(status), _stream()), "ptstore_kv_write")
+
+
+def kv_read(layout, cache, layer, slots, dtype, k=None, v=None, status=None):
+    """ptstore_kv_read: the values at `slots` as rows [tokens, heads, dim]; rows whose slot is -1 are left as they were.  Returns (k, v)."""
+    desc = layout.of(cache, layer)
+    _want(slots, torch.int64, [None], "slots")
+    n = slots.numel()
+    if k is None:
+        k = torch.empty((n, layout.heads, layout.dim), dtype=dtype, device=cache.tensors[layer].device)
+    if v is None:
+        v = torch.empty_like(k)
+    _rows(k, layout, layout.heads, "k", n)
+    _rows(v, layout, layout.heads, "v", n)
+    if k.dtype != dtype or v.dtype != dtype:
+        raise ValueError("k and v: need the type asked for")
+    _status_word(status)
+    _check(lib.ptstore_kv_read(C.byref(desc), _ptr(slots), n, _KV_DTYPES[dtype], _ptr(k), k.stride(0), k.stride(1), _ptr(v), v.stride(0), v.stride(1),
+                               _ptr(status), _stream()), "ptstore_kv_read")
+    return k, v
+
+
+def attend_workspace(layout):
+    """A workspace for attend on the current device.  Calls that share one must not overlap; they may differ in every size."""
+    n = int(lib.ptstore_attend_workspace_bytes(layout.dim))
+    raw = torch.zeros(n + 256, dtype=torch.uint8, device="cuda")
+    at = -raw.data_ptr() % 256
+    return raw[at:at + n]
+
+
+def attend(layout, cache, layer, q, token_offsets, lengths, block_tables, max_new, scale=None, out=None, workspace=None, status=None):
+    """ptstore_attend: causal attention of the new tokens q [tokens, num_heads, dim] over the paged cache (which holds their own K/V
+    already).  Request r owns rows token_offsets[r] .. token_offsets[r+1]-1 and lengths[r] tokens of cache; max_new (host) is at least the
+    rows of any request.  workspace: from attend_workspace (a program that calls often keeps one per stream).  Returns out."""
+    desc = layout.of(cache, layer)
+    if q is None or q.dim() != 3:
+        raise ValueError("q: needs [tokens, num_heads, dim]")
+    T, heads = q.shape[0], q.shape[1]
+    _rows(q, layout, heads, "q")
+    R = lengths.numel()
+    _want(lengths, torch.int32, [R], "lengths")
+    _want(token_offsets, torch.int32, [R + 1], "token_offsets")
+    _want(block_tables, torch.int32, [R, None], "block_tables")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _rows(out, layout, heads, "out", T)
+    if out.dtype != q.dtype:
+        raise ValueError("out: needs the type of q")
+    if workspace is None:
+        workspace = attend_workspace(layout)
+    _here(workspace, "workspace")
+    _status_word(status)
+    args = Attend(C.sizeof(Attend), _KV_DTYPES[q.dtype], q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1),
+                  token_offsets.data_ptr(), lengths.data_ptr(), block_tables.data_ptr(), R, block_tables.shape[1], heads, T, max_new,
+                  layout.dim ** -0.5 if scale is None else scale)
+    _check(lib.ptstore_attend(C.byref(args), C.byref(desc), _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(status), _stream()),
+           "ptstore_attend")
+    return out
 
 
 class PTStore:

@@ -6,9 +6,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libptstore.so")
-SOURCES = ["ptstore.cu", "fetch_static.cu", "copy_probe.cu"]
+SOURCES = ["ptstore.cu", "fetch_static.cu", "copy_probe.cu", "plan.cu", "kvcache.cu", "attend.cu"]
 NVCC_FLAGS = ["-std=c++17", "-O3", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a", "-Xcompiler", "-fPIC",
-              "-shared", "-cudart", "shared"]
+              "-shared", "-cudart", "shared", "--threads", "0"]
 
 
 def _source_hash():

@@ -1,0 +1,91 @@
+// ptstore_attend: host side and dispatch of the attention over the paged cache.
+#include "attend_split.cuh"
+
+using namespace ptk;
+
+namespace {
+
+constexpr int MAX_SMS = 160;                 // the workspace does not depend on the device: a B200 has 148 SMs
+
+// rows of an item: 8 where a request's rows of one kv head fit, else 16
+inline int n_tiles_of(i64 rows) { return rows <= 8 ? 1 : 2; }
+
+constexpr u64 counters_bytes(int ctas) { return ((u64)ctas * 4 + 255) / 256 * 256; }
+
+int sm_count(int* sms) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || *sms <= 0) {
+    (void)cudaGetLastError();
+    return PTSTORE_E_CUDA;
+  }
+  if (*sms > MAX_SMS) *sms = MAX_SMS;
+  return PTSTORE_OK;
+}
+
+template <int FMT, bool QFP16, int D, int NT>
+int launch_split(const Attend& a, int sms, cudaStream_t s) {
+  using Shape = SplitShape<FMT, D>;
+  static_assert(Shape::RING >= SP_WARPS * 8 * NT * (D + 4) * 4, "the ring holds the warps' sums at the end of an item");
+  auto* kernel = attend_split_kernel<FMT, QFP16, D, NT>;
+  // set on every call: the setting belongs to the current device
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::RING) != cudaSuccess) { (void)cudaGetLastError(); return PTSTORE_E_CUDA; }
+  kernel<<<sms * (NT == 1 ? SP_CTAS : 2), SP_THREADS, Shape::RING, s>>>(a);
+  return cudaGetLastError() == cudaSuccess ? PTSTORE_OK : PTSTORE_E_CUDA;
+}
+
+template <int FMT, bool QFP16>
+int launch_split_shape(const Attend& a, int D, int nt, int sms, cudaStream_t s) {
+  if (D == 64) return nt == 1 ? launch_split<FMT, QFP16, 64, 1>(a, sms, s) : launch_split<FMT, QFP16, 64, 2>(a, sms, s);
+  return nt == 1 ? launch_split<FMT, QFP16, 128, 1>(a, sms, s) : launch_split<FMT, QFP16, 128, 2>(a, sms, s);
+}
+
+}  // namespace
+
+extern "C" uint64_t ptstore_attend_workspace_bytes(uint32_t head_dim) {
+  if (head_dim != 64 && head_dim != 128) return 0;
+  const u64 ctas = (u64)MAX_SMS * SP_CTAS;
+  return counters_bytes((int)ctas) + ctas * 2 * 16 * (head_dim + 2) * 4;
+}
+
+extern "C" int ptstore_attend(const ptstore_attend_t* p, const ptstore_kv_cache_t* cache, void* workspace, uint64_t workspace_bytes,
+                              uint32_t* status, ptstore_stream_t stream) {
+  if (!p || p->struct_size != sizeof(ptstore_attend_t)) return PTSTORE_E_INVAL;
+  const int rc = check_cache(cache);
+  if (rc) return rc;
+  const int D = (int)cache->head_dim;
+  if (p->requests < 0 || p->max_blocks < 1 || p->tokens < 0 || p->max_new < 0 || p->num_heads < 1) return PTSTORE_E_INVAL;
+  if (p->num_heads % (int)cache->num_kv_heads || p->num_heads > 65535) return PTSTORE_E_INVAL;
+  if (p->dtype != PTSTORE_KV_BF16 && p->dtype != PTSTORE_KV_FP16) return PTSTORE_E_INVAL;
+  if (cache->format != PTSTORE_KV_PACKED && cache->format != p->dtype) return PTSTORE_E_INVAL;
+  if (!isfinite(p->scale)) return PTSTORE_E_INVAL;
+  if (p->requests == 0 || p->tokens == 0 || p->max_new == 0) return PTSTORE_OK;
+  if (!p->q || !p->out || !p->token_offsets || !p->lengths || !p->block_tables) return PTSTORE_E_INVAL;
+  if (!rows_aligned(p->q, p->q_token_stride, p->q_head_stride) || !rows_aligned(p->out, p->out_token_stride, p->out_head_stride)) return PTSTORE_E_INVAL;
+  if (p->requests > 1 << 20 || (i64)p->tokens * p->num_heads > 0x7FFFFFFF) return PTSTORE_E_LIMIT;     // row indexes of a kv head are 32 bits wide
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PTSTORE_E_INVAL;
+  if (workspace_bytes < ptstore_attend_workspace_bytes(cache->head_dim)) return PTSTORE_E_NOMEM;
+  const bool packed = cache->format == PTSTORE_KV_PACKED;
+  Attend a;
+  a.cache = cache_of(cache);
+  a.q = static_cast<const unsigned char*>(p->q);
+  a.out = static_cast<unsigned char*>(p->out);
+  a.q_token = p->q_token_stride; a.q_head = p->q_head_stride;
+  a.o_token = p->out_token_stride; a.o_head = p->out_head_stride;
+  a.offsets = p->token_offsets; a.lengths = p->lengths; a.tables = p->block_tables;
+  a.R = p->requests; a.max_blocks = p->max_blocks; a.heads = p->num_heads; a.tokens = p->tokens;
+  a.group = p->num_heads / (int)cache->num_kv_heads;
+  a.scale2 = p->scale * LOG2E * (packed ? cache->k_scale * DEQ_FACTOR : 1.0f);
+  a.v_factor = packed ? cache->v_scale * DEQ_FACTOR : 1.0f;
+  a.work = static_cast<unsigned char*>(workspace);
+  a.status = status;
+  int sms = 0;
+  (void)cudaGetLastError();
+  const int rs = sm_count(&sms);
+  if (rs) return rs;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const int most = p->max_new < p->tokens ? p->max_new : p->tokens;
+  const int nt = n_tiles_of((i64)most * a.group);
+  const bool half = p->dtype == PTSTORE_KV_FP16;
+  if (packed) return half ? launch_split_shape<PTSTORE_KV_PACKED, true>(a, D, nt, sms, s) : launch_split_shape<PTSTORE_KV_PACKED, false>(a, D, nt, sms, s);
+  return half ? launch_split_shape<PTSTORE_KV_FP16, true>(a, D, nt, sms, s) : launch_split_shape<PTSTORE_KV_BF16, false>(a, D, nt, sms, s);
+}

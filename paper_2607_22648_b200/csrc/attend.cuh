@@ -1,0 +1,102 @@
+// What the attention kernels share: their arguments and small pieces of PTX.
+#pragma once
+#include "kvcache.cuh"
+
+namespace ptk {
+
+constexpr u32 FULL = 0xFFFFFFFFu;
+constexpr float LOG2E = 1.4426950408889634f;
+
+struct Attend {
+  Cache cache;
+  const unsigned char* q;
+  unsigned char* out;
+  i64 q_token, q_head, o_token, o_head;       // strides in elements
+  const int* offsets;                         // [R + 1] rows of q of every request
+  const int* lengths;                         // [R] tokens in the cache, the new ones among them
+  const int* tables;                          // [R][max_blocks]
+  int R, max_blocks, heads, group, tokens;    // query heads, query heads per kv head, rows of q
+  float scale2;                               // softmax scale * log2 e (* K's tensor scale and format factor for the 4-bit cache)
+  float v_factor;                             // what the 4-bit values of V are multiplied by at the end (1 for 16-bit caches)
+  unsigned char* work;
+  u32* status;
+};
+
+// rows of request r (clamped to the rows that exist), its keys, and the position of its first new token (may be negative)
+struct Req { int row0, fresh, keys, pos0; };
+__device__ __forceinline__ Req request(const Attend& a, int r) {
+  Req q;
+  int lo = a.offsets[r], hi = a.offsets[r + 1];
+  const int len = a.lengths[r];
+  lo = lo < 0 ? 0 : lo > a.tokens ? a.tokens : lo;
+  hi = hi < lo ? lo : hi > a.tokens ? a.tokens : hi;
+  q.row0 = lo;
+  q.fresh = hi - lo;
+  const i64 room = (i64)a.max_blocks * a.cache.block_tokens;
+  q.keys = len < 0 ? 0 : len > room ? (int)room : len;
+  q.pos0 = len - q.fresh;                     // a length the table cannot hold keeps its positions; the keys it lacks are not seen
+  return q;
+}
+
+__device__ __forceinline__ u32 smem_addr(const void* p) { return (u32)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void cp_async16(u32 dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async16_or_zero(u32 dst, const void* src, bool ok) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+template <bool FP16>
+__device__ __forceinline__ u32 pack2(float lo, float hi) {
+  u32 r;
+  if (FP16) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <bool FP16>
+__device__ __forceinline__ float2 unpack2(u32 v) {
+  if (FP16) return __half22float2(*reinterpret_cast<const __half2*>(&v));
+  return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v));
+}
+__device__ __forceinline__ u32 hfma2(u32 a, u32 b, u32 c) {
+  u32 r;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
+}
+__device__ __forceinline__ u32 hmul2(u32 a, u32 b) {
+  u32 r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// 4-bit codes to fp16.  A code n at bits p .. p+3 of 0x6400 reads as 1024 + n 2^p, and (1024 + n 2^p) * (s / 2^p) - (1024 / 2^p + 8) s
+// = (n - 8) s in one fused multiply-add.  It is exact: every constant below fits 11 bits for p >= 1 (520 s: 7 + 4 bits), so the
+// codes are read at bits 1..4 and 5..8.  s is the scale times 2^-8, which keeps 520 s inside fp16; the 2^8 is put back at the end.
+struct Deq { u32 s1, c1, s5, c5; };
+__device__ __forceinline__ Deq deq_of(u32 scale2) {          // two e4m3 scales as fp16 pairs
+  Deq d;
+  const u32 s = hmul2(scale2, 0x1C001C00u);                  // 2^-8
+  d.s1 = hmul2(s, 0x38003800u);                              // 2^-1
+  d.c1 = hmul2(s, 0xE010E010u);                              // -520
+  d.s5 = hmul2(s, 0x28002800u);                              // 2^-5
+  d.c5 = hmul2(s, 0xD100D100u);                              // -40
+  return d;
+}
+constexpr float DEQ_FACTOR = 256.0f;
+// the four nibbles of each 16-bit half: o[j] = (nibble j of the low half, nibble j of the high half)
+__device__ __forceinline__ void deq4(u32 x, const Deq& d, u32 (&o)[4]) {
+  const u32 l = x << 1, h = x >> 7;
+  o[0] = hfma2((l & 0x001E001Eu) | 0x64006400u, d.s1, d.c1);
+  o[1] = hfma2((l & 0x01E001E0u) | 0x64006400u, d.s5, d.c5);
+  o[2] = hfma2((h & 0x001E001Eu) | 0x64006400u, d.s1, d.c1);
+  o[3] = hfma2((h & 0x01E001E0u) | 0x64006400u, d.s5, d.c5);
+}
+
+}  // namespace ptk

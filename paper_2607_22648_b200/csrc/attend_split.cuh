@@ -1,0 +1,643 @@
+// Attention of a few query rows per request over a long paged cache (decode, speculative tokens): bounded by reading K and V once.
+//
+// o = sum_j p_j v_j / sum_j p_j, p_j = exp2(scale2 q.k_j - m): one pass over the cache with the running maximum m and sum per row.
+// Work is cut into units of 64 tokens of one (request, row tile, kv head) item; all units stand in one line and every CTA
+// takes the same number of them, so ragged batches load every SM alike and one long request is spread over all of them.  An item that
+// spans several CTAs leaves partial sums (o, m, l in 32 bits) in the workspace, and the CTA that arrives last joins them in CTA
+// order: the result does not depend on who that is.  One launch; the arrival counters are left zero.
+//
+// A row tile is 8 or 16 (query head of the group, new token) rows.  The tensor instructions (mma.sync m16n8k16; the work is a
+// twentieth of what the tensor cores could do, and tcgen05's 64 or 128 rows would be mostly empty) take TOKENS as their 16 rows and
+// queries as their 8 columns: S^T = K q^T, O^T = V^T P^T, so nothing is spent on rows that do not exist, and the 4-bit
+// values are unpacked straight into the A operand.  P^T changes from accumulator to operand layout by movmatrix.
+//
+// The four warps of a CTA run alone, each on every fourth 16-token tile through its own ring of shared-memory stages (cp.async), and
+// meet at the end of an item.
+#pragma once
+#include "attend.cuh"
+
+namespace ptk {
+
+constexpr int SP_WARPS = 4, SP_THREADS = 32 * SP_WARPS;
+constexpr int UNIT = SP_WARPS * TILE;        // tokens of a unit: one tile per warp
+constexpr int MIN_UNITS = 4;                 // a CTA takes at least this many, so that joining does not cost more than it saves
+constexpr int SP_CTAS = 3;                   // per SM
+
+template <int FMT, int D>
+struct SplitShape {
+  static constexpr bool PACKED = FMT == PTSTORE_KV_PACKED;
+  static constexpr int STAGE = PACKED ? 2 * tile_bytes(D) : 2 * TILE * D * 2;      // K tile, V tile
+  static constexpr int STAGES = PACKED ? 6 : 2 * (128 / D);
+  static constexpr int STEP = PACKED ? 2 : 1;                                      // tiles per softmax step
+  static constexpr int RING = SP_WARPS * STAGES * STAGE;
+};
+
+template <int NT, int D>
+__host__ __device__ constexpr int part_floats() { return 8 * NT * (D + 2); }      // partial sums of one item in one CTA: o, m, l
+
+template <bool FP16>
+__device__ __forceinline__ void mma16816(float (&c)[4], const u32 (&a)[4], const u32 (&b)[2]) {
+  if (FP16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+__device__ __forceinline__ u32 transpose8x8(u32 v) {
+  u32 r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ void ldsm4(u32 (&r)[4], u32 addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ void ldsm4_t(u32 (&r)[4], u32 addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+
+// keys row tile rt of a request can see (of its last row), and its units (at least one: a row that sees nothing is written too)
+template <int NQ>
+__device__ __forceinline__ int tile_keys(const Attend& a, const Req& q, int rt) {
+  const i64 rows = (i64)q.fresh * a.group;
+  const i64 end = (i64)(rt + 1) * NQ;
+  const int last = end >= rows ? q.fresh - 1 : (int)((end - 1) / a.group);
+  const i64 k = (i64)q.pos0 + last + 1;
+  return k <= 0 ? 0 : k > q.keys ? q.keys : (int)k;
+}
+__device__ __forceinline__ int units_of(int keys) { return keys <= UNIT ? 1 : (keys + UNIT - 1) / UNIT; }
+template <int NQ>
+__device__ __forceinline__ int row_tiles(const Attend& a, const Req& q) { return (int)(((i64)q.fresh * a.group + NQ - 1) / NQ); }
+template <int NQ>
+__device__ __forceinline__ i64 request_units(const Attend& a, int r) {
+  const Req q = request(a, r);
+  const int n = row_tiles<NQ>(a, q);
+  i64 u = 0;
+  for (int rt = 0; rt < n; ++rt) u += units_of(tile_keys<NQ>(a, q, rt));
+  return u * a.cache.heads;
+}
+
+template <int FMT, bool QFP16, int D, int NT>
+__global__ void __launch_bounds__(SP_THREADS, NT == 1 ? SP_CTAS : 2) attend_split_kernel(Attend a) {
+  using Shape = SplitShape<FMT, D>;
+  constexpr bool PACKED = Shape::PACKED;
+  constexpr bool F16 = PACKED || FMT == PTSTORE_KV_FP16;      // type of the products' operands
+  constexpr int NQ = 8 * NT, STAGE = Shape::STAGE, STAGES = Shape::STAGES, STEP = Shape::STEP;
+  constexpr int KS = D / 16, MT = D / 16;                     // k steps of q.k, m tiles of o
+  constexpr int OS = D + 4;                                   // row stride of the joined o in shared memory (floats)
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ i64 s_scan[SP_WARPS];
+  __shared__ i64 s_left;
+  __shared__ int s_r, s_last;
+  __shared__ float s_m[SP_WARPS][NQ], s_l[SP_WARPS][NQ], s_qf[NQ];
+  __shared__ __align__(16) unsigned short s_q[NQ][D + 8];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+
+  // ---- which units are this CTA's: every CTA sums the units of all requests, consecutive requests per thread
+  const int per_thread = (a.R + SP_THREADS - 1) / SP_THREADS;
+  const int rb = tid * per_thread < a.R ? tid * per_thread : a.R, re = rb + per_thread < a.R ? rb + per_thread : a.R;
+  i64 mine = 0;
+  for (int r = rb; r < re; ++r) mine += request_units<NQ>(a, r);
+  i64 x = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const i64 y = __shfl_up_sync(FULL, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) s_scan[warp] = x;
+  __syncthreads();
+  i64 total = 0, before = x - mine;
+#pragma unroll
+  for (int w = 0; w < SP_WARPS; ++w) {
+    if (w < warp) before += s_scan[w];
+    total += s_scan[w];
+  }
+  i64 per = (total + gridDim.x - 1) / gridDim.x;
+  if (per < MIN_UNITS) per = MIN_UNITS;
+  const i64 u_begin = blockIdx.x * per, u_end = u_begin + per < total ? u_begin + per : total;
+  if (u_begin >= u_end) return;
+  if (u_begin >= before && u_begin < before + mine) {         // exactly one thread
+    i64 left = u_begin - before;
+    int r = rb;
+    for (;; ++r) {
+      const i64 n = request_units<NQ>(a, r);
+      if (left < n) break;
+      left -= n;
+    }
+    s_r = r;
+    s_left = left;
+  }
+  __syncthreads();
+  int r = s_r;
+  i64 left = s_left;
+  i64 u = u_begin;
+
+  unsigned char* const ring = smem + warp * STAGES * STAGE;
+  const u32 ring_addr = smem_addr(ring);
+  int rt = 0;
+  Req rq = request(a, r);
+  while (u < u_end) {
+    // ---- the item under u: request r, row tile rt, kv head h, and the part [ua, ub) of its units
+    int keys, n_units;
+    for (;;) {
+      if (rt >= row_tiles<NQ>(a, rq)) {
+        if (++r >= a.R) return;                               // cannot happen while offsets and lengths hold still
+        rt = 0;
+        rq = request(a, r);
+        continue;
+      }
+      keys = tile_keys<NQ>(a, rq, rt);
+      n_units = units_of(keys);
+      const i64 all = (i64)n_units * a.cache.heads;
+      if (left < all) break;
+      left -= all;
+      ++rt;
+    }
+    const int h = (int)(left / n_units), ua = (int)(left % n_units);
+    const int ub = u_end - u < n_units - ua ? ua + (int)(u_end - u) : n_units;
+    const i64 item_begin = u - ua, item_end = item_begin + n_units;
+    const int row_base = rt * NQ, rows_left = rq.fresh * a.group - row_base, rows = rows_left < NQ ? rows_left : NQ;
+
+    // ---- loads of this warp's tiles: tile i of the part is tokens (ua + i) * 64 + warp * 16 ..
+    const int n_tiles = ub - ua;
+    const int* table = a.tables + (i64)r * a.max_blocks;
+    const u32 B = a.cache.block_tokens;
+    const u32 step_blk = UNIT / B, step_off = UNIT % B;
+    const u32 my_tok0 = (u32)ua * UNIT + warp * TILE + (PACKED ? 0 : lane & 15);
+    u32 n_blk = my_tok0 / B, n_off = my_tok0 % B;             // of the next tile to issue (16-bit caches: of row lane & 15 of it)
+    int n_tok = (int)my_tok0;
+    auto look_up = [&]() { return n_tok < keys ? table[n_blk] : -1; };
+    int n_id = n_tiles > 0 ? look_up() : -1;
+    u32 seen_bits = 0;                                        // bit s: stage s holds a tile (16-bit: bits of this lane's row)
+    bool bounds = false;
+    auto issue = [&](int i, int s) {
+      seen_bits &= ~(1u << s);
+      if (i < n_tiles) {
+        const int id = n_id;
+        const u32 blk_off = n_off;
+        const bool in_len = n_tok < keys;
+        const bool ok = in_len && (u32)id < a.cache.num_blocks;
+        bounds |= in_len && !ok;
+        n_off += step_off;
+        n_blk += step_blk;
+        n_tok += UNIT;
+        if (n_off >= B) { n_off -= B; ++n_blk; }
+        if (i + 1 < n_tiles) n_id = look_up();
+        if (ok) seen_bits |= 1u << s;
+        const u32 dst = ring_addr + s * STAGE;
+        if (PACKED) {
+          if (ok) {
+            constexpr int N16 = tile_bytes(D) / 16;
+            const unsigned char* ks = tile_ptr(a.cache, false, id, h, blk_off, D);
+            const unsigned char* vs = ks + a.cache.kv_stride;
+#pragma unroll
+            for (int c = lane; c < 2 * N16; c += 32) cp_async16(dst + c * 16, c < N16 ? ks + c * 16 : vs + (c - N16) * 16);
+          }
+        } else {
+          // two rows per instruction; 16-byte chunk c of row n sits at c ^ (n & 7), which ldmatrix reads without conflicts
+          constexpr int CPR = D / 8, RPI = 32 / CPR;          // chunks per row, rows per instruction
+          const u64 row_off = ok ? (u64)id * a.cache.block_stride + ((u64)blk_off * a.cache.heads + h) * (D * 2) : 0;
+#pragma unroll
+          for (int j = 0; j < TILE / RPI; ++j) {
+            const int n = j * RPI + lane / CPR, c = lane % CPR;
+            const u64 off = __shfl_sync(FULL, row_off, n);
+            const bool has = __shfl_sync(FULL, ok, n);
+            const unsigned char* ks = a.cache.base + off + c * 16;
+            const u32 d = dst + n * (D * 2) + ((c ^ (n & 7)) * 16);
+            cp_async16_or_zero(d, ks, has);
+            cp_async16_or_zero(d + TILE * D * 2, ks + a.cache.kv_stride, has);
+          }
+        }
+      }
+      cp_commit();
+    };
+    const int P = STAGES;
+#pragma unroll
+    for (int i = 0; i < P; ++i) issue(i, i);
+
+    // ---- q of the item into shared memory in the products' type; rows that do not exist are zero
+    {
+      constexpr int TPR = SP_THREADS / NQ, E = D / TPR;       // threads per row, elements per thread
+      const int row = tid / TPR, e0 = (tid % TPR) * E;
+      __align__(16) u32 raw[E / 2];
+      const bool live = row < rows;
+      if (live) {
+        const int fr = (row_base + row) / a.group, hq = h * a.group + (row_base + row) % a.group;
+        const unsigned char* src = a.q + 2 * ((i64)(rq.row0 + fr) * a.q_token + (i64)hq * a.q_head + e0);
+        if (E >= 8) {
+#pragma unroll
+          for (int i = 0; i < E / 8; ++i) *reinterpret_cast<uint4*>(raw + 4 * i) = reinterpret_cast<const uint4*>(src)[i];
+        } else *reinterpret_cast<uint2*>(raw) = *reinterpret_cast<const uint2*>(src);
+      } else {
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) raw[i] = 0;
+      }
+      float factor = 1.0f;
+      if (PACKED && !QFP16) {
+        // bf16 rows go into the products as fp16, scaled by a power of two so that the largest element is in [1, 2): exact but
+        // for elements below 2^-14 of the largest, which lose at most 2^-25 of it
+        float amax = 0.0f;
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+          const float2 f = unpack2<false>(raw[i]);
+          amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));
+        }
+#pragma unroll
+        for (int o = 1; o < TPR; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(FULL, amax, o));
+        int e = amax > 0.0f ? (int)(__float_as_uint(amax) >> 23) - 127 : 0;
+        e = e < -126 ? -126 : e > 126 ? 126 : e;
+        factor = __uint_as_float((u32)(127 + e) << 23);
+        const float down = __uint_as_float((u32)(127 - e) << 23);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+          const float2 f = unpack2<false>(raw[i]);
+          raw[i] = pack2<true>(f.x * down, f.y * down);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < E / 2; ++i) *reinterpret_cast<u32*>(&s_q[row][e0 + 2 * i]) = raw[i];
+      if (e0 == 0) s_qf[row] = factor * a.scale2;
+    }
+    __syncthreads();
+    u32 qb[NT][KS][2];
+    float qs[NT][2];
+    int see[NT][2];                                           // keys the lane's two query rows see
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (PACKED) {                                       // element order of the 4-bit rows: word w, nibbles j and j + 4
+            const unsigned short* p = &s_q[8 * n + g][(D / 4) * t + 8 * (k >> 1) + 2 * (k & 1) + i];
+            qb[n][k][i] = (u32)p[0] | ((u32)p[4] << 16);
+          } else qb[n][k][i] = *reinterpret_cast<const u32*>(&s_q[8 * n + g][16 * k + 2 * t + 8 * i]);
+        }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int row = 8 * n + 2 * t + i;
+        qs[n][i] = s_qf[row];
+        const i64 p = (i64)rq.pos0 + (row_base + row) / a.group + 1;
+        see[n][i] = row >= rows ? 0 : p < 0 ? 0 : p > keys ? keys : (int)p;
+      }
+    }
+    // tokens below this are seen by every row of the tile
+    int all_see = rows > 0 ? rq.pos0 + row_base / a.group + 1 : 0;
+    all_see = all_see < 0 ? 0 : all_see > keys ? keys : all_see;
+
+    float o[NT][MT][4], m[NT][2], l[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[n][i][c] = 0.0f;
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.0f;
+    }
+
+    // token of accumulator row (c >> 1) of tile tok0
+    auto token_of = [&](int half) { return PACKED ? 4 * (g >> 1) + (g & 1) + 2 * half : g + 8 * half; };
+
+    // o += V^T p for one tile; with `limit`, tokens from limit on count as zero whatever they hold
+    auto pv = [&](const unsigned char* st, u32 st_addr, const u32 (&pb)[NT][2], int tok0, int limit, bool mask) {
+      if (PACKED) {
+        const unsigned char* vt = st + tile_bytes(D);
+        u32 sc = *reinterpret_cast<const u32*>(vt + 8 * D + (D == 128 ? g : g >> 1) * TILE + 4 * t);
+        if (mask) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (tok0 + 4 * t + i >= limit) sc &= ~(0xFFu << (8 * i));
+        }
+        const Deq da = deq_of(e4m3x2_to_half2(sc & 0xFFFFu)), db = deq_of(e4m3x2_to_half2(sc >> 16));
+#pragma unroll
+        for (int w = 0; w < D / 64; ++w) {
+          u32 c[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int chunk = D == 128 ? g >> 1 : g >> 2, byte = D == 128 ? (g & 1) * 8 + 4 * w : (g & 3) * 4;
+            // a token's place inside its tile, with n = 4 t + i written out
+            const int rho = 256 / D, place = ((4 * t + i) / rho) * 8 + (((i % rho) * (D / 32) + chunk) ^ (2 * t));
+            c[i] = *reinterpret_cast<const u32*>(vt + place * 16 + byte);
+          }
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            u32 va[4], vb[4];
+            const u32 sel = half ? 0x7632u : 0x5410u;
+            deq4(__byte_perm(c[0], c[1], sel), da, va);
+            deq4(__byte_perm(c[2], c[3], sel), db, vb);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const u32 av[4] = {va[2 * i], va[2 * i + 1], vb[2 * i], vb[2 * i + 1]};
+#pragma unroll
+              for (int n = 0; n < NT; ++n) mma16816<F16>(o[n][4 * w + 2 * half + i], av, pb[n]);
+            }
+          }
+        }
+      } else {
+        const u32 vt = st_addr + TILE * D * 2;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          // matrices of the transposing load: (d 0-7, tokens 0-7), (d 8-15, tokens 0-7), (d 0-7, tokens 8-15), (d 8-15, tokens 8-15)
+          const int row = (lane & 7) + ((lane >> 4) & 1) * 8, chunk = 2 * i + ((lane >> 3) & 1);
+          u32 av[4];
+          ldsm4_t(av, vt + row * (D * 2) + ((chunk ^ (row & 7)) * 16));
+          if (mask) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const int tok = tok0 + 2 * t + (c >> 1) * 8;
+              if (tok >= limit) av[c] = 0;
+              else if (tok + 1 >= limit) av[c] &= 0xFFFFu;
+            }
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma16816<F16>(o[n][i], av, pb[n]);
+        }
+      }
+    };
+    // does V of this tile hold an infinity or a NaN
+    auto odd_values = [&](const unsigned char* st) {
+      bool odd = false;
+      if (PACKED) {
+        const u32* s = reinterpret_cast<const u32*>(st + tile_bytes(D) + 8 * D);
+#pragma unroll
+        for (int i = lane; i < D / 4; i += 32)
+#pragma unroll
+          for (int b = 0; b < 4; ++b) odd |= ((s[i] >> (8 * b)) & 0x7Fu) == 0x7Fu;
+      } else {
+        const u32* s = reinterpret_cast<const u32*>(st + TILE * D * 2);
+        const u32 ex = F16 ? 0x7C00u : 0x7F80u;
+        for (int i = lane; i < TILE * D / 2; i += 32) odd |= (s[i] & ex) == ex || ((s[i] >> 16) & ex) == ex;
+      }
+      return __any_sync(FULL, odd);
+    };
+
+    // ---- the tiles, STEP at a time
+    int s0 = 0;                                               // stage of tile i
+    for (int i = 0; i < n_tiles; i += STEP) {
+      cp_wait<STAGES - STEP>();
+      __syncwarp();
+      float sc[STEP][NT][4];
+      bool held[STEP];
+#pragma unroll
+      for (int k = 0; k < STEP; ++k) {
+        const int s = s0 + k;
+        const unsigned char* st = ring + s * STAGE;
+        const int tok0 = (ua + i + k) * UNIT + warp * TILE;
+        const u32 rows_in = PACKED ? ((seen_bits >> s) & 1 ? 0xFFFFu : 0u) : __ballot_sync(FULL, (seen_bits >> s) & 1) & 0xFFFFu;
+        held[k] = i + k < n_tiles && rows_in != 0;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) sc[k][n][c] = 0.0f;
+        if (held[k]) {
+          if (PACKED) {
+            const int n0 = token_of(0), n1 = token_of(1);
+            __align__(16) u32 c0[D / 32], c1[D / 32];
+            u32 z0, z1;
+            if (D == 128) {
+              *reinterpret_cast<uint4*>(c0) = *reinterpret_cast<const uint4*>(st + code_place(D, n0, t) * 16);
+              *reinterpret_cast<uint4*>(c1) = *reinterpret_cast<const uint4*>(st + code_place(D, n1, t) * 16);
+              z0 = e4m3x2_to_half2(*reinterpret_cast<const unsigned short*>(st + 8 * D + n0 * 8 + 2 * t));
+              z1 = e4m3x2_to_half2(*reinterpret_cast<const unsigned short*>(st + 8 * D + n1 * 8 + 2 * t));
+            } else {
+              *reinterpret_cast<uint2*>(c0) = *reinterpret_cast<const uint2*>(st + code_place(D, n0, t >> 1) * 16 + (t & 1) * 8);
+              *reinterpret_cast<uint2*>(c1) = *reinterpret_cast<const uint2*>(st + code_place(D, n1, t >> 1) * 16 + (t & 1) * 8);
+              z0 = e4m3x2_to_half2(st[8 * D + n0 * 4 + t]);
+              z1 = e4m3x2_to_half2(st[8 * D + n1 * 4 + t]);
+            }
+#pragma unroll
+            for (int gr = 0; gr < D / 64; ++gr) {             // the lane's scale groups of 16 elements
+              const u32 sel = gr ? 0x3232u : 0x1010u;
+              const Deq d0 = deq_of(__byte_perm(z0, z0, sel)), d1 = deq_of(__byte_perm(z1, z1, sel));
+#pragma unroll
+              for (int w = 2 * gr; w < 2 * gr + 2; ++w) {
+                u32 v0[4], v1[4];
+                deq4(c0[w], d0, v0);
+                deq4(c1[w], d1, v1);
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                  const u32 av[4] = {v0[2 * b], v1[2 * b], v0[2 * b + 1], v1[2 * b + 1]};
+#pragma unroll
+                  for (int n = 0; n < NT; ++n) mma16816<F16>(sc[k][n], av, qb[n][2 * w + b]);
+                }
+              }
+            }
+          } else {
+            const u32 sa = ring_addr + s * STAGE;
+#pragma unroll
+            for (int kk = 0; kk < KS; ++kk) {
+              const int row = (lane & 7) + ((lane >> 3) & 1) * 8, chunk = 2 * kk + (lane >> 4);
+              u32 av[4];
+              ldsm4(av, sa + row * (D * 2) + ((chunk ^ (row & 7)) * 16));
+#pragma unroll
+              for (int n = 0; n < NT; ++n) mma16816<F16>(sc[k][n], av, qb[n][kk]);
+            }
+          }
+        }
+        const bool whole = held[k] && rows_in == 0xFFFFu && tok0 + TILE <= all_see;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            sc[k][n][c] *= qs[n][c & 1];
+            if (!whole) {
+              const int in = token_of(c >> 1);
+              if (!held[k] || tok0 + in >= see[n][c & 1] || !((rows_in >> in) & 1)) sc[k][n][c] = -INFINITY;
+            }
+          }
+      }
+      // running maximum over the step, then the weights
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float x = m[n][c];
+#pragma unroll
+          for (int k = 0; k < STEP; ++k) x = fmaxf(x, fmaxf(sc[k][n][c], sc[k][n][c + 2]));
+#pragma unroll
+          for (int w = 4; w < 32; w <<= 1) x = fmaxf(x, __shfl_xor_sync(FULL, x, w));
+          if (__any_sync(FULL, x != m[n][c])) {
+            const float f = x == -INFINITY ? 1.0f : exp2_fast(m[n][c] - x);
+            m[n][c] = x;
+            l[n][c] *= f;
+#pragma unroll
+            for (int i2 = 0; i2 < MT; ++i2) { o[n][i2][c] *= f; o[n][i2][c + 2] *= f; }
+          }
+        }
+#pragma unroll
+      for (int k = 0; k < STEP; ++k) {
+        if (!held[k]) continue;
+        const int s = s0 + k;
+        const int tok0 = (ua + i + k) * UNIT + warp * TILE;
+        u32 pb[NT][2];
+        float p[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            p[n][c] = exp2_fast(sc[k][n][c] - (m[n][c & 1] == -INFINITY ? 0.0f : m[n][c & 1]));
+            l[n][c & 1] += p[n][c];
+          }
+          pb[n][0] = transpose8x8(pack2<F16>(p[n][0], p[n][1]));
+          pb[n][1] = transpose8x8(pack2<F16>(p[n][2], p[n][3]));
+        }
+        const unsigned char* st = ring + s * STAGE;
+        const u32 sa = ring_addr + s * STAGE;
+        if (tok0 + TILE <= all_see) pv(st, sa, pb, tok0, 0, false);
+        else if (rq.fresh == 1 || !odd_values(st)) pv(st, sa, pb, tok0, keys, true);
+        else {
+          // a weight of zero times an infinity is not zero: one new token's rows at a time, V cut off at what they see
+          for (int fr = row_base / a.group; fr <= (row_base + rows - 1) / a.group; ++fr) {
+            u32 pf[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              const bool own = (row_base + 8 * n + g) / a.group == fr;     // operand column g
+              pf[n][0] = own ? pb[n][0] : 0;
+              pf[n][1] = own ? pb[n][1] : 0;
+            }
+            const int lim = rq.pos0 + fr + 1;
+            // columns of other rows would still meet what this limit lets through: their sums are kept aside
+            float keep[NT][MT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int i2 = 0; i2 < MT; ++i2)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) keep[n][i2][c] = o[n][i2][c];
+            pv(st, sa, pf, tok0, lim < keys ? lim : keys, true);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int c = 0; c < 4; ++c)
+                if ((row_base + 8 * n + 2 * t + (c & 1)) / a.group != fr) {
+#pragma unroll
+                  for (int i2 = 0; i2 < MT; ++i2) o[n][i2][c] = keep[n][i2][c];
+                }
+          }
+        }
+      }
+      __syncwarp();
+#pragma unroll
+      for (int k = 0; k < STEP; ++k) issue(i + STAGES + k, s0 + k);
+      s0 += STEP;
+      if (s0 == STAGES) s0 = 0;
+    }
+    cp_wait<0>();
+    if (bounds && a.status) atomicOr(a.status, PTSTORE_S_BOUNDS);
+
+    // ---- join the four warps
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1) l[n][c] += __shfl_xor_sync(FULL, l[n][c], w);
+        if (g == 0) {
+          s_m[warp][8 * n + 2 * t + c] = m[n][c];
+          s_l[warp][8 * n + 2 * t + c] = l[n][c];
+        }
+      }
+    __syncthreads();                                          // the ring is idle from here on: it holds the warps' sums
+    float* s_o = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int row = 8 * n + 2 * t + c;
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < SP_WARPS; ++w) top = fmaxf(top, s_m[w][row]);
+        const float f = m[n][c] == -INFINITY ? 0.0f : exp2_fast(m[n][c] - top);
+        const bool none = m[n][c] == -INFINITY && l[n][c] == 0.0f;          // a NaN keeps its way through
+        float* dst = s_o + (warp * NQ + row) * OS;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const int d0 = PACKED ? (D / 8) * g + 2 * i : 16 * i + g, d1 = PACKED ? d0 + 1 : d0 + 8;
+          dst[d0] = none ? 0.0f : o[n][i][c] * (m[n][c] == -INFINITY ? 1.0f : f);
+          dst[d1] = none ? 0.0f : o[n][i][c + 2] * (m[n][c] == -INFINITY ? 1.0f : f);
+        }
+      }
+    __syncthreads();
+    constexpr int TPR = SP_THREADS / NQ, E = D / TPR;         // threads per row, elements per thread
+    const int row = tid / TPR, e0 = (tid % TPR) * E;
+    float acc[E], top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < SP_WARPS; ++w) top = fmaxf(top, s_m[w][row]);
+#pragma unroll
+    for (int w = 0; w < SP_WARPS; ++w) {
+      const float lw = s_l[w][row], mw = s_m[w][row];
+      sum += mw == -INFINITY ? lw : lw * exp2_fast(mw - top);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      acc[e] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < SP_WARPS; ++w) acc[e] += s_o[(w * NQ + row) * OS + e0 + e];
+    }
+    const i64 first_cta = item_begin / per, last_cta = (item_end - 1) / per;
+    bool write = true;
+    if (first_cta != last_cta) {
+      // partial sums: slot 1 of the CTA the item begins in, slot 0 of the others
+      constexpr int PF = part_floats<NT, D>();
+      u32* counters = reinterpret_cast<u32*>(a.work);
+      float* parts = reinterpret_cast<float*>(a.work + ((gridDim.x * 4 + 255) / 256) * 256);
+      float* my = parts + (2 * (i64)blockIdx.x + (blockIdx.x == first_cta ? 1 : 0)) * PF;
+      if (row < rows) {
+#pragma unroll
+        for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(my + row * D + e0 + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+        if (e0 == 0) { my[NQ * D + row] = top; my[NQ * D + NQ + row] = sum; }
+      }
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        const u32 n = (u32)(last_cta - first_cta);
+        const bool last = atomicAdd(&counters[first_cta], 1u) == n;
+        if (last) counters[first_cta] = 0;
+        s_last = last;
+      }
+      __syncthreads();
+      write = s_last != 0;
+      if (write && row < rows) {
+        __threadfence();
+        top = -INFINITY;
+        for (i64 c = first_cta; c <= last_cta; ++c) top = fmaxf(top, __ldcg(parts + (2 * c + (c == first_cta ? 1 : 0)) * PF + NQ * D + row));
+        sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+#pragma unroll 4
+        for (i64 c = first_cta; c <= last_cta; ++c) {
+          const float* p = parts + (2 * c + (c == first_cta ? 1 : 0)) * PF;
+          const float mc = __ldcg(p + NQ * D + row), lc = __ldcg(p + NQ * D + NQ + row);
+          const float f = mc == -INFINITY ? 1.0f : exp2_fast(mc - top);     // nothing seen: sums of zero (or NaN)
+          sum += lc * f;
+#pragma unroll
+          for (int e = 0; e < E; e += 4) {
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(p + row * D + e0 + e));
+            acc[e] += v.x * f;
+            acc[e + 1] += v.y * f;
+            acc[e + 2] += v.z * f;
+            acc[e + 3] += v.w * f;
+          }
+        }
+      }
+    }
+    if (write && row < rows) {
+      const float f = sum == 0.0f ? 0.0f : a.v_factor / sum;               // a row that sees nothing is zero
+      const int fr = (row_base + row) / a.group, hq = h * a.group + (row_base + row) % a.group;
+      unsigned char* dst = a.out + 2 * ((i64)(rq.row0 + fr) * a.o_token + (i64)hq * a.o_head + e0);
+      __align__(16) u32 v[E / 2];
+#pragma unroll
+      for (int e = 0; e < E / 2; ++e) v[e] = pack2<QFP16>(acc[2 * e] * f, acc[2 * e + 1] * f);
+      if (E >= 8) {
+#pragma unroll
+        for (int i = 0; i < E / 8; ++i) reinterpret_cast<uint4*>(dst)[i] = *reinterpret_cast<const uint4*>(v + 4 * i);
+      } else *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(v);
+    }
+    __syncthreads();                                          // the ring and the small arrays are free again
+    u += ub - ua;
+    left += ub - ua;
+  }
+}
+
+}  // namespace ptk

@@ -1,0 +1,202 @@
+// ptstore_kv_write / ptstore_kv_read: rows of a model's K and V into the paged cache through a slot map, and back.
+//
+// Bound: HBM.  A 16-bit element costs 2 bytes on the model's side and 2 or 0.5625 in the cache, nothing is read twice.  One thread
+// takes 16 consecutive elements (a scale group): two 16-byte loads, its own maximum, eight bytes of codes and a scale, so there
+// is no exchange between threads.  What the quantiser computes is defined in exact terms (nearest code of x / (scale * tensor
+// scale), ties to even); 32 bits give exactly that: x has at most 11 significant bits and the divisor 4, so a quotient that is not
+// on a rounding border is at least 2^-16 away from it, and one that is comes out exactly (the division below is corrected by its residual).
+#include "kvcache.cuh"
+
+using namespace ptk;
+
+namespace {
+
+constexpr int WRITE_THREADS = 256;
+
+struct Rows {
+  unsigned char* k;
+  unsigned char* v;
+  i64 k_token, k_head, v_token, v_head;        // strides in elements
+};
+
+struct KvArgs {
+  Cache cache;
+  Rows rows;
+  const i64* slots;
+  i64 items;                                   // T * heads * (D / 16)
+  float k_scale, v_scale;
+  u32* status;
+};
+
+template <bool FP16>
+__device__ __forceinline__ float2 widen(u32 two) {
+  if (FP16) return __half22float2(*reinterpret_cast<const __half2*>(&two));
+  return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&two));
+}
+template <bool FP16>
+__device__ __forceinline__ u32 narrow(float a, float b) {
+  if (FP16) { const __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<const u32*>(&h); }
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const u32*>(&h);
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// cache position of item -> false if it is skipped
+struct Where { u32 block, token, head, group; i64 row; };
+template <int D>
+__device__ __forceinline__ bool locate(const KvArgs& a, i64 item, Where& w) {
+  constexpr u32 G = D / GROUP;
+  w.group = (u32)item % G;
+  const u64 rest = (u64)item / G;
+  if (rest <= 0xFFFFFFFFull) { w.row = (u32)rest / a.cache.heads; w.head = (u32)rest % a.cache.heads; }
+  else { w.row = (i64)(rest / a.cache.heads); w.head = (u32)(rest % a.cache.heads); }
+  const i64 slot = a.slots[w.row];
+  if (slot == -1) return false;
+  u64 block;
+  if ((u64)slot <= 0xFFFFFFFFull) { block = (u32)slot / a.cache.block_tokens; w.token = (u32)slot % a.cache.block_tokens; }
+  else { block = (u64)slot / a.cache.block_tokens; w.token = (u32)((u64)slot % a.cache.block_tokens); }
+  if (slot < 0 || block >= a.cache.num_blocks) {
+    if (a.status) atomicOr(a.status, PTSTORE_S_BOUNDS);
+    return false;
+  }
+  w.block = (u32)block;
+  return true;
+}
+
+__device__ __forceinline__ const unsigned char* model_row(const Rows& r, bool is_v, const Where& w) {
+  return is_v ? r.v + 2 * (w.row * r.v_token + w.head * r.v_head + w.group * GROUP) : r.k + 2 * (w.row * r.k_token + w.head * r.k_head + w.group * GROUP);
+}
+
+template <int D, bool FP16, bool PACKED>
+__global__ void __launch_bounds__(WRITE_THREADS) kv_write_kernel(KvArgs a) {
+  const i64 item = (i64)blockIdx.x * WRITE_THREADS + threadIdx.x;
+  if (item >= a.items) return;
+  const bool is_v = blockIdx.y != 0;
+  Where w;
+  if (!locate<D>(a, item, w)) return;
+  const uint4* src = reinterpret_cast<const uint4*>(model_row(a.rows, is_v, w));
+  const uint4 lo = src[0], hi = src[1];
+  if (!PACKED) {
+    uint4* dst = reinterpret_cast<uint4*>(row_ptr(a.cache, is_v, w.block, w.head, w.token, D) + w.group * GROUP * 2);
+    dst[0] = lo;
+    dst[1] = hi;
+    return;
+  }
+  const u32 raw[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  float x[16], amax = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float2 f = widen<FP16>(raw[i]);
+    x[2 * i] = f.x;
+    x[2 * i + 1] = f.y;
+    amax = max_nan(amax, max_nan(fabsf(f.x), fabsf(f.y)));
+  }
+  const float t = is_v ? a.v_scale : a.k_scale;
+  const u32 sb = e4m3_of(__fdiv_rn(amax, 7.0f * t));
+  const float e = e4m3_value(sb) * t;                  // exact: 4 significant bits times a power of two
+  u32 code[2] = {0x88888888u, 0x88888888u};            // code 8 is zero
+  if (e > 0.0f) {
+    const float inv = __frcp_rn(e), most = 9.0f * e;
+    code[0] = code[1] = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float c = fminf(fmaxf(x[i], -most), most); // codes saturate far inside this; an infinity becomes finite
+      const float y = c * inv;
+      const float q = fmaf(fmaf(-y, e, c), inv, y);    // the quotient, exact where it is representable
+      const float n = fminf(fmaxf(q, -8.0f), 7.0f) + 12582912.0f;      // 1.5 * 2^23: rounds to an integer, ties to even
+      code[i >> 3] |= ((__float_as_uint(n) + 8u) & 15u) << (4 * (i & 7));
+    }
+  }
+  unsigned char* tile = tile_ptr(a.cache, is_v, w.block, w.head, w.token, D);
+  const int n = w.token % TILE;
+  *reinterpret_cast<uint2*>(tile + code_place(D, n, w.group >> 1) * 16 + (w.group & 1) * 8) = make_uint2(code[0], code[1]);
+  tile[scale_at(D, is_v, n, w.group)] = (unsigned char)sb;
+}
+
+template <int D, bool FP16, bool PACKED>
+__global__ void __launch_bounds__(WRITE_THREADS) kv_read_kernel(KvArgs a) {
+  const i64 item = (i64)blockIdx.x * WRITE_THREADS + threadIdx.x;
+  if (item >= a.items) return;
+  const bool is_v = blockIdx.y != 0;
+  Where w;
+  if (!locate<D>(a, item, w)) return;
+  uint4* dst = reinterpret_cast<uint4*>(const_cast<unsigned char*>(model_row(a.rows, is_v, w)));
+  if (!PACKED) {
+    const uint4* src = reinterpret_cast<const uint4*>(row_ptr(a.cache, is_v, w.block, w.head, w.token, D) + w.group * GROUP * 2);
+    const uint4 lo = src[0], hi = src[1];
+    dst[0] = lo;
+    dst[1] = hi;
+    return;
+  }
+  const unsigned char* tile = tile_ptr(a.cache, is_v, w.block, w.head, w.token, D);
+  const int n = w.token % TILE;
+  const uint2 code = *reinterpret_cast<const uint2*>(tile + code_place(D, n, w.group >> 1) * 16 + (w.group & 1) * 8);
+  const float e = e4m3_value(tile[scale_at(D, is_v, n, w.group)]) * (is_v ? a.v_scale : a.k_scale);
+  u32 out[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const u32 c = i < 4 ? code.x : code.y;
+    const int s = 8 * (i & 3);
+    out[i] = narrow<FP16>(e * ((int)((c >> s) & 15u) - 8), e * ((int)((c >> (s + 4)) & 15u) - 8));
+  }
+  dst[0] = make_uint4(out[0], out[1], out[2], out[3]);
+  dst[1] = make_uint4(out[4], out[5], out[6], out[7]);
+}
+
+// shared checks and launch; WRITE picks the kernel
+template <bool WRITE>
+int run(const void* k, const void* v, i64 k_token, i64 k_head, i64 v_token, i64 v_head, i64 tokens, u32 dtype, const int64_t* slots,
+        const ptstore_kv_cache_t* cache, u32* status, ptstore_stream_t stream) {
+  const int rc = check_cache(cache);
+  if (rc) return rc;
+  if (tokens < 0 || (dtype != PTSTORE_KV_BF16 && dtype != PTSTORE_KV_FP16)) return PTSTORE_E_INVAL;
+  if (cache->format != PTSTORE_KV_PACKED && cache->format != dtype) return PTSTORE_E_INVAL;
+  if (tokens == 0) return PTSTORE_OK;
+  if (!k || !v || !slots || !rows_aligned(k, k_token, k_head) || !rows_aligned(v, v_token, v_head)) return PTSTORE_E_INVAL;
+  const int D = (int)cache->head_dim;
+  KvArgs a = {cache_of(cache), {(unsigned char*)k, (unsigned char*)v, k_token, k_head, v_token, v_head}, reinterpret_cast<const i64*>(slots), 0,
+              cache->k_scale, cache->v_scale, status};
+  const u64 per_token = (u64)a.cache.heads * (D / GROUP);
+  if ((u64)tokens > (u64)0x7FFFFFFF * WRITE_THREADS / per_token) return PTSTORE_E_LIMIT;       // grid of one launch
+  a.items = (i64)((u64)tokens * per_token);
+  const dim3 grid((unsigned)((a.items + WRITE_THREADS - 1) / WRITE_THREADS), 2);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const bool half = dtype == PTSTORE_KV_FP16, packed = cache->format == PTSTORE_KV_PACKED;
+  (void)cudaGetLastError();
+#define PTK_LAUNCH(D_, H_, P_) \
+  if (D == D_ && half == H_ && packed == P_) { \
+    if (WRITE) kv_write_kernel<D_, H_, P_><<<grid, WRITE_THREADS, 0, s>>>(a); \
+    else kv_read_kernel<D_, H_, P_><<<grid, WRITE_THREADS, 0, s>>>(a); \
+  }
+  PTK_LAUNCH(64, false, false) PTK_LAUNCH(64, false, true) PTK_LAUNCH(64, true, true)
+  PTK_LAUNCH(128, false, false) PTK_LAUNCH(128, false, true) PTK_LAUNCH(128, true, true)
+  // a 16-bit cache is copied, whatever the 16 bits mean: the kernels compiled for bf16 serve fp16 too
+  if (half && !packed) {
+    if (D == 64) { if (WRITE) kv_write_kernel<64, false, false><<<grid, WRITE_THREADS, 0, s>>>(a); else kv_read_kernel<64, false, false><<<grid, WRITE_THREADS, 0, s>>>(a); }
+    else { if (WRITE) kv_write_kernel<128, false, false><<<grid, WRITE_THREADS, 0, s>>>(a); else kv_read_kernel<128, false, false><<<grid, WRITE_THREADS, 0, s>>>(a); }
+  }
+#undef PTK_LAUNCH
+  return cudaGetLastError() == cudaSuccess ? PTSTORE_OK : PTSTORE_E_CUDA;
+}
+
+}  // namespace
+
+extern "C" uint64_t ptstore_kv_chunk_bytes(uint32_t format, uint32_t block_tokens, uint32_t num_kv_heads, uint32_t head_dim) {
+  return chunk_bytes_of(format, block_tokens, num_kv_heads, head_dim);
+}
+
+extern "C" int ptstore_kv_write(const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
+                                int64_t v_head_stride, int64_t tokens, uint32_t dtype, const int64_t* slots, const ptstore_kv_cache_t* cache,
+                                uint32_t* status, ptstore_stream_t stream) {
+  return run<true>(k, v, k_token_stride, k_head_stride, v_token_stride, v_head_stride, tokens, dtype, slots, cache, status, stream);
+}
+
+extern "C" int ptstore_kv_read(const ptstore_kv_cache_t* cache, const int64_t* slots, int64_t tokens, uint32_t dtype, void* k,
+                               int64_t k_token_stride, int64_t k_head_stride, void* v, int64_t v_token_stride, int64_t v_head_stride,
+                               uint32_t* status, ptstore_stream_t stream) {
+  return run<false>(k, v, k_token_stride, k_head_stride, v_token_stride, v_head_stride, tokens, dtype, slots, cache, status, stream);
+}
