@@ -1,4 +1,5 @@
 // ptstore_attend: host side and dispatch of the attention over the paged cache.
+#include "attend_prompt.cuh"
 #include "attend_split.cuh"
 
 using namespace ptk;
@@ -38,6 +39,26 @@ int launch_split_shape(const Attend& a, int D, int nt, int sms, cudaStream_t s) 
   if (D == 64) return nt == 1 ? launch_split<FMT, QFP16, 64, 1>(a, sms, s) : launch_split<FMT, QFP16, 64, 2>(a, sms, s);
   return nt == 1 ? launch_split<FMT, QFP16, 128, 1>(a, sms, s) : launch_split<FMT, QFP16, 128, 2>(a, sms, s);
 }
+
+template <int FMT, bool QFP16, int D>
+int launch_prompt(const Attend& a, cudaStream_t s) {
+  auto* kernel = attend_prompt_kernel<FMT, QFP16, D>;
+  constexpr int SMEM = PromptShape<D>::SMEM;
+  // the kernel's warps trade registers, which is only sound if the block is launched with all of the SM's
+  cudaFuncAttributes attr;
+  if (cudaFuncGetAttributes(&attr, kernel) != cudaSuccess || attr.numRegs * PR_THREADS != 65536 ||
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return PTSTORE_E_CUDA;
+  }
+  const i64 tiles = (i64)a.tokens * a.group / PR_ROWS + a.R;            // at most this many, wherever the requests' rows end
+  if (tiles * a.cache.heads > 0x7FFFFFFF) return PTSTORE_E_LIMIT;
+  kernel<<<(unsigned)(tiles * a.cache.heads), PR_THREADS, SMEM, s>>>(a);
+  return cudaGetLastError() == cudaSuccess ? PTSTORE_OK : PTSTORE_E_CUDA;
+}
+
+// Rows of one kv head from which a request's attention goes to the tensor-memory kernel.
+constexpr i64 PROMPT_ROWS = 33;
 
 }  // namespace
 
@@ -86,6 +107,14 @@ extern "C" int ptstore_attend(const ptstore_attend_t* p, const ptstore_kv_cache_
   const int most = p->max_new < p->tokens ? p->max_new : p->tokens;
   const int nt = n_tiles_of((i64)most * a.group);
   const bool half = p->dtype == PTSTORE_KV_FP16;
+  if ((i64)most * a.group >= PROMPT_ROWS) {
+    if (D == 64) {
+      if (packed) return half ? launch_prompt<PTSTORE_KV_PACKED, true, 64>(a, s) : launch_prompt<PTSTORE_KV_PACKED, false, 64>(a, s);
+      return half ? launch_prompt<PTSTORE_KV_FP16, true, 64>(a, s) : launch_prompt<PTSTORE_KV_BF16, false, 64>(a, s);
+    }
+    if (packed) return half ? launch_prompt<PTSTORE_KV_PACKED, true, 128>(a, s) : launch_prompt<PTSTORE_KV_PACKED, false, 128>(a, s);
+    return half ? launch_prompt<PTSTORE_KV_FP16, true, 128>(a, s) : launch_prompt<PTSTORE_KV_BF16, false, 128>(a, s);
+  }
   if (packed) return half ? launch_split_shape<PTSTORE_KV_PACKED, true>(a, D, nt, sms, s) : launch_split_shape<PTSTORE_KV_PACKED, false>(a, D, nt, sms, s);
   return half ? launch_split_shape<PTSTORE_KV_FP16, true>(a, D, nt, sms, s) : launch_split_shape<PTSTORE_KV_BF16, false>(a, D, nt, sms, s);
 }

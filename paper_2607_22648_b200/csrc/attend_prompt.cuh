@@ -1,0 +1,612 @@
+// Attention of many new tokens per request over the paged cache (prompts, suffixes of found prefixes): bounded by the tensor cores.
+//
+// A CTA takes 256 rows of one (request, kv head): a row is a (new token, query head of the group) pair, so all rows share their keys and
+// grouped heads fill the 128-row tensor tiles even when a request has few new tokens.  Two tiles of 128 rows alternate: while
+// the softmax of one runs, the tensor cores work for the other.  Per step of 128 keys and tile:
+//     S = Q K^T (tcgen05.mma, both operands in shared memory, S in tensor memory)
+//     P = exp2(scale2 S - m), written over S in 16 bits     (one thread per row: no exchange between threads)
+//     O += P V (A operand from tensor memory, V read as it lies: d contiguous, the "MN-major" form)
+// O stays in tensor memory for the whole row of steps.  m is a running reference, not the exact maximum: it is moved (and O and the sum
+// rescaled) only when a score exceeds it by more than 2^8, so weights stay below 256 and the rescaling, a read and a write of all of O,
+// is rare after the first steps.
+//
+// Warps: 0-3 and 4-7 softmax of tile 0 and 1 (and their part of Q at the start and of the output at the end), 8-11 load K and V into a ring of
+// four 128-token tiles, 12 issues the tensor instructions (one thread).  13-15 only complete the warpgroup that gives its
+// registers to the softmax warps.
+//
+// Tensor memory (512 columns): S/P of tile 0, S/P of tile 1, O 0, O 1.  Shared memory operands are in the 128-byte swizzled form: 64
+// elements of a row are 128 bytes, 16-byte chunk c of row r at c ^ (r & 7), 64-element halves one after the other.
+#pragma once
+#include "attend.cuh"
+
+namespace ptk {
+
+constexpr int PR_THREADS = 512;
+constexpr int PR_ROWS = 256, PR_KEYS = 128;
+constexpr int PR_SLOTS = 4;
+constexpr u32 PR_POLLS = 1u << 22;           // polls of a wait before the CTA gives up (each may suspend for a while)
+
+template <int D>
+struct PromptShape {
+  static constexpr int TILE_BYTES = PR_KEYS * D * 2;                    // one K or V tile, one 128-row half of Q
+  static constexpr int SMEM = (2 + PR_SLOTS) * TILE_BYTES + 1024;       // + alignment
+};
+
+__device__ __forceinline__ void bar_init(u64* bar, u32 count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count) : "memory"); }
+__device__ __forceinline__ void bar_arrive(u64* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory"); }
+__device__ __forceinline__ bool bar_try(u64* bar, u32 parity) {
+  u32 ok;
+  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity) : "memory");
+  return ok != 0;
+}
+// false: this wait, or another one of the CTA, ran out
+__device__ __forceinline__ bool bar_wait(u64* bar, u32 parity, volatile int* gave_up) {
+  if (bar_try(bar, parity)) return true;
+  for (u32 i = 0; i < PR_POLLS; ++i) {
+    if (bar_try(bar, parity)) return true;
+    if (*gave_up) return false;
+  }
+  *gave_up = 1;
+  return false;
+}
+
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(u64* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+// 32 columns of this warp's 32 lanes, one row per thread
+__device__ __forceinline__ void tc_ld32(float (&v)[32], u32 addr) {
+  float* r = v;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]),
+                 "=f"(r[13]), "=f"(r[14]), "=f"(r[15]), "=f"(r[16]), "=f"(r[17]), "=f"(r[18]), "=f"(r[19]), "=f"(r[20]), "=f"(r[21]), "=f"(r[22]), "=f"(r[23]), "=f"(r[24]),
+                 "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
+               : "r"(addr) : "memory");
+}
+// values of a load may be used from here on (after tc_wait_ld): keeps the compiler from moving their uses above the wait
+__device__ __forceinline__ void tc_loaded(float (&v)[32]) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 8)
+    asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]), "+f"(v[i + 6]), "+f"(v[i + 7]));
+}
+__device__ __forceinline__ void tc_st32(u32 addr, const u32 (&r)[32]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+               ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+                 "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
+                 "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr) : "memory");
+}
+
+// Shared-memory operand descriptor: 128-byte swizzle; `lead` only matters where the operand is MN-major (bytes between its 64-element
+// halves), stride is 8 rows of 128 bytes.
+__device__ __forceinline__ u64 operand_desc(u32 addr, u32 lead_bytes) {
+  return (u64)((addr >> 4) & 0x3FFFu) | ((u64)((lead_bytes >> 4) & 0x3FFFu) << 16) | ((u64)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// Instruction descriptor of kind::f16: 32-bit accumulator, both operands fp16 or both bf16, M = 128
+__host__ __device__ constexpr u32 mma_desc(bool fp16, int N, bool b_mn_major) {
+  return (1u << 4) | ((fp16 ? 0u : 1u) << 7) | ((fp16 ? 0u : 1u) << 10) | ((b_mn_major ? 1u : 0u) << 16) | ((u32)(N >> 3) << 17) | ((u32)(128 >> 4) << 24);
+}
+__device__ __forceinline__ void mma_ss(u32 d, u64 a, u64 b, u32 desc, bool add) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"((u32)add) : "memory");
+}
+__device__ __forceinline__ void mma_ts(u32 d, u32 a, u64 b, u32 desc, bool add) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(desc), "r"((u32)add) : "memory");
+}
+__device__ __forceinline__ u64 pair(float lo, float hi) { return (u64)__float_as_uint(lo) | ((u64)__float_as_uint(hi) << 32); }
+__device__ __forceinline__ u64 fma_pair(u64 a, u64 b, u64 c) {
+  u64 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ u64 add_pair(u64 a, u64 b) {
+  u64 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float lo_of(u64 v) { return __uint_as_float((u32)v); }
+__device__ __forceinline__ float hi_of(u64 v) { return __uint_as_float((u32)(v >> 32)); }
+template <int R>
+__device__ __forceinline__ void regs_more() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
+template <int R>
+__device__ __forceinline__ void regs_fewer() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R)); }
+
+// byte of 16-byte chunk c of row r in an operand tile of 128 rows
+__device__ __forceinline__ u32 operand_at(int r, int c) { return (u32)((c >> 3) * (PR_KEYS * 128) + r * 128 + (((c & 7) ^ (r & 7)) * 16)); }
+
+__device__ __forceinline__ i64 prompt_tiles(const Attend& a, int r) {
+  const Req q = request(a, r);
+  return ((i64)q.fresh * a.group + PR_ROWS - 1) / PR_ROWS;
+}
+
+template <int FMT, bool QFP16, int D>
+__global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) {
+  constexpr bool PACKED = FMT == PTSTORE_KV_PACKED;
+  constexpr bool F16 = PACKED || FMT == PTSTORE_KV_FP16;
+  constexpr int TB = PromptShape<D>::TILE_BYTES, CPR = D / 8;           // bytes of a tile, 16-byte chunks of a row
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* const smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
+  __shared__ __align__(8) u64 b_q[2], b_full[PR_SLOTS], b_empty[PR_SLOTS], b_s[2], b_p[2], b_o[2], b_end;
+  __shared__ u32 s_tmem;
+  __shared__ int s_gave_up, s_any_bad, s_r, s_tile;
+  __shared__ i64 s_scan[PR_THREADS / 32];
+  __shared__ i64 s_row[2][PR_KEYS];          // byte offset of a key's row (4-bit: of its tile), -1: not there
+  __shared__ u32 s_valid[4][4];              // keys of a step that are there, by step & 3
+  __shared__ int s_bad[3][D];                // first key whose V holds NaN, +inf, -inf in column d, among keys that some rows do not see
+  __shared__ float s_qf[PR_ROWS];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+  // ---- which 256 rows: heads vary fastest; a request's tiles come last to first, the ones with most keys first
+  const int h = blockIdx.x % a.cache.heads;
+  const i64 index = blockIdx.x / a.cache.heads;
+  {
+    const int per_thread = (a.R + PR_THREADS - 1) / PR_THREADS;
+    const int rb = tid * per_thread < a.R ? tid * per_thread : a.R, re = rb + per_thread < a.R ? rb + per_thread : a.R;
+    i64 mine = 0;
+    for (int r = rb; r < re; ++r) mine += prompt_tiles(a, r);
+    i64 x = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const i64 y = __shfl_up_sync(FULL, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) s_scan[warp] = x;
+    if (tid == 0) { s_r = -1; s_gave_up = 0; s_any_bad = 0; }
+    __syncthreads();
+    i64 before = x - mine;
+    for (int w = 0; w < warp; ++w) before += s_scan[w];
+    if (index >= before && index < before + mine) {
+      i64 left = index - before;
+      int r = rb;
+      for (; r < re - 1; ++r) {
+        const i64 n = prompt_tiles(a, r);
+        if (left < n) break;
+        left -= n;
+      }
+      s_r = r;
+      s_tile = (int)(prompt_tiles(a, r) - 1 - left);
+    }
+    if (tid == 0) {
+      for (int i = 0; i < 2; ++i) { bar_init(&b_q[i], 128); bar_init(&b_s[i], 1); bar_init(&b_p[i], 128); bar_init(&b_o[i], 1); }
+      for (int i = 0; i < PR_SLOTS; ++i) { bar_init(&b_full[i], 128); bar_init(&b_empty[i], 1); }
+      bar_init(&b_end, 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    for (int i = tid; i < 3 * D; i += PR_THREADS) (&s_bad[0][0])[i] = 0x7FFFFFFF;
+    __syncthreads();
+  }
+  const int r = s_r;
+  if (r < 0) return;                          // a CTA beyond the last tile
+  const Req rq = request(a, r);
+  const int row_base = s_tile * PR_ROWS, rows = min(PR_ROWS, rq.fresh * a.group - row_base);
+  // keys the rows of each tile see (its last row), and the first row
+  auto keys_of = [&](int row) {
+    const i64 k = (i64)rq.pos0 + (row_base + row) / a.group + 1;
+    return k < 0 ? 0 : k > rq.keys ? rq.keys : (int)k;
+  };
+  const int keys0 = keys_of(min(rows, 128) - 1), keys1 = rows > 128 ? keys_of(rows - 1) : 0;
+  const int keys = max(keys0, keys1), all_see = keys_of(0);
+  const int steps[2] = {(keys0 + PR_KEYS - 1) / PR_KEYS, (keys1 + PR_KEYS - 1) / PR_KEYS};
+  const int n_steps = max(steps[0], steps[1]);
+  const u32 smem_q = smem_addr(smem), smem_kv = smem_q + 2 * TB;
+
+  if (warp == 12) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const u32 tmem = s_tmem;
+
+  if (warp >= 12) {
+    // ======== tensor instructions
+    regs_fewer<40>();
+    if (warp == 12 && lane == 0) {
+      constexpr u32 QK = mma_desc(F16, PR_KEYS, false), PV = mma_desc(F16, D, true);
+      auto wait = [&](u64* b, u32 parity) { return bar_wait(b, parity, &s_gave_up); };
+      auto slot_wait = [&](int op) { return wait(&b_full[op % PR_SLOTS], (op / PR_SLOTS) & 1); };
+      auto scores = [&](int w, int op) {
+        const u64 qa = operand_desc(smem_q + w * TB, 0), kb = operand_desc(smem_kv + (op % PR_SLOTS) * TB, 0);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {    // 16 elements: 32 bytes further in a row, or the next 64-element half
+          const u64 off = (u64)(((k >> 2) * (PR_KEYS * 128) + (k & 3) * 32) >> 4);
+          mma_ss(tmem + w * 128, qa + off, kb + off, QK, k > 0);
+        }
+        tc_commit(&b_s[w]);
+      };
+      auto values = [&](int w, int op, bool add) {
+        const u64 vb = operand_desc(smem_kv + (op % PR_SLOTS) * TB, PR_KEYS * 128);
+#pragma unroll
+        for (int k = 0; k < PR_KEYS / 16; ++k)   // 16 keys: 16 rows of 128 bytes; 8 columns of P
+          mma_ts(tmem + 256 + w * 128, tmem + w * 128 + k * 8, vb + (u64)((k * 16 * 128) >> 4), PV, add || k > 0);
+      };
+      bool ok = true;
+      for (int w = 0; w < 2 && ok; ++w)
+        if (steps[w] > 0) ok = wait(&b_q[w], 0);
+      if (ok && n_steps > 0) {
+        ok = slot_wait(0);
+        tc_fence_after();
+        if (ok) {
+          for (int w = 0; w < 2; ++w)
+            if (steps[w] > 0) scores(w, 0);
+          tc_commit(&b_empty[0]);
+        }
+      }
+      for (int j = 0; j < n_steps && ok; ++j) {
+        const int kop = 2 * (j + 1), vop = 2 * j + 1;
+        bool have_k = false;
+        ok = slot_wait(vop);
+        for (int w = 0; w < 2 && ok; ++w) {
+          if (j < steps[w]) {
+            ok = wait(&b_p[w], j & 1);
+            if (!ok) break;
+            tc_fence_after();
+            values(w, vop, j > 0);
+            if (j + 1 == steps[w]) tc_commit(&b_o[w]);
+          }
+          if (j + 1 < steps[w]) {
+            if (!have_k) { ok = slot_wait(kop); have_k = true; tc_fence_after(); }
+            if (ok) scores(w, kop);
+          }
+        }
+        if (ok) {
+          tc_commit(&b_empty[vop % PR_SLOTS]);
+          if (have_k) tc_commit(&b_empty[kop % PR_SLOTS]);
+        }
+      }
+      if (!ok) {                              // everything issued has ended before tensor memory is given back
+        tc_commit(&b_end);
+        for (u32 i = 0; i < PR_POLLS && !bar_try(&b_end, 0); ++i) {}
+      }
+    }
+    __syncwarp();
+  } else if (warp >= 8) {
+    // ======== K and V into the ring
+    regs_fewer<72>();
+    const int pt = tid - 256;
+    const int* table = a.tables + (i64)r * a.max_blocks;
+    const u32 B = a.cache.block_tokens;
+    bool bounds = false, ok = true;
+    // where key `pt` of a step lies
+    auto where = [&](int j) -> i64 {
+      const int key = j * PR_KEYS + pt;
+      if (key >= keys) return -1;
+      const u32 blk = (u32)key / B, in = (u32)key % B;
+      const u32 id = (u32)table[blk];
+      if (id >= a.cache.num_blocks) { bounds = true; return -1; }
+      const i64 base = (i64)((u64)id * a.cache.block_stride);
+      if (PACKED) return base + (i64)((u64)h * (B / TILE) + in / TILE) * tile_bytes(D);
+      return base + (i64)(((u64)in * a.cache.heads + h) * (D * 2));
+    };
+    auto wait_empty = [&](int op) { return op < PR_SLOTS || bar_wait(&b_empty[op % PR_SLOTS], ((op / PR_SLOTS) - 1) & 1, &s_gave_up); };
+    auto note_bad = [&](int d, int kind, int key) {
+      atomicMin(&s_bad[kind][d], key);
+      s_any_bad = 1;
+    };
+    if (!PACKED) {
+      // chunk pt % CPR of rows pt / CPR, pt / CPR + 128 / CPR, ...
+      constexpr int RPP = 128 / CPR;
+      const int c = pt % CPR, r0 = pt / CPR;
+      auto finish = [&](int op) {             // the copies of op have landed
+        if ((op & 1) && (op >> 1) * PR_KEYS + PR_KEYS > all_see) {
+          // keys that some of the rows do not see: a weight of zero would not hide an infinity or a NaN, so they are taken out here
+          // and put into the rows that see them at the end
+          unsigned char* t = smem + (2 + op % PR_SLOTS) * TB;
+          constexpr u32 EX = F16 ? 0x7C00u : 0x7F80u, MANT = F16 ? 0x03FFu : 0x007Fu;
+          for (int i = 0; i < CPR; ++i) {
+            const int n = i * RPP + r0, key = (op >> 1) * PR_KEYS + n;
+            if (key < all_see) continue;
+            unsigned short* p = reinterpret_cast<unsigned short*>(t + operand_at(n, c));
+            const uint4 v = *reinterpret_cast<const uint4*>(p);
+            const u32 w[4] = {v.x, v.y, v.z, v.w};
+            bool odd = false;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) odd |= (w[k] & EX) == EX || ((w[k] >> 16) & EX) == EX;
+            if (odd)
+              for (int k = 0; k < 8; ++k)
+                if ((p[k] & EX) == EX) {
+                  note_bad(c * 8 + k, (p[k] & MANT) ? 0 : (p[k] & 0x8000u) ? 2 : 1, key);
+                  p[k] = 0;
+                }
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        bar_arrive(&b_full[op % PR_SLOTS]);
+      };
+      i64 next = n_steps > 0 ? where(0) : -1;
+      for (int op = 0; op < 2 * n_steps && ok; ++op) {
+        const int j = op >> 1;
+        if (!(op & 1)) {
+          s_row[j & 1][pt] = next;
+          const u32 there = __ballot_sync(FULL, next >= 0);
+          if (lane == 0) s_valid[j & 3][warp - 8] = there;
+          if (j + 1 < n_steps) next = where(j + 1);
+          asm volatile("bar.sync 1, 128;" ::: "memory");
+        }
+        ok = wait_empty(op);
+        if (!ok) break;
+        const unsigned char* base = a.cache.base + (op & 1 ? a.cache.kv_stride : 0) + c * 16;
+        const u32 dst = smem_kv + (op % PR_SLOTS) * TB;
+#pragma unroll
+        for (int i = 0; i < CPR; ++i) {
+          const int n = i * RPP + r0;
+          const i64 off = s_row[j & 1][n];
+          cp_async16_or_zero(dst + operand_at(n, c), base + (off < 0 ? 0 : off), off >= 0);
+        }
+        cp_commit();
+        if (op >= 2) { cp_wait<2>(); finish(op - 2); }
+      }
+      if (ok) {
+        if (n_steps > 0) {
+          cp_wait<1>();
+          finish(2 * n_steps - 2);
+          cp_wait<0>();
+          finish(2 * n_steps - 1);
+        }
+      } else cp_wait<0>();
+    } else {
+      // one key per thread: its codes and scales are loaded one operand ahead, unpacked and stored as fp16.  Element order inside
+      // eight is 0 4 1 5 2 6 3 7, as the unpacking yields it: Q is stored likewise, and O's columns are put back at the end.
+      __align__(16) u32 code[D / 8];
+      u32 scale[D / 64];
+      bool has = false;
+      auto load = [&](int op) {
+        const int j = op >> 1;
+        const bool is_v = op & 1;
+        const i64 off = where(j);
+        has = off >= 0;
+        if (!is_v) {
+          const u32 there = __ballot_sync(FULL, has);
+          if (lane == 0) s_valid[j & 3][warp - 8] = there;
+        }
+        if (has) {
+          const int n = (int)((u32)(j * PR_KEYS + pt) % B % TILE);
+          const unsigned char* t = a.cache.base + (is_v ? a.cache.kv_stride : 0) + off;
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) *reinterpret_cast<uint4*>(code + 4 * c) = __ldg(reinterpret_cast<const uint4*>(t + code_place(D, n, c) * 16));
+          if (is_v) {
+#pragma unroll
+            for (int w = 0; w < D / 64; ++w) {
+              scale[w] = 0;
+#pragma unroll
+              for (int b = 0; b < 4; ++b) scale[w] |= (u32)__ldg(t + scale_at(D, true, n, 4 * w + b)) << (8 * b);
+            }
+          } else {
+#pragma unroll
+            for (int w = 0; w < D / 64; ++w) scale[w] = __ldg(reinterpret_cast<const u32*>(t + scale_at(D, false, n, 4 * w)));
+          }
+        }
+      };
+      if (n_steps > 0) load(0);
+      for (int op = 0; op < 2 * n_steps && ok; ++op) {
+        u32 cur[D / 8], sc[D / 64];
+        const bool cur_has = has;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) cur[i] = code[i];
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) sc[i] = scale[i];
+        if (op + 1 < 2 * n_steps) load(op + 1);
+        ok = wait_empty(op);
+        if (!ok) break;
+        const int key = (op >> 1) * PR_KEYS + pt;
+        if ((op & 1) && cur_has && key >= all_see) {
+#pragma unroll
+          for (int g = 0; g < D / 16; ++g) {
+            const u32 sh = 8 * (g & 3);
+            if (((sc[g >> 2] >> sh) & 0x7Fu) == 0x7Fu) {
+              for (int k = 0; k < 16; ++k) note_bad(16 * g + k, 0, key);
+              sc[g >> 2] &= ~(0xFFu << sh);
+            }
+          }
+        }
+        unsigned char* t = smem + (2 + op % PR_SLOTS) * TB;
+#pragma unroll
+        for (int g = 0; g < D / 16; ++g) {    // a scale group: two words, two 16-byte chunks of the operand
+          const u32 two = (sc[g >> 2] >> (8 * (g & 3))) & 0xFFu;
+          const Deq d = deq_of(e4m3x2_to_half2(two | (two << 8)));
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            u32 o[4];
+            deq4(cur[2 * g + w], d, o);
+            *reinterpret_cast<uint4*>(t + operand_at(pt, 2 * g + w)) = cur_has ? make_uint4(o[0], o[1], o[2], o[3]) : make_uint4(0, 0, 0, 0);
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        bar_arrive(&b_full[op % PR_SLOTS]);
+      }
+    }
+    if (bounds && a.status) atomicOr(a.status, PTSTORE_S_BOUNDS);
+  } else {
+    // ======== softmax of tile w
+    regs_more<200>();
+    const int w = warp >> 2, t = tid & 127, row = w * 128 + t;
+    // its half of Q: chunk t % CPR of rows t / CPR, ...; the sign of the softmax scale goes into Q
+    {
+      constexpr int RPP = 128 / CPR;
+      const int c = t % CPR;
+      const bool flip = a.scale2 < 0.0f;
+#pragma unroll 4
+      for (int i = 0; i < CPR; ++i) {
+        const int n = i * RPP + t / CPR, gr = w * 128 + n;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (gr < rows) {
+          const int fr = (row_base + gr) / a.group, hq = h * a.group + (row_base + gr) % a.group;
+          v = *reinterpret_cast<const uint4*>(a.q + 2 * ((i64)(rq.row0 + fr) * a.q_token + (i64)hq * a.q_head + c * 8));
+        }
+        u32 x[4] = {v.x, v.y, v.z, v.w};
+        float factor = 1.0f;
+        if (PACKED && !QFP16) {
+          // bf16 rows as fp16, scaled by a power of two so that the largest element is in [1, 2): elements below 2^-14 of it lose
+          // at most 2^-25 of it, all others nothing
+          float amax = 0.0f;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float2 f = unpack2<false>(x[k]);
+            amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));
+          }
+#pragma unroll
+          for (int o = 1; o < CPR; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(FULL, amax, o));
+          int e = amax > 0.0f ? (int)(__float_as_uint(amax) >> 23) - 127 : 0;
+          e = e < -126 ? -126 : e > 126 ? 126 : e;
+          factor = __uint_as_float((u32)(127 + e) << 23);
+          const float down = __uint_as_float((u32)(127 - e) << 23);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float2 f = unpack2<false>(x[k]);
+            x[k] = pack2<true>(f.x * down, f.y * down);
+          }
+        }
+        if (flip) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) x[k] ^= 0x80008000u;
+        }
+        if (PACKED) {                         // element order 0 4 1 5 2 6 3 7
+          const u32 y[4] = {__byte_perm(x[0], x[2], 0x5410), __byte_perm(x[0], x[2], 0x7632), __byte_perm(x[1], x[3], 0x5410), __byte_perm(x[1], x[3], 0x7632)};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) x[k] = y[k];
+        }
+        *reinterpret_cast<uint4*>(smem + w * TB + operand_at(n, c)) = make_uint4(x[0], x[1], x[2], x[3]);
+        if (c == 0) s_qf[gr] = factor;
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      bar_arrive(&b_q[w]);
+      if (w == 0) asm volatile("bar.sync 2, 128;" ::: "memory");
+      else asm volatile("bar.sync 3, 128;" ::: "memory");
+    }
+    // scale2 as a positive number: of zero, the smallest that keeps masked scores at minus infinity
+    const float scale2 = fmaxf(fabsf(a.scale2) * s_qf[row], 0x1p-126f);
+    const int see = row < rows ? keys_of(row) : 0;
+    const u32 lane_base = (u32)(32 * (warp & 3)) << 16;
+    const u32 ts = tmem + lane_base + w * 128, to = tmem + lane_base + 256 + w * 128;
+    float m = -INFINITY, l = 0.0f;
+    bool ok = true;
+    for (int j = 0; j < steps[w]; ++j) {
+      ok = bar_wait(&b_s[w], j & 1, &s_gave_up);
+      if (__any_sync(FULL, !ok)) { ok = false; break; }
+      tc_fence_after();
+      float s[4][32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tc_ld32(s[c], ts + 32 * c);
+      tc_wait_ld();
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tc_loaded(s[c]);
+      u32 there[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) there[c] = s_valid[j & 3][c];
+      const int k0 = j * PR_KEYS;
+      if (k0 + PR_KEYS > all_see || (there[0] & there[1] & there[2] & there[3]) != FULL) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int left = see - k0 - 32 * c;             // keys of this chunk the row sees
+          const u32 mask = there[c] & (left >= 32 ? FULL : left <= 0 ? 0u : (1u << left) - 1u);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) s[c][i] = (mask >> i) & 1 ? s[c][i] : -INFINITY;
+        }
+      }
+      float x[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        x[c] = s[c][0];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) x[c] = fmaxf(x[c], s[c][i]);
+      }
+      const float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * scale2;
+      // the reference moves only when a weight would pass 2^8
+      const bool move = top > m + 8.0f || (m == -INFINITY && top > m);
+      if (__any_sync(FULL, move)) {
+        const float f = move ? exp2_fast(m - top) : 1.0f;
+        if (move) { m = top; l *= f; }
+        if (j > 0) {
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            float o[32];
+            tc_ld32(o, to + c);
+            tc_wait_ld();
+            tc_loaded(o);
+            u32 scaled[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) scaled[i] = __float_as_uint(o[i] * f);
+            tc_st32(to + c, scaled);
+          }
+        }
+      }
+      const float ref = m == -INFINITY ? 0.0f : m;
+      const u64 sc2 = pair(scale2, scale2), neg = pair(-ref, -ref);
+      u64 sum[2] = {0, 0};
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        u32 p[32];
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const u64 e = fma_pair(pair(s[2 * half + c][i], s[2 * half + c][i + 1]), sc2, neg);
+            const float e0 = exp2_fast(lo_of(e)), e1 = exp2_fast(hi_of(e));
+            sum[c] = add_pair(sum[c], pair(e0, e1));
+            p[16 * c + i / 2] = pack2<F16>(e0, e1);
+          }
+        tc_st32(ts + 32 * half, p);
+      }
+      const u64 both = add_pair(sum[0], sum[1]);
+      l += lo_of(both) + hi_of(both);
+      tc_wait_st();
+      tc_fence_before();
+      bar_arrive(&b_p[w]);
+    }
+    // ---- output
+    if (ok && steps[w] > 0) {
+      ok = bar_wait(&b_o[w], 0, &s_gave_up);
+      ok = !__any_sync(FULL, !ok);
+      tc_fence_after();
+    }
+    if (ok) {
+      const float f = l == 0.0f ? 0.0f : a.v_factor / l;
+      const bool live = row < rows;
+      const int fr = live ? (row_base + row) / a.group : 0, hq = live ? h * a.group + (row_base + row) % a.group : 0;
+      unsigned char* dst = a.out + 2 * ((i64)(rq.row0 + fr) * a.o_token + (i64)hq * a.o_head);
+#pragma unroll 1
+      for (int c = 0; c < D; c += 32) {
+        float o[32];
+        if (steps[w] > 0) {
+          tc_ld32(o, to + c);
+          tc_wait_ld();
+          tc_loaded(o);
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) o[i] = l == 0.0f ? 0.0f : o[i] * f;
+        if (PACKED) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 8) {
+            const float v[8] = {o[i], o[i + 1], o[i + 2], o[i + 3], o[i + 4], o[i + 5], o[i + 6], o[i + 7]};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[i + (k >> 1) + 4 * (k & 1)] = v[k];
+          }
+        }
+        if (s_any_bad) {
+          for (int i = 0; i < 32; ++i) {
+            const bool nan = s_bad[0][c + i] < see, pos = s_bad[1][c + i] < see, neg = s_bad[2][c + i] < see;
+            if (nan || (pos && neg)) o[i] = NAN;
+            else if (pos) o[i] = o[i] + INFINITY;
+            else if (neg) o[i] = o[i] - INFINITY;
+          }
+        }
+        if (live) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 8)
+            *reinterpret_cast<uint4*>(dst + 2 * (c + i)) = make_uint4(pack2<QFP16>(o[i], o[i + 1]), pack2<QFP16>(o[i + 2], o[i + 3]), pack2<QFP16>(o[i + 4], o[i + 5]),
+                                                                      pack2<QFP16>(o[i + 6], o[i + 7]));
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 12) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (lane == 0 && s_gave_up && a.status) atomicOr(a.status, PTSTORE_S_TIMEOUT);
+  }
+}
+
+}  // namespace ptk
