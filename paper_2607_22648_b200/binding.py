@@ -5,6 +5,7 @@ Importing this module loads the library and raises if it has not been built (the
 """
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -119,11 +120,11 @@ def _load():
     lib.ptstore_kv_chunk_bytes.argtypes = [u32, u32, u32, u32]
     lib.ptstore_assign_blocks.argtypes = [vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp]
     lib.ptstore_map_slots.argtypes = [vp, vp, i32, i32, i32, vp, i32, i32, i64, vp, vp, vp, vp, vp]
-    lib.ptstore_kv_write.argtypes = [vp, i64, i64, vp, i64, i64, i64, u32, vp, C.POINTER(KvCache), vp, vp]
-    lib.ptstore_kv_read.argtypes = [C.POINTER(KvCache), vp, i64, u32, vp, i64, i64, vp, i64, i64, vp, vp]
+    lib.ptstore_kv_write.argtypes = [vp, i64, i64, vp, i64, i64, i64, u32, vp, vp, vp, vp]
+    lib.ptstore_kv_read.argtypes = [vp, vp, i64, u32, vp, i64, i64, vp, i64, i64, vp, vp]
     lib.ptstore_attend_workspace_bytes.restype = u64
     lib.ptstore_attend_workspace_bytes.argtypes = [u32]
-    lib.ptstore_attend.argtypes = [C.POINTER(Attend), C.POINTER(KvCache), vp, u64, vp, vp]
+    lib.ptstore_attend.argtypes = [vp, vp, vp, u64, vp, vp]
     lib.ptstore_strerror.restype = C.c_char_p
     lib.ptstore_strerror.argtypes = [C.c_int]
     return lib
@@ -190,7 +191,14 @@ def fetch_static(hbm_pool, hbm_blocks, layers, chunk_bytes, ids, matched, cache,
 
 
 # ---- operators around the paged cache: no store handle, work on the stream and device that are current -------------------------------
+# A decode step calls these once per layer with kernels of ten microseconds, so the checks are written out flat and the C structs
+# are packed as bytes.
 _KV_DTYPES = {torch.bfloat16: KV_BF16, torch.float16: KV_FP16}
+_KV_CACHE = struct.Struct("PQQIIIIIIff")
+_ATTEND = struct.Struct("IIPqqPqqPPPiiiiif")
+assert _KV_CACHE.size == C.sizeof(KvCache) and _ATTEND.size <= C.sizeof(Attend)
+_ATTEND_SIZE = C.sizeof(Attend)
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _check(rc, what):
@@ -198,34 +206,44 @@ def _check(rc, what):
         raise PTStoreError(rc, what)
 
 
-def _want(t, dtype, shape, what):
-    """An array argument of the operators: a contiguous tensor of this type on the current device (or pinned); shape None matches any size."""
-    ok = t is not None and t.dtype == dtype and t.dim() == len(shape) and all(n is None or n == m for n, m in zip(shape, t.shape))
-    if not ok or not t.is_contiguous():
-        raise ValueError("%s: needs a contiguous %s tensor of shape %s" % (what, dtype, [n if n is not None else "any" for n in shape]))
-    _here(t, what)
+def _vec(t, dtype, n, dev, what):
+    """n contiguous elements on the current device, or pinned; returns their address."""
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s: needs a contiguous %s vector of %d elements" % (what, dtype, n))
+    if t.get_device() != dev:
+        _elsewhere(t, what)
+    return t.data_ptr()
 
 
-def _here(t, what):
+def _table(t, R, dev, what):
+    if t.dtype is not torch.int32 or t.dim() != 2 or t.shape[0] != R or not t.is_contiguous():
+        raise ValueError("%s: needs a contiguous int32 tensor of %d rows" % (what, R))
+    if t.get_device() != dev:
+        _elsewhere(t, what)
+    return t.data_ptr()
+
+
+def _elsewhere(t, what):
     if t.is_cuda:
-        if t.device.index != torch.cuda.current_device():
-            raise ValueError("%s: is on another device than the current one" % what)
-    elif not t.is_pinned():
+        raise ValueError("%s: is on another device than the current one" % what)
+    if not t.is_pinned():
         raise ValueError("%s: needs device or pinned memory" % what)
 
 
-def _rows(t, layout, heads, what, tokens=None):
-    """[tokens][heads][dim] rows of 16-bit elements, any token and head strides."""
-    if t is None or t.dim() != 3 or t.dtype not in _KV_DTYPES or tuple(t.shape[1:]) != (heads, layout.dim) or t.stride(2) != 1:
-        raise ValueError("%s: needs a bfloat16 or float16 tensor [tokens, %d, %d], contiguous along the last axis" % (what, heads, layout.dim))
-    if tokens is not None and t.shape[0] != tokens:
-        raise ValueError("%s: needs %d rows" % (what, tokens))
-    _here(t, what)
+def _rows(t, heads, dim, n, dtype, dev, what):
+    """[n][heads][dim] rows of 16-bit elements, any token and head strides; returns the address."""
+    if t.dtype is not dtype or t.shape != (n, heads, dim) or t.stride(2) != 1:
+        raise ValueError("%s: needs a %s tensor [%d, %d, %d], contiguous along the last axis" % (what, dtype, n, heads, dim))
+    if t.get_device() != dev:
+        _elsewhere(t, what)
+    return t.data_ptr()
 
 
-def _status_word(status):
-    if status is not None:
-        _want(status, torch.int32, [1], "status")
+def _kv_dtype(t, what):
+    code = _KV_DTYPES.get(t.dtype)
+    if code is None or t.dim() != 3:
+        raise ValueError("%s: needs a bfloat16 or float16 tensor [tokens, heads, dim]" % what)
+    return code
 
 
 class KVLayout:
@@ -243,39 +261,38 @@ class KVLayout:
         """dim and elem_bytes for a PTStore that holds chunks of this layout (the store moves opaque bytes)."""
         return {"dim": self.dim * 9 // 16, "elem_bytes": 1} if self.format == KV_PACKED else {"dim": self.dim, "elem_bytes": 2}
 
-    def of(self, cache, layer):
-        """The C descriptor of one layer of a PagedKV."""
+    def of(self, cache, layer, dev=None):
+        """The C descriptor of one layer of a PagedKV, as bytes."""
         if not 0 <= layer < len(cache.tensors):
             raise ValueError("layer %d of a cache of %d layers" % (layer, len(cache.tensors)))
         t = cache.tensors[layer]
-        _here(t, "cache")
-        size = t.element_size()
-        if t.dim() < 2 or t.shape[0] != 2 or (t.numel() and t[0, 0].numel() * size != self.chunk_bytes) or not t[0, 0].is_contiguous():
+        if t.get_device() != (torch.cuda.current_device() if dev is None else dev):
+            _elsewhere(t, "cache")
+        size, shape, stride = t.element_size(), t.shape, t.stride()
+        inner = 1
+        for n, s in zip(shape[:1:-1], stride[:1:-1]):            # the axes of a chunk, last first
+            if s != inner and n != 1:
+                inner = 0
+            inner *= n
+        if len(shape) < 2 or shape[0] != 2 or inner * size != self.chunk_bytes:
             raise ValueError("cache: needs [2, blocks, chunk] with contiguous chunks of %d bytes" % self.chunk_bytes)
-        return KvCache(t.data_ptr(), t.stride(0) * size, t.stride(1) * size, t.shape[1], self.block_tokens, self.heads, self.dim, self.format, 0,
-                       self.k_scale, self.v_scale)
+        return _KV_CACHE.pack(t.data_ptr(), stride[0] * size, stride[1] * size, shape[1], self.block_tokens, self.heads, self.dim, self.format, 0,
+                              self.k_scale, self.v_scale)
 
 
 def assign_blocks(lengths, held, block_tables, free_ids, free_count, block_tokens, held_out=None, free_count_out=None, status=None):
     """ptstore_assign_blocks: grows and shrinks block-table rows to the lengths, from and to the stack free_ids[:free_count].  held (None:
     nothing held yet) and free_count are updated in place unless held_out / free_count_out are given.  Returns (held, free_count)."""
-    R = lengths.numel()
-    _want(lengths, torch.int32, [R], "lengths")
-    _want(block_tables, torch.int32, [R, None], "block_tables")
-    _want(free_ids, torch.int32, [None], "free_ids")
-    _want(free_count, torch.int32, [1], "free_count")
-    if held is not None:
-        _want(held, torch.int32, [R], "held")
+    dev, i32, R = torch.cuda.current_device(), torch.int32, lengths.numel()
     if held_out is None:
         held_out = held if held is not None else torch.empty_like(lengths)
     if free_count_out is None:
         free_count_out = free_count
-    _want(held_out, torch.int32, [R], "held_out")
-    _want(free_count_out, torch.int32, [1], "free_count_out")
-    _status_word(status)
-    _check(lib.ptstore_assign_blocks(_ptr(lengths), _ptr(held), R, block_tokens, _ptr(block_tables), block_tables.shape[1], _ptr(free_ids),
-                                     free_ids.numel(), _ptr(free_count), _ptr(held_out), _ptr(free_count_out), _ptr(status), _stream()),
-           "ptstore_assign_blocks")
+    _check(lib.ptstore_assign_blocks(_vec(lengths, i32, R, dev, "lengths"), None if held is None else _vec(held, i32, R, dev, "held"), R, block_tokens,
+                                     _table(block_tables, R, dev, "block_tables"), block_tables.shape[1], _vec(free_ids, i32, free_ids.numel(), dev, "free_ids"),
+                                     free_ids.numel(), _vec(free_count, i32, 1, dev, "free_count"), _vec(held_out, i32, R, dev, "held_out"),
+                                     _vec(free_count_out, i32, 1, dev, "free_count_out"), None if status is None else _vec(status, i32, 1, dev, "status"),
+                                     _raw_stream(dev)), "ptstore_assign_blocks")
     return held_out, free_count_out
 
 
@@ -283,57 +300,43 @@ def map_slots(lengths, done, block_tables, block_tokens, max_tokens, done_unit=1
               status=None):
     """ptstore_map_slots: the new tokens of a batch.  done (tokens, times done_unit; None: none) are in the cache already; after a lookup
     pass its matched lengths with done_unit=block_tokens, min_new=1.  Returns (token_offsets [R+1], slots int64 [max_tokens], positions)."""
-    R = lengths.numel()
-    _want(lengths, torch.int32, [R], "lengths")
-    if done is not None:
-        _want(done, torch.int32, [R], "done")
-    _want(block_tables, torch.int32, [R, None], "block_tables")
-    dev = lengths.device if lengths.is_cuda else torch.device("cuda", torch.cuda.current_device())
+    dev, i32, R = torch.cuda.current_device(), torch.int32, lengths.numel()
+    where = block_tables.device if block_tables.is_cuda else torch.device("cuda", dev)
     if token_offsets is None:
-        token_offsets = torch.empty(R + 1, dtype=torch.int32, device=dev)
+        token_offsets = torch.empty(R + 1, dtype=i32, device=where)
     if slots is None:
-        slots = torch.empty(max_tokens, dtype=torch.int64, device=dev)
+        slots = torch.empty(max_tokens, dtype=torch.int64, device=where)
     if positions is None:
-        positions = torch.empty(max_tokens, dtype=torch.int32, device=dev)
-    _want(token_offsets, torch.int32, [R + 1], "token_offsets")
-    _want(slots, torch.int64, [max_tokens], "slots")
-    _want(positions, torch.int32, [max_tokens], "positions")
-    _status_word(status)
-    _check(lib.ptstore_map_slots(_ptr(lengths), _ptr(done), done_unit, min_new, R, _ptr(block_tables), block_tables.shape[1], block_tokens,
-                                 max_tokens, _ptr(token_offsets), _ptr(slots), _ptr(positions), _ptr(status), _stream()), "ptstore_map_slots")
+        positions = torch.empty(max_tokens, dtype=i32, device=where)
+    _check(lib.ptstore_map_slots(_vec(lengths, i32, R, dev, "lengths"), None if done is None else _vec(done, i32, R, dev, "done"), done_unit, min_new, R,
+                                 _table(block_tables, R, dev, "block_tables"), block_tables.shape[1], block_tokens, max_tokens,
+                                 _vec(token_offsets, i32, R + 1, dev, "token_offsets"), _vec(slots, torch.int64, max_tokens, dev, "slots"),
+                                 _vec(positions, i32, max_tokens, dev, "positions"), None if status is None else _vec(status, i32, 1, dev, "status"),
+                                 _raw_stream(dev)), "ptstore_map_slots")
     return token_offsets, slots, positions
 
 
 def kv_write(layout, cache, layer, k, v, slots, status=None):
     """ptstore_kv_write: rows k, v [tokens, heads, dim] into one layer of the paged cache at `slots` (int64; -1 skips a row)."""
-    desc = layout.of(cache, layer)
-    _want(slots, torch.int64, [None], "slots")
-    n = slots.numel()
-    _rows(k, layout, layout.heads, "k", n)
-    _rows(v, layout, layout.heads, "v", n)
-    if v.dtype != k.dtype:
-        raise ValueError("k and v: need one type")
-    _status_word(status)
-    _check(lib.ptstore_kv_write(_ptr(k), k.stride(0), k.stride(1), _ptr(v), v.stride(0), v.stride(1), n, _KV_DTYPES[k.dtype], _ptr(slots),
-                                C.byref(desc), _ptr(status), _stream()), "ptstore_kv_write")
+    dev, n, code = torch.cuda.current_device(), slots.numel(), _kv_dtype(k, "k")
+    _check(lib.ptstore_kv_write(_rows(k, layout.heads, layout.dim, n, k.dtype, dev, "k"), k.stride(0), k.stride(1),
+                                _rows(v, layout.heads, layout.dim, n, k.dtype, dev, "v"), v.stride(0), v.stride(1), n, code,
+                                _vec(slots, torch.int64, n, dev, "slots"), layout.of(cache, layer, dev),
+                                None if status is None else _vec(status, torch.int32, 1, dev, "status"), _raw_stream(dev)), "ptstore_kv_write")
 
 
 def kv_read(layout, cache, layer, slots, dtype, k=None, v=None, status=None):
     """ptstore_kv_read: the values at `slots` as rows [tokens, heads, dim]; rows whose slot is -1 are left as they were.  Returns (k, v)."""
-    desc = layout.of(cache, layer)
-    _want(slots, torch.int64, [None], "slots")
-    n = slots.numel()
+    dev, n = torch.cuda.current_device(), slots.numel()
     if k is None:
-        k = torch.empty((n, layout.heads, layout.dim), dtype=dtype, device=cache.tensors[layer].device)
+        k = torch.empty((n, layout.heads, layout.dim), dtype=dtype, device=torch.device("cuda", dev))
     if v is None:
         v = torch.empty_like(k)
-    _rows(k, layout, layout.heads, "k", n)
-    _rows(v, layout, layout.heads, "v", n)
-    if k.dtype != dtype or v.dtype != dtype:
-        raise ValueError("k and v: need the type asked for")
-    _status_word(status)
-    _check(lib.ptstore_kv_read(C.byref(desc), _ptr(slots), n, _KV_DTYPES[dtype], _ptr(k), k.stride(0), k.stride(1), _ptr(v), v.stride(0), v.stride(1),
-                               _ptr(status), _stream()), "ptstore_kv_read")
+    code = _kv_dtype(k, "k")
+    _check(lib.ptstore_kv_read(layout.of(cache, layer, dev), _vec(slots, torch.int64, n, dev, "slots"), n, code,
+                               _rows(k, layout.heads, layout.dim, n, dtype, dev, "k"), k.stride(0), k.stride(1),
+                               _rows(v, layout.heads, layout.dim, n, dtype, dev, "v"), v.stride(0), v.stride(1),
+                               None if status is None else _vec(status, torch.int32, 1, dev, "status"), _raw_stream(dev)), "ptstore_kv_read")
     return k, v
 
 
@@ -349,29 +352,22 @@ def attend(layout, cache, layer, q, token_offsets, lengths, block_tables, max_ne
     """ptstore_attend: causal attention of the new tokens q [tokens, num_heads, dim] over the paged cache (which holds their own K/V
     already).  Request r owns rows token_offsets[r] .. token_offsets[r+1]-1 and lengths[r] tokens of cache; max_new (host) is at least the
     rows of any request.  workspace: from attend_workspace (a program that calls often keeps one per stream).  Returns out."""
-    desc = layout.of(cache, layer)
-    if q is None or q.dim() != 3:
-        raise ValueError("q: needs [tokens, num_heads, dim]")
-    T, heads = q.shape[0], q.shape[1]
-    _rows(q, layout, heads, "q")
-    R = lengths.numel()
-    _want(lengths, torch.int32, [R], "lengths")
-    _want(token_offsets, torch.int32, [R + 1], "token_offsets")
-    _want(block_tables, torch.int32, [R, None], "block_tables")
+    dev, i32, code = torch.cuda.current_device(), torch.int32, _kv_dtype(q, "q")
+    R, (T, heads, dim) = lengths.numel(), q.shape
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _rows(out, layout, heads, "out", T)
-    if out.dtype != q.dtype:
-        raise ValueError("out: needs the type of q")
+        out = torch.empty((T, heads, dim), dtype=q.dtype, device=q.device)
     if workspace is None:
         workspace = attend_workspace(layout)
-    _here(workspace, "workspace")
-    _status_word(status)
-    args = Attend(C.sizeof(Attend), _KV_DTYPES[q.dtype], q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1),
-                  token_offsets.data_ptr(), lengths.data_ptr(), block_tables.data_ptr(), R, block_tables.shape[1], heads, T, max_new,
-                  layout.dim ** -0.5 if scale is None else scale)
-    _check(lib.ptstore_attend(C.byref(args), C.byref(desc), _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(status), _stream()),
-           "ptstore_attend")
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace: needs contiguous memory on the current device")
+    q_stride, o_stride = q.stride(), out.stride()
+    args = _ATTEND.pack(_ATTEND_SIZE, code, _rows(q, heads, layout.dim, T, q.dtype, dev, "q"), q_stride[0], q_stride[1],
+                        _rows(out, heads, layout.dim, T, q.dtype, dev, "out"), o_stride[0], o_stride[1],
+                        _vec(token_offsets, i32, R + 1, dev, "token_offsets"), _vec(lengths, i32, R, dev, "lengths"),
+                        _table(block_tables, R, dev, "block_tables"), R, block_tables.shape[1], heads, T, max_new,
+                        layout.dim ** -0.5 if scale is None else scale)
+    _check(lib.ptstore_attend(args, layout.of(cache, layer, dev), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                              None if status is None else _vec(status, i32, 1, dev, "status"), _raw_stream(dev)), "ptstore_attend")
     return out
 
 

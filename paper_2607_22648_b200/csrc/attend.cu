@@ -27,6 +27,7 @@ template <int FMT, bool QFP16, int D, int NT>
 int launch_split(const Attend& a, int sms, cudaStream_t s) {
   using Shape = SplitShape<FMT, D>;
   static_assert(Shape::RING >= SP_WARPS * 8 * NT * (D + 4) * 4, "the ring holds the warps' sums at the end of an item");
+  static_assert(Shape::RING >= MAX_SMS * (NT == 1 ? SP_CTAS : 2) * 8 * NT * 8, "and the maxima and sums of an item's parts when they are joined");
   auto* kernel = attend_split_kernel<FMT, QFP16, D, NT>;
   // set on every call: the setting belongs to the current device
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::RING) != cudaSuccess) { (void)cudaGetLastError(); return PTSTORE_E_CUDA; }

@@ -27,7 +27,7 @@ template <int FMT, int D>
 struct SplitShape {
   static constexpr bool PACKED = FMT == PTSTORE_KV_PACKED;
   static constexpr int STAGE = PACKED ? 2 * tile_bytes(D) : 2 * TILE * D * 2;      // K tile, V tile
-  static constexpr int STAGES = PACKED ? 6 : 2 * (128 / D);
+  static constexpr int STAGES = (PACKED ? 6 : 2) * (128 / D);
   static constexpr int STEP = PACKED ? 2 : 1;                                      // tiles per softmax step
   static constexpr int RING = SP_WARPS * STAGES * STAGE;
 };
@@ -597,28 +597,40 @@ __global__ void __launch_bounds__(SP_THREADS, NT == 1 ? SP_CTAS : 2) attend_spli
         s_last = last;
       }
       __syncthreads();
-      write = s_last != 0;
-      if (write && row < rows) {
+      write = false;
+      if (s_last) {
+        // all parts are there: maxima and sums into shared memory first, then the weighted sums with many loads in flight
         __threadfence();
-        top = -INFINITY;
-        for (i64 c = first_cta; c <= last_cta; ++c) top = fmaxf(top, __ldcg(parts + (2 * c + (c == first_cta ? 1 : 0)) * PF + NQ * D + row));
-        sum = 0.0f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = 0.0f;
-#pragma unroll 4
-        for (i64 c = first_cta; c <= last_cta; ++c) {
-          const float* p = parts + (2 * c + (c == first_cta ? 1 : 0)) * PF;
-          const float mc = __ldcg(p + NQ * D + row), lc = __ldcg(p + NQ * D + NQ + row);
-          const float f = mc == -INFINITY ? 1.0f : exp2_fast(mc - top);     // nothing seen: sums of zero (or NaN)
-          sum += lc * f;
-#pragma unroll
-          for (int e = 0; e < E; e += 4) {
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(p + row * D + e0 + e));
-            acc[e] += v.x * f;
-            acc[e + 1] += v.y * f;
-            acc[e + 2] += v.z * f;
-            acc[e + 3] += v.w * f;
+        const int n_parts = (int)(last_cta - first_cta) + 1;
+        float* s_pm = reinterpret_cast<float*>(smem);
+        float* s_pl = s_pm + n_parts * rows;
+        auto part = [&](int c) { return parts + (2 * (first_cta + c) + (c == 0 ? 1 : 0)) * PF; };
+        for (int i = tid; i < n_parts * rows; i += SP_THREADS) {
+          const float* p = part(i / rows) + NQ * D + i % rows;
+          s_pm[i] = __ldcg(p);
+          s_pl[i] = __ldcg(p + NQ);
+        }
+        __syncthreads();
+        for (int i = tid; i < rows * (D / 4); i += SP_THREADS) {
+          const int rw = i / (D / 4), e = (i % (D / 4)) * 4;
+          float high = -INFINITY, all = 0.0f;
+          for (int c = 0; c < n_parts; ++c) high = fmaxf(high, s_pm[c * rows + rw]);
+          float4 o4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+          for (int c = 0; c < n_parts; ++c) {
+            const float mc = s_pm[c * rows + rw];
+            const float f = mc == -INFINITY ? 1.0f : exp2_fast(mc - high);  // nothing seen: sums of zero (or NaN)
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(part(c) + rw * D + e));
+            all += s_pl[c * rows + rw] * f;
+            o4.x += v.x * f;
+            o4.y += v.y * f;
+            o4.z += v.z * f;
+            o4.w += v.w * f;
           }
+          const float f = all == 0.0f ? 0.0f : a.v_factor / all;
+          const int fr = (row_base + rw) / a.group, hq = h * a.group + (row_base + rw) % a.group;
+          *reinterpret_cast<uint2*>(a.out + 2 * ((i64)(rq.row0 + fr) * a.o_token + (i64)hq * a.o_head + e)) =
+              make_uint2(pack2<QFP16>(o4.x * f, o4.y * f), pack2<QFP16>(o4.z * f, o4.w * f));
         }
       }
     }

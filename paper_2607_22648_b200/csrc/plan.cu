@@ -3,8 +3,8 @@
 //
 // Both are prefix sums over the requests followed by a flat pass over what moves (blocks, tokens), and both are latency bound:
 // a few kilobytes to a few megabytes against a launch, two or three dependent memory round trips and a block-wide scan.  So
-// each is ONE launch in which every CTA scans all requests for itself (16,384 of them per step, 16 consecutive ones per
-// thread), and the entries that move are dealt out evenly and find their request by a binary search in shared memory.
+// each is ONE launch in which every CTA scans all requests for itself (16,384 of them per step, up to 16 per
+// thread, both sums of an assignment in one 64-bit value), and the entries that move are dealt out evenly and find their request by a binary search in shared memory.
 // B200, plan of one decode step of 64 requests / of 16,384 requests with 0.5 M new tokens: see the table of measurements.
 #include <cuda_runtime.h>
 #include <limits.h>
@@ -14,9 +14,10 @@
 namespace {
 
 typedef long long i64;
+typedef unsigned long long u64;
 
 constexpr int THREADS = 1024;
-constexpr int ITEMS = 16;                    // consecutive requests of one thread
+constexpr int ITEMS = 16;                    // requests of one thread
 constexpr int CHUNK = THREADS * ITEMS;       // requests scanned per step
 constexpr int CLUSTER = 8;                   // CTAs of an assignment (the portable cluster size)
 
@@ -28,28 +29,47 @@ __device__ __forceinline__ void raise_status(uint32_t* status, uint32_t bits) {
   if (status) atomicOr(status, bits);
 }
 
-// Exclusive prefix sum of one value per thread over the CTA; total in every thread.  Called by all threads.
-__device__ __forceinline__ i64 block_scan(i64 v, i64* s_warp, i64& total) {
+// Exclusive prefix sums over a chunk: v[i] belongs to request i * THREADS + threadIdx.x of it (so that loads are coalesced and the
+// warps' scans of the rows are independent), rows of them are in use.  total in every thread.  Called by all threads.
+__device__ __forceinline__ void scan_chunk(u64 (&v)[ITEMS], int rows, u64* s_tot /*[ITEMS * 32]*/, u64& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  i64 x = v;
+  __syncthreads();                           // the previous scan's readers are done with s_tot
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const i64 y = __shfl_up_sync(0xFFFFFFFFu, x, o);
-    if (lane >= o) x += y;
-  }
-  __syncthreads();                           // the previous scan's readers are done with s_warp
-  if (lane == 31) s_warp[warp] = x;
+  for (int i = 0; i < ITEMS; ++i)
+    if (i < rows) {
+      const u64 own = v[i];
+      u64 x = own;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const u64 y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+        if (lane >= o) x += y;
+      }
+      if (lane == 31) s_tot[i * 32 + warp] = x;
+      v[i] = x - own;
+    }
   __syncthreads();
-  const i64 w = s_warp[lane];                // 32 warps: one total per lane
-  i64 z = w;
+  if (warp == 0) {                           // lane l: the totals l * rows .. of the rows * 32 in order
+    u64 sum = 0;
+    for (int k = 0; k < rows; ++k) sum += s_tot[lane * rows + k];
+    u64 x = sum;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const i64 y = __shfl_up_sync(0xFFFFFFFFu, z, o);
-    if (lane >= o) z += y;
+    for (int o = 1; o < 32; o <<= 1) {
+      const u64 y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+      if (lane >= o) x += y;
+    }
+    u64 run = x - sum;
+    for (int k = 0; k < rows; ++k) {
+      const u64 t = s_tot[lane * rows + k];
+      s_tot[lane * rows + k] = run;
+      run += t;
+    }
+    if (lane == 31) s_tot[ITEMS * 32] = run;
   }
-  total = __shfl_sync(0xFFFFFFFFu, z, 31);
-  const i64 before = __shfl_sync(0xFFFFFFFFu, z - w, warp);
-  return before + x - v;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i)
+    if (i < rows) v[i] += s_tot[i * 32 + warp];
+  total = s_tot[ITEMS * 32];
 }
 
 // last index i in [0, n) with first[i] <= k; first is non-decreasing, first[0] <= k
@@ -85,12 +105,13 @@ __device__ __forceinline__ void want(const Assign& a, int r, int& held, int& nee
 
 __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS) assign_blocks_kernel(Assign a) {
   extern __shared__ uint32_t s_dyn[];
-  __shared__ i64 s_warp[32];
-  __shared__ unsigned long long s_taken;
+  __shared__ u64 s_tot[ITEMS * 32 + 1];
+  __shared__ u64 s_taken;
   const int cap_items = a.R < CHUNK ? a.R : CHUNK;
   uint32_t* s_grow = s_dyn;                  // exclusive prefix sums inside the chunk
   uint32_t* s_back = s_dyn + cap_items;
-  const int items = (cap_items + THREADS - 1) / THREADS;
+  uint32_t* s_held = s_dyn + 2 * cap_items;
+  const int rows = (cap_items + THREADS - 1) / THREADS;
   const int gtid = blockIdx.x * THREADS + threadIdx.x, gthreads = CLUSTER * THREADS;
   uint32_t bad = 0;
   const int c0 = *a.free_count;
@@ -98,91 +119,82 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS) assig
   if (count != c0) bad = PTSTORE_S_BOUNDS;
   if (threadIdx.x == 0) s_taken = 0;
 
-  auto scan_chunk = [&](int base, int n, i64& grow_total, i64& back_total) {
-    i64 g = 0, b = 0;
-    const int i0 = threadIdx.x * items;
-    uint32_t gi[ITEMS], bi[ITEMS];
+  u64 moves = 0;                             // growth of the chunk, and in the upper half what it gives back
+  auto scan = [&](int base, int n) {
+    u64 v[ITEMS];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      gi[i] = bi[i] = 0;
-      if (i < items && i0 + i < n) {
+      v[i] = 0;
+      const int k = i * THREADS + threadIdx.x;
+      if (i < rows && k < n) {
         int held, need;
-        want(a, base + i0 + i, held, need, bad);
-        gi[i] = need > held ? need - held : 0;
-        bi[i] = need < held ? held - need : 0;
+        want(a, base + k, held, need, bad);
+        s_held[k] = held;
+        v[i] = need > held ? (u64)(need - held) : (u64)(held - need) << 32;
       }
-      g += gi[i];
-      b += bi[i];
     }
-    i64 ge = block_scan(g, s_warp, grow_total), be = block_scan(b, s_warp, back_total);
+    scan_chunk(v, rows, s_tot, moves);
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i)
-      if (i < items && i0 + i < n) {
-        s_grow[i0 + i] = (uint32_t)ge;
-        s_back[i0 + i] = (uint32_t)be;
-        ge += gi[i];
-        be += bi[i];
+    for (int i = 0; i < ITEMS; ++i) {
+      const int k = i * THREADS + threadIdx.x;
+      if (i < rows && k < n) {
+        s_grow[k] = (uint32_t)v[i];
+        s_back[k] = (uint32_t)(v[i] >> 32);
       }
+    }
     __syncthreads();
   };
+  auto after = [&](const uint32_t* s, int k, int n, uint32_t end) { return k + 1 < n ? s[k + 1] : end; };
 
   // surplus blocks of shrinking rows go onto the stack, in (request, block) order
-  i64 pushed = 0, grow_total = 0, back_total = 0;
+  i64 pushed = 0;
   for (int base = 0; base < a.R; base += CHUNK) {
     const int n = a.R - base < CHUNK ? a.R - base : CHUNK;
-    scan_chunk(base, n, grow_total, back_total);
-    for (i64 k = gtid; k < back_total; k += gthreads) {
-      const int i = owner_of(s_back, n, (uint32_t)k), r = base + i;
-      int held, need;
-      want(a, r, held, need, bad);
-      const i64 to = count + pushed + k;
-      if (to < a.capacity) a.free_ids[to] = a.tables[(i64)r * a.max_blocks + need + (k - s_back[i])];
-      else bad = PTSTORE_S_BOUNDS;           // more ids than the stack has room for: the surplus ones are lost
+    scan(base, n);
+    const uint32_t back = (uint32_t)(moves >> 32);
+    for (u64 k = gtid; k < back; k += gthreads) {
+      const int i = owner_of(s_back, n, (uint32_t)k);
+      const uint32_t first = s_back[i], need = s_held[i] - (after(s_back, i, n, back) - first);
+      const i64 to = count + pushed + (i64)k;
+      if (to < a.capacity) a.free_ids[to] = a.tables[(i64)(base + i) * a.max_blocks + need + ((uint32_t)k - first)];
+      else bad |= PTSTORE_S_BOUNDS;          // more ids than the stack has room for: the surplus ones are lost
     }
-    pushed += back_total;
-    __syncthreads();
+    pushed += back;
   }
   i64 top = count + pushed;
   if (top > a.capacity) top = a.capacity;
-  cluster_sync();                            // the pushed ids are visible; nothing has been popped yet
+  cluster_sync();                            // the pushed ids are visible, and every CTA has read held and free_count
 
   // growing rows pop from the top; a request is granted its blocks iff all growth up to and including it fits
   i64 wanted = 0;
   for (int base = 0; base < a.R; base += CHUNK) {
     const int n = a.R - base < CHUNK ? a.R - base : CHUNK;
     if (a.R > CHUNK) {                       // a single chunk's sums are still in shared memory
-      scan_chunk(base, n, grow_total, back_total);
+      scan(base, n);
       cluster_sync();                        // every CTA has read held of this chunk before one overwrites it
     }
-    i64 fits = top - wanted;                 // pops of this chunk that the stack can serve
-    const int i0 = threadIdx.x * items;
-    for (int i = 0; i < items; ++i)
-      if (i0 + i < n) {
-        const int r = base + i0 + i;
-        int held, need;
-        want(a, r, held, need, bad);
-        const i64 upto = (i64)s_grow[i0 + i] + (need - held);
-        if (need > held) {
-          if (upto <= fits) atomicMax(&s_taken, (unsigned long long)(wanted + upto));
-          else { bad |= PTSTORE_S_NOSPACE; need = held; }
-        }
+    const uint32_t grow = (uint32_t)moves, back = (uint32_t)(moves >> 32);
+    const i64 fits = top - wanted;           // pops of this chunk that the stack can serve
+    uint32_t best = 0;                       // grants are a prefix of the pops: the largest granted end is their number
+    for (int k = threadIdx.x; k < n; k += THREADS) {
+      const uint32_t g0 = s_grow[k], g = after(s_grow, k, n, grow) - g0, held = s_held[k];
+      const bool granted = (i64)g0 + g <= fits;
+      if (g > 0) {
+        if (granted) best = g0 + g;
+        else bad |= PTSTORE_S_NOSPACE;
       }
+      if (k / (THREADS / CLUSTER) % CLUSTER == blockIdx.x)       // each CTA writes its share
+        a.held_out[base + k] = held + (granted ? g : 0) - (after(s_back, k, n, back) - s_back[k]);
+    }
+    best = __reduce_max_sync(0xFFFFFFFFu, best);
+    if ((threadIdx.x & 31) == 0 && best > 0) atomicMax(&s_taken, (u64)(wanted + best));
     __syncthreads();
     const i64 end = (i64)s_taken - wanted;   // pops granted in this chunk: the first `end` of them
     for (i64 k = gtid; k < end; k += gthreads) {
-      const int i = owner_of(s_grow, n, (uint32_t)k), r = base + i;
-      int held, need;
-      want(a, r, held, need, bad);
-      a.tables[(i64)r * a.max_blocks + held + (k - s_grow[i])] = a.free_ids[top - 1 - (wanted + k)];
+      const int i = owner_of(s_grow, n, (uint32_t)k);
+      a.tables[(i64)(base + i) * a.max_blocks + s_held[i] + ((uint32_t)k - s_grow[i])] = a.free_ids[top - 1 - (wanted + k)];
     }
-    // held is read by every CTA above, so one CTA's writes wait for all of them
-    cluster_sync();
-    for (int i = gtid; i < n; i += gthreads) {
-      int held, need;
-      want(a, base + i, held, need, bad);
-      a.held_out[base + i] = need <= held || (i64)s_grow[i] + (need - held) <= fits ? need : held;
-    }
-    wanted += grow_total;
+    wanted += grow;
     __syncthreads();
   }
   if (gtid == 0) *a.free_count_out = (int)(top - (i64)s_taken);
@@ -214,50 +226,53 @@ __device__ __forceinline__ void done_new(const MapSlots& m, int r, int& done, in
 }
 
 __global__ void __launch_bounds__(THREADS) map_slots_kernel(MapSlots m) {
-  extern __shared__ uint32_t s_first[];      // exclusive prefix sums inside the chunk
-  __shared__ i64 s_warp[32];
+  extern __shared__ uint32_t s_dyn[];
+  __shared__ u64 s_tot[ITEMS * 32 + 1];
   const int cap_items = m.R < CHUNK ? m.R : CHUNK;
-  const int items = (cap_items + THREADS - 1) / THREADS;
+  uint32_t* s_first = s_dyn;                 // exclusive prefix sums inside the chunk
+  int* s_done = reinterpret_cast<int*>(s_dyn + cap_items);
+  const int rows = (cap_items + THREADS - 1) / THREADS;
   const i64 t0 = blockIdx.x * m.per_cta, t1 = t0 + m.per_cta < m.max_tokens ? t0 + m.per_cta : m.max_tokens;
   uint32_t bad = 0;
   i64 base_tok = 0;
   for (int base = 0; base < m.R; base += CHUNK) {
     const int n = m.R - base < CHUNK ? m.R - base : CHUNK;
-    const int i0 = threadIdx.x * items;
-    i64 sum = 0;
-    int f[ITEMS];
+    u64 v[ITEMS], sum;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      f[i] = 0;
-      int done;
-      if (i < items && i0 + i < n) done_new(m, base + i0 + i, done, f[i], bad);
-      sum += f[i];
-    }
-    i64 total;
-    i64 e = block_scan(sum, s_warp, total);
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i)
-      if (i < items && i0 + i < n) {
-        // a chunk's sums can pass 32 bits only where they pass max_tokens too; those are never searched for
-        s_first[i0 + i] = e > UINT_MAX ? UINT_MAX : (uint32_t)e;
-        if (blockIdx.x == 0) {
-          const i64 at = base_tok + e;
-          m.offsets[base + i0 + i] = at > INT_MAX ? INT_MAX : (int)at;
-        }
-        e += f[i];
+      v[i] = 0;
+      const int k = i * THREADS + threadIdx.x;
+      if (i < rows && k < n) {
+        int done, fresh;
+        done_new(m, base + k, done, fresh, bad);
+        s_done[k] = done;
+        v[i] = (u64)fresh;
       }
+    }
+    scan_chunk(v, rows, s_tot, sum);
+    const i64 total = (i64)sum;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int k = i * THREADS + threadIdx.x;
+      if (i < rows && k < n) {
+        // a chunk's sums can pass 32 bits only where they pass max_tokens too; those are never searched for
+        s_first[k] = v[i] > UINT_MAX ? UINT_MAX : (uint32_t)v[i];
+        if (blockIdx.x == 0) {
+          const i64 at = base_tok + (i64)v[i];
+          m.offsets[base + k] = at > INT_MAX ? INT_MAX : (int)at;
+        }
+      }
+    }
     __syncthreads();
     const i64 lo = t0 > base_tok ? t0 : base_tok, hi = t1 < base_tok + total ? t1 : base_tok + total;
     for (i64 t = lo + threadIdx.x; t < hi; t += THREADS) {
       const uint32_t k = (uint32_t)(t - base_tok);
-      const int i = owner_of(s_first, n, k), r = base + i;
-      int done, fresh;
-      done_new(m, r, done, fresh, bad);
-      const int pos = done + (int)(k - s_first[i]);
+      const int i = owner_of(s_first, n, k);
+      const int pos = s_done[i] + (int)(k - s_first[i]);
       const int j = pos / m.block_tokens;
       i64 slot = -1;
       if (j < m.max_blocks) {
-        const int b = m.tables[(i64)r * m.max_blocks + j];
+        const int b = m.tables[(i64)(base + i) * m.max_blocks + j];
         if (b >= 0) slot = (i64)b * m.block_tokens + (pos - j * m.block_tokens);
       } else bad = PTSTORE_S_BOUNDS;
       m.slots[t] = slot;
@@ -301,7 +316,7 @@ extern "C" int ptstore_assign_blocks(const int32_t* lengths, const int32_t* held
   if (R > 1 << 30) return PTSTORE_E_LIMIT;
   if ((i64)(R < CHUNK ? R : CHUNK) * max_blocks > (i64)UINT_MAX) return PTSTORE_E_LIMIT;      // sums inside a chunk are 32 bits wide
   const Assign a = {lengths, held, R, block_tokens, max_blocks, free_capacity, block_tables, free_ids, free_count, held_out, free_count_out, status};
-  const size_t smem = 8 * (size_t)(R < CHUNK ? R : CHUNK);
+  const size_t smem = 12 * (size_t)(R < CHUNK ? R : CHUNK);
   (void)cudaGetLastError();
   const int rc = allow_smem(assign_blocks_kernel, smem);
   if (rc) return rc;
@@ -324,7 +339,7 @@ extern "C" int ptstore_map_slots(const int32_t* lengths, const int32_t* done, in
   m.per_cta = per;
   i64 grid = (max_tokens + per - 1) / per;
   if (grid < 1) grid = 1;
-  const size_t smem = 4 * (size_t)(R < CHUNK ? R : CHUNK);
+  const size_t smem = 8 * (size_t)(R < CHUNK ? R : CHUNK);
   (void)cudaGetLastError();
   const int rc = allow_smem(map_slots_kernel, smem);
   if (rc) return rc;
