@@ -301,13 +301,12 @@ def map_slots(lengths, done, block_tables, block_tokens, max_tokens, done_unit=1
     """ptstore_map_slots: the new tokens of a batch.  done (tokens, times done_unit; None: none) are in the cache already; after a lookup
     pass its matched lengths with done_unit=block_tokens, min_new=1.  Returns (token_offsets [R+1], slots int64 [max_tokens], positions)."""
     dev, i32, R = torch.cuda.current_device(), torch.int32, lengths.numel()
-    where = block_tables.device if block_tables.is_cuda else torch.device("cuda", dev)
     if token_offsets is None:
-        token_offsets = torch.empty(R + 1, dtype=i32, device=where)
+        token_offsets = torch.empty(R + 1, dtype=i32, device="cuda")
     if slots is None:
-        slots = torch.empty(max_tokens, dtype=torch.int64, device=where)
+        slots = torch.empty(max_tokens, dtype=torch.int64, device="cuda")
     if positions is None:
-        positions = torch.empty(max_tokens, dtype=i32, device=where)
+        positions = torch.empty(max_tokens, dtype=i32, device="cuda")
     _check(lib.ptstore_map_slots(_vec(lengths, i32, R, dev, "lengths"), None if done is None else _vec(done, i32, R, dev, "done"), done_unit, min_new, R,
                                  _table(block_tables, R, dev, "block_tables"), block_tables.shape[1], block_tokens, max_tokens,
                                  _vec(token_offsets, i32, R + 1, dev, "token_offsets"), _vec(slots, torch.int64, max_tokens, dev, "slots"),
@@ -329,7 +328,7 @@ def kv_read(layout, cache, layer, slots, dtype, k=None, v=None, status=None):
     """ptstore_kv_read: the values at `slots` as rows [tokens, heads, dim]; rows whose slot is -1 are left as they were.  Returns (k, v)."""
     dev, n = torch.cuda.current_device(), slots.numel()
     if k is None:
-        k = torch.empty((n, layout.heads, layout.dim), dtype=dtype, device=torch.device("cuda", dev))
+        k = torch.empty((n, layout.heads, layout.dim), dtype=dtype, device="cuda")
     if v is None:
         v = torch.empty_like(k)
     code = _kv_dtype(k, "k")

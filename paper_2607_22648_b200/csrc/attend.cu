@@ -1,4 +1,6 @@
 // ptstore_attend: host side and dispatch of the attention over the paged cache.
+#include <atomic>
+
 #include "attend_prompt.cuh"
 #include "attend_split.cuh"
 
@@ -6,52 +8,63 @@ using namespace ptk;
 
 namespace {
 
-constexpr int MAX_SMS = 160;                 // the workspace does not depend on the device: a B200 has 148 SMs
-
 // rows of an item: 8 where a request's rows of one kv head fit, else 16
 inline int n_tiles_of(i64 rows) { return rows <= 8 ? 1 : 2; }
 
 constexpr u64 counters_bytes(int ctas) { return ((u64)ctas * 4 + 255) / 256 * 256; }
 
-int sm_count(int* sms) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || *sms <= 0) {
+struct Gpu { int dev, sms; };
+int current_gpu(Gpu* g) {
+  if (cudaGetDevice(&g->dev) != cudaSuccess || cudaDeviceGetAttribute(&g->sms, cudaDevAttrMultiProcessorCount, g->dev) != cudaSuccess || g->sms <= 0) {
     (void)cudaGetLastError();
     return PTSTORE_E_CUDA;
   }
-  if (*sms > MAX_SMS) *sms = MAX_SMS;
+  if (g->sms > MAX_SMS) g->sms = MAX_SMS;    // a B200 has 148; the workspace does not depend on the device
+  return PTSTORE_OK;
+}
+
+// Lets a kernel use its shared memory, once per device (the setting belongs to the device; concurrent first calls set it twice).
+template <typename F>
+int allow_smem(F* kernel, int bytes, std::atomic<u64>& devices, int dev) {
+  const u64 bit = 1ull << (dev & 63);
+  if (dev < 64 && (devices.load(std::memory_order_acquire) & bit)) return PTSTORE_OK;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return PTSTORE_E_CUDA;
+  }
+  if (dev < 64) devices.fetch_or(bit, std::memory_order_release);
   return PTSTORE_OK;
 }
 
 template <int FMT, bool QFP16, int D, int NT>
-int launch_split(const Attend& a, int sms, cudaStream_t s) {
-  using Shape = SplitShape<FMT, D>;
-  static_assert(Shape::RING >= SP_WARPS * 8 * NT * (D + 4) * 4, "the ring holds the warps' sums at the end of an item");
-  static_assert(Shape::RING >= MAX_SMS * (NT == 1 ? SP_CTAS : 2) * 8 * NT * 8, "and the maxima and sums of an item's parts when they are joined");
+int launch_split(const Attend& a, const Gpu& gpu, cudaStream_t s) {
+  constexpr int SMEM = split_smem<FMT, D, NT>();
+  static std::atomic<u64> devices{0};
   auto* kernel = attend_split_kernel<FMT, QFP16, D, NT>;
-  // set on every call: the setting belongs to the current device
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape::RING) != cudaSuccess) { (void)cudaGetLastError(); return PTSTORE_E_CUDA; }
-  kernel<<<sms * (NT == 1 ? SP_CTAS : 2), SP_THREADS, Shape::RING, s>>>(a);
+  const int rc = allow_smem(kernel, SMEM, devices, gpu.dev);
+  if (rc) return rc;
+  kernel<<<gpu.sms * split_ctas<FMT, NT>(), SP_THREADS, SMEM, s>>>(a);
   return cudaGetLastError() == cudaSuccess ? PTSTORE_OK : PTSTORE_E_CUDA;
 }
 
 template <int FMT, bool QFP16>
-int launch_split_shape(const Attend& a, int D, int nt, int sms, cudaStream_t s) {
-  if (D == 64) return nt == 1 ? launch_split<FMT, QFP16, 64, 1>(a, sms, s) : launch_split<FMT, QFP16, 64, 2>(a, sms, s);
-  return nt == 1 ? launch_split<FMT, QFP16, 128, 1>(a, sms, s) : launch_split<FMT, QFP16, 128, 2>(a, sms, s);
+int launch_split_shape(const Attend& a, int D, int nt, const Gpu& gpu, cudaStream_t s) {
+  if (D == 64) return nt == 1 ? launch_split<FMT, QFP16, 64, 1>(a, gpu, s) : launch_split<FMT, QFP16, 64, 2>(a, gpu, s);
+  return nt == 1 ? launch_split<FMT, QFP16, 128, 1>(a, gpu, s) : launch_split<FMT, QFP16, 128, 2>(a, gpu, s);
 }
 
 template <int FMT, bool QFP16, int D>
-int launch_prompt(const Attend& a, cudaStream_t s) {
+int launch_prompt(const Attend& a, const Gpu& gpu, cudaStream_t s) {
   auto* kernel = attend_prompt_kernel<FMT, QFP16, D>;
   constexpr int SMEM = PromptShape<D>::SMEM;
-  // the kernel's warps trade registers, which is only sound if the block is launched with all of the SM's
-  cudaFuncAttributes attr;
-  if (cudaFuncGetAttributes(&attr, kernel) != cudaSuccess || attr.numRegs * PR_THREADS != 65536 ||
-      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return PTSTORE_E_CUDA;
+  static std::atomic<u64> devices{0};
+  if (gpu.dev >= 64 || !(devices.load(std::memory_order_acquire) >> gpu.dev & 1)) {
+    // the kernel's warps trade registers, which is only sound if the block is launched with all of the SM's
+    cudaFuncAttributes attr;
+    if (cudaFuncGetAttributes(&attr, kernel) != cudaSuccess || attr.numRegs * PR_THREADS != 65536) { (void)cudaGetLastError(); return PTSTORE_E_CUDA; }
   }
+  const int rc = allow_smem(kernel, SMEM, devices, gpu.dev);
+  if (rc) return rc;
   const i64 tiles = (i64)a.tokens * a.group / PR_ROWS + a.R;            // at most this many, wherever the requests' rows end
   if (tiles * a.cache.heads > 0x7FFFFFFF) return PTSTORE_E_LIMIT;
   kernel<<<(unsigned)(tiles * a.cache.heads), PR_THREADS, SMEM, s>>>(a);
@@ -65,8 +78,8 @@ constexpr i64 PROMPT_ROWS = 33;
 
 extern "C" uint64_t ptstore_attend_workspace_bytes(uint32_t head_dim) {
   if (head_dim != 64 && head_dim != 128) return 0;
-  const u64 ctas = (u64)MAX_SMS * SP_CTAS;
-  return counters_bytes((int)ctas) + ctas * 2 * 16 * (head_dim + 2) * 4;
+  // counters, and two parts per CTA: of 8 rows where 4 CTAs share an SM, of 16 where 2 do
+  return counters_bytes(MAX_SMS * 4) + (u64)MAX_SMS * 4 * 2 * 8 * (head_dim + 2) * 4;
 }
 
 extern "C" int ptstore_attend(const ptstore_attend_t* p, const ptstore_kv_cache_t* cache, void* workspace, uint64_t workspace_bytes,
@@ -100,9 +113,9 @@ extern "C" int ptstore_attend(const ptstore_attend_t* p, const ptstore_kv_cache_
   a.v_factor = packed ? cache->v_scale * DEQ_FACTOR : 1.0f;
   a.work = static_cast<unsigned char*>(workspace);
   a.status = status;
-  int sms = 0;
+  Gpu gpu;
   (void)cudaGetLastError();
-  const int rs = sm_count(&sms);
+  const int rs = current_gpu(&gpu);
   if (rs) return rs;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const int most = p->max_new < p->tokens ? p->max_new : p->tokens;
@@ -110,12 +123,12 @@ extern "C" int ptstore_attend(const ptstore_attend_t* p, const ptstore_kv_cache_
   const bool half = p->dtype == PTSTORE_KV_FP16;
   if ((i64)most * a.group >= PROMPT_ROWS) {
     if (D == 64) {
-      if (packed) return half ? launch_prompt<PTSTORE_KV_PACKED, true, 64>(a, s) : launch_prompt<PTSTORE_KV_PACKED, false, 64>(a, s);
-      return half ? launch_prompt<PTSTORE_KV_FP16, true, 64>(a, s) : launch_prompt<PTSTORE_KV_BF16, false, 64>(a, s);
+      if (packed) return half ? launch_prompt<PTSTORE_KV_PACKED, true, 64>(a, gpu, s) : launch_prompt<PTSTORE_KV_PACKED, false, 64>(a, gpu, s);
+      return half ? launch_prompt<PTSTORE_KV_FP16, true, 64>(a, gpu, s) : launch_prompt<PTSTORE_KV_BF16, false, 64>(a, gpu, s);
     }
-    if (packed) return half ? launch_prompt<PTSTORE_KV_PACKED, true, 128>(a, s) : launch_prompt<PTSTORE_KV_PACKED, false, 128>(a, s);
-    return half ? launch_prompt<PTSTORE_KV_FP16, true, 128>(a, s) : launch_prompt<PTSTORE_KV_BF16, false, 128>(a, s);
+    if (packed) return half ? launch_prompt<PTSTORE_KV_PACKED, true, 128>(a, gpu, s) : launch_prompt<PTSTORE_KV_PACKED, false, 128>(a, gpu, s);
+    return half ? launch_prompt<PTSTORE_KV_FP16, true, 128>(a, gpu, s) : launch_prompt<PTSTORE_KV_BF16, false, 128>(a, gpu, s);
   }
-  if (packed) return half ? launch_split_shape<PTSTORE_KV_PACKED, true>(a, D, nt, sms, s) : launch_split_shape<PTSTORE_KV_PACKED, false>(a, D, nt, sms, s);
-  return half ? launch_split_shape<PTSTORE_KV_FP16, true>(a, D, nt, sms, s) : launch_split_shape<PTSTORE_KV_BF16, false>(a, D, nt, sms, s);
+  if (packed) return half ? launch_split_shape<PTSTORE_KV_PACKED, true>(a, D, nt, gpu, s) : launch_split_shape<PTSTORE_KV_PACKED, false>(a, D, nt, gpu, s);
+  return half ? launch_split_shape<PTSTORE_KV_FP16, true>(a, D, nt, gpu, s) : launch_split_shape<PTSTORE_KV_BF16, false>(a, D, nt, gpu, s);
 }

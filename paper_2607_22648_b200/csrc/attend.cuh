@@ -45,6 +45,20 @@ __device__ __forceinline__ void cp_async16(u32 dst, const void* src) {
 __device__ __forceinline__ void cp_async16_or_zero(u32 dst, const void* src, bool ok) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void bar_init(u64* bar, u32 count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count) : "memory"); }
+__device__ __forceinline__ void bar_arrive(u64* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory"); }
+__device__ __forceinline__ void bar_expect(u64* bar, u32 bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(u64* bar, u32 parity) {
+  u32 ok;
+  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity) : "memory");
+  return ok != 0;
+}
+// `bytes` contiguous bytes (16-byte aligned, a multiple of 16) into shared memory, counted by the barrier
+__device__ __forceinline__ void bulk_load(u32 dst, const void* src, u32 bytes, u64* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_addr(bar)) : "memory");
+}
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -79,24 +93,35 @@ __device__ __forceinline__ u32 hmul2(u32 a, u32 b) {
 // 4-bit codes to fp16.  A code n at bits p .. p+3 of 0x6400 reads as 1024 + n 2^p, and (1024 + n 2^p) * (s / 2^p) - (1024 / 2^p + 8) s
 // = (n - 8) s in one fused multiply-add.  It is exact: every constant below fits 11 bits for p >= 1 (520 s: 7 + 4 bits), so the
 // codes are read at bits 1..4 and 5..8.  s is the scale times 2^-8, which keeps 520 s inside fp16; the 2^8 is put back at the end.
+// `(x & mask) | 0x6400..` is ONE instruction only if the constants are in registers, hence Magic.
+struct Magic { u32 m1, m5, one; };
+__device__ __forceinline__ Magic magic() {
+  Magic m;
+  asm volatile("mov.b32 %0, 0x001E001E;\n mov.b32 %1, 0x01E001E0;\n mov.b32 %2, 0x64006400;" : "=r"(m.m1), "=r"(m.m5), "=r"(m.one));
+  return m;
+}
+__device__ __forceinline__ u32 and_or(u32 a, u32 b, u32 c) {
+  u32 r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
+}
 struct Deq { u32 s1, c1, s5, c5; };
 __device__ __forceinline__ Deq deq_of(u32 scale2) {          // two e4m3 scales as fp16 pairs
   Deq d;
-  const u32 s = hmul2(scale2, 0x1C001C00u);                  // 2^-8
-  d.s1 = hmul2(s, 0x38003800u);                              // 2^-1
-  d.c1 = hmul2(s, 0xE010E010u);                              // -520
-  d.s5 = hmul2(s, 0x28002800u);                              // 2^-5
-  d.c5 = hmul2(s, 0xD100D100u);                              // -40
+  d.s1 = hmul2(scale2, 0x18001800u);                         // 2^-8 2^-1 (a multiple of 2^-18: exact)
+  d.c1 = hmul2(d.s1, 0xE410E410u);                           // -1040
+  d.s5 = hmul2(d.s1, 0x2C002C00u);                           // 2^-4
+  d.c5 = hmul2(d.s1, 0xD500D500u);                           // -80
   return d;
 }
 constexpr float DEQ_FACTOR = 256.0f;
 // the four nibbles of each 16-bit half: o[j] = (nibble j of the low half, nibble j of the high half)
-__device__ __forceinline__ void deq4(u32 x, const Deq& d, u32 (&o)[4]) {
+__device__ __forceinline__ void deq4(u32 x, const Deq& d, const Magic& k, u32 (&o)[4]) {
   const u32 l = x << 1, h = x >> 7;
-  o[0] = hfma2((l & 0x001E001Eu) | 0x64006400u, d.s1, d.c1);
-  o[1] = hfma2((l & 0x01E001E0u) | 0x64006400u, d.s5, d.c5);
-  o[2] = hfma2((h & 0x001E001Eu) | 0x64006400u, d.s1, d.c1);
-  o[3] = hfma2((h & 0x01E001E0u) | 0x64006400u, d.s5, d.c5);
+  o[0] = hfma2(and_or(l, k.m1, k.one), d.s1, d.c1);
+  o[1] = hfma2(and_or(l, k.m5, k.one), d.s5, d.c5);
+  o[2] = hfma2(and_or(h, k.m1, k.one), d.s1, d.c1);
+  o[3] = hfma2(and_or(h, k.m5, k.one), d.s5, d.c5);
 }
 
 }  // namespace ptk

@@ -32,13 +32,6 @@ struct PromptShape {
   static constexpr int SMEM = (2 + PR_SLOTS) * TILE_BYTES + 1024;       // + alignment
 };
 
-__device__ __forceinline__ void bar_init(u64* bar, u32 count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count) : "memory"); }
-__device__ __forceinline__ void bar_arrive(u64* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory"); }
-__device__ __forceinline__ bool bar_try(u64* bar, u32 parity) {
-  u32 ok;
-  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity) : "memory");
-  return ok != 0;
-}
 // false: this wait, or another one of the CTA, ran out
 __device__ __forceinline__ bool bar_wait(u64* bar, u32 parity, volatile int* gave_up) {
   if (bar_try(bar, parity)) return true;
@@ -379,6 +372,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
           }
         }
       };
+      const Magic mg = magic();
       if (n_steps > 0) load(0);
       for (int op = 0; op < 2 * n_steps && ok; ++op) {
         u32 cur[D / 8], sc[D / 64];
@@ -409,7 +403,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
 #pragma unroll
           for (int w = 0; w < 2; ++w) {
             u32 o[4];
-            deq4(cur[2 * g + w], d, o);
+            deq4(cur[2 * g + w], d, mg, o);
             *reinterpret_cast<uint4*>(t + operand_at(pt, 2 * g + w)) = cur_has ? make_uint4(o[0], o[1], o[2], o[3]) : make_uint4(0, 0, 0, 0);
           }
         }

@@ -21,16 +21,27 @@ namespace ptk {
 constexpr int SP_WARPS = 4, SP_THREADS = 32 * SP_WARPS;
 constexpr int UNIT = SP_WARPS * TILE;        // tokens of a unit: one tile per warp
 constexpr int MIN_UNITS = 4;                 // a CTA takes at least this many, so that joining does not cost more than it saves
-constexpr int SP_CTAS = 3;                   // per SM
+constexpr u32 SP_POLLS = 1u << 22;           // polls of a wait for a tile before the warp gives up (each may suspend for a while)
 
 template <int FMT, int D>
 struct SplitShape {
   static constexpr bool PACKED = FMT == PTSTORE_KV_PACKED;
   static constexpr int STAGE = PACKED ? 2 * tile_bytes(D) : 2 * TILE * D * 2;      // K tile, V tile
-  static constexpr int STAGES = (PACKED ? 6 : 2) * (128 / D);
+  static constexpr int STAGES = (PACKED ? 4 : 2) * (128 / D);
   static constexpr int STEP = PACKED ? 2 : 1;                                      // tiles per softmax step
   static constexpr int RING = SP_WARPS * STAGES * STAGE;
 };
+// CTAs per SM, by registers: 128 per thread where a row tile has 8 rows of a 4-bit cache
+template <int FMT, int NT>
+__host__ __device__ constexpr int split_ctas() { return NT == 2 ? 2 : FMT == PTSTORE_KV_PACKED ? 4 : 3; }
+// shared memory: the ring, which at the end of an item holds the warps' sums and then the maxima and sums of an item's parts (at most
+// one part per CTA of MAX_SMS SMs)
+constexpr int MAX_SMS = 160;
+template <int FMT, int D, int NT>
+constexpr int split_smem() {
+  const int ring = SplitShape<FMT, D>::RING, sums = SP_WARPS * 8 * NT * (D + 4) * 4, parts = MAX_SMS * split_ctas<FMT, NT>() * 8 * NT * 8;
+  return ring > sums ? (ring > parts ? ring : parts) : (sums > parts ? sums : parts);
+}
 
 template <int NT, int D>
 __host__ __device__ constexpr int part_floats() { return 8 * NT * (D + 2); }      // partial sums of one item in one CTA: o, m, l
@@ -56,6 +67,12 @@ __device__ __forceinline__ void ldsm4_t(u32 (&r)[4], u32 addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 
+__device__ __forceinline__ bool bar_wait_or_give_up(u64* bar, u32 parity) {
+  for (u32 i = 0; i < SP_POLLS; ++i)
+    if (bar_try(bar, parity)) return true;
+  return false;
+}
+
 // keys row tile rt of a request can see (of its last row), and its units (at least one: a row that sees nothing is written too)
 template <int NQ>
 __device__ __forceinline__ int tile_keys(const Attend& a, const Req& q, int rt) {
@@ -78,7 +95,7 @@ __device__ __forceinline__ i64 request_units(const Attend& a, int r) {
 }
 
 template <int FMT, bool QFP16, int D, int NT>
-__global__ void __launch_bounds__(SP_THREADS, NT == 1 ? SP_CTAS : 2) attend_split_kernel(Attend a) {
+__global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_split_kernel(Attend a) {
   using Shape = SplitShape<FMT, D>;
   constexpr bool PACKED = Shape::PACKED;
   constexpr bool F16 = PACKED || FMT == PTSTORE_KV_FP16;      // type of the products' operands
@@ -88,7 +105,9 @@ __global__ void __launch_bounds__(SP_THREADS, NT == 1 ? SP_CTAS : 2) attend_spli
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ i64 s_scan[SP_WARPS];
   __shared__ i64 s_left;
-  __shared__ int s_r, s_last;
+  __shared__ int s_r, s_last, s_any_bad;
+  __shared__ __align__(8) u64 s_bar[SP_WARPS][STAGES];
+  __shared__ int s_bad[3][D];                // first key whose V holds NaN, +inf, -inf in column d, among keys that some rows do not see
   __shared__ float s_m[SP_WARPS][NQ], s_l[SP_WARPS][NQ], s_qf[NQ];
   __shared__ __align__(16) unsigned short s_q[NQ][D + 8];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -132,6 +151,15 @@ __global__ void __launch_bounds__(SP_THREADS, NT == 1 ? SP_CTAS : 2) attend_spli
   i64 left = s_left;
   i64 u = u_begin;
 
+  if (PACKED && lane == 0) {
+    for (int i = 0; i < STAGES; ++i) bar_init(&s_bar[warp][i], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  u32 phases = 0;                            // parity of every stage's barrier
+  bool gave_up = false;
+  const Magic mg = magic();
+
   unsigned char* const ring = smem + warp * STAGES * STAGE;
   const u32 ring_addr = smem_addr(ring);
   int rt = 0;
@@ -162,58 +190,85 @@ __global__ void __launch_bounds__(SP_THREADS, NT == 1 ? SP_CTAS : 2) attend_spli
     const int n_tiles = ub - ua;
     const int* table = a.tables + (i64)r * a.max_blocks;
     const u32 B = a.cache.block_tokens;
-    const u32 step_blk = UNIT / B, step_off = UNIT % B;
-    const u32 my_tok0 = (u32)ua * UNIT + warp * TILE + (PACKED ? 0 : lane & 15);
-    u32 n_blk = my_tok0 / B, n_off = my_tok0 % B;             // of the next tile to issue (16-bit caches: of row lane & 15 of it)
-    int n_tok = (int)my_tok0;
-    auto look_up = [&]() { return n_tok < keys ? table[n_blk] : -1; };
-    int n_id = n_tiles > 0 ? look_up() : -1;
     u32 seen_bits = 0;                                        // bit s: stage s holds a tile (16-bit: bits of this lane's row)
     bool bounds = false;
+    // 4-bit: lane l finds tile base + l, 32 tiles at a time; the table entries of the next 32 are on their way meanwhile
+    i64 tile_off = -1;
+    int n_id = -1;
+    auto look_up32 = [&](int base) {
+      const int tok = (ua + base + lane) * UNIT + warp * TILE;
+      n_id = base + lane < n_tiles && tok < keys ? table[(u32)tok / B] : -1;
+    };
+    auto resolve32 = [&](int base) {
+      const u32 tok = (u32)(ua + base + lane) * UNIT + warp * TILE;
+      const bool ok = (u32)n_id < a.cache.num_blocks;
+      bounds |= base + lane < n_tiles && (int)tok < keys && !ok;
+      tile_off = ok ? (i64)((u64)(u32)n_id * a.cache.block_stride + ((u64)h * (B / TILE) + tok % B / TILE) * tile_bytes(D)) : -1;
+      look_up32(base + 32);
+    };
+    // 16-bit: lane l follows row l & 15 of the tiles
+    const u32 step_blk = UNIT / B, step_off = UNIT % B;
+    int n_tok = ua * UNIT + warp * TILE + (lane & 15);
+    u32 n_blk = (u32)n_tok / B, n_off = (u32)n_tok % B;
+    if (PACKED) look_up32(0);
+    else n_id = n_tiles > 0 && n_tok < keys ? table[n_blk] : -1;
     auto issue = [&](int i, int s) {
       seen_bits &= ~(1u << s);
+      if (PACKED) {
+        if (i < n_tiles) {
+          if ((i & 31) == 0) resolve32(i);
+          const i64 off = __shfl_sync(FULL, tile_off, i & 31);
+          if (off >= 0) {
+            seen_bits |= 1u << s;
+            if (lane == 0) {
+              u64* bar = &s_bar[warp][s];
+              const unsigned char* src = a.cache.base + off;
+              const u32 dst = ring_addr + s * STAGE;
+              bar_expect(bar, STAGE);
+              bulk_load(dst, src, tile_bytes(D), bar);
+              bulk_load(dst + tile_bytes(D), src + a.cache.kv_stride, tile_bytes(D), bar);
+            }
+          }
+        }
+        return;
+      }
       if (i < n_tiles) {
-        const int id = n_id;
-        const u32 blk_off = n_off;
         const bool in_len = n_tok < keys;
-        const bool ok = in_len && (u32)id < a.cache.num_blocks;
+        const bool ok = in_len && (u32)n_id < a.cache.num_blocks;
         bounds |= in_len && !ok;
+        const u64 row_off = ok ? (u64)(u32)n_id * a.cache.block_stride + ((u64)n_off * a.cache.heads + h) * (D * 2) : 0;
         n_off += step_off;
         n_blk += step_blk;
         n_tok += UNIT;
         if (n_off >= B) { n_off -= B; ++n_blk; }
-        if (i + 1 < n_tiles) n_id = look_up();
+        if (i + 1 < n_tiles) n_id = n_tok < keys ? table[n_blk] : -1;
         if (ok) seen_bits |= 1u << s;
         const u32 dst = ring_addr + s * STAGE;
-        if (PACKED) {
-          if (ok) {
-            constexpr int N16 = tile_bytes(D) / 16;
-            const unsigned char* ks = tile_ptr(a.cache, false, id, h, blk_off, D);
-            const unsigned char* vs = ks + a.cache.kv_stride;
+        // some rows per instruction; 16-byte chunk c of row n sits at c ^ (n & 7), which ldmatrix reads without conflicts
+        constexpr int CPR = D / 8, RPI = 32 / CPR;            // chunks per row, rows per instruction
 #pragma unroll
-            for (int c = lane; c < 2 * N16; c += 32) cp_async16(dst + c * 16, c < N16 ? ks + c * 16 : vs + (c - N16) * 16);
-          }
-        } else {
-          // two rows per instruction; 16-byte chunk c of row n sits at c ^ (n & 7), which ldmatrix reads without conflicts
-          constexpr int CPR = D / 8, RPI = 32 / CPR;          // chunks per row, rows per instruction
-          const u64 row_off = ok ? (u64)id * a.cache.block_stride + ((u64)blk_off * a.cache.heads + h) * (D * 2) : 0;
-#pragma unroll
-          for (int j = 0; j < TILE / RPI; ++j) {
-            const int n = j * RPI + lane / CPR, c = lane % CPR;
-            const u64 off = __shfl_sync(FULL, row_off, n);
-            const bool has = __shfl_sync(FULL, ok, n);
-            const unsigned char* ks = a.cache.base + off + c * 16;
-            const u32 d = dst + n * (D * 2) + ((c ^ (n & 7)) * 16);
-            cp_async16_or_zero(d, ks, has);
-            cp_async16_or_zero(d + TILE * D * 2, ks + a.cache.kv_stride, has);
-          }
+        for (int j = 0; j < TILE / RPI; ++j) {
+          const int n = j * RPI + lane / CPR, c = lane % CPR;
+          const u64 off = __shfl_sync(FULL, row_off, n);
+          const bool has = __shfl_sync(FULL, ok, n);
+          const unsigned char* ks = a.cache.base + off + c * 16;
+          const u32 d = dst + n * (D * 2) + ((c ^ (n & 7)) * 16);
+          cp_async16_or_zero(d, ks, has);
+          cp_async16_or_zero(d + TILE * D * 2, ks + a.cache.kv_stride, has);
         }
       }
       cp_commit();
     };
-    const int P = STAGES;
+    // the tile in stage s has landed
+    auto landed = [&](int s) {
+      if (!bar_wait_or_give_up(&s_bar[warp][s], (phases >> s) & 1)) gave_up = true;
+      phases ^= 1u << s;
+    };
 #pragma unroll
-    for (int i = 0; i < P; ++i) issue(i, i);
+    for (int i = 0; i < STAGES; ++i) issue(i, i);
+    if (tid == 0) s_any_bad = 0;
+    if (rq.fresh > 1)
+      for (int i = tid; i < 3 * D; i += SP_THREADS) (&s_bad[0][0])[i] = 0x7FFFFFFF;
 
     // ---- q of the item into shared memory in the products' type; rows that do not exist are zero
     {
@@ -299,33 +354,33 @@ __global__ void __launch_bounds__(SP_THREADS, NT == 1 ? SP_CTAS : 2) attend_spli
     // token of accumulator row (c >> 1) of tile tok0
     auto token_of = [&](int half) { return PACKED ? 4 * (g >> 1) + (g & 1) + 2 * half : g + 8 * half; };
 
-    // o += V^T p for one tile; with `limit`, tokens from limit on count as zero whatever they hold
-    auto pv = [&](const unsigned char* st, u32 st_addr, const u32 (&pb)[NT][2], int tok0, int limit, bool mask) {
+    // o += V^T p for one tile
+    auto pv = [&](const unsigned char* st, u32 st_addr, const u32 (&pb)[NT][2]) {
       if (PACKED) {
         const unsigned char* vt = st + tile_bytes(D);
-        u32 sc = *reinterpret_cast<const u32*>(vt + 8 * D + (D == 128 ? g : g >> 1) * TILE + 4 * t);
-        if (mask) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (tok0 + 4 * t + i >= limit) sc &= ~(0xFFu << (8 * i));
-        }
+        const u32 sc = *reinterpret_cast<const u32*>(vt + 8 * D + (D == 128 ? g : g >> 1) * TILE + 4 * t);
         const Deq da = deq_of(e4m3x2_to_half2(sc & 0xFFFFu)), db = deq_of(e4m3x2_to_half2(sc >> 16));
+        constexpr int W = D / 64;                             // words of 8 codes of the lane's elements, per token
+        u32 c[4][W];
 #pragma unroll
-        for (int w = 0; w < D / 64; ++w) {
-          u32 c[4];
+        for (int i = 0; i < 4; ++i) {
+          const int chunk = D == 128 ? g >> 1 : g >> 2, byte = D == 128 ? (g & 1) * 8 : (g & 3) * 4;
+          // a token's place inside its tile, with n = 4 t + i written out
+          const int rho = 256 / D, place = ((4 * t + i) / rho) * 8 + (((i % rho) * (D / 32) + chunk) ^ (2 * t));
+          if (W == 2) {
+            const uint2 two = *reinterpret_cast<const uint2*>(vt + place * 16 + byte);
+            c[i][0] = two.x;
+            c[i][W - 1] = two.y;
+          } else c[i][0] = *reinterpret_cast<const u32*>(vt + place * 16 + byte);
+        }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int chunk = D == 128 ? g >> 1 : g >> 2, byte = D == 128 ? (g & 1) * 8 + 4 * w : (g & 3) * 4;
-            // a token's place inside its tile, with n = 4 t + i written out
-            const int rho = 256 / D, place = ((4 * t + i) / rho) * 8 + (((i % rho) * (D / 32) + chunk) ^ (2 * t));
-            c[i] = *reinterpret_cast<const u32*>(vt + place * 16 + byte);
-          }
+        for (int w = 0; w < W; ++w)
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
             u32 va[4], vb[4];
             const u32 sel = half ? 0x7632u : 0x5410u;
-            deq4(__byte_perm(c[0], c[1], sel), da, va);
-            deq4(__byte_perm(c[2], c[3], sel), db, vb);
+            deq4(__byte_perm(c[0][w], c[1][w], sel), da, mg, va);
+            deq4(__byte_perm(c[2][w], c[3][w], sel), db, mg, vb);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
               const u32 av[4] = {va[2 * i], va[2 * i + 1], vb[2 * i], vb[2 * i + 1]};
@@ -333,7 +388,6 @@ __global__ void __launch_bounds__(SP_THREADS, NT == 1 ? SP_CTAS : 2) attend_spli
               for (int n = 0; n < NT; ++n) mma16816<F16>(o[n][4 * w + 2 * half + i], av, pb[n]);
             }
           }
-        }
       } else {
         const u32 vt = st_addr + TILE * D * 2;
 #pragma unroll
@@ -342,119 +396,106 @@ __global__ void __launch_bounds__(SP_THREADS, NT == 1 ? SP_CTAS : 2) attend_spli
           const int row = (lane & 7) + ((lane >> 4) & 1) * 8, chunk = 2 * i + ((lane >> 3) & 1);
           u32 av[4];
           ldsm4_t(av, vt + row * (D * 2) + ((chunk ^ (row & 7)) * 16));
-          if (mask) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const int tok = tok0 + 2 * t + (c >> 1) * 8;
-              if (tok >= limit) av[c] = 0;
-              else if (tok + 1 >= limit) av[c] &= 0xFFFFu;
-            }
-          }
 #pragma unroll
           for (int n = 0; n < NT; ++n) mma16816<F16>(o[n][i], av, pb[n]);
         }
       }
     };
-    // does V of this tile hold an infinity or a NaN
-    auto odd_values = [&](const unsigned char* st) {
-      bool odd = false;
+    // V of a tile that not all rows see whole.  A weight of zero does not hide an infinity or a NaN: tokens behind the last row's position
+    // count as zero (a 16-bit tile has zeros there already), and what is not finite in tokens that only some rows see is taken out
+    // here and put into the sums of the rows that see it when the warps are joined.
+    auto mend = [&](unsigned char* st, int tok0) {
       if (PACKED) {
-        const u32* s = reinterpret_cast<const u32*>(st + tile_bytes(D) + 8 * D);
-#pragma unroll
-        for (int i = lane; i < D / 4; i += 32)
-#pragma unroll
-          for (int b = 0; b < 4; ++b) odd |= ((s[i] >> (8 * b)) & 0x7Fu) == 0x7Fu;
-      } else {
-        const u32* s = reinterpret_cast<const u32*>(st + TILE * D * 2);
-        const u32 ex = F16 ? 0x7C00u : 0x7F80u;
-        for (int i = lane; i < TILE * D / 2; i += 32) odd |= (s[i] & ex) == ex || ((s[i] >> 16) & ex) == ex;
+        unsigned char* sc = st + tile_bytes(D) + 8 * D;
+        for (int i = lane; i < TILE * (D / GROUP); i += 32) {
+          const int tok = tok0 + i % TILE, gr = i / TILE;
+          if (tok >= keys) sc[i] = 0;
+          else if (rq.fresh > 1 && (sc[i] & 0x7F) == 0x7F) {
+            sc[i] = 0;
+            s_any_bad = 1;
+            for (int d = 0; d < GROUP; ++d) atomicMin(&s_bad[0][gr * GROUP + d], tok);
+          }
+        }
+      } else if (rq.fresh > 1) {
+        constexpr u32 EX = F16 ? 0x7C00u : 0x7F80u, MANT = F16 ? 0x03FFu : 0x007Fu;
+        unsigned short* v = reinterpret_cast<unsigned short*>(st + TILE * D * 2);
+        for (int i = lane; i < TILE * D; i += 32) {
+          const int n = i / D, d = i % D, at = n * D + (((d >> 3) ^ (n & 7)) << 3) + (d & 7);
+          const u32 x = v[at];
+          if ((x & EX) == EX) {
+            v[at] = 0;
+            s_any_bad = 1;
+            atomicMin(&s_bad[(x & MANT) ? 0 : (x & 0x8000u) ? 2 : 1][d], tok0 + n);
+          }
+        }
       }
-      return __any_sync(FULL, odd);
+      __syncwarp();
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");        // the stage's next tile comes through the async proxy
     };
 
-    // ---- the tiles, STEP at a time
-    int s0 = 0;                                               // stage of tile i
-    for (int i = 0; i < n_tiles; i += STEP) {
-      cp_wait<STAGES - STEP>();
-      __syncwarp();
-      float sc[STEP][NT][4];
-      bool held[STEP];
+    // s = q . k for one tile (not yet scaled)
+    auto qk = [&](const unsigned char* st, u32 st_addr, float (&sc)[NT][4]) {
 #pragma unroll
-      for (int k = 0; k < STEP; ++k) {
-        const int s = s0 + k;
-        const unsigned char* st = ring + s * STAGE;
-        const int tok0 = (ua + i + k) * UNIT + warp * TILE;
-        const u32 rows_in = PACKED ? ((seen_bits >> s) & 1 ? 0xFFFFu : 0u) : __ballot_sync(FULL, (seen_bits >> s) & 1) & 0xFFFFu;
-        held[k] = i + k < n_tiles && rows_in != 0;
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int c = 0; c < 4; ++c) sc[n][c] = 0.0f;
+      if (PACKED) {
+        const int n0 = token_of(0), n1 = token_of(1);
+        __align__(16) u32 c0[D / 32], c1[D / 32];
+        u32 z0, z1;
+        if (D == 128) {
+          *reinterpret_cast<uint4*>(c0) = *reinterpret_cast<const uint4*>(st + code_place(D, n0, t) * 16);
+          *reinterpret_cast<uint4*>(c1) = *reinterpret_cast<const uint4*>(st + code_place(D, n1, t) * 16);
+          z0 = e4m3x2_to_half2(*reinterpret_cast<const unsigned short*>(st + 8 * D + n0 * 8 + 2 * t));
+          z1 = e4m3x2_to_half2(*reinterpret_cast<const unsigned short*>(st + 8 * D + n1 * 8 + 2 * t));
+        } else {
+          *reinterpret_cast<uint2*>(c0) = *reinterpret_cast<const uint2*>(st + code_place(D, n0, t >> 1) * 16 + (t & 1) * 8);
+          *reinterpret_cast<uint2*>(c1) = *reinterpret_cast<const uint2*>(st + code_place(D, n1, t >> 1) * 16 + (t & 1) * 8);
+          z0 = e4m3x2_to_half2(st[8 * D + n0 * 4 + t]);
+          z1 = e4m3x2_to_half2(st[8 * D + n1 * 4 + t]);
+        }
 #pragma unroll
-          for (int c = 0; c < 4; ++c) sc[k][n][c] = 0.0f;
-        if (held[k]) {
-          if (PACKED) {
-            const int n0 = token_of(0), n1 = token_of(1);
-            __align__(16) u32 c0[D / 32], c1[D / 32];
-            u32 z0, z1;
-            if (D == 128) {
-              *reinterpret_cast<uint4*>(c0) = *reinterpret_cast<const uint4*>(st + code_place(D, n0, t) * 16);
-              *reinterpret_cast<uint4*>(c1) = *reinterpret_cast<const uint4*>(st + code_place(D, n1, t) * 16);
-              z0 = e4m3x2_to_half2(*reinterpret_cast<const unsigned short*>(st + 8 * D + n0 * 8 + 2 * t));
-              z1 = e4m3x2_to_half2(*reinterpret_cast<const unsigned short*>(st + 8 * D + n1 * 8 + 2 * t));
-            } else {
-              *reinterpret_cast<uint2*>(c0) = *reinterpret_cast<const uint2*>(st + code_place(D, n0, t >> 1) * 16 + (t & 1) * 8);
-              *reinterpret_cast<uint2*>(c1) = *reinterpret_cast<const uint2*>(st + code_place(D, n1, t >> 1) * 16 + (t & 1) * 8);
-              z0 = e4m3x2_to_half2(st[8 * D + n0 * 4 + t]);
-              z1 = e4m3x2_to_half2(st[8 * D + n1 * 4 + t]);
-            }
+        for (int gr = 0; gr < D / 64; ++gr) {                 // the lane's scale groups of 16 elements
+          const u32 sel = gr ? 0x3232u : 0x1010u;
+          const Deq d0 = deq_of(__byte_perm(z0, z0, sel)), d1 = deq_of(__byte_perm(z1, z1, sel));
 #pragma unroll
-            for (int gr = 0; gr < D / 64; ++gr) {             // the lane's scale groups of 16 elements
-              const u32 sel = gr ? 0x3232u : 0x1010u;
-              const Deq d0 = deq_of(__byte_perm(z0, z0, sel)), d1 = deq_of(__byte_perm(z1, z1, sel));
+          for (int w = 2 * gr; w < 2 * gr + 2; ++w) {
+            u32 v0[4], v1[4];
+            deq4(c0[w], d0, mg, v0);
+            deq4(c1[w], d1, mg, v1);
 #pragma unroll
-              for (int w = 2 * gr; w < 2 * gr + 2; ++w) {
-                u32 v0[4], v1[4];
-                deq4(c0[w], d0, v0);
-                deq4(c1[w], d1, v1);
+            for (int b = 0; b < 2; ++b) {
+              const u32 av[4] = {v0[2 * b], v1[2 * b], v0[2 * b + 1], v1[2 * b + 1]};
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                  const u32 av[4] = {v0[2 * b], v1[2 * b], v0[2 * b + 1], v1[2 * b + 1]};
-#pragma unroll
-                  for (int n = 0; n < NT; ++n) mma16816<F16>(sc[k][n], av, qb[n][2 * w + b]);
-                }
-              }
-            }
-          } else {
-            const u32 sa = ring_addr + s * STAGE;
-#pragma unroll
-            for (int kk = 0; kk < KS; ++kk) {
-              const int row = (lane & 7) + ((lane >> 3) & 1) * 8, chunk = 2 * kk + (lane >> 4);
-              u32 av[4];
-              ldsm4(av, sa + row * (D * 2) + ((chunk ^ (row & 7)) * 16));
-#pragma unroll
-              for (int n = 0; n < NT; ++n) mma16816<F16>(sc[k][n], av, qb[n][kk]);
+              for (int n = 0; n < NT; ++n) mma16816<F16>(sc[n], av, qb[n][2 * w + b]);
             }
           }
         }
-        const bool whole = held[k] && rows_in == 0xFFFFu && tok0 + TILE <= all_see;
+      } else {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int kk = 0; kk < KS; ++kk) {
+          const int row = (lane & 7) + ((lane >> 3) & 1) * 8, chunk = 2 * kk + (lane >> 4);
+          u32 av[4];
+          ldsm4(av, st_addr + row * (D * 2) + ((chunk ^ (row & 7)) * 16));
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            sc[k][n][c] *= qs[n][c & 1];
-            if (!whole) {
-              const int in = token_of(c >> 1);
-              if (!held[k] || tok0 + in >= see[n][c & 1] || !((rows_in >> in) & 1)) sc[k][n][c] = -INFINITY;
-            }
-          }
+          for (int n = 0; n < NT; ++n) mma16816<F16>(sc[n], av, qb[n][kk]);
+        }
       }
-      // running maximum over the step, then the weights
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) sc[n][c] *= qs[n][c & 1];
+    };
+    // running maximum and weights of K tiles, then their values; held: tiles that are there
+    auto accumulate = [&](auto& sc, int s0, auto held) {
+      constexpr int K = sizeof(sc) / sizeof(sc[0]);
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           float x = m[n][c];
 #pragma unroll
-          for (int k = 0; k < STEP; ++k) x = fmaxf(x, fmaxf(sc[k][n][c], sc[k][n][c + 2]));
+          for (int k = 0; k < K; ++k) x = fmaxf(x, fmaxf(sc[k][n][c], sc[k][n][c + 2]));
 #pragma unroll
           for (int w = 4; w < 32; w <<= 1) x = fmaxf(x, __shfl_xor_sync(FULL, x, w));
           if (__any_sync(FULL, x != m[n][c])) {
@@ -465,66 +506,83 @@ __global__ void __launch_bounds__(SP_THREADS, NT == 1 ? SP_CTAS : 2) attend_spli
             for (int i2 = 0; i2 < MT; ++i2) { o[n][i2][c] *= f; o[n][i2][c + 2] *= f; }
           }
         }
+      float ref[NT][2];
 #pragma unroll
-      for (int k = 0; k < STEP; ++k) {
-        if (!held[k]) continue;
-        const int s = s0 + k;
-        const int tok0 = (ua + i + k) * UNIT + warp * TILE;
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) ref[n][c] = m[n][c] == -INFINITY ? 0.0f : m[n][c];
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        if (!held(k)) continue;
         u32 pb[NT][2];
-        float p[NT][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
+          float p[4];
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            p[n][c] = exp2_fast(sc[k][n][c] - (m[n][c & 1] == -INFINITY ? 0.0f : m[n][c & 1]));
-            l[n][c & 1] += p[n][c];
+            p[c] = exp2_fast(sc[k][n][c] - ref[n][c & 1]);
+            l[n][c & 1] += p[c];
           }
-          pb[n][0] = transpose8x8(pack2<F16>(p[n][0], p[n][1]));
-          pb[n][1] = transpose8x8(pack2<F16>(p[n][2], p[n][3]));
+          pb[n][0] = transpose8x8(pack2<F16>(p[0], p[1]));
+          pb[n][1] = transpose8x8(pack2<F16>(p[2], p[3]));
         }
-        const unsigned char* st = ring + s * STAGE;
-        const u32 sa = ring_addr + s * STAGE;
-        if (tok0 + TILE <= all_see) pv(st, sa, pb, tok0, 0, false);
-        else if (rq.fresh == 1 || !odd_values(st)) pv(st, sa, pb, tok0, keys, true);
-        else {
-          // a weight of zero times an infinity is not zero: one new token's rows at a time, V cut off at what they see
-          for (int fr = row_base / a.group; fr <= (row_base + rows - 1) / a.group; ++fr) {
-            u32 pf[NT][2];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              const bool own = (row_base + 8 * n + g) / a.group == fr;     // operand column g
-              pf[n][0] = own ? pb[n][0] : 0;
-              pf[n][1] = own ? pb[n][1] : 0;
-            }
-            const int lim = rq.pos0 + fr + 1;
-            // columns of other rows would still meet what this limit lets through: their sums are kept aside
-            float keep[NT][MT][4];
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-              for (int i2 = 0; i2 < MT; ++i2)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) keep[n][i2][c] = o[n][i2][c];
-            pv(st, sa, pf, tok0, lim < keys ? lim : keys, true);
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-              for (int c = 0; c < 4; ++c)
-                if ((row_base + 8 * n + 2 * t + (c & 1)) / a.group != fr) {
-#pragma unroll
-                  for (int i2 = 0; i2 < MT; ++i2) o[n][i2][c] = keep[n][i2][c];
-                }
-          }
-        }
+        pv(ring + (s0 + k) * STAGE, ring_addr + (s0 + k) * STAGE, pb);
       }
+    };
+
+    // ---- the tiles, STEP at a time: steps that every row sees whole, then the rest with masks
+    int s0 = 0, i = 0;                                        // stage of tile i
+    auto next = [&]() {
       __syncwarp();
 #pragma unroll
       for (int k = 0; k < STEP; ++k) issue(i + STAGES + k, s0 + k);
       s0 += STEP;
       if (s0 == STAGES) s0 = 0;
+      i += STEP;
+    };
+    const u32 all_held = (1u << STEP) - 1u;
+    while (i < n_tiles) {
+      if (!PACKED) {
+        cp_wait<STAGES - STEP>();
+        __syncwarp();
+      }
+      const int tok_end = (ua + i + STEP - 1) * UNIT + warp * TILE + TILE;
+      const bool there = PACKED ? ((seen_bits >> s0) & all_held) == all_held : __all_sync(FULL, ((seen_bits >> s0) & all_held) == all_held);
+      float sc[STEP][NT][4];
+      if (i + STEP <= n_tiles && there && tok_end <= all_see) {
+#pragma unroll
+        for (int k = 0; k < STEP; ++k) {
+          if (PACKED) landed(s0 + k);
+          qk(ring + (s0 + k) * STAGE, ring_addr + (s0 + k) * STAGE, sc[k]);
+        }
+        accumulate(sc, s0, [](int) { return true; });
+        next();
+        continue;
+      }
+      u32 held = 0;
+#pragma unroll
+      for (int k = 0; k < STEP; ++k) {
+        const int s = s0 + k, tok0 = (ua + i + k) * UNIT + warp * TILE;
+        if (PACKED && ((seen_bits >> s) & 1)) landed(s);
+        const u32 rows_in = PACKED ? ((seen_bits >> s) & 1 ? 0xFFFFu : 0u) : __ballot_sync(FULL, (seen_bits >> s) & 1) & 0xFFFFu;
+        if (i + k < n_tiles && rows_in != 0) {
+          held |= 1u << k;
+          mend(ring + s * STAGE, tok0);
+          qk(ring + s * STAGE, ring_addr + s * STAGE, sc[k]);
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const int in = token_of(c >> 1);
+            if (!((held >> k) & 1) || tok0 + in >= see[n][c & 1] || !((rows_in >> in) & 1)) sc[k][n][c] = -INFINITY;
+          }
+      }
+      accumulate(sc, s0, [&](int k) { return (held >> k) & 1; });
+      next();
     }
     cp_wait<0>();
-    if (bounds && a.status) atomicOr(a.status, PTSTORE_S_BOUNDS);
+    if ((bounds || gave_up) && a.status) atomicOr(a.status, (bounds ? PTSTORE_S_BOUNDS : 0) | (gave_up ? PTSTORE_S_TIMEOUT : 0));
 
     // ---- join the four warps
 #pragma unroll
@@ -574,6 +632,16 @@ __global__ void __launch_bounds__(SP_THREADS, NT == 1 ? SP_CTAS : 2) attend_spli
       acc[e] = 0.0f;
 #pragma unroll
       for (int w = 0; w < SP_WARPS; ++w) acc[e] += s_o[(w * NQ + row) * OS + e0 + e];
+    }
+    if (s_any_bad && row < rows) {
+      const i64 p = (i64)rq.pos0 + (row_base + row) / a.group;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const bool nan = s_bad[0][e0 + e] <= p, pos = s_bad[1][e0 + e] <= p, neg = s_bad[2][e0 + e] <= p;
+        if (nan || (pos && neg)) acc[e] = NAN;
+        else if (pos) acc[e] += INFINITY;
+        else if (neg) acc[e] -= INFINITY;
+      }
     }
     const i64 first_cta = item_begin / per, last_cta = (item_end - 1) / per;
     bool write = true;

@@ -29,46 +29,53 @@ __device__ __forceinline__ void raise_status(uint32_t* status, uint32_t bits) {
   if (status) atomicOr(status, bits);
 }
 
+__device__ __forceinline__ u64 plus(u64 a, u64 b) { return a + b; }
+__device__ __forceinline__ uint32_t plus(uint32_t a, uint32_t b) {        // saturates
+  const uint32_t s = a + b;
+  return s < a ? UINT_MAX : s;
+}
+
 // Exclusive prefix sums over a chunk: v[i] belongs to request i * THREADS + threadIdx.x of it (so that loads are coalesced and the
 // warps' scans of the rows are independent), rows of them are in use.  total in every thread.  Called by all threads.
-__device__ __forceinline__ void scan_chunk(u64 (&v)[ITEMS], int rows, u64* s_tot /*[ITEMS * 32]*/, u64& total) {
+template <typename T>
+__device__ __forceinline__ void scan_chunk(T (&v)[ITEMS], int rows, T* s_tot /*[ITEMS * 32 + 1]*/, T& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   __syncthreads();                           // the previous scan's readers are done with s_tot
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i)
     if (i < rows) {
-      const u64 own = v[i];
-      u64 x = own;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const u64 y = __shfl_up_sync(0xFFFFFFFFu, x, o);
-        if (lane >= o) x += y;
+        const T y = __shfl_up_sync(0xFFFFFFFFu, v[i], o);
+        if (lane >= o) v[i] = plus(v[i], y);
       }
-      if (lane == 31) s_tot[i * 32 + warp] = x;
-      v[i] = x - own;
+      if (lane == 31) s_tot[i * 32 + warp] = v[i];
+      v[i] = __shfl_up_sync(0xFFFFFFFFu, v[i], 1);
+      if (lane == 0) v[i] = 0;
     }
   __syncthreads();
   if (warp == 0) {                           // lane l: the totals l * rows .. of the rows * 32 in order
-    u64 sum = 0;
-    for (int k = 0; k < rows; ++k) sum += s_tot[lane * rows + k];
-    u64 x = sum;
+    T sum = 0;
+    for (int k = 0; k < rows; ++k) sum = plus(sum, s_tot[lane * rows + k]);
+    T x = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const u64 y = __shfl_up_sync(0xFFFFFFFFu, x, o);
-      if (lane >= o) x += y;
+      const T y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+      if (lane >= o) x = plus(x, y);
     }
-    u64 run = x - sum;
+    if (lane == 31) s_tot[ITEMS * 32] = x;
+    T run = __shfl_up_sync(0xFFFFFFFFu, x, 1);
+    if (lane == 0) run = 0;
     for (int k = 0; k < rows; ++k) {
-      const u64 t = s_tot[lane * rows + k];
+      const T t = s_tot[lane * rows + k];
       s_tot[lane * rows + k] = run;
-      run += t;
+      run = plus(run, t);
     }
-    if (lane == 31) s_tot[ITEMS * 32] = run;
   }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < ITEMS; ++i)
-    if (i < rows) v[i] += s_tot[i * 32 + warp];
+    if (i < rows) v[i] = plus(v[i], s_tot[i * 32 + warp]);
   total = s_tot[ITEMS * 32];
 }
 
@@ -99,8 +106,8 @@ __device__ __forceinline__ void want(const Assign& a, int r, int& held, int& nee
   const int h = a.held ? a.held[r] : 0, len = a.lengths[r];
   held = h < 0 ? 0 : h > a.max_blocks ? a.max_blocks : h;
   if (held != h || len < 0) bad = PTSTORE_S_BOUNDS;
-  const i64 n = len <= 0 ? 0 : ((i64)len + a.block_tokens - 1) / a.block_tokens;
-  if (n > a.max_blocks) { need = held; bad = PTSTORE_S_BOUNDS; } else need = (int)n;
+  const uint32_t n = len <= 0 ? 0 : (uint32_t)(len - 1) / (uint32_t)a.block_tokens + 1;
+  if (n > (uint32_t)a.max_blocks) { need = held; bad = PTSTORE_S_BOUNDS; } else need = (int)n;
 }
 
 __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS) assign_blocks_kernel(Assign a) {
@@ -227,7 +234,7 @@ __device__ __forceinline__ void done_new(const MapSlots& m, int r, int& done, in
 
 __global__ void __launch_bounds__(THREADS) map_slots_kernel(MapSlots m) {
   extern __shared__ uint32_t s_dyn[];
-  __shared__ u64 s_tot[ITEMS * 32 + 1];
+  __shared__ uint32_t s_tot[ITEMS * 32 + 1];
   const int cap_items = m.R < CHUNK ? m.R : CHUNK;
   uint32_t* s_first = s_dyn;                 // exclusive prefix sums inside the chunk
   int* s_done = reinterpret_cast<int*>(s_dyn + cap_items);
@@ -237,7 +244,7 @@ __global__ void __launch_bounds__(THREADS) map_slots_kernel(MapSlots m) {
   i64 base_tok = 0;
   for (int base = 0; base < m.R; base += CHUNK) {
     const int n = m.R - base < CHUNK ? m.R - base : CHUNK;
-    u64 v[ITEMS], sum;
+    uint32_t v[ITEMS], sum;                  // sums saturate at 2^32 - 1: no token beyond max_tokens < 2^31 is listed
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
       v[i] = 0;
@@ -246,19 +253,18 @@ __global__ void __launch_bounds__(THREADS) map_slots_kernel(MapSlots m) {
         int done, fresh;
         done_new(m, base + k, done, fresh, bad);
         s_done[k] = done;
-        v[i] = (u64)fresh;
+        v[i] = (uint32_t)fresh;
       }
     }
     scan_chunk(v, rows, s_tot, sum);
-    const i64 total = (i64)sum;
+    const i64 total = sum;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
       const int k = i * THREADS + threadIdx.x;
       if (i < rows && k < n) {
-        // a chunk's sums can pass 32 bits only where they pass max_tokens too; those are never searched for
-        s_first[k] = v[i] > UINT_MAX ? UINT_MAX : (uint32_t)v[i];
+        s_first[k] = v[i];
         if (blockIdx.x == 0) {
-          const i64 at = base_tok + (i64)v[i];
+          const i64 at = base_tok + v[i];
           m.offsets[base + k] = at > INT_MAX ? INT_MAX : (int)at;
         }
       }
