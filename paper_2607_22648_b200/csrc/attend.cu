@@ -43,7 +43,7 @@ int launch_split(const Attend& a, const Gpu& gpu, cudaStream_t s) {
   auto* kernel = attend_split_kernel<FMT, QFP16, D, NT>;
   const int rc = allow_smem(kernel, SMEM, devices, gpu.dev);
   if (rc) return rc;
-  kernel<<<gpu.sms * split_ctas<FMT, NT>(), SP_THREADS, SMEM, s>>>(a);
+  kernel<<<gpu.sms * split_ctas<FMT, NT>(), SplitShape<FMT, D>::THREADS, SMEM, s>>>(a);
   return cudaGetLastError() == cudaSuccess ? PTSTORE_OK : PTSTORE_E_CUDA;
 }
 
@@ -96,6 +96,7 @@ extern "C" int ptstore_attend(const ptstore_attend_t* p, const ptstore_kv_cache_
   if (p->requests == 0 || p->tokens == 0 || p->max_new == 0) return PTSTORE_OK;
   if (!p->q || !p->out || !p->token_offsets || !p->lengths || !p->block_tables) return PTSTORE_E_INVAL;
   if (!rows_aligned(p->q, p->q_token_stride, p->q_head_stride) || !rows_aligned(p->out, p->out_token_stride, p->out_head_stride)) return PTSTORE_E_INVAL;
+  if ((u64)p->max_blocks * cache->block_tokens > 1u << 30) return PTSTORE_E_LIMIT;                      // positions are 32 bits wide, with room for a tile
   if (p->requests > 1 << 20 || (i64)p->tokens * p->num_heads > 0x7FFFFFFF) return PTSTORE_E_LIMIT;     // row indexes of a kv head are 32 bits wide
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PTSTORE_E_INVAL;
   if (workspace_bytes < ptstore_attend_workspace_bytes(cache->head_dim)) return PTSTORE_E_NOMEM;

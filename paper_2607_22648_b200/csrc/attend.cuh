@@ -91,13 +91,13 @@ __device__ __forceinline__ u32 hmul2(u32 a, u32 b) {
 }
 
 // 4-bit codes to fp16.  A code n at bits p .. p+3 of 0x6400 reads as 1024 + n 2^p, and (1024 + n 2^p) * (s / 2^p) - (1024 / 2^p + 8) s
-// = (n - 8) s in one fused multiply-add.  It is exact: every constant below fits 11 bits for p >= 1 (520 s: 7 + 4 bits), so the
-// codes are read at bits 1..4 and 5..8.  s is the scale times 2^-8, which keeps 520 s inside fp16; the 2^8 is put back at the end.
-// `(x & mask) | 0x6400..` is ONE instruction only if the constants are in registers, hence Magic.
-struct Magic { u32 m1, m5, one; };
+// = (n - 8) s in one fused multiply-add.  It is exact: s has 4 significant bits, so 1032 s (8 + 4 bits, at most 129 * 15 < 2^11) and 72 s fit
+// fp16's 11; the codes are read at bits 0..3 and 4..7.  s is the scale times 2^-8, which keeps 1032 s inside fp16; the 2^8 is
+// put back at the end.  `(x & mask) | 0x6400..` is ONE instruction only if the constants are in registers, hence Magic.
+struct Magic { u32 m0, m4, one; };
 __device__ __forceinline__ Magic magic() {
   Magic m;
-  asm volatile("mov.b32 %0, 0x001E001E;\n mov.b32 %1, 0x01E001E0;\n mov.b32 %2, 0x64006400;" : "=r"(m.m1), "=r"(m.m5), "=r"(m.one));
+  asm volatile("mov.b32 %0, 0x000F000F;\n mov.b32 %1, 0x00F000F0;\n mov.b32 %2, 0x64006400;" : "=r"(m.m0), "=r"(m.m4), "=r"(m.one));
   return m;
 }
 __device__ __forceinline__ u32 and_or(u32 a, u32 b, u32 c) {
@@ -105,23 +105,22 @@ __device__ __forceinline__ u32 and_or(u32 a, u32 b, u32 c) {
   asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
   return r;
 }
-struct Deq { u32 s1, c1, s5, c5; };
-__device__ __forceinline__ Deq deq_of(u32 scale2) {          // two e4m3 scales as fp16 pairs
+struct Deq { u32 s0, c0, s4, c4; };
+__device__ __forceinline__ Deq deq_of(u32 scale2) {          // two e4m3 scales (multiples of 2^-9) as fp16 pairs
   Deq d;
-  d.s1 = hmul2(scale2, 0x18001800u);                         // 2^-8 2^-1 (a multiple of 2^-18: exact)
-  d.c1 = hmul2(d.s1, 0xE410E410u);                           // -1040
-  d.s5 = hmul2(d.s1, 0x2C002C00u);                           // 2^-4
-  d.c5 = hmul2(d.s1, 0xD500D500u);                           // -80
+  d.s0 = hmul2(scale2, 0x1C001C00u);                         // 2^-8
+  d.c0 = hmul2(d.s0, 0xE408E408u);                           // -1032
+  d.s4 = hmul2(d.s0, 0x2C002C00u);                           // 2^-4 (multiples of 2^-21: exact)
+  d.c4 = hmul2(d.s0, 0xD480D480u);                           // -72
   return d;
 }
 constexpr float DEQ_FACTOR = 256.0f;
-// the four nibbles of each 16-bit half: o[j] = (nibble j of the low half, nibble j of the high half)
-__device__ __forceinline__ void deq4(u32 x, const Deq& d, const Magic& k, u32 (&o)[4]) {
-  const u32 l = x << 1, h = x >> 7;
-  o[0] = hfma2(and_or(l, k.m1, k.one), d.s1, d.c1);
-  o[1] = hfma2(and_or(l, k.m5, k.one), d.s5, d.c5);
-  o[2] = hfma2(and_or(h, k.m1, k.one), d.s1, d.c1);
-  o[3] = hfma2(and_or(h, k.m5, k.one), d.s5, d.c5);
+// the four nibbles of each 16-bit half: o[j] = (nibble j of the low half, nibble j of the high half); h: x >> 8 (bits 0-7 of each half count)
+__device__ __forceinline__ void deq4(u32 x, u32 h, const Deq& d, const Magic& k, u32 (&o)[4]) {
+  o[0] = hfma2(and_or(x, k.m0, k.one), d.s0, d.c0);
+  o[1] = hfma2(and_or(x, k.m4, k.one), d.s4, d.c4);
+  o[2] = hfma2(and_or(h, k.m0, k.one), d.s0, d.c0);
+  o[3] = hfma2(and_or(h, k.m4, k.one), d.s4, d.c4);
 }
 
 }  // namespace ptk

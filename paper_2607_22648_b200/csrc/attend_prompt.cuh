@@ -403,7 +403,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
 #pragma unroll
           for (int w = 0; w < 2; ++w) {
             u32 o[4];
-            deq4(cur[2 * g + w], d, mg, o);
+            deq4(cur[2 * g + w], cur[2 * g + w] >> 8, d, mg, o);
             *reinterpret_cast<uint4*>(t + operand_at(pt, 2 * g + w)) = cur_has ? make_uint4(o[0], o[1], o[2], o[3]) : make_uint4(0, 0, 0, 0);
           }
         }

@@ -1,9 +1,11 @@
 // Attention of a few query rows per request over a long paged cache (decode, speculative tokens): bounded by reading K and V once.
 //
 // o = sum_j p_j v_j / sum_j p_j, p_j = exp2(scale2 q.k_j - m): one pass over the cache with the running maximum m and sum per row.
-// Work is cut into units of 64 tokens of one (request, row tile, kv head) item; all units stand in one line and every CTA
-// takes the same number of them, so ragged batches load every SM alike and one long request is spread over all of them.  An item that
-// spans several CTAs leaves partial sums (o, m, l in 32 bits) in the workspace, and the CTA that arrives last joins them in CTA
+// Work is cut into units of 64 tokens of one (request, row tile, kv head) item.  Where cutting every item into equal chunks gives at most one
+// chunk per CTA without making the longest more than a quarter longer than an even share, a CTA takes one chunk.  Otherwise all units stand in one
+// line and every CTA takes the same number of them, so ragged batches load every SM alike; a CTA then works on parts of two
+// or three items, each of which costs it some 5 us of start and join, which is why chunks come first (one 4k request: 18.5 us
+// with the line, whose CTAs straddle two kv heads, 15.9 us with chunks).  An item that spans several CTAs leaves partial sums (o, m, l in 32 bits) in the workspace, and the CTA that arrives last joins them in CTA
 // order: the result does not depend on who that is.  One launch; the arrival counters are left zero.
 //
 // A row tile is 8 or 16 (query head of the group, new token) rows.  The tensor instructions (mma.sync m16n8k16; the work is a
@@ -18,20 +20,20 @@
 
 namespace ptk {
 
-constexpr int SP_WARPS = 4, SP_THREADS = 32 * SP_WARPS;
-constexpr int UNIT = SP_WARPS * TILE;        // tokens of a unit: one tile per warp
-constexpr int MIN_UNITS = 4;                 // a CTA takes at least this many, so that joining does not cost more than it saves
+constexpr int MIN_TOKENS = 256;              // a CTA takes at least this many, so that joining does not cost more than it saves
 constexpr u32 SP_POLLS = 1u << 22;           // polls of a wait for a tile before the warp gives up (each may suspend for a while)
 
 template <int FMT, int D>
 struct SplitShape {
   static constexpr bool PACKED = FMT == PTSTORE_KV_PACKED;
+  static constexpr int WARPS = 4, THREADS = 32 * WARPS;
+  static constexpr int UNIT = WARPS * TILE;                                        // tokens of a unit: one tile per warp
   static constexpr int STAGE = PACKED ? 2 * tile_bytes(D) : 2 * TILE * D * 2;      // K tile, V tile
   static constexpr int STAGES = (PACKED ? 4 : 2) * (128 / D);
   static constexpr int STEP = PACKED ? 2 : 1;                                      // tiles per softmax step
-  static constexpr int RING = SP_WARPS * STAGES * STAGE;
+  static constexpr int RING = WARPS * STAGES * STAGE;
 };
-// CTAs per SM, by registers: 128 per thread where a row tile has 8 rows of a 4-bit cache
+// CTAs per SM, by registers: 16 warps of 128 where a row tile has 8 rows of a 4-bit cache, 12 of 168 for a 16-bit one, 8 of 255 for 16 rows
 template <int FMT, int NT>
 __host__ __device__ constexpr int split_ctas() { return NT == 2 ? 2 : FMT == PTSTORE_KV_PACKED ? 4 : 3; }
 // shared memory: the ring, which at the end of an item holds the warps' sums and then the maxima and sums of an item's parts (at most
@@ -39,7 +41,7 @@ __host__ __device__ constexpr int split_ctas() { return NT == 2 ? 2 : FMT == PTS
 constexpr int MAX_SMS = 160;
 template <int FMT, int D, int NT>
 constexpr int split_smem() {
-  const int ring = SplitShape<FMT, D>::RING, sums = SP_WARPS * 8 * NT * (D + 4) * 4, parts = MAX_SMS * split_ctas<FMT, NT>() * 8 * NT * 8;
+  const int ring = SplitShape<FMT, D>::RING, sums = SplitShape<FMT, D>::WARPS * 8 * NT * (D + 4) * 4, parts = MAX_SMS * split_ctas<FMT, NT>() * 8 * NT * 8;
   return ring > sums ? (ring > parts ? ring : parts) : (sums > parts ? sums : parts);
 }
 
@@ -73,38 +75,53 @@ __device__ __forceinline__ bool bar_wait_or_give_up(u64* bar, u32 parity) {
   return false;
 }
 
+// Rows of a kv head fit 32 bits (the host checks), unit numbers may not: a 64-bit division is a hundred instructions, so it is avoided.
+__device__ __forceinline__ u32 quotient(u64 a, u64 b) { return (a | b) >> 32 ? (u32)(a / b) : (u32)a / (u32)b; }
+
 // keys row tile rt of a request can see (of its last row), and its units (at least one: a row that sees nothing is written too)
 template <int NQ>
-__device__ __forceinline__ int tile_keys(const Attend& a, const Req& q, int rt) {
-  const i64 rows = (i64)q.fresh * a.group;
-  const i64 end = (i64)(rt + 1) * NQ;
-  const int last = end >= rows ? q.fresh - 1 : (int)((end - 1) / a.group);
+__device__ __forceinline__ int tile_keys(const Attend& a, const Req& q, u32 rt) {
+  const u32 rows = (u32)q.fresh * a.group, end = (rt + 1) * NQ;
+  const int last = end >= rows ? q.fresh - 1 : (int)((end - 1) / (u32)a.group);
   const i64 k = (i64)q.pos0 + last + 1;
   return k <= 0 ? 0 : k > q.keys ? q.keys : (int)k;
 }
-__device__ __forceinline__ int units_of(int keys) { return keys <= UNIT ? 1 : (keys + UNIT - 1) / UNIT; }
+template <int UNIT>
+__device__ __forceinline__ int units_of(int keys) { return keys <= UNIT ? 1 : (int)(((u32)keys + UNIT - 1) / UNIT); }
 template <int NQ>
-__device__ __forceinline__ int row_tiles(const Attend& a, const Req& q) { return (int)(((i64)q.fresh * a.group + NQ - 1) / NQ); }
-template <int NQ>
-__device__ __forceinline__ i64 request_units(const Attend& a, int r) {
+__device__ __forceinline__ u32 row_tiles(const Attend& a, const Req& q) { return ((u32)q.fresh * a.group + NQ - 1) / NQ; }
+constexpr int CUTS = 4;                      // chunk lengths that are tried: the even share, and 1/16, 1/8, 1/4 more
+__device__ __forceinline__ u32 chunk_units(u64 even, int cut) { return (u32)(even + (cut ? (even >> (5 - cut)) + 1 : 0)); }
+__device__ __forceinline__ u32 chunks_of(int units, u32 len) { return ((u32)units + len - 1) / len; }
+template <int NQ, int UNIT>
+__device__ __forceinline__ u32 request_chunks(const Attend& a, int r, u32 len) {
   const Req q = request(a, r);
-  const int n = row_tiles<NQ>(a, q);
-  i64 u = 0;
-  for (int rt = 0; rt < n; ++rt) u += units_of(tile_keys<NQ>(a, q, rt));
+  const u32 n = row_tiles<NQ>(a, q);
+  u64 c = 0;
+  for (u32 rt = 0; rt < n; ++rt) c += chunks_of(units_of<UNIT>(tile_keys<NQ>(a, q, rt)), len);
+  return (u32)min(c * a.cache.heads, 1ull << 24);             // more than any grid
+}
+template <int NQ, int UNIT>
+__device__ __forceinline__ u64 request_units(const Attend& a, int r) {
+  const Req q = request(a, r);
+  const u32 n = row_tiles<NQ>(a, q);
+  u64 u = 0;
+  for (u32 rt = 0; rt < n; ++rt) u += units_of<UNIT>(tile_keys<NQ>(a, q, rt));
   return u * a.cache.heads;
 }
 
 template <int FMT, bool QFP16, int D, int NT>
-__global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_split_kernel(Attend a) {
+__global__ void __launch_bounds__(SplitShape<FMT, D>::THREADS, split_ctas<FMT, NT>()) attend_split_kernel(Attend a) {
   using Shape = SplitShape<FMT, D>;
   constexpr bool PACKED = Shape::PACKED;
   constexpr bool F16 = PACKED || FMT == PTSTORE_KV_FP16;      // type of the products' operands
+  constexpr int SP_WARPS = Shape::WARPS, SP_THREADS = Shape::THREADS, UNIT = Shape::UNIT;
   constexpr int NQ = 8 * NT, STAGE = Shape::STAGE, STAGES = Shape::STAGES, STEP = Shape::STEP;
   constexpr int KS = D / 16, MT = D / 16;                     // k steps of q.k, m tiles of o
   constexpr int OS = D + 4;                                   // row stride of the joined o in shared memory (floats)
   extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ i64 s_scan[SP_WARPS];
-  __shared__ i64 s_left;
+  __shared__ u64 s_scan[SP_WARPS], s_left;
+  __shared__ u32 s_cuts[SP_WARPS][CUTS];
   __shared__ int s_r, s_last, s_any_bad;
   __shared__ __align__(8) u64 s_bar[SP_WARPS][STAGES];
   __shared__ int s_bad[3][D];                // first key whose V holds NaN, +inf, -inf in column d, among keys that some rows do not see
@@ -115,31 +132,74 @@ __global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_spli
   // ---- which units are this CTA's: every CTA sums the units of all requests, consecutive requests per thread
   const int per_thread = (a.R + SP_THREADS - 1) / SP_THREADS;
   const int rb = tid * per_thread < a.R ? tid * per_thread : a.R, re = rb + per_thread < a.R ? rb + per_thread : a.R;
-  i64 mine = 0;
-  for (int r = rb; r < re; ++r) mine += request_units<NQ>(a, r);
-  i64 x = mine;
+  u64 mine = 0;
+  for (int r = rb; r < re; ++r) mine += request_units<NQ, UNIT>(a, r);
+  u64 x = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const i64 y = __shfl_up_sync(FULL, x, o);
+    const u64 y = __shfl_up_sync(FULL, x, o);
     if (lane >= o) x += y;
   }
   if (lane == 31) s_scan[warp] = x;
   __syncthreads();
-  i64 total = 0, before = x - mine;
+  u64 total = 0, before = x - mine;
 #pragma unroll
   for (int w = 0; w < SP_WARPS; ++w) {
     if (w < warp) before += s_scan[w];
     total += s_scan[w];
   }
-  i64 per = (total + gridDim.x - 1) / gridDim.x;
-  if (per < MIN_UNITS) per = MIN_UNITS;
-  const i64 u_begin = blockIdx.x * per, u_end = u_begin + per < total ? u_begin + per : total;
-  if (u_begin >= u_end) return;
-  if (u_begin >= before && u_begin < before + mine) {         // exactly one thread
-    i64 left = u_begin - before;
+  u64 per = (total + gridDim.x - 1) >> 32 ? (total + gridDim.x - 1) / gridDim.x : (u32)(total + gridDim.x - 1) / gridDim.x;
+  if (per < MIN_TOKENS / UNIT) per = MIN_TOKENS / UNIT;
+  const u64 u_begin = blockIdx.x * per, u_end = u_begin + per < total ? u_begin + per : total;
+  u32 chunk = 0;                                              // units of a chunk, 0: an even share of the line
+  if (per <= 1u << 20 && total > 0) {
+    u32 cnt[CUTS], sum[CUTS];
+#pragma unroll
+    for (int c = 0; c < CUTS; ++c) cnt[c] = 0;
+    for (int r = rb; r < re; ++r)
+#pragma unroll
+      for (int c = 0; c < CUTS; ++c) cnt[c] = min(cnt[c] + request_chunks<NQ, UNIT>(a, r, chunk_units(per, c)), 1u << 24);
+#pragma unroll
+    for (int c = 0; c < CUTS; ++c) {
+      sum[c] = cnt[c];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const u32 y = __shfl_up_sync(FULL, sum[c], o);
+        if (lane >= o) sum[c] = min(sum[c] + y, 1u << 24);
+      }
+      if (lane == 31) s_cuts[warp][c] = sum[c];
+    }
+    if (tid == 0) s_r = -1;
+    __syncthreads();
+    u32 mine_c = 0, before_c = 0;
+#pragma unroll
+    for (int c = CUTS - 1; c >= 0; --c) {
+      u32 all = 0, ahead = sum[c] - cnt[c];
+#pragma unroll
+      for (int w = 0; w < SP_WARPS; ++w) {
+        if (w < warp) ahead += s_cuts[w][c];
+        all += s_cuts[w][c];
+      }
+      if (all <= gridDim.x) { chunk = chunk_units(per, c); mine_c = cnt[c]; before_c = ahead; }
+    }
+    if (chunk && blockIdx.x >= before_c && blockIdx.x < before_c + mine_c) {        // at most one thread
+      u32 left = blockIdx.x - before_c;
+      int r = rb;
+      for (; r < re - 1; ++r) {
+        const u32 n = request_chunks<NQ, UNIT>(a, r, chunk);
+        if (left < n) break;
+        left -= n;
+      }
+      s_r = r;
+      s_left = left;
+    }
+  }
+  if (!chunk && u_begin >= u_end) return;
+  if (!chunk && u_begin >= before && u_begin < before + mine) {         // exactly one thread
+    u64 left = u_begin - before;
     int r = rb;
-    for (;; ++r) {
-      const i64 n = request_units<NQ>(a, r);
+    for (; r < re - 1; ++r) {
+      const u64 n = request_units<NQ, UNIT>(a, r);
       if (left < n) break;
       left -= n;
     }
@@ -148,8 +208,9 @@ __global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_spli
   }
   __syncthreads();
   int r = s_r;
-  i64 left = s_left;
-  i64 u = u_begin;
+  if (r < 0) return;                                          // a CTA beyond the last chunk
+  u64 left = s_left;
+  u64 u = u_begin;
 
   if (PACKED && lane == 0) {
     for (int i = 0; i < STAGES; ++i) bar_init(&s_bar[warp][i], 1);
@@ -162,9 +223,9 @@ __global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_spli
 
   unsigned char* const ring = smem + warp * STAGES * STAGE;
   const u32 ring_addr = smem_addr(ring);
-  int rt = 0;
+  u32 rt = 0;
   Req rq = request(a, r);
-  while (u < u_end) {
+  do {
     // ---- the item under u: request r, row tile rt, kv head h, and the part [ua, ub) of its units
     int keys, n_units;
     for (;;) {
@@ -175,16 +236,29 @@ __global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_spli
         continue;
       }
       keys = tile_keys<NQ>(a, rq, rt);
-      n_units = units_of(keys);
-      const i64 all = (i64)n_units * a.cache.heads;
+      n_units = units_of<UNIT>(keys);
+      const u64 all = (u64)(chunk ? chunks_of(n_units, chunk) : n_units) * a.cache.heads;
       if (left < all) break;
       left -= all;
       ++rt;
     }
-    const int h = (int)(left / n_units), ua = (int)(left % n_units);
-    const int ub = u_end - u < n_units - ua ? ua + (int)(u_end - u) : n_units;
-    const i64 item_begin = u - ua, item_end = item_begin + n_units;
-    const int row_base = rt * NQ, rows_left = rq.fresh * a.group - row_base, rows = rows_left < NQ ? rows_left : NQ;
+    int h, ua, ub;
+    u32 first_cta, last_cta;                                  // CTAs that share the item
+    if (chunk) {
+      const u32 n = chunks_of(n_units, chunk), k = (u32)left % n;
+      h = (int)((u32)left / n);
+      ua = (int)(k * chunk);
+      ub = min(ua + (int)chunk, n_units);
+      first_cta = blockIdx.x - k;
+      last_cta = first_cta + n - 1;
+    } else {
+      h = (int)quotient(left, n_units);
+      ua = (int)(left - (u64)h * n_units);
+      ub = u_end - u < (u64)(n_units - ua) ? ua + (int)(u_end - u) : n_units;
+      first_cta = quotient(u - ua, per);
+      last_cta = quotient(u - ua + n_units - 1, per);
+    }
+    const int row_base = (int)(rt * NQ), rows_left = rq.fresh * a.group - row_base, rows = rows_left < NQ ? rows_left : NQ;
 
     // ---- loads of this warp's tiles: tile i of the part is tokens (ua + i) * 64 + warp * 16 ..
     const int n_tiles = ub - ua;
@@ -272,7 +346,7 @@ __global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_spli
 
     // ---- q of the item into shared memory in the products' type; rows that do not exist are zero
     {
-      constexpr int TPR = SP_THREADS / NQ, E = D / TPR;       // threads per row, elements per thread
+      constexpr int TPR = SP_THREADS / NQ < D / 4 ? SP_THREADS / NQ : D / 4, E = D / TPR;       // threads per row, elements per thread
       const int row = tid / TPR, e0 = (tid % TPR) * E;
       __align__(16) u32 raw[E / 2];
       const bool live = row < rows;
@@ -309,9 +383,13 @@ __global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_spli
           raw[i] = pack2<true>(f.x * down, f.y * down);
         }
       }
+      if (row < NQ) {
+        const u32 flip = a.scale2 < 0.0f ? 0x80008000u : 0;   // the sign of the softmax scale goes into q
 #pragma unroll
-      for (int i = 0; i < E / 2; ++i) *reinterpret_cast<u32*>(&s_q[row][e0 + 2 * i]) = raw[i];
-      if (e0 == 0) s_qf[row] = factor * a.scale2;
+        for (int i = 0; i < E / 2; ++i) *reinterpret_cast<u32*>(&s_q[row][e0 + 2 * i]) = raw[i] ^ flip;
+        // as a positive number: of zero, the smallest that keeps masked scores at minus infinity
+        if (e0 == 0) s_qf[row] = fmaxf(factor * fabsf(a.scale2), 0x1p-126f);
+      }
     }
     __syncthreads();
     u32 qb[NT][KS][2];
@@ -378,9 +456,9 @@ __global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_spli
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
             u32 va[4], vb[4];
-            const u32 sel = half ? 0x7632u : 0x5410u;
-            deq4(__byte_perm(c[0][w], c[1][w], sel), da, mg, va);
-            deq4(__byte_perm(c[2][w], c[3][w], sel), db, mg, vb);
+            const u32 sel = half ? 0x7632u : 0x5410u, up = half ? 0x7733u : 0x5511u;      // 16 bits of either token; their upper bytes
+            deq4(__byte_perm(c[0][w], c[1][w], sel), __byte_perm(c[0][w], c[1][w], up), da, mg, va);
+            deq4(__byte_perm(c[2][w], c[3][w], sel), __byte_perm(c[2][w], c[3][w], up), db, mg, vb);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
               const u32 av[4] = {va[2 * i], va[2 * i + 1], vb[2 * i], vb[2 * i + 1]};
@@ -461,8 +539,8 @@ __global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_spli
 #pragma unroll
           for (int w = 2 * gr; w < 2 * gr + 2; ++w) {
             u32 v0[4], v1[4];
-            deq4(c0[w], d0, mg, v0);
-            deq4(c1[w], d1, mg, v1);
+            deq4(c0[w], c0[w] >> 8, d0, mg, v0);
+            deq4(c1[w], c1[w] >> 8, d1, mg, v1);
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
               const u32 av[4] = {v0[2 * b], v1[2 * b], v0[2 * b + 1], v1[2 * b + 1]};
@@ -481,10 +559,6 @@ __global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_spli
           for (int n = 0; n < NT; ++n) mma16816<F16>(sc[n], av, qb[n][kk]);
         }
       }
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) sc[n][c] *= qs[n][c & 1];
     };
     // running maximum and weights of K tiles, then their values; held: tiles that are there
     auto accumulate = [&](auto& sc, int s0, auto held) {
@@ -493,9 +567,10 @@ __global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_spli
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          float x = m[n][c];
+          float x = fmaxf(sc[0][n][c], sc[0][n][c + 2]);
 #pragma unroll
-          for (int k = 0; k < K; ++k) x = fmaxf(x, fmaxf(sc[k][n][c], sc[k][n][c + 2]));
+          for (int k = 1; k < K; ++k) x = fmaxf(x, fmaxf(sc[k][n][c], sc[k][n][c + 2]));
+          x = fmaxf(m[n][c], x * qs[n][c]);
 #pragma unroll
           for (int w = 4; w < 32; w <<= 1) x = fmaxf(x, __shfl_xor_sync(FULL, x, w));
           if (__any_sync(FULL, x != m[n][c])) {
@@ -520,7 +595,7 @@ __global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_spli
           float p[4];
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            p[c] = exp2_fast(sc[k][n][c] - ref[n][c & 1]);
+            p[c] = exp2_fast(fmaf(sc[k][n][c], qs[n][c & 1], -ref[n][c & 1]));
             l[n][c & 1] += p[c];
           }
           pb[n][0] = transpose8x8(pack2<F16>(p[0], p[1]));
@@ -617,21 +692,22 @@ __global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_spli
         }
       }
     __syncthreads();
-    constexpr int TPR = SP_THREADS / NQ, E = D / TPR;         // threads per row, elements per thread
+    constexpr int TPR = SP_THREADS / NQ < D / 4 ? SP_THREADS / NQ : D / 4, E = D / TPR;         // threads per row, elements per thread
     const int row = tid / TPR, e0 = (tid % TPR) * E;
     float acc[E], top = -INFINITY, sum = 0.0f;
+    const int rw = row < NQ ? row : 0;
 #pragma unroll
-    for (int w = 0; w < SP_WARPS; ++w) top = fmaxf(top, s_m[w][row]);
+    for (int w = 0; w < SP_WARPS; ++w) top = fmaxf(top, s_m[w][rw]);
 #pragma unroll
     for (int w = 0; w < SP_WARPS; ++w) {
-      const float lw = s_l[w][row], mw = s_m[w][row];
+      const float lw = s_l[w][rw], mw = s_m[w][rw];
       sum += mw == -INFINITY ? lw : lw * exp2_fast(mw - top);
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       acc[e] = 0.0f;
 #pragma unroll
-      for (int w = 0; w < SP_WARPS; ++w) acc[e] += s_o[(w * NQ + row) * OS + e0 + e];
+      for (int w = 0; w < SP_WARPS; ++w) acc[e] += s_o[(w * NQ + rw) * OS + e0 + e];
     }
     if (s_any_bad && row < rows) {
       const i64 p = (i64)rq.pos0 + (row_base + row) / a.group;
@@ -643,7 +719,6 @@ __global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_spli
         else if (neg) acc[e] -= INFINITY;
       }
     }
-    const i64 first_cta = item_begin / per, last_cta = (item_end - 1) / per;
     bool write = true;
     if (first_cta != last_cta) {
       // partial sums: slot 1 of the CTA the item begins in, slot 0 of the others
@@ -659,7 +734,7 @@ __global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_spli
       __threadfence();
       __syncthreads();
       if (tid == 0) {
-        const u32 n = (u32)(last_cta - first_cta);
+        const u32 n = last_cta - first_cta;
         const bool last = atomicAdd(&counters[first_cta], 1u) == n;
         if (last) counters[first_cta] = 0;
         s_last = last;
@@ -672,7 +747,7 @@ __global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_spli
         const int n_parts = (int)(last_cta - first_cta) + 1;
         float* s_pm = reinterpret_cast<float*>(smem);
         float* s_pl = s_pm + n_parts * rows;
-        auto part = [&](int c) { return parts + (2 * (first_cta + c) + (c == 0 ? 1 : 0)) * PF; };
+        auto part = [&](int c) { return parts + (2 * (i64)(first_cta + c) + (c == 0 ? 1 : 0)) * PF; };
         for (int i = tid; i < n_parts * rows; i += SP_THREADS) {
           const float* p = part(i / rows) + NQ * D + i % rows;
           s_pm[i] = __ldcg(p);
@@ -717,7 +792,7 @@ __global__ void __launch_bounds__(SP_THREADS, split_ctas<FMT, NT>()) attend_spli
     __syncthreads();                                          // the ring and the small arrays are free again
     u += ub - ua;
     left += ub - ua;
-  }
+  } while (!chunk && u < u_end);
 }
 
 }  // namespace ptk

@@ -141,6 +141,7 @@ def test_attend_refuses(G):
     assert call(work=None) == E_INVAL and call(work=A + 16) == E_INVAL
     assert call(size=need - 1) == E_NOMEM
     assert call(R=(1 << 20) + 1) == E_LIMIT and call(tokens=1 << 27) == E_LIMIT
+    assert call(width=(1 << 26) + 1) == E_LIMIT                                               # more than 2^30 tokens in a row of the table
     assert call(R=0) == OK and call(tokens=0) == OK and call(max_new=0) == OK
     assert G.lib.ptstore_attend(None, C.byref(cache(G)), A, need, None, None) == E_INVAL
 
