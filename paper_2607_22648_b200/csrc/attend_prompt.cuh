@@ -34,15 +34,15 @@ struct PromptShape {
 
 // false: this wait, or another one of the CTA, ran out
 __device__ __forceinline__ bool bar_wait(u64* bar, u32 parity, volatile int* gave_up) {
-  if (bar_try(bar, parity)) return true;
   for (u32 i = 0; i < PR_POLLS; ++i) {
     if (bar_try(bar, parity)) return true;
-    if (*gave_up) return false;
+    if ((i & 63) == 63 && *gave_up) return false;
   }
   *gave_up = 1;
   return false;
 }
 
+__device__ __forceinline__ void cp_arrive(u64* bar) { asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(bar)) : "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -199,7 +199,11 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
     if (warp == 12 && lane == 0) {
       constexpr u32 QK = mma_desc(F16, PR_KEYS, false), PV = mma_desc(F16, D, true);
       auto wait = [&](u64* b, u32 parity) { return bar_wait(b, parity, &s_gave_up); };
-      auto slot_wait = [&](int op) { return wait(&b_full[op % PR_SLOTS], (op / PR_SLOTS) & 1); };
+      auto slot_wait = [&](int op) {
+        const bool ok = wait(&b_full[op % PR_SLOTS], (op / PR_SLOTS) & 1);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the tiles were written through the generic proxy
+        return ok;
+      };
       auto scores = [&](int w, int op) {
         const u64 qa = operand_desc(smem_q + w * TB, 0), kb = operand_desc(smem_kv + (op % PR_SLOTS) * TB, 0);
 #pragma unroll
@@ -282,31 +286,27 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
       // chunk pt % CPR of rows pt / CPR, pt / CPR + 128 / CPR, ...
       constexpr int RPP = 128 / CPR;
       const int c = pt % CPR, r0 = pt / CPR;
-      auto finish = [&](int op) {             // the copies of op have landed
-        if ((op & 1) && (op >> 1) * PR_KEYS + PR_KEYS > all_see) {
-          // keys that some of the rows do not see: a weight of zero would not hide an infinity or a NaN, so they are taken out here
-          // and put into the rows that see them at the end
-          unsigned char* t = smem + (2 + op % PR_SLOTS) * TB;
-          constexpr u32 EX = F16 ? 0x7C00u : 0x7F80u, MANT = F16 ? 0x03FFu : 0x007Fu;
-          for (int i = 0; i < CPR; ++i) {
-            const int n = i * RPP + r0, key = (op >> 1) * PR_KEYS + n;
-            if (key < all_see) continue;
-            unsigned short* p = reinterpret_cast<unsigned short*>(t + operand_at(n, c));
-            const uint4 v = *reinterpret_cast<const uint4*>(p);
-            const u32 w[4] = {v.x, v.y, v.z, v.w};
-            bool odd = false;
+      // keys that some of the rows do not see: a weight of zero would not hide an infinity or a NaN, so they are taken out here
+      // and put into the rows that see them at the end
+      auto mend = [&](int op) {
+        unsigned char* t = smem + (2 + op % PR_SLOTS) * TB;
+        constexpr u32 EX = F16 ? 0x7C00u : 0x7F80u, MANT = F16 ? 0x03FFu : 0x007Fu;
+        for (int i = 0; i < CPR; ++i) {
+          const int n = i * RPP + r0, key = (op >> 1) * PR_KEYS + n;
+          if (key < all_see) continue;
+          unsigned short* p = reinterpret_cast<unsigned short*>(t + operand_at(n, c));
+          const uint4 v = *reinterpret_cast<const uint4*>(p);
+          const u32 w[4] = {v.x, v.y, v.z, v.w};
+          bool odd = false;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) odd |= (w[k] & EX) == EX || ((w[k] >> 16) & EX) == EX;
-            if (odd)
-              for (int k = 0; k < 8; ++k)
-                if ((p[k] & EX) == EX) {
-                  note_bad(c * 8 + k, (p[k] & MANT) ? 0 : (p[k] & 0x8000u) ? 2 : 1, key);
-                  p[k] = 0;
-                }
-          }
+          for (int k = 0; k < 4; ++k) odd |= (w[k] & EX) == EX || ((w[k] >> 16) & EX) == EX;
+          if (odd)
+            for (int k = 0; k < 8; ++k)
+              if ((p[k] & EX) == EX) {
+                note_bad(c * 8 + k, (p[k] & MANT) ? 0 : (p[k] & 0x8000u) ? 2 : 1, key);
+                p[k] = 0;
+              }
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        bar_arrive(&b_full[op % PR_SLOTS]);
       };
       i64 next = n_steps > 0 ? where(0) : -1;
       for (int op = 0; op < 2 * n_steps && ok; ++op) {
@@ -328,17 +328,16 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
           const i64 off = s_row[j & 1][n];
           cp_async16_or_zero(dst + operand_at(n, c), base + (off < 0 ? 0 : off), off >= 0);
         }
-        cp_commit();
-        if (op >= 2) { cp_wait<2>(); finish(op - 2); }
-      }
-      if (ok) {
-        if (n_steps > 0) {
-          cp_wait<1>();
-          finish(2 * n_steps - 2);
+        if ((op & 1) && (j + 1) * PR_KEYS > all_see) {
+          cp_commit();
           cp_wait<0>();
-          finish(2 * n_steps - 1);
-        }
-      } else cp_wait<0>();
+          mend(op);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          bar_arrive(&b_full[op % PR_SLOTS]);
+        } else cp_arrive(&b_full[op % PR_SLOTS]);             // arrives when this thread's copies have landed
+      }
+      cp_commit();
+      cp_wait<0>();
     } else {
       // one key per thread: its codes and scales are loaded one operand ahead, unpacked and stored as fp16.  Element order inside
       // eight is 0 4 1 5 2 6 3 7, as the unpacking yields it: Q is stored likewise, and O's columns are put back at the end.
