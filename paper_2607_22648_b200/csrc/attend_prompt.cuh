@@ -72,6 +72,13 @@ __device__ __forceinline__ void tc_st32(u32 addr, const u32 (&r)[32]) {
                  "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr) : "memory");
 }
 
+// One lane of a converged warp, the same every time
+__device__ __forceinline__ bool elected() {
+  u32 p;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+  return p != 0;
+}
+
 // Shared-memory operand descriptor: 128-byte swizzle; `lead` only matters where the operand is MN-major (bytes between its 64-element
 // halves), stride is 8 rows of 128 bytes.
 __device__ __forceinline__ u64 operand_desc(u32 addr, u32 lead_bytes) {
@@ -128,7 +135,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
   __shared__ u32 s_valid[4][4];              // keys of a step that are there, by step & 3
   __shared__ int s_bad[3][D];                // first key whose V holds NaN, +inf, -inf in column d, among keys that some rows do not see
   __shared__ float s_qf[PR_ROWS];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0);
 
   // ---- which 256 rows: heads vary fastest; a request's tiles come last to first, the ones with most keys first
   const int h = blockIdx.x % a.cache.heads;
@@ -196,9 +203,9 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
   if (warp >= 12) {
     // ======== tensor instructions
     regs_fewer<40>();
-    if (warp == 12 && lane == 0) {
+    if (warp == 12) {                         // the whole warp walks the steps, one lane issues: operands stay warp-uniform
       constexpr u32 QK = mma_desc(F16, PR_KEYS, false), PV = mma_desc(F16, D, true);
-      auto wait = [&](u64* b, u32 parity) { return bar_wait(b, parity, &s_gave_up); };
+      auto wait = [&](u64* b, u32 parity) { return __all_sync(FULL, bar_wait(b, parity, &s_gave_up)); };
       auto slot_wait = [&](int op) {
         const bool ok = wait(&b_full[op % PR_SLOTS], (op / PR_SLOTS) & 1);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the tiles were written through the generic proxy
@@ -206,18 +213,29 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
       };
       auto scores = [&](int w, int op) {
         const u64 qa = operand_desc(smem_q + w * TB, 0), kb = operand_desc(smem_kv + (op % PR_SLOTS) * TB, 0);
+        if (elected()) {
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {    // 16 elements: 32 bytes further in a row, or the next 64-element half
-          const u64 off = (u64)(((k >> 2) * (PR_KEYS * 128) + (k & 3) * 32) >> 4);
-          mma_ss(tmem + w * 128, qa + off, kb + off, QK, k > 0);
+          for (int k = 0; k < D / 16; ++k) {  // 16 elements: 32 bytes further in a row, or the next 64-element half
+            const u64 off = (u64)(((k >> 2) * (PR_KEYS * 128) + (k & 3) * 32) >> 4);
+            mma_ss(tmem + w * 128, qa + off, kb + off, QK, k > 0);
+          }
+          tc_commit(&b_s[w]);
         }
-        tc_commit(&b_s[w]);
+        __syncwarp();
       };
-      auto values = [&](int w, int op, bool add) {
+      auto values = [&](int w, int op, bool add, bool last) {
         const u64 vb = operand_desc(smem_kv + (op % PR_SLOTS) * TB, PR_KEYS * 128);
+        if (elected()) {
 #pragma unroll
-        for (int k = 0; k < PR_KEYS / 16; ++k)   // 16 keys: 16 rows of 128 bytes; 8 columns of P
-          mma_ts(tmem + 256 + w * 128, tmem + w * 128 + k * 8, vb + (u64)((k * 16 * 128) >> 4), PV, add || k > 0);
+          for (int k = 0; k < PR_KEYS / 16; ++k)   // 16 keys: 16 rows of 128 bytes; 8 columns of P
+            mma_ts(tmem + 256 + w * 128, tmem + w * 128 + k * 8, vb + (u64)((k * 16 * 128) >> 4), PV, add || k > 0);
+          if (last) tc_commit(&b_o[w]);
+        }
+        __syncwarp();
+      };
+      auto release = [&](int op) {
+        if (elected()) tc_commit(&b_empty[op % PR_SLOTS]);
+        __syncwarp();
       };
       bool ok = true;
       for (int w = 0; w < 2 && ok; ++w)
@@ -228,7 +246,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
         if (ok) {
           for (int w = 0; w < 2; ++w)
             if (steps[w] > 0) scores(w, 0);
-          tc_commit(&b_empty[0]);
+          release(0);
         }
       }
       for (int j = 0; j < n_steps && ok; ++j) {
@@ -240,8 +258,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
             ok = wait(&b_p[w], j & 1);
             if (!ok) break;
             tc_fence_after();
-            values(w, vop, j > 0);
-            if (j + 1 == steps[w]) tc_commit(&b_o[w]);
+            values(w, vop, j > 0, j + 1 == steps[w]);
           }
           if (j + 1 < steps[w]) {
             if (!have_k) { ok = slot_wait(kop); have_k = true; tc_fence_after(); }
@@ -249,12 +266,13 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
           }
         }
         if (ok) {
-          tc_commit(&b_empty[vop % PR_SLOTS]);
-          if (have_k) tc_commit(&b_empty[kop % PR_SLOTS]);
+          release(vop);
+          if (have_k) release(kop);
         }
       }
       if (!ok) {                              // everything issued has ended before tensor memory is given back
-        tc_commit(&b_end);
+        if (elected()) tc_commit(&b_end);
+        __syncwarp();
         for (u32 i = 0; i < PR_POLLS && !bar_try(&b_end, 0); ++i) {}
       }
     }
