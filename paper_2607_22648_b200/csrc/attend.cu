@@ -53,8 +53,34 @@ int launch_split_shape(const Attend& a, int D, int nt, const Gpu& gpu, cudaStrea
   return nt == 1 ? launch_split<FMT, QFP16, 128, 1>(a, gpu, s) : launch_split<FMT, QFP16, 128, 2>(a, gpu, s);
 }
 
+// The tensor map of one layer's 16-bit cache: {head_dim, heads, tokens of a block, blocks, K or V}, boxes of 64 elements of one head and up to 128
+// tokens of one block.  Returns the tokens of a box, 0 where the block size (or the strides) allows none.
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+u32 make_tensor_map(const Attend& a, bool half, int D, CUtensorMap* map) {
+  static std::atomic<void*> entry{nullptr};
+  const u32 B = a.cache.block_tokens;
+  if (B % 8 || (PR_KEYS % B && B % PR_KEYS)) return 0;
+  void* fn = entry.load(std::memory_order_acquire);
+  if (!fn) {
+    cudaDriverEntryPointQueryResult got;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &got) != cudaSuccess || got != cudaDriverEntryPointSuccess) {
+      (void)cudaGetLastError();
+      return 0;
+    }
+    entry.store(fn, std::memory_order_release);
+  }
+  const u32 box = B < PR_KEYS ? B : PR_KEYS;
+  const cuuint64_t dims[5] = {(cuuint64_t)D, a.cache.heads, B, a.cache.num_blocks, 2};
+  const cuuint64_t strides[4] = {(cuuint64_t)D * 2, (cuuint64_t)a.cache.heads * D * 2, a.cache.block_stride, a.cache.kv_stride};
+  const cuuint32_t boxes[5] = {64, 1, box, 1, 1}, steps[5] = {1, 1, 1, 1, 1};
+  const CUresult r = reinterpret_cast<EncodeTiled>(fn)(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, a.cache.base, dims, strides, boxes, steps,
+                                                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? box : 0;
+}
+
 template <int FMT, bool QFP16, int D>
-int launch_prompt(const Attend& a, const Gpu& gpu, cudaStream_t s) {
+int launch_prompt(Attend a, const Gpu& gpu, cudaStream_t s) {
   auto* kernel = attend_prompt_kernel<FMT, QFP16, D>;
   constexpr int SMEM = PromptShape<D>::SMEM;
   static std::atomic<u64> devices{0};
@@ -67,7 +93,9 @@ int launch_prompt(const Attend& a, const Gpu& gpu, cudaStream_t s) {
   if (rc) return rc;
   const i64 tiles = (i64)a.tokens * a.group / PR_ROWS + a.R;            // at most this many, wherever the requests' rows end
   if (tiles * a.cache.heads > 0x7FFFFFFF) return PTSTORE_E_LIMIT;
-  kernel<<<(unsigned)(tiles * a.cache.heads), PR_THREADS, SMEM, s>>>(a);
+  CUtensorMap map = {};
+  a.box_tokens = FMT == PTSTORE_KV_PACKED ? 0 : make_tensor_map(a, FMT == PTSTORE_KV_FP16, D, &map);
+  kernel<<<(unsigned)(tiles * a.cache.heads), PR_THREADS, SMEM, s>>>(a, map);
   return cudaGetLastError() == cudaSuccess ? PTSTORE_OK : PTSTORE_E_CUDA;
 }
 
@@ -114,6 +142,7 @@ extern "C" int ptstore_attend(const ptstore_attend_t* p, const ptstore_kv_cache_
   a.v_factor = packed ? cache->v_scale * DEQ_FACTOR : 1.0f;
   a.work = static_cast<unsigned char*>(workspace);
   a.status = status;
+  a.box_tokens = 0;
   Gpu gpu;
   (void)cudaGetLastError();
   const int rs = current_gpu(&gpu);

@@ -19,6 +19,7 @@ struct Attend {
   float scale2;                               // softmax scale * log2 e (* K's tensor scale and format factor for the 4-bit cache)
   float v_factor;                             // what the 4-bit values of V are multiplied by at the end (1 for 16-bit caches)
   unsigned char* work;
+  u32 box_tokens;                             // tokens of a box of the cache's tensor map, 0: there is none
   u32* status;
 };
 

@@ -17,6 +17,8 @@
 // Tensor memory (512 columns): S/P of tile 0, S/P of tile 1, O 0, O 1.  Shared memory operands are in the 128-byte swizzled form: 64
 // elements of a row are 128 bytes, 16-byte chunk c of row r at c ^ (r & 7), 64-element halves one after the other.
 #pragma once
+#include <cuda.h>
+
 #include "attend.cuh"
 
 namespace ptk {
@@ -24,6 +26,7 @@ namespace ptk {
 constexpr int PR_THREADS = 512;
 constexpr int PR_ROWS = 256, PR_KEYS = 128;
 constexpr int PR_SLOTS = 4;
+constexpr int PR_POLY = 4;                   // one pair of weights in this many is computed without the special function unit (0: none)
 constexpr u32 PR_POLLS = 1u << 22;           // polls of a wait before the CTA gives up (each may suspend for a while)
 
 template <int D>
@@ -43,6 +46,11 @@ __device__ __forceinline__ bool bar_wait(u64* bar, u32 parity, volatile int* gav
 }
 
 __device__ __forceinline__ void cp_arrive(u64* bar) { asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(bar)) : "memory"); }
+// one box of the cache's tensor map {64 elements of a head, head, tokens of a block, block, K or V} into swizzled rows of 128 bytes
+__device__ __forceinline__ void tensor_load(u32 dst, const CUtensorMap* map, int element, int head, int token, int block, int v, u64* bar) {
+  asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst), "l"(map), "r"(element),
+               "r"(head), "r"(token), "r"(block), "r"(v), "r"(smem_addr(bar)) : "memory");
+}
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -107,6 +115,30 @@ __device__ __forceinline__ u64 add_pair(u64 a, u64 b) {
 }
 __device__ __forceinline__ float lo_of(u64 v) { return __uint_as_float((u32)v); }
 __device__ __forceinline__ float hi_of(u64 v) { return __uint_as_float((u32)(v >> 32)); }
+__device__ __forceinline__ u64 mul_pair(u64 a, u64 b) {
+  u64 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// 2^x of two values on the multiply-add units, x <= 9: the special function unit's 4 results per clock and scheduler are what bounds
+// the softmax.  x = n + f, f in [-1/2, 1/2] (adding 1.5 * 2^23 rounds to an integer); 2^f by a polynomial of degree 5 (minimax in the
+// relative error by Remez exchange, 2^-23.7, 2^-22.1 with the roundings); 2^n as the bits of its exponent.  From 2^-127 down the
+// result is zero (the exponent's bits are).  A NaN stays a NaN.
+__device__ __forceinline__ u64 exp2_pair(u64 x) {
+  float lo, hi;
+  asm("max.NaN.f32 %0, %1, 0fC2FE0000;" : "=f"(lo) : "f"(lo_of(x)));      // -127
+  asm("max.NaN.f32 %0, %1, 0fC2FE0000;" : "=f"(hi) : "f"(hi_of(x)));
+  x = pair(lo, hi);
+  const u64 t = add_pair(x, pair(12582912.0f, 12582912.0f)), n = add_pair(t, pair(-12582912.0f, -12582912.0f));
+  const u64 f = fma_pair(n, pair(-1.0f, -1.0f), x);
+  u64 y = fma_pair(f, pair(0.0013276472454890609f, 0.0013276472454890609f), pair(0.009675540961325169f, 0.009675540961325169f));
+  y = fma_pair(y, f, pair(0.05550713092088699f, 0.05550713092088699f));
+  y = fma_pair(y, f, pair(0.24022120237350464f, 0.24022120237350464f));
+  y = fma_pair(y, f, pair(0.6931469440460205f, 0.6931469440460205f));
+  y = fma_pair(y, f, pair(1.0000001192092896f, 1.0000001192092896f));
+  const u32 e0 = (u32)t * (1u << 23) + 0x3F800000u, e1 = (u32)(t >> 32) * (1u << 23) + 0x3F800000u;
+  return mul_pair(y, pair(__uint_as_float(e0), __uint_as_float(e1)));
+}
 template <int R>
 __device__ __forceinline__ void regs_more() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
 template <int R>
@@ -121,13 +153,13 @@ __device__ __forceinline__ i64 prompt_tiles(const Attend& a, int r) {
 }
 
 template <int FMT, bool QFP16, int D>
-__global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) {
+__global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Attend a, const __grid_constant__ CUtensorMap map) {
   constexpr bool PACKED = FMT == PTSTORE_KV_PACKED;
   constexpr bool F16 = PACKED || FMT == PTSTORE_KV_FP16;
   constexpr int TB = PromptShape<D>::TILE_BYTES, CPR = D / 8;           // bytes of a tile, 16-byte chunks of a row
   extern __shared__ unsigned char smem_raw[];
   unsigned char* const smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
-  __shared__ __align__(8) u64 b_q[2], b_full[PR_SLOTS], b_empty[PR_SLOTS], b_s[2], b_p[2], b_o[2], b_end;
+  __shared__ __align__(8) u64 b_q[2], b_full[PR_SLOTS], b_empty[PR_SLOTS], b_s[2], b_pa[2], b_pb[2], b_o[2], b_end;
   __shared__ u32 s_tmem;
   __shared__ int s_gave_up, s_any_bad, s_r, s_tile;
   __shared__ i64 s_scan[PR_THREADS / 32];
@@ -168,7 +200,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
       s_tile = (int)(prompt_tiles(a, r) - 1 - left);
     }
     if (tid == 0) {
-      for (int i = 0; i < 2; ++i) { bar_init(&b_q[i], 128); bar_init(&b_s[i], 1); bar_init(&b_p[i], 128); bar_init(&b_o[i], 1); }
+      for (int i = 0; i < 2; ++i) { bar_init(&b_q[i], 128); bar_init(&b_s[i], 1); bar_init(&b_pa[i], 128); bar_init(&b_pb[i], 128); bar_init(&b_o[i], 1); }
       for (int i = 0; i < PR_SLOTS; ++i) { bar_init(&b_full[i], 128); bar_init(&b_empty[i], 1); }
       bar_init(&b_end, 1);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -208,7 +240,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
       auto wait = [&](u64* b, u32 parity) { return __all_sync(FULL, bar_wait(b, parity, &s_gave_up)); };
       auto slot_wait = [&](int op) {
         const bool ok = wait(&b_full[op % PR_SLOTS], (op / PR_SLOTS) & 1);
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the tiles were written through the generic proxy
+        if (!PACKED && !a.box_tokens) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // tiles written through the generic proxy
         return ok;
       };
       auto scores = [&](int w, int op) {
@@ -223,13 +255,14 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
         }
         __syncwarp();
       };
-      auto values = [&](int w, int op, bool add, bool last) {
+      auto values = [&](int w, int op, int half, bool add) {
         const u64 vb = operand_desc(smem_kv + (op % PR_SLOTS) * TB, PR_KEYS * 128);
         if (elected()) {
 #pragma unroll
-          for (int k = 0; k < PR_KEYS / 16; ++k)   // 16 keys: 16 rows of 128 bytes; 8 columns of P
+          for (int i = 0; i < PR_KEYS / 32; ++i) {   // 16 keys: 16 rows of 128 bytes; 8 columns of P
+            const int k = half * (PR_KEYS / 32) + i;
             mma_ts(tmem + 256 + w * 128, tmem + w * 128 + k * 8, vb + (u64)((k * 16 * 128) >> 4), PV, add || k > 0);
-          if (last) tc_commit(&b_o[w]);
+          }
         }
         __syncwarp();
       };
@@ -251,24 +284,23 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
       }
       for (int j = 0; j < n_steps && ok; ++j) {
         const int kop = 2 * (j + 1), vop = 2 * j + 1;
-        bool have_k = false;
-        ok = slot_wait(vop);
+        ok = slot_wait(vop) && (j + 1 >= n_steps || slot_wait(kop));
         for (int w = 0; w < 2 && ok; ++w) {
           if (j < steps[w]) {
-            ok = wait(&b_p[w], j & 1);
+            ok = wait(&b_pa[w], j & 1);
             if (!ok) break;
             tc_fence_after();
-            values(w, vop, j > 0, j + 1 == steps[w]);
+            values(w, vop, 0, j > 0);
+            ok = wait(&b_pb[w], j & 1);
+            if (!ok) break;
+            tc_fence_after();
+            values(w, vop, 1, true);
+            if (j + 1 == steps[w]) { if (elected()) tc_commit(&b_o[w]); __syncwarp(); }
           }
-          if (j + 1 < steps[w]) {
-            if (!have_k) { ok = slot_wait(kop); have_k = true; tc_fence_after(); }
-            if (ok) scores(w, kop);
-          }
+          if (w == 1) release(vop);
+          if (j + 1 < steps[w]) scores(w, kop);
         }
-        if (ok) {
-          release(vop);
-          if (have_k) release(kop);
-        }
+        if (ok && j + 1 < n_steps) release(kop);
       }
       if (!ok) {                              // everything issued has ended before tensor memory is given back
         if (elected()) tc_commit(&b_end);
@@ -285,11 +317,12 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
     const u32 B = a.cache.block_tokens;
     bool bounds = false, ok = true;
     // where key `pt` of a step lies
+    u32 id = 0;
     auto where = [&](int j) -> i64 {
       const int key = j * PR_KEYS + pt;
       if (key >= keys) return -1;
       const u32 blk = (u32)key / B, in = (u32)key % B;
-      const u32 id = (u32)table[blk];
+      id = (u32)table[blk];
       if (id >= a.cache.num_blocks) { bounds = true; return -1; }
       const i64 base = (i64)((u64)id * a.cache.block_stride);
       if (PACKED) return base + (i64)((u64)h * (B / TILE) + in / TILE) * tile_bytes(D);
@@ -326,33 +359,55 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
               }
         }
       };
+      // A step whose keys are all there and seen by all rows comes through the tensor map where the block size allows one (blocks that
+      // divide 128 tokens or are multiples of it): the first thread of every box issues it.  Other steps are copied 16 bytes at a
+      // time, with zeros for keys that are not there.  (All by 16-byte copies: 4600 clocks per step of 2 x 32 KB and the tensor
+      // cores waiting for them half of the time.)
+      const u32 box = a.box_tokens;
+      const bool leads = box && pt % box == 0;
       i64 next = n_steps > 0 ? where(0) : -1;
-      for (int op = 0; op < 2 * n_steps && ok; ++op) {
-        const int j = op >> 1;
-        if (!(op & 1)) {
-          s_row[j & 1][pt] = next;
-          const u32 there = __ballot_sync(FULL, next >= 0);
-          if (lane == 0) s_valid[j & 3][warp - 8] = there;
-          if (j + 1 < n_steps) next = where(j + 1);
-          asm volatile("bar.sync 1, 128;" ::: "memory");
-        }
-        ok = wait_empty(op);
-        if (!ok) break;
-        const unsigned char* base = a.cache.base + (op & 1 ? a.cache.kv_stride : 0) + c * 16;
-        const u32 dst = smem_kv + (op % PR_SLOTS) * TB;
+      for (int j = 0; j < n_steps && ok; ++j) {
+        const u32 block = id;
+        s_row[j & 1][pt] = next;
+        const u32 present = __ballot_sync(FULL, next >= 0);
+        if (lane == 0) s_valid[j & 3][warp - 8] = present;
+        if (j + 1 < n_steps) next = where(j + 1);
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        const bool plain = box && (j + 1) * PR_KEYS <= all_see && (s_valid[j & 3][0] & s_valid[j & 3][1] & s_valid[j & 3][2] & s_valid[j & 3][3]) == FULL;
+        for (int is_v = 0; is_v < 2 && ok; ++is_v) {
+          const int op = 2 * j + is_v;
+          ok = wait_empty(op);
+          if (!ok) break;
+          const u32 dst = smem_kv + (op % PR_SLOTS) * TB;
+          u64* full = &b_full[op % PR_SLOTS];
+          if (plain) {
+            if (leads) {
+              bar_expect(full, box * D * 2);
 #pragma unroll
-        for (int i = 0; i < CPR; ++i) {
-          const int n = i * RPP + r0;
-          const i64 off = s_row[j & 1][n];
-          cp_async16_or_zero(dst + operand_at(n, c), base + (off < 0 ? 0 : off), off >= 0);
+              for (int e = 0; e < D / 64; ++e)
+                tensor_load(dst + e * (PR_KEYS * 128) + pt * 128, &map, e * 64, h, (int)((u32)(j * PR_KEYS + pt) % B), (int)block, is_v, full);
+            } else bar_arrive(full);
+            continue;
+          }
+          const unsigned char* base = a.cache.base + (is_v ? a.cache.kv_stride : 0) + c * 16;
+#pragma unroll 4
+          for (int i = 0; i < CPR; ++i) {
+            const int n = i * RPP + r0;
+            const i64 off = s_row[j & 1][n];
+            cp_async16_or_zero(dst + operand_at(n, c), base + (off < 0 ? 0 : off), off >= 0);
+          }
+          if (box || (is_v && (j + 1) * PR_KEYS > all_see)) {
+            cp_commit();
+            cp_wait<0>();
+            if (is_v && (j + 1) * PR_KEYS > all_see) mend(op);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            bar_arrive(full);
+          } else cp_arrive(full);             // arrives when this thread's copies have landed
         }
-        if ((op & 1) && (j + 1) * PR_KEYS > all_see) {
-          cp_commit();
-          cp_wait<0>();
-          mend(op);
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          bar_arrive(&b_full[op % PR_SLOTS]);
-        } else cp_arrive(&b_full[op % PR_SLOTS]);             // arrives when this thread's copies have landed
+        if (!ok) {                            // what is in flight lands before the CTA gives its memory back
+          for (int op = max(0, 2 * j - PR_SLOTS); op < 2 * j; ++op)
+            for (u32 i = 0; i < PR_POLLS && !bar_try(&b_full[op % PR_SLOTS], (op / PR_SLOTS) & 1); ++i) {}
+        }
       }
       cp_commit();
       cp_wait<0>();
@@ -516,6 +571,26 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
           for (int i = 0; i < 32; ++i) s[c][i] = (mask >> i) & 1 ? s[c][i] : -INFINITY;
         }
       }
+      // weights of keys 64 half .. + 63 from the reference, into P; on the multiply-add units one pair in POLY
+      u64 sum[2];
+      auto weights = [&](int half, u32 (&p)[32]) {
+        const float ref = m == -INFINITY ? 0.0f : m;
+        const u64 sc2 = pair(scale2, scale2), neg = pair(-ref, -ref);
+        sum[half] = 0;
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            u64 e = fma_pair(pair(s[2 * half + c][i], s[2 * half + c][i + 1]), sc2, neg);
+            if (PR_POLY > 0 && (i / 2) % (PR_POLY > 0 ? PR_POLY : 1) == 1) e = exp2_pair(e);
+            else e = pair(exp2_fast(lo_of(e)), exp2_fast(hi_of(e)));
+            sum[half] = add_pair(sum[half], e);
+            p[16 * c + i / 2] = pack2<F16>(lo_of(e), hi_of(e));
+          }
+      };
+      // the first half starts from the reference as it is, while the maximum is still being found
+      u32 p[32];
+      weights(0, p);
       float x[4];
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
@@ -542,29 +617,19 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(Attend a) 
             tc_st32(to + c, scaled);
           }
         }
+        weights(0, p);
       }
-      const float ref = m == -INFINITY ? 0.0f : m;
-      const u64 sc2 = pair(scale2, scale2), neg = pair(-ref, -ref);
-      u64 sum[2] = {0, 0};
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        u32 p[32];
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            const u64 e = fma_pair(pair(s[2 * half + c][i], s[2 * half + c][i + 1]), sc2, neg);
-            const float e0 = exp2_fast(lo_of(e)), e1 = exp2_fast(hi_of(e));
-            sum[c] = add_pair(sum[c], pair(e0, e1));
-            p[16 * c + i / 2] = pack2<F16>(e0, e1);
-          }
-        tc_st32(ts + 32 * half, p);
-      }
+      tc_st32(ts, p);
+      tc_wait_st();
+      tc_fence_before();
+      bar_arrive(&b_pa[w]);                   // the tensor cores start on these while the second half is computed
+      weights(1, p);
+      tc_st32(ts + 32, p);
       const u64 both = add_pair(sum[0], sum[1]);
       l += lo_of(both) + hi_of(both);
       tc_wait_st();
       tc_fence_before();
-      bar_arrive(&b_p[w]);
+      bar_arrive(&b_pb[w]);
     }
     // ---- output
     if (ok && steps[w] > 0) {
