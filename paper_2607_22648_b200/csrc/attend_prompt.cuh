@@ -26,7 +26,6 @@ namespace ptk {
 constexpr int PR_THREADS = 512;
 constexpr int PR_ROWS = 256, PR_KEYS = 128;
 constexpr int PR_SLOTS = 4;
-constexpr int PR_POLY = 4;                   // one pair of weights in this many is computed without the special function unit (0: none)
 constexpr u32 PR_POLLS = 1u << 22;           // polls of a wait before the CTA gives up (each may suspend for a while)
 
 template <int D>
@@ -115,30 +114,6 @@ __device__ __forceinline__ u64 add_pair(u64 a, u64 b) {
 }
 __device__ __forceinline__ float lo_of(u64 v) { return __uint_as_float((u32)v); }
 __device__ __forceinline__ float hi_of(u64 v) { return __uint_as_float((u32)(v >> 32)); }
-__device__ __forceinline__ u64 mul_pair(u64 a, u64 b) {
-  u64 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-// 2^x of two values on the multiply-add units, x <= 9: the special function unit's 4 results per clock and scheduler are what bounds
-// the softmax.  x = n + f, f in [-1/2, 1/2] (adding 1.5 * 2^23 rounds to an integer); 2^f by a polynomial of degree 5 (minimax in the
-// relative error by Remez exchange, 2^-23.7, 2^-22.1 with the roundings); 2^n as the bits of its exponent.  From 2^-127 down the
-// result is zero (the exponent's bits are).  A NaN stays a NaN.
-__device__ __forceinline__ u64 exp2_pair(u64 x) {
-  float lo, hi;
-  asm("max.NaN.f32 %0, %1, 0fC2FE0000;" : "=f"(lo) : "f"(lo_of(x)));      // -127
-  asm("max.NaN.f32 %0, %1, 0fC2FE0000;" : "=f"(hi) : "f"(hi_of(x)));
-  x = pair(lo, hi);
-  const u64 t = add_pair(x, pair(12582912.0f, 12582912.0f)), n = add_pair(t, pair(-12582912.0f, -12582912.0f));
-  const u64 f = fma_pair(n, pair(-1.0f, -1.0f), x);
-  u64 y = fma_pair(f, pair(0.0013276472454890609f, 0.0013276472454890609f), pair(0.009675540961325169f, 0.009675540961325169f));
-  y = fma_pair(y, f, pair(0.05550713092088699f, 0.05550713092088699f));
-  y = fma_pair(y, f, pair(0.24022120237350464f, 0.24022120237350464f));
-  y = fma_pair(y, f, pair(0.6931469440460205f, 0.6931469440460205f));
-  y = fma_pair(y, f, pair(1.0000001192092896f, 1.0000001192092896f));
-  const u32 e0 = (u32)t * (1u << 23) + 0x3F800000u, e1 = (u32)(t >> 32) * (1u << 23) + 0x3F800000u;
-  return mul_pair(y, pair(__uint_as_float(e0), __uint_as_float(e1)));
-}
 template <int R>
 __device__ __forceinline__ void regs_more() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R)); }
 template <int R>
@@ -223,18 +198,23 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
   const int n_steps = max(steps[0], steps[1]);
   const u32 smem_q = smem_addr(smem), smem_kv = smem_q + 2 * TB;
 
-  if (warp == 12) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const u32 tmem = s_tmem;
+  // tensor memory: allocated by warp 12 while the others load; 12 and the softmax warps meet before they use it
+  auto tmem_there = [&]() {
+    tc_fence_before();
+    asm volatile("bar.sync 4, 288;" ::: "memory");
+    tc_fence_after();
+    return *reinterpret_cast<volatile u32*>(&s_tmem);
+  };
 
   if (warp >= 12) {
     // ======== tensor instructions
     regs_fewer<40>();
+    u32 tmem = 0;
+    if (warp == 12) {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_addr(&s_tmem)) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+      tmem = tmem_there();
+    }
     if (warp == 12) {                         // the whole warp walks the steps, one lane issues: operands stay warp-uniform
       constexpr u32 QK = mma_desc(F16, PR_KEYS, false), PV = mma_desc(F16, D, true);
       auto wait = [&](u64* b, u32 parity) { return __all_sync(FULL, bar_wait(b, parity, &s_gave_up)); };
@@ -488,19 +468,27 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     // ======== softmax of tile w
     regs_more<200>();
     const int w = warp >> 2, t = tid & 127, row = w * 128 + t;
-    // its half of Q: chunk t % CPR of rows t / CPR, ...; the sign of the softmax scale goes into Q
+    // its half of Q: chunk t % CPR of rows t / CPR, ..., all on their way before the first is used; the sign of the softmax scale goes into Q
     {
       constexpr int RPP = 128 / CPR;
       const int c = t % CPR;
       const bool flip = a.scale2 < 0.0f;
-#pragma unroll 4
+      uint4 raw[CPR];
+      const u32 first = row_base + w * 128 + t / CPR, group = a.group, step_fr = RPP / group, step_hq = RPP % group;
+      u32 fr = first / group, hq = first % group;
+      const unsigned char* const q0 = a.q + 2 * ((i64)rq.row0 * a.q_token + (i64)h * group * a.q_head + c * 8);
+#pragma unroll
+      for (int i = 0; i < CPR; ++i) {
+        raw[i] = make_uint4(0, 0, 0, 0);
+        if (w * 128 + i * RPP + t / CPR < rows) raw[i] = __ldg(reinterpret_cast<const uint4*>(q0 + 2 * (fr * a.q_token + hq * a.q_head)));
+        hq += step_hq;
+        fr += step_fr;
+        if (hq >= group) { hq -= group; ++fr; }
+      }
+#pragma unroll
       for (int i = 0; i < CPR; ++i) {
         const int n = i * RPP + t / CPR, gr = w * 128 + n;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (gr < rows) {
-          const int fr = (row_base + gr) / a.group, hq = h * a.group + (row_base + gr) % a.group;
-          v = *reinterpret_cast<const uint4*>(a.q + 2 * ((i64)(rq.row0 + fr) * a.q_token + (i64)hq * a.q_head + c * 8));
-        }
+        const uint4 v = raw[i];
         u32 x[4] = {v.x, v.y, v.z, v.w};
         float factor = 1.0f;
         if (PACKED && !QFP16) {
@@ -538,9 +526,8 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       bar_arrive(&b_q[w]);
-      if (w == 0) asm volatile("bar.sync 2, 128;" ::: "memory");
-      else asm volatile("bar.sync 3, 128;" ::: "memory");
     }
+    const u32 tmem = tmem_there();            // (and every row's factor is there)
     // scale2 as a positive number: of zero, the smallest that keeps masked scores at minus infinity
     const float scale2 = fmaxf(fabsf(a.scale2) * s_qf[row], 0x1p-126f);
     const int see = row < rows ? keys_of(row) : 0;
@@ -571,37 +558,51 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
           for (int i = 0; i < 32; ++i) s[c][i] = (mask >> i) & 1 ? s[c][i] : -INFINITY;
         }
       }
-      // weights of keys 64 half .. + 63 from the reference, into P; on the multiply-add units one pair in POLY
-      u64 sum[2];
-      auto weights = [&](int half, u32 (&p)[32]) {
+      // Weights of keys 64 half .. + 63 from the reference, into P.  The first half starts from the reference as it
+      // stands while the maximum over all 128 keys is found in between (two keys with every weight).  All on the special function unit:
+      // a quarter / a third / half of them by a polynomial on the multiply-add units cost 4 / 8 / 19 % of a 16k prompt's
+      // time, since what bounds this loop is its instructions.
+      float x[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};
+      float sum0, sum1;
+      auto weights = [&](int half, bool find, u32 (&p)[32]) {
         const float ref = m == -INFINITY ? 0.0f : m;
         const u64 sc2 = pair(scale2, scale2), neg = pair(-ref, -ref);
-        sum[half] = 0;
+        u64 sum[2] = {0, 0};
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
+        for (int b = 0; b < 64; b += 16) {    // eight pairs at a time, so that no result is waited for
+          u64 e[8];
 #pragma unroll
-          for (int i = 0; i < 32; i += 2) {
-            u64 e = fma_pair(pair(s[2 * half + c][i], s[2 * half + c][i + 1]), sc2, neg);
-            if (PR_POLY > 0 && (i / 2) % (PR_POLY > 0 ? PR_POLY : 1) == 1) e = exp2_pair(e);
-            else e = pair(exp2_fast(lo_of(e)), exp2_fast(hi_of(e)));
-            sum[half] = add_pair(sum[half], e);
-            p[16 * c + i / 2] = pack2<F16>(lo_of(e), hi_of(e));
+          for (int i = 0; i < 8; ++i) e[i] = fma_pair(pair(s[2 * half + b / 32][b % 32 + 2 * i], s[2 * half + b / 32][b % 32 + 2 * i + 1]), sc2, neg);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            e[i] = pair(exp2_fast(lo_of(e[i])), exp2_fast(hi_of(e[i])));
+            if (find) {
+              const int k = 2 * b + 4 * i;
+#pragma unroll
+              for (int y = 0; y < 4; y += 2) x[(i & 1) * 2 + y / 2] = fmaxf(x[(i & 1) * 2 + y / 2], fmaxf(s[k / 32][k % 32 + y], s[k / 32][k % 32 + y + 1]));
+            }
           }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            sum[i & 1] = add_pair(sum[i & 1], e[i]);
+            p[b / 2 + i] = pack2<F16>(lo_of(e[i]), hi_of(e[i]));
+          }
+        }
+        const u64 both = add_pair(sum[0], sum[1]);
+        (half ? sum1 : sum0) = lo_of(both) + hi_of(both);
       };
-      // the first half starts from the reference as it is, while the maximum is still being found
       u32 p[32];
-      weights(0, p);
-      float x[4];
+      if (j > 0) weights(0, true, p);
+      else {                                  // there is no reference yet
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        x[c] = s[c][0];
+        for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int i = 1; i < 32; ++i) x[c] = fmaxf(x[c], s[c][i]);
+          for (int i = 0; i < 32; ++i) x[c] = fmaxf(x[c], s[c][i]);
       }
       const float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * scale2;
       // the reference moves only when a weight would pass 2^8
       const bool move = top > m + 8.0f || (m == -INFINITY && top > m);
-      if (__any_sync(FULL, move)) {
+      if (__any_sync(FULL, move) || j == 0) {
         const float f = move ? exp2_fast(m - top) : 1.0f;
         if (move) { m = top; l *= f; }
         if (j > 0) {
@@ -617,16 +618,15 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
             tc_st32(to + c, scaled);
           }
         }
-        weights(0, p);
+        weights(0, false, p);
       }
       tc_st32(ts, p);
       tc_wait_st();
       tc_fence_before();
       bar_arrive(&b_pa[w]);                   // the tensor cores start on these while the second half is computed
-      weights(1, p);
+      weights(1, false, p);
       tc_st32(ts + 32, p);
-      const u64 both = add_pair(sum[0], sum[1]);
-      l += lo_of(both) + hi_of(both);
+      l += sum0 + sum1;
       tc_wait_st();
       tc_fence_before();
       bar_arrive(&b_pb[w]);
@@ -639,9 +639,13 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     }
     if (ok) {
       const float f = l == 0.0f ? 0.0f : a.v_factor / l;
-      const bool live = row < rows;
-      const int fr = live ? (row_base + row) / a.group : 0, hq = live ? h * a.group + (row_base + row) % a.group : 0;
-      unsigned char* dst = a.out + 2 * ((i64)(rq.row0 + fr) * a.o_token + (i64)hq * a.o_head);
+      // through shared memory (the tile's Q is not needed any more), so that the stores are whole rows
+      i64 at = -1;                            // of this thread's row, in elements
+      if (row < rows) {
+        const u32 flat = row_base + row, fr = flat / (u32)a.group;
+        at = (i64)(rq.row0 + (int)fr) * a.o_token + (i64)(h * a.group + (int)(flat - fr * a.group)) * a.o_head;
+      }
+      unsigned char* const mine = smem + w * TB;
 #pragma unroll 1
       for (int c = 0; c < D; c += 32) {
         float o[32];
@@ -668,19 +672,24 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
             else if (neg) o[i] = o[i] - INFINITY;
           }
         }
-        if (live) {
 #pragma unroll
-          for (int i = 0; i < 32; i += 8)
-            *reinterpret_cast<uint4*>(dst + 2 * (c + i)) = make_uint4(pack2<QFP16>(o[i], o[i + 1]), pack2<QFP16>(o[i + 2], o[i + 3]), pack2<QFP16>(o[i + 4], o[i + 5]),
-                                                                      pack2<QFP16>(o[i + 6], o[i + 7]));
-        }
+        for (int i = 0; i < 32; i += 8)
+          *reinterpret_cast<uint4*>(mine + operand_at(t, (c + i) / 8)) =
+              make_uint4(pack2<QFP16>(o[i], o[i + 1]), pack2<QFP16>(o[i + 2], o[i + 3]), pack2<QFP16>(o[i + 4], o[i + 5]), pack2<QFP16>(o[i + 6], o[i + 7]));
+      }
+      __syncwarp();
+#pragma unroll 8
+      for (int i = 0; i < CPR; ++i) {         // this warp's 32 rows, whole rows at a time
+        const int n = i * (32 / CPR) + lane / CPR, c = lane % CPR;
+        const i64 to = __shfl_sync(FULL, at, n);
+        if (to >= 0) *reinterpret_cast<uint4*>(a.out + 2 * (to + c * 8)) = *reinterpret_cast<const uint4*>(mine + operand_at((warp & 3) * 32 + n, c));
       }
     }
   }
   tc_fence_before();
   __syncthreads();
   if (warp == 12) {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(s_tmem) : "memory");
     if (lane == 0 && s_gave_up && a.status) atomicOr(a.status, PTSTORE_S_TIMEOUT);
   }
 }
