@@ -34,16 +34,24 @@ struct PromptShape {
   static constexpr int SMEM = (2 + PR_SLOTS) * TILE_BYTES + 1024;       // + alignment
 };
 
-// false: this wait, or another one of the CTA, ran out
-__device__ __forceinline__ bool bar_wait(u64* bar, u32 parity, volatile int* gave_up) {
+// Waits, at most PR_POLLS polls; a wait that runs out says so and lets its caller go on (with whatever is there: every access stays in bounds
+// whatever the data), and the roles leave their loops at the next step.
+__device__ __forceinline__ void bar_wait(u64* bar, u32 parity, volatile int* gave_up) {
+  if (bar_try(bar, parity)) return;
+#pragma unroll 1
   for (u32 i = 0; i < PR_POLLS; ++i) {
-    if (bar_try(bar, parity)) return true;
-    if ((i & 63) == 63 && *gave_up) return false;
+    if (bar_try(bar, parity)) return;
+    if ((i & 1023) == 1023 && *gave_up) return;
   }
   *gave_up = 1;
-  return false;
 }
 
+// barrier of the 128 loading threads, and whether the value was set in any of them
+__device__ __forceinline__ bool any_of_128(int v) {
+  u32 r;
+  asm volatile("{\n .reg .pred p, q;\n setp.ne.s32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 128, p;\n selp.u32 %0, 1, 0, q;\n}" : "=r"(r) : "r"(v) : "memory");
+  return r != 0;
+}
 __device__ __forceinline__ void cp_arrive(u64* bar) { asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_addr(bar)) : "memory"); }
 // one box of the cache's tensor map {64 elements of a head, head, tokens of a block, block, K or V} into swizzled rows of 128 bytes
 __device__ __forceinline__ void tensor_load(u32 dst, const CUtensorMap* map, int element, int head, int token, int block, int v, u64* bar) {
@@ -217,11 +225,13 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     }
     if (warp == 12) {                         // the whole warp walks the steps, one lane issues: operands stay warp-uniform
       constexpr u32 QK = mma_desc(F16, PR_KEYS, false), PV = mma_desc(F16, D, true);
-      auto wait = [&](u64* b, u32 parity) { return __all_sync(FULL, bar_wait(b, parity, &s_gave_up)); };
+      auto wait = [&](u64* b, u32 parity) {
+        bar_wait(b, parity, &s_gave_up);
+        __syncwarp();
+      };
       auto slot_wait = [&](int op) {
-        const bool ok = wait(&b_full[op % PR_SLOTS], (op / PR_SLOTS) & 1);
+        wait(&b_full[op % PR_SLOTS], (op / PR_SLOTS) & 1);
         if (!PACKED && !a.box_tokens) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // tiles written through the generic proxy
-        return ok;
       };
       auto scores = [&](int w, int op) {
         const u64 qa = operand_desc(smem_q + w * TB, 0), kb = operand_desc(smem_kv + (op % PR_SLOTS) * TB, 0);
@@ -250,43 +260,41 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
         if (elected()) tc_commit(&b_empty[op % PR_SLOTS]);
         __syncwarp();
       };
-      bool ok = true;
-      for (int w = 0; w < 2 && ok; ++w)
-        if (steps[w] > 0) ok = wait(&b_q[w], 0);
-      if (ok && n_steps > 0) {
-        ok = slot_wait(0);
+      for (int w = 0; w < 2; ++w)
+        if (steps[w] > 0) wait(&b_q[w], 0);
+      if (n_steps > 0) {
+        slot_wait(0);
         tc_fence_after();
-        if (ok) {
-          for (int w = 0; w < 2; ++w)
-            if (steps[w] > 0) scores(w, 0);
-          release(0);
-        }
+        for (int w = 0; w < 2; ++w)
+          if (steps[w] > 0) scores(w, 0);
+        release(0);
+        slot_wait(1);
       }
-      for (int j = 0; j < n_steps && ok; ++j) {
+      // V of step j and K of step j + 1 have been waited for by the time they are needed: the waits sit where the other tile's weights
+      // would be waited for anyway
+      for (int j = 0; j < n_steps && !__any_sync(FULL, *reinterpret_cast<volatile int*>(&s_gave_up)); ++j) {
         const int kop = 2 * (j + 1), vop = 2 * j + 1;
-        ok = slot_wait(vop) && (j + 1 >= n_steps || slot_wait(kop));
-        for (int w = 0; w < 2 && ok; ++w) {
+        if (j + 1 < n_steps) slot_wait(kop);
+        for (int w = 0; w < 2; ++w) {
           if (j < steps[w]) {
-            ok = wait(&b_pa[w], j & 1);
-            if (!ok) break;
+            wait(&b_pa[w], j & 1);
             tc_fence_after();
             values(w, vop, 0, j > 0);
-            ok = wait(&b_pb[w], j & 1);
-            if (!ok) break;
+            wait(&b_pb[w], j & 1);
             tc_fence_after();
             values(w, vop, 1, true);
             if (j + 1 == steps[w]) { if (elected()) tc_commit(&b_o[w]); __syncwarp(); }
           }
           if (w == 1) release(vop);
           if (j + 1 < steps[w]) scores(w, kop);
+          if (w == 0 && j + 1 < n_steps) slot_wait(vop + 2);
         }
-        if (ok && j + 1 < n_steps) release(kop);
+        if (j + 1 < n_steps) release(kop);
       }
-      if (!ok) {                              // everything issued has ended before tensor memory is given back
-        if (elected()) tc_commit(&b_end);
-        __syncwarp();
-        for (u32 i = 0; i < PR_POLLS && !bar_try(&b_end, 0); ++i) {}
-      }
+      // everything issued has ended before tensor memory is given back
+      if (elected()) tc_commit(&b_end);
+      __syncwarp();
+      for (u32 i = 0; i < PR_POLLS && !bar_try(&b_end, 0); ++i) {}
     }
     __syncwarp();
   } else if (warp >= 8) {
@@ -295,7 +303,8 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     const int pt = tid - 256;
     const int* table = a.tables + (i64)r * a.max_blocks;
     const u32 B = a.cache.block_tokens;
-    bool bounds = false, ok = true;
+    bool bounds = false;
+    const volatile int* const gave_up = &s_gave_up;
     // where key `pt` of a step lies
     u32 id = 0;
     auto where = [&](int j) -> i64 {
@@ -308,7 +317,9 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       if (PACKED) return base + (i64)((u64)h * (B / TILE) + in / TILE) * tile_bytes(D);
       return base + (i64)(((u64)in * a.cache.heads + h) * (D * 2));
     };
-    auto wait_empty = [&](int op) { return op < PR_SLOTS || bar_wait(&b_empty[op % PR_SLOTS], ((op / PR_SLOTS) - 1) & 1, &s_gave_up); };
+    auto wait_empty = [&](int op) {
+      if (op >= PR_SLOTS) bar_wait(&b_empty[op % PR_SLOTS], ((op / PR_SLOTS) - 1) & 1, &s_gave_up);
+    };
     auto note_bad = [&](int d, int kind, int key) {
       atomicMin(&s_bad[kind][d], key);
       s_any_bad = 1;
@@ -346,18 +357,19 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       const u32 box = a.box_tokens;
       const bool leads = box && pt % box == 0;
       i64 next = n_steps > 0 ? where(0) : -1;
-      for (int j = 0; j < n_steps && ok; ++j) {
+      int j = 0;
+      bool stop = false;                      // the same in all 128 threads
+      for (; j < n_steps; ++j) {
         const u32 block = id;
         s_row[j & 1][pt] = next;
         const u32 present = __ballot_sync(FULL, next >= 0);
         if (lane == 0) s_valid[j & 3][warp - 8] = present;
         if (j + 1 < n_steps) next = where(j + 1);
-        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (any_of_128(*gave_up)) { stop = true; break; }
         const bool plain = box && (j + 1) * PR_KEYS <= all_see && (s_valid[j & 3][0] & s_valid[j & 3][1] & s_valid[j & 3][2] & s_valid[j & 3][3]) == FULL;
-        for (int is_v = 0; is_v < 2 && ok; ++is_v) {
+        for (int is_v = 0; is_v < 2; ++is_v) {
           const int op = 2 * j + is_v;
-          ok = wait_empty(op);
-          if (!ok) break;
+          wait_empty(op);
           const u32 dst = smem_kv + (op % PR_SLOTS) * TB;
           u64* full = &b_full[op % PR_SLOTS];
           if (plain) {
@@ -384,11 +396,10 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
             bar_arrive(full);
           } else cp_arrive(full);             // arrives when this thread's copies have landed
         }
-        if (!ok) {                            // what is in flight lands before the CTA gives its memory back
-          for (int op = max(0, 2 * j - PR_SLOTS); op < 2 * j; ++op)
-            for (u32 i = 0; i < PR_POLLS && !bar_try(&b_full[op % PR_SLOTS], (op / PR_SLOTS) & 1); ++i) {}
-        }
       }
+      if (stop)                               // what is in flight lands before the CTA gives its memory back
+        for (int op = max(0, 2 * j - PR_SLOTS); op < 2 * j; ++op)
+          for (u32 i = 0; i < PR_POLLS && !bar_try(&b_full[op % PR_SLOTS], (op / PR_SLOTS) & 1); ++i) {}
       cp_commit();
       cp_wait<0>();
     } else {
@@ -426,7 +437,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       };
       const Magic mg = magic();
       if (n_steps > 0) load(0);
-      for (int op = 0; op < 2 * n_steps && ok; ++op) {
+      for (int op = 0; op < 2 * n_steps && !__any_sync(FULL, *gave_up); ++op) {
         u32 cur[D / 8], sc[D / 64];
         const bool cur_has = has;
 #pragma unroll
@@ -434,8 +445,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) sc[i] = scale[i];
         if (op + 1 < 2 * n_steps) load(op + 1);
-        ok = wait_empty(op);
-        if (!ok) break;
+        wait_empty(op);
         const int key = (op >> 1) * PR_KEYS + pt;
         if ((op & 1) && cur_has && key >= all_see) {
 #pragma unroll
@@ -534,10 +544,9 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     const u32 lane_base = (u32)(32 * (warp & 3)) << 16;
     const u32 ts = tmem + lane_base + w * 128, to = tmem + lane_base + 256 + w * 128;
     float m = -INFINITY, l = 0.0f;
-    bool ok = true;
     for (int j = 0; j < steps[w]; ++j) {
-      ok = bar_wait(&b_s[w], j & 1, &s_gave_up);
-      if (__any_sync(FULL, !ok)) { ok = false; break; }
+      bar_wait(&b_s[w], j & 1, &s_gave_up);
+      if (__any_sync(FULL, *reinterpret_cast<volatile int*>(&s_gave_up))) break;
       tc_fence_after();
       float s[4][32];
 #pragma unroll
@@ -567,25 +576,23 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       auto weights = [&](int half, bool find, u32 (&p)[32]) {
         const float ref = m == -INFINITY ? 0.0f : m;
         const u64 sc2 = pair(scale2, scale2), neg = pair(-ref, -ref);
-        u64 sum[2] = {0, 0};
+        u64 sum[2] = {0, 0}, e[32];
+        constexpr int LAG = 4;                // pairs on their way through the special function unit (8 clocks a value, some 40 to the result)
 #pragma unroll
-        for (int b = 0; b < 64; b += 16) {    // eight pairs at a time, so that no result is waited for
-          u64 e[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) e[i] = fma_pair(pair(s[2 * half + b / 32][b % 32 + 2 * i], s[2 * half + b / 32][b % 32 + 2 * i + 1]), sc2, neg);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            e[i] = pair(exp2_fast(lo_of(e[i])), exp2_fast(hi_of(e[i])));
+        for (int i = 0; i < 32 + LAG; ++i) {
+          if (i < 32) {
+            const int c = 2 * half + i / 16, k = 2 * i % 32;
+            const u64 y = fma_pair(pair(s[c][k], s[c][k + 1]), sc2, neg);
+            e[i] = pair(exp2_fast(lo_of(y)), exp2_fast(hi_of(y)));
             if (find) {
-              const int k = 2 * b + 4 * i;
+              const int k4 = 4 * i;
 #pragma unroll
-              for (int y = 0; y < 4; y += 2) x[(i & 1) * 2 + y / 2] = fmaxf(x[(i & 1) * 2 + y / 2], fmaxf(s[k / 32][k % 32 + y], s[k / 32][k % 32 + y + 1]));
+              for (int z = 0; z < 4; z += 2) x[(i & 1) * 2 + z / 2] = fmaxf(x[(i & 1) * 2 + z / 2], fmaxf(s[k4 / 32][k4 % 32 + z], s[k4 / 32][k4 % 32 + z + 1]));
             }
           }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            sum[i & 1] = add_pair(sum[i & 1], e[i]);
-            p[b / 2 + i] = pack2<F16>(lo_of(e[i]), hi_of(e[i]));
+          if (i >= LAG) {
+            sum[i & 1] = add_pair(sum[i & 1], e[i - LAG]);
+            p[i - LAG] = pack2<F16>(lo_of(e[i - LAG]), hi_of(e[i - LAG]));
           }
         }
         const u64 both = add_pair(sum[0], sum[1]);
@@ -632,12 +639,11 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       bar_arrive(&b_pb[w]);
     }
     // ---- output
-    if (ok && steps[w] > 0) {
-      ok = bar_wait(&b_o[w], 0, &s_gave_up);
-      ok = !__any_sync(FULL, !ok);
+    if (steps[w] > 0) {
+      bar_wait(&b_o[w], 0, &s_gave_up);
       tc_fence_after();
     }
-    if (ok) {
+    if (!__any_sync(FULL, *reinterpret_cast<volatile int*>(&s_gave_up))) {
       const float f = l == 0.0f ? 0.0f : a.v_factor / l;
       // through shared memory (the tile's Q is not needed any more), so that the stores are whole rows
       i64 at = -1;                            // of this thread's row, in elements
