@@ -57,26 +57,42 @@ int launch_split_shape(const Attend& a, int D, int nt, const Gpu& gpu, cudaStrea
 // tokens of one block.  Returns the tokens of a box, 0 where the block size (or the strides) allows none.
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-u32 make_tensor_map(const Attend& a, bool half, int D, CUtensorMap* map) {
+EncodeTiled encode_tiled() {                 // null where the driver has none
   static std::atomic<void*> entry{nullptr};
-  const u32 B = a.cache.block_tokens;
-  if (B % 8 || (PR_KEYS % B && B % PR_KEYS)) return 0;
   void* fn = entry.load(std::memory_order_acquire);
   if (!fn) {
     cudaDriverEntryPointQueryResult got;
     if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &got) != cudaSuccess || got != cudaDriverEntryPointSuccess) {
       (void)cudaGetLastError();
-      return 0;
+      return nullptr;
     }
     entry.store(fn, std::memory_order_release);
   }
+  return reinterpret_cast<EncodeTiled>(fn);
+}
+bool encode(CUtensorMap* map, bool half, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* boxes) {
+  const EncodeTiled fn = encode_tiled();
+  const cuuint32_t steps[5] = {1, 1, 1, 1, 1};
+  return fn && fn(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, boxes, steps,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+u32 make_tensor_map(const Attend& a, bool half, int D, CUtensorMap* map) {
+  const u32 B = a.cache.block_tokens;
+  if (B % 8 || (PR_KEYS % B && B % PR_KEYS)) return 0;
   const u32 box = B < PR_KEYS ? B : PR_KEYS;
   const cuuint64_t dims[5] = {(cuuint64_t)D, a.cache.heads, B, a.cache.num_blocks, 2};
   const cuuint64_t strides[4] = {(cuuint64_t)D * 2, (cuuint64_t)a.cache.heads * D * 2, a.cache.block_stride, a.cache.kv_stride};
-  const cuuint32_t boxes[5] = {64, 1, box, 1, 1}, steps[5] = {1, 1, 1, 1, 1};
-  const CUresult r = reinterpret_cast<EncodeTiled>(fn)(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, a.cache.base, dims, strides, boxes, steps,
-                                                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? box : 0;
+  const cuuint32_t boxes[5] = {64, 1, box, 1, 1};
+  return encode(map, half, 5, a.cache.base, dims, strides, boxes) ? box : 0;
+}
+// The tensor map of q: boxes of 128 rows in the order of a row tile (tokens, then the heads of a group), where the group divides 128 and the
+// softmax scale is positive (its sign goes into q).
+bool make_q_map(const Attend& a, bool half, int D, CUtensorMap* map) {
+  if (128 % a.group || a.scale2 < 0.0f || a.q_token <= 0 || a.q_head <= 0) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)a.heads, (cuuint64_t)a.tokens};
+  const cuuint64_t strides[2] = {(cuuint64_t)a.q_head * 2, (cuuint64_t)a.q_token * 2};
+  const cuuint32_t boxes[3] = {64, (cuuint32_t)a.group, 128u / a.group};
+  return encode(map, half, 3, a.q, dims, strides, boxes);
 }
 
 template <int FMT, bool QFP16, int D>
@@ -94,8 +110,12 @@ int launch_prompt(Attend a, const Gpu& gpu, cudaStream_t s) {
   const i64 tiles = (i64)a.tokens * a.group / PR_ROWS + a.R;            // at most this many, wherever the requests' rows end
   if (tiles * a.cache.heads > 0x7FFFFFFF) return PTSTORE_E_LIMIT;
   CUtensorMap map = {};
-  a.box_tokens = FMT == PTSTORE_KV_PACKED ? 0 : make_tensor_map(a, FMT == PTSTORE_KV_FP16, D, &map);
-  kernel<<<(unsigned)(tiles * a.cache.heads), PR_THREADS, SMEM, s>>>(a, map);
+  CUtensorMap q_map = {};
+  if (FMT != PTSTORE_KV_PACKED) {
+    a.box_tokens = make_tensor_map(a, FMT == PTSTORE_KV_FP16, D, &map);
+    a.q_box = make_q_map(a, FMT == PTSTORE_KV_FP16, D, &q_map);
+  }
+  kernel<<<(unsigned)(tiles * a.cache.heads), PR_THREADS, SMEM, s>>>(a, map, q_map);
   return cudaGetLastError() == cudaSuccess ? PTSTORE_OK : PTSTORE_E_CUDA;
 }
 
@@ -142,7 +162,7 @@ extern "C" int ptstore_attend(const ptstore_attend_t* p, const ptstore_kv_cache_
   a.v_factor = packed ? cache->v_scale * DEQ_FACTOR : 1.0f;
   a.work = static_cast<unsigned char*>(workspace);
   a.status = status;
-  a.box_tokens = 0;
+  a.box_tokens = a.q_box = 0;
   Gpu gpu;
   (void)cudaGetLastError();
   const int rs = current_gpu(&gpu);

@@ -20,6 +20,7 @@ struct Attend {
   float v_factor;                             // what the 4-bit values of V are multiplied by at the end (1 for 16-bit caches)
   unsigned char* work;
   u32 box_tokens;                             // tokens of a box of the cache's tensor map, 0: there is none
+  u32 q_box;                                  // there is a tensor map of q
   u32* status;
 };
 

@@ -58,6 +58,11 @@ __device__ __forceinline__ void tensor_load(u32 dst, const CUtensorMap* map, int
   asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst), "l"(map), "r"(element),
                "r"(head), "r"(token), "r"(block), "r"(v), "r"(smem_addr(bar)) : "memory");
 }
+// one box of q's tensor map {64 elements of a head, the heads of a group, tokens}: rows in the order of a row tile
+__device__ __forceinline__ void tensor_load_q(u32 dst, const CUtensorMap* map, int element, int head, int token, u64* bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(element), "r"(head),
+               "r"(token), "r"(smem_addr(bar)) : "memory");
+}
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -136,7 +141,7 @@ __device__ __forceinline__ i64 prompt_tiles(const Attend& a, int r) {
 }
 
 template <int FMT, bool QFP16, int D>
-__global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Attend a, const __grid_constant__ CUtensorMap map) {
+__global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Attend a, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map) {
   constexpr bool PACKED = FMT == PTSTORE_KV_PACKED;
   constexpr bool F16 = PACKED || FMT == PTSTORE_KV_FP16;
   constexpr int TB = PromptShape<D>::TILE_BYTES, CPR = D / 8;           // bytes of a tile, 16-byte chunks of a row
@@ -478,8 +483,18 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     // ======== softmax of tile w
     regs_more<200>();
     const int w = warp >> 2, t = tid & 127, row = w * 128 + t;
-    // its half of Q: chunk t % CPR of rows t / CPR, ..., all on their way before the first is used; the sign of the softmax scale goes into Q
-    {
+    // its half of Q.  Through a tensor map where the group divides a tile (rows behind the request's last bring someone's values or
+    // zeros along and are not stored); else chunk t % CPR of rows t / CPR, ..., all on their way before the first is used, with the
+    // sign of the softmax scale and the changes a 4-bit cache asks for.  (Copied by the threads a CTA's first scores came 6000
+    // clocks later, of 50,000 to 150,000 in all.)
+    if (!PACKED && a.q_box) {
+      if (t == 0) {
+        bar_expect(&b_q[w], TB);
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e)
+          tensor_load_q(smem_q + w * TB + e * (PR_KEYS * 128), &q_map, e * 64, h * a.group, rq.row0 + (row_base + w * 128) / a.group, &b_q[w]);
+      } else bar_arrive(&b_q[w]);
+    } else {
       constexpr int RPP = 128 / CPR;
       const int c = t % CPR;
       const bool flip = a.scale2 < 0.0f;
@@ -532,14 +547,14 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
           for (int k = 0; k < 4; ++k) x[k] = y[k];
         }
         *reinterpret_cast<uint4*>(smem + w * TB + operand_at(n, c)) = make_uint4(x[0], x[1], x[2], x[3]);
-        if (c == 0) s_qf[gr] = factor;
+        if (PACKED && !QFP16 && c == 0) s_qf[gr] = factor;
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       bar_arrive(&b_q[w]);
     }
     const u32 tmem = tmem_there();            // (and every row's factor is there)
     // scale2 as a positive number: of zero, the smallest that keeps masked scores at minus infinity
-    const float scale2 = fmaxf(fabsf(a.scale2) * s_qf[row], 0x1p-126f);
+    const float scale2 = fmaxf(fabsf(a.scale2) * (PACKED && !QFP16 ? s_qf[row] : 1.0f), 0x1p-126f);
     const int see = row < rows ? keys_of(row) : 0;
     const u32 lane_base = (u32)(32 * (warp & 3)) << 16;
     const u32 ts = tmem + lane_base + w * 128, to = tmem + lane_base + 256 + w * 128;
@@ -661,7 +676,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
           tc_loaded(o);
         }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) o[i] = l == 0.0f ? 0.0f : o[i] * f;
+        for (int i = 0; i < 32; ++i) o[i] = steps[w] > 0 ? o[i] * f : 0.0f;        // (weights that are all zero leave zeros)
         if (PACKED) {
 #pragma unroll
           for (int i = 0; i < 32; i += 8) {
