@@ -107,16 +107,22 @@ int launch_prompt(Attend a, const Gpu& gpu, cudaStream_t s) {
   }
   const int rc = allow_smem(kernel, SMEM, devices, gpu.dev);
   if (rc) return rc;
-  const i64 tiles = (i64)a.tokens * a.group / PR_ROWS + a.R;            // at most this many, wherever the requests' rows end
-  if (tiles * a.cache.heads > 0x7FFFFFFF) return PTSTORE_E_LIMIT;
+  const i64 tiles = ((i64)a.tokens * a.group / PR_ROWS + a.R) * a.cache.heads;            // at most this many, wherever the requests' rows end
+  if (tiles > 0x7FFFFFFF) return PTSTORE_E_LIMIT;
+  a.split = tiles <= gpu.sms / 2 ? gpu.sms : 0;
   CUtensorMap map = {};
   CUtensorMap q_map = {};
   if (FMT != PTSTORE_KV_PACKED) {
     a.box_tokens = make_tensor_map(a, FMT == PTSTORE_KV_FP16, D, &map);
     a.q_box = make_q_map(a, FMT == PTSTORE_KV_FP16, D, &q_map);
   }
-  kernel<<<(unsigned)(tiles * a.cache.heads), PR_THREADS, SMEM, s>>>(a, map, q_map);
-  return cudaGetLastError() == cudaSuccess ? PTSTORE_OK : PTSTORE_E_CUDA;
+  kernel<<<a.split ? a.split : (unsigned)tiles, PR_THREADS, SMEM, s>>>(a, map, q_map);
+  if (cudaGetLastError() != cudaSuccess) return PTSTORE_E_CUDA;
+  if (a.split) {
+    attend_join_kernel<QFP16, D><<<(unsigned)(((i64)a.tokens * a.heads + 7) / 8), 256, 0, s>>>(a);
+    if (cudaGetLastError() != cudaSuccess) return PTSTORE_E_CUDA;
+  }
+  return PTSTORE_OK;
 }
 
 // Rows of one kv head from which a request's attention goes to the tensor-memory kernel.
@@ -126,8 +132,11 @@ constexpr i64 PROMPT_ROWS = 33;
 
 extern "C" uint64_t ptstore_attend_workspace_bytes(uint32_t head_dim) {
   if (head_dim != 64 && head_dim != 128) return 0;
-  // counters, and two parts per CTA: of 8 rows where 4 CTAs share an SM, of 16 where 2 do
-  return counters_bytes(MAX_SMS * 4) + (u64)MAX_SMS * 4 * 2 * 8 * (head_dim + 2) * 4;
+  // counters, then two parts per CTA of the split kernel (of 8 rows where 4 CTAs share an SM, of 16 where 2 do), or one of 256 rows per SM
+  static_assert(counters_bytes(MAX_SMS * 4) <= PR_PARTS_AT, "the prompts' parts lie behind the counters");
+  const u64 split = counters_bytes(MAX_SMS * 4) + (u64)MAX_SMS * 4 * 2 * 8 * (head_dim + 2) * 4;
+  const u64 prompt = PR_PARTS_AT + (u64)MAX_SMS * PR_ROWS * (head_dim + 2) * 4;
+  return split > prompt ? split : prompt;
 }
 
 extern "C" int ptstore_attend(const ptstore_attend_t* p, const ptstore_kv_cache_t* cache, void* workspace, uint64_t workspace_bytes,
@@ -162,7 +171,7 @@ extern "C" int ptstore_attend(const ptstore_attend_t* p, const ptstore_kv_cache_
   a.v_factor = packed ? cache->v_scale * DEQ_FACTOR : 1.0f;
   a.work = static_cast<unsigned char*>(workspace);
   a.status = status;
-  a.box_tokens = a.q_box = 0;
+  a.box_tokens = a.q_box = a.split = 0;
   Gpu gpu;
   (void)cudaGetLastError();
   const int rs = current_gpu(&gpu);

@@ -21,6 +21,7 @@ struct Attend {
   unsigned char* work;
   u32 box_tokens;                             // tokens of a box of the cache's tensor map, 0: there is none
   u32 q_box;                                  // there is a tensor map of q
+  u32 split;                                  // CTAs among which the steps of the row tiles may be cut, 0: they are not
   u32* status;
 };
 

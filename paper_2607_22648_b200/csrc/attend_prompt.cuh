@@ -14,6 +14,9 @@
 // four 128-token tiles, 12 issues the tensor instructions (one thread).  13-15 only complete the warpgroup that gives its
 // registers to the softmax warps.
 //
+// When a batch has fewer row tiles than half the SMs (one prompt whose prefix was found), the steps of every tile are cut into as many
+// chunks as there are SMs for it; a chunk leaves its O, m and l in the workspace and attend_join_kernel, one warp per row, joins them.
+//
 // Tensor memory (512 columns): S/P of tile 0, S/P of tile 1, O 0, O 1.  Shared memory operands are in the 128-byte swizzled form: 64
 // elements of a row are 128 bytes, 16-byte chunk c of row r at c ^ (r & 7), 64-element halves one after the other.
 #pragma once
@@ -25,6 +28,7 @@ namespace ptk {
 
 constexpr int PR_THREADS = 512;
 constexpr int PR_ROWS = 256, PR_KEYS = 128;
+constexpr int PR_PARTS_AT = 4096;            // where the parts begin in the workspace (behind the other kernel's counters)
 constexpr int PR_SLOTS = 4;
 constexpr u32 PR_POLLS = 1u << 22;           // polls of a wait before the CTA gives up (each may suspend for a while)
 
@@ -135,6 +139,10 @@ __device__ __forceinline__ void regs_fewer() { asm volatile("setmaxnreg.dec.sync
 // byte of 16-byte chunk c of row r in an operand tile of 128 rows
 __device__ __forceinline__ u32 operand_at(int r, int c) { return (u32)((c >> 3) * (PR_KEYS * 128) + r * 128 + (((c & 7) ^ (r & 7)) * 16)); }
 
+// chunks per row tile (of one kv head), given their number and how many CTAs there are
+__device__ __forceinline__ int prompt_parts(i64 tiles, u32 ctas) { return tiles > 0 && tiles < ctas ? (int)(ctas / (u32)tiles) : 1; }
+template <int D>
+__host__ __device__ constexpr int prompt_part_floats() { return PR_ROWS * (D + 2); }        // o, m, l of a tile's rows
 __device__ __forceinline__ i64 prompt_tiles(const Attend& a, int r) {
   const Req q = request(a, r);
   return ((i64)q.fresh * a.group + PR_ROWS - 1) / PR_ROWS;
@@ -158,8 +166,8 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0);
 
   // ---- which 256 rows: heads vary fastest; a request's tiles come last to first, the ones with most keys first
-  const int h = blockIdx.x % a.cache.heads;
-  const i64 index = blockIdx.x / a.cache.heads;
+  int h, part = 0, parts = 1;                // this CTA's chunk of the tile's steps
+  u32 cta = blockIdx.x;
   {
     const int per_thread = (a.R + PR_THREADS - 1) / PR_THREADS;
     const int rb = tid * per_thread < a.R ? tid * per_thread : a.R, re = rb + per_thread < a.R ? rb + per_thread : a.R;
@@ -176,6 +184,15 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     __syncthreads();
     i64 before = x - mine;
     for (int w = 0; w < warp; ++w) before += s_scan[w];
+    if (a.split) {
+      i64 all = 0;
+      for (int w = 0; w < PR_THREADS / 32; ++w) all += s_scan[w];
+      parts = prompt_parts(all * a.cache.heads, a.split);
+      part = cta % parts;
+      cta /= parts;
+    }
+    h = cta % a.cache.heads;
+    const i64 index = cta / a.cache.heads;
     if (index >= before && index < before + mine) {
       i64 left = index - before;
       int r = rb;
@@ -207,7 +224,14 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
   };
   const int keys0 = keys_of(min(rows, 128) - 1), keys1 = rows > 128 ? keys_of(rows - 1) : 0;
   const int keys = max(keys0, keys1), all_see = keys_of(0);
-  const int steps[2] = {(keys0 + PR_KEYS - 1) / PR_KEYS, (keys1 + PR_KEYS - 1) / PR_KEYS};
+  int steps[2] = {(keys0 + PR_KEYS - 1) / PR_KEYS, (keys1 + PR_KEYS - 1) / PR_KEYS};
+  int key0 = 0;                               // first key of this CTA's steps
+  if (parts > 1) {
+    const int len = (max(steps[0], steps[1]) + parts - 1) / parts, j0 = part * len;
+    steps[0] = min(max(steps[0] - j0, 0), len);
+    steps[1] = min(max(steps[1] - j0, 0), len);
+    key0 = j0 * PR_KEYS;
+  }
   const int n_steps = max(steps[0], steps[1]);
   const u32 smem_q = smem_addr(smem), smem_kv = smem_q + 2 * TB;
 
@@ -313,7 +337,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     // where key `pt` of a step lies
     u32 id = 0;
     auto where = [&](int j) -> i64 {
-      const int key = j * PR_KEYS + pt;
+      const int key = key0 + j * PR_KEYS + pt;
       if (key >= keys) return -1;
       const u32 blk = (u32)key / B, in = (u32)key % B;
       id = (u32)table[blk];
@@ -339,7 +363,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
         unsigned char* t = smem + (2 + op % PR_SLOTS) * TB;
         constexpr u32 EX = F16 ? 0x7C00u : 0x7F80u, MANT = F16 ? 0x03FFu : 0x007Fu;
         for (int i = 0; i < CPR; ++i) {
-          const int n = i * RPP + r0, key = (op >> 1) * PR_KEYS + n;
+          const int n = i * RPP + r0, key = key0 + (op >> 1) * PR_KEYS + n;
           if (key < all_see) continue;
           unsigned short* p = reinterpret_cast<unsigned short*>(t + operand_at(n, c));
           const uint4 v = *reinterpret_cast<const uint4*>(p);
@@ -371,7 +395,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
         if (lane == 0) s_valid[j & 3][warp - 8] = present;
         if (j + 1 < n_steps) next = where(j + 1);
         if (any_of_128(*gave_up)) { stop = true; break; }
-        const bool plain = box && (j + 1) * PR_KEYS <= all_see && (s_valid[j & 3][0] & s_valid[j & 3][1] & s_valid[j & 3][2] & s_valid[j & 3][3]) == FULL;
+        const bool plain = box && key0 + (j + 1) * PR_KEYS <= all_see && (s_valid[j & 3][0] & s_valid[j & 3][1] & s_valid[j & 3][2] & s_valid[j & 3][3]) == FULL;
         for (int is_v = 0; is_v < 2; ++is_v) {
           const int op = 2 * j + is_v;
           wait_empty(op);
@@ -382,7 +406,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
               bar_expect(full, box * D * 2);
 #pragma unroll
               for (int e = 0; e < D / 64; ++e)
-                tensor_load(dst + e * (PR_KEYS * 128) + pt * 128, &map, e * 64, h, (int)((u32)(j * PR_KEYS + pt) % B), (int)block, is_v, full);
+                tensor_load(dst + e * (PR_KEYS * 128) + pt * 128, &map, e * 64, h, (int)((u32)(key0 + j * PR_KEYS + pt) % B), (int)block, is_v, full);
             } else bar_arrive(full);
             continue;
           }
@@ -393,10 +417,10 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
             const i64 off = s_row[j & 1][n];
             cp_async16_or_zero(dst + operand_at(n, c), base + (off < 0 ? 0 : off), off >= 0);
           }
-          if (box || (is_v && (j + 1) * PR_KEYS > all_see)) {
+          if (box || (is_v && key0 + (j + 1) * PR_KEYS > all_see)) {
             cp_commit();
             cp_wait<0>();
-            if (is_v && (j + 1) * PR_KEYS > all_see) mend(op);
+            if (is_v && key0 + (j + 1) * PR_KEYS > all_see) mend(op);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             bar_arrive(full);
           } else cp_arrive(full);             // arrives when this thread's copies have landed
@@ -423,7 +447,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
           if (lane == 0) s_valid[j & 3][warp - 8] = there;
         }
         if (has) {
-          const int n = (int)((u32)(j * PR_KEYS + pt) % B % TILE);
+          const int n = (int)((u32)(key0 + j * PR_KEYS + pt) % B % TILE);
           const unsigned char* t = a.cache.base + (is_v ? a.cache.kv_stride : 0) + off;
 #pragma unroll
           for (int c = 0; c < D / 32; ++c) *reinterpret_cast<uint4*>(code + 4 * c) = __ldg(reinterpret_cast<const uint4*>(t + code_place(D, n, c) * 16));
@@ -451,7 +475,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
         for (int i = 0; i < D / 64; ++i) sc[i] = scale[i];
         if (op + 1 < 2 * n_steps) load(op + 1);
         wait_empty(op);
-        const int key = (op >> 1) * PR_KEYS + pt;
+        const int key = key0 + (op >> 1) * PR_KEYS + pt;
         if ((op & 1) && cur_has && key >= all_see) {
 #pragma unroll
           for (int g = 0; g < D / 16; ++g) {
@@ -572,7 +596,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       u32 there[4];
 #pragma unroll
       for (int c = 0; c < 4; ++c) there[c] = s_valid[j & 3][c];
-      const int k0 = j * PR_KEYS;
+      const int k0 = key0 + j * PR_KEYS;
       if (k0 + PR_KEYS > all_see || (there[0] & there[1] & there[2] & there[3]) != FULL) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
@@ -659,7 +683,12 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       tc_fence_after();
     }
     if (!__any_sync(FULL, *reinterpret_cast<volatile int*>(&s_gave_up))) {
-      const float f = l == 0.0f ? 0.0f : a.v_factor / l;
+      const float f = parts > 1 ? 1.0f : l == 0.0f ? 0.0f : a.v_factor / l;
+      float* const sums = reinterpret_cast<float*>(a.work + PR_PARTS_AT) + (i64)blockIdx.x * prompt_part_floats<D>();
+      if (parts > 1) {
+        sums[PR_ROWS * D + row] = m;
+        sums[PR_ROWS * D + PR_ROWS + row] = l;
+      }
       // through shared memory (the tile's Q is not needed any more), so that the stores are whole rows
       i64 at = -1;                            // of this thread's row, in elements
       if (row < rows) {
@@ -693,6 +722,13 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
             else if (neg) o[i] = o[i] - INFINITY;
           }
         }
+        if (parts > 1) {
+          if (row < rows) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(sums + row * D + c + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+          }
+          continue;
+        }
 #pragma unroll
         for (int i = 0; i < 32; i += 8)
           *reinterpret_cast<uint4*>(mine + operand_at(t, (c + i) / 8)) =
@@ -700,7 +736,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       }
       __syncwarp();
 #pragma unroll 8
-      for (int i = 0; i < CPR; ++i) {         // this warp's 32 rows, whole rows at a time
+      for (int i = 0; i < CPR && parts == 1; ++i) {         // this warp's 32 rows, whole rows at a time
         const int n = i * (32 / CPR) + lane / CPR, c = lane % CPR;
         const i64 to = __shfl_sync(FULL, at, n);
         if (to >= 0) *reinterpret_cast<uint4*>(a.out + 2 * (to + c * 8)) = *reinterpret_cast<const uint4*>(mine + operand_at((warp & 3) * 32 + n, c));
@@ -713,6 +749,48 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(s_tmem) : "memory");
     if (lane == 0 && s_gave_up && a.status) atomicOr(a.status, PTSTORE_S_TIMEOUT);
   }
+}
+
+// Joins the chunks of a batch that was cut (see prompt_parts): one warp per row of q and query head, D / 32 values a lane.
+template <bool QFP16, int D>
+__global__ void __launch_bounds__(256) attend_join_kernel(const Attend a) {
+  const int lane = threadIdx.x & 31, flat = blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int i = flat / a.heads, hq = flat % a.heads;
+  if (i >= a.tokens) return;
+  // the request of row i, and the row tiles before it (at most half as many requests as SMs: see the host)
+  i64 tiles = 0, ahead = 0;
+  int mine = -1;
+  Req q = {};
+  for (int r = 0; r < a.R; ++r) {
+    const Req x = request(a, r);
+    if (i >= x.row0 && i < x.row0 + x.fresh) { mine = r; q = x; ahead = tiles; }
+    tiles += prompt_tiles(a, r);
+  }
+  const int parts = prompt_parts(tiles * a.cache.heads, a.split);
+  if (mine < 0 || parts <= 1) return;         // rows of no request; or nothing was cut and the rows are written
+  const u32 row = (u32)(i - q.row0) * a.group + hq % a.group, tile = row / PR_ROWS;
+  const i64 cta = (ahead + (prompt_tiles(a, mine) - 1 - tile)) * a.cache.heads + hq / a.group;
+  const float* const base = reinterpret_cast<const float*>(a.work + PR_PARTS_AT) + cta * parts * prompt_part_floats<D>();
+  const u32 at = row % PR_ROWS;
+  float top = -INFINITY;
+  for (int p = lane; p < parts; p += 32) top = fmaxf(top, base[(i64)p * prompt_part_floats<D>() + PR_ROWS * D + at]);
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
+  constexpr int E = D / 32;
+  float acc[E] = {}, sum = 0.0f;
+#pragma unroll 4
+  for (int p = 0; p < parts; ++p) {
+    const float* x = base + (i64)p * prompt_part_floats<D>();
+    const float m = x[PR_ROWS * D + at], l = x[PR_ROWS * D + PR_ROWS + at];
+    const float f = m == -INFINITY ? 1.0f : exp2_fast(m - top);      // a chunk that the row sees nothing of: sums of zero (or NaN)
+    sum += l * f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] += x[at * D + lane * E + e] * f;
+  }
+  const float f = sum == 0.0f ? 0.0f : a.v_factor / sum;
+  u32* const dst = reinterpret_cast<u32*>(a.out + 2 * ((i64)i * a.o_token + (i64)hq * a.o_head + lane * E));
+#pragma unroll
+  for (int e = 0; e < E; e += 2) dst[e / 2] = pack2<QFP16>(acc[e] * f, acc[e + 1] * f);
 }
 
 }  // namespace ptk

@@ -399,6 +399,48 @@ def test_infinities_and_nan_in_later_tokens_do_not_reach_earlier_rows(G, fmt, dt
 
 
 @pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("heads,kv_heads,dim,block", [(16, 4, 128, 16), (10, 2, 64, 48), (24, 8, 128, 128)])
+def test_many_prompts(G, fmt, dtype, heads, kv_heads, dim, block):
+    """More row tiles than the GPU has room for at once: steps are not cut into chunks (in the tests above they are)."""
+    rng = random.Random(heads)
+    lens = [rng.randint(1, 220) for _ in range(150 // kv_heads)] + [700]
+    new = [rng.choice([n, n, rng.randint(0, n)]) for n in lens[:-1]] + [400]
+    b = make(G, getattr(G, fmt), dtype, heads, kv_heads, dim, block, lens, new, seed=heads)
+    call(G, b)
+    check(G, b)
+    # the last token of every whole prompt turns into NaN: nothing before it changes
+    clean = b["out"].clone()
+    rows_of = [(r, b["offsets"][r + 1] - 1) for r in range(len(lens)) if new[r] > 1]
+    slots = torch.tensor([int(b["tables"][r, (lens[r] - 1) // block]) * block + (lens[r] - 1) % block for r, _ in rows_of], device="cuda")
+    bad = torch.full((len(rows_of), kv_heads, dim), float("nan"), dtype=dtype, device="cuda")
+    G.kv_write(b["lay"], b["cache"], 0, bad, bad, slots)
+    b["out"].fill_(5.0)
+    call(G, b)
+    keep = torch.ones(b["out"].shape[0], dtype=torch.bool, device="cuda")
+    keep[[i for _, i in rows_of]] = False
+    assert torch.equal(b["out"][keep], clean[keep]) and not bool(torch.isfinite(b["out"][~keep]).any())
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("new", [40, 64, 300])
+def test_one_prompt_behind_a_long_prefix(G, fmt, dtype, new):
+    """One request's steps spread over the GPU and joined; equal bits every time; scores that grow along the prefix."""
+    b = make(G, getattr(G, fmt), dtype, 8, 2, 128, 16, [4096 + new], [new], seed=new)
+    ws = G.attend_workspace(b["lay"])
+    call(G, b, workspace=ws)
+    check(G, b)
+    first = b["out"].clone()
+    for _ in range(2):
+        b["out"].fill_(5.0)
+        call(G, b, workspace=ws)
+        assert torch.equal(first, b["out"])
+    # the split kernel finds its counters as it left them
+    d = make(G, getattr(G, fmt), dtype, 8, 2, 128, 16, [5000, 70], [1, 1], seed=2)
+    call(G, d, workspace=ws)
+    check(G, d)
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
 def test_large_and_equal_scores(G, fmt, dtype):
     """Scores far beyond the range of exp, equal scores, a scale of zero and a negative one."""
     for scale in (None, 0.0, -0.1, 20.0):
