@@ -100,16 +100,25 @@ __global__ void __launch_bounds__(WRITE_THREADS) kv_write_kernel(KvArgs a) {
   const float e = e4m3_value(sb) * t;                  // exact: 4 significant bits times a power of two
   u32 code[2] = {0x88888888u, 0x88888888u};            // code 8 is zero
   if (e > 0.0f) {
-    const float inv = __frcp_rn(e), most = 9.0f * e;
-    code[0] = code[1] = 0;
+    const float inv = __frcp_rn(e);
+    if (amax > 8.4f * e) {                             // the scale is far too small for the largest (at most 448): codes saturate well inside
+      const float most = 9.0f * e;                     // this, and an infinity becomes finite
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = fminf(fmaxf(x[i], -most), most);
+    }
+    u32 sum[2] = {0, 0};
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float c = fminf(fmaxf(x[i], -most), most); // codes saturate far inside this; an infinity becomes finite
-      const float y = c * inv;
-      const float q = fmaf(fmaf(-y, e, c), inv, y);    // the quotient, exact where it is representable
-      const float n = fminf(fmaxf(q, -8.0f), 7.0f) + 12582912.0f;      // 1.5 * 2^23: rounds to an integer, ties to even
-      code[i >> 3] |= ((__float_as_uint(n) + 8u) & 15u) << (4 * (i & 7));
+      const float y = x[i] * inv;
+      const float q = fmaf(fmaf(-y, e, x[i]), inv, y); // the quotient, exact where it is representable
+      // adding 1.5 * 2^23 + 8 rounds to an integer, ties to even, and leaves the code in the low bits: the words are sums of
+      // these bit patterns times powers of 16, less what the constant's bits add up to
+      const float n = fminf(fmaxf(q, -8.0f), 7.0f) + 12582920.0f;
+      sum[i >> 3] += __float_as_uint(n) << (4 * (i & 7));
     }
+    constexpr u32 B = 0x4B400000u, REST = B + (B << 4) + (B << 8) + (B << 12) + (B << 16) + (B << 20) + (B << 24) + (B << 28);
+    code[0] = sum[0] - REST;
+    code[1] = sum[1] - REST;
   }
   unsigned char* tile = tile_ptr(a.cache, is_v, w.block, w.head, w.token, D);
   const int n = w.token % TILE;
@@ -136,12 +145,19 @@ __global__ void __launch_bounds__(WRITE_THREADS) kv_read_kernel(KvArgs a) {
   const int n = w.token % TILE;
   const uint2 code = *reinterpret_cast<const uint2*>(tile + code_place(D, n, w.group >> 1) * 16 + (w.group & 1) * 8);
   const float e = e4m3_value(tile[scale_at(D, is_v, n, w.group)]) * (is_v ? a.v_scale : a.k_scale);
+  // code n at bits p .. p+3 of 2^23 reads as 2^23 + n 2^p: less 2^23 + 8 2^p it is (n - 8) 2^p, exactly (p <= 16)
   u32 out[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const u32 c = i < 4 ? code.x : code.y;
-    const int s = 8 * (i & 3);
-    out[i] = narrow<FP16>(e * ((int)((c >> s) & 15u) - 8), e * ((int)((c >> (s + 4)) & 15u) - 8));
+    const u32 c = (i < 4 ? code.x : code.y) >> (16 * ((i >> 1) & 1));
+    const int p = 8 * (i & 1);
+    float v[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float f = __uint_as_float((c & (15u << (p + 4 * k))) | 0x4B000000u) - (8388608.0f + 8.0f * (float)(1 << (p + 4 * k)));
+      v[k] = f * (e * (1.0f / (float)(1 << (p + 4 * k))));
+    }
+    out[i] = narrow<FP16>(v[0], v[1]);
   }
   dst[0] = make_uint4(out[0], out[1], out[2], out[3]);
   dst[1] = make_uint4(out[4], out[5], out[6], out[7]);
