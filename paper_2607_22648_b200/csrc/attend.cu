@@ -98,7 +98,7 @@ bool make_q_map(const Attend& a, bool half, int D, CUtensorMap* map) {
 template <int FMT, bool QFP16, int D>
 int launch_prompt(Attend a, const Gpu& gpu, cudaStream_t s) {
   auto* kernel = attend_prompt_kernel<FMT, QFP16, D>;
-  constexpr int SMEM = PromptShape<D>::SMEM;
+  constexpr int SMEM = FMT == PTSTORE_KV_PACKED ? PromptShape<D>::SMEM_PACKED : PromptShape<D>::SMEM;
   static std::atomic<u64> devices{0};
   if (gpu.dev >= 64 || !(devices.load(std::memory_order_acquire) >> gpu.dev & 1)) {
     // the kernel's warps trade registers, which is only sound if the block is launched with all of the SM's

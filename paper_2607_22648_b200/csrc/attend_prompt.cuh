@@ -12,7 +12,7 @@
 //
 // Warps: 0-3 and 4-7 softmax of tile 0 and 1 (and their part of Q at the start and of the output at the end), 8-11 load K and V into a ring of
 // four 128-token tiles, 12 issues the tensor instructions (one thread).  13-15 only complete the warpgroup that gives its
-// registers to the softmax warps.
+// registers to the softmax warps; for a 4-bit cache 13 loads its tiles and 8-11 unpack them.
 //
 // When a batch has fewer row tiles than half the SMs (one prompt whose prefix was found), the steps of every tile are cut into as many
 // chunks as there are SMs for it; a chunk leaves its O, m and l in the workspace and attend_join_kernel, one warp per row, joins them.
@@ -30,12 +30,15 @@ constexpr int PR_THREADS = 512;
 constexpr int PR_ROWS = 256, PR_KEYS = 128;
 constexpr int PR_PARTS_AT = 4096;            // where the parts begin in the workspace (behind the other kernel's counters)
 constexpr int PR_SLOTS = 4;
+constexpr int PR_RAW = 3;                    // 4-bit tiles on their way to being unpacked
 constexpr u32 PR_POLLS = 1u << 22;           // polls of a wait before the CTA gives up (each may suspend for a while)
 
 template <int D>
 struct PromptShape {
   static constexpr int TILE_BYTES = PR_KEYS * D * 2;                    // one K or V tile, one 128-row half of Q
+  static constexpr int RAW_BYTES = PR_KEYS / TILE * tile_bytes(D);      // 128 keys of a 4-bit cache as they lie there
   static constexpr int SMEM = (2 + PR_SLOTS) * TILE_BYTES + 1024;       // + alignment
+  static constexpr int SMEM_PACKED = SMEM + PR_RAW * RAW_BYTES;
 };
 
 // Waits, at most PR_POLLS polls; a wait that runs out says so and lets its caller go on (with whatever is there: every access stays in bounds
@@ -155,7 +158,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
   constexpr int TB = PromptShape<D>::TILE_BYTES, CPR = D / 8;           // bytes of a tile, 16-byte chunks of a row
   extern __shared__ unsigned char smem_raw[];
   unsigned char* const smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
-  __shared__ __align__(8) u64 b_q[2], b_full[PR_SLOTS], b_empty[PR_SLOTS], b_s[2], b_pa[2], b_pb[2], b_o[2], b_end;
+  __shared__ __align__(8) u64 b_q[2], b_full[PR_SLOTS], b_empty[PR_SLOTS], b_s[2], b_pa[2], b_pb[2], b_o[2], b_end, b_raw[PR_RAW], b_raw_free[PR_RAW];
   __shared__ u32 s_tmem;
   __shared__ int s_gave_up, s_any_bad, s_r, s_tile;
   __shared__ i64 s_scan[PR_THREADS / 32];
@@ -208,6 +211,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       for (int i = 0; i < 2; ++i) { bar_init(&b_q[i], 128); bar_init(&b_s[i], 1); bar_init(&b_pa[i], 128); bar_init(&b_pb[i], 128); bar_init(&b_o[i], 1); }
       for (int i = 0; i < PR_SLOTS; ++i) { bar_init(&b_full[i], 128); bar_init(&b_empty[i], 1); }
       bar_init(&b_end, 1);
+      for (int i = 0; i < PR_RAW; ++i) { bar_init(&b_raw[i], 1); bar_init(&b_raw_free[i], 128); }
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     for (int i = tid; i < 3 * D; i += PR_THREADS) (&s_bad[0][0])[i] = 0x7FFFFFFF;
@@ -325,10 +329,48 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       __syncwarp();
       for (u32 i = 0; i < PR_POLLS && !bar_try(&b_end, 0); ++i) {}
     }
+    if (PACKED && warp == 13) {
+      // ======== 4-bit tiles as they lie in the cache: lanes 0-7 a 16-token tile each, the table entries of the next step on their way
+      constexpr int RAW = PromptShape<D>::RAW_BYTES, TILES = PR_KEYS / TILE;
+      const u32 raw = smem_kv + PR_SLOTS * TB, B = a.cache.block_tokens;
+      const int* table = a.tables + (i64)r * a.max_blocks;
+      bool bounds = false;
+      int next_id = -1;
+      i64 tile_off = -1;
+      auto look_up = [&](int j) {
+        const int key = key0 + j * PR_KEYS + lane * TILE;
+        next_id = lane < TILES && key < keys ? table[(u32)key / B] : -1;
+      };
+      if (n_steps > 0) look_up(0);
+      int op = 0;
+      for (; op < 2 * n_steps && !__any_sync(FULL, *reinterpret_cast<volatile int*>(&s_gave_up)); ++op) {
+        const int j = op >> 1, key = key0 + j * PR_KEYS + lane * TILE;
+        if (op >= PR_RAW) bar_wait(&b_raw_free[op % PR_RAW], (op / PR_RAW - 1) & 1, &s_gave_up);
+        __syncwarp();
+        if (!(op & 1)) {
+          const bool in = lane < TILES && key < keys, have = in && (u32)next_id < a.cache.num_blocks;
+          bounds |= in && !have;
+          tile_off = have ? (i64)((u64)(u32)next_id * a.cache.block_stride + ((u64)h * (B / TILE) + (u32)key % B / TILE) * tile_bytes(D)) : -1;
+          const u32 bits = !have ? 0 : keys - key >= TILE ? 0xFFFFu : (1u << (keys - key)) - 1u;       // keys of the tile that are there
+          const u32 lo = __shfl_sync(FULL, bits, 2 * lane & 31), hi = __shfl_sync(FULL, bits, (2 * lane + 1) & 31);
+          if (lane < 4) s_valid[j & 3][lane] = lo | (hi << 16);
+          if (j + 1 < n_steps) look_up(j + 1);
+        }
+        const u32 there = __ballot_sync(FULL, tile_off >= 0);
+        u64* bar = &b_raw[op % PR_RAW];
+        if (lane == 0) bar_expect(bar, __popc(there) * tile_bytes(D));
+        __syncwarp();
+        if (tile_off >= 0) bulk_load(raw + (op % PR_RAW) * RAW + lane * tile_bytes(D), a.cache.base + (op & 1 ? a.cache.kv_stride : 0) + tile_off, tile_bytes(D), bar);
+      }
+      // whatever happened, what is in flight lands before the CTA gives its memory back
+      for (int k = max(0, op - PR_RAW); k < op; ++k)
+        for (u32 i = 0; i < PR_POLLS && !bar_try(&b_raw[k % PR_RAW], (k / PR_RAW) & 1); ++i) {}
+      if (bounds && a.status) atomicOr(a.status, PTSTORE_S_BOUNDS);
+    }
     __syncwarp();
   } else if (warp >= 8) {
     // ======== K and V into the ring
-    regs_fewer<72>();
+    regs_fewer<PACKED ? 104 : 72>();
     const int pt = tid - 256;
     const int* table = a.tables + (i64)r * a.max_blocks;
     const u32 B = a.cache.block_tokens;
@@ -432,80 +474,59 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       cp_commit();
       cp_wait<0>();
     } else {
-      // one key per thread: its codes and scales are loaded one operand ahead, unpacked and stored as fp16.  Element order inside
-      // eight is 0 4 1 5 2 6 3 7, as the unpacking yields it: Q is stored likewise, and O's columns are put back at the end.
-      __align__(16) u32 code[D / 8];
-      u32 scale[D / 64];
-      bool has = false;
-      auto load = [&](int op) {
-        const int j = op >> 1;
-        const bool is_v = op & 1;
-        const i64 off = where(j);
-        has = off >= 0;
-        if (!is_v) {
-          const u32 there = __ballot_sync(FULL, has);
-          if (lane == 0) s_valid[j & 3][warp - 8] = there;
-        }
-        if (has) {
-          const int n = (int)((u32)(key0 + j * PR_KEYS + pt) % B % TILE);
-          const unsigned char* t = a.cache.base + (is_v ? a.cache.kv_stride : 0) + off;
-#pragma unroll
-          for (int c = 0; c < D / 32; ++c) *reinterpret_cast<uint4*>(code + 4 * c) = __ldg(reinterpret_cast<const uint4*>(t + code_place(D, n, c) * 16));
-          if (is_v) {
-#pragma unroll
-            for (int w = 0; w < D / 64; ++w) {
-              scale[w] = 0;
-#pragma unroll
-              for (int b = 0; b < 4; ++b) scale[w] |= (u32)__ldg(t + scale_at(D, true, n, 4 * w + b)) << (8 * b);
-            }
-          } else {
-#pragma unroll
-            for (int w = 0; w < D / 64; ++w) scale[w] = __ldg(reinterpret_cast<const u32*>(t + scale_at(D, false, n, 4 * w)));
-          }
-        }
-      };
+      // The tiles come as they lie in the cache, by bulk copies three operands ahead, which warp 13 issues (loaded into registers one
+      // operand ahead a step took 5900 clocks, the time of two dependent loads per operand; issued by warp 8, 6000); one key per thread is unpacked and stored as fp16.  Element order
+      // inside eight is 0 4 1 5 2 6 3 7, as the unpacking yields it: Q is stored likewise, and O's columns are put back at the end.
+      constexpr int RAW = PromptShape<D>::RAW_BYTES;
+      unsigned char* const raw = smem + (2 + PR_SLOTS) * TB;
       const Magic mg = magic();
-      if (n_steps > 0) load(0);
+      // a key's places: 16-byte chunk c of its codes at from ^ 16 c, chunk c of its operand row at to ^ 16 (c % 8)
+      const int n = pt % TILE;
+      const u32 from = (pt / TILE) * tile_bytes(D) + code_place(D, n, 0) * 16, to = (u32)operand_at(pt, 0);
+      const u32 scales = (pt / TILE) * tile_bytes(D);
       for (int op = 0; op < 2 * n_steps && !__any_sync(FULL, *gave_up); ++op) {
-        u32 cur[D / 8], sc[D / 64];
-        const bool cur_has = has;
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) cur[i] = code[i];
-#pragma unroll
-        for (int i = 0; i < D / 64; ++i) sc[i] = scale[i];
-        if (op + 1 < 2 * n_steps) load(op + 1);
+        const int j = op >> 1, key = key0 + j * PR_KEYS + pt;
+        bar_wait(&b_raw[op % PR_RAW], (op / PR_RAW) & 1, &s_gave_up);
+        const bool is_v = op & 1, has = (s_valid[j & 3][pt >> 5] >> (pt & 31)) & 1, look = is_v && has && key >= all_see;
+        const unsigned char* const src = raw + (op % PR_RAW) * RAW;
+        const unsigned char* const sc = src + scales + (is_v ? scale_at(D, true, n, 0) : scale_at(D, false, n, 0));
+        const u32 stride = is_v ? TILE : 1;   // of a key's scales
+        unsigned char* const t = smem + (2 + op % PR_SLOTS) * TB;
         wait_empty(op);
-        const int key = key0 + (op >> 1) * PR_KEYS + pt;
-        if ((op & 1) && cur_has && key >= all_see) {
-#pragma unroll
-          for (int g = 0; g < D / 16; ++g) {
-            const u32 sh = 8 * (g & 3);
-            if (((sc[g >> 2] >> sh) & 0x7Fu) == 0x7Fu) {
-              for (int k = 0; k < 16; ++k) note_bad(16 * g + k, 0, key);
-              sc[g >> 2] &= ~(0xFFu << sh);
+#pragma unroll 2
+        for (int c = 0; c < D / 32; ++c) {    // 32 elements: two scale groups, four chunks of the operand
+          const uint4 four = has ? *reinterpret_cast<const uint4*>(src + (from ^ (u32)(c * 16))) : make_uint4(0, 0, 0, 0);
+          u32 b0 = has ? sc[(2 * c) * stride] : 0, b1 = has ? sc[(2 * c + 1) * stride] : 0;
+          if (look) {
+            if ((b0 & 0x7Fu) == 0x7Fu) {
+              for (int k = 0; k < 16; ++k) note_bad(32 * c + k, 0, key);
+              b0 = 0;
+            }
+            if ((b1 & 0x7Fu) == 0x7Fu) {
+              for (int k = 0; k < 16; ++k) note_bad(32 * c + 16 + k, 0, key);
+              b1 = 0;
             }
           }
-        }
-        unsigned char* t = smem + (2 + op % PR_SLOTS) * TB;
+          // (of a key that is not there the scale is zero, and so are its values)
+          const Deq d0 = deq_of(e4m3x2_to_half2(b0 * 0x101u)), d1 = deq_of(e4m3x2_to_half2(b1 * 0x101u));
+          const u32 code[4] = {four.x, four.y, four.z, four.w};
 #pragma unroll
-        for (int g = 0; g < D / 16; ++g) {    // a scale group: two words, two 16-byte chunks of the operand
-          const u32 two = (sc[g >> 2] >> (8 * (g & 3))) & 0xFFu;
-          const Deq d = deq_of(e4m3x2_to_half2(two | (two << 8)));
-#pragma unroll
-          for (int w = 0; w < 2; ++w) {
+          for (int w = 0; w < 4; ++w) {
             u32 o[4];
-            deq4(cur[2 * g + w], cur[2 * g + w] >> 8, d, mg, o);
-            *reinterpret_cast<uint4*>(t + operand_at(pt, 2 * g + w)) = cur_has ? make_uint4(o[0], o[1], o[2], o[3]) : make_uint4(0, 0, 0, 0);
+            deq4(code[w], code[w] >> 8, w < 2 ? d0 : d1, mg, o);
+            const u32 ch = 4 * c + w;
+            *reinterpret_cast<uint4*>(t + (ch >> 3) * (PR_KEYS * 128) + (to ^ ((ch & 7) * 16))) = make_uint4(o[0], o[1], o[2], o[3]);
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         bar_arrive(&b_full[op % PR_SLOTS]);
+        bar_arrive(&b_raw_free[op % PR_RAW]);
       }
     }
     if (bounds && a.status) atomicOr(a.status, PTSTORE_S_BOUNDS);
   } else {
     // ======== softmax of tile w
-    regs_more<200>();
+    regs_more<PACKED ? 184 : 200>();
     const int w = warp >> 2, t = tid & 127, row = w * 128 + t;
     // its half of Q.  Through a tensor map where the group divides a tile (rows behind the request's last bring someone's values or
     // zeros along and are not stored); else chunk t % CPR of rows t / CPR, ..., all on their way before the first is used, with the
