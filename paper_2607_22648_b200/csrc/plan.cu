@@ -9,6 +9,8 @@
 #include <cuda_runtime.h>
 #include <limits.h>
 
+#include <type_traits>
+
 #include "../../include/ptstore.h"
 
 namespace {
@@ -17,8 +19,9 @@ typedef long long i64;
 typedef unsigned long long u64;
 
 constexpr int THREADS = 1024;
-constexpr int ITEMS = 16;                    // requests of one thread
+constexpr int ITEMS = 16;                    // requests of one thread in a batch of more than THREADS (one otherwise)
 constexpr int CHUNK = THREADS * ITEMS;       // requests scanned per step
+constexpr int RUN = 8;                       // consecutive entries a thread moves: one search, their loads in flight together
 constexpr int CLUSTER = 8;                   // CTAs of an assignment (the portable cluster size)
 
 __device__ __forceinline__ void cluster_sync() {     // orders global memory between the CTAs of the cluster too
@@ -36,47 +39,46 @@ __device__ __forceinline__ uint32_t plus(uint32_t a, uint32_t b) {        // sat
 }
 
 // Exclusive prefix sums over a chunk: v[i] belongs to request i * THREADS + threadIdx.x of it (so that loads are coalesced and the
-// warps' scans of the rows are independent), rows of them are in use.  total in every thread.  Called by all threads.
-template <typename T>
-__device__ __forceinline__ void scan_chunk(T (&v)[ITEMS], int rows, T* s_tot /*[ITEMS * 32 + 1]*/, T& total) {
+// warps' scans of the rows are independent).  total in every thread.  Called by all threads.  Inside a warp sums are of type W (the
+// caller knows that 32 values fit it), between warps of type T; widen() turns one into the other.
+template <int ROWS, typename W, typename T, typename F>
+__device__ __forceinline__ void scan_chunk(const W (&v)[ROWS], T (&first)[ROWS], T* s_tot /*[ROWS * 32 + 1]*/, T& total, F widen) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  W x[ROWS];
   __syncthreads();                           // the previous scan's readers are done with s_tot
 #pragma unroll
-  for (int i = 0; i < ITEMS; ++i)
-    if (i < rows) {
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const T y = __shfl_up_sync(0xFFFFFFFFu, v[i], o);
-        if (lane >= o) v[i] = plus(v[i], y);
-      }
-      if (lane == 31) s_tot[i * 32 + warp] = v[i];
-      v[i] = __shfl_up_sync(0xFFFFFFFFu, v[i], 1);
-      if (lane == 0) v[i] = 0;
-    }
-  __syncthreads();
-  if (warp == 0) {                           // lane l: the totals l * rows .. of the rows * 32 in order
-    T sum = 0;
-    for (int k = 0; k < rows; ++k) sum = plus(sum, s_tot[lane * rows + k]);
-    T x = sum;
+  for (int i = 0; i < ROWS; ++i) {
+    x[i] = v[i];
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const T y = __shfl_up_sync(0xFFFFFFFFu, x, o);
-      if (lane >= o) x = plus(x, y);
+      const W y = __shfl_up_sync(0xFFFFFFFFu, x[i], o);
+      if (lane >= o) x[i] = plus(x[i], y);
     }
-    if (lane == 31) s_tot[ITEMS * 32] = x;
-    T run = __shfl_up_sync(0xFFFFFFFFu, x, 1);
+    if (lane == 31) s_tot[i * 32 + warp] = widen(x[i]);
+    x[i] = __shfl_up_sync(0xFFFFFFFFu, x[i], 1);
+    if (lane == 0) x[i] = 0;
+  }
+  __syncthreads();
+  if (warp == 0) {                           // lane l: the totals l * ROWS .. of the ROWS * 32 in order
+    T t[ROWS], sum = 0;
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) { t[k] = s_tot[lane * ROWS + k]; sum = plus(sum, t[k]); }
+    T run = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const T y = __shfl_up_sync(0xFFFFFFFFu, run, o);
+      if (lane >= o) run = plus(run, y);
+    }
+    if (lane == 31) s_tot[ROWS * 32] = run;
+    run = __shfl_up_sync(0xFFFFFFFFu, run, 1);
     if (lane == 0) run = 0;
-    for (int k = 0; k < rows; ++k) {
-      const T t = s_tot[lane * rows + k];
-      s_tot[lane * rows + k] = run;
-      run = plus(run, t);
-    }
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) { s_tot[lane * ROWS + k] = run; run = plus(run, t[k]); }
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < ITEMS; ++i)
-    if (i < rows) v[i] = plus(v[i], s_tot[i * 32 + warp]);
-  total = s_tot[ITEMS * 32];
+  for (int i = 0; i < ROWS; ++i) first[i] = plus(widen(x[i]), s_tot[i * 32 + warp]);
+  total = s_tot[ROWS * 32];
 }
 
 // last index i in [0, n) with first[i] <= k; first is non-decreasing, first[0] <= k
@@ -92,7 +94,7 @@ __device__ __forceinline__ int owner_of(const uint32_t* first, int n, uint32_t k
 struct Assign {
   const int* lengths;
   const int* held;
-  int R, block_tokens, max_blocks, capacity;
+  int R, block_tokens, shift, max_blocks, capacity;           // shift: block_tokens is 2^shift, or -1
   int* tables;
   int* free_ids;
   const int* free_count;
@@ -102,69 +104,90 @@ struct Assign {
 };
 
 // blocks a request holds and needs; a length its row cannot hold leaves the row as it is
-__device__ __forceinline__ void want(const Assign& a, int r, int& held, int& need, uint32_t& bad) {
-  const int h = a.held ? a.held[r] : 0, len = a.lengths[r];
+__device__ __forceinline__ void want(const Assign& a, int h, int len, int& held, int& need, uint32_t& bad) {
   held = h < 0 ? 0 : h > a.max_blocks ? a.max_blocks : h;
   if (held != h || len < 0) bad = PTSTORE_S_BOUNDS;
-  const uint32_t n = len <= 0 ? 0 : (uint32_t)(len - 1) / (uint32_t)a.block_tokens + 1;
+  const uint32_t n = len <= 0 ? 0 : a.shift >= 0 ? ((uint32_t)(len - 1) >> a.shift) + 1 : (uint32_t)(len - 1) / (uint32_t)a.block_tokens + 1;
   if (n > (uint32_t)a.max_blocks) { need = held; bad = PTSTORE_S_BOUNDS; } else need = (int)n;
 }
 
-__global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS) assign_blocks_kernel(Assign a) {
+// NARROW: 32 requests' blocks fit 16 bits, so a warp scans growth and give-back in one 32-bit value
+template <int ROWS, bool NARROW>
+__global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS) assign_blocks_kernel(const Assign a) {
   extern __shared__ uint32_t s_dyn[];
-  __shared__ u64 s_tot[ITEMS * 32 + 1];
+  __shared__ u64 s_tot[ROWS * 32 + 1];
   __shared__ u64 s_taken;
-  const int cap_items = a.R < CHUNK ? a.R : CHUNK;
+  const int cap_items = a.R < ROWS * THREADS ? a.R : ROWS * THREADS;
   uint32_t* s_grow = s_dyn;                  // exclusive prefix sums inside the chunk
   uint32_t* s_back = s_dyn + cap_items;
   uint32_t* s_held = s_dyn + 2 * cap_items;
-  const int rows = (cap_items + THREADS - 1) / THREADS;
   const int gtid = blockIdx.x * THREADS + threadIdx.x, gthreads = CLUSTER * THREADS;
   uint32_t bad = 0;
-  const int c0 = *a.free_count;
-  const int count = c0 < 0 ? 0 : c0 > a.capacity ? a.capacity : c0;
-  if (count != c0) bad = PTSTORE_S_BOUNDS;
   if (threadIdx.x == 0) s_taken = 0;
 
   u64 moves = 0;                             // growth of the chunk, and in the upper half what it gives back
   auto scan = [&](int base, int n) {
-    u64 v[ITEMS];
+    using W = typename std::conditional<NARROW, uint32_t, u64>::type;
+    constexpr int HALF = NARROW ? 16 : 32;
+    __syncthreads();                         // nobody moves the last chunk's entries any more: s_held is about to change
+    int len[ROWS], h[ROWS];
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      v[i] = 0;
-      const int k = i * THREADS + threadIdx.x;
-      if (i < rows && k < n) {
-        int held, need;
-        want(a, base + k, held, need, bad);
-        s_held[k] = held;
-        v[i] = need > held ? (u64)(need - held) : (u64)(held - need) << 32;
-      }
+    for (int i = 0; i < ROWS; ++i) {         // all loads before the first use; a request beyond the end reads the last one
+      const int k = i * THREADS + threadIdx.x, r = base + (k < n ? k : n - 1);
+      len[i] = a.lengths[r];
+      h[i] = a.held ? a.held[r] : 0;
     }
-    scan_chunk(v, rows, s_tot, moves);
+    W v[ROWS];
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
+    for (int i = 0; i < ROWS; ++i) {
       const int k = i * THREADS + threadIdx.x;
-      if (i < rows && k < n) {
-        s_grow[k] = (uint32_t)v[i];
-        s_back[k] = (uint32_t)(v[i] >> 32);
+      int held, need;
+      want(a, h[i], len[i], held, need, bad);
+      v[i] = k >= n ? 0 : need > held ? (W)(need - held) : (W)(held - need) << HALF;
+      if (k < n) s_held[k] = held;
+    }
+    u64 first[ROWS];
+    scan_chunk<ROWS>(v, first, s_tot, moves, [](W x) { return NARROW ? (u64)(x & 0xFFFFu) | (u64)((u64)x >> 16) << 32 : (u64)x; });
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const int k = i * THREADS + threadIdx.x;
+      if (k < n) {
+        s_grow[k] = (uint32_t)first[i];
+        s_back[k] = (uint32_t)(first[i] >> 32);
       }
     }
     __syncthreads();
   };
   auto after = [&](const uint32_t* s, int k, int n, uint32_t end) { return k + 1 < n ? s[k + 1] : end; };
 
+  const int c0 = *a.free_count;
+  const int count = c0 < 0 ? 0 : c0 > a.capacity ? a.capacity : c0;
+  if (count != c0) bad = PTSTORE_S_BOUNDS;
   // surplus blocks of shrinking rows go onto the stack, in (request, block) order
   i64 pushed = 0;
-  for (int base = 0; base < a.R; base += CHUNK) {
-    const int n = a.R - base < CHUNK ? a.R - base : CHUNK;
+  for (int base = 0; base < a.R; base += ROWS * THREADS) {
+    const int n = a.R - base < ROWS * THREADS ? a.R - base : ROWS * THREADS;
     scan(base, n);
     const uint32_t back = (uint32_t)(moves >> 32);
-    for (u64 k = gtid; k < back; k += gthreads) {
-      const int i = owner_of(s_back, n, (uint32_t)k);
-      const uint32_t first = s_back[i], need = s_held[i] - (after(s_back, i, n, back) - first);
-      const i64 to = count + pushed + (i64)k;
-      if (to < a.capacity) a.free_ids[to] = a.tables[(i64)(base + i) * a.max_blocks + need + ((uint32_t)k - first)];
-      else bad |= PTSTORE_S_BOUNDS;          // more ids than the stack has room for: the surplus ones are lost
+    for (u64 k = (u64)gtid * RUN; k < back; k += (u64)gthreads * RUN) {
+      int i = owner_of(s_back, n, (uint32_t)k), id[RUN];
+#pragma unroll
+      for (int e = 0; e < RUN; ++e) {
+        id[e] = -1;
+        if (k + e < back) {
+          while (after(s_back, i, n, back) <= (uint32_t)k + e) ++i;         // ends: the last request with any reaches `back`
+          const uint32_t first = s_back[i], need = s_held[i] - (after(s_back, i, n, back) - first);
+          id[e] = a.tables[(i64)(base + i) * a.max_blocks + need + ((uint32_t)k + e - first)];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < RUN; ++e) {
+        const i64 to = count + pushed + (i64)k + e;
+        if (k + e < back) {
+          if (to < a.capacity) a.free_ids[to] = id[e];
+          else bad |= PTSTORE_S_BOUNDS;      // more ids than the stack has room for: the surplus ones are lost
+        }
+      }
     }
     pushed += back;
   }
@@ -174,9 +197,9 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS) assig
 
   // growing rows pop from the top; a request is granted its blocks iff all growth up to and including it fits
   i64 wanted = 0;
-  for (int base = 0; base < a.R; base += CHUNK) {
-    const int n = a.R - base < CHUNK ? a.R - base : CHUNK;
-    if (a.R > CHUNK) {                       // a single chunk's sums are still in shared memory
+  for (int base = 0; base < a.R; base += ROWS * THREADS) {
+    const int n = a.R - base < ROWS * THREADS ? a.R - base : ROWS * THREADS;
+    if (a.R > ROWS * THREADS) {              // a single chunk's sums are still in shared memory
       scan(base, n);
       cluster_sync();                        // every CTA has read held of this chunk before one overwrites it
     }
@@ -197,9 +220,16 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS) assig
     if ((threadIdx.x & 31) == 0 && best > 0) atomicMax(&s_taken, (u64)(wanted + best));
     __syncthreads();
     const i64 end = (i64)s_taken - wanted;   // pops granted in this chunk: the first `end` of them
-    for (i64 k = gtid; k < end; k += gthreads) {
-      const int i = owner_of(s_grow, n, (uint32_t)k);
-      a.tables[(i64)(base + i) * a.max_blocks + s_held[i] + ((uint32_t)k - s_grow[i])] = a.free_ids[top - 1 - (wanted + k)];
+    for (i64 k = (i64)gtid * RUN; k < end; k += (i64)gthreads * RUN) {
+      int i = owner_of(s_grow, n, (uint32_t)k), id[RUN];
+#pragma unroll
+      for (int e = 0; e < RUN; ++e) id[e] = k + e < end ? a.free_ids[top - 1 - (wanted + k + e)] : -1;
+#pragma unroll
+      for (int e = 0; e < RUN; ++e)
+        if (k + e < end) {
+          while (after(s_grow, i, n, grow) <= (uint32_t)k + e) ++i;
+          a.tables[(i64)(base + i) * a.max_blocks + s_held[i] + ((uint32_t)k + e - s_grow[i])] = id[e];
+        }
     }
     wanted += grow;
     __syncthreads();
@@ -211,7 +241,7 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS) assig
 struct MapSlots {
   const int* lengths;
   const int* done;
-  int done_unit, min_new, R, block_tokens, max_blocks;
+  int done_unit, min_new, R, block_tokens, shift, max_blocks;
   const int* tables;
   i64 max_tokens, per_cta;
   int* offsets;
@@ -220,11 +250,10 @@ struct MapSlots {
   uint32_t* status;
 };
 
-// tokens of the request that are in the cache already, and new ones
-__device__ __forceinline__ void done_new(const MapSlots& m, int r, int& done, int& fresh, uint32_t& bad) {
-  int len = m.lengths[r];
+// tokens of a request that are in the cache already, and new ones
+__device__ __forceinline__ void done_new(const MapSlots& m, int len, int d0, int& done, int& fresh, uint32_t& bad) {
   if (len < 0) { len = 0; bad = PTSTORE_S_BOUNDS; }
-  i64 d = m.done ? (i64)m.done[r] * m.done_unit : 0;
+  i64 d = (i64)d0 * m.done_unit;
   const i64 most = (i64)len - m.min_new;
   if (d > most) d = most;
   if (d < 0) d = 0;
@@ -232,57 +261,72 @@ __device__ __forceinline__ void done_new(const MapSlots& m, int r, int& done, in
   fresh = len - done;
 }
 
-__global__ void __launch_bounds__(THREADS) map_slots_kernel(MapSlots m) {
+template <int ROWS>
+__global__ void __launch_bounds__(THREADS) map_slots_kernel(const MapSlots m) {
   extern __shared__ uint32_t s_dyn[];
-  __shared__ uint32_t s_tot[ITEMS * 32 + 1];
-  const int cap_items = m.R < CHUNK ? m.R : CHUNK;
+  __shared__ uint32_t s_tot[ROWS * 32 + 1];
+  const int cap_items = m.R < ROWS * THREADS ? m.R : ROWS * THREADS;
   uint32_t* s_first = s_dyn;                 // exclusive prefix sums inside the chunk
   int* s_done = reinterpret_cast<int*>(s_dyn + cap_items);
-  const int rows = (cap_items + THREADS - 1) / THREADS;
   const i64 t0 = blockIdx.x * m.per_cta, t1 = t0 + m.per_cta < m.max_tokens ? t0 + m.per_cta : m.max_tokens;
   uint32_t bad = 0;
   i64 base_tok = 0;
-  for (int base = 0; base < m.R; base += CHUNK) {
-    const int n = m.R - base < CHUNK ? m.R - base : CHUNK;
-    uint32_t v[ITEMS], sum;                  // sums saturate at 2^32 - 1: no token beyond max_tokens < 2^31 is listed
+  for (int base = 0; base < m.R; base += ROWS * THREADS) {
+    const int n = m.R - base < ROWS * THREADS ? m.R - base : ROWS * THREADS;
+    int len[ROWS], d[ROWS];
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      v[i] = 0;
-      const int k = i * THREADS + threadIdx.x;
-      if (i < rows && k < n) {
-        int done, fresh;
-        done_new(m, base + k, done, fresh, bad);
-        s_done[k] = done;
-        v[i] = (uint32_t)fresh;
-      }
+    for (int i = 0; i < ROWS; ++i) {         // all loads before the first use; a request beyond the end reads the last one
+      const int k = i * THREADS + threadIdx.x, r = base + (k < n ? k : n - 1);
+      len[i] = m.lengths[r];
+      d[i] = m.done ? m.done[r] : 0;
     }
-    scan_chunk(v, rows, s_tot, sum);
+    uint32_t v[ROWS], first[ROWS], sum;      // sums saturate at 2^32 - 1: no token beyond max_tokens < 2^31 is listed
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const int k = i * THREADS + threadIdx.x;
+      int done, fresh;
+      done_new(m, len[i], d[i], done, fresh, bad);
+      v[i] = k < n ? (uint32_t)fresh : 0;
+      if (k < n) s_done[k] = done;
+    }
+    scan_chunk<ROWS>(v, first, s_tot, sum, [](uint32_t x) { return x; });
     const i64 total = sum;
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
+    for (int i = 0; i < ROWS; ++i) {
       const int k = i * THREADS + threadIdx.x;
-      if (i < rows && k < n) {
-        s_first[k] = v[i];
+      if (k < n) {
+        s_first[k] = first[i];
         if (blockIdx.x == 0) {
-          const i64 at = base_tok + v[i];
+          const i64 at = base_tok + first[i];
           m.offsets[base + k] = at > INT_MAX ? INT_MAX : (int)at;
         }
       }
     }
     __syncthreads();
     const i64 lo = t0 > base_tok ? t0 : base_tok, hi = t1 < base_tok + total ? t1 : base_tok + total;
-    for (i64 t = lo + threadIdx.x; t < hi; t += THREADS) {
-      const uint32_t k = (uint32_t)(t - base_tok);
-      const int i = owner_of(s_first, n, k);
-      const int pos = s_done[i] + (int)(k - s_first[i]);
-      const int j = pos / m.block_tokens;
-      i64 slot = -1;
-      if (j < m.max_blocks) {
-        const int b = m.tables[(i64)(base + i) * m.max_blocks + j];
-        if (b >= 0) slot = (i64)b * m.block_tokens + (pos - j * m.block_tokens);
-      } else bad = PTSTORE_S_BOUNDS;
-      m.slots[t] = slot;
-      if (m.positions) m.positions[t] = pos;
+    // four tokens of a thread at a time, THREADS apart: their table loads are in flight together and stores stay coalesced
+    constexpr int E = 4;
+    for (i64 t = lo + threadIdx.x; t < hi; t += E * THREADS) {
+      int pos[E], b[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        b[e] = -1;
+        if (t + e * THREADS < hi) {
+          const uint32_t k = (uint32_t)(t + e * THREADS - base_tok);
+          const int i = owner_of(s_first, n, k);
+          pos[e] = s_done[i] + (int)(k - s_first[i]);
+          const int j = m.shift >= 0 ? pos[e] >> m.shift : pos[e] / m.block_tokens;
+          if (j < m.max_blocks) b[e] = m.tables[(i64)(base + i) * m.max_blocks + j];
+          else bad = PTSTORE_S_BOUNDS;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (t + e * THREADS < hi) {
+          const int in = m.shift >= 0 ? pos[e] & (m.block_tokens - 1) : pos[e] % m.block_tokens;
+          m.slots[t + e * THREADS] = b[e] >= 0 ? (i64)b[e] * m.block_tokens + in : -1;
+          if (m.positions) m.positions[t + e * THREADS] = pos[e];
+        }
     }
     base_tok += total;
     __syncthreads();
@@ -297,6 +341,12 @@ __global__ void __launch_bounds__(THREADS) map_slots_kernel(MapSlots m) {
     if (m.positions) m.positions[t] = -1;
   }
   if (bad) raise_status(m.status, bad);
+}
+
+int shift_of(int block_tokens) {             // block_tokens = 2^shift, or -1
+  for (int s = 0; s < 31; ++s)
+    if (block_tokens == 1 << s) return s;
+  return -1;
 }
 
 int launch_ok() { return cudaGetLastError() == cudaSuccess ? PTSTORE_OK : PTSTORE_E_CUDA; }
@@ -321,12 +371,20 @@ extern "C" int ptstore_assign_blocks(const int32_t* lengths, const int32_t* held
   if (R > 0 && (!lengths || !block_tables || !held_out)) return PTSTORE_E_INVAL;
   if (R > 1 << 30) return PTSTORE_E_LIMIT;
   if ((i64)(R < CHUNK ? R : CHUNK) * max_blocks > (i64)UINT_MAX) return PTSTORE_E_LIMIT;      // sums inside a chunk are 32 bits wide
-  const Assign a = {lengths, held, R, block_tokens, max_blocks, free_capacity, block_tables, free_ids, free_count, held_out, free_count_out, status};
+  const Assign a = {lengths, held, R, block_tokens, shift_of(block_tokens), max_blocks, free_capacity, block_tables, free_ids, free_count, held_out, free_count_out, status};
   const size_t smem = 12 * (size_t)(R < CHUNK ? R : CHUNK);
   (void)cudaGetLastError();
-  const int rc = allow_smem(assign_blocks_kernel, smem);
-  if (rc) return rc;
-  assign_blocks_kernel<<<CLUSTER, THREADS, smem, static_cast<cudaStream_t>(stream)>>>(a);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (R <= THREADS) assign_blocks_kernel<1, false><<<CLUSTER, THREADS, smem, st>>>(a);
+  else if (max_blocks < 2048) {
+    const int rc = allow_smem(assign_blocks_kernel<ITEMS, true>, smem);
+    if (rc) return rc;
+    assign_blocks_kernel<ITEMS, true><<<CLUSTER, THREADS, smem, st>>>(a);
+  } else {
+    const int rc = allow_smem(assign_blocks_kernel<ITEMS, false>, smem);
+    if (rc) return rc;
+    assign_blocks_kernel<ITEMS, false><<<CLUSTER, THREADS, smem, st>>>(a);
+  }
   return launch_ok();
 }
 
@@ -336,7 +394,7 @@ extern "C" int ptstore_map_slots(const int32_t* lengths, const int32_t* done, in
   if (R < 0 || block_tokens < 1 || max_blocks < 1 || max_tokens < 0 || max_tokens > INT_MAX || done_unit < 1 || min_new < 0) return PTSTORE_E_INVAL;
   if (!token_offsets || (max_tokens > 0 && !slots) || (R > 0 && (!lengths || !block_tables))) return PTSTORE_E_INVAL;
   if (R > 1 << 30) return PTSTORE_E_LIMIT;
-  MapSlots m = {lengths, done, done_unit, min_new, R, block_tokens, max_blocks, block_tables, max_tokens, 0, token_offsets,
+  MapSlots m = {lengths, done, done_unit, min_new, R, block_tokens, shift_of(block_tokens), max_blocks, block_tables, max_tokens, 0, token_offsets,
                 reinterpret_cast<i64*>(slots), positions, status};
   // at most one CTA per SM (148): every CTA scans all requests, so more of them would only repeat that
   i64 per = (max_tokens + 147) / 148;
@@ -347,8 +405,12 @@ extern "C" int ptstore_map_slots(const int32_t* lengths, const int32_t* done, in
   if (grid < 1) grid = 1;
   const size_t smem = 8 * (size_t)(R < CHUNK ? R : CHUNK);
   (void)cudaGetLastError();
-  const int rc = allow_smem(map_slots_kernel, smem);
-  if (rc) return rc;
-  map_slots_kernel<<<(unsigned)grid, THREADS, smem, static_cast<cudaStream_t>(stream)>>>(m);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (R <= THREADS) map_slots_kernel<1><<<(unsigned)grid, THREADS, smem, st>>>(m);
+  else {
+    const int rc = allow_smem(map_slots_kernel<ITEMS>, smem);
+    if (rc) return rc;
+    map_slots_kernel<ITEMS><<<(unsigned)grid, THREADS, smem, st>>>(m);
+  }
   return launch_ok();
 }
