@@ -21,7 +21,6 @@ typedef unsigned long long u64;
 constexpr int THREADS = 1024;
 constexpr int ITEMS = 16;                    // requests of one thread in a batch of more than THREADS (one otherwise)
 constexpr int CHUNK = THREADS * ITEMS;       // requests scanned per step
-constexpr int RUN = 8;                       // consecutive entries a thread moves: one search, their loads in flight together
 constexpr int CLUSTER = 8;                   // CTAs of an assignment (the portable cluster size)
 
 __device__ __forceinline__ void cluster_sync() {     // orders global memory between the CTAs of the cluster too
@@ -38,47 +37,41 @@ __device__ __forceinline__ uint32_t plus(uint32_t a, uint32_t b) {        // sat
   return s < a ? UINT_MAX : s;
 }
 
-// Exclusive prefix sums over a chunk: v[i] belongs to request i * THREADS + threadIdx.x of it (so that loads are coalesced and the
-// warps' scans of the rows are independent).  total in every thread.  Called by all threads.  Inside a warp sums are of type W (the
-// caller knows that 32 values fit it), between warps of type T; widen() turns one into the other.
-template <int ROWS, typename W, typename T, typename F>
-__device__ __forceinline__ void scan_chunk(const W (&v)[ROWS], T (&first)[ROWS], T* s_tot /*[ROWS * 32 + 1]*/, T& total, F widen) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  W x[ROWS];
-  __syncthreads();                           // the previous scan's readers are done with s_tot
+// Exclusive prefix sum inside a warp; the warp's sum in every lane.
+template <typename W>
+__device__ __forceinline__ W warp_scan(W v, W& sum) {
+  const int lane = threadIdx.x & 31;
+  W x = v;
 #pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    x[i] = v[i];
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const W y = __shfl_up_sync(0xFFFFFFFFu, x[i], o);
-      if (lane >= o) x[i] = plus(x[i], y);
+  for (int o = 1; o < 32; o <<= 1) {
+    const W y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+    if (lane >= o) x = plus(x, y);
+  }
+  sum = __shfl_sync(0xFFFFFFFFu, x, 31);
+  x = __shfl_up_sync(0xFFFFFFFFu, x, 1);
+  return lane == 0 ? (W)0 : x;
+}
+
+// Turns the sums of a chunk's ROWS x 32 warps (row by row) into exclusive prefix sums.  Called by all threads.
+template <int ROWS, typename T>
+__device__ __forceinline__ void scan_totals(T* s_tot /*[ROWS * 32]*/, T& total, T* s_all) {
+  const int lane = threadIdx.x & 31;
+  __syncthreads();
+  if (threadIdx.x < 32) {                    // lane l: the totals l * ROWS ..
+    T sum = 0;
+#pragma unroll 4
+    for (int k = 0; k < ROWS; ++k) sum = plus(sum, s_tot[lane * ROWS + k]);
+    T all, run = warp_scan(sum, all);
+    if (lane == 0) *s_all = all;
+#pragma unroll 4
+    for (int k = 0; k < ROWS; ++k) {
+      const T t = s_tot[lane * ROWS + k];
+      s_tot[lane * ROWS + k] = run;
+      run = plus(run, t);
     }
-    if (lane == 31) s_tot[i * 32 + warp] = widen(x[i]);
-    x[i] = __shfl_up_sync(0xFFFFFFFFu, x[i], 1);
-    if (lane == 0) x[i] = 0;
   }
   __syncthreads();
-  if (warp == 0) {                           // lane l: the totals l * ROWS .. of the ROWS * 32 in order
-    T t[ROWS], sum = 0;
-#pragma unroll
-    for (int k = 0; k < ROWS; ++k) { t[k] = s_tot[lane * ROWS + k]; sum = plus(sum, t[k]); }
-    T run = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const T y = __shfl_up_sync(0xFFFFFFFFu, run, o);
-      if (lane >= o) run = plus(run, y);
-    }
-    if (lane == 31) s_tot[ROWS * 32] = run;
-    run = __shfl_up_sync(0xFFFFFFFFu, run, 1);
-    if (lane == 0) run = 0;
-#pragma unroll
-    for (int k = 0; k < ROWS; ++k) { s_tot[lane * ROWS + k] = run; run = plus(run, t[k]); }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i) first[i] = plus(widen(x[i]), s_tot[i * 32 + warp]);
-  total = s_tot[ROWS * 32];
+  total = *s_all;
 }
 
 // last index i in [0, n) with first[i] <= k; first is non-decreasing, first[0] <= k
@@ -115,8 +108,8 @@ __device__ __forceinline__ void want(const Assign& a, int h, int len, int& held,
 template <int ROWS, bool NARROW>
 __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS) assign_blocks_kernel(const Assign a) {
   extern __shared__ uint32_t s_dyn[];
-  __shared__ u64 s_tot[ROWS * 32 + 1];
-  __shared__ u64 s_taken;
+  __shared__ u64 s_tot[ROWS * 32], s_all, s_taken;
+  constexpr int RUN = ROWS == 1 ? 1 : 8;     // consecutive entries a thread moves: one search, their loads in flight together
   const int cap_items = a.R < ROWS * THREADS ? a.R : ROWS * THREADS;
   uint32_t* s_grow = s_dyn;                  // exclusive prefix sums inside the chunk
   uint32_t* s_back = s_dyn + cap_items;
@@ -128,33 +121,41 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS) assig
   u64 moves = 0;                             // growth of the chunk, and in the upper half what it gives back
   auto scan = [&](int base, int n) {
     using W = typename std::conditional<NARROW, uint32_t, u64>::type;
-    constexpr int HALF = NARROW ? 16 : 32;
-    __syncthreads();                         // nobody moves the last chunk's entries any more: s_held is about to change
-    int len[ROWS], h[ROWS];
+    constexpr int HALF = NARROW ? 16 : 32, BATCH = ROWS < 4 ? ROWS : 4;
+    __syncthreads();                         // nobody moves the last chunk's entries any more
+    // four rows' loads at a time; loops stay rolled, since the code of a launch this short comes from afar
+#pragma unroll 1
+    for (int row = 0; row < ROWS; row += BATCH) {
+      int len[BATCH], h[BATCH];
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {         // all loads before the first use; a request beyond the end reads the last one
-      const int k = i * THREADS + threadIdx.x, r = base + (k < n ? k : n - 1);
-      len[i] = a.lengths[r];
-      h[i] = a.held ? a.held[r] : 0;
-    }
-    W v[ROWS];
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-      const int k = i * THREADS + threadIdx.x;
-      int held, need;
-      want(a, h[i], len[i], held, need, bad);
-      v[i] = k >= n ? 0 : need > held ? (W)(need - held) : (W)(held - need) << HALF;
-      if (k < n) s_held[k] = held;
-    }
-    u64 first[ROWS];
-    scan_chunk<ROWS>(v, first, s_tot, moves, [](W x) { return NARROW ? (u64)(x & 0xFFFFu) | (u64)((u64)x >> 16) << 32 : (u64)x; });
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-      const int k = i * THREADS + threadIdx.x;
-      if (k < n) {
-        s_grow[k] = (uint32_t)first[i];
-        s_back[k] = (uint32_t)(first[i] >> 32);
+      for (int i = 0; i < BATCH; ++i) {      // a request beyond the end reads the last one
+        const int k = (row + i) * THREADS + threadIdx.x, r = base + (k < n ? k : n - 1);
+        len[i] = a.lengths[r];
+        h[i] = a.held ? a.held[r] : 0;
       }
+#pragma unroll
+      for (int i = 0; i < BATCH; ++i) {
+        const int k = (row + i) * THREADS + threadIdx.x;
+        int held, need;
+        want(a, h[i], len[i], held, need, bad);
+        const W v = k >= n ? 0 : need > held ? (W)(need - held) : (W)(held - need) << HALF;
+        W sum;
+        const W first = warp_scan(v, sum);
+        auto wide = [](W x) { return NARROW ? (u64)(x & 0xFFFFu) | (u64)((u64)x >> 16) << 32 : (u64)x; };
+        if ((threadIdx.x & 31) == 0) s_tot[(row + i) * 32 + (threadIdx.x >> 5)] = wide(sum);
+        if (k < n) {
+          s_held[k] = held;
+          s_grow[k] = (uint32_t)wide(first);
+          s_back[k] = (uint32_t)(wide(first) >> 32);
+        }
+      }
+    }
+    scan_totals<ROWS>(s_tot, moves, &s_all);
+#pragma unroll 4
+    for (int k = threadIdx.x; k < n; k += THREADS) {
+      const u64 before = s_tot[k >> 5];
+      s_grow[k] += (uint32_t)before;
+      s_back[k] += (uint32_t)(before >> 32);
     }
     __syncthreads();
   };
@@ -175,7 +176,7 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS) assig
       for (int e = 0; e < RUN; ++e) {
         id[e] = -1;
         if (k + e < back) {
-          while (after(s_back, i, n, back) <= (uint32_t)k + e) ++i;         // ends: the last request with any reaches `back`
+          if (after(s_back, i, n, back) <= (uint32_t)k + e) i = owner_of(s_back, n, (uint32_t)k + e);        // few requests shrink: the next may be far
           const uint32_t first = s_back[i], need = s_held[i] - (after(s_back, i, n, back) - first);
           id[e] = a.tables[(i64)(base + i) * a.max_blocks + need + ((uint32_t)k + e - first)];
         }
@@ -227,7 +228,7 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS) assig
 #pragma unroll
       for (int e = 0; e < RUN; ++e)
         if (k + e < end) {
-          while (after(s_grow, i, n, grow) <= (uint32_t)k + e) ++i;
+          while (after(s_grow, i, n, grow) <= (uint32_t)k + e) ++i;         // most requests grow; ends: the last that does reaches `grow`
           a.tables[(i64)(base + i) * a.max_blocks + s_held[i] + ((uint32_t)k + e - s_grow[i])] = id[e];
         }
     }
@@ -264,7 +265,7 @@ __device__ __forceinline__ void done_new(const MapSlots& m, int len, int d0, int
 template <int ROWS>
 __global__ void __launch_bounds__(THREADS) map_slots_kernel(const MapSlots m) {
   extern __shared__ uint32_t s_dyn[];
-  __shared__ uint32_t s_tot[ROWS * 32 + 1];
+  __shared__ uint32_t s_tot[ROWS * 32], s_all;
   const int cap_items = m.R < ROWS * THREADS ? m.R : ROWS * THREADS;
   uint32_t* s_first = s_dyn;                 // exclusive prefix sums inside the chunk
   int* s_done = reinterpret_cast<int*>(s_dyn + cap_items);
@@ -273,33 +274,40 @@ __global__ void __launch_bounds__(THREADS) map_slots_kernel(const MapSlots m) {
   i64 base_tok = 0;
   for (int base = 0; base < m.R; base += ROWS * THREADS) {
     const int n = m.R - base < ROWS * THREADS ? m.R - base : ROWS * THREADS;
-    int len[ROWS], d[ROWS];
+    constexpr int BATCH = ROWS < 4 ? ROWS : 4;
+    uint32_t sum;                            // sums saturate at 2^32 - 1: no token beyond max_tokens < 2^31 is listed
+#pragma unroll 1
+    for (int row = 0; row < ROWS; row += BATCH) {
+      int len[BATCH], d[BATCH];
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {         // all loads before the first use; a request beyond the end reads the last one
-      const int k = i * THREADS + threadIdx.x, r = base + (k < n ? k : n - 1);
-      len[i] = m.lengths[r];
-      d[i] = m.done ? m.done[r] : 0;
-    }
-    uint32_t v[ROWS], first[ROWS], sum;      // sums saturate at 2^32 - 1: no token beyond max_tokens < 2^31 is listed
+      for (int i = 0; i < BATCH; ++i) {      // a request beyond the end reads the last one
+        const int k = (row + i) * THREADS + threadIdx.x, r = base + (k < n ? k : n - 1);
+        len[i] = m.lengths[r];
+        d[i] = m.done ? m.done[r] : 0;
+      }
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-      const int k = i * THREADS + threadIdx.x;
-      int done, fresh;
-      done_new(m, len[i], d[i], done, fresh, bad);
-      v[i] = k < n ? (uint32_t)fresh : 0;
-      if (k < n) s_done[k] = done;
-    }
-    scan_chunk<ROWS>(v, first, s_tot, sum, [](uint32_t x) { return x; });
-    const i64 total = sum;
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-      const int k = i * THREADS + threadIdx.x;
-      if (k < n) {
-        s_first[k] = first[i];
-        if (blockIdx.x == 0) {
-          const i64 at = base_tok + first[i];
-          m.offsets[base + k] = at > INT_MAX ? INT_MAX : (int)at;
+      for (int i = 0; i < BATCH; ++i) {
+        const int k = (row + i) * THREADS + threadIdx.x;
+        int done, fresh;
+        done_new(m, len[i], d[i], done, fresh, bad);
+        uint32_t all;
+        const uint32_t first = warp_scan(k < n ? (uint32_t)fresh : 0u, all);
+        if ((threadIdx.x & 31) == 0) s_tot[(row + i) * 32 + (threadIdx.x >> 5)] = all;
+        if (k < n) {
+          s_done[k] = done;
+          s_first[k] = first;
         }
+      }
+    }
+    scan_totals<ROWS>(s_tot, sum, &s_all);
+    const i64 total = sum;
+#pragma unroll 4
+    for (int k = threadIdx.x; k < n; k += THREADS) {
+      const uint32_t first = plus(s_first[k], s_tot[k >> 5]);
+      s_first[k] = first;
+      if (blockIdx.x == 0) {
+        const i64 at = base_tok + first;
+        m.offsets[base + k] = at > INT_MAX ? INT_MAX : (int)at;
       }
     }
     __syncthreads();
