@@ -491,7 +491,7 @@ int ptstore_map_slots(const int32_t* lengths, const int32_t* done, int32_t done_
 /*
  * Rows of K and V into the cache / out of it.  Row i of a head: head_dim contiguous 16-bit elements (dtype PTSTORE_KV_BF16 or _FP16) at
  * i * token_stride + head * head_stride elements (multiples of 8; pointers 16-byte aligned); it belongs to cache slot slots[i] =
- * block * block_tokens + token.  A slot of -1 is skipped (its row is neither written nor read); any other slot outside the cache too (S_BOUNDS).  Slots
+ * block * block_tokens + token.  A slot of -1 is skipped (a write ignores its row, a read leaves it as it was); any other slot outside the cache too (S_BOUNDS).  Slots
  * of a write other than -1 must be distinct.  A 16-bit cache takes rows of its own type only.
  * PACKED, per 16 elements: scale = e4m3 nearest to max|x| / (7 t), at most 448 (t: the tensor scale); code = x / (scale t) to the nearest
  * integer, ties to even, within -8 .. 7, plus 8.  All zero where the scale is zero.  Infinities saturate; a NaN makes its 16 elements NaN.

@@ -199,6 +199,7 @@ _ATTEND = struct.Struct("IIPqqPqqPPPiiiiif")
 assert _KV_CACHE.size == C.sizeof(KvCache) and _ATTEND.size <= C.sizeof(Attend)
 _ATTEND_SIZE = C.sizeof(Attend)
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_device = torch.cuda.current_device
 
 
 def _check(rc, what):
@@ -266,14 +267,17 @@ class KVLayout:
         if not 0 <= layer < len(cache.tensors):
             raise ValueError("layer %d of a cache of %d layers" % (layer, len(cache.tensors)))
         t = cache.tensors[layer]
-        if t.get_device() != (torch.cuda.current_device() if dev is None else dev):
+        if t.get_device() != (_device() if dev is None else dev):
             _elsewhere(t, "cache")
         size, shape, stride = t.element_size(), t.shape, t.stride()
-        inner = 1
-        for n, s in zip(shape[:1:-1], stride[:1:-1]):            # the axes of a chunk, last first
-            if s != inner and n != 1:
-                inner = 0
-            inner *= n
+        if len(shape) == 3:
+            inner = shape[2] if stride[2] == 1 or shape[2] == 1 else 0
+        else:
+            inner = 1
+            for n, s in zip(shape[:1:-1], stride[:1:-1]):        # the axes of a chunk, last first
+                if s != inner and n != 1:
+                    inner = 0
+                inner *= n
         if len(shape) < 2 or shape[0] != 2 or inner * size != self.chunk_bytes:
             raise ValueError("cache: needs [2, blocks, chunk] with contiguous chunks of %d bytes" % self.chunk_bytes)
         return _KV_CACHE.pack(t.data_ptr(), stride[0] * size, stride[1] * size, shape[1], self.block_tokens, self.heads, self.dim, self.format, 0,
@@ -283,7 +287,7 @@ class KVLayout:
 def assign_blocks(lengths, held, block_tables, free_ids, free_count, block_tokens, held_out=None, free_count_out=None, status=None):
     """ptstore_assign_blocks: grows and shrinks block-table rows to the lengths, from and to the stack free_ids[:free_count].  held (None:
     nothing held yet) and free_count are updated in place unless held_out / free_count_out are given.  Returns (held, free_count)."""
-    dev, i32, R = torch.cuda.current_device(), torch.int32, lengths.numel()
+    dev, i32, R = _device(), torch.int32, lengths.numel()
     if held_out is None:
         held_out = held if held is not None else torch.empty_like(lengths)
     if free_count_out is None:
@@ -300,42 +304,54 @@ def map_slots(lengths, done, block_tables, block_tokens, max_tokens, done_unit=1
               status=None):
     """ptstore_map_slots: the new tokens of a batch.  done (tokens, times done_unit; None: none) are in the cache already; after a lookup
     pass its matched lengths with done_unit=block_tokens, min_new=1.  Returns (token_offsets [R+1], slots int64 [max_tokens], positions)."""
-    dev, i32, R = torch.cuda.current_device(), torch.int32, lengths.numel()
+    dev, i32, R = _device(), torch.int32, lengths.numel()
     if token_offsets is None:
         token_offsets = torch.empty(R + 1, dtype=i32, device="cuda")
+        offsets_at = token_offsets.data_ptr()
+    else:
+        offsets_at = _vec(token_offsets, i32, R + 1, dev, "token_offsets")
     if slots is None:
         slots = torch.empty(max_tokens, dtype=torch.int64, device="cuda")
+        slots_at = slots.data_ptr()
+    else:
+        slots_at = _vec(slots, torch.int64, max_tokens, dev, "slots")
     if positions is None:
         positions = torch.empty(max_tokens, dtype=i32, device="cuda")
+        positions_at = positions.data_ptr()
+    else:
+        positions_at = _vec(positions, i32, max_tokens, dev, "positions")
     _check(lib.ptstore_map_slots(_vec(lengths, i32, R, dev, "lengths"), None if done is None else _vec(done, i32, R, dev, "done"), done_unit, min_new, R,
                                  _table(block_tables, R, dev, "block_tables"), block_tables.shape[1], block_tokens, max_tokens,
-                                 _vec(token_offsets, i32, R + 1, dev, "token_offsets"), _vec(slots, torch.int64, max_tokens, dev, "slots"),
-                                 _vec(positions, i32, max_tokens, dev, "positions"), None if status is None else _vec(status, i32, 1, dev, "status"),
+                                 offsets_at, slots_at, positions_at, None if status is None else _vec(status, i32, 1, dev, "status"),
                                  _raw_stream(dev)), "ptstore_map_slots")
     return token_offsets, slots, positions
 
 
 def kv_write(layout, cache, layer, k, v, slots, status=None):
     """ptstore_kv_write: rows k, v [tokens, heads, dim] into one layer of the paged cache at `slots` (int64; -1 skips a row)."""
-    dev, n, code = torch.cuda.current_device(), slots.numel(), _kv_dtype(k, "k")
-    _check(lib.ptstore_kv_write(_rows(k, layout.heads, layout.dim, n, k.dtype, dev, "k"), k.stride(0), k.stride(1),
-                                _rows(v, layout.heads, layout.dim, n, k.dtype, dev, "v"), v.stride(0), v.stride(1), n, code,
+    dev, n, code, k_stride, v_stride = _device(), slots.numel(), _kv_dtype(k, "k"), k.stride(), v.stride()
+    _check(lib.ptstore_kv_write(_rows(k, layout.heads, layout.dim, n, k.dtype, dev, "k"), k_stride[0], k_stride[1],
+                                _rows(v, layout.heads, layout.dim, n, k.dtype, dev, "v"), v_stride[0], v_stride[1], n, code,
                                 _vec(slots, torch.int64, n, dev, "slots"), layout.of(cache, layer, dev),
                                 None if status is None else _vec(status, torch.int32, 1, dev, "status"), _raw_stream(dev)), "ptstore_kv_write")
 
 
 def kv_read(layout, cache, layer, slots, dtype, k=None, v=None, status=None):
     """ptstore_kv_read: the values at `slots` as rows [tokens, heads, dim]; rows whose slot is -1 are left as they were.  Returns (k, v)."""
-    dev, n = torch.cuda.current_device(), slots.numel()
+    dev, n, heads, dim = _device(), slots.numel(), layout.heads, layout.dim
     if k is None:
-        k = torch.empty((n, layout.heads, layout.dim), dtype=dtype, device="cuda")
+        k = torch.empty((n, heads, dim), dtype=dtype, device="cuda")
+        k_at, k_stride = k.data_ptr(), (heads * dim, dim)
+    else:
+        k_at, k_stride = _rows(k, heads, dim, n, dtype, dev, "k"), k.stride()
     if v is None:
-        v = torch.empty_like(k)
+        v = torch.empty((n, heads, dim), dtype=dtype, device="cuda")
+        v_at, v_stride = v.data_ptr(), (heads * dim, dim)
+    else:
+        v_at, v_stride = _rows(v, heads, dim, n, dtype, dev, "v"), v.stride()
     code = _kv_dtype(k, "k")
-    _check(lib.ptstore_kv_read(layout.of(cache, layer, dev), _vec(slots, torch.int64, n, dev, "slots"), n, code,
-                               _rows(k, layout.heads, layout.dim, n, dtype, dev, "k"), k.stride(0), k.stride(1),
-                               _rows(v, layout.heads, layout.dim, n, dtype, dev, "v"), v.stride(0), v.stride(1),
-                               None if status is None else _vec(status, torch.int32, 1, dev, "status"), _raw_stream(dev)), "ptstore_kv_read")
+    _check(lib.ptstore_kv_read(layout.of(cache, layer, dev), _vec(slots, torch.int64, n, dev, "slots"), n, code, k_at, k_stride[0], k_stride[1],
+                               v_at, v_stride[0], v_stride[1], None if status is None else _vec(status, torch.int32, 1, dev, "status"), _raw_stream(dev)), "ptstore_kv_read")
     return k, v
 
 
@@ -351,7 +367,7 @@ def attend(layout, cache, layer, q, token_offsets, lengths, block_tables, max_ne
     """ptstore_attend: causal attention of the new tokens q [tokens, num_heads, dim] over the paged cache (which holds their own K/V
     already).  Request r owns rows token_offsets[r] .. token_offsets[r+1]-1 and lengths[r] tokens of cache; max_new (host) is at least the
     rows of any request.  workspace: from attend_workspace (a program that calls often keeps one per stream).  Returns out."""
-    dev, i32, code = torch.cuda.current_device(), torch.int32, _kv_dtype(q, "q")
+    dev, i32, code = _device(), torch.int32, _kv_dtype(q, "q")
     R, (T, heads, dim) = lengths.numel(), q.shape
     if out is None:
         out = torch.empty((T, heads, dim), dtype=q.dtype, device=q.device)

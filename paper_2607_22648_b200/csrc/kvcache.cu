@@ -1,8 +1,9 @@
 // ptstore_kv_write / ptstore_kv_read: rows of a model's K and V into the paged cache through a slot map, and back.
 //
 // Bound: HBM.  A 16-bit element costs 2 bytes on the model's side and 2 or 0.5625 in the cache, nothing is read twice.  One thread
-// takes 16 consecutive elements (a scale group): two 16-byte loads, its own maximum, eight bytes of codes and a scale, so there
-// is no exchange between threads.  What the quantiser computes is defined in exact terms (nearest code of x / (scale * tensor
+// takes 32 consecutive elements (two scale groups): four 16-byte loads, its own maxima, 16 bytes of codes and two scales, so there
+// is no exchange between threads (with 16 elements finding the row and the slot was half of 327 instructions, which is what bounds the
+// writer: 23.3 us for K and V of 16384 tokens of 8 x 128).  What the quantiser computes is defined in exact terms (nearest code of x / (scale * tensor
 // scale), ties to even); 32 bits give exactly that: x has at most 11 significant bits and the divisor 4, so a quotient that is not
 // on a rounding border is at least 2^-16 away from it, and one that is comes out exactly (the division below is corrected by its residual).
 #include "kvcache.cuh"
@@ -12,6 +13,7 @@ using namespace ptk;
 namespace {
 
 constexpr int WRITE_THREADS = 256;
+constexpr int WRITE_SPAN = 32, READ_SPAN = 16;  // elements of a thread (a reader of 32 stores in pieces that are further apart: 21.1 us, 19.1 with 16)
 
 struct Rows {
   unsigned char* k;
@@ -23,7 +25,7 @@ struct KvArgs {
   Cache cache;
   Rows rows;
   const i64* slots;
-  i64 items;                                   // T * heads * (D / 16)
+  i64 items;                                   // T * heads * (D / span)
   float k_scale, v_scale;
   u32* status;
 };
@@ -45,16 +47,17 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
-// cache position of item -> false if it is skipped
-struct Where { u32 block, token, head, group; i64 row; };
-template <int D>
-__device__ __forceinline__ bool locate(const KvArgs& a, i64 item, Where& w) {
-  constexpr u32 G = D / GROUP;
-  w.group = (u32)item % G;
+struct Where { u32 block, token, head, span; i64 row; };
+template <int D, int SPAN>
+__device__ __forceinline__ void find_row(const KvArgs& a, i64 item, Where& w) {
+  constexpr u32 G = D / SPAN;
+  w.span = (u32)item % G;
   const u64 rest = (u64)item / G;
   if (rest <= 0xFFFFFFFFull) { w.row = (u32)rest / a.cache.heads; w.head = (u32)rest % a.cache.heads; }
   else { w.row = (i64)(rest / a.cache.heads); w.head = (u32)(rest % a.cache.heads); }
-  const i64 slot = a.slots[w.row];
+}
+// cache position of a row's slot -> false if it is skipped
+__device__ __forceinline__ bool find_slot(const KvArgs& a, i64 slot, Where& w) {
   if (slot == -1) return false;
   u64 block;
   if ((u64)slot <= 0xFFFFFFFFull) { block = (u32)slot / a.cache.block_tokens; w.token = (u32)slot % a.cache.block_tokens; }
@@ -67,8 +70,9 @@ __device__ __forceinline__ bool locate(const KvArgs& a, i64 item, Where& w) {
   return true;
 }
 
+template <int SPAN>
 __device__ __forceinline__ const unsigned char* model_row(const Rows& r, bool is_v, const Where& w) {
-  return is_v ? r.v + 2 * (w.row * r.v_token + w.head * r.v_head + w.group * GROUP) : r.k + 2 * (w.row * r.k_token + w.head * r.k_head + w.group * GROUP);
+  return is_v ? r.v + 2 * (w.row * r.v_token + w.head * r.v_head + w.span * SPAN) : r.k + 2 * (w.row * r.k_token + w.head * r.k_head + w.span * SPAN);
 }
 
 template <int D, bool FP16, bool PACKED>
@@ -77,53 +81,61 @@ __global__ void __launch_bounds__(WRITE_THREADS) kv_write_kernel(KvArgs a) {
   if (item >= a.items) return;
   const bool is_v = blockIdx.y != 0;
   Where w;
-  if (!locate<D>(a, item, w)) return;
-  const uint4* src = reinterpret_cast<const uint4*>(model_row(a.rows, is_v, w));
-  const uint4 lo = src[0], hi = src[1];
+  find_row<D, WRITE_SPAN>(a, item, w);
+  const i64 slot = a.slots[w.row];
+  const uint4* src = reinterpret_cast<const uint4*>(model_row<WRITE_SPAN>(a.rows, is_v, w));
+  const uint4 in[4] = {src[0], src[1], src[2], src[3]};       // on their way together with the slot
+  if (!find_slot(a, slot, w)) return;
   if (!PACKED) {
-    uint4* dst = reinterpret_cast<uint4*>(row_ptr(a.cache, is_v, w.block, w.head, w.token, D) + w.group * GROUP * 2);
-    dst[0] = lo;
-    dst[1] = hi;
+    uint4* dst = reinterpret_cast<uint4*>(row_ptr(a.cache, is_v, w.block, w.head, w.token, D) + w.span * WRITE_SPAN * 2);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dst[i] = in[i];
     return;
   }
-  const u32 raw[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-  float x[16], amax = 0.0f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float2 f = widen<FP16>(raw[i]);
-    x[2 * i] = f.x;
-    x[2 * i + 1] = f.y;
-    amax = max_nan(amax, max_nan(fabsf(f.x), fabsf(f.y)));
-  }
   const float t = is_v ? a.v_scale : a.k_scale;
-  const u32 sb = e4m3_of(__fdiv_rn(amax, 7.0f * t));
-  const float e = e4m3_value(sb) * t;                  // exact: 4 significant bits times a power of two
-  u32 code[2] = {0x88888888u, 0x88888888u};            // code 8 is zero
-  if (e > 0.0f) {
-    const float inv = __frcp_rn(e);
-    if (amax > 8.4f * e) {                             // the scale is far too small for the largest (at most 448): codes saturate well inside
-      const float most = 9.0f * e;                     // this, and an infinity becomes finite
+  u32 code[4], sb[2];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = fminf(fmaxf(x[i], -most), most);
-    }
-    u32 sum[2] = {0, 0};
+  for (int g = 0; g < 2; ++g) {
+    const u32 raw[8] = {in[2 * g].x, in[2 * g].y, in[2 * g].z, in[2 * g].w, in[2 * g + 1].x, in[2 * g + 1].y, in[2 * g + 1].z, in[2 * g + 1].w};
+    float x[16], amax = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float y = x[i] * inv;
-      const float q = fmaf(fmaf(-y, e, x[i]), inv, y); // the quotient, exact where it is representable
-      // adding 1.5 * 2^23 + 8 rounds to an integer, ties to even, and leaves the code in the low bits: the words are sums of
-      // these bit patterns times powers of 16, less what the constant's bits add up to
-      const float n = fminf(fmaxf(q, -8.0f), 7.0f) + 12582920.0f;
-      sum[i >> 3] += __float_as_uint(n) << (4 * (i & 7));
+    for (int i = 0; i < 8; ++i) {
+      const float2 f = widen<FP16>(raw[i]);
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
+      amax = max_nan(amax, max_nan(fabsf(f.x), fabsf(f.y)));
     }
-    constexpr u32 B = 0x4B400000u, REST = B + (B << 4) + (B << 8) + (B << 12) + (B << 16) + (B << 20) + (B << 24) + (B << 28);
-    code[0] = sum[0] - REST;
-    code[1] = sum[1] - REST;
+    sb[g] = e4m3_of(__fdiv_rn(amax, 7.0f * t));
+    const float e = e4m3_value(sb[g]) * t;             // exact: 4 significant bits times a power of two
+    code[2 * g] = code[2 * g + 1] = 0x88888888u;       // code 8 is zero
+    if (e > 0.0f) {
+      const float inv = __frcp_rn(e);
+      if (amax > 8.4f * e) {                           // the scale is far too small for the largest (at most 448, or next to zero): an infinity
+        const float most = 8.0f * e;                   // becomes finite, and codes stay above -9
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = fminf(fmaxf(x[i], -most), most);
+      }
+      u32 sum[2] = {0, 0};
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float y = x[i] * inv;
+        const float q = fmaf(fmaf(-y, e, x[i]), inv, y);       // the quotient, exact where it is representable; at least -8.4
+        // adding 1.5 * 2^23 + 8 rounds to an integer, ties to even, and leaves the code in the low bits: the words are sums of
+        // these bit patterns times powers of 16, less what the constant's bits add up to
+        sum[i >> 3] += __float_as_uint(fminf(q, 7.0f) + 12582920.0f) << (4 * (i & 7));
+      }
+      constexpr u32 B = 0x4B400000u, REST = B + (B << 4) + (B << 8) + (B << 12) + (B << 16) + (B << 20) + (B << 24) + (B << 28);
+      code[2 * g] = sum[0] - REST;
+      code[2 * g + 1] = sum[1] - REST;
+    }
   }
   unsigned char* tile = tile_ptr(a.cache, is_v, w.block, w.head, w.token, D);
   const int n = w.token % TILE;
-  *reinterpret_cast<uint2*>(tile + code_place(D, n, w.group >> 1) * 16 + (w.group & 1) * 8) = make_uint2(code[0], code[1]);
-  tile[scale_at(D, is_v, n, w.group)] = (unsigned char)sb;
+  *reinterpret_cast<uint4*>(tile + code_place(D, n, w.span) * 16) = make_uint4(code[0], code[1], code[2], code[3]);
+  if (is_v) {
+    tile[scale_at(D, true, n, 2 * w.span)] = (unsigned char)sb[0];
+    tile[scale_at(D, true, n, 2 * w.span + 1)] = (unsigned char)sb[1];
+  } else *reinterpret_cast<unsigned short*>(tile + scale_at(D, false, n, 2 * w.span)) = (unsigned short)(sb[0] | (sb[1] << 8));
 }
 
 template <int D, bool FP16, bool PACKED>
@@ -132,10 +144,11 @@ __global__ void __launch_bounds__(WRITE_THREADS) kv_read_kernel(KvArgs a) {
   if (item >= a.items) return;
   const bool is_v = blockIdx.y != 0;
   Where w;
-  if (!locate<D>(a, item, w)) return;
-  uint4* dst = reinterpret_cast<uint4*>(const_cast<unsigned char*>(model_row(a.rows, is_v, w)));
+  find_row<D, READ_SPAN>(a, item, w);
+  if (!find_slot(a, a.slots[w.row], w)) return;
+  uint4* dst = reinterpret_cast<uint4*>(const_cast<unsigned char*>(model_row<READ_SPAN>(a.rows, is_v, w)));
   if (!PACKED) {
-    const uint4* src = reinterpret_cast<const uint4*>(row_ptr(a.cache, is_v, w.block, w.head, w.token, D) + w.group * GROUP * 2);
+    const uint4* src = reinterpret_cast<const uint4*>(row_ptr(a.cache, is_v, w.block, w.head, w.token, D) + w.span * READ_SPAN * 2);
     const uint4 lo = src[0], hi = src[1];
     dst[0] = lo;
     dst[1] = hi;
@@ -143,24 +156,27 @@ __global__ void __launch_bounds__(WRITE_THREADS) kv_read_kernel(KvArgs a) {
   }
   const unsigned char* tile = tile_ptr(a.cache, is_v, w.block, w.head, w.token, D);
   const int n = w.token % TILE;
-  const uint2 code = *reinterpret_cast<const uint2*>(tile + code_place(D, n, w.group >> 1) * 16 + (w.group & 1) * 8);
-  const float e = e4m3_value(tile[scale_at(D, is_v, n, w.group)]) * (is_v ? a.v_scale : a.k_scale);
+  const uint2 two = *reinterpret_cast<const uint2*>(tile + code_place(D, n, w.span >> 1) * 16 + (w.span & 1) * 8);
+  const u32 code[2] = {two.x, two.y};
+  const float e = e4m3_value(tile[scale_at(D, is_v, n, w.span)]) * (is_v ? a.v_scale : a.k_scale);
   // code n at bits p .. p+3 of 2^23 reads as 2^23 + n 2^p: less 2^23 + 8 2^p it is (n - 8) 2^p, exactly (p <= 16)
-  u32 out[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const u32 c = (i < 4 ? code.x : code.y) >> (16 * ((i >> 1) & 1));
-    const int p = 8 * (i & 1);
-    float v[2];
+  for (int o = 0; o < 2; ++o) {                        // eight elements: a word of codes
+    u32 out[4];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const float f = __uint_as_float((c & (15u << (p + 4 * k))) | 0x4B000000u) - (8388608.0f + 8.0f * (float)(1 << (p + 4 * k)));
-      v[k] = f * (e * (1.0f / (float)(1 << (p + 4 * k))));
+    for (int i = 0; i < 4; ++i) {
+      const u32 c = code[o] >> (16 * (i >> 1));
+      const int p = 8 * (i & 1);
+      float v[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const float f = __uint_as_float((c & (15u << (p + 4 * k))) | 0x4B000000u) - (8388608.0f + 8.0f * (float)(1 << (p + 4 * k)));
+        v[k] = f * (e * (1.0f / (float)(1 << (p + 4 * k))));
+      }
+      out[i] = narrow<FP16>(v[0], v[1]);
     }
-    out[i] = narrow<FP16>(v[0], v[1]);
+    dst[o] = make_uint4(out[0], out[1], out[2], out[3]);
   }
-  dst[0] = make_uint4(out[0], out[1], out[2], out[3]);
-  dst[1] = make_uint4(out[4], out[5], out[6], out[7]);
 }
 
 // shared checks and launch; WRITE picks the kernel
@@ -176,7 +192,7 @@ int run(const void* k, const void* v, i64 k_token, i64 k_head, i64 v_token, i64 
   const int D = (int)cache->head_dim;
   KvArgs a = {cache_of(cache), {(unsigned char*)k, (unsigned char*)v, k_token, k_head, v_token, v_head}, reinterpret_cast<const i64*>(slots), 0,
               cache->k_scale, cache->v_scale, status};
-  const u64 per_token = (u64)a.cache.heads * (D / GROUP);
+  const u64 per_token = (u64)a.cache.heads * (D / (WRITE ? WRITE_SPAN : READ_SPAN));
   if ((u64)tokens > (u64)0x7FFFFFFF * WRITE_THREADS / per_token) return PTSTORE_E_LIMIT;       // grid of one launch
   a.items = (i64)((u64)tokens * per_token);
   const dim3 grid((unsigned)((a.items + WRITE_THREADS - 1) / WRITE_THREADS), 2);
