@@ -109,17 +109,20 @@ int launch_prompt(Attend a, const Gpu& gpu, cudaStream_t s) {
   if (rc) return rc;
   const i64 tiles = ((i64)a.tokens * a.group / PR_ROWS + a.R) * a.cache.heads;            // at most this many, wherever the requests' rows end
   if (tiles > 0x7FFFFFFF) return PTSTORE_E_LIMIT;
-  a.split = tiles <= gpu.sms / 2 ? gpu.sms : 0;
+  a.split = tiles <= 4 * gpu.sms ? gpu.sms : 0;                        // few row tiles: the last of them may be cut
   CUtensorMap map = {};
   CUtensorMap q_map = {};
   if (FMT != PTSTORE_KV_PACKED) {
     a.box_tokens = make_tensor_map(a, FMT == PTSTORE_KV_FP16, D, &map);
     a.q_box = make_q_map(a, FMT == PTSTORE_KV_FP16, D, &q_map);
   }
-  kernel<<<a.split ? a.split : (unsigned)tiles, PR_THREADS, SMEM, s>>>(a, map, q_map);
+  kernel<<<(unsigned)(tiles + a.split), PR_THREADS, SMEM, s>>>(a, map, q_map);
   if (cudaGetLastError() != cudaSuccess) return PTSTORE_E_CUDA;
   if (a.split) {
-    attend_join_kernel<QFP16, D><<<(unsigned)(((i64)a.tokens * a.heads + 7) / 8), 256, 0, s>>>(a);
+    // at most half as many tiles are cut as there are SMs
+    const unsigned most = (unsigned)(tiles < gpu.sms / 2 ? tiles : gpu.sms / 2);
+    if (most <= 32) attend_join_kernel<QFP16, D, 1><<<dim3(most, PR_ROWS / 8), 256, 0, s>>>(a);
+    else attend_join_kernel<QFP16, D, 4><<<dim3(most, PR_ROWS / 32), 256, 0, s>>>(a);
     if (cudaGetLastError() != cudaSuccess) return PTSTORE_E_CUDA;
   }
   return PTSTORE_OK;

@@ -14,8 +14,9 @@
 // four 128-token tiles, 12 issues the tensor instructions (one thread).  13-15 only complete the warpgroup that gives its
 // registers to the softmax warps; for a 4-bit cache 13 loads its tiles and 8-11 unpack them.
 //
-// When a batch has fewer row tiles than half the SMs (one prompt whose prefix was found), the steps of every tile are cut into as many
-// chunks as there are SMs for it; a chunk leaves its O, m and l in the workspace and attend_join_kernel, one warp per row, joins them.
+// A CTA has an SM to itself, so what a batch leaves over from whole rounds of SMs (one prompt whose prefix was found: everything) would leave
+// most of them idle: the steps of those last row tiles are cut into as many chunks as there are SMs for them.  A chunk leaves
+// its O, m and l in the workspace, and attend_join_kernel, one warp per row, joins them.
 //
 // Tensor memory (512 columns): S/P of tile 0, S/P of tile 1, O 0, O 1.  Shared memory operands are in the 128-byte swizzled form: 64
 // elements of a row are 128 bytes, 16-byte chunk c of row r at c ^ (r & 7), 64-element halves one after the other.
@@ -142,13 +143,56 @@ __device__ __forceinline__ void regs_fewer() { asm volatile("setmaxnreg.dec.sync
 // byte of 16-byte chunk c of row r in an operand tile of 128 rows
 __device__ __forceinline__ u32 operand_at(int r, int c) { return (u32)((c >> 3) * (PR_KEYS * 128) + r * 128 + (((c & 7) ^ (r & 7)) * 16)); }
 
-// chunks per row tile (of one kv head), given their number and how many CTAs there are
-__device__ __forceinline__ int prompt_parts(i64 tiles, u32 ctas) { return tiles > 0 && tiles < ctas ? (int)(ctas / (u32)tiles) : 1; }
+// Row tiles (of all kv heads, in CTA order) from `first` on are cut into `parts` chunks: what is left over from whole rounds of `sms` CTAs.
+// After three rounds or more it is not worth the join.
+struct Cut { i64 first; int parts; };
+__device__ __forceinline__ Cut cut_of(i64 tiles, u32 sms) {
+  const i64 rounds = tiles / sms;
+  const u32 rest = (u32)(tiles - rounds * sms);
+  if (rest == 0 || rounds > 3 || sms / rest < 2) return {tiles, 1};
+  return {tiles - rest, (int)(sms / rest)};
+}
 template <int D>
 __host__ __device__ constexpr int prompt_part_floats() { return PR_ROWS * (D + 2); }        // o, m, l of a tile's rows
 __device__ __forceinline__ i64 prompt_tiles(const Attend& a, int r) {
   const Req q = request(a, r);
   return ((i64)q.fresh * a.group + PR_ROWS - 1) / PR_ROWS;
+}
+
+// Row tiles of all requests (of one kv head), counted by the whole CTA, consecutive requests per thread; mine, before: this thread's
+// requests' and those of the requests before them.
+template <int THREADS>
+__device__ __forceinline__ i64 count_tiles(const Attend& a, i64* s_scan /*[THREADS / 32]*/, i64& mine, i64& before) {
+  const int tid = threadIdx.x, per = (a.R + THREADS - 1) / THREADS;
+  const int rb = min(tid * per, a.R), re = min(rb + per, a.R);
+  mine = 0;
+  for (int r = rb; r < re; ++r) mine += prompt_tiles(a, r);
+  i64 x = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const i64 y = __shfl_up_sync(FULL, x, o);
+    if ((tid & 31) >= o) x += y;
+  }
+  if ((tid & 31) == 31) s_scan[tid >> 5] = x;
+  __syncthreads();
+  before = x - mine;
+  i64 all = 0;
+  for (int w = 0; w < THREADS / 32; ++w) {
+    if (w < (tid >> 5)) before += s_scan[w];
+    all += s_scan[w];
+  }
+  return all;
+}
+// The thread whose requests tile `index` belongs to writes its request and its number there; a request's tiles come last to first.
+template <int THREADS>
+__device__ __forceinline__ void find_tile(const Attend& a, i64 index, i64 mine, i64 before, int* s_r, int* s_tile) {
+  if (index < before || index >= before + mine) return;
+  const int per = (a.R + THREADS - 1) / THREADS;
+  int r = min((int)threadIdx.x * per, a.R);
+  i64 left = index - before, n = prompt_tiles(a, r);
+  for (; left >= n; n = prompt_tiles(a, ++r)) left -= n;
+  *s_r = r;
+  *s_tile = (int)(n - 1 - left);
 }
 
 template <int FMT, bool QFP16, int D>
@@ -170,43 +214,25 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
 
   // ---- which 256 rows: heads vary fastest; a request's tiles come last to first, the ones with most keys first
   int h, part = 0, parts = 1;                // this CTA's chunk of the tile's steps
-  u32 cta = blockIdx.x;
+  u32 cta = blockIdx.x, slot = 0;            // row tile; where a chunk leaves its sums
   {
-    const int per_thread = (a.R + PR_THREADS - 1) / PR_THREADS;
-    const int rb = tid * per_thread < a.R ? tid * per_thread : a.R, re = rb + per_thread < a.R ? rb + per_thread : a.R;
-    i64 mine = 0;
-    for (int r = rb; r < re; ++r) mine += prompt_tiles(a, r);
-    i64 x = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const i64 y = __shfl_up_sync(FULL, x, o);
-      if (lane >= o) x += y;
-    }
-    if (lane == 31) s_scan[warp] = x;
-    if (tid == 0) { s_r = -1; s_gave_up = 0; s_any_bad = 0; }
-    __syncthreads();
-    i64 before = x - mine;
-    for (int w = 0; w < warp; ++w) before += s_scan[w];
+    if (tid == 0) { s_gave_up = 0; s_any_bad = 0; }
+    i64 mine, before;
+    const i64 all = count_tiles<PR_THREADS>(a, s_scan, mine, before);
     if (a.split) {
-      i64 all = 0;
-      for (int w = 0; w < PR_THREADS / 32; ++w) all += s_scan[w];
-      parts = prompt_parts(all * a.cache.heads, a.split);
-      part = cta % parts;
-      cta /= parts;
+      const Cut cut = cut_of(all * a.cache.heads, a.split);
+      if (cta >= cut.first && cut.parts > 1) {
+        slot = cta - (u32)cut.first;
+        parts = cut.parts;
+        part = slot % parts;
+        cta = (u32)cut.first + slot / parts;
+      }
     }
     h = cta % a.cache.heads;
     const i64 index = cta / a.cache.heads;
-    if (index >= before && index < before + mine) {
-      i64 left = index - before;
-      int r = rb;
-      for (; r < re - 1; ++r) {
-        const i64 n = prompt_tiles(a, r);
-        if (left < n) break;
-        left -= n;
-      }
-      s_r = r;
-      s_tile = (int)(prompt_tiles(a, r) - 1 - left);
-    }
+    if (tid == 0) s_r = -1;
+    __syncthreads();
+    find_tile<PR_THREADS>(a, index, mine, before, &s_r, &s_tile);
     if (tid == 0) {
       for (int i = 0; i < 2; ++i) { bar_init(&b_q[i], 128); bar_init(&b_s[i], 1); bar_init(&b_pa[i], 128); bar_init(&b_pb[i], 128); bar_init(&b_o[i], 1); }
       for (int i = 0; i < PR_SLOTS; ++i) { bar_init(&b_full[i], 128); bar_init(&b_empty[i], 1); }
@@ -705,7 +731,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     }
     if (!__any_sync(FULL, *reinterpret_cast<volatile int*>(&s_gave_up))) {
       const float f = parts > 1 ? 1.0f : l == 0.0f ? 0.0f : a.v_factor / l;
-      float* const sums = reinterpret_cast<float*>(a.work + PR_PARTS_AT) + (i64)blockIdx.x * prompt_part_floats<D>();
+      float* const sums = reinterpret_cast<float*>(a.work + PR_PARTS_AT) + (i64)slot * prompt_part_floats<D>();
       if (parts > 1) {
         sums[PR_ROWS * D + row] = m;
         sums[PR_ROWS * D + PR_ROWS + row] = l;
@@ -772,46 +798,79 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
   }
 }
 
-// Joins the chunks of a batch that was cut (see prompt_parts): one warp per row of q and query head, D / 32 values a lane.
-template <bool QFP16, int D>
+// Joins the chunks of the row tiles that were cut: blockIdx.x the tile (behind the uncut ones), blockIdx.y some of its rows, a warp
+// for K, whose loads are in flight together (K = 1 spreads few tiles over more warps).
+template <bool QFP16, int D, int K>
 __global__ void __launch_bounds__(256) attend_join_kernel(const Attend a) {
-  const int lane = threadIdx.x & 31, flat = blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int i = flat / a.heads, hq = flat % a.heads;
-  if (i >= a.tokens) return;
-  // the request of row i, and the row tiles before it (at most half as many requests as SMs: see the host)
-  i64 tiles = 0, ahead = 0;
-  int mine = -1;
-  Req q = {};
-  for (int r = 0; r < a.R; ++r) {
-    const Req x = request(a, r);
-    if (i >= x.row0 && i < x.row0 + x.fresh) { mine = r; q = x; ahead = tiles; }
-    tiles += prompt_tiles(a, r);
-  }
-  const int parts = prompt_parts(tiles * a.cache.heads, a.split);
-  if (mine < 0 || parts <= 1) return;         // rows of no request; or nothing was cut and the rows are written
-  const u32 row = (u32)(i - q.row0) * a.group + hq % a.group, tile = row / PR_ROWS;
-  const i64 cta = (ahead + (prompt_tiles(a, mine) - 1 - tile)) * a.cache.heads + hq / a.group;
-  const float* const base = reinterpret_cast<const float*>(a.work + PR_PARTS_AT) + cta * parts * prompt_part_floats<D>();
-  const u32 at = row % PR_ROWS;
-  float top = -INFINITY;
-  for (int p = lane; p < parts; p += 32) top = fmaxf(top, base[(i64)p * prompt_part_floats<D>() + PR_ROWS * D + at]);
+  __shared__ i64 s_scan[8];
+  __shared__ int s_r, s_tile;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  i64 mine, before;
+  const i64 all = count_tiles<256>(a, s_scan, mine, before) * a.cache.heads;
+  const Cut cut = cut_of(all, a.split);
+  const i64 cta = cut.first + blockIdx.x;
+  if (cut.parts <= 1 || cta >= all) return;
+  if (threadIdx.x == 0) s_r = -1;
+  __syncthreads();
+  find_tile<256>(a, cta / a.cache.heads, mine, before, &s_r, &s_tile);
+  __syncthreads();
+  if (s_r < 0) return;
+  const Req q = request(a, s_r);
+  const int h = (int)(cta % a.cache.heads), parts = cut.parts, row_base = s_tile * PR_ROWS, rows = min(PR_ROWS, q.fresh * a.group - row_base);
+  const float* const base = reinterpret_cast<const float*>(a.work + PR_PARTS_AT) + (i64)blockIdx.x * parts * prompt_part_floats<D>();
+  constexpr int E = D / 32, PF = prompt_part_floats<D>();
+  const int at0 = (blockIdx.y * 8 + warp) * K;
+  if (at0 >= rows) return;
+  // lane p holds m and l of part p (of 32 at a time); rows behind the last one are read, not written (the tile's memory holds 256)
+  float top[K], sum[K] = {}, acc[K][E] = {};
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
-  constexpr int E = D / 32;
-  float acc[E] = {}, sum = 0.0f;
+  for (int k = 0; k < K; ++k) {
+    top[k] = -INFINITY;
+    for (int p = lane; p < parts; p += 32) top[k] = fmaxf(top[k], base[(i64)p * PF + PR_ROWS * D + at0 + k]);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) top[k] = fmaxf(top[k], __shfl_xor_sync(FULL, top[k], o));
+  }
+  for (int p0 = 0; p0 < parts; p0 += 32) {
+    float f[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      f[k] = 0.0f;
+      if (p0 + lane < parts) {
+        const float* x = base + (i64)(p0 + lane) * PF + PR_ROWS * D + at0 + k;
+        const float m = x[0];
+        f[k] = m == -INFINITY ? 1.0f : exp2_fast(m - top[k]);        // a chunk that the row sees nothing of: sums of zero (or NaN)
+        sum[k] += x[PR_ROWS] * f[k];
+      }
+    }
+    const int n = min(32, parts - p0);
 #pragma unroll 4
-  for (int p = 0; p < parts; ++p) {
-    const float* x = base + (i64)p * prompt_part_floats<D>();
-    const float m = x[PR_ROWS * D + at], l = x[PR_ROWS * D + PR_ROWS + at];
-    const float f = m == -INFINITY ? 1.0f : exp2_fast(m - top);      // a chunk that the row sees nothing of: sums of zero (or NaN)
-    sum += l * f;
+    for (int p = 0; p < n; ++p) {
+      __align__(16) float v[K][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] += x[at * D + lane * E + e] * f;
+      for (int k = 0; k < K; ++k) {
+        const float* x = base + (i64)(p0 + p) * PF + (at0 + k) * D + lane * E;
+        if (E == 4) *reinterpret_cast<float4*>(v[k]) = *reinterpret_cast<const float4*>(x);
+        else *reinterpret_cast<float2*>(v[k]) = *reinterpret_cast<const float2*>(x);
+      }
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const float w = __shfl_sync(FULL, f[k], p);
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[k][e] += v[k][e] * w;
+      }
+    }
   }
-  const float f = sum == 0.0f ? 0.0f : a.v_factor / sum;
-  u32* const dst = reinterpret_cast<u32*>(a.out + 2 * ((i64)i * a.o_token + (i64)hq * a.o_head + lane * E));
 #pragma unroll
-  for (int e = 0; e < E; e += 2) dst[e / 2] = pack2<QFP16>(acc[e] * f, acc[e + 1] * f);
+  for (int k = 0; k < K; ++k) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) sum[k] += __shfl_xor_sync(FULL, sum[k], o);
+    if (at0 + k >= rows) continue;
+    const float f = sum[k] == 0.0f ? 0.0f : a.v_factor / sum[k];
+    const u32 flat = row_base + at0 + k, fr = flat / (u32)a.group;
+    u32* const dst = reinterpret_cast<u32*>(a.out + 2 * ((i64)(q.row0 + (int)fr) * a.o_token + (i64)(h * a.group + (int)(flat - fr * a.group)) * a.o_head + lane * E));
+#pragma unroll
+    for (int e = 0; e < E; e += 2) dst[e / 2] = pack2<QFP16>(acc[k][e] * f, acc[k][e + 1] * f);
+  }
 }
 
 }  // namespace ptk
