@@ -464,6 +464,66 @@ def test_large_max_new_gives_the_same_answers(G):
     check(G, b)
 
 
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("new", [1, 3, 45])
+def test_blocks_that_hold_k_and_v_side_by_side(G, fmt, dtype, new):
+    """A cache laid out [blocks][K, V][chunk]: strides of the other order."""
+    b = make(G, getattr(G, fmt), dtype, 8, 2, 128, 16, [100, 45, 260], [new, new, new], seed=21)
+    t = b["cache"].tensors[0]
+    other = t.transpose(0, 1).contiguous().transpose(0, 1)
+    assert other.stride() != t.stride()
+    b["cache"] = G.PagedKV(1, t.shape[1], t.shape[2], tensors=[other])
+    call(G, b)
+    check(G, b)
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("new,block", [(1, 16), (5, 16), (60, 16), (60, 256)])
+def test_a_row_of_nan_stays_alone(G, fmt, dtype, new, block):
+    b = make(G, getattr(G, fmt), dtype, 6, 2, 64, block, [200, new], [new, new], seed=22)
+    call(G, b)
+    clean = b["out"].clone()
+    b["q"][new // 2, 3] = float("nan")
+    b["out"].fill_(5.0)
+    call(G, b)
+    assert bool(b["out"][new // 2, 3].isnan().all())
+    b["out"][new // 2, 3] = clean[new // 2, 3]
+    assert torch.equal(b["out"], clean)
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("new", [2, 50])
+def test_one_query_row_for_all_tokens(G, fmt, dtype, new):
+    """q expanded over the tokens: a token stride of zero."""
+    b = make(G, getattr(G, fmt), dtype, 8, 2, 128, 16, [130, new], [new, new], seed=23, tail_rows=0)
+    one = b["q"][:1].clone()
+    b["q"] = one.expand(2 * new, -1, -1)
+    call(G, b)
+    check(G, b)
+
+
+def test_two_graphs_share_a_workspace(G):
+    """Captured calls of different shapes over one workspace, replayed in turn; the arrival counters are zero after every call."""
+    ws, graphs, want, batches = None, [], [], []
+    for i, (lens, new, fmt) in enumerate([([6000, 10], [1, 1], G.KV_PACKED), ([3000], [70], G.KV_BF16), ([900, 4000], [2, 1], G.KV_BF16)]):
+        b = make(G, fmt, torch.bfloat16, 8, 2, 128, 16, lens, new, seed=30 + i)
+        ws = G.attend_workspace(b["lay"]) if ws is None else ws
+        call(G, b, workspace=ws)
+        check(G, b)
+        want.append(b["out"].clone())
+        args = (b["lay"], b["cache"], 0, b["q"], dev(b["offsets"]), dev(b["lens"]), b["tables"], max(new))
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            G.attend(*args, out=b["out"], workspace=ws)
+        graphs.append(g)
+        batches.append((b, args))
+    for k in (0, 1, 2, 1, 0, 0, 2):
+        batches[k][0]["out"].fill_(5.0)
+        graphs[k].replay()
+        assert torch.equal(batches[k][0]["out"], want[k])
+        assert not bool(ws[:2560].any())
+
+
 def test_offsets_beyond_32_bits(G):
     """A cache larger than 4 GiB, the request in its last blocks."""
     lay = G.KVLayout(8, 128, 16, G.KV_BF16)
