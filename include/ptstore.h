@@ -512,7 +512,8 @@ int ptstore_kv_read(const ptstore_kv_cache_t* cache /*host struct*/, const int64
  * behind a row's position has no influence, infinities and NaN included.
  * Products take 16-bit operands (the cache's type; fp16 for PACKED) and add in 32 bits; maxima, sums and outputs up to the last rounding
  * are 32 bits wide; probabilities are rounded to 16 bits before they meet V.
- * The result of a call does not depend on timing: equal inputs give equal bits.
+ * The result of a call does not depend on timing: equal inputs give equal bits.  Every wait inside the kernels is bounded: S_TIMEOUT means that
+ * one ran out and rows of this call are missing or wrong.
  */
 typedef struct ptstore_attend {
   uint32_t struct_size;          /* sizeof(ptstore_attend_t) */

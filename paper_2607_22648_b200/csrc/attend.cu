@@ -128,8 +128,10 @@ int launch_prompt(Attend a, const Gpu& gpu, cudaStream_t s) {
   return PTSTORE_OK;
 }
 
-// Rows of one kv head from which a request's attention goes to the tensor-memory kernel.
-constexpr i64 PROMPT_ROWS = 33;
+// Rows of one kv head from which a request's attention goes to the tensor-memory kernel: more than the split kernel's largest row tile, so that
+// K and V are not read again.  4160 keys, 8 kv heads x 128, split / tensor-memory kernel: 20 rows 183 / 128 us (32 requests, 16-bit), 148 / 138 us
+// (4-bit), 24.9 / 20.9 and 24.9 / 22.9 us (one request); 16 rows 95 / 128 and 80 / 138 us (32 requests).
+constexpr i64 PROMPT_ROWS = 17;
 
 }  // namespace
 

@@ -1,20 +1,26 @@
 // Attention of a few query rows per request over a long paged cache (decode, speculative tokens): bounded by reading K and V once.
 //
 // o = sum_j p_j v_j / sum_j p_j, p_j = exp2(scale2 q.k_j - m): one pass over the cache with the running maximum m and sum per row.
-// Work is cut into units of 64 tokens of one (request, row tile, kv head) item.  Where cutting every item into equal chunks gives at most one
-// chunk per CTA without making the longest more than a quarter longer than an even share, a CTA takes one chunk.  Otherwise all units stand in one
-// line and every CTA takes the same number of them, so ragged batches load every SM alike; a CTA then works on parts of two
-// or three items, each of which costs it some 5 us of start and join, which is why chunks come first (one 4k request: 18.5 us
-// with the line, whose CTAs straddle two kv heads, 15.9 us with chunks).  An item that spans several CTAs leaves partial sums (o, m, l in 32 bits) in the workspace, and the CTA that arrives last joins them in CTA
-// order: the result does not depend on who that is.  One launch; the arrival counters are left zero.
+// Work is cut into units of 64 tokens of one (request, row tile, kv head) item.  Where cutting every item into equal chunks
+// gives at most one chunk per CTA without making the longest more than a quarter longer than an even share, a CTA takes one
+// chunk.  Otherwise all units stand in one line and every CTA takes the same number of them, so ragged batches load every SM
+// alike; a CTA then works on parts of two or three items, each of which costs it some 5 us of start and join, which is why
+// chunks come first (one 4k request: 18.5 us with the line, whose CTAs straddle two kv heads, 15.9 us with chunks).  An item
+// that spans several CTAs leaves partial sums (o, m, l in 32 bits) in the workspace, and the CTA that arrives last joins them
+// in CTA order: the result does not depend on who that is.  One launch; the arrival counters are left zero.
 //
 // A row tile is 8 or 16 (query head of the group, new token) rows.  The tensor instructions (mma.sync m16n8k16; the work is a
 // twentieth of what the tensor cores could do, and tcgen05's 64 or 128 rows would be mostly empty) take TOKENS as their 16 rows and
 // queries as their 8 columns: S^T = K q^T, O^T = V^T P^T, so nothing is spent on rows that do not exist, and the 4-bit
 // values are unpacked straight into the A operand.  P^T changes from accumulator to operand layout by movmatrix.
 //
-// The four warps of a CTA run alone, each on every fourth 16-token tile through its own ring of shared-memory stages (cp.async), and
-// meet at the end of an item.
+// The four warps of a CTA run alone, each on every fourth 16-token tile through its own ring of shared-memory stages (bulk copies of
+// whole tiles of a 4-bit cache, 16-byte copies of a 16-bit one, whose blocks may have any size), and meet at the end of an item.
+//
+// B200, 64 ragged requests of 2064 to 6256 tokens, 32 query and 8 kv heads x 128: 16-bit cache 173 us = 6.0 TB/s (bound by HBM); 4-bit cache 98 us
+// = 3.1 TB/s.  The latter is bound by instructions: 400 per 16 tokens and warp, of which 184 unpack codes (one LOP3 and one fused
+// multiply-add per pair), 0.6 a clock and scheduler at 16 warps an SM; two accumulator chains for S, one or four tiles per softmax step, 12 or
+// 20 warps an SM were each measured no better (99, 104, 161, 102, 152 us).
 #pragma once
 #include "attend.cuh"
 
