@@ -223,6 +223,10 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
   u32 cta = blockIdx.x, slot = 0;            // row tile; where a chunk leaves its sums
   {
     if (tid == 0) { s_gave_up = 0; s_any_bad = 0; }
+    if (!PACKED && tid == 32) {               // the maps are fetched while the tile is being found
+      if (a.box_tokens) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
+      if (a.q_box) asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
+    }
     i64 mine, before;
     const i64 all = count_tiles<PR_THREADS>(a, s_scan, mine, before);
     if (a.split) {
@@ -749,7 +753,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
         at = (i64)(rq.row0 + (int)fr) * a.o_token + (i64)(h * a.group + (int)(flat - fr * a.group)) * a.o_head;
       }
       unsigned char* const mine = smem + w * TB;
-#pragma unroll 1
+#pragma unroll
       for (int c = 0; c < D; c += 32) {
         float o[32];
         if (steps[w] > 0) {
