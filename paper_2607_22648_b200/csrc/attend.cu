@@ -157,7 +157,8 @@ extern "C" int ptstore_attend(const ptstore_attend_t* p, const ptstore_kv_cache_
   if (!isfinite(p->scale)) return PTSTORE_E_INVAL;
   if (p->requests == 0 || p->tokens == 0 || p->max_new == 0) return PTSTORE_OK;
   if (!p->q || !p->out || !p->token_offsets || !p->lengths || !p->block_tables) return PTSTORE_E_INVAL;
-  if (!rows_aligned(p->q, p->q_token_stride, p->q_head_stride) || !rows_aligned(p->out, p->out_token_stride, p->out_head_stride)) return PTSTORE_E_INVAL;
+  if (!rows_aligned(p->q, p->tokens, p->q_token_stride, p->num_heads, p->q_head_stride) ||
+      !rows_aligned(p->out, p->tokens, p->out_token_stride, p->num_heads, p->out_head_stride)) return PTSTORE_E_INVAL;
   if ((u64)p->max_blocks * cache->block_tokens > 1u << 30) return PTSTORE_E_LIMIT;                      // positions are 32 bits wide, with room for a tile
   if (p->requests > 1 << 20 || (i64)p->tokens * p->num_heads > 0x7FFFFFFF) return PTSTORE_E_LIMIT;     // row indexes of a kv head are 32 bits wide
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PTSTORE_E_INVAL;

@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(SplitShape<FMT, D>::THREADS, split_ctas<FMT, N
     };
     // the tile in stage s has landed
     auto landed = [&](int s) {
-      if (!bar_wait_or_give_up(&s_bar[warp][s], (phases >> s) & 1)) gave_up = true;
+      if (!gave_up) gave_up = !bar_wait_or_give_up(&s_bar[warp][s], (phases >> s) & 1);
       phases ^= 1u << s;
     };
 #pragma unroll

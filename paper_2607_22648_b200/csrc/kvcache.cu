@@ -188,7 +188,8 @@ int run(const void* k, const void* v, i64 k_token, i64 k_head, i64 v_token, i64 
   if (tokens < 0 || (dtype != PTSTORE_KV_BF16 && dtype != PTSTORE_KV_FP16)) return PTSTORE_E_INVAL;
   if (cache->format != PTSTORE_KV_PACKED && cache->format != dtype) return PTSTORE_E_INVAL;
   if (tokens == 0) return PTSTORE_OK;
-  if (!k || !v || !slots || !rows_aligned(k, k_token, k_head) || !rows_aligned(v, v_token, v_head)) return PTSTORE_E_INVAL;
+  if (!k || !v || !slots || !rows_aligned(k, tokens, k_token, cache->num_kv_heads, k_head) ||
+      !rows_aligned(v, tokens, v_token, cache->num_kv_heads, v_head)) return PTSTORE_E_INVAL;
   const int D = (int)cache->head_dim;
   KvArgs a = {cache_of(cache), {(unsigned char*)k, (unsigned char*)v, k_token, k_head, v_token, v_head}, reinterpret_cast<const i64*>(slots), 0,
               cache->k_scale, cache->v_scale, status};

@@ -82,8 +82,9 @@ inline int check_cache(const ptstore_kv_cache_t* c) {
 inline Cache cache_of(const ptstore_kv_cache_t* c) {
   return {static_cast<unsigned char*>(c->base), c->kv_stride_bytes, c->block_stride_bytes, c->num_blocks, c->block_tokens, c->num_kv_heads};
 }
-inline bool rows_aligned(const void* p, i64 token_stride, i64 head_stride) {       // 16-byte loads and stores of 16-bit elements
-  return !(reinterpret_cast<uintptr_t>(p) & 15u) && token_stride % 8 == 0 && head_stride % 8 == 0;
+// 16-byte loads and stores of 16-bit elements; the stride of an axis of one does not matter
+inline bool rows_aligned(const void* p, i64 tokens, i64 token_stride, i64 heads, i64 head_stride) {
+  return !(reinterpret_cast<uintptr_t>(p) & 15u) && (tokens == 1 || token_stride % 8 == 0) && (heads == 1 || head_stride % 8 == 0);
 }
 
 }  // namespace ptk

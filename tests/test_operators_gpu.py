@@ -502,6 +502,21 @@ def test_one_query_row_for_all_tokens(G, fmt, dtype, new):
     check(G, b)
 
 
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+def test_one_row_of_any_stride(G, fmt, dtype):
+    """One token, one kv head: the strides of axes of one do not matter."""
+    b = make(G, getattr(G, fmt), dtype, 24, 1, 64, 16, [77], [1], seed=24, tail_rows=0)
+    b["q"] = b["q"].as_strided((1, 24, 64), (24 * 64 + 5, 64, 1))
+    call(G, b)
+    check(G, b)
+    call(G, b, max_new=40)
+    check(G, b)
+    rows1 = torch.zeros(64, dtype=dtype, device="cuda").as_strided((1, 1, 64), (67, 65, 1))
+    G.kv_write(b["lay"], b["cache"], 0, rows1, rows1, torch.zeros(1, dtype=torch.int64, device="cuda"))
+    k, v = G.kv_read(b["lay"], b["cache"], 0, torch.zeros(1, dtype=torch.int64, device="cuda"), dtype)
+    assert not bool(k.any()) and not bool(v.any())
+
+
 def test_two_graphs_share_a_workspace(G):
     """Captured calls of different shapes over one workspace, replayed in turn; the arrival counters are zero after every call."""
     ws, graphs, want, batches = None, [], [], []
