@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(SplitShape<FMT, D>::THREADS, split_ctas<FMT, N
     auto issue = [&](int i, int s) {
       seen_bits &= ~(1u << s);
       if (PACKED) {
-        if (i < n_tiles) {
+        if (i < n_tiles && !gave_up) {
           if ((i & 31) == 0) resolve32(i);
           const i64 off = __shfl_sync(FULL, tile_off, i & 31);
           if (off >= 0) {
@@ -339,9 +339,13 @@ __global__ void __launch_bounds__(SplitShape<FMT, D>::THREADS, split_ctas<FMT, N
       }
       cp_commit();
     };
-    // the tile in stage s has landed
+    // The tile in stage s has landed.  After a wait that ran out no copy is issued any more; what is in flight is still waited for,
+    // stage by stage, so that none lands after the CTA has ended.
     auto landed = [&](int s) {
-      if (!gave_up) gave_up = !bar_wait_or_give_up(&s_bar[warp][s], (phases >> s) & 1);
+      if (__any_sync(FULL, !bar_wait_or_give_up(&s_bar[warp][s], (phases >> s) & 1))) {
+        gave_up = true;
+        bar_wait_or_give_up(&s_bar[warp][s], (phases >> s) & 1);
+      }
       phases ^= 1u << s;
     };
 #pragma unroll
