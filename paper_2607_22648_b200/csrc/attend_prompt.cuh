@@ -360,7 +360,10 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
         }
         if (j + 1 < n_steps) release(kop);
       }
-      // everything issued has ended before tensor memory is given back
+      // everything issued has ended before tensor and shared memory are given back (q's loads too, where their wait ran out)
+      for (int w = 0; w < 2; ++w)
+        if (steps[w] > 0)
+          for (u32 i = 0; i < PR_POLLS && !bar_try(&b_q[w], 0); ++i) {}
       if (elected()) tc_commit(&b_end);
       __syncwarp();
       for (u32 i = 0; i < PR_POLLS && !bar_try(&b_end, 0); ++i) {}
@@ -465,14 +468,13 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       const bool leads = box && pt % box == 0;
       i64 next = n_steps > 0 ? where(0) : -1;
       int j = 0;
-      bool stop = false;                      // the same in all 128 threads
       for (; j < n_steps; ++j) {
         const u32 block = id;
         s_row[j & 1][pt] = next;
         const u32 present = __ballot_sync(FULL, next >= 0);
         if (lane == 0) s_valid[j & 3][warp - 8] = present;
         if (j + 1 < n_steps) next = where(j + 1);
-        if (any_of_128(*gave_up)) { stop = true; break; }
+        if (any_of_128(*gave_up)) break;      // the same in all 128 threads
         const bool plain = box && key0 + (j + 1) * PR_KEYS <= all_see && (s_valid[j & 3][0] & s_valid[j & 3][1] & s_valid[j & 3][2] & s_valid[j & 3][3]) == FULL;
         for (int is_v = 0; is_v < 2; ++is_v) {
           const int op = 2 * j + is_v;
@@ -504,9 +506,9 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
           } else cp_arrive(full);             // arrives when this thread's copies have landed
         }
       }
-      if (stop)                               // what is in flight lands before the CTA gives its memory back
-        for (int op = max(0, 2 * j - PR_SLOTS); op < 2 * j; ++op)
-          for (u32 i = 0; i < PR_POLLS && !bar_try(&b_full[op % PR_SLOTS], (op / PR_SLOTS) & 1); ++i) {}
+      // whatever happened, what is in flight lands before the CTA gives its memory back
+      for (int op = max(0, 2 * j - PR_SLOTS); op < 2 * j; ++op)
+        for (u32 i = 0; i < PR_POLLS && !bar_try(&b_full[op % PR_SLOTS], (op / PR_SLOTS) & 1); ++i) {}
       cp_commit();
       cp_wait<0>();
     } else {
@@ -568,8 +570,10 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     // zeros along and are not stored); else chunk t % CPR of rows t / CPR, ..., all on their way before the first is used, with the
     // sign of the softmax scale and the changes a 4-bit cache asks for.  (Copied by the threads a CTA's first scores came 6000
     // clocks later, of 50,000 to 150,000 in all.)
+    // A tile without steps loads none: nobody would wait for it, and the tile's output goes through the same memory.
     if (!PACKED && a.q_box) {
-      if (t == 0) {
+      if (steps[w] == 0) {
+      } else if (t == 0) {
         bar_expect(&b_q[w], TB);
 #pragma unroll
         for (int e = 0; e < D / 64; ++e)

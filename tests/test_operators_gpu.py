@@ -502,6 +502,18 @@ def test_one_query_row_for_all_tokens(G, fmt, dtype, new):
     check(G, b)
 
 
+@pytest.mark.parametrize("many", [20, 300])
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+def test_row_tiles_that_see_nothing(G, fmt, dtype, many):
+    """Whole row tiles in front of the first key, beside tiles that see some: their rows are zeros, run after run."""
+    b = make(G, getattr(G, fmt), dtype, 8, 2, 128, 16, [0] * many + [40, 700], [64] * many + [300, 100], seed=25)
+    for _ in range(3):
+        b["out"].fill_(5.0)
+        call(G, b)
+        assert not bool(b["out"][:64 * many + 260].any())
+    check(G, b)
+
+
 @pytest.mark.parametrize("fmt,dtype", FORMATS)
 def test_one_row_of_any_stride(G, fmt, dtype):
     """One token, one kv head: the strides of axes of one do not matter."""
