@@ -11,8 +11,6 @@ namespace {
 // rows of an item: 8 where a request's rows of one kv head fit, else 16
 inline int n_tiles_of(i64 rows) { return rows <= 8 ? 1 : 2; }
 
-constexpr u64 counters_bytes(int ctas) { return ((u64)ctas * 4 + 255) / 256 * 256; }
-
 struct Gpu { int dev, sms; };
 int current_gpu(Gpu* g) {
   if (cudaGetDevice(&g->dev) != cudaSuccess || cudaDeviceGetAttribute(&g->sms, cudaDevAttrMultiProcessorCount, g->dev) != cudaSuccess || g->sms <= 0) {
@@ -138,8 +136,8 @@ constexpr i64 PROMPT_ROWS = 17;
 extern "C" uint64_t ptstore_attend_workspace_bytes(uint32_t head_dim) {
   if (head_dim != 64 && head_dim != 128) return 0;
   // counters, then two parts per CTA of the split kernel (of 8 rows where 4 CTAs share an SM, of 16 where 2 do), or one of 256 rows per SM
-  static_assert(counters_bytes(MAX_SMS * 4) <= PR_PARTS_AT, "the prompts' parts lie behind the counters");
-  const u64 split = counters_bytes(MAX_SMS * 4) + (u64)MAX_SMS * 4 * 2 * 8 * (head_dim + 2) * 4;
+  static_assert(MAX_SMS * 4 * 4 <= PR_PARTS_AT && MAX_SMS * 4 * 4 <= SP_PARTS_AT, "parts lie behind the counters of any grid");
+  const u64 split = SP_PARTS_AT + (u64)MAX_SMS * 4 * 2 * 8 * (head_dim + 2) * 4;
   const u64 prompt = PR_PARTS_AT + (u64)MAX_SMS * PR_ROWS * (head_dim + 2) * 4;
   return split > prompt ? split : prompt;
 }

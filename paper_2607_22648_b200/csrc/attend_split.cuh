@@ -27,6 +27,7 @@
 namespace ptk {
 
 constexpr int MIN_TOKENS = 256;              // a CTA takes at least this many, so that joining does not cost more than it saves
+constexpr int SP_PARTS_AT = 4096;            // where the parts begin in the workspace, behind the counters of the largest grid
 constexpr u32 SP_POLLS = 1u << 22;           // polls of a wait for a tile before the warp gives up (each may suspend for a while)
 
 template <int FMT, int D>
@@ -734,7 +735,7 @@ __global__ void __launch_bounds__(SplitShape<FMT, D>::THREADS, split_ctas<FMT, N
       // partial sums: slot 1 of the CTA the item begins in, slot 0 of the others
       constexpr int PF = part_floats<NT, D>();
       u32* counters = reinterpret_cast<u32*>(a.work);
-      float* parts = reinterpret_cast<float*>(a.work + ((gridDim.x * 4 + 255) / 256) * 256);
+      float* parts = reinterpret_cast<float*>(a.work + SP_PARTS_AT);
       float* my = parts + (2 * (i64)blockIdx.x + (blockIdx.x == first_cta ? 1 : 0)) * PF;
       if (row < rows) {
 #pragma unroll

@@ -502,6 +502,28 @@ def test_one_query_row_for_all_tokens(G, fmt, dtype, new):
     check(G, b)
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+def test_calls_of_all_shapes_share_a_workspace(G, dim):
+    """Grids of 8 and 16 rows, of 4-bit and 16-bit caches and whole prompts leave the workspace as the next call needs it."""
+    lens = [333 + 97 * i for i in range(24)]
+    batches = []
+    for i, (fmt, dtype) in enumerate([("KV_PACKED", torch.bfloat16), ("KV_BF16", torch.bfloat16)]):
+        for new in (1, 4, 40):
+            batches.append(make(G, getattr(G, fmt), dtype, 8, 2, dim, 16, lens, [new] * 24, seed=30 + i))
+    work = G.attend_workspace(batches[0]["lay"])
+    right = []
+    for b in batches:
+        call(G, b)
+        check(G, b)
+        right.append(b["out"].clone())
+    for first in range(len(batches)):
+        for second in range(len(batches)):
+            for i in (first, second, first):
+                batches[i]["out"].fill_(5.0)
+                call(G, batches[i], workspace=work)
+                assert torch.equal(batches[i]["out"], right[i]), (first, second, i)
+
+
 @pytest.mark.parametrize("many", [20, 300])
 @pytest.mark.parametrize("fmt,dtype", FORMATS)
 def test_row_tiles_that_see_nothing(G, fmt, dtype, many):
