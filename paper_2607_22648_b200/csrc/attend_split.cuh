@@ -800,6 +800,8 @@ __global__ void __launch_bounds__(SplitShape<FMT, D>::THREADS, split_ctas<FMT, N
         for (int i = 0; i < E / 8; ++i) reinterpret_cast<uint4*>(dst)[i] = *reinterpret_cast<const uint4*>(v + 4 * i);
       } else *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(v);
     }
+    // the joins' sums lay in the ring: they come before the next item's bulk copies, which write it through the async proxy
+    if (PACKED) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncthreads();                                          // the ring and the small arrays are free again
     u += ub - ua;
     left += ub - ua;

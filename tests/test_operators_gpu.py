@@ -731,3 +731,21 @@ def test_the_binding_refuses(G):
         G.kv_write(lay, c, 0, b["q"][:2, :2], b["q"][:3, :2], torch.arange(2, device="cuda"))
     with pytest.raises(ValueError):
         G.map_slots(dev([3]), dev([1, 2]), b["tables"], 16, 4)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("dim,new", [(128, 1), (128, 4), (64, 1), (64, 3)])
+def test_a_cta_goes_from_item_to_item_of_a_ragged_batch(G, dtype, dim, new):
+    """A CTA of the split kernel works on parts of several items of a 4-bit cache one after the other: the next one's tiles arrive where the last
+    one's sums were joined.  Equal bits every time, and right."""
+    rng = random.Random(41)
+    lens = [rng.choice([5, 70, 200, rng.randint(100, 900)]) for _ in range(96)]
+    b = make(G, G.KV_PACKED, dtype, 16, 4, dim, 16, lens, [min(new, n) for n in lens], seed=41)
+    work = G.attend_workspace(b["lay"])
+    call(G, b, workspace=work)
+    check(G, b)
+    first = b["out"].clone()
+    for _ in range(20):
+        b["out"].fill_(5.0)
+        call(G, b, workspace=work)
+        assert torch.equal(first, b["out"])
