@@ -101,9 +101,9 @@ struct Assign {
 // blocks a request holds and needs; a length its row cannot hold leaves the row as it is
 __device__ __forceinline__ void want(const Assign& a, int h, int len, int& held, int& need, uint32_t& bad) {
   held = h < 0 ? 0 : h > a.max_blocks ? a.max_blocks : h;
-  if (held != h || len < 0) bad = PTSTORE_S_BOUNDS;
+  if (held != h || len < 0) bad |= PTSTORE_S_BOUNDS;
   const uint32_t n = len <= 0 ? 0 : a.shift >= 0 ? ((uint32_t)(len - 1) >> a.shift) + 1 : (uint32_t)(len - 1) / (uint32_t)a.block_tokens + 1;
-  if (n > (uint32_t)a.max_blocks) { need = held; bad = PTSTORE_S_BOUNDS; } else need = (int)n;
+  if (n > (uint32_t)a.max_blocks) { need = held; bad |= PTSTORE_S_BOUNDS; } else need = (int)n;
 }
 
 // NARROW: 32 requests' blocks fit 16 bits, so a warp scans growth and give-back in one 32-bit value
@@ -165,7 +165,7 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS) assig
 
   const int c0 = *a.free_count;
   const int count = c0 < 0 ? 0 : c0 > a.capacity ? a.capacity : c0;
-  if (count != c0) bad = PTSTORE_S_BOUNDS;
+  if (count != c0) bad |= PTSTORE_S_BOUNDS;
   // surplus blocks of shrinking rows go onto the stack, in (request, block) order
   i64 pushed = 0;
   for (int base = 0; base < a.R; base += ROWS * THREADS) {
@@ -255,7 +255,7 @@ struct MapSlots {
 
 // tokens of a request that are in the cache already, and new ones
 __device__ __forceinline__ void done_new(const MapSlots& m, int len, int d0, int& done, int& fresh, uint32_t& bad) {
-  if (len < 0) { len = 0; bad = PTSTORE_S_BOUNDS; }
+  if (len < 0) { len = 0; bad |= PTSTORE_S_BOUNDS; }
   i64 d = (i64)d0 * m.done_unit;
   const i64 most = (i64)len - m.min_new;
   if (d > most) d = most;
@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(THREADS) map_slots_kernel(const MapSlots m) {
           pos[e] = s_done[i] + (int)(k - s_first[i]);
           const int j = m.shift >= 0 ? pos[e] >> m.shift : pos[e] / m.block_tokens;
           if (j < m.max_blocks) b[e] = m.tables[(i64)(base + i) * m.max_blocks + j];
-          else bad = PTSTORE_S_BOUNDS;
+          else bad |= PTSTORE_S_BOUNDS;
         }
       }
 #pragma unroll
@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(THREADS) map_slots_kernel(const MapSlots m) {
   }
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     m.offsets[m.R] = base_tok > INT_MAX ? INT_MAX : (int)base_tok;
-    if (base_tok > m.max_tokens) bad = PTSTORE_S_BOUNDS;
+    if (base_tok > m.max_tokens) bad |= PTSTORE_S_BOUNDS;
   }
   // entries behind the last token are empty slots, so a write of a padded batch skips them
   for (i64 t = (t0 > base_tok ? t0 : base_tok) + threadIdx.x; t < t1; t += THREADS) {

@@ -749,3 +749,15 @@ def test_a_cta_goes_from_item_to_item_of_a_ragged_batch(G, dtype, dim, new):
         b["out"].fill_(5.0)
         call(G, b, workspace=work)
         assert torch.equal(first, b["out"])
+
+
+def test_plan_keeps_both_complaints_of_a_large_batch(G):
+    """More than one scan step: a denied row in the first, and a length beyond its row handled by the same thread in the second."""
+    R, block, width = 16384 + 1024, 16, 2
+    for lane in (0, 5, 1023):
+        lengths, held = [0] * R, [0] * R
+        lengths[lane], lengths[16384 + lane] = 32, 33
+        t, st, count, status = torch.full((R, width), -1, dtype=torch.int32, device="cuda"), dev([7, 8]), dev([1]), dev([0])
+        h, c = G.assign_blocks(dev(lengths), dev(held), t, st, count, block, status=status)
+        assert int(status.item()) == G.S_NOSPACE | G.S_BOUNDS, lane
+        assert not bool(h.any()) and c.tolist() == [1] and bool((t == -1).all())
