@@ -25,19 +25,21 @@ struct Attend {
   u32* status;
 };
 
-// rows of request r (clamped to the rows that exist), its keys, and the position of its first new token (may be negative)
+// rows of request r that exist, its keys, and the position of its first row (may be negative).  Rows behind `tokens` count for the
+// positions although they are not there.
 struct Req { int row0, fresh, keys, pos0; };
 __device__ __forceinline__ Req request(const Attend& a, int r) {
   Req q;
-  int lo = a.offsets[r], hi = a.offsets[r + 1];
-  const int len = a.lengths[r];
-  lo = lo < 0 ? 0 : lo > a.tokens ? a.tokens : lo;
-  hi = hi < lo ? lo : hi > a.tokens ? a.tokens : hi;
-  q.row0 = lo;
-  q.fresh = hi - lo;
+  const int lo = a.offsets[r], end = a.offsets[r + 1], len = a.lengths[r];
+  q.row0 = lo < 0 ? 0 : lo > a.tokens ? a.tokens : lo;
+  const int hi = end < q.row0 ? q.row0 : end > a.tokens ? a.tokens : end;
+  q.fresh = hi - q.row0;
   const i64 room = (i64)a.max_blocks * a.cache.block_tokens;
   q.keys = len < 0 ? 0 : len > room ? (int)room : len;
-  q.pos0 = len - q.fresh;                     // a length the table cannot hold keeps its positions; the keys it lacks are not seen
+  // A length the table cannot hold keeps its positions; the keys it lacks are not seen.  Positions from `room` (at most 2^30) on see the same keys, so
+  // 32 bits hold position + row without overflow.
+  const i64 pos = (i64)len - end + q.row0;
+  q.pos0 = pos > room ? (int)room : pos < -0x7FFFFFFF ? -0x7FFFFFFF : (int)pos;
   return q;
 }
 

@@ -761,3 +761,53 @@ def test_plan_keeps_both_complaints_of_a_large_batch(G):
         h, c = G.assign_blocks(dev(lengths), dev(held), t, st, count, block, status=status)
         assert int(status.item()) == G.S_NOSPACE | G.S_BOUNDS, lane
         assert not bool(h.any()) and c.tolist() == [1] and bool((t == -1).all())
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("lens,new,rows_in", [([40, 30, 20, 10], [1, 1, 1, 1], 2), ([50, 70, 9], [4, 4, 4], 6), ([300, 200, 100], [40, 60, 30], 71), ([333, 90], [300, 64], 290)])
+def test_rows_that_do_not_fit_keep_the_positions_of_the_others(G, fmt, dtype, lens, new, rows_in):
+    """Offsets reach beyond q (the outputs of map_slots with too small a max_tokens): the rows that are there are as with all of them, and see
+    no key behind their own position."""
+    b = make(G, getattr(G, fmt), dtype, 8, 2, 128, 16, lens, new, seed=51, tail_rows=0)
+    done = dev([n - m for n, m in zip(lens, new)])
+    status = dev([0])
+    offsets, slots, positions = G.map_slots(dev(lens), done, b["tables"], 16, rows_in, status=status)
+    assert int(status.item()) == G.S_BOUNDS and offsets.tolist() == b["offsets"]
+    out = torch.full_like(b["q"][:rows_in], 5.0)
+    G.attend(b["lay"], b["cache"], 0, b["q"][:rows_in], offsets, dev(lens), b["tables"], max(new), out=out)
+    want, spread, scores, _ = ref.attend(b["q"], b["offsets"], lens, b["tables"], b["values"][0], b["values"][1], 16, 128 ** -0.5)
+    v_max, k_sum = float(b["values"][1].nan_to_num(0).abs().max()), float(b["values"][0].nan_to_num(0).abs().sum(-1).max()) * 128 ** -0.5
+    tol = ref.attend_tolerance(b["q"], want, spread, scores, max(lens), v_max, fmt == "KV_PACKED", k_sum)
+    assert bool(((out.double() - want[:rows_in]).abs() <= tol[:rows_in]).all())
+    # the keys behind the last row that is there do not matter, NaN included
+    r = max(i for i in range(len(lens)) if b["offsets"][i] < rows_in)
+    first = int(positions[rows_in - 1]) + 1
+    if first < lens[r]:
+        behind = torch.tensor([int(b["tables"][r, p // 16]) * 16 + p % 16 for p in range(first, lens[r])], device="cuda")
+        bad = torch.full((len(behind), 2, 128), float("nan"), dtype=dtype, device="cuda")
+        G.kv_write(b["lay"], b["cache"], 0, bad, bad, behind)
+        again = torch.full_like(out, 5.0)
+        G.attend(b["lay"], b["cache"], 0, b["q"][:rows_in], offsets, dev(lens), b["tables"], max(new), out=again)
+        assert torch.equal(again, out)
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("new", [2, 40])
+def test_lengths_and_offsets_at_the_ends_of_their_range(G, fmt, dtype, new):
+    """The largest and smallest 32-bit lengths and offsets: a row sees what its table holds, or nothing."""
+    top, low = 2 ** 31 - 1, -2 ** 31
+    b = make(G, getattr(G, fmt), dtype, 4, 2, 64, 16, [90, 50], [new, new], seed=52, width=6, tail_rows=0)
+    b["tables"] = b["tables"][:, :3].contiguous()                 # rows hold 48 tokens
+    out = torch.full_like(b["q"], 5.0)
+    G.attend(b["lay"], b["cache"], 0, b["q"], dev([0, new, 2 * new]), dev([top, low]), b["tables"], new, out=out)
+    b["lens"] = [48 + new, 0]
+    want = torch.full_like(out, 5.0)
+    G.attend(b["lay"], b["cache"], 0, b["q"], dev([0, new, 2 * new]), dev([48 + new, 0]), b["tables"], new, out=want)
+    assert torch.equal(out, want) and bool(torch.isfinite(out[:new]).all()) and not bool(out[new:].any())
+    # offsets of the whole range: every row there is belongs to the one request and lies in front of its first key, or behind its last
+    out.fill_(5.0)
+    G.attend(b["lay"], b["cache"], 0, b["q"], dev([0, top, top]), dev([48, 48]), b["tables"], new, out=out)
+    assert not bool(out.any())
+    out.fill_(5.0)
+    G.attend(b["lay"], b["cache"], 0, b["q"], dev([low, 2 * new, 2 * new]), dev([48 + 2 * new, 0]), b["tables"], new, out=out)
+    assert torch.equal(out[:new], want[:new])
