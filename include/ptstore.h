@@ -514,10 +514,10 @@ int ptstore_kv_read(const ptstore_kv_cache_t* cache /*host struct*/, const int64
  * Products take 16-bit operands (the cache's type; fp16 for PACKED) and add in 32 bits; maxima, sums and outputs up to the last rounding
  * are 32 bits wide; probabilities are rounded to 16 bits before they meet V.
  * The result of a call does not depend on timing: equal inputs give equal bits.  Every wait inside the kernels is bounded: S_TIMEOUT means that
- * one ran out and rows of this call are missing or wrong.
+ * one ran out and rows of this call are missing or wrong.  The workspace is ready for the next call all the same.
  */
 typedef struct ptstore_attend {
-  uint32_t struct_size;          /* sizeof(ptstore_attend_t) */
+  uint32_t struct_size;          /* sizeof(ptstore_attend_t); PTSTORE_ATTEND_SIZE_1 without the fields behind `scale` */
   uint32_t dtype;                /* of q and out: PTSTORE_KV_BF16 or PTSTORE_KV_FP16; a 16-bit cache has the same */
   const void* q;                 /* [tokens][num_heads][head_dim], strides in elements (multiples of 8), 16-byte aligned */
   int64_t  q_token_stride, q_head_stride;
@@ -530,7 +530,11 @@ typedef struct ptstore_attend {
   int32_t  tokens;               /* rows of q and out */
   int32_t  max_new;              /* at least the rows of any request: chooses the kernel (host) */
   float    scale;                /* of the scores, usually 1 / sqrt(head_dim) */
+  uint32_t wait_polls;           /* polls of a wait for loads and products before a CTA gives up, 0: the built-in limit.  For failure-detection tests: a
+                                    limit of 1 is a single test that never suspends.  What is in flight then is awaited with the built-in limit. */
+  uint32_t reserved;             /* 0 */
 } ptstore_attend_t;
+#define PTSTORE_ATTEND_SIZE_1 104u
 
 /* Bytes of workspace (256-byte aligned device memory, ZERO before its first use).  A call leaves it ready for the next one, whatever that
  * one's sizes; calls that share a workspace must not overlap. */

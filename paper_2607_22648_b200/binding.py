@@ -70,7 +70,7 @@ class Attend(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_uint32), ("q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
                 ("out", C.c_void_p), ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64), ("token_offsets", C.c_void_p),
                 ("lengths", C.c_void_p), ("block_tables", C.c_void_p), ("requests", C.c_int32), ("max_blocks", C.c_int32), ("num_heads", C.c_int32),
-                ("tokens", C.c_int32), ("max_new", C.c_int32), ("scale", C.c_float)]
+                ("tokens", C.c_int32), ("max_new", C.c_int32), ("scale", C.c_float), ("wait_polls", C.c_uint32), ("reserved", C.c_uint32)]
 
 
 EXPORTS = ["ptstore_workspace_bytes", "ptstore_create", "ptstore_destroy", "ptstore_hash", "ptstore_lookup",
@@ -195,8 +195,8 @@ def fetch_static(hbm_pool, hbm_blocks, layers, chunk_bytes, ids, matched, cache,
 # are packed as bytes.
 _KV_DTYPES = {torch.bfloat16: KV_BF16, torch.float16: KV_FP16}
 _KV_CACHE = struct.Struct("PQQIIIIIIff")
-_ATTEND = struct.Struct("IIPqqPqqPPPiiiiif")
-assert _KV_CACHE.size == C.sizeof(KvCache) and _ATTEND.size <= C.sizeof(Attend)
+_ATTEND = struct.Struct("IIPqqPqqPPPiiiiifII")
+assert _KV_CACHE.size == C.sizeof(KvCache) and _ATTEND.size == C.sizeof(Attend)
 _ATTEND_SIZE = C.sizeof(Attend)
 _raw_stream = torch._C._cuda_getCurrentRawStream
 _device = torch.cuda.current_device
@@ -363,10 +363,11 @@ def attend_workspace(layout):
     return raw[at:at + n]
 
 
-def attend(layout, cache, layer, q, token_offsets, lengths, block_tables, max_new, scale=None, out=None, workspace=None, status=None):
+def attend(layout, cache, layer, q, token_offsets, lengths, block_tables, max_new, scale=None, out=None, workspace=None, status=None, wait_polls=0):
     """ptstore_attend: causal attention of the new tokens q [tokens, num_heads, dim] over the paged cache (which holds their own K/V
     already).  Request r owns rows token_offsets[r] .. token_offsets[r+1]-1 and lengths[r] tokens of cache; max_new (host) is at least the
-    rows of any request.  workspace: from attend_workspace (a program that calls often keeps one per stream).  Returns out."""
+    rows of any request.  workspace: from attend_workspace (a program that calls often keeps one per stream).  wait_polls: polls of the kernels' bounded
+    waits, 0 for the built-in limit.  Returns out."""
     dev, i32, code = _device(), torch.int32, _kv_dtype(q, "q")
     R, (T, heads, dim) = lengths.numel(), q.shape
     if out is None:
@@ -380,7 +381,7 @@ def attend(layout, cache, layer, q, token_offsets, lengths, block_tables, max_ne
                         _rows(out, heads, layout.dim, T, q.dtype, dev, "out"), o_stride[0], o_stride[1],
                         _vec(token_offsets, i32, R + 1, dev, "token_offsets"), _vec(lengths, i32, R, dev, "lengths"),
                         _table(block_tables, R, dev, "block_tables"), R, block_tables.shape[1], heads, T, max_new,
-                        layout.dim ** -0.5 if scale is None else scale)
+                        layout.dim ** -0.5 if scale is None else scale, wait_polls, 0)
     _check(lib.ptstore_attend(args, layout.of(cache, layer, dev), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                               None if status is None else _vec(status, i32, 1, dev, "status"), _raw_stream(dev)), "ptstore_attend")
     return out

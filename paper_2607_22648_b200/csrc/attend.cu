@@ -1,5 +1,6 @@
 // ptstore_attend: host side and dispatch of the attention over the paged cache.
 #include <atomic>
+#include <cstddef>
 
 #include "attend_prompt.cuh"
 #include "attend_split.cuh"
@@ -144,7 +145,9 @@ extern "C" uint64_t ptstore_attend_workspace_bytes(uint32_t head_dim) {
 
 extern "C" int ptstore_attend(const ptstore_attend_t* p, const ptstore_kv_cache_t* cache, void* workspace, uint64_t workspace_bytes,
                               uint32_t* status, ptstore_stream_t stream) {
-  if (!p || p->struct_size != sizeof(ptstore_attend_t)) return PTSTORE_E_INVAL;
+  static_assert(offsetof(ptstore_attend_t, wait_polls) == PTSTORE_ATTEND_SIZE_1, "the first form of the struct ends here");
+  if (!p || (p->struct_size != sizeof(ptstore_attend_t) && p->struct_size != PTSTORE_ATTEND_SIZE_1)) return PTSTORE_E_INVAL;
+  const u32 polls = p->struct_size == PTSTORE_ATTEND_SIZE_1 ? 0 : p->wait_polls;
   const int rc = check_cache(cache);
   if (rc) return rc;
   const int D = (int)cache->head_dim;
@@ -174,6 +177,7 @@ extern "C" int ptstore_attend(const ptstore_attend_t* p, const ptstore_kv_cache_
   a.scale2 = p->scale * LOG2E * (packed ? cache->k_scale * DEQ_FACTOR : 1.0f);
   a.v_factor = packed ? cache->v_scale * DEQ_FACTOR : 1.0f;
   a.work = static_cast<unsigned char*>(workspace);
+  a.polls = polls ? polls : POLLS;
   a.status = status;
   a.box_tokens = a.q_box = a.split = 0;
   Gpu gpu;

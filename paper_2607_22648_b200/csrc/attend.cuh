@@ -22,8 +22,10 @@ struct Attend {
   u32 box_tokens;                             // tokens of a box of the cache's tensor map, 0: there is none
   u32 q_box;                                  // there is a tensor map of q
   u32 split;                                  // CTAs among which the steps of the row tiles may be cut, 0: they are not
+  u32 polls;                                  // polls of a wait before its CTA gives up
   u32* status;
 };
+constexpr u32 POLLS = 1u << 22;               // the built-in limit (each poll may suspend for a while), and that of waits for what is in flight at the end
 
 // rows of request r that exist, its keys, and the position of its first row (may be negative).  Rows behind `tokens` count for the
 // positions although they are not there.
@@ -54,6 +56,11 @@ __device__ __forceinline__ void bar_init(u64* bar, u32 count) { asm volatile("mb
 __device__ __forceinline__ void bar_arrive(u64* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory"); }
 __device__ __forceinline__ void bar_expect(u64* bar, u32 bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_test(u64* bar, u32 parity) {         // never suspends
+  u32 ok;
+  asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity) : "memory");
+  return ok != 0;
 }
 __device__ __forceinline__ bool bar_try(u64* bar, u32 parity) {
   u32 ok;

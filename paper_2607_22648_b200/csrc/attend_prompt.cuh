@@ -38,7 +38,6 @@ constexpr int PR_ROWS = 256, PR_KEYS = 128;
 constexpr int PR_PARTS_AT = 4096;            // where the parts begin in the workspace (behind the other kernel's counters)
 constexpr int PR_SLOTS = 4;
 constexpr int PR_RAW = 3;                    // 4-bit tiles on their way to being unpacked
-constexpr u32 PR_POLLS = 1u << 22;           // polls of a wait before the CTA gives up (each may suspend for a while)
 
 template <int D>
 struct PromptShape {
@@ -48,16 +47,21 @@ struct PromptShape {
   static constexpr int SMEM_PACKED = SMEM + PR_RAW * RAW_BYTES;
 };
 
-// Waits, at most PR_POLLS polls; a wait that runs out says so and lets its caller go on (with whatever is there: every access stays in bounds
-// whatever the data), and the roles leave their loops at the next step.
-__device__ __forceinline__ void bar_wait(u64* bar, u32 parity, volatile int* gave_up) {
-  if (bar_try(bar, parity)) return;
+// Waits, at most `polls` polls, and says whether what it waited for has come.  A wait that ran out sets *gave_up.  Its caller then issues no copy
+// and no tensor instruction that needed it, the other roles see *gave_up or run out of polls themselves, and every role waits for what it has in
+// flight (with the built-in limit) before it leaves.
+__device__ __forceinline__ bool bar_wait(u64* bar, u32 parity, u32 polls, volatile int* gave_up) {
+  if (bar_test(bar, parity)) return true;
 #pragma unroll 1
-  for (u32 i = 0; i < PR_POLLS; ++i) {
-    if (bar_try(bar, parity)) return;
-    if ((i & 1023) == 1023 && *gave_up) return;
+  for (u32 i = 1; i < polls; ++i) {
+    if (bar_try(bar, parity)) return true;
+    if ((i & 1023) == 1023 && *gave_up) return false;
   }
   *gave_up = 1;
+  return false;
+}
+__device__ __forceinline__ void bar_drain(u64* bar, u32 parity) {
+  for (u32 i = 0; i < POLLS && !bar_try(bar, parity); ++i) {}
 }
 
 // barrier of the 128 loading threads, and whether the value was set in any of them
@@ -294,9 +298,9 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     }
     if (warp == 12) {                         // the whole warp walks the steps, one lane issues: operands stay warp-uniform
       constexpr u32 QK = mma_desc(F16, PR_KEYS, false), PV = mma_desc(F16, D, true);
+      bool quit = false;                      // a wait ran out: nothing is issued from there on
       auto wait = [&](u64* b, u32 parity) {
-        bar_wait(b, parity, &s_gave_up);
-        __syncwarp();
+        if (!quit && !__all_sync(FULL, bar_wait(b, parity, a.polls, &s_gave_up))) quit = true;
       };
       auto slot_wait = [&](int op) {
         wait(&b_full[op % PR_SLOTS], (op / PR_SLOTS) & 1);
@@ -304,7 +308,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       };
       auto scores = [&](int w, int op) {
         const u64 qa = operand_desc(smem_q + w * TB, 0), kb = operand_desc(smem_kv + (op % PR_SLOTS) * TB, 0);
-        if (elected()) {
+        if (!quit && elected()) {
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {  // 16 elements: 32 bytes further in a row, or the next 64-element half
             const u64 off = (u64)(((k >> 2) * (PR_KEYS * 128) + (k & 3) * 32) >> 4);
@@ -316,7 +320,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       };
       auto values = [&](int w, int op, int half, bool add) {
         const u64 vb = operand_desc(smem_kv + (op % PR_SLOTS) * TB, PR_KEYS * 128);
-        if (elected()) {
+        if (!quit && elected()) {
 #pragma unroll
           for (int i = 0; i < PR_KEYS / 32; ++i) {   // 16 keys: 16 rows of 128 bytes; 8 columns of P
             const int k = half * (PR_KEYS / 32) + i;
@@ -326,7 +330,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
         __syncwarp();
       };
       auto release = [&](int op) {
-        if (elected()) tc_commit(&b_empty[op % PR_SLOTS]);
+        if (!quit && elected()) tc_commit(&b_empty[op % PR_SLOTS]);
         __syncwarp();
       };
       for (int w = 0; w < 2; ++w)
@@ -341,7 +345,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       }
       // V of step j and K of step j + 1 have been waited for by the time they are needed: the waits sit where the other tile's weights
       // would be waited for anyway
-      for (int j = 0; j < n_steps && !__any_sync(FULL, *reinterpret_cast<volatile int*>(&s_gave_up)); ++j) {
+      for (int j = 0; j < n_steps && !quit && !__any_sync(FULL, *reinterpret_cast<volatile int*>(&s_gave_up)); ++j) {
         const int kop = 2 * (j + 1), vop = 2 * j + 1;
         if (j + 1 < n_steps) slot_wait(kop);
         for (int w = 0; w < 2; ++w) {
@@ -352,7 +356,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
             wait(&b_pb[w], j & 1);
             tc_fence_after();
             values(w, vop, 1, true);
-            if (j + 1 == steps[w]) { if (elected()) tc_commit(&b_o[w]); __syncwarp(); }
+            if (j + 1 == steps[w]) { if (!quit && elected()) tc_commit(&b_o[w]); __syncwarp(); }
           }
           if (w == 1) release(vop);
           if (j + 1 < steps[w]) scores(w, kop);
@@ -362,11 +366,10 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       }
       // everything issued has ended before tensor and shared memory are given back (q's loads too, where their wait ran out)
       for (int w = 0; w < 2; ++w)
-        if (steps[w] > 0)
-          for (u32 i = 0; i < PR_POLLS && !bar_try(&b_q[w], 0); ++i) {}
+        if (steps[w] > 0) bar_drain(&b_q[w], 0);
       if (elected()) tc_commit(&b_end);
       __syncwarp();
-      for (u32 i = 0; i < PR_POLLS && !bar_try(&b_end, 0); ++i) {}
+      bar_drain(&b_end, 0);
     }
     if (PACKED && warp == 13) {
       // ======== 4-bit tiles as they lie in the cache: lanes 0-7 a 16-token tile each, the table entries of the next step on their way
@@ -384,7 +387,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       int op = 0;
       for (; op < 2 * n_steps && !__any_sync(FULL, *reinterpret_cast<volatile int*>(&s_gave_up)); ++op) {
         const int j = op >> 1, key = key0 + j * PR_KEYS + lane * TILE;
-        if (op >= PR_RAW) bar_wait(&b_raw_free[op % PR_RAW], (op / PR_RAW - 1) & 1, &s_gave_up);
+        if (op >= PR_RAW && !__all_sync(FULL, bar_wait(&b_raw_free[op % PR_RAW], (op / PR_RAW - 1) & 1, a.polls, &s_gave_up))) break;
         __syncwarp();
         if (!(op & 1)) {
           const bool in = lane < TILES && key < keys, have = in && (u32)next_id < a.cache.num_blocks;
@@ -403,7 +406,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       }
       // whatever happened, what is in flight lands before the CTA gives its memory back
       for (int k = max(0, op - PR_RAW); k < op; ++k)
-        for (u32 i = 0; i < PR_POLLS && !bar_try(&b_raw[k % PR_RAW], (k / PR_RAW) & 1); ++i) {}
+        bar_drain(&b_raw[k % PR_RAW], (k / PR_RAW) & 1);
       if (bounds && a.status) atomicOr(a.status, PTSTORE_S_BOUNDS);
     }
     __syncwarp();
@@ -427,9 +430,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       if (PACKED) return base + (i64)((u64)h * (B / TILE) + in / TILE) * tile_bytes(D);
       return base + (i64)(((u64)in * a.cache.heads + h) * (D * 2));
     };
-    auto wait_empty = [&](int op) {
-      if (op >= PR_SLOTS) bar_wait(&b_empty[op % PR_SLOTS], ((op / PR_SLOTS) - 1) & 1, &s_gave_up);
-    };
+    auto wait_empty = [&](int op) { return op < PR_SLOTS || bar_wait(&b_empty[op % PR_SLOTS], ((op / PR_SLOTS) - 1) & 1, a.polls, &s_gave_up); };
     auto note_bad = [&](int d, int kind, int key) {
       atomicMin(&s_bad[kind][d], key);
       s_any_bad = 1;
@@ -478,11 +479,14 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
         const bool plain = box && key0 + (j + 1) * PR_KEYS <= all_see && (s_valid[j & 3][0] & s_valid[j & 3][1] & s_valid[j & 3][2] & s_valid[j & 3][3]) == FULL;
         for (int is_v = 0; is_v < 2; ++is_v) {
           const int op = 2 * j + is_v;
-          wait_empty(op);
+          const bool free = wait_empty(op);
+          // A slot that is not free gets no copy.  This thread arrives all the same, so that the operand's phase ends when the others' copies have landed,
+          // but not before the phase of the operand that lies there has ended (all its arrivals are in, its copies may be on their way).
+          if (!free) bar_drain(&b_full[op % PR_SLOTS], ((op / PR_SLOTS) - 1) & 1);
           const u32 dst = smem_kv + (op % PR_SLOTS) * TB;
           u64* full = &b_full[op % PR_SLOTS];
           if (plain) {
-            if (leads) {
+            if (leads && free) {
               bar_expect(full, box * D * 2);
 #pragma unroll
               for (int e = 0; e < D / 64; ++e)
@@ -492,7 +496,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
           }
           const unsigned char* base = a.cache.base + (is_v ? a.cache.kv_stride : 0) + c * 16;
 #pragma unroll 4
-          for (int i = 0; i < CPR; ++i) {
+          for (int i = 0; i < CPR && free; ++i) {
             const int n = i * RPP + r0;
             const i64 off = s_row[j & 1][n];
             cp_async16_or_zero(dst + operand_at(n, c), base + (off < 0 ? 0 : off), off >= 0);
@@ -500,7 +504,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
           if (box || (is_v && key0 + (j + 1) * PR_KEYS > all_see)) {
             cp_commit();
             cp_wait<0>();
-            if (is_v && key0 + (j + 1) * PR_KEYS > all_see) mend(op);
+            if (free && is_v && key0 + (j + 1) * PR_KEYS > all_see) mend(op);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             bar_arrive(full);
           } else cp_arrive(full);             // arrives when this thread's copies have landed
@@ -508,7 +512,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       }
       // whatever happened, what is in flight lands before the CTA gives its memory back
       for (int op = max(0, 2 * j - PR_SLOTS); op < 2 * j; ++op)
-        for (u32 i = 0; i < PR_POLLS && !bar_try(&b_full[op % PR_SLOTS], (op / PR_SLOTS) & 1); ++i) {}
+        bar_drain(&b_full[op % PR_SLOTS], (op / PR_SLOTS) & 1);
       cp_commit();
       cp_wait<0>();
     } else {
@@ -524,13 +528,13 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       const u32 scales = (pt / TILE) * tile_bytes(D);
       for (int op = 0; op < 2 * n_steps && !__any_sync(FULL, *gave_up); ++op) {
         const int j = op >> 1, key = key0 + j * PR_KEYS + pt;
-        bar_wait(&b_raw[op % PR_RAW], (op / PR_RAW) & 1, &s_gave_up);
+        if (!__all_sync(FULL, bar_wait(&b_raw[op % PR_RAW], (op / PR_RAW) & 1, a.polls, &s_gave_up))) break;
         const bool is_v = op & 1, has = (s_valid[j & 3][pt >> 5] >> (pt & 31)) & 1, look = is_v && has && key >= all_see;
         const unsigned char* const src = raw + (op % PR_RAW) * RAW;
         const unsigned char* const sc = src + scales + (is_v ? scale_at(D, true, n, 0) : scale_at(D, false, n, 0));
         const u32 stride = is_v ? TILE : 1;   // of a key's scales
         unsigned char* const t = smem + (2 + op % PR_SLOTS) * TB;
-        wait_empty(op);
+        if (!__all_sync(FULL, wait_empty(op))) break;
 #pragma unroll 2
         for (int c = 0; c < D / 32; ++c) {    // 32 elements: two scale groups, four chunks of the operand
           const uint4 four = has ? *reinterpret_cast<const uint4*>(src + (from ^ (u32)(c * 16))) : make_uint4(0, 0, 0, 0);
@@ -645,7 +649,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     const u32 ts = tmem + lane_base + w * 128, to = tmem + lane_base + 256 + w * 128;
     float m = -INFINITY, l = 0.0f;
     for (int j = 0; j < steps[w]; ++j) {
-      bar_wait(&b_s[w], j & 1, &s_gave_up);
+      bar_wait(&b_s[w], j & 1, a.polls, &s_gave_up);
       if (__any_sync(FULL, *reinterpret_cast<volatile int*>(&s_gave_up))) break;
       tc_fence_after();
       float s[4][32];
@@ -740,7 +744,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     }
     // ---- output
     if (steps[w] > 0) {
-      bar_wait(&b_o[w], 0, &s_gave_up);
+      bar_wait(&b_o[w], 0, a.polls, &s_gave_up);
       tc_fence_after();
     }
     if (!__any_sync(FULL, *reinterpret_cast<volatile int*>(&s_gave_up))) {

@@ -28,7 +28,6 @@ namespace ptk {
 
 constexpr int MIN_TOKENS = 256;              // a CTA takes at least this many, so that joining does not cost more than it saves
 constexpr int SP_PARTS_AT = 4096;            // where the parts begin in the workspace, behind the counters of the largest grid
-constexpr u32 SP_POLLS = 1u << 22;           // polls of a wait for a tile before the warp gives up (each may suspend for a while)
 
 template <int FMT, int D>
 struct SplitShape {
@@ -76,8 +75,9 @@ __device__ __forceinline__ void ldsm4_t(u32 (&r)[4], u32 addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
 }
 
-__device__ __forceinline__ bool bar_wait_or_give_up(u64* bar, u32 parity) {
-  for (u32 i = 0; i < SP_POLLS; ++i)
+__device__ __forceinline__ bool bar_wait_or_give_up(u64* bar, u32 parity, u32 polls) {
+  if (bar_test(bar, parity)) return true;
+  for (u32 i = 1; i < polls; ++i)
     if (bar_try(bar, parity)) return true;
   return false;
 }
@@ -343,9 +343,9 @@ __global__ void __launch_bounds__(SplitShape<FMT, D>::THREADS, split_ctas<FMT, N
     // The tile in stage s has landed.  After a wait that ran out no copy is issued any more; what is in flight is still waited for,
     // stage by stage, so that none lands after the CTA has ended.
     auto landed = [&](int s) {
-      if (__any_sync(FULL, !bar_wait_or_give_up(&s_bar[warp][s], (phases >> s) & 1))) {
+      if (__any_sync(FULL, !bar_wait_or_give_up(&s_bar[warp][s], (phases >> s) & 1, a.polls))) {
         gave_up = true;
-        bar_wait_or_give_up(&s_bar[warp][s], (phases >> s) & 1);
+        bar_wait_or_give_up(&s_bar[warp][s], (phases >> s) & 1, POLLS);
       }
       phases ^= 1u << s;
     };

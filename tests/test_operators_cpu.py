@@ -160,3 +160,12 @@ def test_reference_e4m3_against_torch():
     x = torch.cat([torch.linspace(0, 500, 20001, dtype=torch.float64), torch.linspace(0, 0.1, 20001, dtype=torch.float64)])
     want = x.clamp(max=448).float().to(torch.float8_e4m3fn).double()
     assert torch.equal(ref.e4m3_nearest(x.float().double()), want)
+
+
+def test_attend_takes_both_sizes_of_its_struct(G):
+    """A caller built without the fields behind `scale` passes the first size; any other size is refused."""
+    need = G.lib.ptstore_attend_workspace_bytes(128)
+    assert G.Attend.wait_polls.offset == 104 and C.sizeof(G.Attend) == 112
+    for size, want in ((104, OK), (112, OK), (0, E_INVAL), (100, E_INVAL), (108, E_INVAL), (120, E_INVAL)):
+        a = attend_args(G, size=size, R=0)
+        assert G.lib.ptstore_attend(C.byref(a), C.byref(cache(G)), A, need, None, None) == want, size

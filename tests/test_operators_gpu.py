@@ -811,3 +811,78 @@ def test_lengths_and_offsets_at_the_ends_of_their_range(G, fmt, dtype, new):
     out.fill_(5.0)
     G.attend(b["lay"], b["cache"], 0, b["q"], dev([low, 2 * new, 2 * new]), dev([48 + 2 * new, 0]), b["tables"], new, out=out)
     assert torch.equal(out[:new], want[:new])
+
+
+@pytest.mark.parametrize("polls", [1, 2, 5])
+@pytest.mark.parametrize("fmt,dtype,heads,block,lens,new", [
+    ("KV_PACKED", torch.bfloat16, 8, 16, [5000, 70, 3000, 900], [1, 1, 1, 1]),          # split kernel: its tiles are awaited long after they were asked for
+    ("KV_PACKED", torch.float16, 8, 32, [2000 + 11 * i for i in range(40)], [4] * 40),    # ... CTAs that go on to other items
+    ("KV_PACKED", torch.bfloat16, 8, 16, [4000, 300], [70, 300]),                        # 256-row tiles cut into chunks, 4-bit
+    ("KV_PACKED", torch.float16, 8, 16, [300 + i for i in range(90)], [250] * 90),        # ... uncut
+    ("KV_BF16", torch.bfloat16, 8, 16, [4000, 300], [70, 300]),                          # 16-bit through tensor maps
+    ("KV_FP16", torch.float16, 8, 32, [300 + i for i in range(90)], [250] * 90),
+    ("KV_BF16", torch.bfloat16, 6, 24, [2000, 300], [70, 300]),                          # 16-byte copies, a group that does not divide 128
+    ("KV_FP16", torch.float16, 6, 24, [300 + i for i in range(90)], [250] * 90)])
+def test_a_wait_that_runs_out_is_reported_and_leaves_the_workspace_ready(G, fmt, dtype, heads, block, lens, new, polls):
+    """Limits of a few polls on a healthy GPU: a wait that runs out raises S_TIMEOUT and the call returns; without one the answers are right.  The same
+    workspace then serves calls with the usual limit."""
+    b = make(G, getattr(G, fmt), dtype, heads, 2, 128, block, lens, new, seed=61)
+    ws = G.attend_workspace(b["lay"])
+    call(G, b, workspace=ws)
+    if max(new) < 200:
+        check(G, b)
+    want = b["out"].clone()
+    seen, big = 0, torch.empty(256 << 20, dtype=torch.uint8, device="cuda")
+    for _ in range(8):
+        status = dev([0])
+        b["out"].fill_(5.0)
+        big.fill_(1)                                              # the cache comes from memory, not from L2
+        G.attend(b["lay"], b["cache"], 0, b["q"], dev(b["offsets"]), dev(lens), b["tables"], max(new), out=b["out"], workspace=ws, status=status, wait_polls=polls)
+        assert int(status.item()) in (0, G.S_TIMEOUT)
+        if int(status.item()):
+            seen += 1
+        else:
+            assert torch.equal(b["out"], want)
+        assert bool((b["out"][b["offsets"][-1]:] == 5.0).all()) and not bool(ws[:2560].any())
+    if polls == 1 and max(new) > 4:                               # the first wait follows its copy at once
+        assert seen > 0
+    status = dev([0])
+    b["out"].fill_(5.0)
+    call(G, b, workspace=ws, status=status)
+    assert torch.equal(b["out"], want) and int(status.item()) == 0
+
+
+@pytest.mark.parametrize("dtype,new,dim", [(torch.bfloat16, 1, 128), (torch.float16, 4, 128), (torch.bfloat16, 1, 64)])
+def test_a_wait_of_the_split_kernel_that_runs_out(G, dtype, new, dim):
+    """As above where tiles come late: every SM asks for its first tiles at once, while another stream copies at the memory's full rate."""
+    lens = [6000 + 37 * (i % 5) for i in range(64)]
+    b = make(G, G.KV_PACKED, dtype, 8, 2, dim, 16, lens, [new] * 64, seed=62)
+    ws = G.attend_workspace(b["lay"])
+    call(G, b, workspace=ws)
+    check(G, b)
+    want = b["out"].clone()
+    src, dst, side, seen = (*torch.zeros(2, 1 << 30, dtype=torch.uint8, device="cuda"), torch.cuda.Stream(), 0)
+    offsets, lengths = dev(b["offsets"]), dev(lens)
+    for _ in range(6):
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            for _ in range(10):
+                dst.copy_(src)
+        for _ in range(5):
+            status = dev([0])
+            b["out"].fill_(5.0)
+            G.attend(b["lay"], b["cache"], 0, b["q"], offsets, lengths, b["tables"], new, out=b["out"], workspace=ws, status=status, wait_polls=1)
+            assert int(status.item()) in (0, G.S_TIMEOUT)
+            if int(status.item()):
+                seen += 1
+            else:
+                assert torch.equal(b["out"], want)
+            assert bool((b["out"][b["offsets"][-1]:] == 5.0).all()) and not bool(ws[:2560].any())
+    torch.cuda.current_stream().wait_stream(side)
+    print("ran out in %d of 30 calls" % seen)
+    if dim == 128:                                                # of head size 64 twice as many tiles are asked for ahead
+        assert seen > 0
+    status = dev([0])
+    b["out"].fill_(5.0)
+    call(G, b, workspace=ws, status=status)
+    assert torch.equal(b["out"], want) and int(status.item()) == 0
