@@ -594,7 +594,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
 #pragma unroll
       for (int i = 0; i < CPR; ++i) {
         raw[i] = make_uint4(0, 0, 0, 0);
-        if (w * 128 + i * RPP + t / CPR < rows) raw[i] = __ldg(reinterpret_cast<const uint4*>(q0 + 2 * (fr * a.q_token + hq * a.q_head)));
+        if (w * 128 + i * RPP + t / CPR < rows) raw[i] = *reinterpret_cast<const uint4*>(q0 + 2 * (fr * a.q_token + hq * a.q_head));       // (out may be q)
         hq += step_hq;
         fr += step_fr;
         if (hq >= group) { hq -= group; ++fr; }

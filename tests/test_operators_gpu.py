@@ -886,3 +886,24 @@ def test_a_wait_of_the_split_kernel_that_runs_out(G, dtype, new, dim):
     b["out"].fill_(5.0)
     call(G, b, workspace=ws, status=status)
     assert torch.equal(b["out"], want) and int(status.item()) == 0
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("heads", [8, 6])
+@pytest.mark.parametrize("new,many", [(1, 3), (1, 60), (3, 3), (3, 60), (40, 3), (40, 400), (300, 3), (300, 100)])
+def test_every_kernel_writes_over_its_q(G, fmt, dtype, heads, new, many):
+    """out is q itself: one token, a few, whole row tiles; items and steps that are cut and joined, and ones that are not; groups that divide a row
+    tile and that do not."""
+    rng = random.Random(new + many)
+    lens = [new + (rng.randint(0, 2000) if many == 3 else rng.randint(0, 60)) for _ in range(many)]
+    b = make(G, getattr(G, fmt), dtype, heads, 2, 64, 16, lens, [new] * many, seed=71, tail_rows=2)
+    q = b["q"].clone()
+    call(G, b)
+    if new * many < 2000:
+        check(G, b)
+    want = b["out"].clone()
+    want[-2:] = q[-2:]
+    for _ in range(2):
+        b["q"].copy_(q)
+        call(G, b, out=b["q"])
+        assert torch.equal(b["q"], want)
