@@ -508,7 +508,7 @@ int ptstore_kv_read(const ptstore_kv_cache_t* cache /*host struct*/, const int64
  *   out[i, hq] = sum_j softmax_j(scale * q[i, hq] . k[j, hq / group]) * v[j, hq / group],  group = num_heads / num_kv_heads,
  * over the tokens j of the row's request with j <= pos, pos = lengths[r] - token_offsets[r + 1] + i.  (Rows that the offsets put behind `tokens`
  * do not exist; the positions of a request's other rows are what they would be beside them.)
- * A row that sees nothing (pos < 0, or no valid block) is zero; rows that belong to no request are left as they were.  Tokens whose table
+ * A row that sees nothing (pos < 0, or no valid block) is zero, one whose scores are all minus infinity NaN; rows that belong to no request are left as they were.  Tokens whose table
  * entry is outside the cache, or beyond the row of the table, are not seen (S_BOUNDS for the former).  What the cache holds
  * behind a row's position has no influence, infinities and NaN included.
  * Products take 16-bit operands (the cache's type; fp16 for PACKED) and add in 32 bits; maxima, sums and outputs up to the last rounding

@@ -45,6 +45,18 @@ __device__ __forceinline__ Req request(const Attend& a, int r) {
   return q;
 }
 
+// What a row's sums are multiplied by.  Weights that add up to nothing: a row that sees no key is zero, one whose scores are all minus infinity has no
+// softmax (NaN).  pos: the row's position.
+__device__ __forceinline__ float row_factor(const Attend& a, int r, i64 pos, float sum) {
+  if (sum != 0.0f) return a.v_factor / sum;
+  const Req q = request(a, r);                // (read again: kept from the start it would cost the kernels registers)
+  const int last = pos < q.keys ? (int)pos : q.keys - 1;
+  if (last >= 0)
+    for (u32 b = 0; b <= (u32)last / a.cache.block_tokens; ++b)
+      if ((u32)a.tables[(i64)r * a.max_blocks + b] < a.cache.num_blocks) return NAN;
+  return 0.0f;
+}
+
 __device__ __forceinline__ u32 smem_addr(const void* p) { return (u32)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void cp_async16(u32 dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");

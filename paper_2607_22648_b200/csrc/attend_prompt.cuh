@@ -806,6 +806,20 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
         const i64 to = __shfl_sync(FULL, at, n);
         if (to >= 0) *reinterpret_cast<uint4*>(a.out + 2 * (to + c * 8)) = *reinterpret_cast<const uint4*>(mine + operand_at((warp & 3) * 32 + n, c));
       }
+      // A row without weights, written as zeros, may be one whose scores are all minus infinity.  (Looked at here: chosen together with f it costs the
+      // 4-bit kernel registers, and suffixes 2 to 6 %.)
+      if (__any_sync(FULL, f == 0.0f && at >= 0)) {
+        __syncwarp();
+        if (f == 0.0f && at >= 0) {
+          const int req = *reinterpret_cast<volatile int*>(&s_r), first = *reinterpret_cast<volatile int*>(&s_tile) * PR_ROWS;
+          const float nan = row_factor(a, req, (i64)request(a, req).pos0 + (first + row) / a.group, 0.0f);
+          if (nan != 0.0f)
+            for (int c = 0; c < D; c += 8) {
+              const u32 two = pack2<QFP16>(nan, nan);
+              *reinterpret_cast<uint4*>(a.out + 2 * (at + c)) = make_uint4(two, two, two, two);
+            }
+        }
+      }
     }
   }
   tc_fence_before();
@@ -817,9 +831,9 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
 }
 
 // Joins the chunks of the row tiles that were cut: blockIdx.x the tile (behind the uncut ones), blockIdx.y some of its rows, a warp
-// for K, whose loads are in flight together (K = 1 spreads few tiles over more warps).
+// for K, whose loads are in flight together (K = 1 spreads few tiles over more warps).  Four CTAs an SM: the largest grid, 74 x 8, is one round.
 template <bool QFP16, int D, int K>
-__global__ void __launch_bounds__(256) attend_join_kernel(const Attend a) {
+__global__ void __launch_bounds__(256, 4) attend_join_kernel(const Attend a) {
   __shared__ i64 s_scan[8];
   __shared__ int s_r, s_tile;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -878,16 +892,26 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const Attend a) {
       }
     }
   }
+  u32 none = 0;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) sum[k] += __shfl_xor_sync(FULL, sum[k], o);
     if (at0 + k >= rows) continue;
-    const float f = sum[k] == 0.0f ? 0.0f : a.v_factor / sum[k];
     const u32 flat = row_base + at0 + k, fr = flat / (u32)a.group;
+    const float f = sum[k] == 0.0f ? 0.0f : a.v_factor / sum[k];
+    if (sum[k] == 0.0f) none |= 1u << k;
     u32* const dst = reinterpret_cast<u32*>(a.out + 2 * ((i64)(q.row0 + (int)fr) * a.o_token + (i64)(h * a.group + (int)(flat - fr * a.group)) * a.o_head + lane * E));
 #pragma unroll
     for (int e = 0; e < E; e += 2) dst[e / 2] = pack2<QFP16>(acc[k][e] * f, acc[k][e + 1] * f);
+  }
+  // rows without weights, written as zeros: as in the other kernel
+  for (; none; none &= none - 1) {
+    const int row = at0 + __ffs(none) - 1;
+    const u32 flat = row_base + row, fr = flat / (u32)a.group;
+    const float nan = row_factor(a, s_r, (i64)q.pos0 + fr, 0.0f);
+    u32* const dst = reinterpret_cast<u32*>(a.out + 2 * ((i64)(q.row0 + (int)fr) * a.o_token + (i64)(h * a.group + (int)(flat - fr * a.group)) * a.o_head + lane * E));
+    for (int e = 0; e < E && nan != 0.0f; e += 2) dst[e / 2] = pack2<QFP16>(nan, nan);
   }
 }
 

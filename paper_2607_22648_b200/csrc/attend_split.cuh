@@ -781,7 +781,7 @@ __global__ void __launch_bounds__(SplitShape<FMT, D>::THREADS, split_ctas<FMT, N
             o4.z += v.z * f;
             o4.w += v.w * f;
           }
-          const float f = all == 0.0f ? 0.0f : a.v_factor / all;
+          const float f = row_factor(a, r, (i64)rq.pos0 + (row_base + rw) / a.group, all);
           const int fr = (row_base + rw) / a.group, hq = h * a.group + (row_base + rw) % a.group;
           *reinterpret_cast<uint2*>(a.out + 2 * ((i64)(rq.row0 + fr) * a.o_token + (i64)hq * a.o_head + e)) =
               make_uint2(pack2<QFP16>(o4.x * f, o4.y * f), pack2<QFP16>(o4.z * f, o4.w * f));
@@ -789,7 +789,7 @@ __global__ void __launch_bounds__(SplitShape<FMT, D>::THREADS, split_ctas<FMT, N
       }
     }
     if (write && row < rows) {
-      const float f = sum == 0.0f ? 0.0f : a.v_factor / sum;               // a row that sees nothing is zero
+      const float f = row_factor(a, r, (i64)rq.pos0 + (row_base + row) / a.group, sum);
       const int fr = (row_base + row) / a.group, hq = h * a.group + (row_base + row) % a.group;
       unsigned char* dst = a.out + 2 * ((i64)(rq.row0 + fr) * a.o_token + (i64)hq * a.o_head + e0);
       __align__(16) u32 v[E / 2];

@@ -907,3 +907,36 @@ def test_every_kernel_writes_over_its_q(G, fmt, dtype, heads, new, many):
         b["q"].copy_(q)
         call(G, b, out=b["q"])
         assert torch.equal(b["q"], want)
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("lens,new", [([1, 40, 900], [1, 1, 1]), ([5000], [1]), ([3, 70, 2000], [3, 3, 3]), ([40, 3000], [40, 40]), ([200 + i for i in range(160)], [200] * 160)])
+def test_scores_that_are_all_minus_infinity(G, fmt, dtype, lens, new):
+    """A row that sees keys, all of them with a score of minus infinity, has no softmax: NaN, and only it.  A row that sees nothing is zero all the same."""
+    b = make(G, getattr(G, fmt), dtype, 8, 2, 64, 16, lens + [5], new + [9], seed=81)
+    slots = torch.tensor([int(b["tables"][r, p // 16]) * 16 + p % 16 for r, n in enumerate(lens + [5]) for p in range(n)], device="cuda") if len(lens) < 9 else None
+    if slots is None:                                              # many: the same by whole rows of the table
+        t = b["tables"].long()
+        tok = torch.arange(t.shape[1] * 16, device="cuda")
+        at = t[:, tok // 16] * 16 + tok % 16
+        slots = at[tok[None, :] < dev(lens + [5])[:, None]]
+    k = rows(gen_of(82), (len(slots), 2, 64), dtype).abs() + 0.5
+    v = rows(gen_of(83), (len(slots), 2, 64), dtype, 0.25)
+    G.kv_write(b["lay"], b["cache"], 0, k, v, slots)
+    call(G, b)
+    clean = b["out"].clone()
+    assert bool(torch.isfinite(clean).all())
+    odd = [(0, 0), (b["offsets"][1] - 1, 5), (b["offsets"][len(lens)] - 1, 7), (b["offsets"][len(lens)], 3)]
+    for i, h in odd:
+        b["q"][i, h] = float("-inf")
+    b["out"].fill_(5.0)
+    call(G, b)
+    for i, h in odd[:3]:
+        assert bool(b["out"][i, h].isnan().all()), (i, h)
+        b["out"][i, h] = clean[i, h]
+    assert torch.equal(b["out"], clean)
+    assert not bool(b["out"][b["offsets"][len(lens)]:b["offsets"][len(lens)] + 4].any())      # nine rows over five keys: four see nothing
+    b["tables"][:] = -1                                            # blocks that are not there are not seen
+    b["out"].fill_(5.0)
+    call(G, b)
+    assert not bool(b["out"][:b["offsets"][-1]].any())
