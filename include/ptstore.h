@@ -529,7 +529,7 @@ typedef struct ptstore_attend {
   int32_t  requests, max_blocks, num_heads;
   int32_t  tokens;               /* rows of q and out */
   int32_t  max_new;              /* at least the rows of any request: chooses the kernel (host) */
-  float    scale;                /* of the scores, usually 1 / sqrt(head_dim) */
+  float    scale;                /* of the scores, usually 1 / sqrt(head_dim); scale * log2 e (* 2^8 * k_scale of a PACKED cache) has to be finite */
   uint32_t wait_polls;           /* polls of a wait for loads and products before a CTA gives up, 0: the built-in limit.  For failure-detection tests: a
                                     limit of 1 is a single test that never suspends.  What is in flight then is awaited with the built-in limit. */
   uint32_t reserved;             /* 0 */

@@ -155,7 +155,9 @@ extern "C" int ptstore_attend(const ptstore_attend_t* p, const ptstore_kv_cache_
   if (p->num_heads % (int)cache->num_kv_heads || p->num_heads > 65535) return PTSTORE_E_INVAL;
   if (p->dtype != PTSTORE_KV_BF16 && p->dtype != PTSTORE_KV_FP16) return PTSTORE_E_INVAL;
   if (cache->format != PTSTORE_KV_PACKED && cache->format != p->dtype) return PTSTORE_E_INVAL;
-  if (!isfinite(p->scale)) return PTSTORE_E_INVAL;
+  const bool packed = cache->format == PTSTORE_KV_PACKED;
+  const float scale2 = p->scale * LOG2E * (packed ? cache->k_scale * DEQ_FACTOR : 1.0f);
+  if (!isfinite(scale2)) return PTSTORE_E_INVAL;             // a score of zero times it would be NaN
   if (p->requests == 0 || p->tokens == 0 || p->max_new == 0) return PTSTORE_OK;
   if (!p->q || !p->out || !p->token_offsets || !p->lengths || !p->block_tables) return PTSTORE_E_INVAL;
   if (!rows_aligned(p->q, p->tokens, p->q_token_stride, p->num_heads, p->q_head_stride) ||
@@ -164,7 +166,6 @@ extern "C" int ptstore_attend(const ptstore_attend_t* p, const ptstore_kv_cache_
   if (p->requests > 1 << 20 || (i64)p->tokens * p->num_heads > 0x7FFFFFFF) return PTSTORE_E_LIMIT;     // row indexes of a kv head are 32 bits wide
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PTSTORE_E_INVAL;
   if (workspace_bytes < ptstore_attend_workspace_bytes(cache->head_dim)) return PTSTORE_E_NOMEM;
-  const bool packed = cache->format == PTSTORE_KV_PACKED;
   Attend a;
   a.cache = cache_of(cache);
   a.q = static_cast<const unsigned char*>(p->q);
@@ -174,7 +175,7 @@ extern "C" int ptstore_attend(const ptstore_attend_t* p, const ptstore_kv_cache_
   a.offsets = p->token_offsets; a.lengths = p->lengths; a.tables = p->block_tables;
   a.R = p->requests; a.max_blocks = p->max_blocks; a.heads = p->num_heads; a.tokens = p->tokens;
   a.group = p->num_heads / (int)cache->num_kv_heads;
-  a.scale2 = p->scale * LOG2E * (packed ? cache->k_scale * DEQ_FACTOR : 1.0f);
+  a.scale2 = scale2;
   a.v_factor = packed ? cache->v_scale * DEQ_FACTOR : 1.0f;
   a.work = static_cast<unsigned char*>(workspace);
   a.polls = polls ? polls : POLLS;

@@ -169,3 +169,17 @@ def test_attend_takes_both_sizes_of_its_struct(G):
     for size, want in ((104, OK), (112, OK), (0, E_INVAL), (100, E_INVAL), (108, E_INVAL), (120, E_INVAL)):
         a = attend_args(G, size=size, R=0)
         assert G.lib.ptstore_attend(C.byref(a), C.byref(cache(G)), A, need, None, None) == want, size
+
+
+def test_attend_refuses_a_scale_that_overflows_with_the_tensor_scale(G):
+    """Scores are multiplied by scale * log2 e (and K's tensor scale and the 4-bit values' factor of 2^8): that has to be finite too."""
+    need = G.lib.ptstore_attend_workspace_bytes(128)
+
+    def call(c, **kw):
+        return G.lib.ptstore_attend(C.byref(attend_args(G, **kw)), C.byref(c), A, need, None, None)
+    plain = dict(fmt=G.KV_BF16, bs=32768, kv=327680)
+    for scale in (3e38, -3e38):
+        assert call(cache(G, **plain), scale=scale) == E_INVAL
+        assert call(cache(G, ks=2.0 ** 20), scale=scale / 2.0 ** 24) == E_INVAL
+    assert call(cache(G, ks=2.0 ** 64), scale=2.0 ** 56) == E_INVAL
+    assert call(cache(G, ks=2.0 ** 64), scale=0.1, R=0) == OK and call(cache(G, **plain), scale=3e38, R=0) == E_INVAL
