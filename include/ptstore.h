@@ -519,7 +519,7 @@ int ptstore_kv_read(const ptstore_kv_cache_t* cache /*host struct*/, const int64
 typedef struct ptstore_attend {
   uint32_t struct_size;          /* sizeof(ptstore_attend_t); PTSTORE_ATTEND_SIZE_1 without the fields behind `scale` */
   uint32_t dtype;                /* of q and out: PTSTORE_KV_BF16 or PTSTORE_KV_FP16; a 16-bit cache has the same */
-  const void* q;                 /* [tokens][num_heads][head_dim], strides in elements (multiples of 8), 16-byte aligned */
+  const void* q;                 /* device, [tokens][num_heads][head_dim], strides in elements (multiples of 8), 16-byte aligned */
   int64_t  q_token_stride, q_head_stride;
   void*    out;                  /* likewise; may be q itself */
   int64_t  out_token_stride, out_head_stride;

@@ -231,6 +231,12 @@ def _elsewhere(t, what):
         raise ValueError("%s: needs device or pinned memory" % what)
 
 
+def _on_device(t, dev, what):
+    """What kernels fetch by bulk copies and tensor maps lies in device memory."""
+    if t.get_device() != dev:
+        raise ValueError("%s: needs memory of the current device" % what)
+
+
 def _rows(t, heads, dim, n, dtype, dev, what):
     """[n][heads][dim] rows of 16-bit elements, any token and head strides; returns the address."""
     if t.dtype is not dtype or t.shape != (n, heads, dim) or t.stride(2) != 1:
@@ -376,13 +382,16 @@ def attend(layout, cache, layer, q, token_offsets, lengths, block_tables, max_ne
         workspace = attend_workspace(layout)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace: needs contiguous memory on the current device")
+    _on_device(q, dev, "q")
+    desc = layout.of(cache, layer, dev)
+    _on_device(cache.tensors[layer], dev, "cache")
     q_stride, o_stride = q.stride(), out.stride()
     args = _ATTEND.pack(_ATTEND_SIZE, code, _rows(q, heads, layout.dim, T, q.dtype, dev, "q"), q_stride[0], q_stride[1],
                         _rows(out, heads, layout.dim, T, q.dtype, dev, "out"), o_stride[0], o_stride[1],
                         _vec(token_offsets, i32, R + 1, dev, "token_offsets"), _vec(lengths, i32, R, dev, "lengths"),
                         _table(block_tables, R, dev, "block_tables"), R, block_tables.shape[1], heads, T, max_new,
                         layout.dim ** -0.5 if scale is None else scale, wait_polls, 0)
-    _check(lib.ptstore_attend(args, layout.of(cache, layer, dev), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+    _check(lib.ptstore_attend(args, desc, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                               None if status is None else _vec(status, i32, 1, dev, "status"), _raw_stream(dev)), "ptstore_attend")
     return out
 

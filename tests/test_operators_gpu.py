@@ -940,3 +940,23 @@ def test_scores_that_are_all_minus_infinity(G, fmt, dtype, lens, new):
     b["out"].fill_(5.0)
     call(G, b)
     assert not bool(b["out"][:b["offsets"][-1]].any())
+
+
+def test_attend_refuses_pinned_q_and_cache(G):
+    """Both are fetched by bulk copies, which serve device memory; what is read by plain loads may be pinned."""
+    for fmt, dtype in FORMATS[1:3]:
+        b = make(G, getattr(G, fmt), dtype, 8, 2, 64, 16, [50, 70], [20, 1], seed=91)
+        q, c = b["q"], b["cache"]
+        for new in (1, 20):
+            b["q"] = torch.empty(q.shape, dtype=q.dtype, pin_memory=True).copy_(q)
+            with pytest.raises(ValueError):
+                call(G, b, max_new=new)
+            b["q"] = q
+            b["cache"] = G.PagedKV(1, c.num_blocks, c.tensors[0].shape[2], tensors=[torch.empty(c.tensors[0].shape, dtype=torch.uint8, pin_memory=True)])
+            with pytest.raises(ValueError):
+                call(G, b, max_new=new)
+            b["cache"] = c
+        lens, offsets = (torch.tensor(x, dtype=torch.int32).pin_memory() for x in (b["lens"], b["offsets"]))
+        tables = torch.empty(b["tables"].shape, dtype=torch.int32, pin_memory=True).copy_(b["tables"])
+        G.attend(b["lay"], c, 0, q, offsets, lens, tables, 20, out=b["out"])
+        check(G, b)
