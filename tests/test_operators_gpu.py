@@ -960,3 +960,53 @@ def test_attend_refuses_pinned_q_and_cache(G):
         tables = torch.empty(b["tables"].shape, dtype=torch.int32, pin_memory=True).copy_(b["tables"])
         G.attend(b["lay"], c, 0, q, offsets, lens, tables, 20, out=b["out"])
         check(G, b)
+
+
+def check_some_rows(G, b, got, picks):
+    """picks: (request, row of it).  Each is compared with a request of its own: one new token behind its position."""
+    lay = b["lay"]
+    every = torch.arange(b["cache"].tensors[0].shape[1] * lay.block_tokens, device="cuda")
+    kv = G.kv_read(lay, b["cache"], 0, every, b["q"].dtype)
+    values = [x.double().view(-1, lay.block_tokens, lay.heads, lay.dim) for x in kv]
+    at = [b["offsets"][r] + i for r, i in picks]
+    lens = [b["lens"][r] - b["new"][r] + i + 1 for r, i in picks]
+    q, tables = b["q"][at], b["tables"][[r for r, _ in picks]]
+    s = lay.dim ** -0.5
+    want, spread, scores, _ = ref.attend(q, list(range(len(at) + 1)), lens, tables, values[0], values[1], lay.block_tokens, s)
+    v_max, k_sum = float(values[1].nan_to_num(0).abs().max()), float(values[0].nan_to_num(0).abs().sum(-1).max()) * s
+    tol = ref.attend_tolerance(q, want, spread, scores, max(lens), v_max, lay.format == G.KV_PACKED, k_sum)
+    err = (got[at].double() - want).abs()
+    assert bool((err <= tol).all()), "worst %.3g of the tolerance" % float((err / tol).nan_to_num(1e9).max())
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("lens,new", [([4000, 900], [1, 1]), ([4000, 900], [3, 3]), ([4000], [60]), ([4000, 2500, 3100], [4000, 2500, 3100])])
+@pytest.mark.parametrize("growth", [0.02, 0.3])
+def test_scores_that_grow_along_the_sequence(G, fmt, dtype, dim, lens, new, growth):
+    """Every score is larger than the ones before: the running maximum moves from step to step, and what was added up so far is scaled down each time.
+    One token, a few, a suffix whose steps are cut, whole prompts whose row tiles are not cut."""
+    b = make(G, getattr(G, fmt), dtype, 8, 2, dim, 16, lens, new, seed=95, tail_rows=0)
+    gen, lay = gen_of(96), b["lay"]
+    u = torch.randn(dim, generator=gen, device="cuda").sign()
+    for r, n in enumerate(lens):
+        pos = torch.arange(n, device="cuda")
+        slots = b["tables"][r].long()[pos // 16] * 16 + pos % 16
+        k = (u * (growth * pos / dim ** 0.5)[:, None, None] + 0.1 * torch.randn(n, 2, dim, generator=gen, device="cuda")).to(dtype)
+        v = rows(gen, (n, 2, dim), dtype, 0.25)
+        G.kv_write(lay, b["cache"], 0, k, v, slots)
+    b["q"].copy_((u + 0.1 * torch.randn(b["q"].shape, generator=gen, device="cuda")).to(dtype))
+    got = call(G, b)
+    picks = [(r, i) for r, m in enumerate(new) for i in sorted({0, m // 3, m // 2, max(0, m - 130), m - 1})]
+    check_some_rows(G, b, got, picks)
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+def test_row_tiles_over_many_keys_that_are_not_cut(G, fmt, dtype):
+    """Whole prompts of some thousand tokens, more row tiles than would be cut; rows at both ends and in the middle of their tiles."""
+    rng = random.Random(97)
+    lens = [3000, 2049, 5000]
+    b = make(G, getattr(G, fmt), dtype, 12, 2, 128, 16, lens, [3000, 2049, 4700], seed=97, tail_rows=0)
+    got = call(G, b)
+    picks = [(r, i) for r, m in enumerate(b["new"]) for i in (0, 42, 43, m // 2, m - 44, m - 1, rng.randrange(m), rng.randrange(m))]
+    check_some_rows(G, b, got, picks)
