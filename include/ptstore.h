@@ -510,7 +510,8 @@ int ptstore_kv_read(const ptstore_kv_cache_t* cache /*host struct*/, const int64
  * do not exist; the positions of a request's other rows are what they would be beside them.)
  * A row that sees nothing (pos < 0, or no valid block) is zero, one whose scores are all minus infinity NaN; rows that belong to no request are left as they were.  Tokens whose table
  * entry is outside the cache, or beyond the row of the table, are not seen (S_BOUNDS for the former).  What the cache holds
- * behind a row's position has no influence, infinities and NaN included.
+ * behind a row's position has no influence, infinities and NaN included.  An infinity of V that a row sees makes its column infinite, or NaN (in both
+ * signs, or where the key's weight rounds to zero).
  * Products take 16-bit operands (the cache's type; fp16 for PACKED) and add in 32 bits; maxima, sums and outputs up to the last rounding
  * are 32 bits wide; probabilities are rounded to 16 bits before they meet V.
  * The result of a call does not depend on timing: equal inputs give equal bits.  Every wait inside the kernels is bounded: S_TIMEOUT means that

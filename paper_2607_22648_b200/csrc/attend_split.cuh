@@ -18,8 +18,9 @@
 // whole tiles of a 4-bit cache, 16-byte copies of a 16-bit one, whose blocks may have any size), and meet at the end of an item.
 //
 // B200, 64 ragged requests of 2064 to 6256 tokens, 32 query and 8 kv heads x 128: 16-bit cache 173 us = 6.0 TB/s (bound by HBM); 4-bit cache 98 us
-// = 3.1 TB/s.  The latter is bound by instructions: 400 per 16 tokens and warp, of which 184 unpack codes (one LOP3 and one fused
-// multiply-add per pair), 0.6 a clock and scheduler at 16 warps an SM; two accumulator chains for S, one or four tiles per softmax step, 12 or
+// = 3.1 TB/s.  The latter waits for neither memory nor issue slots (48 % and 54 % busy) but for its own results: a warp's step is one chain of unpacking, products, a
+// maximum across lanes, exponentials, unpacking, products, and four warps share a scheduler.  It has 400 instructions per 16 tokens and warp, of which 184 unpack
+// codes (one LOP3 and one fused multiply-add per pair).  Two accumulator chains for S, one or four tiles per softmax step, 12 or
 // 20 warps an SM were each measured no better (99, 104, 161, 102, 152 us).
 #pragma once
 #include "attend.cuh"

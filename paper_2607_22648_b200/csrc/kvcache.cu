@@ -2,8 +2,9 @@
 //
 // Bound: HBM.  A 16-bit element costs 2 bytes on the model's side and 2 or 0.5625 in the cache, nothing is read twice.  One thread
 // takes 32 consecutive elements (two scale groups): four 16-byte loads, its own maxima, 16 bytes of codes and two scales, so there
-// is no exchange between threads (with 16 elements finding the row and the slot was half of 327 instructions, which is what bounds the
-// writer: 23.3 us for K and V of 16384 tokens of 8 x 128; with 32 it takes 20.1, the reader 19.0, their bytes 13.2).  What the quantiser computes is defined in exact terms (nearest code of x / (scale * tensor
+// is no exchange between threads (with 16 elements finding the row and the slot was half of 327 instructions: 23.3 us for K and V of 16384 tokens of
+// 8 x 128; with 32 the writer takes 20.1, the reader 19.0, their bytes 13.2.  Issue slots are 65 % busy, and scale bytes leave as parts of
+// sectors.  A 16-bit cache: writer 25.4 us, reader 24.4, bytes 20.5).  What the quantiser computes is defined in exact terms (nearest code of x / (scale * tensor
 // scale), ties to even); 32 bits give exactly that: x has at most 11 significant bits and the divisor 4, so a quotient that is not
 // on a rounding border is at least 2^-16 away from it, and one that is comes out exactly (the division below is corrected by its residual).
 #include "kvcache.cuh"

@@ -5,7 +5,8 @@
 // a few kilobytes to a few megabytes against a launch, two or three dependent memory round trips and a block-wide scan.  So
 // each is ONE launch in which every CTA scans all requests for itself (16,384 of them per step, up to 16 per thread, both
 // sums of an assignment in one value), and the entries that move are dealt out evenly and find their request by a binary
-// search in shared memory.  An assignment is one cluster of eight CTAs, because pops follow all pushes.  Time on a B200,
+// search in shared memory.  An assignment is one cluster of eight CTAs: its pops read ids that pushes of other CTAs have written,
+// and a cluster's barrier orders the two.  (A pop could find such an id in the tables itself; not done.)  Time on a B200,
 // assignment + slots: a decode step of 64 requests 4.5 + 2.8 us; 16,384 requests that push 53,000 blocks, pop 30,000 and list 476,000 tokens
 // 32 + 14 us, of which the assignment's scan takes a quarter and its searches in two to eight SMs most of the rest.
 #include <cuda_runtime.h>
