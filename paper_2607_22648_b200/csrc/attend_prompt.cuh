@@ -110,6 +110,12 @@ __device__ __forceinline__ void tc_st32(u32 addr, const u32 (&r)[32]) {
                  "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr) : "memory");
 }
 
+__device__ __forceinline__ void tc_st16(u32 addr, const u32 (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+               ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+                 "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr) : "memory");
+}
+
 // One lane of a converged warp, the same every time
 __device__ __forceinline__ bool elected() {
   u32 p;
@@ -413,7 +419,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     __syncwarp();
   } else if (warp >= 8) {
     // ======== K and V into the ring
-    regs_fewer<PACKED ? 104 : 72>();
+    regs_fewer<PACKED ? 88 : 72>();
     const int pt = tid - 256;
     const int* table = a.tables + (i64)r * a.max_blocks;
     const u32 B = a.cache.block_tokens;
@@ -569,7 +575,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     if (bounds && a.status) atomicOr(a.status, PTSTORE_S_BOUNDS);
   } else {
     // ======== softmax of tile w
-    regs_more<PACKED ? 184 : 200>();
+    regs_more<PACKED ? 192 : 200>();
     const int w = warp >> 2, t = tid & 127, row = w * 128 + t;
     // its half of Q.  Through a tensor map where the group divides a tile (rows behind the request's last bring someone's values or
     // zeros along and are not stored); else chunk t % CPR of rows t / CPR, ..., all on their way before the first is used, with the
@@ -649,6 +655,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
     const u32 lane_base = (u32)(32 * (warp & 3)) << 16;
     const u32 ts = tmem + lane_base + w * 128, to = tmem + lane_base + 256 + w * 128;
     float m = -INFINITY, l = 0.0f;
+    bool large = false;                       // a row's reference is beyond 2^24
     for (int j = 0; j < steps[w]; ++j) {
       bar_wait(&b_s[w], j & 1, a.polls, &s_gave_up);
       if (__any_sync(FULL, *reinterpret_cast<volatile int*>(&s_gave_up))) break;
@@ -717,6 +724,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       if (__any_sync(FULL, move) || j == 0) {
         const float f = move ? exp2_fast(m - top) : 1.0f;
         if (move) { m = top; l *= f; }
+        large = __any_sync(FULL, fabsf(m) > 0x1p24f && m != -INFINITY);
         if (j > 0) {
 #pragma unroll 1
           for (int c = 0; c < D; c += 32) {
@@ -731,6 +739,36 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
           }
         }
         weights(0, false, p);
+      }
+      // A reference is a rounded product.  Beyond 2^24 its rounding is a step in the exponent or more (a largest weight that is not near 1, or out of
+      // range): products are then rounded likewise before the reference is taken off.  Scores are read once more, 32 keys at a time, their weights go
+      // where scores that have been read lay.
+      if (large) {
+        const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          float v[32];
+          tc_ld32(v, ts + 32 * c);
+          tc_wait_ld();
+          tc_loaded(v);
+          const int left = (row < rows ? keys_of(row) : 0) - key0 - j * PR_KEYS - 32 * c;
+          const u32 mask = s_valid[j & 3][c] & (left >= 32 ? FULL : left <= 0 ? 0u : (1u << left) - 1u);
+          u32 q[16];
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const float e0 = (mask >> i) & 1 ? exp2_fast(__fmul_rn(v[i], scale2) - ref) : 0.0f;
+            const float e1 = (mask >> (i + 1)) & 1 ? exp2_fast(__fmul_rn(v[i + 1], scale2) - ref) : 0.0f;
+            l += e0 + e1;
+            q[i / 2] = pack2<F16>(e0, e1);
+          }
+          tc_st16(ts + 16 * c, q);
+          if (c & 1) {
+            tc_wait_st();
+            tc_fence_before();
+            bar_arrive(c == 1 ? &b_pa[w] : &b_pb[w]);
+          }
+        }
+        continue;
       }
       tc_st32(ts, p);
       tc_wait_st();

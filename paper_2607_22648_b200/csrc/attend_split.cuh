@@ -606,8 +606,8 @@ __global__ void __launch_bounds__(SplitShape<FMT, D>::THREADS, split_ctas<FMT, N
         for (int n = 0; n < NT; ++n) {
           float p[4];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            p[c] = exp2_fast(fmaf(sc[k][n][c], qs[n][c & 1], -ref[n][c & 1]));
+          for (int c = 0; c < 4; ++c) {       // the product rounded as the maximum is, so that the largest weight is 1 however large the scores are
+            p[c] = exp2_fast(__fmul_rn(sc[k][n][c], qs[n][c & 1]) - ref[n][c & 1]);
             l[n][c & 1] += p[c];
           }
           pb[n][0] = transpose8x8(pack2<F16>(p[0], p[1]));

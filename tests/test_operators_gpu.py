@@ -1010,3 +1010,35 @@ def test_row_tiles_over_many_keys_that_are_not_cut(G, fmt, dtype):
     got = call(G, b)
     picks = [(r, i) for r, m in enumerate(b["new"]) for i in (0, 42, 43, m // 2, m - 44, m - 1, rng.randrange(m), rng.randrange(m))]
     check_some_rows(G, b, got, picks)
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("lens,new", [([1, 40, 900], [1, 1, 1]), ([3000, 70], [3, 3]), ([40, 2000], [40, 40]), ([120 + i for i in range(100)], [100] * 100)])
+@pytest.mark.parametrize("scale", [1e6, 3e8, -1e10, 1e14, 1e30])
+def test_scores_larger_than_their_differences_can_be_resolved(G, fmt, dtype, lens, new, scale):
+    """Scores of up to 1e31 times log2 e: the largest one's weight is 1 and the others' are 0, wherever 32-bit sums can tell the two largest apart."""
+    b = make(G, getattr(G, fmt), dtype, 4, 2, 64, 16, lens, new, seed=99, tail_rows=0)
+    got = call(G, b, scale=scale)
+    told = 0
+    for r, (n, m) in enumerate(zip(lens, new)):
+        k, _ = ref.gather(b["values"][0], b["tables"][r], n, 16)
+        v, _ = ref.gather(b["values"][1], b["tables"][r], n, 16)
+        q = b["q"][b["offsets"][r]:b["offsets"][r + 1]].double()
+        s = torch.einsum("ihd,jhd->ihj", q, k.repeat_interleave(2, 1)) * (1 if scale > 0 else -1)
+        # a sum of 64 products is off by at most 64 steps of 2^-23 of the products' magnitudes, bf16 rows as fp16 by 2^-25 of the row's largest element each
+        off = 2.0 ** -16 * torch.einsum("ihd,jhd->ihj", q.abs(), k.abs().repeat_interleave(2, 1)).amax(2) + 2.0 ** -25 * 64 * q.abs().amax(2) * float(k.abs().max())
+        seen = torch.arange(n, device="cuda")[None, None, :] <= (n - m + torch.arange(m, device="cuda"))[:, None, None]
+        s = s.masked_fill(~seen, float("-inf"))
+        top = s.topk(min(2, n), dim=2)
+        gap = top.values[..., 0] - top.values[..., 1] if n > 1 else torch.full(s.shape[:2], float("inf"), dtype=torch.float64, device="cuda")
+        # beyond the sums' error the weights' exponents differ by more than any type's range
+        clear = gap > 2 * off + 2.0 ** -22 * top.values[..., 0].abs() + 400.0 / abs(scale)
+        want = v[top.indices[..., 0], torch.arange(4, device="cuda") // 2]
+        # The one weight is rounded to 16 bits before it meets V and is not before the sum: half a step of its type; then the result once: half a step
+        half = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+        tol = (half[torch.float16 if fmt == "KV_PACKED" else dtype] + half[dtype] + 2.0 ** -20) * want.abs() + 2.0 ** -25
+        err = (got[b["offsets"][r]:b["offsets"][r + 1]].double() - want).abs()
+        assert bool((err <= tol)[clear].all()), "request %d" % r
+        told += int(clear.sum())
+    assert told > 0.5 * 4 * sum(new)
+    assert bool(torch.isfinite(got).all())
