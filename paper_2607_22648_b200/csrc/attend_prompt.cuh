@@ -649,8 +649,8 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
       bar_arrive(&b_q[w]);
     }
     const u32 tmem = tmem_there();            // (and every row's factor is there)
-    // scale2 as a positive number: of zero, the smallest that keeps masked scores at minus infinity
-    const float scale2 = fmaxf(fabsf(a.scale2) * (PACKED && !QFP16 ? s_qf[row] : 1.0f), 0x1p-126f);
+    // scale2 as a positive number: of zero, the smallest that keeps masked scores at minus infinity; finite, so that scores of zero stay zero
+    const float scale2 = fminf(fmaxf(fabsf(a.scale2) * (PACKED && !QFP16 ? s_qf[row] : 1.0f), 0x1p-126f), 0x1.fffffep127f);
     const int see = row < rows ? keys_of(row) : 0;
     const u32 lane_base = (u32)(32 * (warp & 3)) << 16;
     const u32 ts = tmem + lane_base + w * 128, to = tmem + lane_base + 256 + w * 128;

@@ -399,8 +399,8 @@ __global__ void __launch_bounds__(SplitShape<FMT, D>::THREADS, split_ctas<FMT, N
         const u32 flip = a.scale2 < 0.0f ? 0x80008000u : 0;   // the sign of the softmax scale goes into q
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) *reinterpret_cast<u32*>(&s_q[row][e0 + 2 * i]) = raw[i] ^ flip;
-        // as a positive number: of zero, the smallest that keeps masked scores at minus infinity
-        if (e0 == 0) s_qf[row] = fmaxf(factor * fabsf(a.scale2), 0x1p-126f);
+        // as a positive number: of zero, the smallest that keeps masked scores at minus infinity; finite, so that scores of zero stay zero
+        if (e0 == 0) s_qf[row] = fminf(fmaxf(factor * fabsf(a.scale2), 0x1p-126f), 0x1.fffffep127f);
       }
     }
     __syncthreads();

@@ -1042,3 +1042,27 @@ def test_scores_larger_than_their_differences_can_be_resolved(G, fmt, dtype, len
         told += int(clear.sum())
     assert told > 0.5 * 4 * sum(new)
     assert bool(torch.isfinite(got).all())
+
+
+@pytest.mark.parametrize("lens,new", [([1, 40, 900], [1, 1, 1]), ([70, 40], [3, 3]), ([40, 2000], [40, 40]), ([30 + i for i in range(100)], [20] * 100)])
+def test_the_largest_queries_over_a_cache_of_zeros(G, lens, new):
+    """bf16 rows over a 4-bit cache are scaled by a power of two that goes into the softmax scale: of the largest rows the product passes the range of 32 bits,
+    and scores of zero are zero all the same.  Every row is the mean of the values it sees."""
+    b = make(G, G.KV_PACKED, torch.bfloat16, 8, 2, 64, 16, lens, new, seed=101, tail_rows=0)
+    b["lay"] = G.KVLayout(2, 64, 16, G.KV_PACKED, 2.0 ** 20, 2.0 ** -6)
+    t = b["tables"].long()
+    tok = torch.arange(t.shape[1] * 16, device="cuda")
+    slots = (t[:, tok // 16] * 16 + tok % 16)[tok[None, :] < dev(lens)[:, None]]
+    v = rows(gen_of(102), (len(slots), 2, 64), torch.bfloat16, 0.25)
+    G.kv_write(b["lay"], b["cache"], 0, torch.zeros_like(v), v, slots)
+    b["q"].fill_(3e38)
+    b["values"] = [x.double().view(-1, 16, 2, 64) for x in G.kv_read(b["lay"], b["cache"], 0, torch.arange(b["cache"].num_blocks * 16, device="cuda"), torch.bfloat16)]
+    got = call(G, b)
+    for r, n in enumerate(lens):
+        vs, _ = ref.gather(b["values"][1], b["tables"][r], n, 16)
+        for i in sorted({0, new[r] - 1}):
+            see = vs[:n - new[r] + i + 1].repeat_interleave(4, 1)
+            # every weight is 1, exactly; a sum of 32 bits and one rounding
+            tol = 2.0 ** -8 * see.mean(0).abs() + 2.0 ** -22 * n * see.abs().mean(0)
+            bad = ~((got[b["offsets"][r] + i].double() - see.mean(0)).abs() <= tol)
+            assert not bool(bad.any()), (r, i)
