@@ -447,6 +447,12 @@ int ptstore_fetch_static(const void* hbm_pool, uint32_t hbm_blocks, uint32_t num
 #define PTSTORE_KV_BF16    0u
 #define PTSTORE_KV_FP16    1u
 #define PTSTORE_KV_PACKED  2u
+/* LATENT_*: one row of latent_dim + 64 16-bit elements per token that all query heads share, the latent vector and then its rotary part
+ *   (ptstore_latent_attend): num_kv_heads 1, head_dim 320 or 576 (latent_dim 256 or 512), block_tokens a multiple of 8; kv_stride_bytes is
+ *   not used.  A layer has one chunk per block, so a store layer, which has two (K and V), holds two of a model's layers. */
+#define PTSTORE_KV_LATENT_BF16  4u
+#define PTSTORE_KV_LATENT_FP16  5u
+#define PTSTORE_LATENT_ROPE     64u
 
 typedef struct ptstore_kv_cache {
   void*    base;                 /* K of cache block 0 in this layer (device, 16-byte aligned) */
@@ -542,6 +548,147 @@ typedef struct ptstore_attend {
 uint64_t ptstore_attend_workspace_bytes(uint32_t head_dim);
 int ptstore_attend(const ptstore_attend_t* args /*host struct*/, const ptstore_kv_cache_t* cache /*host struct*/, void* workspace,
                    uint64_t workspace_bytes, uint32_t* status, ptstore_stream_t stream);
+
+/*
+ * ptstore_attend that also writes the logarithm of every row's sum, which ptstore_attend_weights starts from:
+ *   lse[i, hq] = ln sum_j exp(scale * q[i, hq] . k[j, hq / group]), minus infinity for a row that sees nothing.
+ *   lse  [tokens][num_heads] contiguous 32-bit floats, or NULL (then this is ptstore_attend); rows of no request are left as they were
+ */
+int ptstore_attend_lse(const ptstore_attend_t* args /*host struct*/, const ptstore_kv_cache_t* cache /*host struct*/, void* workspace,
+                       uint64_t workspace_bytes, float* lse, uint32_t* status, ptstore_stream_t stream);
+
+/* ---- attention with keys and values from one latent vector a token ---------------------------------------------------------------
+ * The cache (PTSTORE_KV_LATENT_*) holds a latent vector c_j and a rotary key r_j per token.  A model has two ways to attend over it.  Absorbed: its
+ * projections to keys and values are multiplied into q and into the output instead, and all heads attend over the rows as they lie
+ * (ptstore_latent_attend; single tokens, short suffixes).  Expanded: keys and values of every head are computed from the rows
+ * (ptstore_latent_read and a matrix product for tokens found in the store) and attended over with far fewer operations a pair of tokens
+ * (ptstore_expanded_attend; prompts).
+ */
+
+/*
+ * Latent rows into the cache / out of it.  Row i: head_dim - 64 contiguous elements of the cache's type at latent + i * latent_stride and 64 at
+ * rope + i * rope_stride (strides in elements, multiples of 8; pointers 16-byte aligned); slots as for ptstore_kv_write / _read.  Values are copied as they are.
+ */
+int ptstore_latent_write(const void* latent, int64_t latent_stride, const void* rope, int64_t rope_stride, int64_t tokens, const int64_t* slots,
+                         const ptstore_kv_cache_t* cache /*host struct*/, uint32_t* status, ptstore_stream_t stream);
+int ptstore_latent_read(const ptstore_kv_cache_t* cache /*host struct*/, const int64_t* slots, int64_t tokens, void* latent, int64_t latent_stride,
+                        void* rope, int64_t rope_stride, uint32_t* status, ptstore_stream_t stream);
+
+/*
+ * Causal attention of a batch's new tokens over the latent cache, which holds their own rows too (ptstore_latent_write comes first), absorbed form:
+ *   out[i, h] = sum_j softmax_j(scale * (q_latent[i, h] . c_j + q_rope[i, h] . r_j)) * c_j
+ * over the tokens that ptstore_attend's rows see, with its rules for positions, tables, rows that see nothing or belong to no request, and timing.
+ * What the cache holds behind a row's position has no influence.  An infinity or a NaN in the row of a token that is seen makes the output NaN, in that
+ * element's column at least.  q, out and the cache have the same type; sums, maxima and outputs up to the last rounding are 32 bits wide, probabilities
+ * are rounded to 16 bits before they meet c.
+ */
+typedef struct ptstore_latent_attend {
+  uint32_t struct_size;          /* sizeof(ptstore_latent_attend_t) */
+  uint32_t wait_polls;           /* as in ptstore_attend_t */
+  const void* q_latent;          /* device, [tokens][num_heads][head_dim - 64], strides in elements (multiples of 8), 16-byte aligned */
+  int64_t  q_latent_token_stride, q_latent_head_stride;
+  const void* q_rope;            /* [tokens][num_heads][64], likewise */
+  int64_t  q_rope_token_stride, q_rope_head_stride;
+  void*    out;                  /* [tokens][num_heads][head_dim - 64], likewise; may be q_latent itself if its strides are the same */
+  int64_t  out_token_stride, out_head_stride;
+  float*   lse;                  /* [tokens][num_heads] contiguous, or NULL: as in ptstore_attend_lse */
+  const int32_t* token_offsets;  /* [requests + 1] */
+  const int32_t* lengths;        /* [requests] */
+  const int32_t* block_tables;   /* [requests][max_blocks] */
+  int32_t  requests, max_blocks, num_heads, tokens;
+  int32_t  max_new;              /* at least the rows of any request */
+  float    scale;                /* finite with log2 e */
+} ptstore_latent_attend_t;
+
+/* Bytes of workspace (256-byte aligned device memory; its contents do not matter).  Calls that share a workspace must not overlap.  head_dim of the cache. */
+uint64_t ptstore_latent_workspace_bytes(uint32_t head_dim);
+int ptstore_latent_attend(const ptstore_latent_attend_t* args /*host struct*/, const ptstore_kv_cache_t* cache /*host struct*/, void* workspace,
+                          uint64_t workspace_bytes, uint32_t* status, ptstore_stream_t stream);
+
+/*
+ * Causal attention over expanded keys and values (no cache, no workspace): request r has rows token_offsets[r] .. token_offsets[r + 1] - 1 of q and out and
+ * keys key_offsets[r] .. key_offsets[r + 1] - 1 of k, k_rope and v, the last of which are its rows' own:
+ *   out[i, h] = sum_j softmax_j(scale * (q[i, h, :128] . k[j, h] + q[i, h, 128:] . k_rope[j])) * v[j, h]
+ * over the request's keys j with j <= pos, pos = keys - rows + i (within the request).  A row that sees nothing is zero; rows of no request are left as they
+ * were.  What lies behind a row's position, or in other requests' keys, has no influence.  An infinity of V that a row sees: as in ptstore_attend.  16-bit operands, 32-bit
+ * sums; probabilities are rounded to 16 bits before they meet v.
+ */
+typedef struct ptstore_expanded_attend {
+  uint32_t struct_size;          /* sizeof(ptstore_expanded_attend_t) */
+  uint32_t dtype;                /* PTSTORE_KV_BF16 or PTSTORE_KV_FP16, of q, k, k_rope, v and out */
+  const void* q;                 /* device, [tokens][heads][192], strides in elements (multiples of 8), 16-byte aligned */
+  int64_t  q_token_stride, q_head_stride;
+  const void* k;                 /* [keys][heads][128] */
+  int64_t  k_token_stride, k_head_stride;
+  const void* k_rope;            /* [keys][64] */
+  int64_t  k_rope_token_stride;
+  const void* v;                 /* [keys][heads][128] */
+  int64_t  v_token_stride, v_head_stride;
+  void*    out;                  /* [tokens][heads][128]; overlaps nothing else */
+  int64_t  out_token_stride, out_head_stride;
+  const int32_t* token_offsets;  /* [requests + 1] */
+  const int32_t* key_offsets;    /* [requests + 1] */
+  int32_t  requests, heads, tokens, keys;
+  int32_t  max_new;              /* at least the rows of any request */
+  float    scale;                /* finite with log2 e */
+  uint32_t wait_polls, reserved;
+} ptstore_expanded_attend_t;
+int ptstore_expanded_attend(const ptstore_expanded_attend_t* args /*host struct*/, uint32_t* status, ptstore_stream_t stream);
+
+/* ---- eviction of tokens by the attention they were given ---------------------------------------------------------------------------
+ * A program adds up what every cached token was given (ptstore_attend_weights behind the attention of its steps, or once behind a prompt for the prompt's last rows), and
+ * when a request's cache passes a limit keeps some tokens per kv head (ptstore_select_tokens), moves them together (ptstore_kv_compact) and goes on
+ * with the shorter length (ptstore_assign_blocks gives the blocks back).  Requests whose blocks are shared are compacted into other blocks.
+ */
+
+/*
+ * What the rows of q gave to the cached tokens:
+ *   weights[r, h, j] = (accumulate ? weights[r, h, j] : 0) + sum over the request's rows i and the query heads hq of kv head h of exp(scale * q[i, hq] . k[j, h] - lse[i, hq])
+ * over rows with j <= pos (as in ptstore_attend) and lse other than minus infinity.  Any cache format (LATENT: keys are whole rows, q is [tokens][num_heads][head_dim], the latent
+ * part and then the rotary part).  Entries from the request's length on: as they were, or zero without accumulate; so are tokens whose block is not there (S_BOUNDS
+ * where its id is outside the cache).  Tokens from `width` on are not counted.  Equal inputs give equal bits.
+ */
+typedef struct ptstore_attend_weights {
+  uint32_t struct_size;          /* sizeof(ptstore_attend_weights_t) */
+  uint32_t dtype;                /* of q: a 16-bit cache has the same */
+  const void* q;                 /* device, [tokens][num_heads][head_dim], strides in elements (multiples of 8), 16-byte aligned */
+  int64_t  q_token_stride, q_head_stride;
+  const float* lse;              /* [tokens][num_heads] contiguous */
+  const int32_t* token_offsets;  /* [requests + 1] */
+  const int32_t* lengths;        /* [requests] */
+  const int32_t* block_tables;   /* [requests][max_blocks] */
+  int32_t  requests, max_blocks, num_heads, tokens;
+  float*   weights;              /* [requests][num_kv_heads][width], the last axis contiguous */
+  int64_t  weights_request_stride, weights_head_stride;
+  int32_t  width;
+  uint32_t accumulate;           /* 0 or 1 */
+  float    scale;                /* the attention's */
+  uint32_t wait_polls;
+} ptstore_attend_weights_t;
+int ptstore_attend_weights(const ptstore_attend_weights_t* args /*host struct*/, const ptstore_kv_cache_t* cache /*host struct*/, uint32_t* status, ptstore_stream_t stream);
+
+/*
+ * The tokens to keep.  A request of at most `budget` tokens keeps all of them.  Of a longer one every head keeps its first `first` tokens, its last `recent`, and of those in
+ * between the budget - first - recent with the largest weights (equal weights: the lower index; a NaN is larger than any number).
+ *   weights     [R][heads][width], the last axis contiguous
+ *   kept        out [R][heads][budget] indexes of the kept tokens, ascending, -1 behind the last
+ *   lengths_out out [R] min(length, budget); not `lengths` itself
+ *   weights_out out [R][heads][width] the kept tokens' weights, zero behind them; may be weights itself (the same strides), otherwise overlaps nothing
+ * A length outside 0 .. width is clamped (S_BOUNDS).  first + recent <= budget <= width.
+ */
+int ptstore_select_tokens(const float* weights, int64_t weights_request_stride, int64_t weights_head_stride, const int32_t* lengths, int32_t R, int32_t heads,
+                          int32_t width, int32_t budget, int32_t first, int32_t recent, int32_t* kept, int32_t* lengths_out, float* weights_out,
+                          int64_t out_request_stride, int64_t out_head_stride, uint32_t* status, ptstore_stream_t stream);
+
+/*
+ * Moves kept tokens together in one layer of the cache: for i < lengths[r] (at most `width`) and every kv head h, K and V (or the latent row) of token kept[r, h, i] of row r of
+ * from_tables become those of token i of row r of to_tables.  Bytes are moved as they are.
+ *   kept  [R][num_kv_heads][width], as from ptstore_select_tokens; an index outside the row of from_tables is skipped, as is a table entry outside the cache (S_BOUNDS for both)
+ * to_tables is from_tables itself (the same pointer: moved in place; every list of kept tokens has to ascend, and no block may be in two rows) or names blocks that
+ * from_tables does not, each once.
+ */
+int ptstore_kv_compact(const ptstore_kv_cache_t* cache /*host struct*/, const int32_t* kept, const int32_t* lengths, int32_t R, int32_t width,
+                       const int32_t* from_tables, int32_t from_max_blocks, const int32_t* to_tables, int32_t to_max_blocks, uint32_t* status, ptstore_stream_t stream);
 
 /* Static text for a PTSTORE_E_* code. */
 const char* ptstore_strerror(int code);

@@ -57,7 +57,8 @@ class Stats(C.Structure):
                 ("blocks_demoted", C.c_uint64), ("far_keys", C.c_uint64), ("blocks_promoted", C.c_uint64), ("gdsf_clock", C.c_uint64), ("blocks_fetched_distinct", C.c_uint64)]
 
 
-KV_BF16, KV_FP16, KV_PACKED = 0, 1, 2
+KV_BF16, KV_FP16, KV_PACKED, KV_LATENT_BF16, KV_LATENT_FP16 = 0, 1, 2, 4, 5
+LATENT_ROPE = 64
 
 
 class KvCache(C.Structure):
@@ -73,12 +74,21 @@ class Attend(C.Structure):
                 ("tokens", C.c_int32), ("max_new", C.c_int32), ("scale", C.c_float), ("wait_polls", C.c_uint32), ("reserved", C.c_uint32)]
 
 
+class LatentAttend(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("wait_polls", C.c_uint32), ("q_latent", C.c_void_p), ("q_latent_token_stride", C.c_int64),
+                ("q_latent_head_stride", C.c_int64), ("q_rope", C.c_void_p), ("q_rope_token_stride", C.c_int64), ("q_rope_head_stride", C.c_int64),
+                ("out", C.c_void_p), ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64), ("lse", C.c_void_p), ("token_offsets", C.c_void_p),
+                ("lengths", C.c_void_p), ("block_tables", C.c_void_p), ("requests", C.c_int32), ("max_blocks", C.c_int32), ("num_heads", C.c_int32),
+                ("tokens", C.c_int32), ("max_new", C.c_int32), ("scale", C.c_float)]
+
+
 EXPORTS = ["ptstore_workspace_bytes", "ptstore_create", "ptstore_destroy", "ptstore_hash", "ptstore_lookup",
            "ptstore_fetch", "ptstore_insert", "ptstore_release", "ptstore_evict", "ptstore_status", "ptstore_stats",
            "ptstore_launch_count", "ptstore_last_cuda_error", "ptstore_strerror", "ptstore_fetch_static", "ptstore_promote", "ptstore_evict_async", "ptstore_join", "ptstore_stats_enqueue", "ptstore_lookup_fetch",
            "ptstore_reserve", "ptstore_set_wait_limit", "ptstore_time_next_copy", "ptstore_copy_probe",
            "ptstore_insert_after_lookup", "ptstore_resumed_inserts", "ptstore_kv_chunk_bytes", "ptstore_assign_blocks", "ptstore_map_slots",
-           "ptstore_kv_write", "ptstore_kv_read", "ptstore_attend_workspace_bytes", "ptstore_attend"]
+           "ptstore_kv_write", "ptstore_kv_read", "ptstore_attend_workspace_bytes", "ptstore_attend",
+           "ptstore_latent_write", "ptstore_latent_read", "ptstore_latent_workspace_bytes", "ptstore_latent_attend"]
 
 
 def _load():
@@ -125,6 +135,11 @@ def _load():
     lib.ptstore_attend_workspace_bytes.restype = u64
     lib.ptstore_attend_workspace_bytes.argtypes = [u32]
     lib.ptstore_attend.argtypes = [vp, vp, vp, u64, vp, vp]
+    lib.ptstore_latent_write.argtypes = [vp, i64, vp, i64, i64, vp, vp, vp, vp]
+    lib.ptstore_latent_read.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, vp]
+    lib.ptstore_latent_workspace_bytes.restype = u64
+    lib.ptstore_latent_workspace_bytes.argtypes = [u32]
+    lib.ptstore_latent_attend.argtypes = [vp, vp, vp, u64, vp, vp]
     lib.ptstore_strerror.restype = C.c_char_p
     lib.ptstore_strerror.argtypes = [C.c_int]
     return lib
@@ -196,6 +211,8 @@ def fetch_static(hbm_pool, hbm_blocks, layers, chunk_bytes, ids, matched, cache,
 _KV_DTYPES = {torch.bfloat16: KV_BF16, torch.float16: KV_FP16}
 _KV_CACHE = struct.Struct("PQQIIIIIIff")
 _ATTEND = struct.Struct("IIPqqPqqPPPiiiiifII")
+_LATENT_ATTEND = struct.Struct("IIPqqPqqPqqPPPPiiiiif")
+assert _LATENT_ATTEND.size == C.sizeof(LatentAttend)
 assert _KV_CACHE.size == C.sizeof(KvCache) and _ATTEND.size == C.sizeof(Attend)
 _ATTEND_SIZE = C.sizeof(Attend)
 _raw_stream = torch._C._cuda_getCurrentRawStream
@@ -255,11 +272,13 @@ def _kv_dtype(t, what):
 
 class KVLayout:
     """How a layer's K and V lie in the chunks of a PagedKV: kv heads, head size, tokens per block and format.  k_scale / v_scale are the
-    tensor scales of KV_PACKED (powers of two)."""
+    tensor scales of KV_PACKED (powers of two).  KV_LATENT_BF16 / _FP16: heads 1, dim the latent vector's and LATENT_ROPE; a layer has one
+    chunk per block, so layer i lies in half i % 2 of the PagedKV's (and the store's) layer i // 2."""
 
     def __init__(self, heads, dim, block_tokens, format=KV_BF16, k_scale=1.0, v_scale=1.0):
         self.heads, self.dim, self.block_tokens, self.format = heads, dim, block_tokens, format
         self.k_scale, self.v_scale = k_scale, v_scale
+        self.latent = format in (KV_LATENT_BF16, KV_LATENT_FP16)
         self.chunk_bytes = int(lib.ptstore_kv_chunk_bytes(format, block_tokens, heads, dim))
         if self.chunk_bytes == 0:
             raise PTStoreError(E_INVAL, "ptstore_kv_chunk_bytes")
@@ -270,6 +289,9 @@ class KVLayout:
 
     def of(self, cache, layer, dev=None):
         """The C descriptor of one layer of a PagedKV, as bytes."""
+        half = 0
+        if self.latent:
+            layer, half = layer >> 1, layer & 1
         if not 0 <= layer < len(cache.tensors):
             raise ValueError("layer %d of a cache of %d layers" % (layer, len(cache.tensors)))
         t = cache.tensors[layer]
@@ -286,7 +308,7 @@ class KVLayout:
                 inner *= n
         if len(shape) < 2 or shape[0] != 2 or inner * size != self.chunk_bytes:
             raise ValueError("cache: needs [2, blocks, chunk] with contiguous chunks of %d bytes" % self.chunk_bytes)
-        return _KV_CACHE.pack(t.data_ptr(), stride[0] * size, stride[1] * size, shape[1], self.block_tokens, self.heads, self.dim, self.format, 0,
+        return _KV_CACHE.pack(t.data_ptr() + half * stride[0] * size, stride[0] * size, stride[1] * size, shape[1], self.block_tokens, self.heads, self.dim, self.format, 0,
                               self.k_scale, self.v_scale)
 
 
@@ -393,6 +415,83 @@ def attend(layout, cache, layer, q, token_offsets, lengths, block_tables, max_ne
                         layout.dim ** -0.5 if scale is None else scale, wait_polls, 0)
     _check(lib.ptstore_attend(args, desc, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                               None if status is None else _vec(status, i32, 1, dev, "status"), _raw_stream(dev)), "ptstore_attend")
+    return out
+
+
+_LATENT_DTYPES = {KV_LATENT_BF16: torch.bfloat16, KV_LATENT_FP16: torch.float16}
+
+
+def _latent_dtype(layout):
+    if not layout.latent:
+        raise ValueError("layout: needs KV_LATENT_BF16 or KV_LATENT_FP16")
+    return _LATENT_DTYPES[layout.format]
+
+
+def _rows2(t, dim, n, dtype, dev, what):
+    """[n][dim] rows of 16-bit elements, any token stride; returns the address."""
+    if t.dtype is not dtype or t.shape != (n, dim) or t.stride(1) != 1:
+        raise ValueError("%s: needs a %s tensor [%d, %d], contiguous along the last axis" % (what, dtype, n, dim))
+    if t.get_device() != dev:
+        _elsewhere(t, what)
+    return t.data_ptr()
+
+
+def latent_write(layout, cache, layer, latent, rope, slots, status=None):
+    """ptstore_latent_write: rows latent [tokens, dim - 64], rope [tokens, 64] into one layer of the paged cache at `slots` (int64; -1 skips a row)."""
+    dev, n, dtype = _device(), slots.numel(), _latent_dtype(layout)
+    _check(lib.ptstore_latent_write(_rows2(latent, layout.dim - LATENT_ROPE, n, dtype, dev, "latent"), latent.stride(0), _rows2(rope, LATENT_ROPE, n, dtype, dev, "rope"),
+                                    rope.stride(0), n, _vec(slots, torch.int64, n, dev, "slots"), layout.of(cache, layer, dev),
+                                    None if status is None else _vec(status, torch.int32, 1, dev, "status"), _raw_stream(dev)), "ptstore_latent_write")
+
+
+def latent_read(layout, cache, layer, slots, latent=None, rope=None, status=None):
+    """ptstore_latent_read: the rows at `slots`; rows whose slot is -1 are left as they were.  Returns (latent [tokens, dim - 64], rope [tokens, 64])."""
+    dev, n, dtype = _device(), slots.numel(), _latent_dtype(layout)
+    if latent is None:
+        latent = torch.empty((n, layout.dim - LATENT_ROPE), dtype=dtype, device="cuda")
+    if rope is None:
+        rope = torch.empty((n, LATENT_ROPE), dtype=dtype, device="cuda")
+    _check(lib.ptstore_latent_read(layout.of(cache, layer, dev), _vec(slots, torch.int64, n, dev, "slots"), n,
+                                   _rows2(latent, layout.dim - LATENT_ROPE, n, dtype, dev, "latent"), latent.stride(0),
+                                   _rows2(rope, LATENT_ROPE, n, dtype, dev, "rope"), rope.stride(0),
+                                   None if status is None else _vec(status, torch.int32, 1, dev, "status"), _raw_stream(dev)), "ptstore_latent_read")
+    return latent, rope
+
+
+def latent_workspace(layout):
+    """A workspace for latent_attend on the current device.  Calls that share one must not overlap; they may differ in every size."""
+    _latent_dtype(layout)
+    raw = torch.empty(int(lib.ptstore_latent_workspace_bytes(layout.dim)) + 256, dtype=torch.uint8, device="cuda")
+    return raw[-raw.data_ptr() % 256:]
+
+
+def latent_attend(layout, cache, layer, q_latent, q_rope, token_offsets, lengths, block_tables, max_new, scale, out=None, lse=None, workspace=None, status=None,
+                  wait_polls=0):
+    """ptstore_latent_attend: causal attention of the new tokens over the latent cache (which holds their own rows already), absorbed form.
+    q_latent [tokens, num_heads, dim - 64] (q times the key projection), q_rope [tokens, num_heads, 64]; scale: that of the scores, 1 / sqrt of the
+    size of a head that is not absorbed.  out [tokens, num_heads, dim - 64], to be multiplied by the value projection.  lse: float32 [tokens, num_heads]
+    that receives the logarithms of the rows' sums.  The rest as for attend; workspace: from latent_workspace.  Returns out."""
+    dev, i32, dtype, L = _device(), torch.int32, _latent_dtype(layout), layout.dim - LATENT_ROPE
+    if q_latent.dim() != 3:
+        raise ValueError("q_latent: needs a tensor [tokens, heads, dim]")
+    R, (T, heads, _) = lengths.numel(), q_latent.shape
+    if out is None:
+        out = torch.empty((T, heads, L), dtype=dtype, device=q_latent.device)
+    if workspace is None:
+        workspace = latent_workspace(layout)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace: needs contiguous memory on the current device")
+    desc = layout.of(cache, layer, dev)
+    _on_device(cache.tensors[layer >> 1], dev, "cache")
+    ql, qr, o = q_latent.stride(), q_rope.stride(), out.stride()
+    at = _rows(q_latent, heads, L, T, dtype, dev, "q_latent"), _rows(q_rope, heads, LATENT_ROPE, T, dtype, dev, "q_rope"), _rows(out, heads, L, T, dtype, dev, "out")
+    if at[2] == at[0] and T > 0 and (o[:2] != ql[:2]):
+        raise ValueError("out: is q_latent with other strides")
+    args = _LATENT_ATTEND.pack(_LATENT_ATTEND.size, wait_polls, at[0], ql[0], ql[1], at[1], qr[0], qr[1], at[2], o[0], o[1],
+                               0 if lse is None else _vec(lse, torch.float32, T * heads, dev, "lse"), _vec(token_offsets, i32, R + 1, dev, "token_offsets"),
+                               _vec(lengths, i32, R, dev, "lengths"), _table(block_tables, R, dev, "block_tables"), R, block_tables.shape[1], heads, T, max_new, scale)
+    _check(lib.ptstore_latent_attend(args, desc, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                     None if status is None else _vec(status, i32, 1, dev, "status"), _raw_stream(dev)), "ptstore_latent_attend")
     return out
 
 

@@ -1,9 +1,9 @@
 // ptstore_attend: host side and dispatch of the attention over the paged cache.
-#include <atomic>
 #include <cstddef>
 
 #include "attend_prompt.cuh"
 #include "attend_split.cuh"
+#include "launch.cuh"
 
 using namespace ptk;
 
@@ -11,29 +11,6 @@ namespace {
 
 // rows of an item: 8 where a request's rows of one kv head fit, else 16
 inline int n_tiles_of(i64 rows) { return rows <= 8 ? 1 : 2; }
-
-struct Gpu { int dev, sms; };
-int current_gpu(Gpu* g) {
-  if (cudaGetDevice(&g->dev) != cudaSuccess || cudaDeviceGetAttribute(&g->sms, cudaDevAttrMultiProcessorCount, g->dev) != cudaSuccess || g->sms <= 0) {
-    (void)cudaGetLastError();
-    return PTSTORE_E_CUDA;
-  }
-  if (g->sms > MAX_SMS) g->sms = MAX_SMS;    // a B200 has 148; the workspace does not depend on the device
-  return PTSTORE_OK;
-}
-
-// Lets a kernel use its shared memory, once per device (the setting belongs to the device; concurrent first calls set it twice).
-template <typename F>
-int allow_smem(F* kernel, int bytes, std::atomic<u64>& devices, int dev) {
-  const u64 bit = 1ull << (dev & 63);
-  if (dev < 64 && (devices.load(std::memory_order_acquire) & bit)) return PTSTORE_OK;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return PTSTORE_E_CUDA;
-  }
-  if (dev < 64) devices.fetch_or(bit, std::memory_order_release);
-  return PTSTORE_OK;
-}
 
 template <int FMT, bool QFP16, int D, int NT>
 int launch_split(const Attend& a, const Gpu& gpu, cudaStream_t s) {
@@ -54,27 +31,6 @@ int launch_split_shape(const Attend& a, int D, int nt, const Gpu& gpu, cudaStrea
 
 // The tensor map of one layer's 16-bit cache: {head_dim, heads, tokens of a block, blocks, K or V}, boxes of 64 elements of one head and up to 128
 // tokens of one block.  Returns the tokens of a box, 0 where the block size (or the strides) allows none.
-typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                                CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiled encode_tiled() {                 // null where the driver has none
-  static std::atomic<void*> entry{nullptr};
-  void* fn = entry.load(std::memory_order_acquire);
-  if (!fn) {
-    cudaDriverEntryPointQueryResult got;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &got) != cudaSuccess || got != cudaDriverEntryPointSuccess) {
-      (void)cudaGetLastError();
-      return nullptr;
-    }
-    entry.store(fn, std::memory_order_release);
-  }
-  return reinterpret_cast<EncodeTiled>(fn);
-}
-bool encode(CUtensorMap* map, bool half, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* boxes) {
-  const EncodeTiled fn = encode_tiled();
-  const cuuint32_t steps[5] = {1, 1, 1, 1, 1};
-  return fn && fn(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, boxes, steps,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
 u32 make_tensor_map(const Attend& a, bool half, int D, CUtensorMap* map) {
   const u32 B = a.cache.block_tokens;
   if (B % 8 || (PR_KEYS % B && B % PR_KEYS)) return 0;

@@ -66,18 +66,28 @@ inline bool power_of_two(float x) {
   int e;
   return isfinite(x) && x > 0.0f && frexpf(x, &e) == 0.5f && e >= -63 && e <= 65;
 }
+inline bool is_latent(u32 format) { return format == PTSTORE_KV_LATENT_BF16 || format == PTSTORE_KV_LATENT_FP16; }
 inline u64 chunk_bytes_of(u32 format, u64 block_tokens, u64 heads, u64 dim) {
+  if (is_latent(format)) return block_tokens < 1 || block_tokens > 65536 || block_tokens % 8 || heads != 1 || (dim != 320 && dim != 576) ? 0 : block_tokens * dim * 2;
   if (block_tokens < 1 || heads < 1 || (dim != 64 && dim != 128) || heads > 65535 || block_tokens > 65536) return 0;
   if (format == PTSTORE_KV_BF16 || format == PTSTORE_KV_FP16) return block_tokens * heads * dim * 2;
   if (format == PTSTORE_KV_PACKED) return block_tokens % TILE ? 0 : block_tokens * heads * dim * 9 / 16;
   return 0;
 }
-inline int check_cache(const ptstore_kv_cache_t* c) {
+inline int check_any_cache(const ptstore_kv_cache_t* c) {
   if (!c || !c->base || (reinterpret_cast<uintptr_t>(c->base) & 15u) || c->num_blocks == 0 || c->num_blocks > 0x7FFFFFFFu) return PTSTORE_E_INVAL;
   const u64 chunk = chunk_bytes_of(c->format, c->block_tokens, c->num_kv_heads, c->head_dim);
   if (chunk == 0 || c->kv_stride_bytes % 16 || c->block_stride_bytes % 16 || c->block_stride_bytes < chunk) return PTSTORE_E_INVAL;
   if (c->format == PTSTORE_KV_PACKED && (!power_of_two(c->k_scale) || !power_of_two(c->v_scale))) return PTSTORE_E_INVAL;
   return PTSTORE_OK;
+}
+inline int check_cache(const ptstore_kv_cache_t* c) {        // K and V
+  const int rc = check_any_cache(c);
+  return rc ? rc : is_latent(c->format) ? PTSTORE_E_INVAL : PTSTORE_OK;
+}
+inline int check_latent_cache(const ptstore_kv_cache_t* c) {
+  const int rc = check_any_cache(c);
+  return rc ? rc : is_latent(c->format) ? PTSTORE_OK : PTSTORE_E_INVAL;
 }
 inline Cache cache_of(const ptstore_kv_cache_t* c) {
   return {static_cast<unsigned char*>(c->base), c->kv_stride_bytes, c->block_stride_bytes, c->num_blocks, c->block_tokens, c->num_kv_heads};
