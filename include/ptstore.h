@@ -661,9 +661,10 @@ typedef struct ptstore_attend_weights {
   float*   weights;              /* [requests][num_kv_heads][width], the last axis contiguous */
   int64_t  weights_request_stride, weights_head_stride;
   int32_t  width;
+  int32_t  max_new;              /* at least the rows of any request: chooses the kernel (host) */
   uint32_t accumulate;           /* 0 or 1 */
-  float    scale;                /* the attention's */
-  uint32_t wait_polls;
+  float    scale;                /* the attention's; as in ptstore_attend_t */
+  uint32_t wait_polls, reserved;
 } ptstore_attend_weights_t;
 int ptstore_attend_weights(const ptstore_attend_weights_t* args /*host struct*/, const ptstore_kv_cache_t* cache /*host struct*/, uint32_t* status, ptstore_stream_t stream);
 

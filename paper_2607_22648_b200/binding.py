@@ -82,13 +82,22 @@ class LatentAttend(C.Structure):
                 ("tokens", C.c_int32), ("max_new", C.c_int32), ("scale", C.c_float)]
 
 
+class AttendWeights(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_uint32), ("q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("lse", C.c_void_p), ("token_offsets", C.c_void_p), ("lengths", C.c_void_p), ("block_tables", C.c_void_p), ("requests", C.c_int32),
+                ("max_blocks", C.c_int32), ("num_heads", C.c_int32), ("tokens", C.c_int32), ("weights", C.c_void_p), ("weights_request_stride", C.c_int64),
+                ("weights_head_stride", C.c_int64), ("width", C.c_int32), ("max_new", C.c_int32), ("accumulate", C.c_uint32), ("scale", C.c_float),
+                ("wait_polls", C.c_uint32), ("reserved", C.c_uint32)]
+
+
 EXPORTS = ["ptstore_workspace_bytes", "ptstore_create", "ptstore_destroy", "ptstore_hash", "ptstore_lookup",
            "ptstore_fetch", "ptstore_insert", "ptstore_release", "ptstore_evict", "ptstore_status", "ptstore_stats",
            "ptstore_launch_count", "ptstore_last_cuda_error", "ptstore_strerror", "ptstore_fetch_static", "ptstore_promote", "ptstore_evict_async", "ptstore_join", "ptstore_stats_enqueue", "ptstore_lookup_fetch",
            "ptstore_reserve", "ptstore_set_wait_limit", "ptstore_time_next_copy", "ptstore_copy_probe",
            "ptstore_insert_after_lookup", "ptstore_resumed_inserts", "ptstore_kv_chunk_bytes", "ptstore_assign_blocks", "ptstore_map_slots",
            "ptstore_kv_write", "ptstore_kv_read", "ptstore_attend_workspace_bytes", "ptstore_attend",
-           "ptstore_latent_write", "ptstore_latent_read", "ptstore_latent_workspace_bytes", "ptstore_latent_attend"]
+           "ptstore_latent_write", "ptstore_latent_read", "ptstore_latent_workspace_bytes", "ptstore_latent_attend",
+           "ptstore_attend_lse", "ptstore_attend_weights", "ptstore_select_tokens", "ptstore_kv_compact"]
 
 
 def _load():
@@ -140,6 +149,10 @@ def _load():
     lib.ptstore_latent_workspace_bytes.restype = u64
     lib.ptstore_latent_workspace_bytes.argtypes = [u32]
     lib.ptstore_latent_attend.argtypes = [vp, vp, vp, u64, vp, vp]
+    lib.ptstore_attend_lse.argtypes = [vp, vp, vp, u64, vp, vp, vp]
+    lib.ptstore_attend_weights.argtypes = [vp, vp, vp, vp]
+    lib.ptstore_select_tokens.argtypes = [vp, i64, i64, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, i64, i64, vp, vp]
+    lib.ptstore_kv_compact.argtypes = [vp, vp, vp, i32, i32, vp, i32, vp, i32, vp, vp]
     lib.ptstore_strerror.restype = C.c_char_p
     lib.ptstore_strerror.argtypes = [C.c_int]
     return lib
@@ -212,6 +225,8 @@ _KV_DTYPES = {torch.bfloat16: KV_BF16, torch.float16: KV_FP16}
 _KV_CACHE = struct.Struct("PQQIIIIIIff")
 _ATTEND = struct.Struct("IIPqqPqqPPPiiiiifII")
 _LATENT_ATTEND = struct.Struct("IIPqqPqqPqqPPPPiiiiif")
+_ATTEND_WEIGHTS = struct.Struct("IIPqqPPPPiiiiPqqiiIfII")
+assert _ATTEND_WEIGHTS.size == C.sizeof(AttendWeights)
 assert _LATENT_ATTEND.size == C.sizeof(LatentAttend)
 assert _KV_CACHE.size == C.sizeof(KvCache) and _ATTEND.size == C.sizeof(Attend)
 _ATTEND_SIZE = C.sizeof(Attend)
@@ -391,11 +406,12 @@ def attend_workspace(layout):
     return raw[at:at + n]
 
 
-def attend(layout, cache, layer, q, token_offsets, lengths, block_tables, max_new, scale=None, out=None, workspace=None, status=None, wait_polls=0):
+def attend(layout, cache, layer, q, token_offsets, lengths, block_tables, max_new, scale=None, out=None, workspace=None, status=None, wait_polls=0, lse=None):
     """ptstore_attend: causal attention of the new tokens q [tokens, num_heads, dim] over the paged cache (which holds their own K/V
     already).  Request r owns rows token_offsets[r] .. token_offsets[r+1]-1 and lengths[r] tokens of cache; max_new (host) is at least the
     rows of any request.  workspace: from attend_workspace (a program that calls often keeps one per stream).  wait_polls: polls of the kernels' bounded
-    waits, 0 for the built-in limit.  Returns out."""
+    waits, 0 for the built-in limit.  lse: float32 [tokens, num_heads] that receives the logarithms of the rows' sums (ptstore_attend_lse), for attend_weights.
+    Returns out."""
     dev, i32, code = _device(), torch.int32, _kv_dtype(q, "q")
     R, (T, heads, dim) = lengths.numel(), q.shape
     if out is None:
@@ -413,8 +429,11 @@ def attend(layout, cache, layer, q, token_offsets, lengths, block_tables, max_ne
                         _vec(token_offsets, i32, R + 1, dev, "token_offsets"), _vec(lengths, i32, R, dev, "lengths"),
                         _table(block_tables, R, dev, "block_tables"), R, block_tables.shape[1], heads, T, max_new,
                         layout.dim ** -0.5 if scale is None else scale, wait_polls, 0)
-    _check(lib.ptstore_attend(args, desc, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                              None if status is None else _vec(status, i32, 1, dev, "status"), _raw_stream(dev)), "ptstore_attend")
+    work, room, bits = workspace.data_ptr(), workspace.numel() * workspace.element_size(), None if status is None else _vec(status, i32, 1, dev, "status")
+    if lse is None:
+        _check(lib.ptstore_attend(args, desc, work, room, bits, _raw_stream(dev)), "ptstore_attend")
+    else:
+        _check(lib.ptstore_attend_lse(args, desc, work, room, _vec(lse, torch.float32, T * heads, dev, "lse"), bits, _raw_stream(dev)), "ptstore_attend_lse")
     return out
 
 
@@ -493,6 +512,71 @@ def latent_attend(layout, cache, layer, q_latent, q_rope, token_offsets, lengths
     _check(lib.ptstore_latent_attend(args, desc, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                      None if status is None else _vec(status, i32, 1, dev, "status"), _raw_stream(dev)), "ptstore_latent_attend")
     return out
+
+
+def _weights(t, R, heads, dev, what):
+    """[R][heads][width] 32-bit floats, any request and head strides; returns the address."""
+    if t.dtype is not torch.float32 or t.dim() != 3 or t.shape[0] != R or t.shape[1] != heads or (t.stride(2) != 1 and t.shape[2] > 1):
+        raise ValueError("%s: needs a float32 tensor [%d, %d, width], contiguous along the last axis" % (what, R, heads))
+    if t.get_device() != dev:
+        _elsewhere(t, what)
+    return t.data_ptr()
+
+
+def attend_weights(layout, cache, layer, q, lse, token_offsets, lengths, block_tables, max_new, weights, scale=None, accumulate=True, status=None, wait_polls=0):
+    """ptstore_attend_weights: adds to weights [requests, kv heads, width] what the rows of q [tokens, num_heads, dim] gave to every cached token; lse from attend or
+    latent_attend (of a latent cache q is the latent and the rotary part side by side, and scale has no default).  accumulate=False: writes
+    instead, zeros behind a request's tokens.  Returns weights."""
+    dev, i32, code = _device(), torch.int32, _kv_dtype(q, "q")
+    R, (T, heads, _) = lengths.numel(), q.shape
+    if scale is None:
+        if layout.latent:
+            raise ValueError("scale: has no default for a latent cache")
+        scale = layout.dim ** -0.5
+    desc, at = layout.of(cache, layer, dev), _weights(weights, R, layout.heads, dev, "weights")
+    q_stride, w_stride = q.stride(), weights.stride()
+    args = _ATTEND_WEIGHTS.pack(_ATTEND_WEIGHTS.size, code, _rows(q, heads, layout.dim, T, q.dtype, dev, "q"), q_stride[0], q_stride[1],
+                                _vec(lse, torch.float32, T * heads, dev, "lse"), _vec(token_offsets, i32, R + 1, dev, "token_offsets"),
+                                _vec(lengths, i32, R, dev, "lengths"), _table(block_tables, R, dev, "block_tables"), R, block_tables.shape[1], heads, T, at,
+                                w_stride[0], w_stride[1], weights.shape[2], max_new, 1 if accumulate else 0, scale, wait_polls, 0)
+    _check(lib.ptstore_attend_weights(args, desc, None if status is None else _vec(status, i32, 1, dev, "status"), _raw_stream(dev)), "ptstore_attend_weights")
+    return weights
+
+
+def select_tokens(weights, lengths, budget, first, recent, kept=None, lengths_out=None, weights_out=None, status=None):
+    """ptstore_select_tokens: of every request longer than `budget` the tokens each kv head keeps, its first `first`, last `recent` and the ones with the largest weights in between.
+    weights [requests, kv heads, width] float32; the kept tokens' weights go to weights_out (weights itself by default).  Returns (kept int32 [requests, kv heads, budget],
+    ascending, -1 behind the last; lengths_out int32 [requests]; weights_out)."""
+    dev, i32, R = _device(), torch.int32, lengths.numel()
+    if weights.dim() != 3:
+        raise ValueError("weights: needs a float32 tensor [requests, heads, width]")
+    heads, width = weights.shape[1:]
+    if kept is None:
+        kept = torch.empty((R, heads, max(budget, 0)), dtype=i32, device="cuda")
+    if lengths_out is None:
+        lengths_out = torch.empty(R, dtype=i32, device="cuda")
+    if weights_out is None:
+        weights_out = weights
+    elif weights_out.shape != weights.shape:
+        raise ValueError("weights_out: needs the shape of weights")
+    w, o = weights.stride(), weights_out.stride()
+    _check(lib.ptstore_select_tokens(_weights(weights, R, heads, dev, "weights"), w[0], w[1], _vec(lengths, i32, R, dev, "lengths"), R, heads, width, budget, first, recent,
+                                     _vec(kept, i32, R * heads * max(budget, 0), dev, "kept"), _vec(lengths_out, i32, R, dev, "lengths_out"),
+                                     _weights(weights_out, R, heads, dev, "weights_out"), o[0], o[1], None if status is None else _vec(status, i32, 1, dev, "status"),
+                                     _raw_stream(dev)), "ptstore_select_tokens")
+    return kept, lengths_out, weights_out
+
+
+def kv_compact(layout, cache, layer, kept, lengths, block_tables, to_tables=None, status=None):
+    """ptstore_kv_compact: in one layer of the cache, token i < lengths[r] of request r and kv head h becomes its token kept[r, h, i] (int32 [requests, kv heads, n]).  to_tables None: in
+    place (kept ascends, and no block belongs to two requests); else the tokens go to the blocks of to_tables, none of which block_tables names."""
+    dev, i32, R = _device(), torch.int32, lengths.numel()
+    if kept.dim() != 3 or kept.shape[0] != R or kept.shape[1] != layout.heads:
+        raise ValueError("kept: needs an int32 tensor [%d, %d, n]" % (R, layout.heads))
+    to = block_tables if to_tables is None else to_tables
+    _check(lib.ptstore_kv_compact(layout.of(cache, layer, dev), _vec(kept, i32, kept.numel(), dev, "kept"), _vec(lengths, i32, R, dev, "lengths"), R, kept.shape[2],
+                                  _table(block_tables, R, dev, "block_tables"), block_tables.shape[1], _table(to, R, dev, "to_tables"), to.shape[1],
+                                  None if status is None else _vec(status, i32, 1, dev, "status"), _raw_stream(dev)), "ptstore_kv_compact")
 
 
 class PTStore:

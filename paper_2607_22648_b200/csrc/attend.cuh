@@ -24,6 +24,7 @@ struct Attend {
   u32 split;                                  // CTAs among which the steps of the row tiles may be cut, 0: they are not
   u32 polls;                                  // polls of a wait before its CTA gives up
   u32* status;
+  float* lse;                                 // [tokens][heads] logarithms of the rows' sums, or null
 };
 constexpr u32 POLLS = 1u << 22;               // the built-in limit (each poll may suspend for a while), and that of waits for what is in flight at the end
 
@@ -56,6 +57,9 @@ __device__ __forceinline__ float row_factor(const Attend& a, int r, i64 pos, flo
       if ((u32)a.tables[(i64)r * a.max_blocks + b] < a.cache.num_blocks) return NAN;
   return 0.0f;
 }
+
+// Logarithm (natural) of a row's sum l of powers of two from its reference m on; minus infinity where there is nothing to add up
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f; }
 
 __device__ __forceinline__ u32 smem_addr(const void* p) { return (u32)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void cp_async16(u32 dst, const void* src) {

@@ -212,7 +212,7 @@ __device__ __forceinline__ void find_tile(const Attend& a, i64 index, i64 mine, 
   *s_tile = (int)(n - 1 - left);
 }
 
-template <int FMT, bool QFP16, int D>
+template <int FMT, bool QFP16, int D, bool LSE>
 __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Attend a, const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap q_map) {
   constexpr bool PACKED = FMT == PTSTORE_KV_PACKED;
   constexpr bool F16 = PACKED || FMT == PTSTORE_KV_FP16;
@@ -799,6 +799,10 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
         const u32 flat = row_base + row, fr = flat / (u32)a.group;
         at = (i64)(rq.row0 + (int)fr) * a.o_token + (i64)(h * a.group + (int)(flat - fr * a.group)) * a.o_head;
       }
+      if (LSE && parts == 1 && row < rows) {
+        const u32 flat = row_base + row, fr = flat / (u32)a.group;
+        a.lse[(i64)(rq.row0 + (int)fr) * a.heads + h * a.group + (int)(flat - fr * a.group)] = lse_of(m, l);
+      }
       unsigned char* const mine = smem + w * TB;
 #pragma unroll
       for (int c = 0; c < D; c += 32) {
@@ -871,7 +875,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) attend_prompt_kernel(const Atte
 
 // Joins the chunks of the row tiles that were cut: blockIdx.x the tile (behind the uncut ones), blockIdx.y some of its rows, a warp
 // for K, whose loads are in flight together (K = 1 spreads few tiles over more warps).  Four CTAs an SM: the largest grid, 74 x 8, is one round.
-template <bool QFP16, int D, int K>
+template <bool QFP16, int D, int K, bool LSE>
 __global__ void __launch_bounds__(256, 4) attend_join_kernel(const Attend a) {
   __shared__ i64 s_scan[8];
   __shared__ int s_r, s_tile;
@@ -940,6 +944,7 @@ __global__ void __launch_bounds__(256, 4) attend_join_kernel(const Attend a) {
     const u32 flat = row_base + at0 + k, fr = flat / (u32)a.group;
     const float f = sum[k] == 0.0f ? 0.0f : a.v_factor / sum[k];
     if (sum[k] == 0.0f) none |= 1u << k;
+    if (LSE && lane == 0) a.lse[(i64)(q.row0 + (int)fr) * a.heads + h * a.group + (int)(flat - fr * a.group)] = lse_of(top[k], sum[k]);
     u32* const dst = reinterpret_cast<u32*>(a.out + 2 * ((i64)(q.row0 + (int)fr) * a.o_token + (i64)(h * a.group + (int)(flat - fr * a.group)) * a.o_head + lane * E));
 #pragma unroll
     for (int e = 0; e < E; e += 2) dst[e / 2] = pack2<QFP16>(acc[k][e] * f, acc[k][e + 1] * f);

@@ -118,7 +118,7 @@ __device__ __forceinline__ u64 request_units(const Attend& a, int r) {
   return u * a.cache.heads;
 }
 
-template <int FMT, bool QFP16, int D, int NT>
+template <int FMT, bool QFP16, int D, int NT, bool LSE>
 __global__ void __launch_bounds__(SplitShape<FMT, D>::THREADS, split_ctas<FMT, NT>()) attend_split_kernel(Attend a) {
   using Shape = SplitShape<FMT, D>;
   constexpr bool PACKED = Shape::PACKED;
@@ -784,6 +784,7 @@ __global__ void __launch_bounds__(SplitShape<FMT, D>::THREADS, split_ctas<FMT, N
           }
           const float f = row_factor(a, r, (i64)rq.pos0 + (row_base + rw) / a.group, all);
           const int fr = (row_base + rw) / a.group, hq = h * a.group + (row_base + rw) % a.group;
+          if (LSE && e == 0) a.lse[(i64)(rq.row0 + fr) * a.heads + hq] = lse_of(high, all);
           *reinterpret_cast<uint2*>(a.out + 2 * ((i64)(rq.row0 + fr) * a.o_token + (i64)hq * a.o_head + e)) =
               make_uint2(pack2<QFP16>(o4.x * f, o4.y * f), pack2<QFP16>(o4.z * f, o4.w * f));
         }
@@ -792,6 +793,7 @@ __global__ void __launch_bounds__(SplitShape<FMT, D>::THREADS, split_ctas<FMT, N
     if (write && row < rows) {
       const float f = row_factor(a, r, (i64)rq.pos0 + (row_base + row) / a.group, sum);
       const int fr = (row_base + row) / a.group, hq = h * a.group + (row_base + row) % a.group;
+      if (LSE && e0 == 0) a.lse[(i64)(rq.row0 + fr) * a.heads + hq] = lse_of(top, sum);
       unsigned char* dst = a.out + 2 * ((i64)(rq.row0 + fr) * a.o_token + (i64)hq * a.o_head + e0);
       __align__(16) u32 v[E / 2];
 #pragma unroll

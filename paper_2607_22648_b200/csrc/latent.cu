@@ -144,7 +144,7 @@ extern "C" int ptstore_latent_attend(const ptstore_latent_attend_t* p, const pts
   a.status = status;
   la.q_rope = static_cast<const unsigned char*>(p->q_rope);
   la.qr_token = p->q_rope_token_stride; la.qr_head = p->q_rope_head_stride;
-  la.lse = p->lse;
+  a.lse = p->lse;
   Gpu gpu;
   (void)cudaGetLastError();
   const int rs = current_gpu(&gpu);

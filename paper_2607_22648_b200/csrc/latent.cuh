@@ -50,7 +50,6 @@ struct Latent {
   Attend a;                  // q: q_latent; cache.heads 1, group = heads
   const unsigned char* q_rope;
   i64 qr_token, qr_head;
-  float* lse;                // [tokens][heads] or null
 };
 // what the join needs of an item that begins in a CTA and goes on in others
 struct LatentPart { int parts, r; u32 rt; };
@@ -114,9 +113,6 @@ __device__ __forceinline__ bool any_of_softmax(bool v) {      // barrier of the 
   asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 2, 128, p;\n selp.u32 %0, 1, 0, q;\n}" : "=r"(r) : "r"((u32)v) : "memory");
   return r != 0;
 }
-
-// Logarithm (natural) of a row's sum from its reference and its sum in powers of two
-__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f; }
 
 template <int L, bool F16, int PAIR>
 __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Latent la, const __grid_constant__ CUtensorMap map) {
@@ -436,7 +432,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
         const i64 pos = (i64)rq.pos0 + (row_base + row) / a.group;
         if (whole) {
           s.f[row] = row_factor(a, r, pos, l);
-          if (la.lse) la.lse[(i64)(rq.row0 + (row_base + row) / a.group) * a.heads + (row_base + row) % a.group] = lse_of(m, l);
+          if (a.lse) a.lse[(i64)(rq.row0 + (row_base + row) / a.group) * a.heads + (row_base + row) % a.group] = lse_of(m, l);
         } else {
           s.f[row] = 1.0f;
           my[LA_ROWS * L + row] = m;
@@ -519,7 +515,7 @@ __global__ void __launch_bounds__(L / 4) latent_join_kernel(const Latent la, int
     const int fr = (row_base + row) / a.group, hq = (row_base + row) % a.group;
     const float f = row_factor(a, part.r, (i64)q.pos0 + fr, sum);
     *reinterpret_cast<uint2*>(a.out + 2 * ((i64)(q.row0 + fr) * a.o_token + (i64)hq * a.o_head + e)) = make_uint2(pack2<F16>(o.x * f, o.y * f), pack2<F16>(o.z * f, o.w * f));
-    if (la.lse && threadIdx.x == 0) la.lse[(i64)(q.row0 + fr) * a.heads + hq] = lse_of(top, sum);
+    if (a.lse && threadIdx.x == 0) a.lse[(i64)(q.row0 + fr) * a.heads + hq] = lse_of(top, sum);
   }
 }
 
