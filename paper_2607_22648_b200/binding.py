@@ -82,6 +82,14 @@ class LatentAttend(C.Structure):
                 ("tokens", C.c_int32), ("max_new", C.c_int32), ("scale", C.c_float)]
 
 
+class ExpandedAttend(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_uint32), ("q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("k", C.c_void_p), ("k_token_stride", C.c_int64), ("k_head_stride", C.c_int64), ("k_rope", C.c_void_p), ("k_rope_token_stride", C.c_int64),
+                ("v", C.c_void_p), ("v_token_stride", C.c_int64), ("v_head_stride", C.c_int64), ("out", C.c_void_p), ("out_token_stride", C.c_int64),
+                ("out_head_stride", C.c_int64), ("token_offsets", C.c_void_p), ("key_offsets", C.c_void_p), ("requests", C.c_int32), ("heads", C.c_int32),
+                ("tokens", C.c_int32), ("keys", C.c_int32), ("max_new", C.c_int32), ("scale", C.c_float), ("wait_polls", C.c_uint32), ("reserved", C.c_uint32)]
+
+
 class AttendWeights(C.Structure):
     _fields_ = [("struct_size", C.c_uint32), ("dtype", C.c_uint32), ("q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
                 ("lse", C.c_void_p), ("token_offsets", C.c_void_p), ("lengths", C.c_void_p), ("block_tables", C.c_void_p), ("requests", C.c_int32),
@@ -97,7 +105,7 @@ EXPORTS = ["ptstore_workspace_bytes", "ptstore_create", "ptstore_destroy", "ptst
            "ptstore_insert_after_lookup", "ptstore_resumed_inserts", "ptstore_kv_chunk_bytes", "ptstore_assign_blocks", "ptstore_map_slots",
            "ptstore_kv_write", "ptstore_kv_read", "ptstore_attend_workspace_bytes", "ptstore_attend",
            "ptstore_latent_write", "ptstore_latent_read", "ptstore_latent_workspace_bytes", "ptstore_latent_attend",
-           "ptstore_attend_lse", "ptstore_attend_weights", "ptstore_select_tokens", "ptstore_kv_compact"]
+           "ptstore_expanded_attend", "ptstore_attend_lse", "ptstore_attend_weights", "ptstore_select_tokens", "ptstore_kv_compact"]
 
 
 def _load():
@@ -149,6 +157,7 @@ def _load():
     lib.ptstore_latent_workspace_bytes.restype = u64
     lib.ptstore_latent_workspace_bytes.argtypes = [u32]
     lib.ptstore_latent_attend.argtypes = [vp, vp, vp, u64, vp, vp]
+    lib.ptstore_expanded_attend.argtypes = [vp, vp, vp]
     lib.ptstore_attend_lse.argtypes = [vp, vp, vp, u64, vp, vp, vp]
     lib.ptstore_attend_weights.argtypes = [vp, vp, vp, vp]
     lib.ptstore_select_tokens.argtypes = [vp, i64, i64, vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, i64, i64, vp, vp]
@@ -225,6 +234,8 @@ _KV_DTYPES = {torch.bfloat16: KV_BF16, torch.float16: KV_FP16}
 _KV_CACHE = struct.Struct("PQQIIIIIIff")
 _ATTEND = struct.Struct("IIPqqPqqPPPiiiiifII")
 _LATENT_ATTEND = struct.Struct("IIPqqPqqPqqPPPPiiiiif")
+_EXPANDED_ATTEND = struct.Struct("IIPqqPqqPqPqqPqqPPiiiiifII")
+assert _EXPANDED_ATTEND.size == C.sizeof(ExpandedAttend)
 _ATTEND_WEIGHTS = struct.Struct("IIPqqPPPPiiiiPqqiiIfII")
 assert _ATTEND_WEIGHTS.size == C.sizeof(AttendWeights)
 assert _LATENT_ATTEND.size == C.sizeof(LatentAttend)
@@ -511,6 +522,28 @@ def latent_attend(layout, cache, layer, q_latent, q_rope, token_offsets, lengths
                                _vec(lengths, i32, R, dev, "lengths"), _table(block_tables, R, dev, "block_tables"), R, block_tables.shape[1], heads, T, max_new, scale)
     _check(lib.ptstore_latent_attend(args, desc, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                      None if status is None else _vec(status, i32, 1, dev, "status"), _raw_stream(dev)), "ptstore_latent_attend")
+    return out
+
+
+def expanded_attend(q, k, k_rope, v, token_offsets, key_offsets, max_new, scale=None, out=None, status=None, wait_polls=0):
+    """ptstore_expanded_attend: causal attention of the new tokens q [tokens, heads, 192] over the requests' keys k [keys, heads, 128] and k_rope [keys, 64] (shared by the heads; q's
+    last 64 elements meet them) and values v [keys, heads, 128], the last keys of a request being its rows' own.  k and v may be views of one tensor, and their head
+    strides 0.  Request r owns rows token_offsets[r] .. and keys key_offsets[r] ..; scale: 192 ** -0.5 by default.  Returns out [tokens, heads, 128]."""
+    dev, i32, code = _device(), torch.int32, _kv_dtype(q, "q")
+    R, (T, heads, _), dtype = token_offsets.numel() - 1, q.shape, q.dtype
+    if k.dim() != 3 or R < 0:
+        raise ValueError("k: needs a tensor [keys, heads, 128], token_offsets at least one entry")
+    N = k.shape[0]
+    if out is None:
+        out = torch.empty((T, heads, 128), dtype=dtype, device=q.device)
+    for t, what in ((q, "q"), (k, "k"), (k_rope, "k_rope"), (v, "v")):
+        _on_device(t, dev, what)
+    qs, ks, rs, vs, os_ = q.stride(), k.stride(), k_rope.stride(), v.stride(), out.stride()
+    args = _EXPANDED_ATTEND.pack(_EXPANDED_ATTEND.size, code, _rows(q, heads, 192, T, dtype, dev, "q"), qs[0], qs[1], _rows(k, heads, 128, N, dtype, dev, "k"), ks[0], ks[1],
+                                 _rows2(k_rope, 64, N, dtype, dev, "k_rope"), rs[0], _rows(v, heads, 128, N, dtype, dev, "v"), vs[0], vs[1],
+                                 _rows(out, heads, 128, T, dtype, dev, "out"), os_[0], os_[1], _vec(token_offsets, i32, R + 1, dev, "token_offsets"),
+                                 _vec(key_offsets, i32, R + 1, dev, "key_offsets"), R, heads, T, N, max_new, 192 ** -0.5 if scale is None else scale, wait_polls, 0)
+    _check(lib.ptstore_expanded_attend(args, None if status is None else _vec(status, i32, 1, dev, "status"), _raw_stream(dev)), "ptstore_expanded_attend")
     return out
 
 
