@@ -97,6 +97,14 @@ __device__ __forceinline__ void tc_ld32(float (&v)[32], u32 addr) {
                  "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
                : "r"(addr) : "memory");
 }
+// 16 columns likewise, into the first half of v
+__device__ __forceinline__ void tc_ld16(float (&v)[32], u32 addr) {
+  float* r = v;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]),
+                 "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
+               : "r"(addr) : "memory");
+}
 // values of a load may be used from here on (after tc_wait_ld): keeps the compiler from moving their uses above the wait
 __device__ __forceinline__ void tc_loaded(float (&v)[32]) {
 #pragma unroll

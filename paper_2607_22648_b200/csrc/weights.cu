@@ -2,10 +2,13 @@
 //
 //     w[j] = sum over rows i that see token j of exp2(scale2 k_j.q_i - lse2_i)
 //
-// A CTA takes a tile of one request's and kv head's tokens and goes over the rows in chunks: S^T = K Q^T with the TOKENS as the tensor instruction's rows, so that a thread has
-// one token's scores against all rows of a chunk and adds them up by itself; no exchange, no atomics, one order of addition.  The softmax's sum is known (lse), so K is read
-// once and nothing else of the cache.  A decode step is bound by reading K (many small CTAs an SM, whose loads overlap the others' work), a window of many rows by its
-// exponentials.
+// A CTA takes some consecutive tiles of one request's and kv head's tokens and goes over the rows in chunks: S^T = K Q^T with the TOKENS as the tensor instruction's rows, so that
+// a thread has one token's scores against all rows of a chunk and adds them up by itself; no exchange, no atomics, one order of addition.  The softmax's sum is known (lse), so K is
+// read once and nothing else of the cache.  The next tile is on its way while one is computed with, and Q stays where it is while its rows fit.  A decode step is bound by
+// reading K, a window of many rows by its exponentials.
+//
+// Weights keep what 32 bits can hold of them: scores are summed up in two or three accumulators (the tensor cores cut off what does not fit the running sum, an error that grows with its
+// length and size), and scale and lse, times log2 e, are kept as two numbers each (a rounding of an exponent of 20 is 2^-20 of the weight).
 #include "attend_prompt.cuh"
 #include "launch.cuh"
 
@@ -18,19 +21,23 @@ struct Weights {
   const float* lse;
   float* out;
   i64 o_request, o_head;
-  int width, tiles;          // tiles of a request
+  float scale_hi, scale_lo;  // scale * log2 e (and the 4-bit values' factors, powers of two)
+  int width, tiles, each;    // CTAs of a request and kv head, and tiles of a CTA
   bool add;
 };
 
 constexpr int AW_THREADS = 128;
-// tokens of a tile: all 128 rows of the instruction, but for latent rows, of which twice as many CTAs fit an SM with 64
-template <int D>
-__host__ __device__ constexpr int aw_keys() { return D > 128 ? 64 : 128; }
-// rows of a chunk: few for a decode step, more for many rows (as many as leave two CTAs an SM)
-template <int D>
-__host__ __device__ constexpr int aw_many() { return D > 128 ? 32 : 64; }
-template <int D, int NR>
-constexpr int aw_smem() { return (aw_keys<D>() + NR) * D * 2 + 1024; }
+constexpr float LOG2E_REST = (float)(1.4426950408889634074 - (double)LOG2E);          // what 32 bits leave of log2 e
+template <bool PACKED, int D, int NR>
+struct WeightsShape {
+  // tokens of a tile: all 128 rows of the instruction, but for latent rows, of which two tiles have to fit an SM beside Q
+  static constexpr int KT = D > 128 ? 64 : 128;
+  static constexpr int BOXES = D / 64, SUMS = D == 64 ? 1 : D == 128 ? 2 : 3, PER = (BOXES + SUMS - 1) / SUMS;      // accumulators, boxes of 64 elements of each
+  static constexpr int HELD = NR == 16 ? 16 : D > 128 ? 64 : 128;                                                   // rows of Q that stay in shared memory
+  static constexpr int STAGES = PACKED ? 1 : 2, K_BYTES = KT * D * 2, Q_BYTES = HELD * D * 2;
+  static constexpr int SMEM = STAGES * K_BYTES + Q_BYTES + 1024;
+  static constexpr int NEED = 2 * SUMS * NR, COLS = NEED <= 32 ? 32 : NEED <= 64 ? 64 : NEED <= 128 ? 128 : NEED <= 256 ? 256 : 512;
+};
 
 __host__ __device__ constexpr u32 aw_desc(bool fp16, int M, int N) {       // both operands with a row's elements contiguous
   return (1u << 4) | ((fp16 ? 0u : 1u) << 7) | ((fp16 ? 0u : 1u) << 10) | ((u32)(N >> 3) << 17) | ((u32)(M >> 4) << 24);
@@ -38,104 +45,122 @@ __host__ __device__ constexpr u32 aw_desc(bool fp16, int M, int N) {       // bo
 
 template <bool PACKED, bool F16, bool QFP16, int D, int NR>
 __global__ void __launch_bounds__(AW_THREADS) weights_kernel(const Weights wa) {
-  constexpr int KT = aw_keys<D>(), CPR = D / 8, COLS = NR < 32 ? 32 : NR;
+  using Shape = WeightsShape<PACKED, D, NR>;
+  constexpr int KT = Shape::KT, CPR = D / 8, SUMS = Shape::SUMS, HELD = Shape::HELD, KB = Shape::K_BYTES;
+  constexpr bool SCALED = PACKED && !QFP16;                   // bf16 rows over the 4-bit cache have a factor each
   extern __shared__ unsigned char smem_raw[];
   unsigned char* const smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
-  unsigned char* const smem_q = smem + KT * D * 2;
-  __shared__ __align__(8) u64 s_bar;
+  unsigned char* const smem_q = smem + Shape::STAGES * KB;
+  __shared__ __align__(8) u64 s_bar[2];
   __shared__ u32 s_tmem;
-  __shared__ int s_gave_up;
-  __shared__ i64 s_row[KT];
-  __shared__ float s_scale[NR], s_lse[NR];
-  __shared__ int s_see[NR];
+  __shared__ int s_gave_up, s_min;
+  __shared__ i64 s_row[2][KT];                                // where a tile's rows lie, -1: not there
+  __shared__ float2 s_lse[HELD];
+  __shared__ float s_factor[SCALED ? HELD : 1];
+  __shared__ int s_see[HELD];
   const Attend& a = wa.a;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0);
   const u32 rh = blockIdx.x / (u32)wa.tiles, h = rh % a.cache.heads;
-  const int r = (int)(rh / a.cache.heads), key0 = (int)(blockIdx.x % (u32)wa.tiles) * KT;
+  const int r = (int)(rh / a.cache.heads), first = (int)(blockIdx.x % (u32)wa.tiles) * wa.each * KT;
   const Req rq = request(a, r);
-  const int n = min(rq.keys, wa.width), rows = rq.fresh * a.group;
-  // thread t < KT has token key0 + t; the scores of 64 tokens lie in the first 16 lanes of each warp
+  const int rows = rq.fresh * a.group;
+  // tokens that count: those some row sees
+  const i64 top = (i64)rq.pos0 + rq.fresh;
+  const int n = rows <= 0 || top <= 0 ? 0 : (int)min((i64)min(rq.keys, wa.width), top);
+  const int end = min(first + wa.each * KT, wa.width);
+  float* const out = wa.out + r * wa.o_request + h * wa.o_head;
+  if (!wa.add)                                                // tokens that nobody sees
+    for (int j = max(first, n) + tid; j < end; j += AW_THREADS) out[j] = 0.0f;
+  if (first >= n) return;
+  const int tiles = (min(n, end) - first + KT - 1) / KT;
+  // the scores of 64 tokens lie in the first 16 lanes of each warp
   const int mine = KT == 128 ? tid : warp * 16 + (lane & 15);
   const bool writes = KT == 128 || lane < 16;
-  const int key = key0 + mine;
-  float* const out = wa.out + r * wa.o_request + h * wa.o_head;
-  if (key0 >= n || rows <= 0 || (i64)rq.pos0 + rq.fresh - 1 < key0) {        // nothing there, or nothing seen
-    if (!wa.add && writes && key < wa.width) out[key] = 0.0f;
-    return;
-  }
-  // ---- K into shared memory
+
   const u32 B = a.cache.block_tokens;
-  bool have = false;
-  if (tid < KT) {
-    const int k = key0 + tid;
-    i64 at = -1;
-    if (k < n) {
-      const u32 id = (u32)a.tables[(i64)r * a.max_blocks + (u32)k / B], in = (u32)k % B;
-      if (id < a.cache.num_blocks) {
-        at = (i64)((u64)id * a.cache.block_stride);
-        at += PACKED ? (i64)((u64)h * (B / TILE) + in / TILE) * tile_bytes(D) : (i64)((u64)in * a.cache.heads + h) * (D * 2);
-        have = true;
-      } else if (a.status) atomicOr(a.status, PTSTORE_S_BOUNDS);
+  const int* const table = a.tables + (i64)r * a.max_blocks;
+  bool bounds = false;
+  // where token `tid` of tile t lies
+  auto look_up = [&](int t) { return tid < KT && t < tiles && first + t * KT + tid < n ? table[(u32)(first + t * KT + tid) / B] : -1; };
+  auto place = [&](int t, int id) -> i64 {
+    const int k = first + t * KT + tid;
+    if (tid >= KT || t >= tiles || k >= n) return -1;
+    if ((u32)id >= a.cache.num_blocks) { bounds = true; return -1; }
+    const u32 in = (u32)k % B;
+    return (i64)((u64)(u32)id * a.cache.block_stride) +
+           (PACKED ? (i64)((u64)h * (B / TILE) + in / TILE) * tile_bytes(D) : (i64)((u64)in * a.cache.heads + h) * (D * 2));
+  };
+  // 16-bit: the tile's rows into a stage, zeros for those that are not there
+  auto issue = [&](int t) {
+    const u32 dst = smem_addr(smem) + (t & 1) * KB;
+#pragma unroll 8
+    for (int i = tid; i < KT * CPR; i += AW_THREADS) {
+      const int row = i / CPR, c = i % CPR;
+      const i64 at = s_row[t & 1][row];
+      cp_async16_or_zero(dst + (c >> 3) * (KT * 128) + row * 128 + (((c & 7) ^ (row & 7)) * 16), a.cache.base + (at < 0 ? 0 : at) + c * 16, at >= 0);
     }
-    s_row[tid] = at;
-    if (PACKED) {            // one token a thread: codes to fp16, element order 0 4 1 5 2 6 3 7 inside eight, as the unpacking yields them (and Q is stored)
-      const Magic mg = magic();
-      const int m = (u32)k % TILE;
-      const unsigned char* const src = a.cache.base + (have ? at : 0);
-      __align__(8) unsigned char sc[D / 16] = {};
-      uint4 code[D / 32];
+  };
+  // 4-bit: one token a thread, codes and scales on their way in registers, then unpacked to fp16 (element order 0 4 1 5 2 6 3 7 inside eight, as the unpacking yields them; Q is stored likewise)
+  uint4 code[PACKED ? D / 32 : 1];
+  uint2 scales;
+  const Magic mg = magic();
+  auto fetch = [&](int t, i64 at) {
+    if (!PACKED) return;
+    const int m = (u32)(first + t * KT + tid) % TILE;
+    const unsigned char* const src = a.cache.base + (at < 0 ? 0 : at);
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) code[c] = have ? *reinterpret_cast<const uint4*>(src + code_place(D, m, c) * 16) : make_uint4(0, 0, 0, 0);
-      if (have) {
-        if (D == 128) *reinterpret_cast<uint2*>(sc) = *reinterpret_cast<const uint2*>(src + scale_at(D, false, m, 0));
-        else *reinterpret_cast<u32*>(sc) = *reinterpret_cast<const u32*>(src + scale_at(D, false, m, 0));
-      }
+    for (int c = 0; c < D / 32; ++c) code[PACKED ? c : 0] = at >= 0 ? *reinterpret_cast<const uint4*>(src + code_place(D, m, c) * 16) : make_uint4(0, 0, 0, 0);
+    scales = make_uint2(0, 0);
+    if (at >= 0) {
+      if (D == 128) scales = *reinterpret_cast<const uint2*>(src + scale_at(D, false, m, 0));
+      else scales.x = *reinterpret_cast<const u32*>(src + scale_at(D, false, m, 0));
+    }
+  };
+  auto unpack = [&]() {
+    if (!PACKED) return;
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) {
-        const Deq d0 = deq_of(e4m3x2_to_half2(sc[2 * c] * 0x101u)), d1 = deq_of(e4m3x2_to_half2(sc[2 * c + 1] * 0x101u));
-        const u32 w[4] = {code[c].x, code[c].y, code[c].z, code[c].w};
+    for (int c = 0; c < D / 32; ++c) {
+      const u32 two = ((c & 2 ? scales.y : scales.x) >> (16 * (c & 1))) & 0xFFFFu;          // two scale groups of a chunk of 32 elements
+      const Deq d0 = deq_of(e4m3x2_to_half2((two & 0xFFu) * 0x101u)), d1 = deq_of(e4m3x2_to_half2((two >> 8) * 0x101u));
+      const uint4 four = code[PACKED ? c : 0];
+      const u32 w[4] = {four.x, four.y, four.z, four.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          u32 o[4];
-          deq4(w[i], w[i] >> 8, i < 2 ? d0 : d1, mg, o);
-          *reinterpret_cast<uint4*>(smem + operand_at(tid, 4 * c + i)) = make_uint4(o[0], o[1], o[2], o[3]);
-        }
+      for (int i = 0; i < 4; ++i) {
+        u32 o[4];
+        deq4(w[i], w[i] >> 8, i < 2 ? d0 : d1, mg, o);
+        *reinterpret_cast<uint4*>(smem + operand_at(tid, 4 * c + i)) = make_uint4(o[0], o[1], o[2], o[3]);
       }
     }
-  }
+  };
+  i64 at = place(0, look_up(0));
+  int id = look_up(1);
+  if (tid < KT) s_row[0][tid] = at;
+  if (PACKED) fetch(0, at);
   if (tid == 0) {
-    bar_init(&s_bar, 1);
+    bar_init(&s_bar[0], 1);
+    bar_init(&s_bar[1], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s_gave_up = 0;
+    s_min = 0x7FFFFFFF;
   }
   if (warp == 0) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "n"(COLS) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "n"(Shape::COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const u32 tmem = s_tmem;
+  const u32 tmem = s_tmem, lanes = tmem + ((u32)(32 * warp) << 16);
   if (!PACKED) {
-#pragma unroll 8
-    for (int i = tid; i < KT * CPR; i += AW_THREADS) {
-      const int t = i / CPR, c = i % CPR;
-      const i64 at = s_row[t];
-      cp_async16_or_zero(smem_addr(smem) + (c >> 3) * (KT * 128) + t * 128 + (((c & 7) ^ (t & 7)) * 16), a.cache.base + (at < 0 ? 0 : at) + c * 16, at >= 0);
-    }
+    issue(0);
     cp_commit();
   }
-  have = s_row[mine] >= 0;
-  // ---- rows, a chunk at a time
-  const u32 smem_k = smem_addr(smem), smem_qa = smem_addr(smem_q);
-  float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  bool timeout = false;
-  u32 phase = 0;
-  for (int row0 = 0; row0 < rows; row0 += NR) {
-    const int m = min(NR, rows - row0);
-    // threads of a row hold all of it, for its largest element
+  // ---- rows row0 .. row0 + HELD - 1 of Q, in the products' type; rows that do not exist are zero and give nothing
+  auto load_q = [&](int row0) {
     constexpr int TPR = D > 128 ? 32 : CPR, EACH = (CPR + TPR - 1) / TPR, PASS = AW_THREADS / TPR;
-    for (int p = 0; p < NR; p += PASS) {
+    const int m = min(HELD, rows - row0);
+#pragma unroll 2
+    for (int p = 0; p < HELD && p < ((m + NR - 1) / NR) * NR; p += PASS) {
       const int t = p + tid / TPR, c0 = tid % TPR;
       const int flat = row0 + t, fr = flat / a.group, hq = (int)h * a.group + flat % a.group;
       const bool live = t < m;
@@ -148,7 +173,7 @@ __global__ void __launch_bounds__(AW_THREADS) weights_kernel(const Weights wa) {
         x[e][0] = v.x; x[e][1] = v.y; x[e][2] = v.z; x[e][3] = v.w;
       }
       float factor = 1.0f;
-      if (PACKED && !QFP16) {
+      if (SCALED) {
         // bf16 rows as fp16, scaled by a power of two so that the largest element is in [1, 2): elements below 2^-14 of it lose at most 2^-25 of it
         float amax = 0.0f;
 #pragma unroll
@@ -174,88 +199,148 @@ __global__ void __launch_bounds__(AW_THREADS) weights_kernel(const Weights wa) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) x[0][k] = y[k];
       }
-      if (t < NR) {
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-          const int c = c0 + e * TPR;
-          if (c < CPR) *reinterpret_cast<uint4*>(smem_q + (c >> 3) * (NR * 128) + t * 128 + (((c & 7) ^ (t & 7)) * 16)) = make_uint4(x[e][0], x[e][1], x[e][2], x[e][3]);
-        }
-        if (c0 == 0) {
-          const float l = live ? wa.lse[(i64)(rq.row0 + fr) * a.heads + hq] : -INFINITY;
-          const i64 see = (i64)rq.pos0 + fr + 1;
-          s_scale[t] = a.scale2 * factor;
-          s_lse[t] = l * LOG2E;
-          s_see[t] = l == -INFINITY || see < 0 ? 0 : see > n ? n : (int)see;          // a row that saw nothing gave nothing
-        }
+      for (int e = 0; e < EACH; ++e) {
+        const int c = c0 + e * TPR;
+        if (c < CPR) *reinterpret_cast<uint4*>(smem_q + (c >> 3) * (HELD * 128) + t * 128 + (((c & 7) ^ (t & 7)) * 16)) = make_uint4(x[e][0], x[e][1], x[e][2], x[e][3]);
+      }
+      if (c0 == 0) {
+        const float l = live ? wa.lse[(i64)(rq.row0 + fr) * a.heads + hq] : INFINITY;
+        const float hi = l * LOG2E;
+        // l log2 e as two numbers; an infinity is one
+        s_lse[t] = make_float2(hi, fabsf(hi) < INFINITY ? fmaf(l, LOG2E, -hi) + l * LOG2E_REST : 0.0f);
+        if (SCALED) s_factor[t] = factor;
+        const i64 see = (i64)rq.pos0 + fr + 1;
+        const int s = !live ? 0x7FFFFFFF : l == -INFINITY || see < 0 ? 0 : see > n ? n : (int)see;          // a row that saw nothing gave nothing
+        s_see[t] = s;
+        atomicMin(&s_min, s);
       }
     }
-    if (!PACKED) cp_wait<0>();
+  };
+  load_q(0);
+  const u32 smem_k = smem_addr(smem), smem_qa = smem_addr(smem_q);
+  constexpr u32 QK = aw_desc(F16, KT, NR);
+  const bool fits = rows <= HELD;
+  bool timeout = false;
+  u32 phases = 0;                              // parity of both barriers
+  for (int t = 0; t < tiles; ++t) {
+    if (PACKED) unpack();
+    // the next tile: its rows' places, then its bytes
+    const i64 next = place(t + 1, id);
+    id = look_up(t + 2);
+    if (tid < KT) s_row[(t + 1) & 1][tid] = next;
+    if (PACKED) fetch(t + 1, next);
+    else {
+      __syncthreads();
+      if (t + 1 < tiles) issue(t + 1);
+      cp_commit();
+      cp_wait<1>();
+    }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    if (warp == 0 && elected()) {
-      constexpr u32 QK = aw_desc(F16, KT, NR);
-      const u64 ka = operand_desc(smem_k, 0), qb = operand_desc(smem_qa, 0);
+    const int key0 = first + t * KT, key = key0 + mine;
+    const bool have = s_row[t & 1][mine] >= 0;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int row0 = 0; row0 < rows; row0 += HELD) {
+      if (!fits && (t > 0 || row0 > 0)) {
+        __syncthreads();                      // (all scores against the rows that lie there have been read)
+        if (tid == 0) s_min = 0x7FFFFFFF;
+        __syncthreads();
+        load_q(row0);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      }
+      tc_fence_before();
+      __syncthreads();
+      tc_fence_after();
+      const int chunks = (min(HELD, rows - row0) + NR - 1) / NR;
+      auto products = [&](int c) {
+        if (warp == 0 && elected()) {
+          const u64 ka = operand_desc(smem_k + (PACKED ? 0 : t & 1) * KB, 0), qb = operand_desc(smem_qa + c * NR * 128, 0);
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k)
-        mma_ss(tmem, ka + (u64)(((k >> 2) * (KT * 128) + (k & 3) * 32) >> 4), qb + (u64)(((k >> 2) * (NR * 128) + (k & 3) * 32) >> 4), QK, k > 0);
-      tc_commit(&s_bar);
-    }
-    __syncwarp();
-    const bool ok = bar_wait(&s_bar, phase, a.polls, &s_gave_up);
-    if (__syncthreads_or(!ok)) {              // what is in flight is awaited with the built-in limit
-      bar_drain(&s_bar, phase);
-      timeout = true;
-      break;
-    }
-    phase ^= 1;
-    tc_fence_after();
-    const u32 base = tmem + ((u32)(32 * warp) << 16);
+          for (int k = 0; k < D / 16; ++k) {
+            const int box = k >> 2, x = box / Shape::PER;
+            mma_ss(tmem + ((c & 1) * SUMS + x) * NR, ka + (u64)((box * (KT * 128) + (k & 3) * 32) >> 4), qb + (u64)((box * (HELD * 128) + (k & 3) * 32) >> 4), QK, k > 4 * x * Shape::PER);
+          }
+          tc_commit(&s_bar[c & 1]);
+        }
+        __syncwarp();
+      };
+      products(0);
+      const bool whole = s_min >= key0 + KT;  // every row sees every token of the tile
+      for (int c = 0; c < chunks; ++c) {
+        if (c + 1 < chunks) {
+          tc_fence_before();
+          if (c > 0) __syncthreads();         // the scores before these have been read by all
+          tc_fence_after();
+          products(c + 1);
+        }
+        if (!bar_wait(&s_bar[c & 1], (phases >> (c & 1)) & 1, a.polls, &s_gave_up)) {       // what is in flight is awaited with the built-in limit
+          timeout = true;
+          bar_drain(&s_bar[c & 1], (phases >> (c & 1)) & 1);
+        }
+        phases ^= 1u << (c & 1);
+        tc_fence_after();
+        const u32 base = lanes + (c & 1) * SUMS * NR;
 #pragma unroll
-    for (int c = 0; c < COLS; c += 32) {
-      float v[32];
-      tc_ld32(v, base + c);
-      tc_wait_ld();
-      tc_loaded(v);
+        for (int i0 = 0; i0 < NR; i0 += 32) {
+          constexpr int W = NR < 32 ? NR : 32;
+          float v[SUMS][32];
 #pragma unroll
-      for (int i = 0; i < (NR < 32 ? NR : 32); ++i) {
-        const float p = exp2_fast(__fmul_rn(v[i], s_scale[c + i]) - s_lse[c + i]);
-        sum[i & 3] += key < s_see[c + i] ? p : 0.0f;
+          for (int x = 0; x < SUMS; ++x) {
+            if (W == 32) tc_ld32(v[x], base + x * NR + i0);
+            else tc_ld16(v[x], base + x * NR);
+          }
+          tc_wait_ld();
+#pragma unroll
+          for (int x = 0; x < SUMS; ++x) tc_loaded(v[x]);
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            const int row = c * NR + i0 + i;
+            float s = v[0][i];
+#pragma unroll
+            for (int x = 1; x < SUMS; ++x) s += v[x][i];
+            if (SCALED) s *= s_factor[row];
+            const float2 l = s_lse[row];
+            const float p = exp2_fast(fmaf(s, wa.scale_hi, -l.x) + fmaf(s, wa.scale_lo, -l.y));
+            if (whole) sum[i & 3] += p;
+            else sum[i & 3] += key < s_see[row] ? p : 0.0f;
+          }
+        }
       }
     }
+    if (writes && key < n) {
+      const float w = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      if (!have) {
+        if (!wa.add) out[key] = 0.0f;
+      } else out[key] = wa.add ? out[key] + w : w;
+    }
     tc_fence_before();
-    __syncthreads();                          // before the next chunk takes Q's place
+    __syncthreads();                          // before the next tile takes the place of this one
+    tc_fence_after();
   }
-  if (writes && key < wa.width && !timeout) {
-    const float w = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    if (key >= n || !have) {
-      if (!wa.add) out[key] = 0.0f;
-    } else out[key] = wa.add ? out[key] + w : w;
-  }
-  tc_fence_before();
-  __syncthreads();
-  if (warp == 0) {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(COLS) : "memory");
-    if (lane == 0 && timeout && a.status) atomicOr(a.status, PTSTORE_S_TIMEOUT);
-  }
+  cp_wait<0>();
+  if ((bounds || timeout) && a.status) atomicOr(a.status, (bounds ? PTSTORE_S_BOUNDS : 0) | (timeout ? PTSTORE_S_TIMEOUT : 0));
+  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(Shape::COLS) : "memory");
 }
 
 template <bool PACKED, bool F16, bool QFP16, int D, int NR>
 int launch(Weights wa, const Gpu& gpu, cudaStream_t s) {
+  using Shape = WeightsShape<PACKED, D, NR>;
   static std::atomic<u64> devices{0};
   auto* kernel = weights_kernel<PACKED, F16, QFP16, D, NR>;
-  const int rc = allow_smem(kernel, aw_smem<D, NR>(), devices, gpu.dev);
+  const int rc = allow_smem(kernel, Shape::SMEM, devices, gpu.dev);
   if (rc) return rc;
-  wa.tiles = (wa.width + aw_keys<D>() - 1) / aw_keys<D>();
+  // Tiles of a CTA: as many as leave every SM several CTAs, at most eight (what a CTA does once is then an eighth of a tile's work)
+  const i64 tiles = (wa.width + Shape::KT - 1) / Shape::KT, all = tiles * wa.a.R * wa.a.cache.heads, fill = (i64)gpu.sms * (D > 128 ? 2 : 6);
+  wa.each = (int)(all / fill < 1 ? 1 : all / fill > 8 ? 8 : all / fill);
+  wa.tiles = (int)((tiles + wa.each - 1) / wa.each);
   const u64 grid = (u64)wa.tiles * wa.a.R * wa.a.cache.heads;
   if (grid > 0x7FFFFFFF) return PTSTORE_E_LIMIT;
-  kernel<<<(unsigned)grid, AW_THREADS, aw_smem<D, NR>(), s>>>(wa);
+  kernel<<<(unsigned)grid, AW_THREADS, Shape::SMEM, s>>>(wa);
   return cudaGetLastError() == cudaSuccess ? PTSTORE_OK : PTSTORE_E_CUDA;
 }
 template <bool PACKED, bool F16, bool QFP16, int D>
 int launch_rows(const Weights& wa, i64 rows, const Gpu& gpu, cudaStream_t s) {
-  return rows <= 16 ? launch<PACKED, F16, QFP16, D, 16>(wa, gpu, s) : launch<PACKED, F16, QFP16, D, aw_many<D>()>(wa, gpu, s);
+  return rows <= 16 ? launch<PACKED, F16, QFP16, D, 16>(wa, gpu, s) : launch<PACKED, F16, QFP16, D, 64>(wa, gpu, s);
 }
 
 }  // namespace
@@ -269,8 +354,9 @@ extern "C" int ptstore_attend_weights(const ptstore_attend_weights_t* p, const p
   if (p->dtype != PTSTORE_KV_BF16 && p->dtype != PTSTORE_KV_FP16) return PTSTORE_E_INVAL;
   const bool packed = cache->format == PTSTORE_KV_PACKED, half = p->dtype == PTSTORE_KV_FP16;
   if (!packed && (cache->format & 3u) != p->dtype) return PTSTORE_E_INVAL;                   // (the latent formats' lowest bits are the 16-bit types)
-  const float scale2 = p->scale * LOG2E * (packed ? cache->k_scale * DEQ_FACTOR : 1.0f);
-  if (!isfinite(scale2)) return PTSTORE_E_INVAL;
+  const double scale2 = (double)p->scale * 1.4426950408889634074 * (packed ? (double)cache->k_scale * DEQ_FACTOR : 1.0);
+  const float scale_hi = (float)scale2;
+  if (!isfinite(scale_hi)) return PTSTORE_E_INVAL;
   if (p->requests == 0 || p->width == 0 || (p->accumulate && p->tokens == 0)) return PTSTORE_OK;
   if (!p->token_offsets || !p->lengths || !p->block_tables || !p->weights) return PTSTORE_E_INVAL;
   if (p->tokens > 0 && (!p->q || !p->lse || !rows_aligned(p->q, p->tokens, p->q_token_stride, p->num_heads, p->q_head_stride))) return PTSTORE_E_INVAL;
@@ -285,7 +371,6 @@ extern "C" int ptstore_attend_weights(const ptstore_attend_weights_t* p, const p
   a.offsets = p->token_offsets; a.lengths = p->lengths; a.tables = p->block_tables;
   a.R = p->requests; a.max_blocks = p->max_blocks; a.heads = p->num_heads; a.tokens = p->tokens;
   a.group = p->num_heads / (int)cache->num_kv_heads;
-  a.scale2 = scale2;
   a.polls = p->wait_polls ? p->wait_polls : POLLS;
   a.status = status;
   wa.lse = p->lse;
@@ -293,6 +378,8 @@ extern "C" int ptstore_attend_weights(const ptstore_attend_weights_t* p, const p
   wa.o_request = p->weights_request_stride; wa.o_head = p->weights_head_stride;
   wa.width = p->width;
   wa.add = p->accumulate != 0;
+  wa.scale_hi = scale_hi;
+  wa.scale_lo = (float)(scale2 - scale_hi);
   Gpu gpu;
   (void)cudaGetLastError();
   const int rs = current_gpu(&gpu);
