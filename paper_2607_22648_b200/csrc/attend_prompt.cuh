@@ -97,18 +97,22 @@ __device__ __forceinline__ void tc_ld32(float (&v)[32], u32 addr) {
                  "=f"(r[25]), "=f"(r[26]), "=f"(r[27]), "=f"(r[28]), "=f"(r[29]), "=f"(r[30]), "=f"(r[31])
                : "r"(addr) : "memory");
 }
-// 16 columns likewise, into the first half of v
-__device__ __forceinline__ void tc_ld16(float (&v)[32], u32 addr) {
-  float* r = v;
+// 8 and 16 columns likewise
+__device__ __forceinline__ void tc_ld(float (&r)[8], u32 addr) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tc_ld(float (&r)[16], u32 addr) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]), "=f"(r[10]), "=f"(r[11]), "=f"(r[12]),
                  "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
                : "r"(addr) : "memory");
 }
 // values of a load may be used from here on (after tc_wait_ld): keeps the compiler from moving their uses above the wait
-__device__ __forceinline__ void tc_loaded(float (&v)[32]) {
+template <int N>
+__device__ __forceinline__ void tc_loaded(float (&v)[N]) {
 #pragma unroll
-  for (int i = 0; i < 32; i += 8)
+  for (int i = 0; i < N; i += 8)
     asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]), "+f"(v[i + 6]), "+f"(v[i + 7]));
 }
 __device__ __forceinline__ void tc_st32(u32 addr, const u32 (&r)[32]) {
@@ -155,6 +159,11 @@ __device__ __forceinline__ u64 fma_pair(u64 a, u64 b, u64 c) {
 __device__ __forceinline__ u64 add_pair(u64 a, u64 b) {
   u64 r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ u64 mul_pair(u64 a, u64 b) {
+  u64 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
 __device__ __forceinline__ float lo_of(u64 v) { return __uint_as_float((u32)v); }

@@ -7,8 +7,10 @@
 // read once and nothing else of the cache.  The next tile is on its way while one is computed with, and Q stays where it is while its rows fit.  A decode step is bound by
 // reading K, a window of many rows by its exponentials.
 //
-// Weights keep what 32 bits can hold of them: scores are summed up in two or three accumulators (the tensor cores cut off what does not fit the running sum, an error that grows with its
-// length and size), and scale and lse, times log2 e, are kept as two numbers each (a rounding of an exponent of 20 is 2^-20 of the weight).
+// Weights keep what 32 bits can hold of them: scores are summed up in several accumulators (the tensor cores cut off what does not fit the running sum, an error that grows with its
+// length: rows of 576 elements in one / three / nine / eighteen sums were 9.5 / 3.6 / 1.7 / 1.4e-6 off, 32-bit products of a library 1.1e-6), and scale and lse, times log2 e, are kept as two numbers each (a rounding of an exponent of 20 is 2^-20 of the weight).
+#include <type_traits>
+
 #include "attend_prompt.cuh"
 #include "launch.cuh"
 
@@ -26,17 +28,19 @@ struct Weights {
   bool add;
 };
 
-constexpr int AW_THREADS = 128;
+constexpr int AW_THREADS = 256;             // two warpgroups, which share the rows of a chunk
 constexpr float LOG2E_REST = (float)(1.4426950408889634074 - (double)LOG2E);          // what 32 bits leave of log2 e
 template <bool PACKED, int D, int NR>
 struct WeightsShape {
   // tokens of a tile: all 128 rows of the instruction, but for latent rows, of which two tiles have to fit an SM beside Q
   static constexpr int KT = D > 128 ? 64 : 128;
-  static constexpr int BOXES = D / 64, SUMS = D == 64 ? 1 : D == 128 ? 2 : 3, PER = (BOXES + SUMS - 1) / SUMS;      // accumulators, boxes of 64 elements of each
+  // instructions of 16 elements that share an accumulator, accumulators
+  static constexpr int PER = NR == 16 ? 2 : D > 128 ? 6 : 4, SUMS = (D / 16 + PER - 1) / PER;
   static constexpr int HELD = NR == 16 ? 16 : D > 128 ? 64 : 128;                                                   // rows of Q that stay in shared memory
   static constexpr int STAGES = PACKED ? 1 : 2, K_BYTES = KT * D * 2, Q_BYTES = HELD * D * 2;
   static constexpr int SMEM = STAGES * K_BYTES + Q_BYTES + 1024;
-  static constexpr int NEED = 2 * SUMS * NR, COLS = NEED <= 32 ? 32 : NEED <= 64 ? 64 : NEED <= 128 ? 128 : NEED <= 256 ? 256 : 512;
+  static constexpr int CTAS = 230000 / (SMEM + 3072) < 1 ? 1 : 230000 / (SMEM + 3072);       // of an SM, by shared memory
+  static constexpr int NEED = SUMS * NR, COLS = NEED <= 32 ? 32 : NEED <= 64 ? 64 : NEED <= 128 ? 128 : NEED <= 256 ? 256 : 512;
 };
 
 __host__ __device__ constexpr u32 aw_desc(bool fp16, int M, int N) {       // both operands with a row's elements contiguous
@@ -44,20 +48,21 @@ __host__ __device__ constexpr u32 aw_desc(bool fp16, int M, int N) {       // bo
 }
 
 template <bool PACKED, bool F16, bool QFP16, int D, int NR>
-__global__ void __launch_bounds__(AW_THREADS) weights_kernel(const Weights wa) {
+__global__ void __launch_bounds__(AW_THREADS, D > 128 ? 1 : 3) weights_kernel(const Weights wa) {
   using Shape = WeightsShape<PACKED, D, NR>;
   constexpr int KT = Shape::KT, CPR = D / 8, SUMS = Shape::SUMS, HELD = Shape::HELD, KB = Shape::K_BYTES;
   constexpr bool SCALED = PACKED && !QFP16;                   // bf16 rows over the 4-bit cache have a factor each
   extern __shared__ unsigned char smem_raw[];
   unsigned char* const smem = smem_raw + ((1024 - (smem_addr(smem_raw) & 1023)) & 1023);
   unsigned char* const smem_q = smem + Shape::STAGES * KB;
-  __shared__ __align__(8) u64 s_bar[2];
+  __shared__ __align__(8) u64 s_bar;
   __shared__ u32 s_tmem;
   __shared__ int s_gave_up, s_min;
   __shared__ i64 s_row[2][KT];                                // where a tile's rows lie, -1: not there
-  __shared__ float2 s_lse[HELD];
-  __shared__ float s_factor[SCALED ? HELD : 1];
-  __shared__ int s_see[HELD];
+  __shared__ __align__(16) float s_lse[2 * HELD];             // of two rows at a time: - lse log2 e, what 32 bits leave of it
+  __shared__ __align__(8) float s_factor[SCALED ? HELD : 2];
+  __shared__ float s_part[KT];
+  __shared__ __align__(8) int s_see[HELD];
   const Attend& a = wa.a;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0);
   const u32 rh = blockIdx.x / (u32)wa.tiles, h = rh % a.cache.heads;
@@ -73,8 +78,8 @@ __global__ void __launch_bounds__(AW_THREADS) weights_kernel(const Weights wa) {
     for (int j = max(first, n) + tid; j < end; j += AW_THREADS) out[j] = 0.0f;
   if (first >= n) return;
   const int tiles = (min(n, end) - first + KT - 1) / KT;
-  // the scores of 64 tokens lie in the first 16 lanes of each warp
-  const int mine = KT == 128 ? tid : warp * 16 + (lane & 15);
+  // the thread's token; the scores of 64 tokens lie in the first 16 lanes of each warp
+  const int group = warp >> 2, mine = KT == 128 ? tid & 127 : (warp & 3) * 16 + (lane & 15);
   const bool writes = KT == 128 || lane < 16;
 
   const u32 B = a.cache.block_tokens;
@@ -100,45 +105,43 @@ __global__ void __launch_bounds__(AW_THREADS) weights_kernel(const Weights wa) {
       cp_async16_or_zero(dst + (c >> 3) * (KT * 128) + row * 128 + (((c & 7) ^ (row & 7)) * 16), a.cache.base + (at < 0 ? 0 : at) + c * 16, at >= 0);
     }
   };
-  // 4-bit: one token a thread, codes and scales on their way in registers, then unpacked to fp16 (element order 0 4 1 5 2 6 3 7 inside eight, as the unpacking yields them; Q is stored likewise)
-  uint4 code[PACKED ? D / 32 : 1];
-  uint2 scales;
+  // 4-bit: half a token a thread, codes and scales on their way in registers, then unpacked to fp16 (element order 0 4 1 5 2 6 3 7 inside eight, as the unpacking yields them; Q is stored likewise)
+  constexpr int HALF = PACKED ? D / 64 : 1;    // chunks of 32 elements of a thread: two threads have a token
+  uint4 code[HALF];
+  u32 scales;
   const Magic mg = magic();
-  auto fetch = [&](int t, i64 at) {
+  auto fetch = [&](int t) {
     if (!PACKED) return;
-    const int m = (u32)(first + t * KT + tid) % TILE;
+    const i64 at = s_row[t & 1][mine];
+    const int m = (u32)(first + t * KT + mine) % TILE;
     const unsigned char* const src = a.cache.base + (at < 0 ? 0 : at);
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c) code[PACKED ? c : 0] = at >= 0 ? *reinterpret_cast<const uint4*>(src + code_place(D, m, c) * 16) : make_uint4(0, 0, 0, 0);
-    scales = make_uint2(0, 0);
+    for (int c = 0; c < HALF; ++c) code[c] = at >= 0 ? *reinterpret_cast<const uint4*>(src + code_place(D, m, group * HALF + c) * 16) : make_uint4(0, 0, 0, 0);
+    scales = 0;
     if (at >= 0) {
-      if (D == 128) scales = *reinterpret_cast<const uint2*>(src + scale_at(D, false, m, 0));
-      else scales.x = *reinterpret_cast<const u32*>(src + scale_at(D, false, m, 0));
+      const unsigned char* const sc = src + scale_at(D, false, m, 0);
+      scales = D == 128 ? *reinterpret_cast<const u32*>(sc + 4 * group) : (u32)*reinterpret_cast<const unsigned short*>(sc + 2 * group);
     }
   };
   auto unpack = [&]() {
     if (!PACKED) return;
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c) {
-      const u32 two = ((c & 2 ? scales.y : scales.x) >> (16 * (c & 1))) & 0xFFFFu;          // two scale groups of a chunk of 32 elements
+    for (int c = 0; c < HALF; ++c) {
+      const u32 two = (scales >> (16 * c)) & 0xFFFFu;          // two scale groups of a chunk of 32 elements
       const Deq d0 = deq_of(e4m3x2_to_half2((two & 0xFFu) * 0x101u)), d1 = deq_of(e4m3x2_to_half2((two >> 8) * 0x101u));
-      const uint4 four = code[PACKED ? c : 0];
-      const u32 w[4] = {four.x, four.y, four.z, four.w};
+      const u32 w[4] = {code[c].x, code[c].y, code[c].z, code[c].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         u32 o[4];
         deq4(w[i], w[i] >> 8, i < 2 ? d0 : d1, mg, o);
-        *reinterpret_cast<uint4*>(smem + operand_at(tid, 4 * c + i)) = make_uint4(o[0], o[1], o[2], o[3]);
+        *reinterpret_cast<uint4*>(smem + operand_at(mine, 4 * (group * HALF + c) + i)) = make_uint4(o[0], o[1], o[2], o[3]);
       }
     }
   };
-  i64 at = place(0, look_up(0));
+  if (tid < KT) s_row[0][tid] = place(0, look_up(0));
   int id = look_up(1);
-  if (tid < KT) s_row[0][tid] = at;
-  if (PACKED) fetch(0, at);
   if (tid == 0) {
-    bar_init(&s_bar[0], 1);
-    bar_init(&s_bar[1], 1);
+    bar_init(&s_bar, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s_gave_up = 0;
     s_min = 0x7FFFFFFF;
@@ -150,17 +153,18 @@ __global__ void __launch_bounds__(AW_THREADS) weights_kernel(const Weights wa) {
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const u32 tmem = s_tmem, lanes = tmem + ((u32)(32 * warp) << 16);
-  if (!PACKED) {
+  const u32 tmem = s_tmem, lanes = tmem + ((u32)(32 * (warp & 3)) << 16);
+  if (PACKED) fetch(0);
+  else {
     issue(0);
     cp_commit();
   }
   // ---- rows row0 .. row0 + HELD - 1 of Q, in the products' type; rows that do not exist are zero and give nothing
   auto load_q = [&](int row0) {
     constexpr int TPR = D > 128 ? 32 : CPR, EACH = (CPR + TPR - 1) / TPR, PASS = AW_THREADS / TPR;
-    const int m = min(HELD, rows - row0);
+    const int m = min(HELD, rows - row0), padded = (m + NR - 1) / NR * NR;
 #pragma unroll 2
-    for (int p = 0; p < HELD && p < ((m + NR - 1) / NR) * NR; p += PASS) {
+    for (int p = 0; p < padded; p += PASS) {
       const int t = p + tid / TPR, c0 = tid % TPR;
       const int flat = row0 + t, fr = flat / a.group, hq = (int)h * a.group + flat % a.group;
       const bool live = t < m;
@@ -199,6 +203,7 @@ __global__ void __launch_bounds__(AW_THREADS) weights_kernel(const Weights wa) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) x[0][k] = y[k];
       }
+      if (t >= padded) continue;
 #pragma unroll
       for (int e = 0; e < EACH; ++e) {
         const int c = c0 + e * TPR;
@@ -208,7 +213,8 @@ __global__ void __launch_bounds__(AW_THREADS) weights_kernel(const Weights wa) {
         const float l = live ? wa.lse[(i64)(rq.row0 + fr) * a.heads + hq] : INFINITY;
         const float hi = l * LOG2E;
         // l log2 e as two numbers; an infinity is one
-        s_lse[t] = make_float2(hi, fabsf(hi) < INFINITY ? fmaf(l, LOG2E, -hi) + l * LOG2E_REST : 0.0f);
+        s_lse[(t & ~1) * 2 + (t & 1)] = -hi;
+        s_lse[(t & ~1) * 2 + 2 + (t & 1)] = fabsf(hi) < INFINITY ? -(fmaf(l, LOG2E, -hi) + l * LOG2E_REST) : 0.0f;
         if (SCALED) s_factor[t] = factor;
         const i64 see = (i64)rq.pos0 + fr + 1;
         const int s = !live ? 0x7FFFFFFF : l == -INFINITY || see < 0 ? 0 : see > n ? n : (int)see;          // a row that saw nothing gave nothing
@@ -222,15 +228,15 @@ __global__ void __launch_bounds__(AW_THREADS) weights_kernel(const Weights wa) {
   constexpr u32 QK = aw_desc(F16, KT, NR);
   const bool fits = rows <= HELD;
   bool timeout = false;
-  u32 phases = 0;                              // parity of both barriers
+  u32 phase = 0;
+  const u64 hi2 = pair(wa.scale_hi, wa.scale_hi), lo2 = pair(wa.scale_lo, wa.scale_lo);
   for (int t = 0; t < tiles; ++t) {
     if (PACKED) unpack();
     // the next tile: its rows' places, then its bytes
     const i64 next = place(t + 1, id);
     id = look_up(t + 2);
     if (tid < KT) s_row[(t + 1) & 1][tid] = next;
-    if (PACKED) fetch(t + 1, next);
-    else {
+    if (!PACKED) {
       __syncthreads();
       if (t + 1 < tiles) issue(t + 1);
       cp_commit();
@@ -239,7 +245,7 @@ __global__ void __launch_bounds__(AW_THREADS) weights_kernel(const Weights wa) {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     const int key0 = first + t * KT, key = key0 + mine;
     const bool have = s_row[t & 1][mine] >= 0;
-    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    u64 sum[2] = {0, 0};
     for (int row0 = 0; row0 < rows; row0 += HELD) {
       if (!fits && (t > 0 || row0 > 0)) {
         __syncthreads();                      // (all scores against the rows that lie there have been read)
@@ -248,74 +254,86 @@ __global__ void __launch_bounds__(AW_THREADS) weights_kernel(const Weights wa) {
         load_q(row0);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       }
-      tc_fence_before();
-      __syncthreads();
-      tc_fence_after();
       const int chunks = (min(HELD, rows - row0) + NR - 1) / NR;
-      auto products = [&](int c) {
+      for (int c = 0; c < chunks; ++c) {
+        // operands are there, and the scores before these have been read by all
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
         if (warp == 0 && elected()) {
           const u64 ka = operand_desc(smem_k + (PACKED ? 0 : t & 1) * KB, 0), qb = operand_desc(smem_qa + c * NR * 128, 0);
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            const int box = k >> 2, x = box / Shape::PER;
-            mma_ss(tmem + ((c & 1) * SUMS + x) * NR, ka + (u64)((box * (KT * 128) + (k & 3) * 32) >> 4), qb + (u64)((box * (HELD * 128) + (k & 3) * 32) >> 4), QK, k > 4 * x * Shape::PER);
-          }
-          tc_commit(&s_bar[c & 1]);
+          for (int k = 0; k < D / 16; ++k)
+            mma_ss(tmem + k / Shape::PER * NR, ka + (u64)(((k >> 2) * (KT * 128) + (k & 3) * 32) >> 4), qb + (u64)(((k >> 2) * (HELD * 128) + (k & 3) * 32) >> 4), QK, k % Shape::PER > 0);
+          tc_commit(&s_bar);
         }
         __syncwarp();
-      };
-      products(0);
-      const bool whole = s_min >= key0 + KT;  // every row sees every token of the tile
-      for (int c = 0; c < chunks; ++c) {
-        if (c + 1 < chunks) {
-          tc_fence_before();
-          if (c > 0) __syncthreads();         // the scores before these have been read by all
-          tc_fence_after();
-          products(c + 1);
-        }
-        if (!bar_wait(&s_bar[c & 1], (phases >> (c & 1)) & 1, a.polls, &s_gave_up)) {       // what is in flight is awaited with the built-in limit
+        if (PACKED && row0 == 0 && c == 0 && t + 1 < tiles) fetch(t + 1);
+        const bool whole = s_min >= key0 + KT;                // every row sees every token of the tile
+        if (!bar_wait(&s_bar, phase, a.polls, &s_gave_up)) {  // what is in flight is awaited with the built-in limit
           timeout = true;
-          bar_drain(&s_bar[c & 1], (phases >> (c & 1)) & 1);
+          bar_drain(&s_bar, phase);
         }
-        phases ^= 1u << (c & 1);
+        phase ^= 1;
         tc_fence_after();
-        const u32 base = lanes + (c & 1) * SUMS * NR;
+        // this warpgroup's rows of the chunk, W at a time
+        constexpr int W = NR == 16 ? 8 : 16;
 #pragma unroll
-        for (int i0 = 0; i0 < NR; i0 += 32) {
-          constexpr int W = NR < 32 ? NR : 32;
-          float v[SUMS][32];
+        for (int i0 = 0; i0 < NR / 2; i0 += W) {
+          const int at0 = group * (NR / 2) + i0;
+          u64 s[W / 2];
 #pragma unroll
-          for (int x = 0; x < SUMS; ++x) {
-            if (W == 32) tc_ld32(v[x], base + x * NR + i0);
-            else tc_ld16(v[x], base + x * NR);
+          for (int x0 = 0; x0 < SUMS; x0 += 2) {
+            float v[2][W];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+              if (x0 + x < SUMS) tc_ld(v[x], lanes + (x0 + x) * NR + at0);
+            tc_wait_ld();
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+              if (x0 + x < SUMS) {
+                tc_loaded(v[x]);
+#pragma unroll
+                for (int i = 0; i < W; i += 2) {
+                  const u64 two = pair(v[x][i], v[x][i + 1]);
+                  s[i / 2] = x0 + x == 0 ? two : add_pair(s[i / 2], two);
+                }
+              }
           }
-          tc_wait_ld();
+          auto give = [&](auto all) {
 #pragma unroll
-          for (int x = 0; x < SUMS; ++x) tc_loaded(v[x]);
-#pragma unroll
-          for (int i = 0; i < W; ++i) {
-            const int row = c * NR + i0 + i;
-            float s = v[0][i];
-#pragma unroll
-            for (int x = 1; x < SUMS; ++x) s += v[x][i];
-            if (SCALED) s *= s_factor[row];
-            const float2 l = s_lse[row];
-            const float p = exp2_fast(fmaf(s, wa.scale_hi, -l.x) + fmaf(s, wa.scale_lo, -l.y));
-            if (whole) sum[i & 3] += p;
-            else sum[i & 3] += key < s_see[row] ? p : 0.0f;
-          }
+            for (int i = 0; i < W; i += 2) {
+              const int row = c * NR + at0 + i;
+              const float4 l = *reinterpret_cast<const float4*>(&s_lse[2 * row]);
+              u64 y = s[i / 2];
+              if (SCALED) y = mul_pair(y, *reinterpret_cast<const u64*>(&s_factor[row]));
+              const u64 e = add_pair(fma_pair(y, hi2, pair(l.x, l.y)), fma_pair(y, lo2, pair(l.z, l.w)));
+              float p0 = exp2_fast(lo_of(e)), p1 = exp2_fast(hi_of(e));
+              if (!decltype(all)::value) {
+                const int2 see = *reinterpret_cast<const int2*>(&s_see[row]);
+                p0 = key < see.x ? p0 : 0.0f;
+                p1 = key < see.y ? p1 : 0.0f;
+              }
+              sum[(i >> 1) & 1] = add_pair(sum[(i >> 1) & 1], pair(p0, p1));
+            }
+          };
+          if (whole) give(std::true_type{});
+          else give(std::false_type{});
         }
       }
     }
-    if (writes && key < n) {
-      const float w = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      if (!have) {
-        if (!wa.add) out[key] = 0.0f;
-      } else out[key] = wa.add ? out[key] + w : w;
-    }
+    const u64 both = add_pair(sum[0], sum[1]);
+    const float w = lo_of(both) + hi_of(both);
+    if (group == 1 && writes) s_part[mine] = w;
     tc_fence_before();
     __syncthreads();                          // before the next tile takes the place of this one
     tc_fence_after();
+    if (group == 0 && writes && key < n) {
+      const float all = w + s_part[mine];
+      if (!have) {
+        if (!wa.add) out[key] = 0.0f;
+      } else out[key] = wa.add ? out[key] + all : all;
+    }
   }
   cp_wait<0>();
   if ((bounds || timeout) && a.status) atomicOr(a.status, (bounds ? PTSTORE_S_BOUNDS : 0) | (timeout ? PTSTORE_S_TIMEOUT : 0));
@@ -329,9 +347,9 @@ int launch(Weights wa, const Gpu& gpu, cudaStream_t s) {
   auto* kernel = weights_kernel<PACKED, F16, QFP16, D, NR>;
   const int rc = allow_smem(kernel, Shape::SMEM, devices, gpu.dev);
   if (rc) return rc;
-  // Tiles of a CTA: as many as leave every SM several CTAs, at most eight (what a CTA does once is then an eighth of a tile's work)
-  const i64 tiles = (wa.width + Shape::KT - 1) / Shape::KT, all = tiles * wa.a.R * wa.a.cache.heads, fill = (i64)gpu.sms * (D > 128 ? 2 : 6);
-  wa.each = (int)(all / fill < 1 ? 1 : all / fill > 8 ? 8 : all / fill);
+  // Tiles of a CTA: one round of CTAs where that takes at most 16 each, else rounds of 8 (what a CTA does once is then a small part of its time)
+  const i64 tiles = (wa.width + Shape::KT - 1) / Shape::KT, rows = (i64)wa.a.R * wa.a.cache.heads, parts = (i64)gpu.sms * Shape::CTAS / rows;
+  wa.each = parts > 0 && (tiles + parts - 1) / parts <= 16 ? (int)((tiles + parts - 1) / parts) : 8;
   wa.tiles = (int)((tiles + wa.each - 1) / wa.each);
   const u64 grid = (u64)wa.tiles * wa.a.R * wa.a.cache.heads;
   if (grid > 0x7FFFFFFF) return PTSTORE_E_LIMIT;
