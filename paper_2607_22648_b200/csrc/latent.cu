@@ -67,30 +67,34 @@ int run_rows(void* latent, i64 latent_stride, void* rope, i64 rope_stride, i64 t
   return cudaGetLastError() == cudaSuccess ? PTSTORE_OK : PTSTORE_E_CUDA;
 }
 
-// The tensor map of the cache: {64 elements, tokens of a block, groups of 64 elements, blocks}, boxes of all elements of 8 tokens
-bool make_rows_map(const Cache& c, bool half, int dim, CUtensorMap* map) {
-  const cuuint64_t dims[4] = {64, c.block_tokens, (cuuint64_t)dim / 64, c.num_blocks};
-  const cuuint64_t strides[3] = {(cuuint64_t)dim * 2, 128, c.block_stride};
-  const cuuint32_t boxes[4] = {64, 8, (cuuint32_t)dim / 64, 1};
-  return encode(map, half, 4, c.base, dims, strides, boxes);
+// The tensor map of the cache: {elements, tokens of a block, blocks}, boxes of 64 elements and the largest power of two of tokens, up to 64, that divides a block's.  Returns the
+// tokens of a box, 0 if there is no map.
+u32 make_rows_map(const Cache& c, bool half, int dim, CUtensorMap* map) {
+  u32 box = LA_KEYS;
+  while (c.block_tokens % box) box >>= 1;
+  const cuuint64_t dims[3] = {(cuuint64_t)dim, c.block_tokens, c.num_blocks};
+  const cuuint64_t strides[2] = {(cuuint64_t)dim * 2, c.block_stride};
+  const cuuint32_t boxes[3] = {64, box, 1};
+  return encode(map, half, 3, c.base, dims, strides, boxes) ? box : 0;
 }
 
-template <int L, bool F16, int PAIR>
+template <int L, bool F16, bool WIDE>
 int launch_latent(const Latent& la, const CUtensorMap& map, const Gpu& gpu, cudaStream_t s) {
+  using Shape = LatentShape<L, WIDE>;
   static std::atomic<u64> devices{0};
-  auto* kernel = latent_attend_kernel<L, F16, PAIR>;
-  constexpr int SMEM = LatentShape<L>::SMEM;
+  auto* kernel = latent_attend_kernel<L, F16, WIDE>;
+  constexpr int SMEM = latent_smem<L, WIDE>();
   const int rc = allow_smem(kernel, SMEM, devices, gpu.dev);
   if (rc) return rc;
-  const int grid = gpu.sms / PAIR * PAIR;
+  const int grid = gpu.sms / Shape::PAIR * Shape::PAIR;
   kernel<<<grid, LA_THREADS, SMEM, s>>>(la, map);
   if (cudaGetLastError() != cudaSuccess) return PTSTORE_E_CUDA;
-  latent_join_kernel<L, F16, PAIR><<<dim3(grid, LA_ROWS / 4), L / 4, 0, s>>>(la, grid);
+  latent_join_kernel<L, F16, WIDE><<<dim3(grid, Shape::ROWS / 8), 256, 0, s>>>(la);
   return cudaGetLastError() == cudaSuccess ? PTSTORE_OK : PTSTORE_E_CUDA;
 }
 template <int L, bool F16>
 int launch_latent_rows(const Latent& la, const CUtensorMap& map, i64 rows, const Gpu& gpu, cudaStream_t s) {
-  return rows > LA_ROWS && gpu.sms >= 2 ? launch_latent<L, F16, 2>(la, map, gpu, s) : launch_latent<L, F16, 1>(la, map, gpu, s);
+  return rows > LatentShape<L, false>::ROWS && gpu.sms >= 2 ? launch_latent<L, F16, true>(la, map, gpu, s) : launch_latent<L, F16, false>(la, map, gpu, s);
 }
 
 }  // namespace
@@ -107,7 +111,8 @@ extern "C" int ptstore_latent_read(const ptstore_kv_cache_t* cache, const int64_
 
 extern "C" uint64_t ptstore_latent_workspace_bytes(uint32_t head_dim) {
   if (head_dim != 320 && head_dim != 576) return 0;
-  return LA_PARTS_AT + (u64)MAX_SMS * 2 * LA_ROWS * (head_dim - LA_ROPE + 2) * 4;            // two sets of sums per CTA
+  // two sets of sums per CTA, of 128 rows and half of the elements or of 32 rows and all of them
+  return LA_PARTS_AT + (u64)MAX_SMS * 2 * 128 * ((head_dim - LA_ROPE) / 2 + 2) * 4;
 }
 
 extern "C" int ptstore_latent_attend(const ptstore_latent_attend_t* p, const ptstore_kv_cache_t* cache, void* workspace, uint64_t workspace_bytes, uint32_t* status,
@@ -151,7 +156,8 @@ extern "C" int ptstore_latent_attend(const ptstore_latent_attend_t* p, const pts
   if (rs) return rs;
   const bool half = cache->format == PTSTORE_KV_LATENT_FP16;
   CUtensorMap map;
-  if (!make_rows_map(a.cache, half, (int)cache->head_dim, &map)) return PTSTORE_E_CUDA;
+  a.box_tokens = make_rows_map(a.cache, half, (int)cache->head_dim, &map);
+  if (!a.box_tokens) return PTSTORE_E_CUDA;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const i64 rows = (i64)(p->max_new < p->tokens ? p->max_new : p->tokens) * a.group;
   if (cache->head_dim == 576) return half ? launch_latent_rows<512, true>(la, map, rows, gpu, s) : launch_latent_rows<512, false>(la, map, rows, gpu, s);

@@ -1,53 +1,59 @@
 // Absorbed attention over a cache of latent vectors: one row c_j | r_j of L + 64 elements a token, which is the key of every query head, and its first
 // L elements the value.  Bounded by reading the rows once up to some 100 rows of q a request, by the tensor cores beyond.
 //
-// A CTA takes 64 rows (new token, query head) of a request and walks 64 cached tokens a step; all of a step's operands are one tile of the cache in shared
-// memory, which is read as keys and as values:
-//     S = Q K^T          M = 64 rows, N = 64 tokens, K = L + 64
+// Rows of q are (new token, query head) pairs.  A step is 64 cached tokens, which lie in shared memory as boxes of 64 elements and serve as keys and as values:
+//     S = Q K^T          M = 128 rows, N = 64 tokens, K = L + 64; Q in tensor memory, as far as it fits
 //     P = exp2(scale2 S - m)                       (one thread per row)
-//     O^T += C^T P^T     M = 128 latent elements, L / 128 times; N = 64 rows, K = 64 tokens
-// The output is held transposed because L columns of 64 rows would run at half the tensor cores' rate and fill tensor memory: as it is they are L / 2 of 512 columns, and S
-// has two buffers beside it, so that the next step's scores are computed while this one's weights are.  m is a running reference, moved only when a scaled score exceeds it by
-// more than 8 (weights are at most 2^8), since that means reading and writing all of O.
+//     O^T += C^T P^T     M = 128 latent elements; N = the rows, K = 64 tokens
+// The output is held transposed so that few rows cost little, and so that both operands lie as the cache has them.  m is a running reference, moved only when a
+// scaled score exceeds it by more than 8 (weights are at most 2^8), since that means reading and writing all of O.
 //
-// Tiles come by one tensor copy per 8 tokens, {64 elements, 8 tokens, L / 64 + 1 groups of elements}: the boxes lie one behind the other as groups of 8 rows of
-// 128 swizzled bytes, 1024 (L / 64 + 1) bytes apart, which both operand forms can step over, whatever the block size.
+// Up to 32 rows (NARROW): a CTA has all L elements of the output; a step's tile of 72 KB is in flight three times.  More rows (WIDE): O of 128 rows and all
+// elements would fill tensor memory and Q shared memory, so two neighbouring CTAs walk the same tokens for 128 rows and have half of the output's elements each.  Both compute
+// all scores, but a tile's boxes beyond a CTA's own half are free again as soon as they are: the boxes that are values too have a ring of three tiles, the others one of
+// eight boxes.
 //
-// Warps 0-3 softmax, and Q and the output of an item; 4 loads; 5 issues the tensor instructions.  One CTA per SM takes an even share of the line of all
-// (request, row tile, 64 tokens) units.  Where requests have more than 64 rows two neighbouring CTAs walk the same units with 64 rows each, so that the second
-// one finds the tiles in L2.  An item that spans several CTAs leaves sums (o, m, l in 32 bits) in the workspace, which latent_join_kernel joins in CTA order.
+// Warps 0-3 softmax, and Q and the output of an item; 4 and 6 load (values and other boxes); 5 issues the tensor instructions.  One CTA (or pair) per SM (or two) takes an
+// even share of the line of all (request, row tile, 64 tokens) units.  An item that spans several CTAs leaves sums (o, m, l in 32 bits) in the workspace,
+// which latent_join_kernel joins in CTA order.
 #pragma once
 #include "attend_prompt.cuh"
 #include "attend_split.cuh"
 
 namespace ptk {
 
-constexpr int LA_THREADS = 192, LA_ROWS = 64, LA_KEYS = 64, LA_ROPE = 64;
-constexpr int LA_MIN_UNITS = 4;              // a CTA takes at least this many, so that joining does not cost more than it saves
+constexpr int LA_THREADS = 224, LA_KEYS = 64, LA_ROPE = 64, LA_BOX = LA_KEYS * 128;      // a box: 64 tokens, 64 elements
+constexpr int LA_MIN_UNITS = 2;              // a CTA takes at least this many, so that joining does not cost more than it saves
 
-template <int L>
+template <int L, bool WIDE>
 struct LatentShape {
-  static constexpr int BOXES = L / 64 + 1, GROUP_BYTES = BOXES * 1024;            // 8 tokens
-  static constexpr int TILE_BYTES = 8 * GROUP_BYTES, Q_BYTES = BOXES * LA_ROWS * 128, P_BYTES = LA_ROWS * 128;
-  static constexpr int STAGES = L == 512 ? 2 : 3;
-  static constexpr int MISC = 2816;                                               // barriers, factors, the first bad token per element
-  static constexpr int SMEM = Q_BYTES + STAGES * TILE_BYTES + P_BYTES + MISC;
-  static constexpr int PART = LA_ROWS * (L + 2);                                  // floats of an item's sums in one CTA: o, m, l
+  static constexpr int BOXES = L / 64 + 1, ROWS = WIDE ? 128 : 32, PAIR = WIDE ? 2 : 1;
+  static constexpr int VALUES = WIDE ? L / 128 : L / 64, OTHERS = BOXES - VALUES;          // boxes of a tile that are values of this CTA, and those that are not
+  static constexpr int DIMS = VALUES * 64, MT = DIMS / 128;                               // output elements, instructions' worth of them
+  // tensor memory: O, S, Q
+  static constexpr int S_AT = MT * ROWS, Q_AT = S_AT + LA_KEYS, Q_MOST = (512 - Q_AT) / 32, Q_TMEM = Q_MOST < BOXES ? Q_MOST : BOXES;
+  // shared memory: the rest of Q, P, the rings
+  static constexpr int Q_BYTES = (BOXES - Q_TMEM) * 128 * 128, P_BYTES = ROWS * 128;
+  static constexpr int STAGES = L == 512 ? 3 : WIDE ? 6 : 5, SLOTS = WIDE ? (L == 512 ? 8 : 12) : STAGES;
+  static constexpr int V_AT = Q_BYTES + P_BYTES, K_AT = V_AT + STAGES * VALUES * LA_BOX, MISC_AT = K_AT + SLOTS * LA_BOX;
+  static constexpr int PART = ROWS * (DIMS + 2);                                          // floats of an item's sums in one CTA: o, m, l
 };
+template <int L, bool WIDE>
 struct LatentMisc {
-  u64 full[3], empty[3], q, q_free, s[2], p, pv, end;
-  u32 valid[3], tmem;
+  using Shape = LatentShape<L, WIDE>;
+  u64 v_full[Shape::STAGES], v_empty[Shape::STAGES], k_full[Shape::SLOTS], k_empty[Shape::SLOTS], q, q_free, s, s_free, p, pv, end, left, scan[LA_THREADS / 32];
+  u32 valid[Shape::STAGES], tmem;
   int gave_up, any_bad, r;
-  u64 left;
-  u64 scan[6];
-  float f[LA_ROWS];
-  int bad[512];              // first token whose element d is not finite, among tokens that some rows do not see
+  float f[Shape::ROWS];
+  int bad[Shape::DIMS];      // first token whose element d is not finite, among tokens that some rows do not see
 };
-static_assert(sizeof(LatentMisc) <= LatentShape<512>::MISC, "fits behind the operands");
-static_assert(LatentShape<512>::SMEM <= 232448, "fits an SM (there is no static shared memory, so the operands begin on a multiple of 1024)");
+template <int L, bool WIDE>
+constexpr int latent_smem() { return LatentShape<L, WIDE>::MISC_AT + (int)sizeof(LatentMisc<L, WIDE>); }
+static_assert(latent_smem<512, true>() <= 232448 && latent_smem<512, false>() <= 232448 && latent_smem<256, true>() <= 232448 && latent_smem<256, false>() <= 232448,
+              "fits an SM (there is no static shared memory, so the operands begin on a multiple of 1024)");
 
 struct Latent {
-  Attend a;                  // q: q_latent; cache.heads 1, group = heads
+  Attend a;                  // q: q_latent; cache.heads 1, group = heads; box_tokens: tokens of a tensor copy
   const unsigned char* q_rope;
   i64 qr_token, qr_head;
 };
@@ -56,11 +62,10 @@ struct LatentPart { int parts, r; u32 rt; };
 constexpr int LA_PARTS_AT = 8192;            // where the sums begin in the workspace, behind the descriptions of the largest grid
 static_assert(MAX_SMS * sizeof(LatentPart) <= LA_PARTS_AT, "descriptions fit");
 
-// The items of one CTA's share of the line, one after the other.  NQ rows are a row tile of the line, of which the CTA has those from `skip` on.
+// The items of one CTA's share of the line, one after the other.  NQ rows are a row tile.
 template <int NQ>
 struct LatentLine {
   const Attend& a;
-  int skip;
   u64 u, u_end, left;
   u32 per;
   int r;
@@ -70,8 +75,8 @@ struct LatentLine {
   int keys, units, ua, ub;
   u32 first, last;
   __device__ __forceinline__ bool next() {
+    if (u >= u_end) return false;
     for (;;) {
-      if (u >= u_end) return false;
       if (rt >= row_tiles<NQ>(a, q)) {
         if (++r >= a.R) return false;                         // cannot happen while offsets and lengths hold still
         rt = 0;
@@ -80,33 +85,28 @@ struct LatentLine {
       }
       keys = tile_keys<NQ>(a, q, rt);
       units = units_of<LA_KEYS>(keys);
-      if (left >= (u64)units) {
-        left -= units;
-        ++rt;
-        continue;
-      }
-      ua = (int)left;
-      ub = u_end - u < (u64)(units - ua) ? ua + (int)(u_end - u) : units;
-      first = quotient(u - ua, per);
-      last = quotient(u - ua + units - 1, per);
-      u += ub - ua;
-      left += ub - ua;
-      if ((i64)rt * NQ + skip < (i64)q.fresh * a.group) return true;
+      if (left < (u64)units) break;
+      left -= units;
+      ++rt;
     }
+    ua = (int)left;
+    ub = u_end - u < (u64)(units - ua) ? ua + (int)(u_end - u) : units;
+    first = quotient(u - ua, per);
+    last = quotient(u - ua + units - 1, per);
+    u += ub - ua;
+    left += ub - ua;
+    return true;
   }
 };
 
-__device__ __forceinline__ u64 operand_desc(u32 addr, u32 lead_bytes, u32 stride_bytes) {
-  return (u64)((addr >> 4) & 0x3FFFu) | ((u64)((lead_bytes >> 4) & 0x3FFFu) << 16) | ((u64)((stride_bytes >> 4) & 0x3FFFu) << 32) | (1ull << 46) | (2ull << 61);
+// instruction descriptor of kind::f16, M = 128, A "MN-major" or not; B has its elements of one row contiguous.  N is added at bit 17 in eights.
+__host__ __device__ constexpr u32 mma_desc_a(bool fp16, bool a_mn_major) {
+  return (1u << 4) | ((fp16 ? 0u : 1u) << 7) | ((fp16 ? 0u : 1u) << 10) | ((a_mn_major ? 1u : 0u) << 15) | ((u32)(128 >> 4) << 24);
 }
-// instruction descriptor of kind::f16 for any M, A "MN-major" or not; B has its elements of one row contiguous
-__host__ __device__ constexpr u32 mma_desc_m(bool fp16, int M, int N, bool a_mn_major) {
-  return (1u << 4) | ((fp16 ? 0u : 1u) << 7) | ((fp16 ? 0u : 1u) << 10) | ((a_mn_major ? 1u : 0u) << 15) | ((u32)(N >> 3) << 17) | ((u32)(M >> 4) << 24);
-}
-// 8 tokens of a block, all their elements: box of the map {64 elements, tokens of a block, groups of 64 elements, blocks}
-__device__ __forceinline__ void tensor_load_rows(u32 dst, const CUtensorMap* map, int token, int block, u64* bar) {
-  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst), "l"(map), "r"(0), "r"(token),
-               "r"(0), "r"(block), "r"(smem_addr(bar)) : "memory");
+// some tokens of a block, 64 elements: box of the map {elements, tokens of a block, blocks}
+__device__ __forceinline__ void tensor_load_box(u32 dst, const CUtensorMap* map, int element, int token, int block, u64* bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(element), "r"(token),
+               "r"(block), "r"(smem_addr(bar)) : "memory");
 }
 __device__ __forceinline__ bool any_of_softmax(bool v) {      // barrier of the 128 softmax threads
   u32 r;
@@ -114,14 +114,15 @@ __device__ __forceinline__ bool any_of_softmax(bool v) {      // barrier of the 
   return r != 0;
 }
 
-template <int L, bool F16, int PAIR>
+template <int L, bool F16, bool WIDE>
 __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Latent la, const __grid_constant__ CUtensorMap map) {
-  using Shape = LatentShape<L>;
-  constexpr int NQ = LA_ROWS * PAIR, STAGES = Shape::STAGES, BOXES = Shape::BOXES, GB = Shape::GROUP_BYTES, MT = L / 128;
-  extern __shared__ __align__(1024) unsigned char latent_smem[];
-  unsigned char* const smem = latent_smem;
+  using Shape = LatentShape<L, WIDE>;
+  constexpr int NQ = Shape::ROWS, STAGES = Shape::STAGES, SLOTS = Shape::SLOTS, BOXES = Shape::BOXES, VALUES = Shape::VALUES, OTHERS = Shape::OTHERS, MT = Shape::MT,
+                DIMS = Shape::DIMS, PAIR = Shape::PAIR;
+  extern __shared__ __align__(1024) unsigned char latent_smem_raw[];
+  unsigned char* const smem = latent_smem_raw;
   const Attend& a = la.a;
-  LatentMisc& s = *reinterpret_cast<LatentMisc*>(smem + Shape::Q_BYTES + STAGES * Shape::TILE_BYTES + Shape::P_BYTES);
+  LatentMisc<L, WIDE>& s = *reinterpret_cast<LatentMisc<L, WIDE>*>(smem + Shape::MISC_AT);
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0);
   const u32 cta = blockIdx.x / PAIR, ctas = gridDim.x / PAIR, half = blockIdx.x % PAIR;
   LatentPart* const part = reinterpret_cast<LatentPart*>(a.work) + blockIdx.x;
@@ -130,10 +131,12 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
   // ---- this CTA's share of the line: every CTA sums the units of all requests, consecutive requests per thread
   if (tid == 0) {
     part->parts = 0;
-    for (int i = 0; i < STAGES; ++i) { bar_init(&s.full[i], 1); bar_init(&s.empty[i], 1); }
+    for (int i = 0; i < STAGES; ++i) { bar_init(&s.v_full[i], 1); bar_init(&s.v_empty[i], 1); }
+    for (int i = 0; i < SLOTS; ++i) { bar_init(&s.k_full[i], 1); bar_init(&s.k_empty[i], 1); }
     bar_init(&s.q, 128);
     bar_init(&s.q_free, 1);
-    for (int i = 0; i < 2; ++i) bar_init(&s.s[i], 1);
+    bar_init(&s.s, 1);
+    bar_init(&s.s_free, 128);
     bar_init(&s.p, 128);
     bar_init(&s.pv, 1);
     bar_init(&s.end, 1);
@@ -142,7 +145,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
     s.r = -1;
   }
   if (tid == 160) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
-  for (int i = tid; i < L; i += LA_THREADS) s.bad[i] = 0x7FFFFFFF;
+  for (int i = tid; i < DIMS; i += LA_THREADS) s.bad[i] = 0x7FFFFFFF;
   const int per_thread = (a.R + LA_THREADS - 1) / LA_THREADS;
   const int rb = min(tid * per_thread, a.R), re = min(rb + per_thread, a.R);
   u64 mine = 0;
@@ -186,54 +189,86 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
   __syncthreads();
   tc_fence_after();
   const u32 tmem = s.tmem;
-  const u32 smem_q = smem_addr(smem), smem_k = smem_q + Shape::Q_BYTES, smem_p = smem_k + STAGES * Shape::TILE_BYTES;
-  LatentLine<NQ> line{a, (int)half * LA_ROWS, u_begin, u_end, s.left, per, s.r, 0, request(a, s.r)};
+  const u32 smem_q = smem_addr(smem), smem_p = smem_q + Shape::Q_BYTES, smem_v = smem_q + Shape::V_AT, smem_k = smem_q + Shape::K_AT;
+  LatentLine<NQ> line{a, u_begin, u_end, s.left, per, s.r, 0, request(a, s.r)};
   const volatile int* const gave_up = &s.gave_up;
+  // the elements of box i of a tile, in the order of the products: this CTA's values, the other half's, the rotary part
+  auto element_of = [&](int i) {
+    return 64 * (i < VALUES ? (int)half * VALUES + i : i < L / 64 ? (int)(1 - half) * VALUES + i - VALUES : L / 64);
+  };
 
   if (warp == 5) {
     // ======== tensor instructions: S of step g + 1 before the output of step g
-    constexpr u32 QK = mma_desc_m(F16, 64, LA_KEYS, false), PV = mma_desc_m(F16, 128, LA_ROWS, true);
-    u32 g = 0, item = 0;
+    constexpr u32 QK = mma_desc_a(F16, false) | (u32)(LA_KEYS >> 3) << 17, PV = mma_desc_a(F16, true);
+    u32 g = 0, item = 0, op = 0;              // step, item, box that is no value
     bool quit = false;
     auto wait = [&](u64* b, u32 parity) {
       if (!quit && !__all_sync(FULL, bar_wait(b, parity, a.polls, &s.gave_up))) quit = true;
     };
-    auto scores = [&](u32 n) {                // of step n, into buffer n & 1
-      wait(&s.full[n % STAGES], (n / STAGES) & 1);
-      tc_fence_after();
+    auto box = [&](int i, u32 at) {           // scores' part of box i, which lies at `at`
       if (!quit && elected()) {
-        const u64 qa = operand_desc(smem_q, 0, 1024), kb = operand_desc(smem_k + (n % STAGES) * Shape::TILE_BYTES, 0, GB);
+        const u64 kb = operand_desc(at, 0);
 #pragma unroll
-        for (int k = 0; k < 4 * BOXES; ++k)   // 16 elements: 32 bytes further in a row, or the next 64 elements
-          mma_ss(tmem + (n & 1) * 64, qa + (u64)(((k >> 2) * (LA_ROWS * 128) + (k & 3) * 32) >> 4), kb + (u64)(((k >> 2) * 1024 + (k & 3) * 32) >> 4), QK, k > 0);
-        tc_commit(&s.s[n & 1]);
+        for (int k = 0; k < 4; ++k) {         // 16 elements: 8 columns, or 32 bytes further in a row
+          if (i < Shape::Q_TMEM) mma_ts(tmem + Shape::S_AT, tmem + Shape::Q_AT + i * 32 + k * 8, kb + (u64)((k * 32) >> 4), QK, i > 0 || k > 0);
+          else mma_ss(tmem + Shape::S_AT, operand_desc(smem_q + (i - Shape::Q_TMEM) * 16384, 0) + (u64)((k * 32) >> 4), kb + (u64)((k * 32) >> 4), QK, i > 0 || k > 0);
+        }
       }
+      __syncwarp();
+    };
+    auto scores = [&](u32 n) {                // of step n
+      if (n > 0) wait(&s.s_free, (n - 1) & 1);
+      wait(&s.v_full[n % STAGES], (n / STAGES) & 1);
+      tc_fence_after();
+#pragma unroll
+      for (int i = 0; i < VALUES; ++i) box(i, smem_v + ((n % STAGES) * VALUES + i) * LA_BOX);
+#pragma unroll
+      for (int i = 0; i < OTHERS; ++i, ++op) {
+        wait(&s.k_full[op % SLOTS], (op / SLOTS) & 1);
+        tc_fence_after();
+        box(VALUES + i, smem_k + (op % SLOTS) * LA_BOX);
+        if (!quit && elected()) tc_commit(&s.k_empty[op % SLOTS]);
+        __syncwarp();
+      }
+      if (!quit && elected()) tc_commit(&s.s);
       __syncwarp();
     };
     while (!quit && line.next()) {
       const u32 n = line.ub - line.ua;
+      const int rows = min(NQ, line.q.fresh * a.group - (int)(line.rt * NQ));
+      const u32 pv = PV | (u32)((rows + 15) / 16 * 2) << 17;
       wait(&s.q, item & 1);
       scores(g);
       for (u32 j = 0; j < n && !quit; ++j, ++g) {
-        if (j + 1 < n) scores(g + 1);
-        else if (!quit && elected()) tc_commit(&s.q_free);
+        // the next step's scores first if its tile is there by now, or else whatever comes first
+        const bool more = j + 1 < n;
+        bool ahead = false;
+        if (more) {
+          u64 *const v = &s.v_full[(g + 1) % STAGES], *const k = &s.k_full[(op + OTHERS - 1) % SLOTS], *const p = &s.p;
+          for (u32 i = 0; i < a.polls && !ahead; ++i) {
+            ahead = __all_sync(FULL, bar_test(v, ((g + 1) / STAGES) & 1) && bar_test(k, ((op + OTHERS - 1) / SLOTS) & 1));
+            if (!ahead && __all_sync(FULL, bar_try(p, g & 1))) break;
+          }
+          if (ahead) scores(g + 1);
+        } else if (!quit && elected()) tc_commit(&s.q_free);
         __syncwarp();
         wait(&s.p, g & 1);
         tc_fence_after();
         if (!quit && elected()) {
-          const u32 tile = smem_k + (g % STAGES) * Shape::TILE_BYTES;
-          const u64 pb = operand_desc(smem_p, 0, 1024);
+          const u32 tile = smem_v + (g % STAGES) * VALUES * LA_BOX;
+          const u64 pb = operand_desc(smem_p, 0);
 #pragma unroll
           for (int i = 0; i < MT; ++i) {
-            const u64 va = operand_desc(tile + 2 * i * 1024, 1024, GB);
+            const u64 va = operand_desc(tile + 2 * i * LA_BOX, LA_BOX);
 #pragma unroll
-            for (int k = 0; k < LA_KEYS / 16; ++k)            // 16 tokens: two groups of 8
-              mma_ss(tmem + 128 + i * 64, va + (u64)((k * 2 * GB) >> 4), pb + (u64)((k * 32) >> 4), PV, j > 0 || k > 0);
+            for (int k = 0; k < LA_KEYS / 16; ++k)            // 16 tokens: 16 rows of 128 bytes
+              mma_ss(tmem + i * NQ, va + (u64)((k * 16 * 128) >> 4), pb + (u64)((k * 32) >> 4), pv, j > 0 || k > 0);
           }
-          tc_commit(&s.empty[g % STAGES]);
+          tc_commit(&s.v_empty[g % STAGES]);
           tc_commit(&s.pv);
         }
         __syncwarp();
+        if (more && !ahead) scores(g + 1);
       }
       ++item;
     }
@@ -241,106 +276,157 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
     if (elected()) tc_commit(&s.end);
     __syncwarp();
     bar_drain(&s.end, 0);
-  } else if (warp == 4) {
-    // ======== tiles: lane i < 8 follows tokens 8 i .. 8 i + 7 of a step
-    u32 g = 0;
-    const u32 B = a.cache.block_tokens;
+  } else if (warp >= 4) {
+    // ======== tiles: warp 4 the boxes that are values, warp 6 the others.  Lane j has the tokens of copy j of a box, some tokens of a block each.
+    const bool values = warp == 4;
+    const u32 B = a.cache.block_tokens, bt = a.box_tokens, copies = LA_KEYS / bt;
+    u32 g = 0, op = 0;
     bool bounds = false, quit = false;
+    const u32 mine_at = lane % copies, team = lane / copies, teams = 32 / copies;
     while (!quit && line.next()) {
       const int* const table = a.tables + (i64)line.r * a.max_blocks;
       auto look_up = [&](int unit) {
-        const int key = unit * LA_KEYS + 8 * lane;
-        return lane < 8 && key < line.keys ? table[(u32)key / B] : -1;
+        const int key = unit * LA_KEYS + (int)(mine_at * bt);
+        return key < line.keys ? table[(u32)key / B] : -1;
       };
       int id = look_up(line.ua);
-      for (int unit = line.ua; unit < line.ub; ++unit, ++g) {
-        const u32 st = g % STAGES;
-        const int key = unit * LA_KEYS + 8 * lane;
-        const bool in = lane < 8 && key < line.keys, have = in && (u32)id < a.cache.num_blocks;
-        bounds |= in && !have;
-        const int block = id;
+      for (int unit = line.ua; unit < line.ub && !quit; ++unit, ++g) {
+        const int key = unit * LA_KEYS + (int)(mine_at * bt);
+        const bool in = key < line.keys, have = in && (u32)id < a.cache.num_blocks;
+        bounds |= values && in && !have;
+        const int block = id, token = (int)((u32)key % B);
         if (unit + 1 < line.ub) id = look_up(unit + 1);
-        const u32 there = __ballot_sync(FULL, have);
-        if (g >= STAGES && !__all_sync(FULL, bar_wait(&s.empty[st], (g / STAGES - 1) & 1, a.polls, &s.gave_up))) { quit = true; break; }
-        if (lane == 0) {
-          s.valid[st] = there;
-          if (there) bar_expect(&s.full[st], __popc(there) * GB);
-          else bar_arrive(&s.full[st]);
+        const u32 there = __ballot_sync(FULL, have && team == 0), bytes = __popc(there) * bt * 128;
+        if (values) {
+          const u32 st = g % STAGES;
+          if (g >= STAGES && !__all_sync(FULL, bar_wait(&s.v_empty[st], (g / STAGES - 1) & 1, a.polls, &s.gave_up))) { quit = true; break; }
+          // groups of 8 tokens that are there
+          const u32 groups = __reduce_or_sync(FULL, have && team == 0 ? ((1u << (bt / 8)) - 1) << (mine_at * (bt / 8)) : 0u);
+          if (lane == 0) {
+            s.valid[st] = groups;
+            if (there) bar_expect(&s.v_full[st], bytes * VALUES);
+            else bar_arrive(&s.v_full[st]);
+          }
+          __syncwarp();
+          if (have)
+            for (u32 i = team; i < VALUES; i += teams)
+              tensor_load_box(smem_v + (st * VALUES + i) * LA_BOX + mine_at * bt * 128, &map, element_of((int)i), token, block, &s.v_full[st]);
+        } else {
+          for (u32 i = 0; i < OTHERS; ++i, ++op) {
+            const u32 st = op % SLOTS;
+            if (op >= SLOTS && !__all_sync(FULL, bar_wait(&s.k_empty[st], (op / SLOTS - 1) & 1, a.polls, &s.gave_up))) { quit = true; break; }
+            if (lane == 0) {
+              if (there) bar_expect(&s.k_full[st], bytes);
+              else bar_arrive(&s.k_full[st]);
+            }
+            __syncwarp();
+            if (have && team == 0) tensor_load_box(smem_k + st * LA_BOX + mine_at * bt * 128, &map, element_of(VALUES + (int)i), token, block, &s.k_full[st]);
+          }
         }
-        __syncwarp();
-        if (have) tensor_load_rows(smem_k + st * Shape::TILE_BYTES + lane * GB, &map, (int)((u32)key % B), block, &s.full[st]);
       }
     }
     // whatever happened, what is in flight lands before the CTA gives its memory back
-    for (u32 k = g > STAGES ? g - STAGES : 0; k < g; ++k) bar_drain(&s.full[k % STAGES], (k / STAGES) & 1);
+    if (values)
+      for (u32 k = g > STAGES ? g - STAGES : 0; k < g; ++k) bar_drain(&s.v_full[k % STAGES], (k / STAGES) & 1);
+    else
+      for (u32 k = op > SLOTS ? op - SLOTS : 0; k < op; ++k) bar_drain(&s.k_full[k % SLOTS], (k / SLOTS) & 1);
     if (bounds && a.status) atomicOr(a.status, PTSTORE_S_BOUNDS);
   } else {
-    // ======== softmax: lanes 0-15 of warp w have rows 16 w + lane; Q before, the output behind an item
-    const int row = warp * 16 + (lane & 15);
-    const u32 lane_base = (u32)(32 * warp) << 16, ts = tmem + lane_base, to = tmem + lane_base + 128;
+    // ======== softmax: thread t has row t; Q before, the output behind an item
+    const int row = tid;
+    const u32 lane_base = (u32)(32 * warp) << 16, ts = tmem + lane_base + Shape::S_AT, to = tmem + lane_base;
     u32 g = 0, item = 0;
     bool quit = false;
     auto wait = [&](u64* b, u32 parity) {
       const bool ok = bar_wait(b, parity, a.polls, &s.gave_up);
       if (__any_sync(FULL, !ok || *gave_up)) quit = true;
     };
-    // Q of an item.  Rows that do not exist keep what lies there: their sums are never looked at, and a row's are its own.
+    // Q of an item, a row a thread.  Rows that do not exist keep what lies there: their sums are never looked at, and a row's are its own.
     auto load_q = [&](const LatentLine<NQ>& it) {
-      const int base = (int)(it.rt * NQ) + (int)half * LA_ROWS, rows = min(LA_ROWS, it.q.fresh * a.group - base);
-      constexpr int CPR = BOXES * 8;
-#pragma unroll 4
-      for (int i = tid; i < rows * CPR; i += 128) {
-        const int n = i / CPR, c = i % CPR, fr = (base + n) / a.group, hq = (base + n) % a.group;
+      const int base = (int)(it.rt * NQ), rows = min(NQ, it.q.fresh * a.group - base);
+      if (warp * 32 < rows) {
+        const bool live = row < rows;
+        const int flat = base + (live ? row : 0), fr = flat / a.group, hq = flat % a.group;
         const i64 tok = it.q.row0 + fr;
-        const unsigned char* src = c < L / 8 ? a.q + 2 * (tok * a.q_token + hq * a.q_head + c * 8) : la.q_rope + 2 * (tok * la.qr_token + hq * la.qr_head + (c - L / 8) * 8);
-        *reinterpret_cast<uint4*>(smem + (c >> 3) * (LA_ROWS * 128) + n * 128 + (((c & 7) ^ (n & 7)) * 16)) = *reinterpret_cast<const uint4*>(src);
+        const unsigned char *const ql = a.q + 2 * (tok * a.q_token + hq * a.q_head), *const qr = la.q_rope + 2 * (tok * la.qr_token + hq * la.qr_head);
+        constexpr int AT_ONCE = 3;            // boxes on their way
+#pragma unroll
+        for (int i0 = 0; i0 < BOXES; i0 += AT_ONCE) {
+          uint4 v[AT_ONCE][8];
+#pragma unroll
+          for (int i = 0; i < AT_ONCE; ++i)
+            if (i0 + i < BOXES) {
+              const int e = element_of(i0 + i);
+              const uint4* src = reinterpret_cast<const uint4*>(e < L ? ql + 2 * e : qr);
+#pragma unroll
+              for (int c = 0; c < 8; ++c) v[i][c] = live ? src[c] : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+          for (int i = 0; i < AT_ONCE; ++i)
+            if (i0 + i < BOXES) {
+              if (i0 + i < Shape::Q_TMEM) {
+                u32 w[32];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) { w[4 * c] = v[i][c].x; w[4 * c + 1] = v[i][c].y; w[4 * c + 2] = v[i][c].z; w[4 * c + 3] = v[i][c].w; }
+                tc_st32(tmem + lane_base + Shape::Q_AT + (i0 + i) * 32, w);
+              } else {
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                  *reinterpret_cast<uint4*>(smem + (i0 + i - Shape::Q_TMEM) * 16384 + row * 128 + ((c ^ (row & 7)) * 16)) = v[i][c];
+              }
+            }
+        }
+        tc_wait_st();
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      tc_fence_before();
       bar_arrive(&s.q);
     };
     bool more = line.next();
     if (more) load_q(line);
     while (more && !quit) {
       const Req rq = line.q;
-      const int r = line.r, keys = line.keys, ua = line.ua, n = line.ub - line.ua, row_base = (int)(line.rt * NQ) + (int)half * LA_ROWS;
+      const int r = line.r, keys = line.keys, ua = line.ua, n = line.ub - line.ua, row_base = (int)(line.rt * NQ);
       const u32 rt = line.rt, first = line.first, last = line.last;
-      const int rows = min(LA_ROWS, rq.fresh * a.group - row_base);
+      const int rows = min(NQ, rq.fresh * a.group - row_base);
+      const bool live = row < rows;
       auto seen_by = [&](int row) {
         const i64 k = (i64)rq.pos0 + (row_base + row) / a.group + 1;
         return k < 0 ? 0 : k > keys ? keys : (int)k;
       };
-      const int see = lane < 16 && row < rows ? seen_by(row) : 0, all_see = seen_by(0);
+      const int see = live ? seen_by(row) : 0, all_see = seen_by(0);
       float m = -INFINITY, l = 0.0f;
       for (int j = 0; j < n; ++j, ++g) {
         const int k0 = (ua + j) * LA_KEYS;
         const u32 st = g % STAGES;
         // (a wait that ran out in one warp shows in all of them at the next barrier: until then its values are of no use, but in bounds)
-        wait(&s.s[g & 1], (g >> 1) & 1);
+        wait(&s.s, g & 1);
         tc_fence_after();
         float v[2][32];
-        tc_ld32(v[0], ts + (g & 1) * 64);
-        tc_ld32(v[1], ts + (g & 1) * 64 + 32);
-        tc_wait_ld();
-        tc_loaded(v[0]);
-        tc_loaded(v[1]);
-        wait(&s.full[st], (g / STAGES) & 1);          // (has ended long ago: makes the tile's bytes and its valid bits this thread's too)
+        const bool busy = warp * 32 < rows;           // this warp has rows
+        if (busy) {
+          tc_ld32(v[0], ts);
+          tc_ld32(v[1], ts + 32);
+          tc_wait_ld();
+          tc_loaded(v[0]);
+          tc_loaded(v[1]);
+          tc_fence_before();
+        }
+        bar_arrive(&s.s_free);
+        wait(&s.v_full[st], (g / STAGES) & 1);        // (has ended long ago: makes the tile's bytes and its valid bits this thread's too)
         const u32 valid = s.valid[st];
         const bool edge = k0 + LA_KEYS > all_see || valid != 0xFFu;
-        float top = -INFINITY;
-        // the products rounded as the maximum is, so that the largest weight is 1 however large the scores are
-#pragma unroll
-        for (int i = 0; i < 64; ++i) v[i >> 5][i & 31] = __fmul_rn(v[i >> 5][i & 31], a.scale2);
         if (edge) {
           // A weight of zero does not hide an infinity or a NaN.  Tokens that no row sees become zero; what is not finite in tokens that only some rows see is
           // taken out, and put into the sums of the rows that see it at the end.  (The scores have been computed by now.)
-          unsigned char* const tile = smem + Shape::Q_BYTES + st * Shape::TILE_BYTES;
+          unsigned char* const tile = smem + Shape::V_AT + st * VALUES * LA_BOX;
           constexpr u32 EX = F16 ? 0x7C00u : 0x7F80u;
           const int from = max(all_see - k0, 0);
-          for (int i = tid; i < LA_KEYS * (L / 8); i += 128) {
-            const int t = i / (L / 8), c = i % (L / 8);
+          for (int i = tid; i < LA_KEYS * (DIMS / 8); i += 128) {
+            const int t = i / (DIMS / 8), c = i % (DIMS / 8);
             const bool there = (valid >> (t >> 3)) & 1;
             if (t < from && there) continue;
-            uint4* const p = reinterpret_cast<uint4*>(tile + (t >> 3) * GB + (c >> 3) * 1024 + (t & 7) * 128 + (((c & 7) ^ (t & 7)) * 16));
+            uint4* const p = reinterpret_cast<uint4*>(tile + (c >> 3) * LA_BOX + t * 128 + (((c & 7) ^ (t & 7)) * 16));
             if (!there || k0 + t >= keys) { *p = make_uint4(0, 0, 0, 0); continue; }
             uint4 w = *p;
             u32 e[4] = {w.x, w.y, w.z, w.w};
@@ -359,17 +445,27 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
               s.any_bad = 1;
             }
           }
-#pragma unroll
-          for (int i = 0; i < 64; ++i)
-            if (k0 + i >= see || !((valid >> (i >> 3)) & 1)) v[i >> 5][i & 31] = -INFINITY;
         }
+        float top = -INFINITY;
+        if (busy) {
+          // the products rounded as the maximum is, so that the largest weight is 1 however large the scores are
 #pragma unroll
-        for (int i = 0; i < 64; i += 4)
-          top = fmaxf(fmaxf(top, fmaxf(v[i >> 5][i & 31], v[i >> 5][(i & 31) + 1])), fmaxf(v[i >> 5][(i & 31) + 2], v[i >> 5][(i & 31) + 3]));
+          for (int i = 0; i < 64; ++i) v[i >> 5][i & 31] = __fmul_rn(v[i >> 5][i & 31], a.scale2);
+          if (edge) {
+#pragma unroll
+            for (int i = 0; i < 64; ++i)
+              if (k0 + i >= see || !((valid >> (i >> 3)) & 1)) v[i >> 5][i & 31] = -INFINITY;
+          }
+          float x4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 0; i < 64; i += 8)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x4[k] = fmaxf(x4[k], fmaxf(v[i >> 5][(i & 31) + 2 * k], v[i >> 5][(i & 31) + 2 * k + 1]));
+          top = fmaxf(fmaxf(x4[0], x4[1]), fmaxf(x4[2], x4[3]));
+        }
         // the output and the weights of the step before are done with
         if (g > 0) wait(&s.pv, (g - 1) & 1);
         tc_fence_after();
-        const bool live = lane < 16 && row < rows;
         const bool move = live && (top > m + 8.0f || (m == -INFINITY && top > m));
         float f = 1.0f;
         if (move) {
@@ -380,17 +476,18 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
         const bool some = any_of_softmax(move || quit);
         if (some && any_of_softmax(quit)) { quit = true; break; }
         if (some && j > 0) {
-          if (lane < 16) s.f[row] = f;
+          if (row < NQ) s.f[row] = f;
           asm volatile("bar.sync 3, 128;" ::: "memory");
 #pragma unroll 1
-          for (int c = 0; c < MT * 64; c += 32) {
+          for (int c = 0; c < MT * NQ; c += 32) {
+            if ((c % NQ) >= rows) continue;
             float o[32];
             tc_ld32(o, to + c);
             tc_wait_ld();
             tc_loaded(o);
             u32 scaled[32];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) scaled[i] = __float_as_uint(o[i] * s.f[(c & 32) + i]);
+            for (int i = 0; i < 32; ++i) scaled[i] = __float_as_uint(o[i] * s.f[c % NQ + i]);
             tc_st32(to + c, scaled);
           }
           tc_wait_st();
@@ -408,7 +505,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
               sum[k] += p0 + p1;
               two[k] = pack2<F16>(p0, p1);
             }
-            *reinterpret_cast<uint4*>(smem + (smem_p - smem_q) + row * 128 + ((c ^ (row & 7)) * 16)) = make_uint4(two[0], two[1], two[2], two[3]);
+            *reinterpret_cast<uint4*>(smem + Shape::Q_BYTES + row * 128 + ((c ^ (row & 7)) * 16)) = make_uint4(two[0], two[1], two[2], two[3]);
           }
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
@@ -419,6 +516,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
       if (quit) break;
       // ---- the next item's Q while the last products run
       wait(&s.q_free, item & 1);
+      tc_fence_after();
       more = line.next();
       if (more && !quit) load_q(line);
       ++item;
@@ -426,25 +524,25 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
       wait(&s.pv, (g - 1) & 1);
       if (any_of_softmax(quit)) break;
       tc_fence_after();
-      const bool whole = first == last, live = lane < 16 && row < rows;
+      const bool whole = first == last;
       float* const my = sums + ((i64)(2 * cta + (cta == first ? 1 : 0)) * PAIR + half) * Shape::PART;
       if (live) {
         const i64 pos = (i64)rq.pos0 + (row_base + row) / a.group;
         if (whole) {
           s.f[row] = row_factor(a, r, pos, l);
-          if (a.lse) a.lse[(i64)(rq.row0 + (row_base + row) / a.group) * a.heads + (row_base + row) % a.group] = lse_of(m, l);
+          if (a.lse && half == 0) a.lse[(i64)(rq.row0 + (row_base + row) / a.group) * a.heads + (row_base + row) % a.group] = lse_of(m, l);
         } else {
           s.f[row] = 1.0f;
-          my[LA_ROWS * L + row] = m;
-          my[LA_ROWS * L + LA_ROWS + row] = l;
+          my[NQ * DIMS + row] = m;
+          my[NQ * DIMS + NQ + row] = l;
         }
       }
       if (tid == 0 && !whole && cta == first) { part->r = r; part->rt = rt; part->parts = (int)(last - first) + 1; }
       asm volatile("bar.sync 3, 128;" ::: "memory");
       const bool any_bad = *reinterpret_cast<volatile int*>(&s.any_bad) != 0;
 #pragma unroll 1
-      for (int c = 0; c < MT * 64; c += 32) {
-        const int d = (c >> 6) * 128 + tid, r0 = c & 32;
+      for (int c = 0; c < MT * NQ; c += 32) {
+        const int d = c / NQ * 128 + tid, r0 = c % NQ;
         if (r0 >= rows) continue;
         float o[32];
         tc_ld32(o, to + c);
@@ -452,7 +550,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
         tc_loaded(o);
         const int bad = any_bad ? s.bad[d] : 0x7FFFFFFF;
         int fr = (row_base + r0) / a.group, hq = (row_base + r0) % a.group;
-        unsigned char* dst = a.out + 2 * ((i64)(rq.row0 + fr) * a.o_token + (i64)hq * a.o_head + d);
+        unsigned char* dst = a.out + 2 * ((i64)(rq.row0 + fr) * a.o_token + (i64)hq * a.o_head + (int)half * DIMS + d);
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
           if (r0 + i < rows) {
@@ -461,7 +559,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
             float y = o[i] * f;
             if (bad != 0x7FFFFFFF && seen_by(r0 + i) > bad) y = NAN;
             if (whole) *reinterpret_cast<unsigned short*>(dst) = (unsigned short)pack2<F16>(y, 0.0f);
-            else my[(r0 + i) * L + d] = y;
+            else my[(r0 + i) * DIMS + d] = y;
             dst += 2 * a.o_head;
             if (++hq == a.group) { hq = 0; dst += 2 * (a.o_token - (i64)a.group * a.o_head); }
           }
@@ -470,7 +568,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
       tc_fence_before();
       asm volatile("bar.sync 3, 128;" ::: "memory");
       if (any_bad) {
-        for (int i = tid; i < L; i += 128) s.bad[i] = 0x7FFFFFFF;
+        for (int i = tid; i < DIMS; i += 128) s.bad[i] = 0x7FFFFFFF;
         if (tid == 0) s.any_bad = 0;
         asm volatile("bar.sync 3, 128;" ::: "memory");
       }
@@ -484,39 +582,56 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
   }
 }
 
-// Joins the sums of the items that span several CTAs: blockIdx.x the CTA an item begins in, blockIdx.y four of its rows, a thread for 4 elements of a row.
-template <int L, bool F16, int PAIR>
-__global__ void __launch_bounds__(L / 4) latent_join_kernel(const Latent la, int grid) {
+// Joins the sums of the items that span several CTAs: blockIdx.x the CTA an item begins in, blockIdx.y eight of its rows, a warp a row.
+template <int L, bool F16, bool WIDE>
+__global__ void __launch_bounds__(256) latent_join_kernel(const Latent la) {
+  using Shape = LatentShape<L, WIDE>;
+  constexpr int NQ = Shape::ROWS, DIMS = Shape::DIMS, PAIR = Shape::PAIR, PF = Shape::PART, E = DIMS / 128;        // float4's of a lane
   const Attend& a = la.a;
   const LatentPart part = reinterpret_cast<const LatentPart*>(a.work)[blockIdx.x];
   if (part.parts == 0) return;
-  constexpr int NQ = LA_ROWS * PAIR, PF = LatentShape<L>::PART;
   const u32 cta = blockIdx.x / PAIR, half = blockIdx.x % PAIR;
   const Req q = request(a, part.r);
-  const int row_base = (int)(part.rt * NQ) + (int)half * LA_ROWS, rows = min(LA_ROWS, q.fresh * a.group - row_base);
+  const int lane = threadIdx.x & 31, row_base = (int)(part.rt * NQ), rows = min(NQ, q.fresh * a.group - row_base), row = blockIdx.y * 8 + (threadIdx.x >> 5);
+  if (row >= rows) return;
   const float* const sums = reinterpret_cast<const float*>(a.work + LA_PARTS_AT) + (i64)half * PF;
   auto at = [&](int p) { return sums + (i64)(2 * (cta + p) + (p == 0 ? 1 : 0)) * PAIR * PF; };
-  const int e = threadIdx.x * 4;
-  for (int row = blockIdx.y * 4; row < min((int)blockIdx.y * 4 + 4, rows); ++row) {
-    float top = -INFINITY, sum = 0.0f;
-    for (int p = 0; p < part.parts; ++p) top = fmaxf(top, at(p)[LA_ROWS * L + row]);
-    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-    for (int p = 0; p < part.parts; ++p) {
-      const float m = at(p)[LA_ROWS * L + row];
-      const float f = m == -INFINITY ? 1.0f : exp2_fast(m - top);             // nothing seen: sums of zero (or NaN)
-      const float4 v = *reinterpret_cast<const float4*>(at(p) + row * L + e);
-      sum += at(p)[LA_ROWS * L + LA_ROWS + row] * f;
-      o.x += v.x * f;
-      o.y += v.y * f;
-      o.z += v.z * f;
-      o.w += v.w * f;
+  // lane p holds m and l of part p (of 32 at a time)
+  float top = -INFINITY, sum = 0.0f;
+  for (int p = lane; p < part.parts; p += 32) top = fmaxf(top, at(p)[NQ * DIMS + row]);
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
+  float4 acc[E] = {};
+  for (int p0 = 0; p0 < part.parts; p0 += 32) {
+    float f = 0.0f;
+    if (p0 + lane < part.parts) {
+      const float m = at(p0 + lane)[NQ * DIMS + row];
+      f = m == -INFINITY ? 1.0f : exp2_fast(m - top);                        // nothing seen: sums of zero (or NaN)
+      sum += at(p0 + lane)[NQ * DIMS + NQ + row] * f;
     }
-    const int fr = (row_base + row) / a.group, hq = (row_base + row) % a.group;
-    const float f = row_factor(a, part.r, (i64)q.pos0 + fr, sum);
-    *reinterpret_cast<uint2*>(a.out + 2 * ((i64)(q.row0 + fr) * a.o_token + (i64)hq * a.o_head + e)) = make_uint2(pack2<F16>(o.x * f, o.y * f), pack2<F16>(o.z * f, o.w * f));
-    if (a.lse && threadIdx.x == 0) a.lse[(i64)(q.row0 + fr) * a.heads + hq] = lse_of(top, sum);
+    const int n = min(32, part.parts - p0);
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) {
+      const float w = __shfl_sync(FULL, f, p);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float4 v = *reinterpret_cast<const float4*>(at(p0 + p) + row * DIMS + e * 128 + lane * 4);
+        acc[e].x += v.x * w;
+        acc[e].y += v.y * w;
+        acc[e].z += v.z * w;
+        acc[e].w += v.w * w;
+      }
+    }
   }
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) sum += __shfl_xor_sync(FULL, sum, o);
+  const int fr = (row_base + row) / a.group, hq = (row_base + row) % a.group;
+  const float f = row_factor(a, part.r, (i64)q.pos0 + fr, sum);
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    *reinterpret_cast<uint2*>(a.out + 2 * ((i64)(q.row0 + fr) * a.o_token + (i64)hq * a.o_head + (int)half * DIMS + e * 128 + lane * 4)) =
+        make_uint2(pack2<F16>(acc[e].x * f, acc[e].y * f), pack2<F16>(acc[e].z * f, acc[e].w * f));
+  if (a.lse && half == 0 && lane == 0) a.lse[(i64)(q.row0 + fr) * a.heads + hq] = lse_of(top, sum);
 }
 
 }  // namespace ptk
