@@ -13,7 +13,7 @@
 // all scores, but a tile's boxes beyond a CTA's own half are free again as soon as they are: the boxes that are values too have a ring of three tiles, the others one of
 // eight boxes.
 //
-// Warps 0-3 softmax, and Q and the output of an item; 4 and 6 load (values and other boxes); 5 issues the tensor instructions.  One CTA (or pair) per SM (or two) takes an
+// Warps 0-3 softmax, and Q and the output of an item; 4 and 6 load (values and other boxes); 5 issues the scores' instructions, 7 the output's.  One CTA (or pair) per SM (or two) takes an
 // even share of the line of all (request, row tile, 64 tokens) units.  An item that spans several CTAs leaves sums (o, m, l in 32 bits) in the workspace,
 // which latent_join_kernel joins in CTA order.
 #pragma once
@@ -22,7 +22,7 @@
 
 namespace ptk {
 
-constexpr int LA_THREADS = 224, LA_KEYS = 64, LA_ROPE = 64, LA_BOX = LA_KEYS * 128;      // a box: 64 tokens, 64 elements
+constexpr int LA_THREADS = 256, LA_KEYS = 64, LA_ROPE = 64, LA_BOX = LA_KEYS * 128;      // a box: 64 tokens, 64 elements
 constexpr int LA_MIN_UNITS = 2;              // a CTA takes at least this many, so that joining does not cost more than it saves
 
 template <int L, bool WIDE>
@@ -41,7 +41,7 @@ struct LatentShape {
 template <int L, bool WIDE>
 struct LatentMisc {
   using Shape = LatentShape<L, WIDE>;
-  u64 v_full[Shape::STAGES], v_empty[Shape::STAGES], k_full[Shape::SLOTS], k_empty[Shape::SLOTS], q, q_free, s, s_free, p, pv, end, left, scan[LA_THREADS / 32];
+  u64 v_full[Shape::STAGES], v_empty[Shape::STAGES], k_full[Shape::SLOTS], k_empty[Shape::SLOTS], q, q_free, s, s_free, p, pv, end[2], left, scan[LA_THREADS / 32];
   u32 valid[Shape::STAGES], tmem;
   int gave_up, any_bad, r;
   float f[Shape::ROWS];
@@ -139,7 +139,8 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
     bar_init(&s.s_free, 128);
     bar_init(&s.p, 128);
     bar_init(&s.pv, 1);
-    bar_init(&s.end, 1);
+    bar_init(&s.end[0], 1);
+    bar_init(&s.end[1], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s.gave_up = s.any_bad = 0;
     s.r = -1;
@@ -198,63 +199,72 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
   };
 
   if (warp == 5) {
-    // ======== tensor instructions: S of step g + 1 before the output of step g
-    constexpr u32 QK = mma_desc_a(F16, false) | (u32)(LA_KEYS >> 3) << 17, PV = mma_desc_a(F16, true);
+    // ======== scores: a step's as soon as its tile is there and the ones before it have been read
+    constexpr u32 QK = mma_desc_a(F16, false) | (u32)(LA_KEYS >> 3) << 17;
     u32 g = 0, item = 0, op = 0;              // step, item, box that is no value
     bool quit = false;
-    auto wait = [&](u64* b, u32 parity) {
-      if (!quit && !__all_sync(FULL, bar_wait(b, parity, a.polls, &s.gave_up))) quit = true;
-    };
-    auto box = [&](int i, u32 at) {           // scores' part of box i, which lies at `at`
-      if (!quit && elected()) {
-        const u64 kb = operand_desc(at, 0);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {         // 16 elements: 8 columns, or 32 bytes further in a row
-          if (i < Shape::Q_TMEM) mma_ts(tmem + Shape::S_AT, tmem + Shape::Q_AT + i * 32 + k * 8, kb + (u64)((k * 32) >> 4), QK, i > 0 || k > 0);
-          else mma_ss(tmem + Shape::S_AT, operand_desc(smem_q + (i - Shape::Q_TMEM) * 16384, 0) + (u64)((k * 32) >> 4), kb + (u64)((k * 32) >> 4), QK, i > 0 || k > 0);
-        }
-      }
+    // lane i of the first n waits for its own barrier
+    auto wait = [&](u32 n, u64* b, u32 parity) {
+      if (!quit && !__all_sync(FULL, lane >= (int)n || bar_wait(b, parity, a.polls, &s.gave_up))) quit = true;
       __syncwarp();
     };
-    auto scores = [&](u32 n) {                // of step n
-      if (n > 0) wait(&s.s_free, (n - 1) & 1);
-      wait(&s.v_full[n % STAGES], (n / STAGES) & 1);
-      tc_fence_after();
+    auto box = [&](int i, u32 at, bool first) {           // scores' part of box i, which lies at `at`
+      const u64 kb = operand_desc(at, 0);
 #pragma unroll
-      for (int i = 0; i < VALUES; ++i) box(i, smem_v + ((n % STAGES) * VALUES + i) * LA_BOX);
-#pragma unroll
-      for (int i = 0; i < OTHERS; ++i, ++op) {
-        wait(&s.k_full[op % SLOTS], (op / SLOTS) & 1);
-        tc_fence_after();
-        box(VALUES + i, smem_k + (op % SLOTS) * LA_BOX);
-        if (!quit && elected()) tc_commit(&s.k_empty[op % SLOTS]);
-        __syncwarp();
+      for (int k = 0; k < 4; ++k) {           // 16 elements: 8 columns, or 32 bytes further in a row
+        if (i < Shape::Q_TMEM) mma_ts(tmem + Shape::S_AT, tmem + Shape::Q_AT + i * 32 + k * 8, kb + (u64)((k * 32) >> 4), QK, !first || k > 0);
+        else mma_ss(tmem + Shape::S_AT, operand_desc(smem_q + (i - Shape::Q_TMEM) * 16384, 0) + (u64)((k * 32) >> 4), kb + (u64)((k * 32) >> 4), QK, !first || k > 0);
       }
-      if (!quit && elected()) tc_commit(&s.s);
-      __syncwarp();
     };
     while (!quit && line.next()) {
-      const u32 n = line.ub - line.ua;
-      const int rows = min(NQ, line.q.fresh * a.group - (int)(line.rt * NQ));
-      const u32 pv = PV | (u32)((rows + 15) / 16 * 2) << 17;
-      wait(&s.q, item & 1);
-      scores(g);
-      for (u32 j = 0; j < n && !quit; ++j, ++g) {
-        // the next step's scores first if its tile is there by now, or else whatever comes first
-        const bool more = j + 1 < n;
-        bool ahead = false;
-        if (more) {
-          u64 *const v = &s.v_full[(g + 1) % STAGES], *const k = &s.k_full[(op + OTHERS - 1) % SLOTS], *const p = &s.p;
-          for (u32 i = 0; i < a.polls && !ahead; ++i) {
-            ahead = __all_sync(FULL, bar_test(v, ((g + 1) / STAGES) & 1) && bar_test(k, ((op + OTHERS - 1) / SLOTS) & 1));
-            if (!ahead && __all_sync(FULL, bar_try(p, g & 1))) break;
+      const int n = line.ub - line.ua;
+      wait(1, &s.q, item & 1);
+      for (int j = 0; j < n && !quit; ++j, ++g, op += OTHERS) {
+        if (g > 0) wait(1, &s.s_free, (g - 1) & 1);
+        // boxes that are no values first, since what follows them is waiting for their places; a few at a time, so that each wait and commit serves several
+        constexpr int PARTS = OTHERS > 2 ? 2 : 1, EACH = (OTHERS + PARTS - 1) / PARTS;
+#pragma unroll
+        for (int i0 = 0; i0 < OTHERS; i0 += EACH) {
+          const u32 o = op + i0 + lane;
+          wait(i0 + EACH <= OTHERS ? EACH : OTHERS - i0, &s.k_full[o % SLOTS], (o / SLOTS) & 1);
+          tc_fence_after();
+          if (!quit && elected()) {
+#pragma unroll
+            for (int i = i0; i < i0 + EACH && i < OTHERS; ++i) box(VALUES + i, smem_k + ((op + i) % SLOTS) * LA_BOX, i == 0);
+#pragma unroll
+            for (int i = i0; i < i0 + EACH && i < OTHERS; ++i) tc_commit(&s.k_empty[(op + i) % SLOTS]);
           }
-          if (ahead) scores(g + 1);
-        } else if (!quit && elected()) tc_commit(&s.q_free);
-        __syncwarp();
-        wait(&s.p, g & 1);
+          __syncwarp();
+        }
+        wait(1, &s.v_full[g % STAGES], (g / STAGES) & 1);
         tc_fence_after();
         if (!quit && elected()) {
+#pragma unroll
+          for (int i = 0; i < VALUES; ++i) box(i, smem_v + ((g % STAGES) * VALUES + i) * LA_BOX, false);
+          tc_commit(&s.s);
+          if (j + 1 == n) tc_commit(&s.q_free);
+        }
+        __syncwarp();
+      }
+      ++item;
+    }
+    // everything issued has ended before tensor and shared memory are given back
+    if (elected()) tc_commit(&s.end[0]);
+    __syncwarp();
+    bar_drain(&s.end[0], 0);
+  } else if (warp == 7) {
+    // ======== the output, when a step's weights are there
+    constexpr u32 PV = mma_desc_a(F16, true);
+    u32 g = 0;
+    bool quit = false;
+    while (!quit && line.next()) {
+      const int n = line.ub - line.ua, rows = min(NQ, line.q.fresh * a.group - (int)(line.rt * NQ));
+      const u32 pv = PV | (u32)((rows + 15) / 16 * 2) << 17;
+      for (int j = 0; j < n; ++j, ++g) {
+        // (the tile has been there since its scores: waited for only so that its bytes are this warp's too)
+        if (!__all_sync(FULL, bar_wait(&s.p, g & 1, a.polls, &s.gave_up) && bar_wait(&s.v_full[g % STAGES], (g / STAGES) & 1, a.polls, &s.gave_up))) { quit = true; break; }
+        tc_fence_after();
+        if (elected()) {
           const u32 tile = smem_v + (g % STAGES) * VALUES * LA_BOX;
           const u64 pb = operand_desc(smem_p, 0);
 #pragma unroll
@@ -268,14 +278,11 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
           tc_commit(&s.pv);
         }
         __syncwarp();
-        if (more && !ahead) scores(g + 1);
       }
-      ++item;
     }
-    // everything issued has ended before tensor and shared memory are given back
-    if (elected()) tc_commit(&s.end);
+    if (elected()) tc_commit(&s.end[1]);
     __syncwarp();
-    bar_drain(&s.end, 0);
+    bar_drain(&s.end[1], 0);
   } else if (warp >= 4) {
     // ======== tiles: warp 4 the boxes that are values, warp 6 the others.  Lane j has the tokens of copy j of a box, some tokens of a block each.
     const bool values = warp == 4;
