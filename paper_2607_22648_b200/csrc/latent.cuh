@@ -192,7 +192,6 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
   const u32 tmem = s.tmem;
   const u32 smem_q = smem_addr(smem), smem_p = smem_q + Shape::Q_BYTES, smem_v = smem_q + Shape::V_AT, smem_k = smem_q + Shape::K_AT;
   LatentLine<NQ> line{a, u_begin, u_end, s.left, per, s.r, 0, request(a, s.r)};
-  const volatile int* const gave_up = &s.gave_up;
   // the elements of box i of a tile, in the order of the products: this CTA's values, the other half's, the rotary part
   auto element_of = [&](int i) {
     return 64 * (i < VALUES ? (int)half * VALUES + i : i < L / 64 ? (int)(1 - half) * VALUES + i - VALUES : L / 64);
@@ -203,9 +202,8 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
     constexpr u32 QK = mma_desc_a(F16, false) | (u32)(LA_KEYS >> 3) << 17;
     u32 g = 0, item = 0, op = 0;              // step, item, box that is no value
     bool quit = false;
-    // lane i of the first n waits for its own barrier
-    auto wait = [&](u32 n, u64* b, u32 parity) {
-      if (!quit && !__all_sync(FULL, lane >= (int)n || bar_wait(b, parity, a.polls, &s.gave_up))) quit = true;
+    auto wait = [&](u64* b, u32 parity) {     // (a lane may have a barrier of its own)
+      if (!quit && !__all_sync(FULL, bar_wait(b, parity, a.polls, &s.gave_up))) quit = true;
       __syncwarp();
     };
     auto box = [&](int i, u32 at, bool first) {           // scores' part of box i, which lies at `at`
@@ -218,27 +216,20 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
     };
     while (!quit && line.next()) {
       const int n = line.ub - line.ua;
-      wait(1, &s.q, item & 1);
       for (int j = 0; j < n && !quit; ++j, ++g, op += OTHERS) {
-        if (g > 0) wait(1, &s.s_free, (g - 1) & 1);
-        // boxes that are no values first, since what follows them is waiting for their places; a few at a time, so that each wait and commit serves several
-        constexpr int PARTS = OTHERS > 2 ? 2 : 1, EACH = (OTHERS + PARTS - 1) / PARTS;
-#pragma unroll
-        for (int i0 = 0; i0 < OTHERS; i0 += EACH) {
-          const u32 o = op + i0 + lane;
-          wait(i0 + EACH <= OTHERS ? EACH : OTHERS - i0, &s.k_full[o % SLOTS], (o / SLOTS) & 1);
-          tc_fence_after();
-          if (!quit && elected()) {
-#pragma unroll
-            for (int i = i0; i < i0 + EACH && i < OTHERS; ++i) box(VALUES + i, smem_k + ((op + i) % SLOTS) * LA_BOX, i == 0);
-#pragma unroll
-            for (int i = i0; i < i0 + EACH && i < OTHERS; ++i) tc_commit(&s.k_empty[(op + i) % SLOTS]);
-          }
-          __syncwarp();
-        }
-        wait(1, &s.v_full[g % STAGES], (g / STAGES) & 1);
+        // the tile (and Q), all at once; then the scores before these have been read
+        const u32 o = op + (lane < OTHERS ? lane : 0);
+        const bool first = j == 0 && lane == OTHERS + 1, value = lane == OTHERS;
+        wait(first ? &s.q : value ? &s.v_full[g % STAGES] : &s.k_full[o % SLOTS], (first ? item : value ? g / STAGES : o / SLOTS) & 1);
+        if (g > 0) wait(&s.s_free, (g - 1) & 1);
         tc_fence_after();
         if (!quit && elected()) {
+          // boxes that are no values first: what follows them is waiting for their places
+#pragma unroll
+          for (int i = 0; i < OTHERS; ++i) {
+            box(VALUES + i, smem_k + ((op + i) % SLOTS) * LA_BOX, i == 0);
+            tc_commit(&s.k_empty[(op + i) % SLOTS]);
+          }
 #pragma unroll
           for (int i = 0; i < VALUES; ++i) box(i, smem_v + ((g % STAGES) * VALUES + i) * LA_BOX, false);
           tc_commit(&s.s);
@@ -345,8 +336,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
     u32 g = 0, item = 0;
     bool quit = false;
     auto wait = [&](u64* b, u32 parity) {
-      const bool ok = bar_wait(b, parity, a.polls, &s.gave_up);
-      if (__any_sync(FULL, !ok || *gave_up)) quit = true;
+      if (__any_sync(FULL, !bar_wait(b, parity, a.polls, &s.gave_up))) quit = true;
     };
     // Q of an item, a row a thread.  Rows that do not exist keep what lies there: their sums are never looked at, and a row's are its own.
     auto load_q = [&](const LatentLine<NQ>& it) {
@@ -407,6 +397,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
         const int k0 = (ua + j) * LA_KEYS;
         const u32 st = g % STAGES;
         // (a wait that ran out in one warp shows in all of them at the next barrier: until then its values are of no use, but in bounds)
+        wait(&s.v_full[st], (g / STAGES) & 1);        // (there before the scores are: makes the tile's bytes and its valid bits this thread's too)
         wait(&s.s, g & 1);
         tc_fence_after();
         float v[2][32];
@@ -420,7 +411,6 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
           tc_fence_before();
         }
         bar_arrive(&s.s_free);
-        wait(&s.v_full[st], (g / STAGES) & 1);        // (has ended long ago: makes the tile's bytes and its valid bits this thread's too)
         const u32 valid = s.valid[st];
         const bool edge = k0 + LA_KEYS > all_see || valid != 0xFFu;
         if (edge) {
