@@ -23,6 +23,10 @@
 namespace ptk {
 
 constexpr int LA_THREADS = 256, LA_KEYS = 64, LA_ROPE = 64, LA_BOX = LA_KEYS * 128;      // a box: 64 tokens, 64 elements
+// A reference moves when a scaled score exceeds it by more than this.  Weights are then at most 2^14 (fp16 holds 2^15): with 8, the tiles of 128 rows whose scores spread over 5
+// octaves (standard deviation) were rescaled in every other step, 1400 clocks each.
+constexpr float LA_MOVE = 14.0f;
+constexpr int LA_AHEAD = 4;                  // units (of a pair of CTAs) that are brought into L2 before they are loaded
 constexpr int LA_MIN_UNITS = 2;              // a CTA takes at least this many, so that joining does not cost more than it saves
 
 template <int L, bool WIDE>
@@ -32,10 +36,10 @@ struct LatentShape {
   static constexpr int DIMS = VALUES * 64, MT = DIMS / 128;                               // output elements, instructions' worth of them
   // tensor memory: O, S, Q
   static constexpr int S_AT = MT * ROWS, Q_AT = S_AT + LA_KEYS, Q_MOST = (512 - Q_AT) / 32, Q_TMEM = Q_MOST < BOXES ? Q_MOST : BOXES;
-  // shared memory: the rest of Q, P, the rings
-  static constexpr int Q_BYTES = (BOXES - Q_TMEM) * 128 * 128, P_BYTES = ROWS * 128;
+  // shared memory: P, the rest of Q (or a box of it on its way to tensor memory), the rings
+  static constexpr int P_BYTES = ROWS * 128, Q_BYTES = (BOXES > Q_TMEM ? BOXES - Q_TMEM : 1) * ROWS * 128;
   static constexpr int STAGES = L == 512 ? 3 : WIDE ? 6 : 5, SLOTS = WIDE ? (L == 512 ? 8 : 12) : STAGES;
-  static constexpr int V_AT = Q_BYTES + P_BYTES, K_AT = V_AT + STAGES * VALUES * LA_BOX, MISC_AT = K_AT + SLOTS * LA_BOX;
+  static constexpr int V_AT = P_BYTES + Q_BYTES, K_AT = V_AT + STAGES * VALUES * LA_BOX, MISC_AT = K_AT + SLOTS * LA_BOX;
   static constexpr int PART = ROWS * (DIMS + 2);                                          // floats of an item's sums in one CTA: o, m, l
 };
 template <int L, bool WIDE>
@@ -44,7 +48,8 @@ struct LatentMisc {
   u64 v_full[Shape::STAGES], v_empty[Shape::STAGES], k_full[Shape::SLOTS], k_empty[Shape::SLOTS], q, q_free, s, s_free, p, pv, end[2], left, scan[LA_THREADS / 32];
   u32 valid[Shape::STAGES], tmem;
   int gave_up, any_bad, r;
-  float f[Shape::ROWS];
+  alignas(16) float f[Shape::ROWS];
+  alignas(16) u32 moved[4];  // of each warp's rows: 1 a reference has moved, 2 a wait ran out
   int bad[Shape::DIMS];      // first token whose element d is not finite, among tokens that some rows do not see
 };
 template <int L, bool WIDE>
@@ -107,6 +112,9 @@ __host__ __device__ constexpr u32 mma_desc_a(bool fp16, bool a_mn_major) {
 __device__ __forceinline__ void tensor_load_box(u32 dst, const CUtensorMap* map, int element, int token, int block, u64* bar) {
   asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(element), "r"(token),
                "r"(block), "r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void tensor_prefetch_box(const CUtensorMap* map, int element, int token, int block) {      // into L2
+  asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(element), "r"(token), "r"(block) : "memory");
 }
 __device__ __forceinline__ bool any_of_softmax(bool v) {      // barrier of the 128 softmax threads
   u32 r;
@@ -190,7 +198,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
   __syncthreads();
   tc_fence_after();
   const u32 tmem = s.tmem;
-  const u32 smem_q = smem_addr(smem), smem_p = smem_q + Shape::Q_BYTES, smem_v = smem_q + Shape::V_AT, smem_k = smem_q + Shape::K_AT;
+  const u32 smem_p = smem_addr(smem), smem_q = smem_p + Shape::P_BYTES, smem_v = smem_p + Shape::V_AT, smem_k = smem_p + Shape::K_AT;
   LatentLine<NQ> line{a, u_begin, u_end, s.left, per, s.r, 0, request(a, s.r)};
   // the elements of box i of a tile, in the order of the products: this CTA's values, the other half's, the rotary part
   auto element_of = [&](int i) {
@@ -287,7 +295,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
         const int key = unit * LA_KEYS + (int)(mine_at * bt);
         return key < line.keys ? table[(u32)key / B] : -1;
       };
-      int id = look_up(line.ua);
+      int id = look_up(line.ua), far_id = WIDE && !values && line.ua + LA_AHEAD < line.ub ? look_up(line.ua + LA_AHEAD) : -1;
       for (int unit = line.ua; unit < line.ub && !quit; ++unit, ++g) {
         const int key = unit * LA_KEYS + (int)(mine_at * bt);
         const bool in = key < line.keys, have = in && (u32)id < a.cache.num_blocks;
@@ -310,6 +318,13 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
             for (u32 i = team; i < VALUES; i += teams)
               tensor_load_box(smem_v + (st * VALUES + i) * LA_BOX + mine_at * bt * 128, &map, element_of((int)i), token, block, &s.v_full[st]);
         } else {
+          if (WIDE) {
+            // Few boxes are on their way at a time, so each CTA of a pair has its half of a later unit's brought nearer
+            const int far = unit + LA_AHEAD, fkey = far * LA_KEYS + (int)(mine_at * bt);
+            if (far < line.ub && (u32)far_id < a.cache.num_blocks)
+              for (u32 i = team; i < VALUES + (half == 0); i += teams) tensor_prefetch_box(&map, i < VALUES ? element_of((int)i) : L, (int)((u32)fkey % B), far_id);
+            far_id = far + 1 < line.ub ? look_up(far + 1) : -1;
+          }
           for (u32 i = 0; i < OTHERS; ++i, ++op) {
             const u32 st = op % SLOTS;
             if (op >= SLOTS && !__all_sync(FULL, bar_wait(&s.k_empty[st], (op / SLOTS - 1) & 1, a.polls, &s.gave_up))) { quit = true; break; }
@@ -338,40 +353,47 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
     auto wait = [&](u64* b, u32 parity) {
       if (__any_sync(FULL, !bar_wait(b, parity, a.polls, &s.gave_up))) quit = true;
     };
-    // Q of an item, a row a thread.  Rows that do not exist keep what lies there: their sums are never looked at, and a row's are its own.
+    // Q of an item, a row a thread.  Eight lanes read 128 bytes of a row at once, and rows change into lanes through shared memory (a row a lane would touch 32 lines with each load).
+    // The loop is short because its code is cold every time.  Rows that do not exist have another row's values: their sums are never looked at, and a row's are its own.
     auto load_q = [&](const LatentLine<NQ>& it) {
       const int base = (int)(it.rt * NQ), rows = min(NQ, it.q.fresh * a.group - base);
       if (warp * 32 < rows) {
-        const bool live = row < rows;
-        const int flat = base + (live ? row : 0), fr = flat / a.group, hq = flat % a.group;
+        const int flat = base + min(row, rows - 1), fr = flat / a.group, hq = flat % a.group;
         const i64 tok = it.q.row0 + fr;
-        const unsigned char *const ql = a.q + 2 * (tok * a.q_token + hq * a.q_head), *const qr = la.q_rope + 2 * (tok * la.qr_token + hq * la.qr_head);
+        const i64 latent_at = 2 * (tok * a.q_token + hq * a.q_head), rope_at = 2 * (tok * la.qr_token + hq * la.qr_head);
         constexpr int AT_ONCE = 3;            // boxes on their way
-#pragma unroll
+#pragma unroll 1
         for (int i0 = 0; i0 < BOXES; i0 += AT_ONCE) {
           uint4 v[AT_ONCE][8];
 #pragma unroll
-          for (int i = 0; i < AT_ONCE; ++i)
-            if (i0 + i < BOXES) {
-              const int e = element_of(i0 + i);
-              const uint4* src = reinterpret_cast<const uint4*>(e < L ? ql + 2 * e : qr);
+          for (int i = 0; i < AT_ONCE; ++i) {
+            const int b = min(i0 + i, BOXES - 1);
+            const i64 mine = b < L / 64 ? latent_at + 2 * element_of(b) : rope_at;
+            const unsigned char* const src = (b < L / 64 ? a.q : la.q_rope) + (lane & 7) * 16;
 #pragma unroll
-              for (int c = 0; c < 8; ++c) v[i][c] = live ? src[c] : make_uint4(0, 0, 0, 0);
+            for (int k = 0; k < 8; ++k) v[i][k] = *reinterpret_cast<const uint4*>(src + __shfl_sync(FULL, mine, k * 4 + (lane >> 3)));
+          }
+#pragma unroll
+          for (int i = 0; i < AT_ONCE; ++i) {
+            const int b = i0 + i;
+            if (b >= BOXES) continue;
+            unsigned char* const z = smem + Shape::P_BYTES + max(b - Shape::Q_TMEM, 0) * (NQ * 128) + warp * 4096;
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const int r = k * 4 + (lane >> 3);
+              *reinterpret_cast<uint4*>(z + r * 128 + (((lane ^ r) & 7) * 16)) = v[i][k];
             }
+            if (b >= Shape::Q_TMEM) continue;
+            __syncwarp();
+            u32 w[32];
 #pragma unroll
-          for (int i = 0; i < AT_ONCE; ++i)
-            if (i0 + i < BOXES) {
-              if (i0 + i < Shape::Q_TMEM) {
-                u32 w[32];
-#pragma unroll
-                for (int c = 0; c < 8; ++c) { w[4 * c] = v[i][c].x; w[4 * c + 1] = v[i][c].y; w[4 * c + 2] = v[i][c].z; w[4 * c + 3] = v[i][c].w; }
-                tc_st32(tmem + lane_base + Shape::Q_AT + (i0 + i) * 32, w);
-              } else {
-#pragma unroll
-                for (int c = 0; c < 8; ++c)
-                  *reinterpret_cast<uint4*>(smem + (i0 + i - Shape::Q_TMEM) * 16384 + row * 128 + ((c ^ (row & 7)) * 16)) = v[i][c];
-              }
+            for (int c = 0; c < 8; ++c) {
+              const uint4 x = *reinterpret_cast<const uint4*>(z + lane * 128 + ((c ^ (lane & 7)) * 16));
+              w[4 * c] = x.x; w[4 * c + 1] = x.y; w[4 * c + 2] = x.z; w[4 * c + 3] = x.w;
             }
+            tc_st32(tmem + lane_base + Shape::Q_AT + b * 32, w);
+          }
         }
         tc_wait_st();
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -443,11 +465,18 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
             }
           }
         }
-        float top = -INFINITY;
+        float f = 1.0f;
+        bool move = false;
+        u32 p[32];
         if (busy) {
           // the products rounded as the maximum is, so that the largest weight is 1 however large the scores are
+          const u64 sc2 = pair(a.scale2, a.scale2);
 #pragma unroll
-          for (int i = 0; i < 64; ++i) v[i >> 5][i & 31] = __fmul_rn(v[i >> 5][i & 31], a.scale2);
+          for (int i = 0; i < 64; i += 2) {
+            const u64 y = mul_pair(pair(v[i >> 5][i & 31], v[i >> 5][(i & 31) + 1]), sc2);
+            v[i >> 5][i & 31] = lo_of(y);
+            v[i >> 5][(i & 31) + 1] = hi_of(y);
+          }
           if (edge) {
 #pragma unroll
             for (int i = 0; i < 64; ++i)
@@ -458,54 +487,62 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
           for (int i = 0; i < 64; i += 8)
 #pragma unroll
             for (int k = 0; k < 4; ++k) x4[k] = fmaxf(x4[k], fmaxf(v[i >> 5][(i & 31) + 2 * k], v[i >> 5][(i & 31) + 2 * k + 1]));
-          top = fmaxf(fmaxf(x4[0], x4[1]), fmaxf(x4[2], x4[3]));
+          const float top = fmaxf(fmaxf(x4[0], x4[1]), fmaxf(x4[2], x4[3]));
+          move = live && (top > m + LA_MOVE || (m == -INFINITY && top > m));
+          if (move) {
+            f = exp2_fast(m - top);
+            m = top;
+            l *= f;
+          }
+          const float ref = m == -INFINITY ? 0.0f : m;
+          float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int i = 0; i < 64; i += 2) {
+            const float p0 = exp2_fast(v[i >> 5][i & 31] - ref), p1 = exp2_fast(v[i >> 5][(i & 31) + 1] - ref);
+            sum[(i >> 1) & 3] += p0 + p1;
+            p[i >> 1] = pack2<F16>(p0, p1);
+          }
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         }
         // the output and the weights of the step before are done with
         if (g > 0) wait(&s.pv, (g - 1) & 1);
         tc_fence_after();
-        const bool move = live && (top > m + 8.0f || (m == -INFINITY && top > m));
-        float f = 1.0f;
-        if (move) {
-          f = exp2_fast(m - top);
-          m = top;
-          l *= f;
-        }
-        const bool some = any_of_softmax(move || quit);
-        if (some && any_of_softmax(quit)) { quit = true; break; }
-        if (some && j > 0) {
-          if (row < NQ) s.f[row] = f;
-          asm volatile("bar.sync 3, 128;" ::: "memory");
-#pragma unroll 1
-          for (int c = 0; c < MT * NQ; c += 32) {
-            if ((c % NQ) >= rows) continue;
-            float o[32];
-            tc_ld32(o, to + c);
-            tc_wait_ld();
-            tc_loaded(o);
-            u32 scaled[32];
+        const bool any = __any_sync(FULL, move);
+        if (lane == 0) s.moved[warp] = (any ? 1u : 0u) | (quit ? 2u : 0u);
+        if (row < NQ) s.f[row] = f;
+        asm volatile("bar.sync 2, 128;" ::: "memory");
+        const uint4 flags = *reinterpret_cast<const uint4*>(s.moved);
+        const u32 moved[4] = {flags.x, flags.y, flags.z, flags.w};
+        if ((moved[0] | moved[1] | moved[2] | moved[3]) & 2) { quit = true; break; }
+        if (j > 0) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) scaled[i] = __float_as_uint(o[i] * s.f[c % NQ + i]);
-            tc_st32(to + c, scaled);
+          for (int w = 0; w < NQ / 32; ++w) {               // 32 rows, where one of them has moved
+            if (!(moved[w] & 1)) continue;
+#pragma unroll 1
+            for (int c = w * 32; c < MT * NQ; c += NQ) {
+              float o[32];
+              tc_ld32(o, to + c);
+              tc_wait_ld();
+              tc_loaded(o);
+              u32 scaled[32];
+#pragma unroll
+              for (int i = 0; i < 32; i += 4) {
+                const float4 f4 = *reinterpret_cast<const float4*>(&s.f[w * 32 + i]);
+                scaled[i] = __float_as_uint(o[i] * f4.x);
+                scaled[i + 1] = __float_as_uint(o[i + 1] * f4.y);
+                scaled[i + 2] = __float_as_uint(o[i + 2] * f4.z);
+                scaled[i + 3] = __float_as_uint(o[i + 3] * f4.w);
+              }
+              tc_st32(to + c, scaled);
+            }
           }
           tc_wait_st();
         }
-        const float ref = m == -INFINITY ? 0.0f : m;
-        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         if (live) {
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            u32 two[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int i = c * 8 + 2 * k;
-              const float p0 = exp2_fast(v[i >> 5][i & 31] - ref), p1 = exp2_fast(v[i >> 5][(i & 31) + 1] - ref);
-              sum[k] += p0 + p1;
-              two[k] = pack2<F16>(p0, p1);
-            }
-            *reinterpret_cast<uint4*>(smem + Shape::Q_BYTES + row * 128 + ((c ^ (row & 7)) * 16)) = make_uint4(two[0], two[1], two[2], two[3]);
-          }
+          for (int c = 0; c < 8; ++c)
+            *reinterpret_cast<uint4*>(smem + row * 128 + ((c ^ (row & 7)) * 16)) = make_uint4(p[4 * c], p[4 * c + 1], p[4 * c + 2], p[4 * c + 3]);
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         tc_fence_before();
         bar_arrive(&s.p);
@@ -545,21 +582,47 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
         tc_ld32(o, to + c);
         tc_wait_ld();
         tc_loaded(o);
-        const int bad = any_bad ? s.bad[d] : 0x7FFFFFFF;
-        int fr = (row_base + r0) / a.group, hq = (row_base + r0) % a.group;
-        unsigned char* dst = a.out + 2 * ((i64)(rq.row0 + fr) * a.o_token + (i64)hq * a.o_head + (int)half * DIMS + d);
+        // (all in registers before the first is stored: a store between the factors' loads would keep them in order, one by one)
+        const int m32 = min(32, rows - r0);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          if (r0 + i < rows) {
-            // weights that are all zero leave zeros (or NaN: what the factor says)
-            const float f = s.f[r0 + i];
-            float y = o[i] * f;
-            if (bad != 0x7FFFFFFF && seen_by(r0 + i) > bad) y = NAN;
-            if (whole) *reinterpret_cast<unsigned short*>(dst) = (unsigned short)pack2<F16>(y, 0.0f);
-            else my[(r0 + i) * DIMS + d] = y;
-            dst += 2 * a.o_head;
-            if (++hq == a.group) { hq = 0; dst += 2 * (a.o_token - (i64)a.group * a.o_head); }
+        for (int i = 0; i < 32; i += 4) {
+          const float4 f4 = *reinterpret_cast<const float4*>(&s.f[r0 + i]);
+          o[i] *= f4.x;                       // weights that are all zero leave zeros (or NaN: what the factor says)
+          o[i + 1] *= f4.y;
+          o[i + 2] *= f4.z;
+          o[i + 3] *= f4.w;
+        }
+        if (any_bad) {
+          const int bad = s.bad[d];
+          if (bad != 0x7FFFFFFF) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (seen_by(r0 + i) > bad) o[i] = NAN;
           }
+        }
+        if (whole) {
+          // whole rows of 128 elements through shared memory (P's, which the last products have read)
+          unsigned char* const z = smem + (WIDE ? ((c >> 5) & 1) * 8192 : 0);
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            const u32 two = pack2<F16>(o[i], o[i + 1]);
+            *reinterpret_cast<unsigned short*>(z + i * 256 + tid * 2) = (unsigned short)two;
+            *reinterpret_cast<unsigned short*>(z + i * 256 + 256 + tid * 2) = (unsigned short)(two >> 16);
+          }
+          asm volatile("bar.sync 3, 128;" ::: "memory");
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int i = k * 8 + (tid >> 4), flat = row_base + r0 + i;
+            if (i < m32)
+              *reinterpret_cast<uint4*>(a.out + 2 * ((i64)(rq.row0 + flat / a.group) * a.o_token + (i64)(flat % a.group) * a.o_head + (int)half * DIMS + c / NQ * 128 + (tid & 15) * 8)) =
+                  *reinterpret_cast<const uint4*>(z + i * 256 + (tid & 15) * 16);
+          }
+          if (!WIDE) asm volatile("bar.sync 3, 128;" ::: "memory");       // (two places take turns where there are two)
+        } else {
+          float* const dst = my + r0 * DIMS + d;
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (i < m32) dst[i * DIMS] = o[i];
         }
       }
       tc_fence_before();
