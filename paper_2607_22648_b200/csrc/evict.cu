@@ -8,11 +8,12 @@ namespace {
 constexpr u32 FULL = 0xFFFFFFFFu;
 
 // ---- which tokens ---------------------------------------------------------------------------------------------------------------------
-// One CTA per request and head.  The smallest weight to keep is found by its bits, four at a time from the top (eight rounds over the candidates, which the
-// threads hold in registers or read again from L2); then one pass in index order writes the kept tokens.  Bound by latency: rounds of counting, each with
-// one exchange among the warps.
-constexpr int SEL_THREADS = 512, SEL_WARPS = SEL_THREADS / 32;
-constexpr int SEL_HELD = 16;                 // weights a thread holds: requests of up to 8192 tokens are read once
+// One CTA per request and head.  The smallest weight to keep is found by its bits, 11 + 11 + 10 from the top: a histogram of the candidates that agree so far in shared memory, a scan
+// of its counts from the largest down.  Then one pass in index order writes the kept tokens: every warp has consecutive ones, so that a scan of the warps' counts is all they exchange.
+// Rows of up to 8192 tokens are read once and stay in registers.  Bound by latency: 4 x 3 barriers and the reads.
+constexpr int SEL_THREADS = 1024, SEL_WARPS = SEL_THREADS / 32;
+constexpr int SEL_HELD = 8, SEL_SEGMENT = SEL_THREADS * SEL_HELD;       // tokens a thread, the CTA holds
+constexpr int SEL_BINS = 2048;
 
 struct SelectArgs {
   const float* weights;
@@ -33,8 +34,9 @@ __device__ __forceinline__ u32 order_of(float w) {
 }
 
 __global__ void __launch_bounds__(SEL_THREADS) select_kernel(SelectArgs a) {
-  __shared__ u32 s_count[2][SEL_WARPS][16];
+  __shared__ u32 s_bins[3][SEL_BINS];
   __shared__ u32 s_scan[2][SEL_WARPS];
+  __shared__ u32 s_digit, s_want;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int r = blockIdx.x / a.heads, h = blockIdx.x % a.heads;
   const int raw = a.lengths[r], len = raw < 0 ? 0 : raw > a.width ? a.width : raw;
@@ -47,98 +49,104 @@ __global__ void __launch_bounds__(SEL_THREADS) select_kernel(SelectArgs a) {
     if (raw != len && a.status) atomicOr(a.status, PTSTORE_S_BOUNDS);
   }
   const int lo = len > a.budget ? a.first : 0, hi = len > a.budget ? len - a.recent : 0;      // candidates
-  int want = a.budget - a.first - a.recent;                                                  // of them
+  u32 want = (u32)(a.budget - a.first - a.recent);                                           // of them
+  // thread's tokens of a segment: consecutive ones a warp, consecutive lanes
+  float held[SEL_HELD];
+  const int mine = warp * (32 * SEL_HELD) + lane;
+  auto load = [&](int segment) {
+#pragma unroll
+    for (int i = 0; i < SEL_HELD; ++i) {
+      const int j = segment + mine + i * 32;
+      held[i] = j < len ? w[j] : 0.0f;
+    }
+  };
+  load(0);
+  const bool once = len <= SEL_SEGMENT;
   // ---- the smallest order that is kept, and how many candidates of just that order
   u32 bound = 0;
   if (hi > lo && want > 0) {
-    u32 held[SEL_HELD];
-    const bool fits = hi - lo <= SEL_HELD * SEL_THREADS;
-    if (fits) {
+    for (int i = tid; i < 3 * SEL_BINS; i += SEL_THREADS) (&s_bins[0][0])[i] = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int round = 0; round < 3; ++round) {
+      const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, above = round == 0 ? 0 : round == 1 ? 21 : 10;
+      const u32 mask = round == 2 ? 1023u : 2047u;
+      for (int segment = 0; segment < len; segment += SEL_SEGMENT) {
+        if (!once) load(segment);
 #pragma unroll
-      for (int i = 0; i < SEL_HELD; ++i) {
-        const int j = lo + i * SEL_THREADS + tid;
-        held[i] = j < hi ? order_of(w[j]) : 0;
-      }
-    }
-    for (int round = 0; round < 8; ++round) {
-      const int shift = 28 - 4 * round;
-      // candidates of every next digit, among those that agree with the bound so far: 16 counts of 16 bits in 8 registers, at most 2^16 - 1 a thread and round of counting
-      u32 total[16];
-#pragma unroll
-      for (int d = 0; d < 16; ++d) total[d] = 0;
-      auto count = [&](u32 o, bool in) {
-        const bool match = in && (round == 0 || (o >> (shift + 4)) == (bound >> (shift + 4)));
-        const u32 digit = (o >> shift) & 15u;
-#pragma unroll
-        for (int d = 0; d < 16; ++d) total[d] += match && digit == (u32)d;
-      };
-      if (fits) {
-#pragma unroll
-        for (int i = 0; i < SEL_HELD; ++i)
-          if (lo + i * SEL_THREADS < hi) count(held[i], lo + i * SEL_THREADS + tid < hi);
-      } else {
-        for (int j = lo + tid; j < hi; j += SEL_THREADS) count(order_of(w[j]), true);
-      }
-#pragma unroll
-      for (int d = 0; d < 16; ++d) {
-        const u32 t = __reduce_add_sync(FULL, total[d]);
-        if (lane == d) s_count[round & 1][warp][d] = t;
+        for (int i = 0; i < SEL_HELD; ++i) {
+          const int j = segment + mine + i * 32;
+          const u32 o = order_of(held[i]);
+          if (j >= lo && j < hi && (round == 0 || o >> above == bound >> above)) atomicAdd(&s_bins[round][(o >> shift) & mask], 1u);
+        }
       }
       __syncthreads();
-      u32 mine = 0;                          // lane d: all candidates of digit d
-      if (lane < 16)
-        for (int x = 0; x < SEL_WARPS; ++x) mine += s_count[round & 1][x][lane];
-      // candidates above digit d
-      u32 above = lane < 16 ? mine : 0;
+      // thread t has the digits 2047 - 2t and 2046 - 2t: counts of those from the largest down to its first
+      const u32 c0 = s_bins[round][SEL_BINS - 1 - 2 * tid], c1 = s_bins[round][SEL_BINS - 2 - 2 * tid];
+      u32 x = c0 + c1;
 #pragma unroll
-      for (int o = 1; o < 16; o <<= 1) {
-        const u32 y = __shfl_down_sync(FULL, above, o);
-        if (lane + o < 16) above += y;
+      for (int o = 1; o < 32; o <<= 1) {
+        const u32 y = __shfl_up_sync(FULL, x, o);
+        if (lane >= o) x += y;
       }
-      const u32 before = above - mine;
-      const u32 hit = __ballot_sync(FULL, lane < 16 && before < (u32)want && above >= (u32)want);
-      const int d = hit ? __ffs(hit) - 1 : 0;
-      want -= (int)__shfl_sync(FULL, before, d);
-      bound |= (u32)d << shift;
+      if (lane == 31) s_scan[0][warp] = x;
+      __syncthreads();
+      const u32 others = lane < warp ? s_scan[0][lane] : 0;
+      const u32 before = __reduce_add_sync(FULL, others) + x - c0 - c1;
+      if (before < want && want <= before + c0 + c1) {        // exactly one thread
+        const bool second = before + c0 < want;
+        s_digit = (u32)(SEL_BINS - 1 - 2 * tid) - (second ? 1u : 0u);
+        s_want = want - before - (second ? c0 : 0u);
+      }
+      __syncthreads();
+      bound |= s_digit << shift;
+      want = s_want;
     }
   } else want = 0;
-  // ---- one pass in index order: kept tokens and their weights to the front.  Tokens behind the ones that are written are read before (a chunk is read whole, then written, and
-  // a token never moves back), so weights may be their own output.
+  // ---- one pass in index order: kept tokens and their weights to the front.  A segment is read whole before it is written, and a token never moves back, so weights may be their
+  // own output.
+  const bool inner_too = a.budget > a.first + a.recent;
   u32 done = 0, equal_done = 0;
-  for (int base = 0; base < len; base += SEL_THREADS) {
-    const int j = base + tid;
-    const float x = j < len ? w[j] : 0.0f;
-    const bool inner = j >= lo && j < hi;
-    const u32 o = order_of(x);
-    const bool equal = inner && o == bound && want > 0;
-    const u32 eq = __ballot_sync(FULL, equal);
-    const u32 sure = __ballot_sync(FULL, j < len && (!inner || (o > bound && a.budget > a.first + a.recent)));
+  for (int segment = 0; segment < len; segment += SEL_SEGMENT) {
+    if (!once) load(segment);
+    u32 sure[SEL_HELD], eq[SEL_HELD], sures = 0, eqs = 0;     // of 32 consecutive tokens each
+#pragma unroll
+    for (int i = 0; i < SEL_HELD; ++i) {
+      const int j = segment + mine + i * 32;
+      const u32 o = order_of(held[i]);
+      const bool inner = j >= lo && j < hi;
+      eq[i] = __ballot_sync(FULL, inner && o == bound && want > 0);
+      sure[i] = __ballot_sync(FULL, j < len && (!inner || (o > bound && inner_too)));
+      sures += __popc(sure[i]);
+      eqs += __popc(eq[i]);
+    }
     if (lane == 0) {
-      s_scan[0][warp] = __popc(eq);
-      s_scan[1][warp] = __popc(sure);
+      s_scan[0][warp] = sures;
+      s_scan[1][warp] = eqs;
     }
     __syncthreads();
     // equal ones are taken in index order while there is room: their rank says whether
-    u32 eq_before = equal_done, eq_all = 0, at = done, sure_all = 0;
-    for (int x2 = 0; x2 < SEL_WARPS; ++x2) {
-      const u32 e = s_scan[0][x2], s = s_scan[1][x2];
-      if (x2 < warp) { eq_before += e; at += s; }
-      eq_all += e;
-      sure_all += s;
+    const u32 all_sure = s_scan[0][lane], all_eq = s_scan[1][lane];
+    u32 rank = equal_done + __reduce_add_sync(FULL, lane < warp ? all_eq : 0u);
+    u32 at = done + __reduce_add_sync(FULL, lane < warp ? all_sure : 0u) + min(rank, want) - min(equal_done, want);
+    const u32 below = (1u << lane) - 1u;
+#pragma unroll
+    for (int i = 0; i < SEL_HELD; ++i) {
+      const u32 my_rank = rank + __popc(eq[i] & below);
+      const bool keep = ((sure[i] >> lane) & 1) || (((eq[i] >> lane) & 1) && my_rank < want);
+      const u32 to = at + __popc(sure[i] & below) + min(my_rank, want) - min(rank, want);
+      if (keep) {
+        kept[to] = segment + mine + i * 32;
+        out[to] = held[i];
+      }
+      const u32 after = rank + __popc(eq[i]);
+      at += __popc(sure[i]) + min(after, want) - min(rank, want);
+      rank = after;
     }
-    const u32 below = (1u << lane) - 1u, w_eq = (u32)want;
-    const u32 rank = eq_before + __popc(eq & below);
-    // taken equals before this thread: those of rank below `want`
-    const u32 taken_before = min(rank, w_eq) - min(equal_done, w_eq);
-    const bool keep = ((sure >> lane) & 1) || (equal && rank < w_eq);
-    at += __popc(sure & below) + taken_before;
-    if (keep) {
-      kept[at] = j;
-      out[at] = x;
-    }
-    done += sure_all + (min(equal_done + eq_all, w_eq) - min(equal_done, w_eq));
-    equal_done += eq_all;
-    __syncthreads();
+    const u32 eq_after = equal_done + __reduce_add_sync(FULL, all_eq);
+    done += __reduce_add_sync(FULL, all_sure) + min(eq_after, want) - min(equal_done, want);
+    equal_done = eq_after;
+    __syncthreads();                          // (everything of this segment has been read before the next one's counts, or the zeros, are written)
   }
   for (int i = n + tid; i < a.budget; i += SEL_THREADS) kept[i] = -1;
   for (int i = n + tid; i < a.width; i += SEL_THREADS) out[i] = 0.0f;
@@ -162,10 +170,10 @@ __global__ void __launch_bounds__(CP_THREADS) compact_kernel(CompactArgs a) {
   constexpr int TOKENS = CP_THREADS / PIECES, CHUNK = TOKENS * CP_EACH;
   const u32 B = a.cache.block_tokens;
   const bool is_v = blockIdx.z != 0;
-  const int r = blockIdx.y / a.cache.heads, h = blockIdx.y % a.cache.heads;
-  const int slice = blockIdx.x % a.slices, step = blockIdx.x / a.slices;
+  // heads of the same tokens side by side: they write neighbouring rows
+  const int r = blockIdx.y, x = blockIdx.x / a.slices, h = x % a.cache.heads, slice = blockIdx.x % a.slices, step = x / a.cache.heads;
   const int n = min(a.lengths[r], a.width);
-  const int* const kept = a.kept + (i64)blockIdx.y * a.width;
+  const int* const kept = a.kept + ((i64)r * a.cache.heads + h) * a.width;
   const int* const from = a.from + (i64)r * a.from_blocks;
   const int* const to = a.to + (i64)r * a.to_blocks;
   const int piece = threadIdx.x % PIECES, t = threadIdx.x / PIECES;
@@ -222,10 +230,9 @@ int launch_compact(CompactArgs a, int R, bool in_place, bool latent, cudaStream_
   constexpr int CHUNK = CP_THREADS / PIECES * CP_EACH;
   a.slices = PACKED ? 1 : D / 8 / PIECES;
   a.steps = in_place ? 1 : (a.width + CHUNK - 1) / CHUNK;
-  const u64 x = (u64)a.slices * a.steps, y = (u64)R * a.cache.heads;
-  if (x > 0x7FFFFFFFull || y > 0xFFFFull * 0x7FFFull) return PTSTORE_E_LIMIT;
-  // the grid's second axis has 16 bits: a launch takes as many requests as fit
-  const int most = (int)(65535 / a.cache.heads);
+  const u64 x = (u64)a.slices * a.steps * a.cache.heads;
+  if (x > 0x7FFFFFFFull) return PTSTORE_E_LIMIT;
+  constexpr int most = 65535;                // requests of a launch: the grid's second axis has 16 bits
   for (int r = 0; r < R; r += most) {
     CompactArgs b = a;
     const int m = R - r < most ? R - r : most;
@@ -233,7 +240,7 @@ int launch_compact(CompactArgs a, int R, bool in_place, bool latent, cudaStream_
     b.lengths += r;
     b.from += (i64)r * a.from_blocks;
     b.to += (i64)r * a.to_blocks;
-    compact_kernel<PACKED, D, PIECES><<<dim3((unsigned)x, (unsigned)(m * a.cache.heads), latent ? 1 : 2), CP_THREADS, 0, s>>>(b);
+    compact_kernel<PACKED, D, PIECES><<<dim3((unsigned)x, (unsigned)m, latent ? 1 : 2), CP_THREADS, 0, s>>>(b);
     if (cudaGetLastError() != cudaSuccess) return PTSTORE_E_CUDA;
   }
   return PTSTORE_OK;
@@ -271,10 +278,10 @@ extern "C" int ptstore_kv_compact(const ptstore_kv_cache_t* cache, const int32_t
   (void)cudaGetLastError();
   if (cache->format == PTSTORE_KV_PACKED)
     return cache->head_dim == 64 ? launch_compact<true, 64, 2>(a, R, in_place, latent, s) : launch_compact<true, 128, 4>(a, R, in_place, latent, s);
-  // slices of 128 bytes, whatever the 16 bits mean
+  // slices of 128 bytes, or whole rows of 256, whatever the 16 bits mean
   switch (cache->head_dim) {
     case 64: return launch_compact<false, 64, 8>(a, R, in_place, latent, s);
-    case 128: return launch_compact<false, 128, 8>(a, R, in_place, latent, s);
+    case 128: return launch_compact<false, 128, 16>(a, R, in_place, latent, s);
     case 320: return launch_compact<false, 320, 8>(a, R, in_place, latent, s);
     default: return launch_compact<false, 576, 8>(a, R, in_place, latent, s);
   }
