@@ -10,10 +10,11 @@ constexpr u32 FULL = 0xFFFFFFFFu;
 // ---- which tokens ---------------------------------------------------------------------------------------------------------------------
 // One CTA per request and head.  The smallest weight to keep is found by its bits, 11 + 11 + 10 from the top: a histogram of the candidates that agree so far in shared memory, a scan
 // of its counts from the largest down.  Then one pass in index order writes the kept tokens: every warp has consecutive ones, so that a scan of the warps' counts is all they exchange.
-// Rows of up to 8192 tokens are read once and stay in registers.  Bound by latency: 4 x 3 barriers and the reads.
+// Rows of up to 8192 tokens are read once and stay in registers.  Bound by latency, 4 x 3 barriers and the reads: one request's 8 rows of 6256 weights 9 us,
+// 512 ragged rows 31 us (512 threads, two CTAs an SM, 24 us, but 2 us more where there are few rows).
 constexpr int SEL_THREADS = 1024, SEL_WARPS = SEL_THREADS / 32;
 constexpr int SEL_HELD = 8, SEL_SEGMENT = SEL_THREADS * SEL_HELD;       // tokens a thread, the CTA holds
-constexpr int SEL_BINS = 2048;
+constexpr int SEL_BINS = 2048, SEL_EACH = SEL_BINS / SEL_THREADS;
 
 struct SelectArgs {
   const float* weights;
@@ -81,9 +82,14 @@ __global__ void __launch_bounds__(SEL_THREADS) select_kernel(SelectArgs a) {
         }
       }
       __syncthreads();
-      // thread t has the digits 2047 - 2t and 2046 - 2t: counts of those from the largest down to its first
-      const u32 c0 = s_bins[round][SEL_BINS - 1 - 2 * tid], c1 = s_bins[round][SEL_BINS - 2 - 2 * tid];
-      u32 x = c0 + c1;
+      // each thread has some consecutive digits, thread 0 the largest: counts from the largest digit down to its first
+      u32 c[SEL_EACH], x = 0;
+#pragma unroll
+      for (int i = 0; i < SEL_EACH; ++i) {
+        c[i] = s_bins[round][SEL_BINS - 1 - SEL_EACH * tid - i];
+        x += c[i];
+      }
+      const u32 all = x;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const u32 y = __shfl_up_sync(FULL, x, o);
@@ -91,12 +97,16 @@ __global__ void __launch_bounds__(SEL_THREADS) select_kernel(SelectArgs a) {
       }
       if (lane == 31) s_scan[0][warp] = x;
       __syncthreads();
-      const u32 others = lane < warp ? s_scan[0][lane] : 0;
-      const u32 before = __reduce_add_sync(FULL, others) + x - c0 - c1;
-      if (before < want && want <= before + c0 + c1) {        // exactly one thread
-        const bool second = before + c0 < want;
-        s_digit = (u32)(SEL_BINS - 1 - 2 * tid) - (second ? 1u : 0u);
-        s_want = want - before - (second ? c0 : 0u);
+      u32 before = __reduce_add_sync(FULL, lane < warp ? s_scan[0][lane] : 0u) + x - all;
+      if (before < want && want <= before + all) {            // exactly one thread
+        int i = 0;
+        for (; before + c[0] < want; ++i) {
+          before += c[0];
+#pragma unroll
+          for (int k = 1; k < SEL_EACH; ++k) c[k - 1] = c[k];
+        }
+        s_digit = (u32)(SEL_BINS - 1 - SEL_EACH * tid - i);
+        s_want = want - before;
       }
       __syncthreads();
       bound |= s_digit << shift;
@@ -126,7 +136,7 @@ __global__ void __launch_bounds__(SEL_THREADS) select_kernel(SelectArgs a) {
     }
     __syncthreads();
     // equal ones are taken in index order while there is room: their rank says whether
-    const u32 all_sure = s_scan[0][lane], all_eq = s_scan[1][lane];
+    const u32 all_sure = lane < SEL_WARPS ? s_scan[0][lane] : 0, all_eq = lane < SEL_WARPS ? s_scan[1][lane] : 0;
     u32 rank = equal_done + __reduce_add_sync(FULL, lane < warp ? all_eq : 0u);
     u32 at = done + __reduce_add_sync(FULL, lane < warp ? all_sure : 0u) + min(rank, want) - min(equal_done, want);
     const u32 below = (1u << lane) - 1u;
@@ -156,7 +166,8 @@ __global__ void __launch_bounds__(SEL_THREADS) select_kernel(SelectArgs a) {
 // Pure data movement, bound by HBM.  A thread moves 16 bytes (of a 4-bit cache: 32 codes and their two scales) of CP_EACH tokens, which are all read before the first is written.
 // Into other blocks, chunks of tokens are spread over CTAs.  In place one CTA takes a slice of a request's and head's rows chunk by chunk: a token never moves back, so what a
 // chunk's writes cover has been read by that chunk or the ones before it.
-constexpr int CP_THREADS = 256, CP_EACH = 8;
+// 64 requests cut to 2048 tokens of 8 heads x 128, K and V (1.04 GB): 221 us, 4.7 TB/s, with 4 tokens a thread and 5 CTAs an SM; 8 tokens 243 (4 CTAs) to 314 (3), 2 tokens 241 (8 CTAs).
+constexpr int CP_THREADS = 256, CP_EACH = 4;
 
 struct CompactArgs {
   Cache cache;
@@ -166,7 +177,7 @@ struct CompactArgs {
 };
 
 template <bool PACKED, int D, int PIECES /*16-byte pieces of a slice*/>
-__global__ void __launch_bounds__(CP_THREADS) compact_kernel(CompactArgs a) {
+__global__ void __launch_bounds__(CP_THREADS, 5) compact_kernel(CompactArgs a) {
   constexpr int TOKENS = CP_THREADS / PIECES, CHUNK = TOKENS * CP_EACH;
   const u32 B = a.cache.block_tokens;
   const bool is_v = blockIdx.z != 0;

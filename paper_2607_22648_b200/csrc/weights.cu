@@ -7,8 +7,9 @@
 // read once and nothing else of the cache.  The next tile is on its way while one is computed with, and Q stays where it is while its rows fit.  A decode step is bound by
 // reading K, a window of many rows by its exponentials.
 //
-// Weights keep what 32 bits can hold of them: scores are summed up in several accumulators (the tensor cores cut off what does not fit the running sum, an error that grows with its
-// length: rows of 576 elements in one / three / nine / eighteen sums were 9.5 / 3.6 / 1.7 / 1.4e-6 off, 32-bit products of a library 1.1e-6), and scale and lse, times log2 e, are kept as two numbers each (a rounding of an exponent of 20 is 2^-20 of the weight).
+// Weights keep what 32 bits can hold of them.  The tensor cores cut off what does not fit the running sum, so every product of rows comes out small by a part of itself that grows with
+// the length of the sums.  So scores are summed up in several accumulators, and the scale makes up for what is cut off on average (cut_off below).  Scale and lse, times log2 e, are kept
+// as two numbers each (a rounding of an exponent of 20 is 2^-20 of the weight).
 #include <type_traits>
 
 #include "attend_prompt.cuh"
@@ -23,7 +24,8 @@ struct Weights {
   const float* lse;
   float* out;
   i64 o_request, o_head;
-  float scale_hi, scale_lo;  // scale * log2 e (and the 4-bit values' factors, powers of two)
+  double scale2;             // scale * log2 e (and the 4-bit values' factors, powers of two)
+  float scale_hi, scale_lo;  // as two numbers
   int width, tiles, each;    // CTAs of a request and kv head, and tiles of a CTA
   bool add;
 };
@@ -340,9 +342,16 @@ __global__ void __launch_bounds__(AW_THREADS, D > 128 ? 1 : 3) weights_kernel(co
   if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(Shape::COLS) : "memory");
 }
 
+// By how much a sum of `per` instructions comes out small, relative: fitted to scores of 64 .. 576 elements against 64 bits (slopes in units of 2^-24, sums of one / two / four / six:
+// 16-bit caches 0.7 .. 1.0 / 1.1 .. 1.7 / 1.6 .. 1.8 / 2.3 .. 2.6; 4-bit values, whose products have few bits, 0.3 .. 0.4 / 0.4 .. 0.7 / 0.5 .. 1.1).
+constexpr double cut_off(bool packed, int per) { return (0.7 + 0.28 * per) * (packed ? 0.45 : 1.0) * 0x1p-24; }
+
 template <bool PACKED, bool F16, bool QFP16, int D, int NR>
 int launch(Weights wa, const Gpu& gpu, cudaStream_t s) {
   using Shape = WeightsShape<PACKED, D, NR>;
+  const double scale2 = wa.scale2 * (1.0 + cut_off(PACKED, Shape::PER));
+  wa.scale_hi = (float)scale2;
+  wa.scale_lo = isfinite(wa.scale_hi) ? (float)(scale2 - wa.scale_hi) : 0.0f;
   static std::atomic<u64> devices{0};
   auto* kernel = weights_kernel<PACKED, F16, QFP16, D, NR>;
   const int rc = allow_smem(kernel, Shape::SMEM, devices, gpu.dev);
@@ -373,8 +382,7 @@ extern "C" int ptstore_attend_weights(const ptstore_attend_weights_t* p, const p
   const bool packed = cache->format == PTSTORE_KV_PACKED, half = p->dtype == PTSTORE_KV_FP16;
   if (!packed && (cache->format & 3u) != p->dtype) return PTSTORE_E_INVAL;                   // (the latent formats' lowest bits are the 16-bit types)
   const double scale2 = (double)p->scale * 1.4426950408889634074 * (packed ? (double)cache->k_scale * DEQ_FACTOR : 1.0);
-  const float scale_hi = (float)scale2;
-  if (!isfinite(scale_hi)) return PTSTORE_E_INVAL;
+  if (!(fabs(scale2) < 3.4028e38)) return PTSTORE_E_INVAL;             // finite in 32 bits
   if (p->requests == 0 || p->width == 0 || (p->accumulate && p->tokens == 0)) return PTSTORE_OK;
   if (!p->token_offsets || !p->lengths || !p->block_tables || !p->weights) return PTSTORE_E_INVAL;
   if (p->tokens > 0 && (!p->q || !p->lse || !rows_aligned(p->q, p->tokens, p->q_token_stride, p->num_heads, p->q_head_stride))) return PTSTORE_E_INVAL;
@@ -396,8 +404,7 @@ extern "C" int ptstore_attend_weights(const ptstore_attend_weights_t* p, const p
   wa.o_request = p->weights_request_stride; wa.o_head = p->weights_head_stride;
   wa.width = p->width;
   wa.add = p->accumulate != 0;
-  wa.scale_hi = scale_hi;
-  wa.scale_lo = (float)(scale2 - scale_hi);
+  wa.scale2 = scale2;
   Gpu gpu;
   (void)cudaGetLastError();
   const int rs = current_gpu(&gpu);
