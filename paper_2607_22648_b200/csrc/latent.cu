@@ -89,7 +89,7 @@ int launch_latent(const Latent& la, const CUtensorMap& map, const Gpu& gpu, cuda
   const int grid = gpu.sms / Shape::PAIR * Shape::PAIR;
   kernel<<<grid, LA_THREADS, SMEM, s>>>(la, map);
   if (cudaGetLastError() != cudaSuccess) return PTSTORE_E_CUDA;
-  latent_join_kernel<L, F16, WIDE><<<dim3(grid, Shape::ROWS / 8), 256, 0, s>>>(la);
+  latent_join_kernel<L, F16, WIDE><<<dim3(grid, Shape::ROWS / 8, WIDE ? 1 : Shape::DIMS / 128), 256, 0, s>>>(la);
   return cudaGetLastError() == cudaSuccess ? PTSTORE_OK : PTSTORE_E_CUDA;
 }
 template <int L, bool F16>

@@ -27,7 +27,8 @@ constexpr int LA_THREADS = 256, LA_KEYS = 64, LA_ROPE = 64, LA_BOX = LA_KEYS * 1
 // octaves (standard deviation) were rescaled in every other step, 1400 clocks each.
 constexpr float LA_MOVE = 14.0f;
 constexpr int LA_AHEAD = 4;                  // units (of a pair of CTAs) that are brought into L2 before they are loaded
-constexpr int LA_MIN_UNITS = 2;              // a CTA takes at least this many, so that joining does not cost more than it saves
+constexpr int LA_MIN_UNITS = 4;              // a CTA takes at least this many, so that joining does not cost more than it saves (one request of 4160 tokens, 16 heads: 1 / 2 / 4 / 8 units
+                                             // 31.0 / 26.8 / 24.7 / 26.8 us)
 
 template <int L, bool WIDE>
 struct LatentShape {
@@ -642,40 +643,45 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
   }
 }
 
-// Joins the sums of the items that span several CTAs: blockIdx.x the CTA an item begins in, blockIdx.y eight of its rows, a warp a row.
+// Joins the sums of the items that span several CTAs: blockIdx.x the CTA an item begins in, y eight of its rows, a warp a row, z some of its
+// elements: 128 of a few rows, whose sums are many, all of many rows.
 template <int L, bool F16, bool WIDE>
 __global__ void __launch_bounds__(256) latent_join_kernel(const Latent la) {
   using Shape = LatentShape<L, WIDE>;
-  constexpr int NQ = Shape::ROWS, DIMS = Shape::DIMS, PAIR = Shape::PAIR, PF = Shape::PART, E = DIMS / 128;        // float4's of a lane
+  constexpr int NQ = Shape::ROWS, DIMS = Shape::DIMS, PAIR = Shape::PAIR, PF = Shape::PART, E = WIDE ? DIMS / 128 : 1;     // float4's of a lane
   const Attend& a = la.a;
   const LatentPart part = reinterpret_cast<const LatentPart*>(a.work)[blockIdx.x];
   if (part.parts == 0) return;
   const u32 cta = blockIdx.x / PAIR, half = blockIdx.x % PAIR;
-  const Req q = request(a, part.r);
-  const int lane = threadIdx.x & 31, row_base = (int)(part.rt * NQ), rows = min(NQ, q.fresh * a.group - row_base), row = blockIdx.y * 8 + (threadIdx.x >> 5);
-  if (row >= rows) return;
+  const int lane = threadIdx.x & 31, row = blockIdx.y * 8 + (threadIdx.x >> 5);
   const float* const sums = reinterpret_cast<const float*>(a.work + LA_PARTS_AT) + (i64)half * PF;
   auto at = [&](int p) { return sums + (i64)(2 * (cta + p) + (p == 0 ? 1 : 0)) * PAIR * PF; };
-  // lane p holds m and l of part p (of 32 at a time)
-  float top = -INFINITY, sum = 0.0f;
-  for (int p = lane; p < part.parts; p += 32) top = fmaxf(top, at(p)[NQ * DIMS + row]);
+  // lane p holds m and l of part p (of 32 at a time); the first 32 are on their way while the request is looked up
+  const bool one = lane < part.parts;
+  const float m0 = one ? at(lane)[NQ * DIMS + row] : -INFINITY, l0 = one ? at(lane)[NQ * DIMS + NQ + row] : 0.0f;
+  const Req q = request(a, part.r);
+  const int row_base = (int)(part.rt * NQ), rows = min(NQ, q.fresh * a.group - row_base);
+  if (row >= rows) return;
+  float top = m0, sum = 0.0f;
+  for (int p = lane + 32; p < part.parts; p += 32) top = fmaxf(top, at(p)[NQ * DIMS + row]);
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
+  const int mine = (int)blockIdx.z * 128 + lane * 4;
   float4 acc[E] = {};
   for (int p0 = 0; p0 < part.parts; p0 += 32) {
     float f = 0.0f;
     if (p0 + lane < part.parts) {
-      const float m = at(p0 + lane)[NQ * DIMS + row];
+      const float m = p0 == 0 ? m0 : at(p0 + lane)[NQ * DIMS + row];
       f = m == -INFINITY ? 1.0f : exp2_fast(m - top);                        // nothing seen: sums of zero (or NaN)
-      sum += at(p0 + lane)[NQ * DIMS + NQ + row] * f;
+      sum += (p0 == 0 ? l0 : at(p0 + lane)[NQ * DIMS + NQ + row]) * f;
     }
     const int n = min(32, part.parts - p0);
-#pragma unroll 4
+#pragma unroll 8
     for (int p = 0; p < n; ++p) {
       const float w = __shfl_sync(FULL, f, p);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const float4 v = *reinterpret_cast<const float4*>(at(p0 + p) + row * DIMS + e * 128 + lane * 4);
+        const float4 v = *reinterpret_cast<const float4*>(at(p0 + p) + row * DIMS + e * 128 + mine);
         acc[e].x += v.x * w;
         acc[e].y += v.y * w;
         acc[e].z += v.z * w;
@@ -689,9 +695,9 @@ __global__ void __launch_bounds__(256) latent_join_kernel(const Latent la) {
   const float f = row_factor(a, part.r, (i64)q.pos0 + fr, sum);
 #pragma unroll
   for (int e = 0; e < E; ++e)
-    *reinterpret_cast<uint2*>(a.out + 2 * ((i64)(q.row0 + fr) * a.o_token + (i64)hq * a.o_head + (int)half * DIMS + e * 128 + lane * 4)) =
+    *reinterpret_cast<uint2*>(a.out + 2 * ((i64)(q.row0 + fr) * a.o_token + (i64)hq * a.o_head + (int)half * DIMS + e * 128 + mine)) =
         make_uint2(pack2<F16>(acc[e].x * f, acc[e].y * f), pack2<F16>(acc[e].z * f, acc[e].w * f));
-  if (a.lse && half == 0 && lane == 0) a.lse[(i64)(q.row0 + fr) * a.heads + hq] = lse_of(top, sum);
+  if (a.lse && half == 0 && blockIdx.z == 0 && lane == 0) a.lse[(i64)(q.row0 + fr) * a.heads + hq] = lse_of(top, sum);
 }
 
 }  // namespace ptk
