@@ -26,7 +26,7 @@ constexpr int LA_THREADS = 256, LA_KEYS = 64, LA_ROPE = 64, LA_BOX = LA_KEYS * 1
 // A reference moves when a scaled score exceeds it by more than this.  Weights are then at most 2^14 (fp16 holds 2^15): with 8, the tiles of 128 rows whose scores spread over 5
 // octaves (standard deviation) were rescaled in every other step, 1400 clocks each.
 constexpr float LA_MOVE = 14.0f;
-constexpr int LA_AHEAD = 4;                  // units (of a pair of CTAs) that are brought into L2 before they are loaded
+constexpr int LA_AHEAD = 2;                  // units (of a pair of CTAs) that are brought into L2 before they are loaded
 constexpr int LA_MIN_UNITS = 4;              // a CTA takes at least this many, so that joining does not cost more than it saves (one request of 4160 tokens, 16 heads: 1 / 2 / 4 / 8 units
                                              // 31.0 / 26.8 / 24.7 / 26.8 us)
 
@@ -114,8 +114,8 @@ __device__ __forceinline__ void tensor_load_box(u32 dst, const CUtensorMap* map,
   asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(element), "r"(token),
                "r"(block), "r"(smem_addr(bar)) : "memory");
 }
-__device__ __forceinline__ void tensor_prefetch_box(const CUtensorMap* map, int element, int token, int block) {      // into L2
-  asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(element), "r"(token), "r"(block) : "memory");
+__device__ __forceinline__ void bulk_prefetch(const void* src, u32 bytes) {      // into L2
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ bool any_of_softmax(bool v) {      // barrier of the 128 softmax threads
   u32 r;
@@ -296,7 +296,8 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
         const int key = unit * LA_KEYS + (int)(mine_at * bt);
         return key < line.keys ? table[(u32)key / B] : -1;
       };
-      int id = look_up(line.ua), far_id = WIDE && !values && line.ua + LA_AHEAD < line.ub ? look_up(line.ua + LA_AHEAD) : -1;
+      const bool alone = WIDE && line.q.fresh * a.group <= NQ;               // the request's only row tile
+      int id = look_up(line.ua), far_id = alone && !values && line.ua + LA_AHEAD < line.ub ? look_up(line.ua + LA_AHEAD) : -1;
       for (int unit = line.ua; unit < line.ub && !quit; ++unit, ++g) {
         const int key = unit * LA_KEYS + (int)(mine_at * bt);
         const bool in = key < line.keys, have = in && (u32)id < a.cache.num_blocks;
@@ -320,11 +321,12 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
               tensor_load_box(smem_v + (st * VALUES + i) * LA_BOX + mine_at * bt * 128, &map, element_of((int)i), token, block, &s.v_full[st]);
         } else {
           if (WIDE) {
-            // Few boxes are on their way at a time, so each CTA of a pair has its half of a later unit's brought nearer
+            // Few boxes are on their way at a time, so later units' rows, which lie together in a block, are brought nearer, by the CTAs of a pair in turn: 64 requests of one row tile
+            // each 170 us, without 177.  Not where a request has several row tiles, whose pairs bring them for one another (16 requests of 8: 252 us, without 240).
             const int far = unit + LA_AHEAD, fkey = far * LA_KEYS + (int)(mine_at * bt);
-            if (far < line.ub && (u32)far_id < a.cache.num_blocks)
-              for (u32 i = team; i < VALUES + (half == 0); i += teams) tensor_prefetch_box(&map, i < VALUES ? element_of((int)i) : L, (int)((u32)fkey % B), far_id);
-            far_id = far + 1 < line.ub ? look_up(far + 1) : -1;
+            if (alone && far < line.ub && team == 0 && (u32)(far & 1) == half && (u32)far_id < a.cache.num_blocks)
+              bulk_prefetch(a.cache.base + (u64)(u32)far_id * a.cache.block_stride + (u64)((u32)fkey % B) * ((L + 64) * 2), bt * (L + 64) * 2);
+            far_id = alone && far + 1 < line.ub ? look_up(far + 1) : -1;
           }
           for (u32 i = 0; i < OTHERS; ++i, ++op) {
             const u32 st = op % SLOTS;
