@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
         return key < line.keys ? table[(u32)key / B] : -1;
       };
       const bool alone = WIDE && line.q.fresh * a.group <= NQ;               // the request's only row tile
-      int id = look_up(line.ua), far_id = alone && !values && line.ua + LA_AHEAD < line.ub ? look_up(line.ua + LA_AHEAD) : -1;
+      int id = look_up(line.ua), far_id = alone && values && line.ua + LA_AHEAD < line.ub ? look_up(line.ua + LA_AHEAD) : -1;
       for (int unit = line.ua; unit < line.ub && !quit; ++unit, ++g) {
         const int key = unit * LA_KEYS + (int)(mine_at * bt);
         const bool in = key < line.keys, have = in && (u32)id < a.cache.num_blocks;
@@ -306,6 +306,14 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
         if (unit + 1 < line.ub) id = look_up(unit + 1);
         const u32 there = __ballot_sync(FULL, have && team == 0), bytes = __popc(there) * bt * 128;
         if (values) {
+          if (WIDE) {
+            // Few boxes are on their way at a time, so later units' rows, which lie together in a block, are brought nearer, by the CTAs of a pair in turn: 64 requests of one row tile
+            // each 170 us, without 177.  Not where a request has several row tiles, whose pairs bring them for one another (16 requests of 8: 252 us, without 240).
+            const int far = unit + LA_AHEAD, fkey = far * LA_KEYS + (int)(mine_at * bt);
+            if (alone && far < line.ub && team == 0 && (u32)(far & 1) == half && (u32)far_id < a.cache.num_blocks)
+              bulk_prefetch(a.cache.base + (u64)(u32)far_id * a.cache.block_stride + (u64)((u32)fkey % B) * ((L + 64) * 2), bt * (L + 64) * 2);
+            far_id = alone && far + 1 < line.ub ? look_up(far + 1) : -1;
+          }
           const u32 st = g % STAGES;
           if (g >= STAGES && !__all_sync(FULL, bar_wait(&s.v_empty[st], (g / STAGES - 1) & 1, a.polls, &s.gave_up))) { quit = true; break; }
           // groups of 8 tokens that are there
@@ -320,14 +328,6 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
             for (u32 i = team; i < VALUES; i += teams)
               tensor_load_box(smem_v + (st * VALUES + i) * LA_BOX + mine_at * bt * 128, &map, element_of((int)i), token, block, &s.v_full[st]);
         } else {
-          if (WIDE) {
-            // Few boxes are on their way at a time, so later units' rows, which lie together in a block, are brought nearer, by the CTAs of a pair in turn: 64 requests of one row tile
-            // each 170 us, without 177.  Not where a request has several row tiles, whose pairs bring them for one another (16 requests of 8: 252 us, without 240).
-            const int far = unit + LA_AHEAD, fkey = far * LA_KEYS + (int)(mine_at * bt);
-            if (alone && far < line.ub && team == 0 && (u32)(far & 1) == half && (u32)far_id < a.cache.num_blocks)
-              bulk_prefetch(a.cache.base + (u64)(u32)far_id * a.cache.block_stride + (u64)((u32)fkey % B) * ((L + 64) * 2), bt * (L + 64) * 2);
-            far_id = alone && far + 1 < line.ub ? look_up(far + 1) : -1;
-          }
           for (u32 i = 0; i < OTHERS; ++i, ++op) {
             const u32 st = op % SLOTS;
             if (op >= SLOTS && !__all_sync(FULL, bar_wait(&s.k_empty[st], (op / SLOTS - 1) & 1, a.polls, &s.gave_up))) { quit = true; break; }
