@@ -64,6 +64,12 @@ __device__ __forceinline__ void bar_drain(u64* bar, u32 parity) {
   for (u32 i = 0; i < POLLS && !bar_try(bar, parity); ++i) {}
 }
 
+// A warp's arrival, by one lane behind what the others have done: arrivals at one barrier are taken one by one, some 6 clocks each, and hold up whatever else goes through shared memory
+__device__ __forceinline__ void warp_arrive(u64* bar) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) bar_arrive(bar);
+}
+
 // barrier of the 128 loading threads, and whether the value was set in any of them
 __device__ __forceinline__ bool any_of_128(int v) {
   u32 r;

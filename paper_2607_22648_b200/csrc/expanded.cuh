@@ -84,8 +84,8 @@ __global__ void __launch_bounds__(PR_THREADS, 1) expanded_kernel(const Expanded 
     }
     if (lane == 31) s_scan[warp] = x;
     if (tid == 0) {
-      for (int i = 0; i < 2; ++i) { bar_init(&b_q[i], 1); bar_init(&b_s[i], 1); bar_init(&b_pa[i], 128); bar_init(&b_pb[i], 128); bar_init(&b_o[i], 1); }
-      for (int i = 0; i < EX_SLOTS; ++i) { bar_init(&b_full[i], 128); bar_init(&b_empty[i], 1); }
+      for (int i = 0; i < 2; ++i) { bar_init(&b_q[i], 1); bar_init(&b_s[i], 1); bar_init(&b_pa[i], 4); bar_init(&b_pb[i], 4); bar_init(&b_o[i], 1); }
+      for (int i = 0; i < EX_SLOTS; ++i) { bar_init(&b_full[i], 1); bar_init(&b_empty[i], 1); }
       bar_init(&b_end, 1);
       bar_init(&b_raw, 1);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -203,76 +203,75 @@ __global__ void __launch_bounds__(PR_THREADS, 1) expanded_kernel(const Expanded 
     }
     __syncwarp();
   } else if (warp >= 8) {
-    // ======== K and V into the ring.  Thread 0 issues; in the last steps all 128 look at V before it counts as there.
+    // ======== K and V into the ring.  Thread 0 loads; in the last steps all 128 look at V before it counts as there.
     regs_fewer<72>();
     const int pt = tid - 256;
     const volatile int* const gave_up = &s_gave_up;
-    auto wait_empty = [&](int op) { return op < EX_SLOTS || bar_wait(&b_empty[op % EX_SLOTS], ((op / EX_SLOTS) - 1) & 1, a.polls, &s_gave_up); };
-    int j = 0;
     u32 raws = 0;
-    for (; j < n_steps; ++j) {
-      if (any_of_128(*gave_up)) break;        // the same in all 128 threads
+    int issued = 0;
+    bool quit = false;                        // a wait ran out: nothing is loaded from there on.  Thread 0 goes on to where the others wait for it.
+    for (int j = 0; j < n_steps; ++j) {
       const int k0 = j * PR_KEYS;
       const bool edge = k0 + PR_KEYS > all_see;
+      if (!edge && pt != 0) continue;
 #pragma unroll 1
       for (int i = 0; i < EX_STEP; ++i) {
         const int op = EX_STEP * j + i;
-        const bool free = wait_empty(op);
-        // A slot that is not free gets no copy.  This thread arrives all the same, so that the slot's phase ends, but not before the phase of what lies there has ended.
-        if (!free) bar_drain(&b_full[op % EX_SLOTS], ((op / EX_SLOTS) - 1) & 1);
         const u32 dst = smem_kv + (op % EX_SLOTS) * EX_SLOT;
         u64* const full = &b_full[op % EX_SLOTS];
         const bool look = edge && i >= 3;
-        if (pt == 0 && free) {
-          u64* const bar = look ? &b_raw : full;
-          bar_expect(bar, EX_SLOT);
-          if (i < 2) tensor_load_3d(dst, &k_map, 64 * i, (int)(a.k_head * (u32)h), rq.key0 + k0, bar);
-          else if (i == 2) tensor_load_2d(dst, &r_map, 0, rq.key0 + k0, bar);
-          else
+        if (pt == 0 && !quit) {
+          if (*gave_up || (op >= EX_SLOTS && !bar_wait(&b_empty[op % EX_SLOTS], ((op / EX_SLOTS) - 1) & 1, a.polls, &s_gave_up))) quit = true;
+          else {
+            u64* const bar = look ? &b_raw : full;
+            bar_expect(bar, EX_SLOT);
+            if (i < 2) tensor_load_3d(dst, &k_map, 64 * i, (int)(a.k_head * (u32)h), rq.key0 + k0, bar);
+            else if (i == 2) tensor_load_2d(dst, &r_map, 0, rq.key0 + k0, bar);
+            else
 #pragma unroll
-            for (int e = 0; e < 2; ++e) tensor_load_3d(dst + e * (EX_SLOT / 2), &v_map, 64 * e, (int)(a.v_head * (u32)h), rq.key0 + k0 + 64 * (i - 3), bar);
-          if (!look) continue;                // (its expectation was its arrival)
+              for (int e = 0; e < 2; ++e) tensor_load_3d(dst + e * (EX_SLOT / 2), &v_map, 64 * e, (int)(a.v_head * (u32)h), rq.key0 + k0 + 64 * (i - 3), bar);
+            issued = op + 1;
+          }
         }
-        if (look) {
-          // thread 0's slot is free for all: they wait for the same barriers in the same order
-          const bool all_free = !any_of_128(!free);
-          if (all_free) {
-            if (!bar_wait(&b_raw, raws & 1, a.polls, &s_gave_up)) bar_drain(&b_raw, raws & 1);
-            // keys that no row of the CTA sees become zero; what is not finite in keys that only some rows see is taken out, and put into the rows that see it at the end
-            constexpr u32 EX = F16 ? 0x7C00u : 0x7F80u, MANT = F16 ? 0x03FFu : 0x007Fu;
-            unsigned char* const t = smem + 2 * EX_Q + (op % EX_SLOTS) * EX_SLOT;
-            for (int x = pt; x < 64 * 16; x += 128) {
-              const int n = x >> 4, c = x & 15, key = k0 + 64 * (i - 3) + n;
-              if (key < all_see) continue;
-              uint4* const p = reinterpret_cast<uint4*>(t + (c >> 3) * (EX_SLOT / 2) + n * 128 + (((c & 7) ^ (n & 7)) * 16));
-              if (key >= keys) { *p = make_uint4(0, 0, 0, 0); continue; }
-              const uint4 v = *p;
-              u32 e[4] = {v.x, v.y, v.z, v.w};
-              bool odd = false;
+        if (!look) continue;
+        if (any_of_128(quit)) { quit = true; break; }         // the same in all 128 threads
+        if (!bar_wait(&b_raw, raws & 1, a.polls, &s_gave_up)) bar_drain(&b_raw, raws & 1);
+        ++raws;
+        // keys that no row of the CTA sees become zero; what is not finite in keys that only some rows see is taken out, and put into the rows that see it at the end
+        constexpr u32 EX = F16 ? 0x7C00u : 0x7F80u, MANT = F16 ? 0x03FFu : 0x007Fu;
+        unsigned char* const t = smem + 2 * EX_Q + (op % EX_SLOTS) * EX_SLOT;
+        for (int x = pt; x < 64 * 16; x += 128) {
+          const int n = x >> 4, c = x & 15, key = k0 + 64 * (i - 3) + n;
+          if (key < all_see) continue;
+          uint4* const p = reinterpret_cast<uint4*>(t + (c >> 3) * (EX_SLOT / 2) + n * 128 + (((c & 7) ^ (n & 7)) * 16));
+          if (key >= keys) { *p = make_uint4(0, 0, 0, 0); continue; }
+          const uint4 v = *p;
+          u32 e[4] = {v.x, v.y, v.z, v.w};
+          bool odd = false;
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const u32 sh = 16 * (k & 1), y = e[k >> 1] >> sh;
-                if ((y & EX) == EX) {
-                  atomicMin(&s_bad[(y & MANT) ? 0 : (y & 0x8000u) ? 2 : 1][c * 8 + k], key);
-                  e[k >> 1] &= ~(0xFFFFu << sh);
-                  odd = true;
-                }
-              }
-              if (odd) {
-                *p = make_uint4(e[0], e[1], e[2], e[3]);
-                s_any_bad = 1;
-              }
+          for (int k = 0; k < 8; ++k) {
+            const u32 sh = 16 * (k & 1), y = e[k >> 1] >> sh;
+            if ((y & EX) == EX) {
+              atomicMin(&s_bad[(y & MANT) ? 0 : (y & 0x8000u) ? 2 : 1][c * 8 + k], key);
+              e[k >> 1] &= ~(0xFFFFu << sh);
+              odd = true;
             }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          } else if (pt == 0 && free) bar_drain(&b_raw, raws & 1);
-          if (all_free) ++raws;
-          else if (any_of_128(pt == 0 && free)) ++raws;
+          }
+          if (odd) {
+            *p = make_uint4(e[0], e[1], e[2], e[3]);
+            s_any_bad = 1;
+          }
         }
-        bar_arrive(full);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        any_of_128(0);
+        if (pt == 0) bar_arrive(full);
       }
+      if (quit && edge) break;
     }
     // whatever happened, what is in flight lands before the CTA gives its memory back
-    for (int op = max(0, EX_STEP * j - EX_SLOTS); op < EX_STEP * j; ++op) bar_drain(&b_full[op % EX_SLOTS], (op / EX_SLOTS) & 1);
+    if (pt == 0)
+      for (int op = max(0, issued - EX_SLOTS); op < issued; ++op) bar_drain(&b_full[op % EX_SLOTS], (op / EX_SLOTS) & 1);
+    __syncwarp();
   } else {
     // ======== softmax of tile w
     regs_more<200>();
@@ -401,7 +400,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1) expanded_kernel(const Expanded 
           if (c & 1) {
             tc_wait_st();
             tc_fence_before();
-            bar_arrive(c == 1 ? &b_pa[w] : &b_pb[w]);
+            warp_arrive(c == 1 ? &b_pa[w] : &b_pb[w]);
           }
         }
         continue;
@@ -409,13 +408,13 @@ __global__ void __launch_bounds__(PR_THREADS, 1) expanded_kernel(const Expanded 
       tc_st32(ts, p);
       tc_wait_st();
       tc_fence_before();
-      bar_arrive(&b_pa[w]);                   // the tensor cores start on these while the second half is computed
+      warp_arrive(&b_pa[w]);                  // the tensor cores start on these while the second half is computed
       weights(1, false, p);
       tc_st32(ts + 32, p);
       l += sum0 + sum1;
       tc_wait_st();
       tc_fence_before();
-      bar_arrive(&b_pb[w]);
+      warp_arrive(&b_pb[w]);
     }
     // ---- output
     if (steps[w] > 0) {

@@ -142,11 +142,11 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
     part->parts = 0;
     for (int i = 0; i < STAGES; ++i) { bar_init(&s.v_full[i], 1); bar_init(&s.v_empty[i], 1); }
     for (int i = 0; i < SLOTS; ++i) { bar_init(&s.k_full[i], 1); bar_init(&s.k_empty[i], 1); }
-    bar_init(&s.q, 128);
+    bar_init(&s.q, 4);
     bar_init(&s.q_free, 1);
     bar_init(&s.s, 1);
-    bar_init(&s.s_free, 128);
-    bar_init(&s.p, 128);
+    bar_init(&s.s_free, 4);
+    bar_init(&s.p, 4);
     bar_init(&s.pv, 1);
     bar_init(&s.end[0], 1);
     bar_init(&s.end[1], 1);
@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       }
       tc_fence_before();
-      bar_arrive(&s.q);
+      warp_arrive(&s.q);
     };
     bool more = line.next();
     if (more) load_q(line);
@@ -435,7 +435,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
           tc_loaded(v[1]);
           tc_fence_before();
         }
-        bar_arrive(&s.s_free);
+        warp_arrive(&s.s_free);
         const u32 valid = s.valid[st];
         const bool edge = k0 + LA_KEYS > all_see || valid != 0xFFu;
         if (edge) {
@@ -548,7 +548,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         tc_fence_before();
-        bar_arrive(&s.p);
+        warp_arrive(&s.p);
       }
       if (quit) break;
       // ---- the next item's Q while the last products run
