@@ -78,23 +78,39 @@ u32 make_rows_map(const Cache& c, bool half, int dim, CUtensorMap* map) {
   return encode(map, half, 3, c.base, dims, strides, boxes) ? box : 0;
 }
 
-template <int L, bool F16, bool WIDE>
+template <int L, bool F16, bool WIDE, bool ALIAS = false>
 int launch_latent(const Latent& la, const CUtensorMap& map, const Gpu& gpu, cudaStream_t s) {
   using Shape = LatentShape<L, WIDE>;
   static std::atomic<u64> devices{0};
-  auto* kernel = latent_attend_kernel<L, F16, WIDE>;
+  auto* kernel = latent_attend_kernel<L, F16, WIDE, ALIAS>;
   constexpr int SMEM = latent_smem<L, WIDE>();
   const int rc = allow_smem(kernel, SMEM, devices, gpu.dev);
   if (rc) return rc;
   const int grid = gpu.sms / Shape::PAIR * Shape::PAIR;
-  kernel<<<grid, LA_THREADS, SMEM, s>>>(la, map);
+  if (WIDE && ALIAS) {
+    cudaLaunchAttribute pair;
+    pair.id = cudaLaunchAttributeClusterDimension;
+    pair.val.clusterDim.x = Shape::PAIR;
+    pair.val.clusterDim.y = pair.val.clusterDim.z = 1;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = grid;
+    config.blockDim = LA_THREADS;
+    config.dynamicSmemBytes = SMEM;
+    config.stream = s;
+    config.attrs = &pair;
+    config.numAttrs = 1;
+    (void)cudaLaunchKernelEx(&config, kernel, la, map);
+  } else {
+    kernel<<<grid, LA_THREADS, SMEM, s>>>(la, map);
+  }
   if (cudaGetLastError() != cudaSuccess) return PTSTORE_E_CUDA;
   latent_join_kernel<L, F16, WIDE><<<dim3(grid, Shape::ROWS / 8, WIDE ? 1 : Shape::DIMS / 128), 256, 0, s>>>(la);
   return cudaGetLastError() == cudaSuccess ? PTSTORE_OK : PTSTORE_E_CUDA;
 }
 template <int L, bool F16>
 int launch_latent_rows(const Latent& la, const CUtensorMap& map, i64 rows, const Gpu& gpu, cudaStream_t s) {
-  return rows > LatentShape<L, false>::ROWS && gpu.sms >= 2 ? launch_latent<L, F16, true>(la, map, gpu, s) : launch_latent<L, F16, false>(la, map, gpu, s);
+  if (rows <= LatentShape<L, false>::ROWS || gpu.sms < 2) return launch_latent<L, F16, false>(la, map, gpu, s);
+  return la.a.out == la.a.q ? launch_latent<L, F16, true, true>(la, map, gpu, s) : launch_latent<L, F16, true>(la, map, gpu, s);
 }
 
 }  // namespace

@@ -47,7 +47,7 @@ template <int L, bool WIDE>
 struct LatentMisc {
   using Shape = LatentShape<L, WIDE>;
   u64 v_full[Shape::STAGES], v_empty[Shape::STAGES], k_full[Shape::SLOTS], k_empty[Shape::SLOTS], q, q_free, s, s_free, p, pv, end[2], left, scan[LA_THREADS / 32];
-  u32 valid[Shape::STAGES], tmem;
+  u32 valid[Shape::STAGES], tmem, loaded[4];         // loaded: items whose q each warp of the other CTA has read
   int gave_up, any_bad, r;
   alignas(16) float f[Shape::ROWS];
   alignas(16) u32 moved[4];  // of each warp's rows: 1 a reference has moved, 2 a wait ran out
@@ -117,13 +117,26 @@ __device__ __forceinline__ void tensor_load_box(u32 dst, const CUtensorMap* map,
 __device__ __forceinline__ void bulk_prefetch(const void* src, u32 bytes) {      // into L2
   asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
 }
+// the other CTA of a pair: a word in its shared memory, written behind what this thread has done, and read before what it does
+__device__ __forceinline__ void tell_other(const u32* word, u32 rank, u32 value) {
+  u32 at;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr(word)), "r"(rank));
+  asm volatile("st.release.cluster.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(value) : "memory");
+}
+__device__ __forceinline__ u32 told(const u32* word) {
+  u32 v;
+  asm volatile("ld.acquire.cluster.shared::cta.u32 %0, [%1];" : "=r"(v) : "r"(smem_addr(word)) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ bool any_of_softmax(bool v) {      // barrier of the 128 softmax threads
   u32 r;
   asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 2, 128, p;\n selp.u32 %0, 1, 0, q;\n}" : "=r"(r) : "r"((u32)v) : "memory");
   return r != 0;
 }
 
-template <int L, bool F16, bool WIDE>
+// ALIAS: the output is q itself.  The two CTAs of a pair are then a cluster and tell each other whose q they have read (which costs calls of many rows 5 %).
+template <int L, bool F16, bool WIDE, bool ALIAS>
 __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Latent la, const __grid_constant__ CUtensorMap map) {
   using Shape = LatentShape<L, WIDE>;
   constexpr int NQ = Shape::ROWS, STAGES = Shape::STAGES, SLOTS = Shape::SLOTS, BOXES = Shape::BOXES, VALUES = Shape::VALUES, OTHERS = Shape::OTHERS, MT = Shape::MT,
@@ -152,6 +165,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
     bar_init(&s.end[1], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     s.gave_up = s.any_bad = 0;
+    for (int i = 0; i < 4; ++i) s.loaded[i] = 0;
     s.r = -1;
   }
   if (tid == 160) asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
@@ -196,6 +210,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
+  if (WIDE && ALIAS) cluster_sync();                   // (the other CTA writes here once this one has begun)
   __syncthreads();
   tc_fence_after();
   const u32 tmem = s.tmem;
@@ -351,7 +366,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
     // ======== softmax: thread t has row t; Q before, the output behind an item
     const int row = tid;
     const u32 lane_base = (u32)(32 * warp) << 16, ts = tmem + lane_base + Shape::S_AT, to = tmem + lane_base;
-    u32 g = 0, item = 0;
+    u32 g = 0, item = 0, loads = 0;
     bool quit = false;
     auto wait = [&](u64* b, u32 parity) {
       if (__any_sync(FULL, !bar_wait(b, parity, a.polls, &s.gave_up))) quit = true;
@@ -403,6 +418,8 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
       }
       tc_fence_before();
       warp_arrive(&s.q);
+      ++loads;
+      if (WIDE && ALIAS && lane == 0) tell_other(&s.loaded[warp], 1 - half, loads);
     };
     bool more = line.next();
     if (more) load_q(line);
@@ -559,6 +576,16 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
       ++item;
       // ---- output
       wait(&s.pv, (g - 1) & 1);
+      if (WIDE && ALIAS) {                    // the other CTA has read all of the item's q
+        bool ok = lane >= 4;
+        for (u32 i = 0; !ok && i < a.polls; ++i) {
+          ok = (int)(told(&s.loaded[lane]) - item) >= 0;
+          if ((i & 1023) == 1023 && *reinterpret_cast<volatile int*>(&s.gave_up)) break;
+        }
+        if (!ok) s.gave_up = 1;
+        if (!__all_sync(FULL, ok)) quit = true;
+        __syncwarp();
+      }
       if (any_of_softmax(quit)) break;
       tc_fence_after();
       const bool whole = first == last;
@@ -639,6 +666,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
   }
   tc_fence_before();
   __syncthreads();
+  if (WIDE && ALIAS) cluster_sync();                   // (and does not any more when this one leaves)
   if (warp == 5) {
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
     if (lane == 0 && s.gave_up && a.status) atomicOr(a.status, PTSTORE_S_TIMEOUT);

@@ -310,6 +310,21 @@ def test_q_may_be_the_output(G, dtype, new, n):
 
 
 @pytest.mark.parametrize("dtype", BOTH)
+def test_q_of_many_short_requests_may_be_the_output(G, dtype):
+    """Two CTAs share 128 rows and go through several requests each, not in step: neither may overwrite what the other has still to read."""
+    lens = [64 + 37 * i % 200 for i in range(700)]
+    b = make(G, 512, dtype, 128, 16, lens, [1] * 700, seed=13)
+    call(G, b)
+    want = b["out"].clone()
+    first = b["ql"].clone()
+    for _ in range(5):
+        again = first.clone()
+        b["ql"] = again
+        call(G, b, out=again)
+        assert torch.equal(again[:700], want[:700])
+
+
+@pytest.mark.parametrize("dtype", BOTH)
 def test_calls_of_all_shapes_share_a_workspace(G, dtype):
     """What a call leaves in the workspace does not reach the next one."""
     shapes = [([9000], [1], 16), ([100], [1], 16), ([3000, 2000], [40, 1], 16), ([5000, 64], [1, 1], 128), ([1], [1], 1)]
