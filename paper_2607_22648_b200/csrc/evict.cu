@@ -1,20 +1,18 @@
 // ptstore_select_tokens, ptstore_kv_compact: which tokens of a cache to keep by the attention they were given, and moving them together.
 #include "kvcache.cuh"
+#include "launch.cuh"
 
 using namespace ptk;
 
 namespace {
 
-constexpr u32 FULL = 0xFFFFFFFFu;
-
 // ---- which tokens ---------------------------------------------------------------------------------------------------------------------
 // One CTA per request and head.  The smallest weight to keep is found by its bits, 11 + 11 + 10 from the top: a histogram of the candidates that agree so far in shared memory, a scan
 // of its counts from the largest down.  Then one pass in index order writes the kept tokens: every warp has consecutive ones, so that a scan of the warps' counts is all they exchange.
-// Rows of up to 8192 tokens are read once and stay in registers.  Bound by latency, 4 x 3 barriers and the reads: one request's 8 rows of 6256 weights 9 us,
-// 512 ragged rows 31 us (512 threads, two CTAs an SM, 24 us, but 2 us more where there are few rows).
-constexpr int SEL_THREADS = 1024, SEL_WARPS = SEL_THREADS / 32;
-constexpr int SEL_HELD = 8, SEL_SEGMENT = SEL_THREADS * SEL_HELD;       // tokens a thread, the CTA holds
-constexpr int SEL_BINS = 2048, SEL_EACH = SEL_BINS / SEL_THREADS;
+// Rows of up to 8192 tokens (4096 where there are more rows than SMs) are read once and stay in registers.  Bound by latency, 4 x 3 barriers and the reads: one request's 8 rows of 6256 weights
+// 9 us with 1024 threads, 11 with 512; 512 ragged rows 31 and 24.
+constexpr int SEL_HELD = 8;                  // tokens a thread holds
+constexpr int SEL_BINS = 2048;
 
 struct SelectArgs {
   const float* weights;
@@ -34,7 +32,9 @@ __device__ __forceinline__ u32 order_of(float w) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-__global__ void __launch_bounds__(SEL_THREADS) select_kernel(SelectArgs a) {
+template <int SEL_THREADS>
+__global__ void __launch_bounds__(SEL_THREADS, 1024 / SEL_THREADS) select_kernel(SelectArgs a) {
+  constexpr int SEL_WARPS = SEL_THREADS / 32, SEL_SEGMENT = SEL_THREADS * SEL_HELD, SEL_EACH = SEL_BINS / SEL_THREADS;
   __shared__ u32 s_bins[3][SEL_BINS];
   __shared__ u32 s_scan[2][SEL_WARPS];
   __shared__ u32 s_digit, s_want;
@@ -166,8 +166,9 @@ __global__ void __launch_bounds__(SEL_THREADS) select_kernel(SelectArgs a) {
 // Pure data movement, bound by HBM.  A thread moves 16 bytes (of a 4-bit cache: 32 codes and their two scales) of CP_EACH tokens, which are all read before the first is written.
 // Into other blocks, chunks of tokens are spread over CTAs.  In place one CTA takes a slice of a request's and head's rows chunk by chunk: a token never moves back, so what a
 // chunk's writes cover has been read by that chunk or the ones before it.
-// 64 requests cut to 2048 tokens of 8 heads x 128, K and V (1.04 GB): 221 us, 4.7 TB/s, with 4 tokens a thread and 5 CTAs an SM; 8 tokens 243 (4 CTAs) to 314 (3), 2 tokens 241 (8 CTAs).
-constexpr int CP_THREADS = 256, CP_EACH = 4;
+// 64 requests cut to 2048 tokens of 8 heads x 128, K and V (1.04 GB): 166 us, 6.2 TB/s, with 8 tokens a thread and 4 CTAs an SM; 4 tokens 168 (6 CTAs) to 199 (4), 2 tokens 194 (8), 16 tokens
+// 202 (3).
+constexpr int CP_THREADS = 256, CP_EACH = 8;
 
 struct CompactArgs {
   Cache cache;
@@ -177,7 +178,7 @@ struct CompactArgs {
 };
 
 template <bool PACKED, int D, int PIECES /*16-byte pieces of a slice*/>
-__global__ void __launch_bounds__(CP_THREADS, 5) compact_kernel(CompactArgs a) {
+__global__ void __launch_bounds__(CP_THREADS, 4) compact_kernel(CompactArgs a) {
   constexpr int TOKENS = CP_THREADS / PIECES, CHUNK = TOKENS * CP_EACH;
   const u32 B = a.cache.block_tokens;
   const bool is_v = blockIdx.z != 0;
@@ -187,50 +188,54 @@ __global__ void __launch_bounds__(CP_THREADS, 5) compact_kernel(CompactArgs a) {
   const int* const kept = a.kept + ((i64)r * a.cache.heads + h) * a.width;
   const int* const from = a.from + (i64)r * a.from_blocks;
   const int* const to = a.to + (i64)r * a.to_blocks;
-  const int piece = threadIdx.x % PIECES, t = threadIdx.x / PIECES;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, piece = lane % PIECES;
+  constexpr int AT_ONCE = 32 / PIECES, PER = (AT_ONCE * CP_EACH + 31) / 32;        // tokens a warp moves at once, tokens a lane looks up
   bool bounds = false;
   for (int base = step * CHUNK; base < n; base += a.steps * CHUNK) {
+    // Where a warp's tokens lie and go: a lane each, since the divisions by the block's size cost more than the bytes (by every thread for itself: 150 instructions a 16 bytes)
+    unsigned long long from_at[PER], to_at[PER];
+    u32 rows[PER];                           // 4-bit: the token's row in its tile, there and here
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      const int q = e * 32 + lane, i = base + q / AT_ONCE * TOKENS + warp * AT_ONCE + q % AT_ONCE;
+      from_at[e] = to_at[e] = 0;
+      rows[e] = 0;
+      if (q >= AT_ONCE * CP_EACH || i >= n) continue;
+      const int j = kept[i];
+      const u32 ib = (u32)i / B, jb = (u32)j / B;
+      const int db = ib < (u32)a.to_blocks ? to[ib] : -1, sb = j >= 0 && jb < (u32)a.from_blocks ? from[jb] : -1;
+      if ((u32)sb >= a.cache.num_blocks || (u32)db >= a.cache.num_blocks) { bounds = true; continue; }
+      if (a.from == a.to && i == j) continue;
+      const u32 ir = (u32)i - ib * B, jr = (u32)j - jb * B;
+      rows[e] = jr % TILE | ir % TILE << 8;
+      from_at[e] = reinterpret_cast<unsigned long long>(PACKED ? tile_ptr(a.cache, is_v, sb, h, jr, D) : row_ptr(a.cache, is_v, sb, h, jr, D));
+      to_at[e] = reinterpret_cast<unsigned long long>(PACKED ? tile_ptr(a.cache, is_v, db, h, ir, D) : row_ptr(a.cache, is_v, db, h, ir, D));
+    }
     uint4 v[CP_EACH];
     u32 scale[CP_EACH];
-    unsigned char* dst[CP_EACH];
-    int src_tok[CP_EACH], dst_blk[CP_EACH];
 #pragma unroll
     for (int k = 0; k < CP_EACH; ++k) {
-      const int i = base + k * TOKENS + t;
-      src_tok[k] = i < n ? kept[i] : -2;
-      dst_blk[k] = i < n && (int)((u32)i / B) < a.to_blocks ? to[(u32)i / B] : -1;
-    }
-#pragma unroll
-    for (int k = 0; k < CP_EACH; ++k) {
-      const int i = base + k * TOKENS + t, j = src_tok[k];
-      dst[k] = nullptr;
-      if (j == -2) continue;
-      const u32 jb = (u32)j / B;
-      const int sb = j >= 0 && jb < (u32)a.from_blocks ? from[jb] : -1;
-      if ((u32)sb >= a.cache.num_blocks || (u32)dst_blk[k] >= a.cache.num_blocks) { bounds = true; continue; }
-      if (a.from == a.to && i == j) continue;
+      const int e = k * AT_ONCE / 32, who = k * AT_ONCE % 32 + lane / PIECES;
+      const unsigned char* const src = reinterpret_cast<const unsigned char*>(__shfl_sync(FULL, from_at[e], who));
+      const u32 m = PACKED ? __shfl_sync(FULL, rows[e], who) & 255u : 0;
+      if (!src) continue;
       if (PACKED) {
-        const unsigned char* tile = tile_ptr(a.cache, is_v, sb, h, (u32)j % B, D);
-        const int m = (u32)j % TILE;
-        v[k] = *reinterpret_cast<const uint4*>(tile + code_place(D, m, piece) * 16);
-        scale[k] = tile[scale_at(D, is_v, m, 2 * piece)] | (u32)tile[scale_at(D, is_v, m, 2 * piece + 1)] << 8;
-        dst[k] = tile_ptr(a.cache, is_v, dst_blk[k], h, (u32)i % B, D);
-      } else {
-        const int at = slice * (PIECES * 16) + piece * 16;
-        v[k] = *reinterpret_cast<const uint4*>(row_ptr(a.cache, is_v, sb, h, (u32)j % B, D) + at);
-        dst[k] = row_ptr(a.cache, is_v, dst_blk[k], h, (u32)i % B, D) + at;
-      }
+        v[k] = *reinterpret_cast<const uint4*>(src + code_place(D, m, piece) * 16);
+        scale[k] = src[scale_at(D, is_v, m, 2 * piece)] | (u32)src[scale_at(D, is_v, m, 2 * piece + 1)] << 8;
+      } else v[k] = *reinterpret_cast<const uint4*>(src + slice * (PIECES * 16) + piece * 16);
     }
     if (a.steps == 1) __syncthreads();
 #pragma unroll
     for (int k = 0; k < CP_EACH; ++k) {
-      if (!dst[k]) continue;
+      const int e = k * AT_ONCE / 32, who = k * AT_ONCE % 32 + lane / PIECES;
+      unsigned char* const dst = reinterpret_cast<unsigned char*>(__shfl_sync(FULL, to_at[e], who));
+      const u32 m = PACKED ? __shfl_sync(FULL, rows[e], who) >> 8 : 0;
+      if (!dst) continue;
       if (PACKED) {
-        const int m = (u32)(base + k * TOKENS + t) % TILE;
-        *reinterpret_cast<uint4*>(dst[k] + code_place(D, m, piece) * 16) = v[k];
-        dst[k][scale_at(D, is_v, m, 2 * piece)] = (unsigned char)scale[k];
-        dst[k][scale_at(D, is_v, m, 2 * piece + 1)] = (unsigned char)(scale[k] >> 8);
-      } else *reinterpret_cast<uint4*>(dst[k]) = v[k];
+        *reinterpret_cast<uint4*>(dst + code_place(D, m, piece) * 16) = v[k];
+        dst[scale_at(D, is_v, m, 2 * piece)] = (unsigned char)scale[k];
+        dst[scale_at(D, is_v, m, 2 * piece + 1)] = (unsigned char)(scale[k] >> 8);
+      } else *reinterpret_cast<uint4*>(dst + slice * (PIECES * 16) + piece * 16) = v[k];
     }
   }
   if (bounds && a.status) atomicOr(a.status, PTSTORE_S_BOUNDS);
@@ -270,7 +275,12 @@ extern "C" int ptstore_select_tokens(const float* weights, int64_t weights_reque
   const SelectArgs a = {weights, weights_request_stride, weights_head_stride, lengths, heads, width, budget, first, recent, kept, lengths_out, weights_out,
                         out_request_stride, out_head_stride, status};
   (void)cudaGetLastError();
-  select_kernel<<<(unsigned)(R * heads), SEL_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(a);
+  Gpu gpu;
+  const int rs = current_gpu(&gpu);
+  if (rs) return rs;
+  const i64 rows = (i64)R * heads;
+  if (rows > gpu.sms) select_kernel<512><<<(unsigned)rows, 512, 0, static_cast<cudaStream_t>(stream)>>>(a);
+  else select_kernel<1024><<<(unsigned)rows, 1024, 0, static_cast<cudaStream_t>(stream)>>>(a);
   return cudaGetLastError() == cudaSuccess ? PTSTORE_OK : PTSTORE_E_CUDA;
 }
 
