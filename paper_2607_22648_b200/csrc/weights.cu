@@ -10,6 +10,10 @@
 // Weights keep what 32 bits can hold of them.  The tensor cores cut off what does not fit the running sum, so every product of rows comes out small by a part of itself that grows with
 // the length of the sums.  So scores are summed up in several accumulators, and the scale makes up for what is cut off on average (cut_off below).  Scale and lse, times log2 e, are kept
 // as two numbers each (a rounding of an exponent of 20 is 2^-20 of the weight).
+//
+// B200: a decode step of 64 requests (2064 .. 6256 tokens, 32 / 8 heads x 128, bf16) 107 us, 5.4 TB/s; 32 last tokens of 16 prompts over 4160 tokens, 4-bit, 70 us: 9 exponentials a
+// clock and SM of 16, since a tile's unpacking, products and sums follow one another and three CTAs an SM cover for that only in part; latent rows (8 x 16.4k, 64 heads) 59 us, 2.6 TB/s:
+// one CTA an SM, whose tile of 72 KB is loaded while one is computed with.
 #include <type_traits>
 
 #include "attend_prompt.cuh"
