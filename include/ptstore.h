@@ -589,7 +589,7 @@ typedef struct ptstore_latent_attend {
   int64_t  q_latent_token_stride, q_latent_head_stride;
   const void* q_rope;            /* [tokens][num_heads][64], likewise */
   int64_t  q_rope_token_stride, q_rope_head_stride;
-  void*    out;                  /* [tokens][num_heads][head_dim - 64], likewise; may be q_latent itself if its strides are the same */
+  void*    out;                  /* [tokens][num_heads][head_dim - 64], likewise; may be q_latent itself if its strides are the same, otherwise overlaps nothing */
   int64_t  out_token_stride, out_head_stride;
   float*   lse;                  /* [tokens][num_heads] contiguous, or NULL: as in ptstore_attend_lse */
   const int32_t* token_offsets;  /* [requests + 1] */
