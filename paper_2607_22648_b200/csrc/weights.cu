@@ -45,7 +45,7 @@ struct WeightsShape {
   static constexpr int HELD = NR == 16 ? 16 : D > 128 ? 64 : 128;                                                   // rows of Q that stay in shared memory
   static constexpr int STAGES = PACKED ? 1 : 2, K_BYTES = KT * D * 2, Q_BYTES = HELD * D * 2;
   static constexpr int SMEM = STAGES * K_BYTES + Q_BYTES + 1024;
-  static constexpr int CTAS = 230000 / (SMEM + 3072) < 1 ? 1 : 230000 / (SMEM + 3072);       // of an SM, by shared memory
+  static constexpr int OTHER = 3 << 10, CTAS = 230000 / (SMEM + OTHER) < 1 ? 1 : 230000 / (SMEM + OTHER);      // static shared memory; CTAs of an SM
   static constexpr int NEED = SUMS * NR, COLS = NEED <= 32 ? 32 : NEED <= 64 ? 64 : NEED <= 128 ? 128 : NEED <= 256 ? 256 : 512;
 };
 
