@@ -610,6 +610,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
       if (tid == 0 && !whole && cta == first) { part->r = r; part->rt = rt; part->parts = (int)(last - first) + 1; }
       asm volatile("bar.sync 3, 128;" ::: "memory");
       const bool any_bad = *reinterpret_cast<volatile int*>(&s.any_bad) != 0;
+      u32 turn = 0;                           // pieces of 32 rows done: rows that are not there have none, so c does not say which place is free
 #pragma unroll 1
       for (int c = 0; c < MT * NQ; c += 32) {
         const int d = c / NQ * 128 + tid, r0 = c % NQ;
@@ -638,7 +639,7 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
         }
         if (whole) {
           // whole rows of 128 elements through shared memory (P's, which the last products have read)
-          unsigned char* const z = smem + (WIDE ? ((c >> 5) & 1) * 8192 : 0);
+          unsigned char* const z = smem + (WIDE ? (turn++ & 1) * 8192 : 0);
 #pragma unroll
           for (int i = 0; i < 32; i += 2) {
             const u32 two = pack2<F16>(o[i], o[i + 1]);
@@ -653,7 +654,8 @@ __global__ void __launch_bounds__(LA_THREADS, 1) latent_attend_kernel(const Late
               *reinterpret_cast<uint4*>(a.out + 2 * ((i64)(rq.row0 + flat / a.group) * a.o_token + (i64)(flat % a.group) * a.o_head + (int)half * DIMS + c / NQ * 128 + (tid & 15) * 8)) =
                   *reinterpret_cast<const uint4*>(z + i * 256 + (tid & 15) * 16);
           }
-          if (!WIDE) asm volatile("bar.sync 3, 128;" ::: "memory");       // (two places take turns where there are two)
+          // (two places take turns where there are two: a piece's writes come behind the barrier of the piece before, which the reads of the one before that precede)
+          if (!WIDE) asm volatile("bar.sync 3, 128;" ::: "memory");
         } else {
           float* const dst = my + r0 * DIMS + d;
 #pragma unroll

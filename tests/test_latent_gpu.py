@@ -416,3 +416,18 @@ def test_offsets_beyond_32_bits(G):
     k = torch.cat([c, r], 1).double()
     want = torch.softmax(q[0].double() @ k.t() * 0.07, 1) @ c.double()
     assert float((out[0].double() - want).abs().max()) < 0.02
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("L,heads,new,max_new", [(512, 80, 1, 1), (512, 96, 1, 1), (512, 20, 1, 2), (512, 16, 9, 9), (512, 32, 3, 3), (256, 72, 1, 1)])
+def test_rows_that_leave_pieces_of_a_tile_out(G, L, heads, new, max_new, dtype):
+    """The output of a pair of CTAs goes out 32 rows and 128 elements at a time, through two places in turn.  Pieces without rows are left out: the turns must not follow the pieces' numbers."""
+    lens = [64 + 37 * i % 200 for i in range(300)]
+    b = make(G, L, dtype, heads, 16, lens, [new] * 300, seed=heads + new)
+    call(G, b, max_new=max_new)
+    check(b, picks={b["offsets"][r] + i for r in range(0, 300, 7) for i in (0, new - 1)})
+    want, lse = b["out"].clone(), b["lse"].clone()
+    for _ in range(20):
+        b["out"].fill_(5.0)
+        call(G, b, max_new=max_new)
+        assert torch.equal(b["out"], want) and torch.equal(b["lse"], lse)
