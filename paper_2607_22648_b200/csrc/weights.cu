@@ -355,8 +355,11 @@ template <bool PACKED, bool F16, bool QFP16, int D, int NR>
 int launch(Weights wa, const Gpu& gpu, cudaStream_t s) {
   using Shape = WeightsShape<PACKED, D, NR>;
   const double scale2 = wa.scale2 * (1.0 + cut_off(PACKED, Shape::PER));
+  // towards zero, and the rest of the same sign and never zero: an infinite score then stays the infinity that it is times the scale
   wa.scale_hi = (float)scale2;
-  wa.scale_lo = isfinite(wa.scale_hi) ? (float)(scale2 - wa.scale_hi) : 0.0f;
+  if (fabs((double)wa.scale_hi) > fabs(scale2)) wa.scale_hi = nextafterf(wa.scale_hi, 0.0f);
+  wa.scale_lo = (float)(scale2 - wa.scale_hi);
+  if (wa.scale_lo == 0.0f && scale2 != 0.0) wa.scale_lo = copysignf(0x1p-126f, wa.scale_hi);
   static std::atomic<u64> devices{0};
   auto* kernel = weights_kernel<PACKED, F16, QFP16, D, NR>;
   const int rc = allow_smem(kernel, Shape::SMEM, devices, gpu.dev);

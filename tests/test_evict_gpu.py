@@ -471,3 +471,58 @@ def test_streams_and_graphs(G):
         torch.cuda.synchronize()
         for x, y in zip((out, kept, new_lens, compacted, b["cache"].tensors[0]), want):
             assert torch.equal(x, y)
+
+
+def with_infinite_key(G, b, r, token, element, value):
+    """One element of a cached token's key, for all heads."""
+    B, lay = b["lay"].block_tokens, b["lay"]
+    slot = dev([int(b["tables"][r, token // B]) * B + token % B], torch.int64)
+    if lay.latent:
+        c, p = G.latent_read(lay, b["cache"], b["layer"], slot)
+        x = torch.cat([c, p], 1)
+        x[:, element] = value
+        G.latent_write(lay, b["cache"], b["layer"], x[:, :b["L"]].contiguous(), x[:, b["L"]:].contiguous(), slot)
+    else:
+        k, v = G.kv_read(lay, b["cache"], 0, slot, b["q"].dtype)
+        k[:, :, element] = value
+        G.kv_write(lay, b["cache"], 0, k, v, slot)
+
+
+def check_infinite_scores(G, b, new, scale):
+    """A token whose scores are all minus infinity was given nothing, one with an infinite score (beside a finite logarithm) infinitely much; the others what they were given before."""
+    element, first = 5, -b["q"].abs()[:, :, 5] - 0.5
+    b["q"][:, :, element] = first if scale > 0 else -first
+    T, heads = b["q"].shape[:2]
+    lse, layer = torch.empty(T, heads, device="cuda"), b.get("layer", 0)
+    args = (dev(b["offsets"]), dev(b["lens"]), b["tables"], new)
+    if b["lay"].latent:
+        L = b["L"]
+        G.latent_attend(b["lay"], b["cache"], layer, b["q"][:, :, :L], b["q"][:, :, L:], *args, scale, lse=lse)
+    else:
+        G.attend(b["lay"], b["cache"], 0, b["q"], *args, scale=scale, lse=lse)
+    w = torch.empty(len(b["lens"]), b["lay"].heads, max(b["lens"]), device="cuda")
+    G.attend_weights(b["lay"], b["cache"], layer, b["q"], lse, *args, w, scale=scale, accumulate=False)
+    want = w.clone()
+    assert bool(want.isfinite().all())
+    for r, token, value, given in ((0, 30, math.inf, 0.0), (0, 141, -math.inf, math.inf), (1, 7, math.inf, 0.0)):
+        with_infinite_key(G, b, r, token, element, value)
+        want[r, :, token] = given
+    G.attend_weights(b["lay"], b["cache"], layer, b["q"], lse, *args, w, scale=scale, accumulate=False)
+    assert torch.equal(w, want)
+
+
+SCALES = [0.08838834764, 0.1, -0.07, 0.05, 0.3, -0.125]
+
+
+@pytest.mark.parametrize("scale", SCALES)
+@pytest.mark.parametrize("fmt,dtype", FORMATS[2:])
+@pytest.mark.parametrize("heads,new", [(32, 1), (8, 16), (32, 20)])
+def test_infinite_scores(G, fmt, dtype, heads, new, scale):
+    check_infinite_scores(G, make(G, getattr(G, fmt), dtype, heads, 2, 128, 16, [200, 40], [new] * 2, seed=6, spread=0.3), new, scale)
+
+
+@pytest.mark.parametrize("scale", SCALES)
+@pytest.mark.parametrize("dtype", latent.BOTH)
+@pytest.mark.parametrize("heads,new", [(16, 1), (64, 1), (64, 3)])
+def test_infinite_scores_of_a_latent_cache(G, dtype, heads, new, scale):
+    check_infinite_scores(G, latent.make(G, 512, dtype, heads, 16, [200, 40], [new] * 2, seed=6, spread=0.3), new, scale)
