@@ -15,6 +15,7 @@
 // clock and SM of 16, since a tile's unpacking, products and sums follow one another and three CTAs an SM cover for that only in part; latent rows (8 x 16.4k, 64 heads) 59 us, 2.6 TB/s:
 // one CTA an SM, whose tile of 72 KB is loaded while one is computed with.  Measured and dropped: chunks of 32 rows, one's products computed while the one before is added up (83 and
 // 65 us).
+#include <cfloat>
 #include <type_traits>
 
 #include "attend_prompt.cuh"
@@ -166,21 +167,22 @@ __global__ void __launch_bounds__(AW_THREADS, D > 128 ? 1 : 3) weights_kernel(co
     issue(0);
     cp_commit();
   }
-  // ---- rows row0 .. row0 + HELD - 1 of Q, in the products' type; rows that do not exist are zero and give nothing
+  // ---- rows row0 .. row0 + HELD - 1 of Q, in the products' type.  Rows that fill a chunk up are the last row once more, with a logarithm so large that they give nothing: rows of zeros
+  // would make NaN of a key that holds an infinity, whatever the real rows' scores are.
   auto load_q = [&](int row0) {
     constexpr int TPR = D > 128 ? 32 : CPR, EACH = (CPR + TPR - 1) / TPR, PASS = AW_THREADS / TPR;
     const int m = min(HELD, rows - row0), padded = (m + NR - 1) / NR * NR;
 #pragma unroll 2
     for (int p = 0; p < padded; p += PASS) {
       const int t = p + tid / TPR, c0 = tid % TPR;
-      const int flat = row0 + t, fr = flat / a.group, hq = (int)h * a.group + flat % a.group;
+      const int flat = row0 + min(t, m - 1), fr = flat / a.group, hq = (int)h * a.group + flat % a.group;
       const bool live = t < m;
       u32 x[EACH][4];
 #pragma unroll
       for (int e = 0; e < EACH; ++e) {
         const int c = c0 + e * TPR;
         uint4 v = make_uint4(0, 0, 0, 0);
-        if (live && c < CPR) v = *reinterpret_cast<const uint4*>(a.q + 2 * ((i64)(rq.row0 + fr) * a.q_token + (i64)hq * a.q_head + c * 8));
+        if (c < CPR) v = *reinterpret_cast<const uint4*>(a.q + 2 * ((i64)(rq.row0 + fr) * a.q_token + (i64)hq * a.q_head + c * 8));
         x[e][0] = v.x; x[e][1] = v.y; x[e][2] = v.z; x[e][3] = v.w;
       }
       float factor = 1.0f;
@@ -217,14 +219,14 @@ __global__ void __launch_bounds__(AW_THREADS, D > 128 ? 1 : 3) weights_kernel(co
         if (c < CPR) *reinterpret_cast<uint4*>(smem_q + (c >> 3) * (HELD * 128) + t * 128 + (((c & 7) ^ (t & 7)) * 16)) = make_uint4(x[e][0], x[e][1], x[e][2], x[e][3]);
       }
       if (c0 == 0) {
-        const float l = live ? wa.lse[(i64)(rq.row0 + fr) * a.heads + hq] : INFINITY;
-        const float hi = l * LOG2E;
+        const float l = wa.lse[(i64)(rq.row0 + fr) * a.heads + hq];
+        const float hi = live ? l * LOG2E : FLT_MAX;
         // l log2 e as two numbers; an infinity is one
         s_lse[(t & ~1) * 2 + (t & 1)] = -hi;
-        s_lse[(t & ~1) * 2 + 2 + (t & 1)] = fabsf(hi) < INFINITY ? -(fmaf(l, LOG2E, -hi) + l * LOG2E_REST) : 0.0f;
+        s_lse[(t & ~1) * 2 + 2 + (t & 1)] = live && fabsf(hi) < INFINITY ? -(fmaf(l, LOG2E, -hi) + l * LOG2E_REST) : 0.0f;
         if (SCALED) s_factor[t] = factor;
         const i64 see = (i64)rq.pos0 + fr + 1;
-        const int s = !live ? 0x7FFFFFFF : l == -INFINITY || see < 0 ? 0 : see > n ? n : (int)see;          // a row that saw nothing gave nothing
+        const int s = l == -INFINITY || see < 0 ? 0 : see > n ? n : (int)see;          // a row that saw nothing gave nothing
         s_see[t] = s;
         atomicMin(&s_min, s);
       }

@@ -526,3 +526,15 @@ def test_infinite_scores(G, fmt, dtype, heads, new, scale):
 @pytest.mark.parametrize("heads,new", [(16, 1), (64, 1), (64, 3)])
 def test_infinite_scores_of_a_latent_cache(G, dtype, heads, new, scale):
     check_infinite_scores(G, latent.make(G, 512, dtype, heads, 16, [200, 40], [new] * 2, seed=6, spread=0.3), new, scale)
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS[2:])
+@pytest.mark.parametrize("heads,new", [(2, 1), (8, 1), (30, 1), (8, 5), (32, 6), (8, 33), (6, 47)])
+def test_infinite_scores_beside_rows_that_do_not_fill_a_chunk(G, fmt, dtype, heads, new):
+    check_infinite_scores(G, make(G, getattr(G, fmt), dtype, heads, 2, 128, 16, [200, 60], [new] * 2, seed=7, spread=0.3), new, 0.09)
+
+
+@pytest.mark.parametrize("dtype", latent.BOTH)
+@pytest.mark.parametrize("L,heads,new", [(512, 5, 1), (256, 40, 1), (512, 20, 4)])
+def test_infinite_scores_of_a_latent_cache_beside_rows_that_do_not_fill_a_chunk(G, L, dtype, heads, new):
+    check_infinite_scores(G, latent.make(G, L, dtype, heads, 16, [200, 60], [new] * 2, seed=7, spread=0.3), new, 0.09)
