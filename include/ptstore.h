@@ -647,6 +647,8 @@ int ptstore_expanded_attend(const ptstore_expanded_attend_t* args /*host struct*
  * over rows with j <= pos (as in ptstore_attend) and lse other than minus infinity.  Any cache format (LATENT: keys are whole rows, q is [tokens][num_heads][head_dim], the latent
  * part and then the rotary part).  Entries from the request's length on: as they were, or zero without accumulate; so are tokens whose block is not there (S_BOUNDS
  * where its id is outside the cache).  Tokens from `width` on are not counted.  Equal inputs give equal bits.
+ * Scores are sums of exact products in 32 bits, which the matrix instructions cut off instead of rounding.  They are enlarged by what that takes away on average
+ * (a score whose sum loses nothing comes out large by that, at most 2.6 parts in 2^24); lse is taken as it is, with the errors of the attention that left it.
  */
 typedef struct ptstore_attend_weights {
   uint32_t struct_size;          /* sizeof(ptstore_attend_weights_t) */

@@ -349,9 +349,14 @@ __global__ void __launch_bounds__(AW_THREADS, D > 128 ? 1 : 3) weights_kernel(co
   if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(Shape::COLS) : "memory");
 }
 
-// By how much a sum of `per` instructions comes out small, relative: fitted to scores of 64 .. 576 elements against 64 bits (slopes in units of 2^-24, sums of one / two / four / six:
-// 16-bit caches 0.7 .. 1.0 / 1.1 .. 1.7 / 1.6 .. 1.8 / 2.3 .. 2.6; 4-bit values, whose products have few bits, 0.3 .. 0.4 / 0.4 .. 0.7 / 0.5 .. 1.1).
-constexpr double cut_off(bool packed, int per) { return (0.7 + 0.28 * per) * (packed ? 0.45 : 1.0) * 0x1p-24; }
+// What the tensor cores cut off a sum of n instructions on average, as a part of it.  They cut after every instruction instead of rounding: half a step, which is 2^-24 / (2 ln 2) of a
+// number whose mantissa is as likely as numbers' are; and the running sum after j of n terms that are alike goes with j / n of the last one.  So 2^-24 / (2 ln 2) (1 + 2 + .. + n) / n.
+// Measured against 64 bits with scores of 64 .. 576 elements, n = 1 / 2 / 4 / 6, in 2^-24: 0.7 .. 1.0 / 1.1 .. 1.7 / 1.6 .. 1.8 / 2.3 .. 2.6 (here 0.72 / 1.08 / 1.80 / 2.52).  A score
+// whose sum is exact is off by as much instead, at most 2.6 2^-24 of it (the header says so).  Products with 4-bit keys have fewer bits, of which less
+// is cut off: half of it (measured 0.3 .. 0.4 / 0.4 .. 0.7 / 0.5 .. 1.1).
+// Weights against 64 bits (norm, in 1e-6) with it / without / 32-bit products of a library: a decode step 0.6 / 0.9 / 0.8, latent rows 1.3 / 2.3 / 1.3.  The loss can also be measured, by
+// sums that go forth and back again (what is left of them over): 0.6 and 1.4, but three times the products, 132 and 84 us in place of 116 and 61.
+constexpr double cut_off(bool packed, int n) { return 0x1p-24 / 1.3862943611198906 * (n + 1) / (packed ? 4 : 2); }
 
 template <bool PACKED, bool F16, bool QFP16, int D, int NR>
 int launch(Weights wa, const Gpu& gpu, cudaStream_t s) {

@@ -538,3 +538,72 @@ def test_infinite_scores_beside_rows_that_do_not_fill_a_chunk(G, fmt, dtype, hea
 @pytest.mark.parametrize("L,heads,new", [(512, 5, 1), (256, 40, 1), (512, 20, 4)])
 def test_infinite_scores_of_a_latent_cache_beside_rows_that_do_not_fill_a_chunk(G, L, dtype, heads, new):
     check_infinite_scores(G, latent.make(G, L, dtype, heads, 16, [200, 60], [new] * 2, seed=7, spread=0.3), new, 0.09)
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS + [("KV_LATENT_BF16", torch.bfloat16), ("KV_LATENT_FP16", torch.float16)])
+@pytest.mark.parametrize("new", [1, 20])
+def test_weights_of_large_scores_that_add_up_exactly(G, fmt, dtype, new):
+    """Keys of two elements and scores near 950: sums of products are exact (at most 17 bits), so nothing is lost but in the exponent, which is the difference of two numbers of 48 bits
+    (2^-40 of a score), rounded to 32 when small (2^-23 of itself), in exp2 (2^-21) and in sums of rows (2^-24 an addend); and in what scores are enlarged by, at most 2.6 parts in
+    2^24."""
+    is_latent = fmt.startswith("KV_LATENT")
+    n, block, scale = 300, 16, 0.08838834764
+    b = latent.make(G, 512, dtype, 8, block, [n], [new]) if is_latent else make(G, getattr(G, fmt), dtype, 8, 2, 128, block, [n], [new])
+    heads, kv_heads, D, lay, gen = 8, b["lay"].heads, b["q"].shape[2], b["lay"], gen_of(1)
+    slots = torch.tensor([int(b["tables"][0, p // block]) * block + p % block for p in range(n)], dtype=torch.int64, device="cuda")
+    k = torch.zeros(n, kv_heads, D, dtype=dtype, device="cuda")
+    k[:, :, 0] = 84.0
+    k[:, :, 16] = 7 * torch.randint(-8, 9, (n, kv_heads), generator=gen, device="cuda").to(dtype) / 8
+    if is_latent:
+        G.latent_write(lay, b["cache"], b["layer"], k[:, 0, :512], k[:, 0, 512:], slots)
+        assert torch.equal(torch.cat(G.latent_read(lay, b["cache"], b["layer"], slots), 1), k[:, 0])
+    else:
+        G.kv_write(lay, b["cache"], 0, k, k, slots)
+        assert torch.equal(G.kv_read(lay, b["cache"], 0, slots, dtype)[0], k)
+    q = b["q"].zero_()
+    q[:, :, 0] = 128.0
+    q[:, :, 16] = torch.randint(-4, 5, q.shape[:2], generator=gen, device="cuda").to(dtype)
+    group = heads // kv_heads
+    s = torch.einsum("ihgd,nhd->ihgn", q[:new].double().unflatten(1, (kv_heads, group)), k.double()) * float(torch.tensor(scale, dtype=torch.float32))
+    s = s.masked_fill(torch.arange(n, device="cuda") > torch.arange(n - new, n, device="cuda")[:, None, None, None], -math.inf)
+    lse = torch.zeros(q.shape[:2], device="cuda")
+    lse[:new] = torch.logsumexp(s, 3).flatten(1).float()
+    e = s - lse[:new].double().unflatten(1, (kv_heads, group))[..., None]
+    p = torch.exp(e)
+    size = torch.where(p > 0, e.abs() * 1.4427, 0.0)
+    tol = (p * (2.0 ** -23 * size + 2.0 ** -21 + (2.0 ** -40 + 2.6 * 2.0 ** -24) * 1000)).sum((0, 2)) + new * group * 2.0 ** -24 * p.sum((0, 2))
+    w = torch.empty(1, kv_heads, n, device="cuda")
+    G.attend_weights(lay, b["cache"], b.get("layer", 0), q, lse, dev(b["offsets"]), dev([n]), b["tables"], new, w, scale=scale, accumulate=False)
+    err = (w[0].double() - p.sum((0, 2))).abs()
+    assert bool((err <= tol).all()), float((err / tol).max())
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS + [("KV_LATENT_BF16", torch.bfloat16), ("KV_LATENT_FP16", torch.float16)])
+@pytest.mark.parametrize("heads,n", [(8, 400), (32, 3000)])
+def test_weights_of_a_row_add_up_to_one(G, fmt, dtype, heads, n):
+    """Products of small integers, whose sums lose nothing, and scores of at most 30.  A logarithm is off by the roundings of its reference and its two last steps, half a step of a number
+    below 64 each (2^-19), its sum by 2^-21 of an exponential and 2^-24 of 2 addends a key block of 16 and of one a block; a weight by half a step of an exponent below 64, by 2^-21 and by
+    the 2.6 parts in 2^24 of its score."""
+    is_latent = fmt.startswith("KV_LATENT")
+    b = latent.make(G, 512, dtype, heads, 16, [n], [1]) if is_latent else make(G, getattr(G, fmt), dtype, heads, 2, 128, 16, [n], [1])
+    lay, gen, kv_heads, D = b["lay"], gen_of(5), b["lay"].heads, b["q"].shape[2]
+    slots = torch.tensor([int(b["tables"][0, p // 16]) * 16 + p % 16 for p in range(n)], dtype=torch.int64, device="cuda")
+    k = (7 * torch.randint(-1, 2, (n, kv_heads, D), generator=gen, device="cuda")).to(dtype) / 8
+    if is_latent:
+        G.latent_write(lay, b["cache"], b["layer"], k[:, 0, :512], k[:, 0, 512:], slots)
+    else:
+        G.kv_write(lay, b["cache"], 0, k, k, slots)
+        assert torch.equal(G.kv_read(lay, b["cache"], 0, slots, dtype)[0], k)
+    q = b["q"]
+    q.copy_(torch.randint(-2, 3, q.shape, generator=gen, device="cuda"))
+    group = heads // kv_heads
+    scale = 25.0 / float((q[:1].double().unflatten(1, (kv_heads, group)) @ k.double().permute(1, 2, 0)).abs().max())
+    lse, args = torch.zeros(q.shape[:2], device="cuda"), (dev(b["offsets"]), dev([n]), b["tables"], 1)
+    if is_latent:
+        G.latent_attend(lay, b["cache"], b["layer"], q[:, :, :512].contiguous(), q[:, :, 512:].contiguous(), *args, scale, lse=lse)
+    else:
+        G.attend(lay, b["cache"], 0, q, *args, scale=scale, lse=lse)
+    w = torch.empty(1, kv_heads, n, device="cuda")
+    G.attend_weights(lay, b["cache"], b.get("layer", 0), q, lse, *args, w, scale=scale, accumulate=False)
+    tol = 3 * 2.0 ** -19 + 2.0 ** -21 + 2.0 ** -24 * (2 + n / 16) + 2.0 ** -19 + 2.0 ** -21 + 2.6 * 2.0 ** -24 * 30
+    assert float((w[0].double().sum(1) / group - 1).abs().max()) < tol
