@@ -607,3 +607,85 @@ def test_weights_of_a_row_add_up_to_one(G, fmt, dtype, heads, n):
     G.attend_weights(lay, b["cache"], b.get("layer", 0), q, lse, *args, w, scale=scale, accumulate=False)
     tol = 3 * 2.0 ** -19 + 2.0 ** -21 + 2.0 ** -24 * (2 + n / 16) + 2.0 ** -19 + 2.0 ** -21 + 2.6 * 2.0 ** -24 * 30
     assert float((w[0].double().sum(1) / group - 1).abs().max()) < tol
+
+
+# ---- batches that give a CTA several tiles -----------------------------------------------------------------------------------------------
+def check_request(b, r, got, lse, k_values, scale, packed):
+    """One request's weights against the definition, all its rows at once; tolerances as in `expected`."""
+    n, a, e = b["lens"][r], b["offsets"][r], b["offsets"][r + 1]
+    if n == 0:
+        assert bool((got[r] == 0).all())
+        return
+    q, heads, D = b["q"][a:e].double(), b["q"].shape[1], b["q"].shape[2]
+    H = b["lay"].heads
+    group = heads // H
+    k, ok = ref.gather(k_values, b["tables"][r], n, b["lay"].block_tokens)
+    assert bool(ok.all())
+    see = torch.arange(n, device="cuda") <= torch.arange(n - (e - a), n, device="cuda")[:, None, None]
+    for h in range(H):
+        mine, given = q[:, h * group:(h + 1) * group], lse[a:e, h * group:(h + 1) * group].double()[..., None]
+        s = (mine @ k[:, h].t()) * scale
+        err = (D + 8) * 2.0 ** -23 * (mine.abs() @ k[:, h].abs().t()).masked_fill(~see, 0.0).amax(2, keepdim=True) * scale + 2.0 ** -20
+        if packed:
+            err = err + 2.0 ** -25 * mine.abs().amax(2, keepdim=True) * k[:, h].abs().sum(1).max() * scale
+        p = torch.exp(s - given).masked_fill(~see, 0.0)
+        want = p.sum((0, 1))
+        tol = (p * (2 * err + 2.0 ** -22 * (s.abs() + given.abs()) + 2.0 ** -21)).sum((0, 1)) + (e - a) * group * 2.0 ** -24 * want + 1e-30
+        off = (got[r, h, :n].double() - want).abs()
+        assert bool((off <= tol).all()), (r, h, float((off / tol).max()))
+    assert bool((got[r, :, n:] == 0).all()), r
+
+
+def check_batch(G, b, lse, layer, max_new, scale, k_values, packed):
+    R, H, width = len(b["lens"]), b["lay"].heads, max(b["lens"])
+    args = (b["lay"], b["cache"], layer, b["q"], lse, dev(b["offsets"]), dev(b["lens"]), b["tables"], max_new)
+    w, status = torch.full((R, H, width), 3.0, device="cuda"), dev([0])
+    G.attend_weights(*args, w, scale=scale, accumulate=False, status=status)
+    for r in (0, 1, 2, 3, R // 2, R - 1):
+        check_request(b, r, w, lse, k_values, scale, packed)
+    start = torch.rand(R, H, width + 9, device="cuda")
+    more = start.clone()
+    G.attend_weights(*args, more, scale=scale, status=status)
+    there = torch.arange(width, device="cuda") < dev(b["lens"])[:, None, None]
+    assert torch.equal(more[:, :, :width], torch.where(there, start[:, :, :width] + w, start[:, :, :width])) and torch.equal(more[:, :, width:], start[:, :, width:])
+    assert int(status.item()) == 0
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("dim,new", [(128, 1), (128, 20), (128, 40), (64, 1), (64, 50)])
+def test_several_tiles(G, fmt, dtype, dim, new):
+    """40 requests x 8 heads of up to 5000 tokens: runs of tiles a CTA, whose rows (4, 80, 160, 200 of a kv head) fill a chunk, several, or more than stay in shared memory."""
+    rng = random.Random(new)
+    lens = [5000, 0, 1000 + new, new] + [rng.randint(2000, 5000) for _ in range(36)]
+    b = make(G, getattr(G, fmt), dtype, 32, 8, dim, 16, lens, [min(new, n) for n in lens], seed=new)
+    lse = torch.zeros(b["q"].shape[:2], device="cuda")
+    scale = dim ** -0.5
+    G.attend(b["lay"], b["cache"], 0, b["q"], dev(b["offsets"]), dev(lens), b["tables"], new, scale=scale, lse=lse)
+    check_batch(G, b, lse, 0, new, scale, b["values"][0], fmt == "KV_PACKED" and dtype == torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", latent.BOTH)
+@pytest.mark.parametrize("L,heads,new", [(512, 16, 1), (512, 64, 1), (512, 50, 3), (256, 128, 1)])
+def test_several_tiles_of_a_latent_cache(G, L, dtype, heads, new):
+    rng = random.Random(heads)
+    lens = [4000, 0, 1000 + new, new] + [rng.randint(1000, 4000) for _ in range(36)]
+    b = latent.make(G, L, dtype, heads, 16, lens, [min(new, n) for n in lens], seed=heads)
+    latent.call(G, b)
+    check_batch(G, b, b["lse"], b["layer"], new, b["scale"], b["values"].unsqueeze(2), False)
+
+
+# ---- the choice where there are more rows than SMs -----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kind", ["spread", "ties", "special"])
+def test_choice_of_more_rows_than_sms(G, kind):
+    gen = gen_of(len(kind))
+    lengths = [4095, 4096, 4097, 8191, 8192, 8193, 9000, 0, 1, 700, 701, 4160, 9001, -1] + [50 + 211 * i for i in range(26)]
+    w = torch.exp(2 * torch.randn(len(lengths), 4, 9000, generator=gen, device="cuda"))
+    if kind == "ties":
+        w = (w * 2).floor()
+        w[:, 1] = 0.5
+    elif kind == "special":
+        w[w < 0.2], w[w > 20] = math.nan, math.inf
+        w[:, 2, ::3] = -math.inf
+        w[:, 3] = math.nan
+    check_choice(G, w, lengths, 700, 4, 64)
+    check_choice(G, w, lengths, 4096, 0, 1)
