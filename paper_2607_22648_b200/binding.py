@@ -515,7 +515,7 @@ def latent_attend(layout, cache, layer, q_latent, q_rope, token_offsets, lengths
     _on_device(cache.tensors[layer >> 1], dev, "cache")
     ql, qr, o = q_latent.stride(), q_rope.stride(), out.stride()
     at = _rows(q_latent, heads, L, T, dtype, dev, "q_latent"), _rows(q_rope, heads, LATENT_ROPE, T, dtype, dev, "q_rope"), _rows(out, heads, L, T, dtype, dev, "out")
-    if at[2] == at[0] and T > 0 and (o[:2] != ql[:2]):
+    if at[2] == at[0] and ((T > 1 and o[0] != ql[0]) or (T > 0 and heads > 1 and o[1] != ql[1])):
         raise ValueError("out: is q_latent with other strides")
     args = _LATENT_ATTEND.pack(_LATENT_ATTEND.size, wait_polls, at[0], ql[0], ql[1], at[1], qr[0], qr[1], at[2], o[0], o[1],
                                0 if lse is None else _vec(lse, torch.float32, T * heads, dev, "lse"), _vec(token_offsets, i32, R + 1, dev, "token_offsets"),

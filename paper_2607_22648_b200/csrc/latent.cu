@@ -144,6 +144,9 @@ extern "C" int ptstore_latent_attend(const ptstore_latent_attend_t* p, const pts
   if (!rows_aligned(p->q_latent, p->tokens, p->q_latent_token_stride, p->num_heads, p->q_latent_head_stride) ||
       !rows_aligned(p->q_rope, p->tokens, p->q_rope_token_stride, p->num_heads, p->q_rope_head_stride) ||
       !rows_aligned(p->out, p->tokens, p->out_token_stride, p->num_heads, p->out_head_stride)) return PTSTORE_E_INVAL;
+  // q itself as output: rows are written where they were read, which other strides are not
+  if (p->out == p->q_latent && ((p->tokens > 1 && p->out_token_stride != p->q_latent_token_stride) || (p->num_heads > 1 && p->out_head_stride != p->q_latent_head_stride)))
+    return PTSTORE_E_INVAL;
   if ((u64)p->max_blocks * cache->block_tokens > 1u << 30) return PTSTORE_E_LIMIT;
   if (p->requests > 1 << 20 || (i64)p->tokens * p->num_heads > 0x7FFFFFFF) return PTSTORE_E_LIMIT;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return PTSTORE_E_INVAL;

@@ -143,3 +143,18 @@ def test_kv_compact_refuses(G):  # noqa: F811
         assert call(**kw) == E_INVAL, kw                     # ({"to": A}: in place with another number of blocks)
     assert call(width=(1 << 30) + 1) == E_LIMIT and call(R=(1 << 20) + 1) == E_LIMIT
     assert call(R=0) == OK and call(width=0) == OK
+
+
+def test_latent_attend_refuses_q_as_output_with_other_strides(G):  # noqa: F811
+    need = G.lib.ptstore_latent_workspace_bytes(576)
+    same = dict(struct_size=C.sizeof(G.LatentAttend), q_latent=A, q_latent_token_stride=16 * 512, q_latent_head_stride=512, q_rope=A + 4096, q_rope_token_stride=16 * 64, q_rope_head_stride=64,
+                out=A, out_token_stride=16 * 512, out_head_stride=512, token_offsets=A, lengths=A, block_tables=A, requests=2, max_blocks=8, num_heads=16, tokens=10, max_new=5, scale=0.1)
+
+    def call(size=need - 1, **kw):                           # (a workspace that is too small is found later)
+        return G.lib.ptstore_latent_attend(C.byref(G.LatentAttend(**dict(same, **kw))), C.byref(latent_cache(G)), A, size, None, None)
+    assert call() == E_NOMEM
+    for kw in ({"out_token_stride": 32 * 512}, {"out_head_stride": 1024}, {"q_latent_token_stride": 16 * 576}, {"tokens": 1, "out_head_stride": 1024}, {"num_heads": 1, "out_token_stride": 1024}):
+        assert call(**kw) == E_INVAL, kw
+    # the stride of an axis of one does not matter, and other memory may have any strides
+    for kw in ({"tokens": 1, "out_token_stride": 8}, {"num_heads": 1, "out_head_stride": 8}, {"out": A + (1 << 20), "out_token_stride": 32 * 512}):
+        assert call(**kw) == E_NOMEM, kw
