@@ -77,7 +77,7 @@ inline u64 chunk_bytes_of(u32 format, u64 block_tokens, u64 heads, u64 dim) {
 inline int check_any_cache(const ptstore_kv_cache_t* c) {
   if (!c || !c->base || (reinterpret_cast<uintptr_t>(c->base) & 15u) || c->num_blocks == 0 || c->num_blocks > 0x7FFFFFFFu) return PTSTORE_E_INVAL;
   const u64 chunk = chunk_bytes_of(c->format, c->block_tokens, c->num_kv_heads, c->head_dim);
-  if (chunk == 0 || c->kv_stride_bytes % 16 || c->block_stride_bytes % 16 || c->block_stride_bytes < chunk) return PTSTORE_E_INVAL;
+  if (chunk == 0 || (!is_latent(c->format) && c->kv_stride_bytes % 16) || c->block_stride_bytes % 16 || c->block_stride_bytes < chunk) return PTSTORE_E_INVAL;
   if (c->format == PTSTORE_KV_PACKED && (!power_of_two(c->k_scale) || !power_of_two(c->v_scale))) return PTSTORE_E_INVAL;
   return PTSTORE_OK;
 }

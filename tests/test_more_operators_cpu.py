@@ -158,3 +158,11 @@ def test_latent_attend_refuses_q_as_output_with_other_strides(G):  # noqa: F811
     # the stride of an axis of one does not matter, and other memory may have any strides
     for kw in ({"tokens": 1, "out_token_stride": 8}, {"num_heads": 1, "out_head_stride": 8}, {"out": A + (1 << 20), "out_token_stride": 32 * 512}):
         assert call(**kw) == E_NOMEM, kw
+
+
+def test_a_latent_cache_has_no_stride_from_k_to_v(G):  # noqa: F811
+    """kv_stride_bytes is not used, so it may hold anything; of K and V it has to be a multiple of 16 as before."""
+    def write(c):
+        return G.lib.ptstore_latent_write(A, 512, A, 64, 0, A, C.byref(c), None, None)
+    assert write(latent_cache(G, kv=8)) == OK and write(latent_cache(G, kv=(1 << 64) - 1)) == OK
+    assert G.lib.ptstore_kv_write(A, 4096, 128, A, 4096, 128, 0, 0, A, C.byref(cache(G, kv=8)), None, None) == E_INVAL
