@@ -578,8 +578,8 @@ int ptstore_latent_read(const ptstore_kv_cache_t* cache /*host struct*/, const i
  * Causal attention of a batch's new tokens over the latent cache, which holds their own rows too (ptstore_latent_write comes first), absorbed form:
  *   out[i, h] = sum_j softmax_j(scale * (q_latent[i, h] . c_j + q_rope[i, h] . r_j)) * c_j
  * over the tokens that ptstore_attend's rows see, with its rules for positions, tables, rows that see nothing or belong to no request, and timing.
- * What the cache holds behind a row's position has no influence.  An infinity or a NaN in the row of a token that is seen makes the output NaN, in that
- * element's column at least.  q, out and the cache have the same type; sums, maxima and outputs up to the last rounding are 32 bits wide, probabilities
+ * What the cache holds behind a row's position has no influence.  An infinity or a NaN in the latent vector of a token that is seen makes the output
+ * NaN, in that element's column at least; in its rotary part it counts by the score: of minus infinity the token has no part, any other makes the row NaN.  q, out and the cache have the same type; sums, maxima and outputs up to the last rounding are 32 bits wide, probabilities
  * are rounded to 16 bits before they meet c.
  */
 typedef struct ptstore_latent_attend {

@@ -431,3 +431,27 @@ def test_rows_that_leave_pieces_of_a_tile_out(G, L, heads, new, max_new, dtype):
         b["out"].fill_(5.0)
         call(G, b, max_new=max_new)
         assert torch.equal(b["out"], want) and torch.equal(b["lse"], lse)
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("heads,new", [(16, 1), (16, 3), (100, 1)])
+def test_an_infinity_in_the_rotary_part_counts_by_its_score(G, dtype, heads, new):
+    """Scores of minus infinity leave the token out; heads whose score is infinite, or not a number, have no output."""
+    b = make(G, 512, dtype, heads, 16, [300, 70], [new] * 2, seed=60)
+    b["qr"][:, :, 9] = -1.0
+    b["qr"][:, 1, 9] = 2.0
+    b["qr"][:, 2, 9] = 0.0
+    b["q"][:, :, 512:] = b["qr"]
+    plane = b["cache"].tensors[0][b["layer"]].view(dtype).view(-1, 16, 576)
+    for r, p in ((0, 150), (1, 3)):
+        plane[int(b["tables"][r, p // 16]), p % 16, 512 + 9] = math.inf
+    call(G, b)
+    got, lse = b["out"].clone(), b["lse"].clone()
+    rows_of = slice(0, b["offsets"][-1])
+    assert bool(got[rows_of, 1:3].isnan().all()) and bool(got[rows_of, 3:].isfinite().all()) and bool(got[rows_of, 0].isfinite().all())
+    # the other heads as if the tokens' scores were far below the rest (powers of two of less than -150 vanish in 32 bits)
+    for r, p in ((0, 150), (1, 3)):
+        plane[int(b["tables"][r, p // 16]), p % 16, 512 + 9] = 60000.0
+    call(G, b)
+    keep = [h for h in range(heads) if h not in (1, 2)]
+    assert torch.equal(got[rows_of][:, keep], b["out"][rows_of][:, keep]) and torch.equal(lse[rows_of][:, keep], b["lse"][rows_of][:, keep])
