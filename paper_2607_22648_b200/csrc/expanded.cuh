@@ -9,9 +9,10 @@
 // part that all heads share, and V in two halves of 64 keys), so that a step is on its way while another is computed with.  All by tensor copies; what they bring along from behind
 // the request's keys is taken out of V where it matters (a weight of zero does not hide a NaN), for which the loading warps look at the last steps' V.
 //
-// B200: 8 whole prompts (2064 .. 6256 tokens, 16 heads, bf16) 823 us, 892 TFLOP/s; 4 suffixes of 1000 .. 2048 tokens over 6000 .. 8192 keys, 32 heads, fp16, 665 us, 1.02 PFLOP/s.  A step
+// B200, ten passes behind a pause / passes for seconds at the power limit: 8 whole prompts (2064 .. 6256 tokens, 16 heads, bf16) 834 / 910 us, 880 / 807 TFLOP/s; 4 suffixes of 1000 .. 2048
+// tokens over 6000 .. 8192 keys, 32 heads, fp16, 678 / 794 us, 997 / 851 TFLOP/s.  A step
 // of both tiles takes 4000 clocks, of which the tensor cores need 2560 and shared memory 2700 (the scores' operands are read at its full rate); the rest is the chain S, 64 + 64 weights, values,
-// next scores, and waits for a ring of 1.6 steps.  One arrival a warp at the barriers and one loading thread in place of 128 each: 880 to 823 us, 790 to 665.  Measured and dropped: the
+// next scores, and waits for a ring of 1.6 steps.  One arrival a warp at the barriers and one loading thread in place of 128 each: 880 to 823 us, 790 to 665 (behind pauses).  Measured and dropped: the
 // three boxes of a step's K awaited together (897 us).
 //
 // Warps: 0-3 and 4-7 softmax of tile 0 and 1, 8-11 load, 12 issues the tensor instructions, 13-15 only complete the warpgroup that gives its registers to the softmax warps.

@@ -17,8 +17,8 @@
 // even share of the line of all (request, row tile, 64 tokens) units.  An item that spans several CTAs leaves sums (o, m, l in 32 bits) in the workspace,
 // which latent_join_kernel joins in CTA order.
 //
-// B200, L = 512, bf16: decode of 64 x 128 heads over 4160 tokens on average 168 us (439 TFLOP/s); 16 x 64 new tokens of 16 heads over 4160, fp16, 245 us (602); one request of 16
-// heads 25 us.  A step of 128 rows has 1856 clocks of tensor instructions and moves 270 KB through shared memory (2100 clocks): 2500 clocks where its tile is there in time, 3000 to 4500
+// B200, L = 512, bf16, ten passes behind a pause / passes for seconds at the power limit: decode of 64 x 128 heads over 4160 tokens on average 169 / 174 us (437 / 425 TFLOP/s); 16 x 64 new
+// tokens of 16 heads over 4160, fp16, 249 / 268 us (592 / 550); one request of 16 heads 25 us.  A step of 128 rows has 1856 clocks of tensor instructions and moves 270 KB through shared memory (2100 clocks): 2500 clocks where its tile is there in time, 3000 to 4500
 // with the waits for it: Q, P and O leave room for 1.6 tiles of the boxes that are no values, and a tensor copy takes 60 clocks + 1.75 a row of 128 bytes whatever its size, so that
 // blocks of 16 tokens (36 copies a step) take 168 us where blocks of 64 take 150.  Measured and dropped: halves of the scores exchanged through distributed shared memory, each CTA
 // with half of the products (324 us: remote stores go at 11 bytes a clock); rings with more room for either kind of box (180 / 282 us for the two batches).

@@ -11,7 +11,7 @@
 // the length of the sums.  So scores are summed up in several accumulators, and the scale makes up for what is cut off on average (cut_off below).  Scale and lse, times log2 e, are kept
 // as two numbers each (a rounding of an exponent of 20 is 2^-20 of the weight).
 //
-// B200: a decode step of 64 requests (2064 .. 6256 tokens, 32 / 8 heads x 128, bf16) 107 us, 5.4 TB/s; 32 last tokens of 16 prompts over 4160 tokens, 4-bit, 70 us: 9 exponentials a
+// B200: a decode step of 64 requests (2064 .. 6256 tokens, 32 / 8 heads x 128, bf16) 109 us, 5.3 TB/s; 32 last tokens of 16 prompts over 4160 tokens, 4-bit, 70 us: 9 exponentials a
 // clock and SM of 16, since a tile's unpacking, products and sums follow one another and three CTAs an SM cover for that only in part; latent rows (8 x 16.4k, 64 heads) 59 us, 2.6 TB/s:
 // one CTA an SM, whose tile of 72 KB is loaded while one is computed with.  Measured and dropped: chunks of 32 rows, one's products computed while the one before is added up (83 and
 // 65 us).
@@ -354,7 +354,7 @@ __global__ void __launch_bounds__(AW_THREADS, D > 128 ? 1 : 3) weights_kernel(co
 // Measured against 64 bits with scores of 64 .. 576 elements, n = 1 / 2 / 4 / 6, in 2^-24: 0.7 .. 1.0 / 1.1 .. 1.7 / 1.6 .. 1.8 / 2.3 .. 2.6 (here 0.72 / 1.08 / 1.80 / 2.52).  A score
 // whose sum is exact is off by as much instead, at most 2.6 2^-24 of it (the header says so).  Products with 4-bit keys have fewer bits, of which less
 // is cut off: half of it (measured 0.3 .. 0.4 / 0.4 .. 0.7 / 0.5 .. 1.1).
-// Weights against 64 bits (norm, in 1e-6) with it / without / 32-bit products of a library: a decode step 0.6 / 0.9 / 0.8, latent rows 1.3 / 2.3 / 1.3.  The loss can also be measured, by
+// Weights against 64 bits (norm, in 1e-6) with it / without / 32-bit products of a library: a decode step 0.6 / 0.9 / 0.8, latent rows 1.4 / 2.3 / 1.3.  The loss can also be measured, by
 // sums that go forth and back again (what is left of them over): 0.6 and 1.4, but three times the products, 132 and 84 us in place of 116 and 61.
 constexpr double cut_off(bool packed, int n) { return 0x1p-24 / 1.3862943611198906 * (n + 1) / (packed ? 4 : 2); }
 
