@@ -455,3 +455,16 @@ def test_an_infinity_in_the_rotary_part_counts_by_its_score(G, dtype, heads, new
     call(G, b)
     keep = [h for h in range(heads) if h not in (1, 2)]
     assert torch.equal(got[rows_of][:, keep], b["out"][rows_of][:, keep]) and torch.equal(lse[rows_of][:, keep], b["lse"][rows_of][:, keep])
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("heads,new,max_new", [(80, 1, 1), (96, 1, 1), (20, 1, 2), (16, 9, 9)])
+def test_q_may_be_the_output_of_rows_that_leave_pieces_out(G, heads, new, max_new, dtype):
+    lens = [64 + 37 * i % 200 for i in range(300)]
+    b = make(G, 512, dtype, heads, 16, lens, [new] * 300, seed=heads + new)
+    call(G, b, max_new=max_new)
+    want, first, T = b["out"].clone(), b["ql"].clone(), b["offsets"][-1]
+    for _ in range(5):
+        b["ql"] = first.clone()
+        call(G, b, max_new=max_new, out=b["ql"])
+        assert torch.equal(b["ql"][:T], want[:T]) and torch.equal(b["ql"][T:], first[T:])
