@@ -579,7 +579,7 @@ def attend_weights(layout, cache, layer, q, lse, token_offsets, lengths, block_t
 def select_tokens(weights, lengths, budget, first, recent, kept=None, lengths_out=None, weights_out=None, status=None):
     """ptstore_select_tokens: of every request longer than `budget` the tokens each kv head keeps, its first `first`, last `recent` and the ones with the largest weights in between.
     weights [requests, kv heads, width] float32; the kept tokens' weights go to weights_out (weights itself by default).  Returns (kept int32 [requests, kv heads, budget],
-    ascending, -1 behind the last; lengths_out int32 [requests]; weights_out)."""
+    ascending, -1 behind the last; lengths_out int32 [requests]; weights_out).  A budget beyond width keeps all."""
     dev, i32, R = _device(), torch.int32, lengths.numel()
     if weights.dim() != 3:
         raise ValueError("weights: needs a float32 tensor [requests, heads, width]")
@@ -592,11 +592,20 @@ def select_tokens(weights, lengths, budget, first, recent, kept=None, lengths_ou
         weights_out = weights
     elif weights_out.shape != weights.shape:
         raise ValueError("weights_out: needs the shape of weights")
-    w, o = weights.stride(), weights_out.stride()
+    w, o, at = weights.stride(), weights_out.stride(), _vec(kept, i32, R * heads * max(budget, 0), dev, "kept")
+    chosen, wide = None, budget
+    if budget > width > 0 and first >= 0 and recent >= 0 and first + recent <= budget:
+        # the library takes a budget of at most width: nothing has to go, and what is written of a row of `kept` is as wide as a row of weights
+        chosen = torch.empty((R, heads, width), dtype=i32, device="cuda")
+        at, budget, first, recent = chosen.data_ptr(), width, 0, 0
     _check(lib.ptstore_select_tokens(_weights(weights, R, heads, dev, "weights"), w[0], w[1], _vec(lengths, i32, R, dev, "lengths"), R, heads, width, budget, first, recent,
-                                     _vec(kept, i32, R * heads * max(budget, 0), dev, "kept"), _vec(lengths_out, i32, R, dev, "lengths_out"),
+                                     at, _vec(lengths_out, i32, R, dev, "lengths_out"),
                                      _weights(weights_out, R, heads, dev, "weights_out"), o[0], o[1], None if status is None else _vec(status, i32, 1, dev, "status"),
                                      _raw_stream(dev)), "ptstore_select_tokens")
+    if chosen is not None:
+        rows = kept.view(R, heads, wide)
+        rows[:, :, :width] = chosen
+        rows[:, :, width:] = -1
     return kept, lengths_out, weights_out
 
 

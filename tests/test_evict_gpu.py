@@ -284,6 +284,19 @@ def test_choice_of_long_requests(G, n):
     check_choice(G, w, [n], n // 2, 0, 0)
 
 
+@pytest.mark.parametrize("budget,first,recent", [(101, 0, 0), (150, 4, 140), (5000, 10, 100)])
+def test_choice_with_a_budget_beyond_the_rows(G, budget, first, recent):
+    w = torch.rand(4, 3, 100, generator=gen_of(8), device="cuda")
+    check_choice(G, w, [100, 0, 37, 99], budget, first, recent)
+    check_choice(G, w, [100, -1, 37, 101], budget, first, recent)
+    kept = torch.full((4, 3, budget), 7, dtype=torch.int32, device="cuda")
+    got = G.select_tokens(w, dev([100, 0, 37, 99]), budget, first, recent, kept=kept, weights_out=torch.empty_like(w))[0]
+    assert got is kept and kept.tolist() == choose(w.tolist(), [100, 0, 37, 99], budget, first, recent)[0]
+    for bad in ((budget, -1, 0), (budget, 0, -1), (budget, budget, 1)):
+        with pytest.raises(G.PTStoreError):
+            G.select_tokens(w, dev([1, 2, 3, 4]), *bad)
+
+
 def test_choice_with_strides(G):
     gen = gen_of(3)
     big = torch.rand(5, 4, 3, 640, generator=gen, device="cuda")
