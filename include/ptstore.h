@@ -616,7 +616,8 @@ int ptstore_latent_attend(const ptstore_latent_attend_t* args /*host struct*/, c
 typedef struct ptstore_expanded_attend {
   uint32_t struct_size;          /* sizeof(ptstore_expanded_attend_t) */
   uint32_t dtype;                /* PTSTORE_KV_BF16 or PTSTORE_KV_FP16, of q, k, k_rope, v and out */
-  const void* q;                 /* device, [tokens][heads][192], strides in elements (multiples of 8), 16-byte aligned */
+  const void* q;                 /* device, [tokens][heads][192], strides in elements (multiples of 8), 16-byte aligned.  Of q, k, k_rope and v: token strides
+                                    positive, head strides not negative (0: all heads share a row) */
   int64_t  q_token_stride, q_head_stride;
   const void* k;                 /* [keys][heads][128] */
   int64_t  k_token_stride, k_head_stride;
